@@ -479,6 +479,46 @@ int vkv_step_run_static(vkv_ctx* ctx, const vkv_step* st, int64_t k, float* key,
 int vkv_check_rows(vkv_ctx* ctx, const vkv_step* st, int64_t k, const int32_t* sel,
                    const int32_t* adm, const int32_t* adm_count, int64_t cap, void* stream);
 
+/* ------------------------------------------------------------ the prompt */
+
+/*
+ * Causal attention over whole prompts (what fills the cache before decoding):
+ * n_seq sequences packed back to back, sequence b the tokens [cu[b], cu[b+1])
+ * of the n_tok packed ones.  For token i of a sequence and query head h, with
+ * g = h / (H / Hk) its key head:
+ *   s_j = scale * ( q[i,h,0:dn] . k[j,g]  +  q[i,h,dn:dn+dr] . k_rope[j] ),  j <= i
+ *   out[i,h,:] = RNE_bf16( sum_j softmax_j(s) v[j,g] ),   lse[i,h] = log sum_j exp(s_j)
+ *   q       [n_tok, H, dn + dr]   token i, head h at q + i*q_tok_stride + h*q_head_stride
+ *   k       [n_tok, Hk, dn], v [n_tok, Hk, dv]   addressed likewise
+ *   k_rope  [n_tok, dr]   the branch all heads share (Sec. 3, Eq. (setup)); NULL iff dr = 0
+ *   cu      [n_seq + 1] int32 (device), ascending, cu[0] = 0
+ *   out     [n_tok, H, dv] bf16 contiguous, lse [n_tok, H] fp32 (natural log)
+ * Supported (dn, dr, dv): (128, 64, 128), the expanded heads of the latent
+ * cache; (128, 0, 128) and (64, 0, 64), plain or grouped heads.
+ * 1 <= H <= 128, Hk divides H, strides multiples of 8 elements (0 allowed: a
+ * broadcast input), pointers 16-byte aligned.  max_len bounds the lengths;
+ * tokens of a sequence past its first max_len are not attended from (their
+ * outputs keep their contents), nor are tokens from cu[n_seq] on.  Offsets
+ * outside [0, n_tok] are taken as the nearest bound.  bf16 MFMA, fp32
+ * accumulation and softmax; the weights are rounded to bf16 for the product
+ * with v.  Allocates nothing, needs no workspace; fit for graph capture.
+ */
+typedef struct vkv_prompt {
+    int64_t n_seq, n_tok, max_len;
+    int64_t H, Hk;
+    int32_t dn, dr, dv, reserved0;
+    const uint16_t* q;
+    int64_t q_tok_stride, q_head_stride;
+    const uint16_t* k;
+    int64_t k_tok_stride, k_head_stride;
+    const uint16_t* k_rope;
+    int64_t k_rope_tok_stride;
+    const uint16_t* v;
+    int64_t v_tok_stride, v_head_stride;
+    const int32_t* cu;
+} vkv_prompt;
+int vkv_prompt_attend(vkv_ctx* ctx, const vkv_prompt* pr, float scale, uint16_t* out, float* lse, void* stream);
+
 /* enable != 0: vkv_step_run records a pair of HIP events around its score
  * scan, on the call's stream, for up to 512 calls; vkv_score_timing reads
  * them.  Either call clears what was recorded. */

@@ -22,7 +22,7 @@ __all__ = [
     "step_run", "step_run_static", "check_rows", "row_max", "trigger", "required_inflation", "conformal_z",
     "step_run_trigger", "sketch_workspace_size", "sketch_basis", "sigma_workspace_size", "sigma_close",
     "sigma_tier_size", "sigma_select", "step_run_kept", "pack_rows", "page_box", "page_bound", "SIGMA_BLOCK",
-    "exported_symbols",
+    "Prompt", "prompt_attend", "exported_symbols",
 ]
 
 VKV_MODE_ROPE, VKV_MODE_DIGEST, VKV_MODE_ROPE_DIGEST = 1, 2, 3
@@ -38,6 +38,7 @@ exported_symbols = (
     "vkv_row_max", "vkv_trigger", "vkv_required_inflation", "vkv_conformal_z", "vkv_step_run_trigger",
     "vkv_sketch_workspace_size", "vkv_sketch_basis", "vkv_sigma_workspace_size", "vkv_sigma_close",
     "vkv_sigma_select", "vkv_step_run_kept", "vkv_pack_rows", "vkv_page_box", "vkv_page_bound",
+    "vkv_prompt_attend",
 )
 SIGMA_BLOCK = 4096
 
@@ -60,6 +61,19 @@ class _Step(ctypes.Structure):
         ("reserved0", ctypes.c_int32),
         ("P", ctypes.c_void_p), ("eta", ctypes.c_void_p), ("eps", ctypes.c_void_p),
         ("gam", ctypes.c_void_p),
+    ]
+
+
+class _Prompt(ctypes.Structure):
+    _fields_ = [
+        ("n_seq", ctypes.c_int64), ("n_tok", ctypes.c_int64), ("max_len", ctypes.c_int64),
+        ("H", ctypes.c_int64), ("Hk", ctypes.c_int64),
+        ("dn", ctypes.c_int32), ("dr", ctypes.c_int32), ("dv", ctypes.c_int32), ("reserved0", ctypes.c_int32),
+        ("q", ctypes.c_void_p), ("q_tok_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64),
+        ("k", ctypes.c_void_p), ("k_tok_stride", ctypes.c_int64), ("k_head_stride", ctypes.c_int64),
+        ("k_rope", ctypes.c_void_p), ("k_rope_tok_stride", ctypes.c_int64),
+        ("v", ctypes.c_void_p), ("v_tok_stride", ctypes.c_int64), ("v_head_stride", ctypes.c_int64),
+        ("cu", ctypes.c_void_p),
     ]
 
 
@@ -115,6 +129,7 @@ def load():
     lib.vkv_pack_rows.argtypes = [P, P, P, i64, i64, P, P, P]
     lib.vkv_page_box.argtypes = [P, sp, i64, P, P]
     lib.vkv_page_bound.argtypes = [P, sp, P, ctypes.c_size_t, i64, P, P, P]
+    lib.vkv_prompt_attend.argtypes = [P, ctypes.POINTER(_Prompt), f32, P, P, P]
     lib.vkv_set_timing.argtypes = [P, ctypes.c_int]
     lib.vkv_score_timing.argtypes = [P, ctypes.POINTER(ctypes.c_float), ctypes.c_int]
     for name in exported_symbols:
@@ -142,6 +157,30 @@ def _stream(stream) -> ctypes.c_void_p:
     if stream is None:
         stream = torch.cuda.current_stream()
     return ctypes.c_void_p(stream.cuda_stream)
+
+
+def _typed(t: Optional[torch.Tensor], dtype, name: str, shape=None, contiguous: bool = True):
+    """The pointer of an argument after its type, its shape (None: any size) and its layout are checked
+    (not contiguous: any strides, neighbouring elements in the last dimension)."""
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if shape is not None and (t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape))):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if contiguous and not t.is_contiguous() or t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name} must be contiguous" + ("" if contiguous else " in its last dimension"))
+    return ctypes.c_void_p(t.data_ptr())
+
+
+def _stride(t: torch.Tensor, dim: int) -> int:
+    """The stride of a dimension; of one that has a single place, which is never stepped over, 0."""
+    return t.stride(dim) if t.shape[dim] > 1 else 0
+
+
+def _call_stream(ctx: "Context", stream) -> ctypes.c_void_p:
+    """The stream of a call: the given one, else the current one of the context's device."""
+    return _stream(torch.cuda.current_stream(ctx.device) if stream is None else stream)
 
 
 class Context:
@@ -423,6 +462,43 @@ def page_bound(ctx: Context, step: Step, ws: torch.Tensor, page: int, box: torch
     """vkv_page_bound: bound [B, ceil(A / page)] float64 <- the pages' interval bounds (after query_prep)."""
     ctx.check(ctx.lib.vkv_page_bound(ctx.handle, step.ref, _ptr(ws), ws.numel(), int(page), _ptr(box), _ptr(bound),
                                      _stream(stream)))
+
+
+class Prompt:
+    """Packed prompts (``vkv_prompt``): q [n,H,dn+dr], k [n,Hk,dn], v [n,Hk,dv] and, with a shared branch,
+    k_rope [n,dr] (bf16, any token and head strides), cu [n_seq+1] int32."""
+
+    def __init__(self, q, k, v, cu, max_len: int, k_rope=None):
+        bf = torch.bfloat16
+        self.tensors = (q, k, v, cu, k_rope)  # keep alive
+        s = _Prompt()
+        s.q = _typed(q, bf, "q", (None, None, None), False)
+        n, s.H = q.shape[0], q.shape[1]
+        s.k, s.v = _typed(k, bf, "k", (n, None, None), False), _typed(v, bf, "v", (n, k.shape[1], None), False)
+        s.k_rope = _typed(k_rope, bf, "k_rope", (n, None), False)
+        s.n_tok, s.n_seq, s.max_len = n, cu.numel() - 1, int(max_len)
+        s.Hk, s.dn, s.dv, s.dr = k.shape[1], k.shape[2], v.shape[2], 0 if k_rope is None else k_rope.shape[1]
+        if q.shape[2] != s.dn + s.dr:
+            raise ValueError(f"q has {q.shape[2]} dims, k and k_rope {s.dn} + {s.dr}")
+        s.q_tok_stride, s.q_head_stride = _stride(q, 0), _stride(q, 1)
+        s.k_tok_stride, s.k_head_stride = _stride(k, 0), _stride(k, 1)
+        s.v_tok_stride, s.v_head_stride = _stride(v, 0), _stride(v, 1)
+        s.k_rope_tok_stride = 0 if k_rope is None else _stride(k_rope, 0)
+        s.cu = _typed(cu, torch.int32, "cu", (None,))
+        self.c = s
+        self.n_tok, self.H, self.dv = n, s.H, s.dv
+
+    @property
+    def ref(self):
+        return ctypes.byref(self.c)
+
+
+def prompt_attend(ctx: Context, prompt: Prompt, scale: float, out: torch.Tensor, lse: torch.Tensor, stream=None):
+    """vkv_prompt_attend: out [n,H,dv] bf16, lse [n,H] fp32."""
+    ctx.check(ctx.lib.vkv_prompt_attend(
+        ctx.handle, prompt.ref, float(scale),
+        _typed(out, torch.bfloat16, "out", (prompt.n_tok, prompt.H, prompt.dv)),
+        _typed(lse, torch.float32, "lse", (prompt.n_tok, prompt.H)), _call_stream(ctx, stream)))
 
 
 def check_rows(ctx: Context, step: Step, k: int, sel: Optional[torch.Tensor],

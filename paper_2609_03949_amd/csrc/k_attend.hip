@@ -25,9 +25,7 @@
 // reference max, running sum) and a second kernel merges the splits by their
 // log-sum-exp (the appendix's kernel mapping: fetched rows are one more
 // split-KV partition).
-#include <type_traits>
-
-#include "vkv_internal.h"
+#include "vkv_tile.h"
 
 namespace vkv {
 
@@ -40,10 +38,6 @@ constexpr int ATT_GROUP = 2;                 // tiles per workgroup barrier
 constexpr float ATT_SLACK = 8.0f;            // lag allowed to the softmax reference maximum (log2 units)
 constexpr int ATT_STAGES = 2 * ATT_GROUP;    // ring depth: the group in use and the next in flight
 constexpr int ROW_BYTES = D_ROW * 2;                         // 1152
-
-typedef __attribute__((address_space(3))) void lds_void_t;
-typedef __attribute__((address_space(1))) void gbl_void_t;
-typedef short i16x4_t __attribute__((ext_vector_type(4)));
 
 // rows attended by sequence b: kept, window, admitted (up to the capacity)
 __device__ __forceinline__ int64_t attended_count(const AttendArgs& a, int b) {
@@ -90,17 +84,6 @@ __device__ __forceinline__ int32_t attended_row(const AttendArgs& a, int b, int6
 // which paired rows 2i and 2i + 1, doubled the K reads' LDS cycles).
 __device__ __forceinline__ int piece_xor(int r) { return r & 7; }
 
-__device__ __forceinline__ void wg_barrier() { asm volatile("s_barrier" ::: "memory"); }
-
-// Compile-time loop: f(std::integral_constant<int, I>) for I = 0 .. N-1.
-template <int I, int N, typename F>
-__device__ __forceinline__ void static_for(F&& f) {
-    if constexpr (I < N) {
-        f(std::integral_constant<int, I>{});
-        static_for<I + 1, N>(f);
-    }
-}
-
 // op-reduction of x over the four 16-lane groups (lanes c, c+16, c+32, c+48),
 // result in all of them: two cross-lane swaps, no LDS traffic
 template <typename Op>
@@ -111,36 +94,6 @@ __device__ __forceinline__ float allreduce_groups(float x, Op op) {
     const uint32_t v = __float_as_uint(y);
     const auto r16 = __builtin_amdgcn_permlane16_swap(v, v, false, false);   // lane l ^ 16
     return op(__uint_as_float(r16[0]), __uint_as_float(r16[1]));
-}
-
-// Operand reads of the tile stages, issued as explicit LDS instructions: the
-// compiler sees no LDS read of a stage, so it never makes them wait for the
-// direct loads still in flight into the other stages, and the lgkmcnt waits
-// before each use are explicit (lds_wait: at most N of this wave's LDS
-// operations outstanding; LDS operations complete in order).  The kernel
-// issues no scalar memory loads inside the tile loop, so lgkmcnt counts LDS
-// operations only there.
-__device__ __forceinline__ uint32_t lds_addr(const void* p) {
-    return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
-}
-template <int OFF>
-__device__ __forceinline__ bf16x8_t lds_read128(uint32_t addr) {
-    bf16x8_t v;
-    asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFF));
-    return v;
-}
-// transposing read: within each 16-lane group, lane j supplies the address of
-// 4 consecutive 16-bit elements D[j][0..3], and lane i receives D[4e + i/4][i % 4]
-// for e = 0..3
-template <int OFF>
-__device__ __forceinline__ i16x4_t lds_read_tr16(uint32_t addr) {
-    i16x4_t v;
-    asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFF));
-    return v;
-}
-template <int N, typename T0, typename T1>
-__device__ __forceinline__ void lds_wait(T0& x, T1& y) {
-    asm volatile("s_waitcnt lgkmcnt(%2)" : "+v"(x), "+v"(y) : "n"(N));
 }
 
 __global__ __launch_bounds__(ATT_THREADS, 1) void attend_kernel(AttendArgs a) {

@@ -51,6 +51,23 @@ static int fail(vkv_ctx* ctx, int code, const char* fmt, ...) {
 static inline bool al16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 static inline size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
 
+// Makes the context's device the current one for a call and puts the caller's back.
+struct DeviceGuard {
+    int before = -1;
+    hipError_t err;
+    explicit DeviceGuard(const vkv_ctx* ctx) {
+        int now = 0;
+        err = hipGetDevice(&now);
+        if (err == hipSuccess && now != ctx->device) {
+            err = hipSetDevice(ctx->device);
+            if (err == hipSuccess) before = now;
+        }
+    }
+    ~DeviceGuard() {
+        if (before >= 0) (void)hipSetDevice(before);
+    }
+};
+
 // ------------------------------------------------------------ validation
 
 static int index_width(const vkv_step* st) {
@@ -655,6 +672,62 @@ int vkv_attend(vkv_ctx* ctx, const vkv_step* st, void* ws, size_t ws_bytes, int6
     if (rc) return rc;
     HIP_TRY(ctx, run_attend(st, (char*)ws, Chunk{0, st->B}, k, sel, adm, adm_count, cap, scale, out, lse,
                             (hipStream_t)stream));
+    return VKV_OK;
+}
+
+static bool bad_scale(float scale) { return !(scale > 0.f) || !(scale < 1e30f); }
+
+int vkv_prompt_attend(vkv_ctx* ctx, const vkv_prompt* pr, float scale, uint16_t* out, float* lse, void* stream) {
+    if (!ctx) return fail(nullptr, VKV_E_ARG, "ctx is NULL");
+    if (!pr) return fail(ctx, VKV_E_ARG, "prompt is NULL");
+    if (pr->n_seq < 1 || pr->n_seq > 65535) return fail(ctx, VKV_E_SHAPE, "n_seq=%lld outside [1, 65535]", (long long)pr->n_seq);
+    if (pr->H < 1 || pr->H > 128) return fail(ctx, VKV_E_SHAPE, "H=%lld outside [1, 128]", (long long)pr->H);
+    if (pr->Hk < 1 || pr->H % pr->Hk)
+        return fail(ctx, VKV_E_SHAPE, "Hk=%lld does not divide H=%lld", (long long)pr->Hk, (long long)pr->H);
+    if (pr->n_tok < 0 || pr->n_tok >= (1ll << 31) || pr->max_len < 0 || pr->max_len >= (1ll << 31))
+        return fail(ctx, VKV_E_SHAPE, "n_tok=%lld or max_len=%lld outside [0, 2^31)", (long long)pr->n_tok, (long long)pr->max_len);
+    if (!((pr->dn == 128 && pr->dr == 64 && pr->dv == 128) || (pr->dn == 128 && pr->dr == 0 && pr->dv == 128) ||
+          (pr->dn == 64 && pr->dr == 0 && pr->dv == 64)))
+        return fail(ctx, VKV_E_UNSUPPORTED, "head dims (%d, %d, %d): need (128, 64, 128), (128, 0, 128) or (64, 0, 64)",
+                    pr->dn, pr->dr, pr->dv);
+    if (bad_scale(scale)) return fail(ctx, VKV_E_ARG, "scale must be positive and finite");
+    const int64_t len = std::min(pr->max_len, pr->n_tok);
+    if (len == 0) return VKV_OK;
+    if (!pr->q || !pr->k || !pr->v || !pr->cu || !out || !lse || (pr->dr > 0) != (pr->k_rope != nullptr))
+        return fail(ctx, VKV_E_ARG, "q, k, v, cu, out and lse are required, and k_rope iff dr > 0");
+    if (!al16(pr->q) || !al16(pr->k) || !al16(pr->v) || !al16(pr->k_rope) || !al16(out))
+        return fail(ctx, VKV_E_ALIGN, "q, k, k_rope, v and out must be 16-byte aligned");
+    for (int64_t st : {pr->q_tok_stride, pr->q_head_stride, pr->k_tok_stride, pr->k_head_stride, pr->v_tok_stride,
+                       pr->v_head_stride, pr->dr > 0 ? pr->k_rope_tok_stride : (int64_t)0})
+        if (st < 0 || st % 8) return fail(ctx, VKV_E_ALIGN, "stride %lld: need a multiple of 8, at least 0", (long long)st);
+    const int64_t nqb = prompt_blocks(len);
+    if (pr->n_seq * pr->H * nqb >= (1ll << 31))
+        return fail(ctx, VKV_E_SHAPE, "n_seq * H * max_len needs %lld workgroups, at most 2^31 - 1", (long long)(pr->n_seq * pr->H * nqb));
+    PromptArgs a{};
+    a.q = pr->q;
+    a.k = pr->k;
+    a.kr = pr->k_rope;
+    a.v = pr->v;
+    a.qts = pr->q_tok_stride;
+    a.qhs = pr->q_head_stride;
+    a.kts = pr->k_tok_stride;
+    a.khs = pr->k_head_stride;
+    a.rts = pr->dr > 0 ? pr->k_rope_tok_stride : 0;
+    a.vts = pr->v_tok_stride;
+    a.vhs = pr->v_head_stride;
+    a.cu = pr->cu;
+    a.n_tok = pr->n_tok;
+    a.n_seq = (int)pr->n_seq;
+    a.H = (int)pr->H;
+    a.Hk = (int)pr->Hk;
+    a.max_len = (int)len;
+    a.nqb = (int)nqb;
+    a.scale_log2 = scale * 1.4426950408889634f;
+    a.out = out;
+    a.lse = lse;
+    DeviceGuard dev(ctx);
+    HIP_TRY(ctx, dev.err);
+    HIP_TRY(ctx, launch_prompt(a, pr->dn, pr->dr, (hipStream_t)stream));
     return VKV_OK;
 }
 

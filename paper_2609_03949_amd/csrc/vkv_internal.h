@@ -293,7 +293,25 @@ struct AttendArgs {
     float* lse;            // [B,H]
 };
 
+struct PromptArgs {
+    const uint16_t* q;     // [n_tok, H, dn + dr]
+    const uint16_t* k;     // [n_tok, Hk, dn]
+    const uint16_t* kr;    // [n_tok, dr] or null
+    const uint16_t* v;     // [n_tok, Hk, dv]
+    int64_t qts, kts, rts, vts;   // token strides, elements
+    int64_t qhs, khs, vhs;        // head strides
+    const int32_t* cu;     // [n_seq + 1]
+    int64_t n_tok;
+    int n_seq, H, Hk, max_len;
+    int nqb;               // blocks of query rows of the longest sequence
+    float scale_log2;      // scale * log2(e)
+    uint16_t* out;         // [n_tok, H, dv]
+    float* lse;            // [n_tok, H]
+};
+
 hipError_t launch_qprep(const QprepArgs& a, hipStream_t s);
+int64_t prompt_blocks(int64_t len);
+hipError_t launch_prompt(const PromptArgs& a, int dn, int dr, hipStream_t s);
 hipError_t launch_score(const ScoreArgs& a, hipStream_t s);
 hipError_t launch_digest(const DigestArgs& a, hipStream_t s);
 // Gershgorin row sums of P P^T: quick sums in gram[0, r) and, unless all of them
