@@ -519,6 +519,75 @@ typedef struct vkv_prompt {
 } vkv_prompt;
 int vkv_prompt_attend(vkv_ctx* ctx, const vkv_prompt* pr, float scale, uint16_t* out, float* lse, void* stream);
 
+/* ------------------------------------------------------- the paged cache */
+
+/*
+ * A paged latent cache: rows of 576 bf16 as in vkv_step, in pages of `page`
+ * consecutive rows that lie anywhere in one buffer.  Row u of sequence b is row
+ * u % page of page table[b*table_stride + u/page]; row r of page p is at
+ * cache + p*page_stride + r*row_stride (elements).  A cache [B, T, 576] is one
+ * whose page j of sequence b is page b*T/page + j.
+ *   table   [B, table_stride] int32 (device), table_stride >= ceil(max_kv / page)
+ *   kv_len  [B] int32 (device): rows of each sequence; values outside
+ *           [0, max_kv] are taken as the nearest bound
+ * page: a power of two in [1, 65536].  1 <= B <= 65535, 0 <= max_kv <= 2^30,
+ * 1 <= n_pages < 2^31; strides multiples of 8, row_stride >= 576, cache
+ * 16-byte aligned.  Rows on a page outside [0, n_pages) do not exist: they are
+ * not read, have no weight and are not written.
+ */
+typedef struct vkv_pages {
+    int64_t B, max_kv, n_pages;
+    int32_t page, reserved0;
+    uint16_t* cache;
+    int64_t row_stride, page_stride;
+    const int32_t* table;
+    int64_t table_stride;
+    const int32_t* kv_len;
+} vkv_pages;
+
+/*
+ * The queries of the newest tokens of every sequence, packed: sequence b has
+ * the tokens [cu[b], cu[b+1]) of n_tok, at most max_q of them (none is allowed,
+ * one is a decode step).  They are the sequence's last ones, so token i of
+ * nq = cu[b+1] - cu[b] sees the rows u <= kv_len[b] - nq + i (their own rows are
+ * in the cache already).
+ *   q_lat   (token, head) row t*H + h at q_lat + (t*H + h)*q_lat_stride: 512 bf16
+ *   q_rope  likewise, 64 bf16
+ *   cu      [B + 1] int32 (device), ascending, cu[0] = 0; offsets outside
+ *           [0, n_tok] are taken as the nearest bound, a sequence's tokens past
+ *           its first max_q are left out
+ * 1 <= H <= 128, 0 <= n_tok < 2^31, 0 <= max_q, max_q*H <= 2^30; strides multiples of
+ * 8, at least 0, pointers 16-byte aligned.
+ */
+typedef struct vkv_chunk {
+    int64_t n_tok, H, max_q;
+    const uint16_t* q_lat;
+    int64_t q_lat_stride;
+    const uint16_t* q_rope;
+    int64_t q_rope_stride;
+    const int32_t* cu;
+} vkv_chunk;
+
+/*
+ * Attention of a chunk over a paged cache: as vkv_attend, on every row the
+ * token sees, for any number of new tokens:
+ *   s_u = scale * ( q_lat . c_u + q_rope . r_u )
+ *   out[t,h,:] = RNE_bf16( sum_u softmax_u(s) c_u[0:512] )   [n_tok, H, 512]
+ *   lse[t,h]   = log sum_u exp(s_u)   (natural log)          [n_tok, H] fp32
+ * A token that sees no row gets out = 0 and lse = -inf.  Tokens from cu[B] on
+ * keep their outputs.  bf16 MFMA, fp32 accumulation, online softmax; the
+ * weights are rounded to bf16 for the product with c_u.  The work is cut into
+ * equal runs of cache tiles whose partial results (fp32, in ws) are joined in a
+ * fixed order: the same inputs and sizes give the same bits.
+ * ws: vkv_chunk_workspace_size bytes, 256-byte aligned; it depends on B, max_kv,
+ * H and max_q only, holds nothing between calls, and may not be shared by calls
+ * (or replayed graphs) that overlap.  Allocates nothing; fit for graph capture:
+ * replays read the then current kv_len, table and cu.
+ */
+int vkv_chunk_workspace_size(const vkv_pages* pg, const vkv_chunk* ch, size_t* bytes);
+int vkv_chunk_attend(vkv_ctx* ctx, const vkv_pages* pg, const vkv_chunk* ch, void* ws, size_t ws_bytes, float scale,
+                     uint16_t* out, float* lse, void* stream);
+
 /* enable != 0: vkv_step_run records a pair of HIP events around its score
  * scan, on the call's stream, for up to 512 calls; vkv_score_timing reads
  * them.  Either call clears what was recorded. */

@@ -22,7 +22,7 @@ __all__ = [
     "step_run", "step_run_static", "check_rows", "row_max", "trigger", "required_inflation", "conformal_z",
     "step_run_trigger", "sketch_workspace_size", "sketch_basis", "sigma_workspace_size", "sigma_close",
     "sigma_tier_size", "sigma_select", "step_run_kept", "pack_rows", "page_box", "page_bound", "SIGMA_BLOCK",
-    "Prompt", "prompt_attend", "exported_symbols",
+    "Prompt", "prompt_attend", "Pages", "Chunk", "chunk_workspace_size", "chunk_attend", "exported_symbols",
 ]
 
 VKV_MODE_ROPE, VKV_MODE_DIGEST, VKV_MODE_ROPE_DIGEST = 1, 2, 3
@@ -38,7 +38,7 @@ exported_symbols = (
     "vkv_row_max", "vkv_trigger", "vkv_required_inflation", "vkv_conformal_z", "vkv_step_run_trigger",
     "vkv_sketch_workspace_size", "vkv_sketch_basis", "vkv_sigma_workspace_size", "vkv_sigma_close",
     "vkv_sigma_select", "vkv_step_run_kept", "vkv_pack_rows", "vkv_page_box", "vkv_page_bound",
-    "vkv_prompt_attend",
+    "vkv_prompt_attend", "vkv_chunk_workspace_size", "vkv_chunk_attend",
 )
 SIGMA_BLOCK = 4096
 
@@ -74,6 +74,23 @@ class _Prompt(ctypes.Structure):
         ("k_rope", ctypes.c_void_p), ("k_rope_tok_stride", ctypes.c_int64),
         ("v", ctypes.c_void_p), ("v_tok_stride", ctypes.c_int64), ("v_head_stride", ctypes.c_int64),
         ("cu", ctypes.c_void_p),
+    ]
+
+
+class _Pages(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int64), ("max_kv", ctypes.c_int64), ("n_pages", ctypes.c_int64),
+        ("page", ctypes.c_int32), ("reserved0", ctypes.c_int32),
+        ("cache", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("page_stride", ctypes.c_int64),
+        ("table", ctypes.c_void_p), ("table_stride", ctypes.c_int64), ("kv_len", ctypes.c_void_p),
+    ]
+
+
+class _Chunk(ctypes.Structure):
+    _fields_ = [
+        ("n_tok", ctypes.c_int64), ("H", ctypes.c_int64), ("max_q", ctypes.c_int64),
+        ("q_lat", ctypes.c_void_p), ("q_lat_stride", ctypes.c_int64),
+        ("q_rope", ctypes.c_void_p), ("q_rope_stride", ctypes.c_int64), ("cu", ctypes.c_void_p),
     ]
 
 
@@ -130,6 +147,9 @@ def load():
     lib.vkv_page_box.argtypes = [P, sp, i64, P, P]
     lib.vkv_page_bound.argtypes = [P, sp, P, ctypes.c_size_t, i64, P, P, P]
     lib.vkv_prompt_attend.argtypes = [P, ctypes.POINTER(_Prompt), f32, P, P, P]
+    pg, ch, sz = ctypes.POINTER(_Pages), ctypes.POINTER(_Chunk), ctypes.c_size_t
+    lib.vkv_chunk_workspace_size.argtypes = [pg, ch, ctypes.POINTER(sz)]
+    lib.vkv_chunk_attend.argtypes = [P, pg, ch, P, sz, f32, P, P, P]
     lib.vkv_set_timing.argtypes = [P, ctypes.c_int]
     lib.vkv_score_timing.argtypes = [P, ctypes.POINTER(ctypes.c_float), ctypes.c_int]
     for name in exported_symbols:
@@ -499,6 +519,93 @@ def prompt_attend(ctx: Context, prompt: Prompt, scale: float, out: torch.Tensor,
         ctx.handle, prompt.ref, float(scale),
         _typed(out, torch.bfloat16, "out", (prompt.n_tok, prompt.H, prompt.dv)),
         _typed(lse, torch.float32, "lse", (prompt.n_tok, prompt.H)), _call_stream(ctx, stream)))
+
+
+class Pages:
+    """A paged latent cache (``vkv_pages``): cache [n_pages, page, 576] bf16 (any page and row strides),
+    table [B, ceil(max_kv / page) or more] int32, kv_len [B] int32."""
+
+    def __init__(self, cache, table, kv_len, max_kv: int):
+        self.tensors = (cache, table, kv_len)  # keep alive
+        s = _Pages()
+        s.cache = _typed(cache, torch.bfloat16, "cache", (None, None, D_ROW), False)
+        s.table = _typed(table, torch.int32, "table", (None, None), False)
+        s.kv_len = _typed(kv_len, torch.int32, "kv_len", (table.shape[0],))
+        s.n_pages, s.page = cache.shape[0], cache.shape[1]
+        s.page_stride = _stride(cache, 0)
+        s.row_stride = cache.stride(1) if cache.shape[1] > 1 else D_ROW
+        s.B, s.max_kv, s.table_stride = table.shape[0], int(max_kv), table.shape[1]
+        if table.shape[0] > 1:   # rows of the table may lie further apart than they are wide
+            if table.stride(0) < table.shape[1]:
+                raise ValueError("table rows overlap")
+            s.table_stride = table.stride(0)
+        if table.shape[1] * cache.shape[1] < int(max_kv):
+            raise ValueError(f"table of {table.shape[1]} pages of {cache.shape[1]} rows holds fewer than {max_kv} rows")
+        self.c = s
+        self.B, self.max_kv = s.B, s.max_kv
+
+    @classmethod
+    def of_cache(cls, cache, kv_len, page: int = 64):
+        """The pages of a contiguous cache [B, T, 576] as the decode step takes it; page divides T."""
+        B, T, _ = cache.shape
+        if T % page:
+            raise ValueError(f"page={page} does not divide T={T}")
+        table = torch.arange(B * T // page, dtype=torch.int32, device=cache.device).view(B, T // page)
+        return cls(cache.view(B * T // page, page, D_ROW), table, kv_len, T)
+
+    @property
+    def ref(self):
+        return ctypes.byref(self.c)
+
+
+class Chunk:
+    """The newest tokens' queries (``vkv_chunk``): q_lat [n,H,512], q_rope [n,H,64] (bf16; contiguous, or parts of
+    rows [n,H,...] that are), cu [B+1] int32, at most max_q tokens a sequence."""
+
+    def __init__(self, q_lat, q_rope, cu, max_q: int):
+        self.tensors = (q_lat, q_rope, cu)  # keep alive
+        n, H = q_lat.shape[0], q_lat.shape[1]
+        s = _Chunk()
+        for name, t, d in (("q_lat", q_lat, D_LAT), ("q_rope", q_rope, D_ROPE)):
+            setattr(s, name, _typed(t, torch.bfloat16, name, (n, H, d), False))
+            step = t.stride(1) if H > 1 else _stride(t, 0)
+            if H > 1 and n > 1 and t.stride(0) != H * step:
+                raise ValueError(f"{name}: the heads of one token must follow those of the one before")
+            setattr(s, name + "_stride", step)
+        s.cu = _typed(cu, torch.int32, "cu", (None,))
+        s.n_tok, s.H, s.max_q = n, H, int(max_q)
+        self.c = s
+        self.n_tok, self.H, self.B = n, H, cu.numel() - 1
+
+    @property
+    def ref(self):
+        return ctypes.byref(self.c)
+
+
+def _sequences(pages: Pages, chunk: Chunk):
+    if pages.B != chunk.B:
+        raise ValueError(f"{pages.B} sequences in the pages, {chunk.B} in the chunk")
+
+
+def chunk_workspace_size(pages: Pages, chunk: Chunk) -> int:
+    _sequences(pages, chunk)
+    lib = load()
+    n = ctypes.c_size_t(0)
+    rc = lib.vkv_chunk_workspace_size(pages.ref, chunk.ref, ctypes.byref(n))
+    if rc != 0:
+        raise VkvError(rc, lib.vkv_last_error(None).decode())
+    return int(n.value)
+
+
+def chunk_attend(ctx: Context, pages: Pages, chunk: Chunk, ws: torch.Tensor, scale: float, out: torch.Tensor,
+                 lse: torch.Tensor, stream=None):
+    """vkv_chunk_attend: out [n,H,512] bf16, lse [n,H] fp32."""
+    _sequences(pages, chunk)
+    n, H = chunk.n_tok, chunk.H
+    ctx.check(ctx.lib.vkv_chunk_attend(
+        ctx.handle, pages.ref, chunk.ref, _ptr(ws), ws.numel() * ws.element_size(), float(scale),
+        _typed(out, torch.bfloat16, "out", (n, H, D_LAT)), _typed(lse, torch.float32, "lse", (n, H)),
+        _call_stream(ctx, stream)))
 
 
 def check_rows(ctx: Context, step: Step, k: int, sel: Optional[torch.Tensor],

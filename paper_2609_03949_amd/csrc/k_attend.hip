@@ -84,18 +84,6 @@ __device__ __forceinline__ int32_t attended_row(const AttendArgs& a, int b, int6
 // which paired rows 2i and 2i + 1, doubled the K reads' LDS cycles).
 __device__ __forceinline__ int piece_xor(int r) { return r & 7; }
 
-// op-reduction of x over the four 16-lane groups (lanes c, c+16, c+32, c+48),
-// result in all of them: two cross-lane swaps, no LDS traffic
-template <typename Op>
-__device__ __forceinline__ float allreduce_groups(float x, Op op) {
-    const uint32_t u = __float_as_uint(x);
-    const auto r32 = __builtin_amdgcn_permlane32_swap(u, u, false, false);   // lane l ^ 32
-    const float y = op(__uint_as_float(r32[0]), __uint_as_float(r32[1]));
-    const uint32_t v = __float_as_uint(y);
-    const auto r16 = __builtin_amdgcn_permlane16_swap(v, v, false, false);   // lane l ^ 16
-    return op(__uint_as_float(r16[0]), __uint_as_float(r16[1]));
-}
-
 __global__ __launch_bounds__(ATT_THREADS, 1) void attend_kernel(AttendArgs a) {
     __shared__ __align__(16) uint8_t s_k[ATT_STAGES * TILE_BYTES];   // the ring of tile stages
     __shared__ int32_t s_rows[ATT_MAX_SPLIT_ROWS];                    // the split's rows

@@ -24,6 +24,7 @@ constexpr int PR_WAVES = 4;
 constexpr int PR_ROWS = 32 * PR_WAVES;   // query rows of a workgroup
 constexpr int PR_KEYS = 64;              // keys of a tile
 constexpr float PR_SLACK = 8.0f;
+constexpr float PR_ROOM = 0x1p-40f;   // the careful pass: a factor of the weights, so that no sum of finite values overflows
 
 // Bytes of one stage: panels [64 keys][DN], [64][DR], [64][DV], row-major, 16-byte
 // pieces permuted within a row by an XOR with a function of the row that spreads the
@@ -64,7 +65,8 @@ __device__ __forceinline__ void load_panel(const uint16_t* base, int64_t ts, int
 // a value that is not finite is not 0, so such a value would reach rows that do not see
 // it.  That shows in the result: the block then stores nothing and returns true, and
 // goes again with SAFE, which takes the values that are not finite apart in the tiles
-// that hold masked keys.
+// that hold masked keys, and keeps the weights small (by a power of two: all else has
+// the same bits), as those above 1 may have made a sum overflow.
 template <int DN, int DR, int DV, bool SAFE>
 __device__ __forceinline__ bool prompt_block(const PromptArgs& a, uint8_t* smem) {
     constexpr int STAGE = prompt_stage_bytes<DN, DR, DV>();
@@ -220,7 +222,7 @@ __device__ __forceinline__ bool prompt_block(const PromptArgs& a, uint8_t* smem)
                     const int mt = s4 >> 1, i = 8 * (s4 & 1) + j;
                     const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[mt][i], a.scale_log2, -ref));
                     psum += x;
-                    pf[s4][j] = (__bf16)x;
+                    pf[s4][j] = (__bf16)(SAFE ? x * PR_ROOM : x);
                 }
             l_run = l_run * alpha + psum;
             if (__ballot(move)) {
@@ -295,7 +297,7 @@ __device__ __forceinline__ bool prompt_block(const PromptArgs& a, uint8_t* smem)
         if (again) return true;
     }
     if (qi >= len) return false;
-    const float inv = 1.0f / l_run;
+    const float inv = (1.0f / l_run) * (SAFE ? 1.0f / PR_ROOM : 1.0f);
     uint16_t* out = a.out + ((start + qi) * a.H + h) * DV + 4 * hh;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
@@ -310,16 +312,17 @@ __device__ __forceinline__ bool prompt_block(const PromptArgs& a, uint8_t* smem)
     return false;
 }
 
-// a call, so that the rare block's registers are not the ordinary one's
+// a call, so that the rare block's registers are not the ordinary one's; by value, so
+// that nothing of the ordinary one has an address
 template <int DN, int DR, int DV>
-__device__ __attribute__((noinline)) void prompt_block_again(const PromptArgs* a, uint8_t* smem) {
-    (void)prompt_block<DN, DR, DV, true>(*a, smem);
+__device__ __attribute__((noinline)) void prompt_block_again(PromptArgs a, uint8_t* smem) {
+    (void)prompt_block<DN, DR, DV, true>(a, smem);
 }
 
 template <int DN, int DR, int DV>
 __global__ __launch_bounds__(64 * PR_WAVES, 2) void prompt_kernel(PromptArgs a) {
     __shared__ __align__(256) uint8_t smem[2 * prompt_stage_bytes<DN, DR, DV>()];
-    if (prompt_block<DN, DR, DV, false>(a, smem)) prompt_block_again<DN, DR, DV>(&a, smem);
+    if (prompt_block<DN, DR, DV, false>(a, smem)) prompt_block_again<DN, DR, DV>(a, smem);
 }
 
 int64_t prompt_blocks(int64_t len) { return (len + PR_ROWS - 1) / PR_ROWS; }

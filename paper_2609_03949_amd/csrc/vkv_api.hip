@@ -731,6 +731,122 @@ int vkv_prompt_attend(vkv_ctx* ctx, const vkv_prompt* pr, float scale, uint16_t*
     return VKV_OK;
 }
 
+// ------------------------------------------------------- the paged cache
+
+static int check_pages(vkv_ctx* ctx, const vkv_pages* pg) {
+    if (!pg) return fail(ctx, VKV_E_ARG, "pages is NULL");
+    if (pg->B < 1 || pg->B > 65535) return fail(ctx, VKV_E_SHAPE, "B=%lld outside [1, 65535]", (long long)pg->B);
+    if (pg->max_kv < 0 || pg->max_kv > (1ll << 30))
+        return fail(ctx, VKV_E_SHAPE, "max_kv=%lld outside [0, 2^30]", (long long)pg->max_kv);
+    if (pg->n_pages < 1 || pg->n_pages >= (1ll << 31))
+        return fail(ctx, VKV_E_SHAPE, "n_pages=%lld outside [1, 2^31)", (long long)pg->n_pages);
+    if (pg->page < 1 || pg->page > 65536 || (pg->page & (pg->page - 1)))
+        return fail(ctx, VKV_E_UNSUPPORTED, "page=%d: need a power of two in [1, 65536]", pg->page);
+    if (!pg->cache || !pg->table || !pg->kv_len) return fail(ctx, VKV_E_ARG, "cache, table and kv_len are required");
+    if (!al16(pg->cache)) return fail(ctx, VKV_E_ALIGN, "cache must be 16-byte aligned");
+    if (((uintptr_t)pg->table & 3u) || ((uintptr_t)pg->kv_len & 3u))
+        return fail(ctx, VKV_E_ALIGN, "table and kv_len must be 4-byte aligned");
+    if (pg->row_stride < D_ROW || pg->row_stride % 8)
+        return fail(ctx, VKV_E_ALIGN, "row_stride=%lld: need >= 576 and a multiple of 8", (long long)pg->row_stride);
+    if (pg->page_stride < 0 || pg->page_stride % 8)
+        return fail(ctx, VKV_E_ALIGN, "page_stride=%lld: need a multiple of 8, at least 0", (long long)pg->page_stride);
+    if (pg->table_stride < (pg->max_kv + pg->page - 1) / pg->page)
+        return fail(ctx, VKV_E_SHAPE, "table_stride=%lld holds fewer than max_kv=%lld rows", (long long)pg->table_stride,
+                    (long long)pg->max_kv);
+    return VKV_OK;
+}
+
+static int check_chunk(vkv_ctx* ctx, const vkv_pages* pg, const vkv_chunk* ch) {
+    int rc = check_pages(ctx, pg);
+    if (rc) return rc;
+    if (!ch) return fail(ctx, VKV_E_ARG, "chunk is NULL");
+    if (ch->H < 1 || ch->H > 128) return fail(ctx, VKV_E_SHAPE, "H=%lld outside [1, 128]", (long long)ch->H);
+    if (ch->n_tok < 0 || ch->n_tok >= (1ll << 31) || ch->max_q < 0 || ch->max_q >= (1ll << 31))
+        return fail(ctx, VKV_E_SHAPE, "n_tok=%lld or max_q=%lld outside [0, 2^31)", (long long)ch->n_tok, (long long)ch->max_q);
+    if (ch->max_q * ch->H > (1ll << 30) || pg->B * chunk_split(pg->B, ch->H, ch->max_q, pg->max_kv).mb >= (1ll << 31))
+        return fail(ctx, VKV_E_SHAPE, "max_q=%lld with H=%lld and B=%lld: too many rows", (long long)ch->max_q,
+                    (long long)ch->H, (long long)pg->B);
+    if (!ch->q_lat || !ch->q_rope || !ch->cu) return fail(ctx, VKV_E_ARG, "q_lat, q_rope and cu are required");
+    if (!al16(ch->q_lat) || !al16(ch->q_rope)) return fail(ctx, VKV_E_ALIGN, "q_lat and q_rope must be 16-byte aligned");
+    if (ch->q_lat_stride < 0 || ch->q_lat_stride % 8 || ch->q_rope_stride < 0 || ch->q_rope_stride % 8)
+        return fail(ctx, VKV_E_ALIGN, "query strides %lld, %lld: need multiples of 8, at least 0", (long long)ch->q_lat_stride,
+                    (long long)ch->q_rope_stride);
+    return VKV_OK;
+}
+
+static ChunkArgs chunk_args(const vkv_pages* pg, const vkv_chunk* ch) {
+    ChunkArgs a{};
+    a.cache = pg->cache;
+    a.rs = pg->row_stride;
+    a.ps = pg->page_stride;
+    while ((1 << a.shift) < pg->page) ++a.shift;
+    a.page_mask = pg->page - 1;
+    a.n_pages = (int)pg->n_pages;
+    a.table = pg->table;
+    a.tstride = pg->table_stride;
+    a.kv_len = pg->kv_len;
+    a.max_kv = (int)pg->max_kv;
+    a.q_lat = ch->q_lat;
+    a.q_rope = ch->q_rope;
+    a.qls = ch->q_lat_stride;
+    a.qrs = ch->q_rope_stride;
+    a.cu = ch->cu;
+    a.n_tok = ch->n_tok;
+    a.B = (int)pg->B;
+    a.H = (int)ch->H;
+    a.max_q = (int)ch->max_q;
+    return a;
+}
+
+// the workspace's arrays
+static size_t chunk_layout(const ChunkSplit& sp, size_t* part_o, size_t* part_ml, size_t* first) {
+    *part_o = 0;
+    *part_ml = up256(sp.part_o);
+    *first = *part_ml + up256(sp.part_ml);
+    return *first + up256(sp.first);
+}
+
+int vkv_chunk_workspace_size(const vkv_pages* pg, const vkv_chunk* ch, size_t* bytes) {
+    if (!bytes) return fail(nullptr, VKV_E_ARG, "bytes is NULL");
+    int rc = check_chunk(nullptr, pg, ch);
+    if (rc) return rc;
+    size_t po, pml, first;
+    *bytes = chunk_layout(chunk_split(pg->B, ch->H, ch->max_q, pg->max_kv), &po, &pml, &first);
+    return VKV_OK;
+}
+
+int vkv_chunk_attend(vkv_ctx* ctx, const vkv_pages* pg, const vkv_chunk* ch, void* ws, size_t ws_bytes, float scale,
+                     uint16_t* out, float* lse, void* stream) {
+    if (!ctx) return fail(nullptr, VKV_E_ARG, "ctx is NULL");
+    int rc = check_chunk(ctx, pg, ch);
+    if (rc) return rc;
+    if (bad_scale(scale)) return fail(ctx, VKV_E_ARG, "scale must be positive and finite");
+    if (!out || !lse) return fail(ctx, VKV_E_ARG, "out and lse are required");
+    if (!al16(out)) return fail(ctx, VKV_E_ALIGN, "out must be 16-byte aligned");
+    const ChunkSplit sp = chunk_split(pg->B, ch->H, ch->max_q, pg->max_kv);
+    size_t po, pml, first;
+    const size_t need = chunk_layout(sp, &po, &pml, &first);
+    if (need > 0 && (rc = check_ws(ctx, ws, ws_bytes, need))) return rc;
+    if (ch->n_tok == 0 || ch->max_q == 0) return VKV_OK;
+    ChunkArgs a = chunk_args(pg, ch);
+    char* w = (char*)ws;
+    a.mb = (int)sp.mb;
+    a.runs = (int)sp.runs;
+    a.min_run = (int)sp.min_run;
+    a.scale_log2 = scale * 1.4426950408889634f;
+    a.out = out;
+    a.lse = lse;
+    if (sp.runs) {
+        a.part_o = reinterpret_cast<float*>(w + po);
+        a.part_ml = reinterpret_cast<float*>(w + pml);
+        a.first = reinterpret_cast<int32_t*>(w + first);
+    }
+    DeviceGuard dev(ctx);
+    HIP_TRY(ctx, dev.err);
+    HIP_TRY(ctx, launch_chunk(a, sp, (hipStream_t)stream));
+    return VKV_OK;
+}
+
 int vkv_set_timing(vkv_ctx* ctx, int enable) {
     if (!ctx) return fail(nullptr, VKV_E_ARG, "ctx is NULL");
     if (enable) {

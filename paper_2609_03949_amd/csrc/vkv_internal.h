@@ -309,6 +309,41 @@ struct PromptArgs {
     float* lse;            // [n_tok, H]
 };
 
+// the queries of a chunk over a paged cache (attention and attention weights)
+struct ChunkArgs {
+    const uint16_t* cache;
+    int64_t rs, ps;        // row and page strides, elements
+    int shift, page_mask;  // log2 of the rows of a page, rows - 1
+    int n_pages;
+    const int32_t* table;  // [B, tstride]
+    int64_t tstride;
+    const int32_t* kv_len; // [B]
+    int max_kv;
+    const uint16_t* q_lat; // [n_tok * H] rows of 512
+    const uint16_t* q_rope;// [n_tok * H] rows of 64
+    int64_t qls, qrs;      // their strides, elements
+    const int32_t* cu;     // [B + 1]
+    int64_t n_tok;
+    int B, H, max_q;
+    int mb;                // blocks of rows of a sequence
+    int runs, min_run;     // most runs the tiles are cut into, fewest tiles of one
+    float scale_log2;
+    uint16_t* out;         // [n_tok, H, 512]
+    float* lse;            // [n_tok, H]
+    int32_t* first;        // [units + 1] first tile of each unit in the run of all tiles
+    float* part_o;         // [2 runs][16 qg rows x 512], accumulator order
+    float* part_ml;        // [2 runs][16 qg rows][2]
+};
+constexpr int CK_MAX_UNITS = 1024;   // units up to which the tiles are cut into equal runs
+constexpr int CK_RUNS = 256;         // one per CU
+// how a chunk is cut: waves by rows (16 qg rows a unit), units, runs (0: a workgroup per unit), workspace bytes
+struct ChunkSplit {
+    int64_t qg, mb, units, runs, min_run;
+    size_t part_o, part_ml, first;
+};
+ChunkSplit chunk_split(int64_t B, int64_t H, int64_t max_q, int64_t max_kv);
+hipError_t launch_chunk(const ChunkArgs& a, const ChunkSplit& sp, hipStream_t s);
+
 hipError_t launch_qprep(const QprepArgs& a, hipStream_t s);
 int64_t prompt_blocks(int64_t len);
 hipError_t launch_prompt(const PromptArgs& a, int dn, int dr, hipStream_t s);

@@ -59,6 +59,18 @@ __device__ __forceinline__ void lds_wait(T0& x) {
     asm volatile("s_waitcnt lgkmcnt(%1)" : "+v"(x) : "n"(N));
 }
 
+// op-reduction of x over the four 16-lane groups (lanes c, c+16, c+32, c+48),
+// result in all of them: two cross-lane swaps, no LDS traffic
+template <typename Op>
+__device__ __forceinline__ float allreduce_groups(float x, Op op) {
+    const uint32_t u = __float_as_uint(x);
+    const auto r32 = __builtin_amdgcn_permlane32_swap(u, u, false, false);   // lane l ^ 32
+    const float y = op(__uint_as_float(r32[0]), __uint_as_float(r32[1]));
+    const uint32_t v = __float_as_uint(y);
+    const auto r16 = __builtin_amdgcn_permlane16_swap(v, v, false, false);   // lane l ^ 16
+    return op(__uint_as_float(r16[0]), __uint_as_float(r16[1]));
+}
+
 // the larger of x in lanes l and l ^ 32, in both
 __device__ __forceinline__ float half_max(float x) {
     const uint32_t u = __float_as_uint(x);

@@ -72,3 +72,97 @@ def test_prompt_binding_checks_its_tensors(vkv):
         with pytest.raises(ValueError):
             a = dict(dict(q=q, k=k, v=v, cu=cu, k_rope=kr), **bad)
             vkv.Prompt(a["q"], a["k"], a["v"], a["cu"], 5, k_rope=a["k_rope"])
+
+
+PAGES = dict(B=3, max_kv=1000, n_pages=64, page=64, cache=FAKE, row_stride=576, page_stride=64 * 576, table=FAKE,
+             table_stride=16, kv_len=FAKE)
+CHUNK = dict(n_tok=7, H=16, max_q=4, q_lat=FAKE, q_lat_stride=512, q_rope=FAKE, q_rope_stride=64, cu=FAKE)
+PAGES_BAD = [
+    (dict(B=0), -2), (dict(B=65536), -2), (dict(max_kv=-1), -2), (dict(max_kv=(1 << 30) + 1), -2), (dict(n_pages=0), -2),
+    (dict(n_pages=1 << 31), -2), (dict(page=0), -4), (dict(page=48), -4), (dict(page=1 << 17), -4), (dict(page=-64), -4),
+    (dict(cache=None), -1), (dict(table=None), -1), (dict(kv_len=None), -1), (dict(cache=FAKE + 8), -3), (dict(table=FAKE + 2), -3),
+    (dict(kv_len=FAKE + 1), -3), (dict(row_stride=568), -3), (dict(row_stride=580), -3), (dict(page_stride=-8), -3),
+    (dict(page_stride=4), -3), (dict(table_stride=15), -2),
+]
+CHUNK_BAD = [
+    (dict(H=0), -2), (dict(H=129), -2), (dict(n_tok=-1), -2), (dict(n_tok=1 << 31), -2), (dict(max_q=-1), -2),
+    (dict(max_q=1 << 27), -2), (dict(q_lat=None), -1), (dict(q_rope=None), -1), (dict(cu=None), -1), (dict(q_lat=FAKE + 8), -3),
+    (dict(q_rope=FAKE + 2), -3), (dict(q_lat_stride=-8), -3), (dict(q_lat_stride=513), -3), (dict(q_rope_stride=68), -3),
+]
+
+
+def chunk(vkv, ctx, change, ws=FAKE, ws_bytes=None, scale=0.1, out=FAKE, lse=FAKE):
+    lib = vkv.load()
+    pg = make(vkv._Pages, PAGES, **{k: v for k, v in change.items() if k in PAGES})
+    ch = make(vkv._Chunk, CHUNK, **{k: v for k, v in change.items() if k in CHUNK})
+    n = ctypes.c_size_t(0)
+    if ws_bytes is None:
+        rc = lib.vkv_chunk_workspace_size(ctypes.byref(pg), ctypes.byref(ch), ctypes.byref(n))
+        if rc:
+            return rc
+        ws_bytes = n.value
+    return lib.vkv_chunk_attend(ctx, ctypes.byref(pg), ctypes.byref(ch), ws, ws_bytes, scale, out, lse, None)
+
+
+@pytest.mark.parametrize("change,code", PAGES_BAD + CHUNK_BAD)
+def test_chunk_refusals(vkv, ctx, change, code):
+    assert chunk(vkv, ctx, change) == code and vkv.load().vkv_last_error(None)
+    assert chunk(vkv, ctx, change, ws_bytes=1 << 40) == code and vkv.load().vkv_last_error(ctx)
+
+
+def test_chunk_call_refusals(vkv, ctx):
+    assert chunk(vkv, ctx, {}, scale=0.0) == -1 and chunk(vkv, ctx, {}, scale=float("nan")) == -1
+    assert chunk(vkv, ctx, {}, out=None) == -1 and chunk(vkv, ctx, {}, lse=None) == -1
+    assert chunk(vkv, ctx, {}, out=FAKE + 8) == -3
+    assert chunk(vkv, ctx, {}, ws=None) == -7 and chunk(vkv, ctx, {}, ws_bytes=100) == -7
+    assert chunk(vkv, ctx, {}, ws=FAKE + 16) == -3
+    lib = vkv.load()
+    assert lib.vkv_chunk_attend(None, None, None, None, 0, 0.1, None, None, None) == -1
+    assert lib.vkv_chunk_attend(ctx, None, None, None, 0, 0.1, None, None, None) == -1
+    assert lib.vkv_chunk_workspace_size(None, None, None) == -1
+
+
+def test_chunk_without_work_needs_no_device(vkv, ctx):
+    assert chunk(vkv, ctx, dict(n_tok=0)) == 0
+    assert chunk(vkv, ctx, dict(max_q=0)) == 0
+
+
+def test_chunk_workspace_depends_on_the_bounds_alone(vkv):
+    lib = vkv.load()
+
+    def size(**kw):
+        n = ctypes.c_size_t(0)
+        pg = make(vkv._Pages, PAGES, **{k: v for k, v in kw.items() if k in PAGES})
+        ch = make(vkv._Chunk, CHUNK, **{k: v for k, v in kw.items() if k in CHUNK})
+        assert lib.vkv_chunk_workspace_size(ctypes.byref(pg), ctypes.byref(ch), ctypes.byref(n)) == 0
+        return n.value
+
+    assert size(n_tok=1) == size(n_tok=1000) and size() % 256 == 0
+    assert size(max_kv=1 << 20, table_stride=1 << 14, max_q=1, H=128) < 160 << 20
+    assert size(B=65535, max_q=64, H=128) == 0        # a workgroup per block of rows: nothing to join
+
+
+def test_pages_and_chunk_bindings_check_their_tensors(vkv):
+    torch = pytest.importorskip("torch")
+    bf, i32 = torch.bfloat16, torch.int32
+    cache, table, kv = torch.zeros(6, 16, 576, dtype=bf), torch.zeros(2, 3, dtype=i32), torch.zeros(2, dtype=i32)
+    pg = vkv.Pages(cache, table, kv, 48)
+    assert (pg.c.page, pg.c.n_pages, pg.c.page_stride, pg.c.row_stride, pg.c.table_stride) == (16, 6, 9216, 576, 3)
+    for bad in (dict(cache=cache.float()), dict(cache=cache[..., :512]), dict(table=table.long()), dict(kv_len=kv[:1]),
+                dict(max_kv=49), dict(table=table.t()), dict(kv_len=kv.long())):
+        with pytest.raises(ValueError):
+            vkv.Pages(**dict(dict(cache=cache, table=table, kv_len=kv, max_kv=48), **bad))
+    dense = vkv.Pages.of_cache(torch.zeros(2, 96, 576, dtype=bf), kv, page=32)
+    assert (dense.c.n_pages, dense.c.page, dense.max_kv) == (6, 32, 96)
+    with pytest.raises(ValueError):
+        vkv.Pages.of_cache(torch.zeros(2, 96, 576, dtype=bf), kv, page=64)
+    q = torch.zeros(5, 4, 576, dtype=bf)
+    cu = torch.tensor([0, 2, 5], dtype=i32)
+    ch = vkv.Chunk(q[..., :512], q[..., 512:], cu, 3)
+    assert (ch.c.q_lat_stride, ch.c.q_rope_stride, ch.c.n_tok, ch.c.H) == (576, 576, 5, 4)
+    for bad in (dict(q_lat=q[..., :500]), dict(q_rope=q[:4, :, 512:]), dict(cu=cu.long()), dict(q_lat=q[..., :512].half()),
+                dict(q_lat=torch.zeros(5, 8, 512, dtype=bf)[:, :4])):
+        with pytest.raises(ValueError):
+            vkv.Chunk(**dict(dict(q_lat=q[..., :512], q_rope=q[..., 512:], cu=cu, max_q=3), **bad))
+    with pytest.raises(ValueError):
+        vkv.chunk_workspace_size(pg, vkv.Chunk(q[..., :512], q[..., 512:], cu[:2], 3))

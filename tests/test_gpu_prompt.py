@@ -138,6 +138,14 @@ def test_what_a_row_does_not_see_does_not_reach_it(ctx, dims):
     assert bool((out[247:] == 7.0).all()) and bool((lse[247:] == 7.0).all())
 
 
+def test_values_near_the_largest(ctx):
+    """Values near the type's largest, whose weighted mean is finite."""
+    x = inputs([200], 2, 1, WIDE, seed=12)
+    x["v"][..., 3] = 3.0e38
+    x["v"][50, :, 4] = -3.0e38
+    compare(x, *run(ctx, x))
+
+
 def test_rows_behind_are_left(ctx):
     x = inputs([20, 44], 3, 3, NARROW, behind=30)
     out, lse = run(ctx, x, fill=3.0)
