@@ -22,6 +22,10 @@
  *                     softmax as exact copies)
  *   vkv_step_run      query_prep -> score -> select -> [admit] -> attend in one call
  *
+ * Around it: causal attention over the prompt (vkv_prompt_attend), attention of one
+ * or more new tokens over a paged cache (vkv_chunk_attend), and eviction by accumulated
+ * attention weight (vkv_weight_accumulate, vkv_weight_select, vkv_cache_evict).
+ *
  * Conventions (all entry points):
  *   - Pointers are DEVICE pointers unless stated.  The caller owns every
  *     buffer; the library never allocates or frees caller memory.  Per-step
@@ -587,6 +591,67 @@ typedef struct vkv_chunk {
 int vkv_chunk_workspace_size(const vkv_pages* pg, const vkv_chunk* ch, size_t* bytes);
 int vkv_chunk_attend(vkv_ctx* ctx, const vkv_pages* pg, const vkv_chunk* ch, void* ws, size_t ws_bytes, float scale,
                      uint16_t* out, float* lse, void* stream);
+
+/* ------------------------------------ eviction by accumulated attention weight */
+
+/*
+ * The attention weight every cache row has drawn, kept up from step to step
+ * (the query-dependent counterpart of sigma: what eviction by accumulated
+ * attention ranks rows by).  After vkv_chunk_attend on the same pages and chunk:
+ *   weight[b,u] = decay * prev[b,u] + sum_{t,h: u seen} exp(s_thu - lse[t,h]),   u < kv_len[b],
+ * s as in vkv_chunk_attend.  The chunk's own rows (the last nq ones) start at 0:
+ * prev is not read there, nor anywhere with decay = 0 or prev = NULL.  A sequence
+ * without new tokens keeps its weights (weight = prev, or 0).  Rows from kv_len[b]
+ * on are left as they are; rows on absent pages draw nothing; queries whose lse is
+ * -inf draw nothing from any row.
+ *   lse           [n_tok, H] fp32, as vkv_chunk_attend wrote it
+ *   prev, weight  row u of sequence b at b*weight_stride + u, fp32; the same
+ *                 buffer or buffers that do not overlap; weight_stride >= max_kv
+ *   decay         finite, >= 0
+ * bf16 MFMA, fp32 accumulation; no atomics: the same inputs give the same bits.
+ * ws: vkv_weight_workspace_size bytes (0 is possible), 256-byte aligned; the rules
+ * of vkv_chunk_attend's.
+ */
+int vkv_weight_workspace_size(const vkv_pages* pg, const vkv_chunk* ch, size_t* bytes);
+int vkv_weight_accumulate(vkv_ctx* ctx, const vkv_pages* pg, const vkv_chunk* ch, const float* lse, void* ws,
+                          size_t ws_bytes, float scale, float decay, const float* prev, float* weight,
+                          int64_t weight_stride, void* stream);
+
+/*
+ * The tier of largest weight: of the n = kv_len[b] rows of sequence b (taken into
+ * [0, max_kv]) the first nsink, the last `recent`, and of the others those of
+ * largest weight (ties: the lower row; NaN ranks below every number), `keep` in
+ * all, or every row where n <= keep.
+ *   kept [B, keep] int32, ascending, -1 from count[b] on;  count [B] int32 = min(n, keep)
+ * 1 <= keep <= 2^30, nsink, recent >= 0, nsink + recent <= keep,
+ * weight_stride >= max_kv.  A tier for vkv_step_run_kept (with kept rows of the
+ * archive) or vkv_cache_evict.
+ */
+int vkv_weight_select(vkv_ctx* ctx, const float* weight, int64_t B, int64_t max_kv, int64_t weight_stride,
+                      const int32_t* kv_len, int64_t keep, int64_t nsink, int64_t recent, int32_t* kept,
+                      int32_t* count, void* stream);
+
+/*
+ * Eviction in place: moves the rows of a tier to the front of a paged cache, where
+ * they are the whole cache of a sequence of count[b] rows (the caller's new
+ * kv_len; pages from ceil(count[b] / page) on are free).  The cache is position-free
+ * (Lemma (Exchangeability)), so rows need not keep their order: kept rows below
+ * count[b] stay, and the r-th slot below count[b] without one takes the r-th kept
+ * row from count[b] on.
+ *   kept   [B, keep] int32: count[b] rows of [0, kv_len[b]), ascending (from
+ *          vkv_weight_select or vkv_sigma_select); count [B] int32
+ *   origin [B, keep] int32 (may be NULL): the row that lies in slot j now, -1 from
+ *          count[b] on
+ *   weight, weight_out (may both be NULL): weight_out[b*keep + j] = weight[b*weight_stride
+ *          + origin[b,j]], 0 from count[b] on; the buffers may not overlap
+ * Rows below kv_len[b] must not lie on pages that another sequence (or another entry of
+ * the table) uses.  Entries that are not rows of an ascending table are not moved
+ * (origin -1); a row is not moved from or to an absent page.  Only slots
+ * below count[b] are written, so a call on the same table and tier may be
+ * repeated.  1 <= keep <= 2^30.
+ */
+int vkv_cache_evict(vkv_ctx* ctx, const vkv_pages* pg, const int32_t* kept, const int32_t* count, int64_t keep,
+                    int32_t* origin, const float* weight, int64_t weight_stride, float* weight_out, void* stream);
 
 /* enable != 0: vkv_step_run records a pair of HIP events around its score
  * scan, on the call's stream, for up to 512 calls; vkv_score_timing reads

@@ -22,7 +22,8 @@ __all__ = [
     "step_run", "step_run_static", "check_rows", "row_max", "trigger", "required_inflation", "conformal_z",
     "step_run_trigger", "sketch_workspace_size", "sketch_basis", "sigma_workspace_size", "sigma_close",
     "sigma_tier_size", "sigma_select", "step_run_kept", "pack_rows", "page_box", "page_bound", "SIGMA_BLOCK",
-    "Prompt", "prompt_attend", "Pages", "Chunk", "chunk_workspace_size", "chunk_attend", "exported_symbols",
+    "Prompt", "prompt_attend", "Pages", "Chunk", "chunk_workspace_size", "chunk_attend",
+    "weight_workspace_size", "weight_accumulate", "weight_select", "cache_evict", "exported_symbols",
 ]
 
 VKV_MODE_ROPE, VKV_MODE_DIGEST, VKV_MODE_ROPE_DIGEST = 1, 2, 3
@@ -38,7 +39,8 @@ exported_symbols = (
     "vkv_row_max", "vkv_trigger", "vkv_required_inflation", "vkv_conformal_z", "vkv_step_run_trigger",
     "vkv_sketch_workspace_size", "vkv_sketch_basis", "vkv_sigma_workspace_size", "vkv_sigma_close",
     "vkv_sigma_select", "vkv_step_run_kept", "vkv_pack_rows", "vkv_page_box", "vkv_page_bound",
-    "vkv_prompt_attend", "vkv_chunk_workspace_size", "vkv_chunk_attend",
+    "vkv_prompt_attend", "vkv_chunk_workspace_size", "vkv_chunk_attend", "vkv_weight_workspace_size",
+    "vkv_weight_accumulate", "vkv_weight_select", "vkv_cache_evict",
 )
 SIGMA_BLOCK = 4096
 
@@ -150,6 +152,10 @@ def load():
     pg, ch, sz = ctypes.POINTER(_Pages), ctypes.POINTER(_Chunk), ctypes.c_size_t
     lib.vkv_chunk_workspace_size.argtypes = [pg, ch, ctypes.POINTER(sz)]
     lib.vkv_chunk_attend.argtypes = [P, pg, ch, P, sz, f32, P, P, P]
+    lib.vkv_weight_workspace_size.argtypes = [pg, ch, ctypes.POINTER(sz)]
+    lib.vkv_weight_accumulate.argtypes = [P, pg, ch, P, P, sz, f32, f32, P, P, i64, P]
+    lib.vkv_weight_select.argtypes = [P, P, i64, i64, i64, P, i64, i64, i64, P, P, P]
+    lib.vkv_cache_evict.argtypes = [P, pg, P, P, i64, P, P, i64, P, P]
     lib.vkv_set_timing.argtypes = [P, ctypes.c_int]
     lib.vkv_score_timing.argtypes = [P, ctypes.POINTER(ctypes.c_float), ctypes.c_int]
     for name in exported_symbols:
@@ -606,6 +612,53 @@ def chunk_attend(ctx: Context, pages: Pages, chunk: Chunk, ws: torch.Tensor, sca
         ctx.handle, pages.ref, chunk.ref, _ptr(ws), ws.numel() * ws.element_size(), float(scale),
         _typed(out, torch.bfloat16, "out", (n, H, D_LAT)), _typed(lse, torch.float32, "lse", (n, H)),
         _call_stream(ctx, stream)))
+
+
+def weight_workspace_size(pages: Pages, chunk: Chunk) -> int:
+    _sequences(pages, chunk)
+    lib = load()
+    n = ctypes.c_size_t(0)
+    rc = lib.vkv_weight_workspace_size(pages.ref, chunk.ref, ctypes.byref(n))
+    if rc != 0:
+        raise VkvError(rc, lib.vkv_last_error(None).decode())
+    return int(n.value)
+
+
+def weight_accumulate(ctx: Context, pages: Pages, chunk: Chunk, lse: torch.Tensor, ws: Optional[torch.Tensor],
+                      scale: float, decay: float, prev: Optional[torch.Tensor], weight: torch.Tensor, stream=None):
+    """vkv_weight_accumulate: weight [B, max_kv or more] fp32 <- decay * prev + the weights the chunk's queries give
+    (lse [n,H] from chunk_attend); prev is None, weight itself, or another buffer of its shape."""
+    _sequences(pages, chunk)
+    f = torch.float32
+    ctx.check(ctx.lib.vkv_weight_accumulate(
+        ctx.handle, pages.ref, chunk.ref, _typed(lse, f, "lse", (chunk.n_tok, chunk.H)), _ptr(ws),
+        0 if ws is None else ws.numel() * ws.element_size(), float(scale), float(decay),
+        _typed(prev, f, "prev", tuple(weight.shape)), _typed(weight, f, "weight", (pages.B, None)), weight.shape[1],
+        _call_stream(ctx, stream)))
+
+
+def weight_select(ctx: Context, weight: torch.Tensor, kv_len: torch.Tensor, max_kv: int, nsink: int, recent: int,
+                  kept: torch.Tensor, count: torch.Tensor, stream=None):
+    """vkv_weight_select: kept [B, keep] int32, count [B] int32 from weight [B, max_kv or more] fp32."""
+    B = weight.shape[0]
+    i32 = torch.int32
+    ctx.check(ctx.lib.vkv_weight_select(
+        ctx.handle, _typed(weight, torch.float32, "weight", (None, None)), B, int(max_kv), weight.shape[1],
+        _typed(kv_len, i32, "kv_len", (B,)), kept.shape[-1], int(nsink), int(recent), _typed(kept, i32, "kept", (B, None)),
+        _typed(count, i32, "count", (B,)), _call_stream(ctx, stream)))
+
+
+def cache_evict(ctx: Context, pages: Pages, kept: torch.Tensor, count: torch.Tensor,
+                origin: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None,
+                weight_out: Optional[torch.Tensor] = None, stream=None):
+    """vkv_cache_evict: the rows kept [B, keep] (count [B] of them) to the front of the cache, in place; origin
+    [B, keep] int32, weight [B, max_kv or more] -> weight_out [B, keep] fp32."""
+    i32, f = torch.int32, torch.float32
+    B, K = pages.B, kept.shape[-1]
+    ctx.check(ctx.lib.vkv_cache_evict(
+        ctx.handle, pages.ref, _typed(kept, i32, "kept", (B, K)), _typed(count, i32, "count", (B,)), K,
+        _typed(origin, i32, "origin", (B, K)), _typed(weight, f, "weight", (B, None)),
+        0 if weight is None else weight.shape[1], _typed(weight_out, f, "weight_out", (B, K)), _call_stream(ctx, stream)))
 
 
 def check_rows(ctx: Context, step: Step, k: int, sel: Optional[torch.Tensor],

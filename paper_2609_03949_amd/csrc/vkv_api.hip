@@ -847,6 +847,119 @@ int vkv_chunk_attend(vkv_ctx* ctx, const vkv_pages* pg, const vkv_chunk* ch, voi
     return VKV_OK;
 }
 
+// ------------------------------------ eviction by accumulated attention weight
+
+int vkv_weight_workspace_size(const vkv_pages* pg, const vkv_chunk* ch, size_t* bytes) {
+    if (!bytes) return fail(nullptr, VKV_E_ARG, "bytes is NULL");
+    int rc = check_chunk(nullptr, pg, ch);
+    if (rc) return rc;
+    const int64_t parts = weight_parts(pg->B, ch->H, ch->max_q, pg->max_kv);
+    *bytes = parts > 1 ? up256((size_t)(parts * pg->B * pg->max_kv) * 4) : 0;
+    return VKV_OK;
+}
+
+int vkv_weight_accumulate(vkv_ctx* ctx, const vkv_pages* pg, const vkv_chunk* ch, const float* lse, void* ws,
+                          size_t ws_bytes, float scale, float decay, const float* prev, float* weight,
+                          int64_t weight_stride, void* stream) {
+    if (!ctx) return fail(nullptr, VKV_E_ARG, "ctx is NULL");
+    int rc = check_chunk(ctx, pg, ch);
+    if (rc) return rc;
+    if (bad_scale(scale)) return fail(ctx, VKV_E_ARG, "scale must be positive and finite");
+    if (!(decay >= 0.f) || !(decay < 1e30f)) return fail(ctx, VKV_E_ARG, "decay must be finite and >= 0");
+    if (!lse || !weight) return fail(ctx, VKV_E_ARG, "lse and weight are required");
+    if (weight_stride < pg->max_kv)
+        return fail(ctx, VKV_E_SHAPE, "weight_stride=%lld smaller than max_kv=%lld", (long long)weight_stride, (long long)pg->max_kv);
+    const int64_t parts = weight_parts(pg->B, ch->H, ch->max_q, pg->max_kv), blocks = weight_blocks(pg->max_kv);
+    if (pg->B * blocks * parts >= (1ll << 31))
+        return fail(ctx, VKV_E_SHAPE, "B=%lld with max_kv=%lld: too many rows", (long long)pg->B, (long long)pg->max_kv);
+    if (parts > 1 && (rc = check_ws(ctx, ws, ws_bytes, up256((size_t)(parts * pg->B * pg->max_kv) * 4)))) return rc;
+    if (pg->max_kv == 0) return VKV_OK;
+    WeightArgs w{};
+    w.c = chunk_args(pg, ch);
+    w.c.scale_log2 = scale * 1.4426950408889634f;
+    w.lse = lse;
+    w.decay = decay;
+    w.prev = prev;
+    w.weight = weight;
+    w.stride = weight_stride;
+    w.nblk = (int)blocks;
+    w.parts = (int)parts;
+    w.part = (float*)ws;
+    DeviceGuard dev(ctx);
+    HIP_TRY(ctx, dev.err);
+    HIP_TRY(ctx, launch_weight(w, (hipStream_t)stream));
+    return VKV_OK;
+}
+
+int vkv_weight_select(vkv_ctx* ctx, const float* weight, int64_t B, int64_t max_kv, int64_t weight_stride,
+                      const int32_t* kv_len, int64_t keep, int64_t nsink, int64_t recent, int32_t* kept,
+                      int32_t* count, void* stream) {
+    if (!ctx) return fail(nullptr, VKV_E_ARG, "ctx is NULL");
+    if (B < 1 || B > 65535) return fail(ctx, VKV_E_SHAPE, "B=%lld outside [1, 65535]", (long long)B);
+    if (max_kv < 0 || max_kv > (1ll << 30)) return fail(ctx, VKV_E_SHAPE, "max_kv=%lld outside [0, 2^30]", (long long)max_kv);
+    if (weight_stride < max_kv)
+        return fail(ctx, VKV_E_SHAPE, "weight_stride=%lld smaller than max_kv=%lld", (long long)weight_stride, (long long)max_kv);
+    if (keep < 1 || keep > (1ll << 30)) return fail(ctx, VKV_E_ARG, "keep=%lld outside [1, 2^30]", (long long)keep);
+    if (nsink < 0 || recent < 0 || nsink > keep || recent > keep - nsink)
+        return fail(ctx, VKV_E_ARG, "nsink=%lld and recent=%lld: need >= 0 and at most keep=%lld together", (long long)nsink,
+                    (long long)recent, (long long)keep);
+    if (!weight || !kv_len || !kept || !count) return fail(ctx, VKV_E_ARG, "weight, kv_len, kept and count are required");
+    WeightSelArgs a{};
+    a.weight = weight;
+    a.stride = weight_stride;
+    a.kv_len = kv_len;
+    a.B = (int)B;
+    a.max_kv = (int)max_kv;
+    a.nsink = (int)nsink;
+    a.recent = (int)recent;
+    a.keep = (int)keep;
+    a.kept = kept;
+    a.count = count;
+    DeviceGuard dev(ctx);
+    HIP_TRY(ctx, dev.err);
+    HIP_TRY(ctx, launch_weight_select(a, (hipStream_t)stream));
+    return VKV_OK;
+}
+
+int vkv_cache_evict(vkv_ctx* ctx, const vkv_pages* pg, const int32_t* kept, const int32_t* count, int64_t keep,
+                    int32_t* origin, const float* weight, int64_t weight_stride, float* weight_out, void* stream) {
+    if (!ctx) return fail(nullptr, VKV_E_ARG, "ctx is NULL");
+    int rc = check_pages(ctx, pg);
+    if (rc) return rc;
+    if (keep < 1 || keep > (1ll << 30)) return fail(ctx, VKV_E_ARG, "keep=%lld outside [1, 2^30]", (long long)keep);
+    if (!kept || !count) return fail(ctx, VKV_E_ARG, "kept and count are required");
+    if ((weight != nullptr) != (weight_out != nullptr)) return fail(ctx, VKV_E_ARG, "weight and weight_out go together");
+    if (weight && weight_stride < pg->max_kv)
+        return fail(ctx, VKV_E_SHAPE, "weight_stride=%lld smaller than max_kv=%lld", (long long)weight_stride, (long long)pg->max_kv);
+    if (pg->B * evict_waves(keep) >= (1ll << 31))
+        return fail(ctx, VKV_E_SHAPE, "B=%lld with keep=%lld: too many rows", (long long)pg->B, (long long)keep);
+    const vkv_chunk none{};
+    const ChunkArgs c = chunk_args(pg, &none);
+    EvictArgs a{};
+    a.cache = pg->cache;
+    a.rs = c.rs;
+    a.ps = c.ps;
+    a.shift = c.shift;
+    a.page_mask = c.page_mask;
+    a.n_pages = c.n_pages;
+    a.table = c.table;
+    a.tstride = c.tstride;
+    a.kv_len = c.kv_len;
+    a.max_kv = c.max_kv;
+    a.B = pg->B;
+    a.keep = (int)keep;
+    a.kept = kept;
+    a.count = count;
+    a.origin = origin;
+    a.weight = weight;
+    a.wstride = weight_stride;
+    a.weight_out = weight_out;
+    DeviceGuard dev(ctx);
+    HIP_TRY(ctx, dev.err);
+    HIP_TRY(ctx, launch_evict(a, (hipStream_t)stream));
+    return VKV_OK;
+}
+
 int vkv_set_timing(vkv_ctx* ctx, int enable) {
     if (!ctx) return fail(nullptr, VKV_E_ARG, "ctx is NULL");
     if (enable) {

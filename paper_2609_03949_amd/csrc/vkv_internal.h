@@ -344,6 +344,51 @@ struct ChunkSplit {
 ChunkSplit chunk_split(int64_t B, int64_t H, int64_t max_q, int64_t max_kv);
 hipError_t launch_chunk(const ChunkArgs& a, const ChunkSplit& sp, hipStream_t s);
 
+struct WeightArgs {
+    ChunkArgs c;           // cache and queries
+    const float* lse;      // [n_tok, H]
+    float decay;
+    const float* prev;     // [B, stride] or null (may be weight)
+    float* weight;         // [B, stride]
+    int64_t stride;
+    int nblk;              // blocks of cache rows of the longest sequence
+    int parts;             // parts the queries are cut into
+    float* part;           // [parts, B, max_kv]
+};
+int64_t weight_blocks(int64_t max_kv);
+int64_t weight_parts(int64_t B, int64_t H, int64_t max_q, int64_t max_kv);
+hipError_t launch_weight(const WeightArgs& w, hipStream_t s);
+
+struct WeightSelArgs {
+    const float* weight;   // [B, stride]
+    int64_t stride;
+    const int32_t* kv_len; // [B]
+    int B, max_kv, nsink, recent, keep;
+    int32_t* kept;         // [B, keep]
+    int32_t* count;        // [B]
+};
+hipError_t launch_weight_select(const WeightSelArgs& a, hipStream_t s);
+
+struct EvictArgs {
+    uint16_t* cache;
+    int64_t rs, ps;
+    int shift, page_mask, n_pages;
+    const int32_t* table;
+    int64_t tstride;
+    const int32_t* kv_len;
+    int max_kv;
+    int64_t B;
+    int keep;
+    const int32_t* kept;   // [B, keep]
+    const int32_t* count;  // [B]
+    int32_t* origin;       // [B, keep] or null
+    const float* weight;   // [B, wstride] or null
+    int64_t wstride;
+    float* weight_out;     // [B, keep] or null
+};
+int64_t evict_waves(int64_t keep);
+hipError_t launch_evict(const EvictArgs& a, hipStream_t s);
+
 hipError_t launch_qprep(const QprepArgs& a, hipStream_t s);
 int64_t prompt_blocks(int64_t len);
 hipError_t launch_prompt(const PromptArgs& a, int dn, int dr, hipStream_t s);

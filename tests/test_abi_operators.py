@@ -166,3 +166,63 @@ def test_pages_and_chunk_bindings_check_their_tensors(vkv):
             vkv.Chunk(**dict(dict(q_lat=q[..., :512], q_rope=q[..., 512:], cu=cu, max_q=3), **bad))
     with pytest.raises(ValueError):
         vkv.chunk_workspace_size(pg, vkv.Chunk(q[..., :512], q[..., 512:], cu[:2], 3))
+
+
+def weights(vkv, ctx, change, ws=FAKE, ws_bytes=1 << 40, scale=0.1, decay=0.9, lse=FAKE, prev=FAKE, weight=FAKE, stride=1000):
+    pg = make(vkv._Pages, PAGES, **{k: v for k, v in change.items() if k in PAGES})
+    ch = make(vkv._Chunk, CHUNK, **{k: v for k, v in change.items() if k in CHUNK})
+    return vkv.load().vkv_weight_accumulate(ctx, ctypes.byref(pg), ctypes.byref(ch), lse, ws, ws_bytes, scale, decay, prev,
+                                            weight, stride, None)
+
+
+@pytest.mark.parametrize("change,code", PAGES_BAD + CHUNK_BAD)
+def test_weight_refusals(vkv, ctx, change, code):
+    assert weights(vkv, ctx, change) == code and vkv.load().vkv_last_error(ctx)
+    n = ctypes.c_size_t(0)
+    pg = make(vkv._Pages, PAGES, **{k: v for k, v in change.items() if k in PAGES})
+    ch = make(vkv._Chunk, CHUNK, **{k: v for k, v in change.items() if k in CHUNK})
+    assert vkv.load().vkv_weight_workspace_size(ctypes.byref(pg), ctypes.byref(ch), ctypes.byref(n)) == code
+
+
+def test_weight_call_refusals(vkv, ctx):
+    assert weights(vkv, ctx, {}, scale=-1.0) == -1
+    for decay in (-0.1, float("nan"), float("inf")):
+        assert weights(vkv, ctx, {}, decay=decay) == -1
+    assert weights(vkv, ctx, {}, lse=None) == -1 and weights(vkv, ctx, {}, weight=None) == -1
+    assert weights(vkv, ctx, {}, stride=999) == -2
+    many = dict(max_q=64, H=128)      # enough queries for parts, which need the workspace
+    assert weights(vkv, ctx, many, ws=None) == -7 and weights(vkv, ctx, many, ws_bytes=64) == -7
+    assert weights(vkv, ctx, many, ws=FAKE + 8) == -3
+    assert weights(vkv, ctx, dict(max_kv=0), ws=None, ws_bytes=0) == 0
+    assert vkv.load().vkv_weight_accumulate(None, None, None, None, None, 0, 0.1, 1.0, None, None, 0, None) == -1
+
+
+SELECT = dict(weight=FAKE, B=2, max_kv=1000, weight_stride=1000, kv_len=FAKE, keep=100, nsink=4, recent=16, kept=FAKE, count=FAKE)
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(B=0), -2), (dict(B=65536), -2), (dict(max_kv=-1), -2), (dict(max_kv=(1 << 30) + 1, weight_stride=1 << 31), -2),
+    (dict(weight_stride=999), -2), (dict(keep=0), -1), (dict(keep=(1 << 30) + 1), -1), (dict(nsink=-1), -1), (dict(recent=-1), -1),
+    (dict(nsink=85), -1), (dict(nsink=1 << 62, recent=1 << 62), -1), (dict(weight=None), -1), (dict(kv_len=None), -1),
+    (dict(kept=None), -1), (dict(count=None), -1),
+])
+def test_select_refusals(vkv, ctx, change, code):
+    a = dict(SELECT, **change)
+    assert vkv.load().vkv_weight_select(ctx, a["weight"], a["B"], a["max_kv"], a["weight_stride"], a["kv_len"], a["keep"],
+                                        a["nsink"], a["recent"], a["kept"], a["count"], None) == code
+    assert vkv.load().vkv_weight_select(None, None, 1, 1, 1, None, 1, 0, 0, None, None, None) == -1
+
+
+EVICT = dict(kept=FAKE, count=FAKE, keep=100, origin=FAKE, weight=FAKE, weight_stride=1000, weight_out=FAKE)
+
+
+@pytest.mark.parametrize("change,code", PAGES_BAD + [
+    (dict(kept=None), -1), (dict(count=None), -1), (dict(keep=0), -1), (dict(keep=(1 << 30) + 1), -1), (dict(weight=None), -1),
+    (dict(weight_out=None), -1), (dict(weight_stride=999), -2), (dict(B=65535, keep=1 << 30), -2),
+])
+def test_evict_refusals(vkv, ctx, change, code):
+    pg = make(vkv._Pages, PAGES, **{k: v for k, v in change.items() if k in PAGES})
+    a = dict(EVICT, **{k: v for k, v in change.items() if k in EVICT})
+    assert vkv.load().vkv_cache_evict(ctx, ctypes.byref(pg), a["kept"], a["count"], a["keep"], a["origin"], a["weight"],
+                                      a["weight_stride"], a["weight_out"], None) == code
+    assert vkv.load().vkv_cache_evict(None, None, None, None, 1, None, None, 0, None, None) == -1

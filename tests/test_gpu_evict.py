@@ -1,0 +1,478 @@
+"""Eviction by accumulated attention weight: vkv_weight_accumulate against the definition in 64 bits,
+vkv_weight_select and vkv_cache_evict exactly, and runs of them with the attention calls around."""
+import math
+
+import pytest
+import torch
+
+import paper_2609_03949_amd as vkv
+
+from _attention import F32, attention, check
+from _paged import Case
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+SCALE = 1.0 / math.sqrt(192.0)
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    c = vkv.Context(0)
+    yield c
+    c.close()
+
+
+# ------------------------------------------------------------------- weights
+
+def true_lse(x):
+    """The log-sum-exp of every (token, head) in 64 bits, rounded to fp32; -inf where nothing is seen."""
+    lse, at = torch.full((x.n_tok, x.H), -math.inf, dtype=torch.float64), 0
+    for b, nq in enumerate(x.q_lens):
+        if nq and x.kv_lens[b]:
+            s = (x.q[at:at + nq].double().cpu() @ x.rows(b).double().cpu().T) * SCALE
+            lse[at:at + nq] = torch.logsumexp(s.masked_fill(~x.seen(b)[:, None, :], -math.inf), 2)
+        at += nq
+    return lse.float().to(DEV)
+
+
+def expected(x, lse, decay, prev, absent=None):
+    """weight and its bound: a term is off by the error of its score and of the exponent's argument (as in
+    _attention), the sum by one rounding a term."""
+    want, tol, at = [], [], 0
+    D = 576
+    for b, nq in enumerate(x.q_lens):
+        n = x.kv_lens[b]
+        old = torch.zeros(n, dtype=torch.float64) if prev is None else prev[b, :n].double().cpu()
+        if nq == 0:
+            want.append(old), tol.append(torch.full((n,), 1e-30, dtype=torch.float64))
+            continue
+        q, k = x.q[at:at + nq].reshape(nq * x.H, D).double().cpu(), x.rows(b).double().cpu()
+        l = lse[at:at + nq].reshape(-1, 1).double().cpu()
+        seen = x.seen(b)[:, None, :].expand(nq, x.H, n).reshape(nq * x.H, n) & (l > -math.inf)
+        if absent is not None:
+            seen = seen & ~absent[b][None, :]
+        s = SCALE * (q @ k.T)
+        p = torch.where(seen, torch.exp(s - l), 0.0)
+        e = 2 * (D + D / 32) * 2 * F32 * SCALE * (q.abs() @ k.abs().T) + 4 * 2 * F32 * (s.abs() + l.abs())
+        old = torch.where(torch.arange(n) < n - nq, decay * old, 0.0) if decay else torch.zeros(n, dtype=torch.float64)
+        total = p.sum(0)
+        want.append(old + total)
+        tol.append(torch.where(seen, p * 2 * e, 0.0).sum(0) + (nq * x.H + 16) * F32 * total + 4 * F32 * old.abs() + 1e-30)
+        at += nq
+    return want, tol
+
+
+def accumulate(ctx, x, lse, decay, prev, weight, stream=None):
+    pages, chunk = vkv.Pages(x.cache, x.table, x.kv_len, x.max_kv), vkv.Chunk(x.q_lat, x.q_rope, x.cu, x.max_q)
+    n = vkv.weight_workspace_size(pages, chunk)
+    ws = torch.full((n,), 0xFF, dtype=torch.uint8, device=DEV) if n else None
+    vkv.weight_accumulate(ctx, pages, chunk, lse, ws, SCALE, decay, prev, weight, stream)
+    return weight
+
+
+@pytest.mark.parametrize("kv_lens,q_lens,H", [
+    ([1, 31, 32, 33, 127, 128, 129, 300], [1] * 8, 16),
+    ([200, 0, 64, 500], [1, 0, 0, 3], 1),
+    ([40, 130, 7], [40, 9, 1], 17),                   # a whole prompt; odd head counts
+    ([300], [60], 128),                               # queries in parts
+    ([5000, 100], [2, 33], 40),
+    ([3, 260], [5, 260], 3),                          # more new tokens than rows
+])
+@pytest.mark.parametrize("decay", [0.0, 0.9, 1.0])
+def test_weights(ctx, kv_lens, q_lens, H, decay):
+    x = Case(kv_lens, q_lens, H, seed=H + len(kv_lens), page=32)
+    lse = true_lse(x)
+    prev = torch.rand(len(kv_lens), x.max_kv + 5, device=DEV)
+    if decay == 0.0:
+        prev[:] = math.nan
+        for b, nq in enumerate(q_lens):
+            if nq == 0:
+                prev[b] = 2.0
+    want, tol = expected(x, lse, decay, prev)
+    out = accumulate(ctx, x, lse, decay, prev, torch.full_like(prev, -3.0))
+    for b, n in enumerate(kv_lens):
+        check(f"weight of sequence {b}", out[b, :n], want[b], tol[b])
+        assert bool((out[b, n:] == -3.0).all())
+    same = prev.clone()
+    accumulate(ctx, x, lse, decay, same, same)        # in place: the same bits, other rows untouched
+    for b, n in enumerate(kv_lens):
+        assert torch.equal(same[b, :n], out[b, :n]) and torch.equal(same[b, n:].nan_to_num(9.0), prev[b, n:].nan_to_num(9.0))
+    if decay == 1.0:
+        want, tol = expected(x, lse, decay, None)
+        out = accumulate(ctx, x, lse, decay, None, torch.full_like(prev, -3.0))
+        for b, n in enumerate(kv_lens):
+            check(f"weight from nothing, sequence {b}", out[b, :n], want[b], tol[b])
+
+
+def test_weights_sum_to_the_queries(ctx):
+    """With the attention call's own lse each token and head gives 1 in all."""
+    x = Case([700, 90], [4, 1], 128, seed=3, page=64)
+    pages, chunk = vkv.Pages(x.cache, x.table, x.kv_len, x.max_kv), vkv.Chunk(x.q_lat, x.q_rope, x.cu, x.max_q)
+    ws = torch.empty(vkv.chunk_workspace_size(pages, chunk), dtype=torch.uint8, device=DEV)
+    out, lse = torch.empty(5, 128, 512, dtype=torch.bfloat16, device=DEV), torch.empty(5, 128, device=DEV)
+    vkv.chunk_attend(ctx, pages, chunk, ws, SCALE, out, lse)
+    w = accumulate(ctx, x, lse, 0.0, None, torch.zeros(2, 700, device=DEV))
+    total = w.double().sum(1).cpu()
+    assert abs(float(total[0]) / 512 - 1) < 1e-4 and abs(float(total[1]) / 128 - 1) < 1e-4
+
+
+def test_weights_of_absent_pages_and_dead_queries(ctx):
+    x = Case([100, 64], [2, 1], 16, seed=4, page=16)
+    lse = true_lse(x)
+    lse[0, 3], lse[2, 5] = -math.inf, -math.inf
+    x.table[0, 2], x.table[0, 6], x.table[1, 1] = -1, 1 << 28, x.cache.shape[0]
+    absent = [torch.zeros(100, dtype=torch.bool), torch.zeros(64, dtype=torch.bool)]
+    absent[0][32:48] = absent[0][96:] = absent[1][16:32] = True
+    prev = torch.rand(2, 100, device=DEV)
+    want, tol = expected(x, lse, 0.5, prev, absent)
+    out = accumulate(ctx, x, lse, 0.5, prev, torch.zeros_like(prev))
+    for b, n in enumerate((100, 64)):
+        check(f"weight of sequence {b}", out[b, :n], want[b], tol[b])
+
+
+def test_weights_ignore_what_is_not_seen(ctx):
+    """NaN in later tokens' rows and behind the end stays there."""
+    x = Case([150], [20], 8, seed=5)
+    lse = true_lse(x)
+    clean = accumulate(ctx, x, lse, 0.0, None, torch.zeros(1, 150, device=DEV))
+    pages, r = x.where[0]
+    x.cache[pages[149], r[149]] = math.nan
+    out = accumulate(ctx, x, lse, 0.0, None, torch.zeros(1, 150, device=DEV))
+    assert torch.equal(out[0, :149], clean[0, :149]) and bool(torch.isnan(out[0, 149]))
+
+
+# ----------------------------------------------------------------- selection
+
+def expected_tier(w, n, keep, nsink, recent):
+    if n <= keep:
+        return list(range(n))
+    always = set(range(nsink)) | set(range(n - recent, n))
+    others = [u for u in range(n) if u not in always]
+    value = [float(v) for v in w[:n].double().cpu()]
+    others.sort(key=lambda u: (-value[u] if value[u] == value[u] else math.inf, value[u] != value[u], u))
+    return sorted(always | set(others[:keep - len(always)]))
+
+
+def select(ctx, w, kv_len, keep, nsink, recent, max_kv=None):
+    B = w.shape[0]
+    kept = torch.full((B, keep), 77, dtype=torch.int32, device=DEV)
+    count = torch.full((B,), 77, dtype=torch.int32, device=DEV)
+    lens = torch.tensor(kv_len, dtype=torch.int32, device=DEV)
+    vkv.weight_select(ctx, w, lens, w.shape[1] if max_kv is None else max_kv, nsink, recent, kept, count)
+    return kept.cpu(), count.cpu()
+
+
+def check_tier(ctx, w, kv_len, keep, nsink, recent):
+    kept, count = select(ctx, w, kv_len, keep, nsink, recent)
+    for b, n in enumerate(kv_len):
+        n = min(max(n, 0), w.shape[1])
+        rows = expected_tier(w[b], n, keep, nsink, recent)
+        assert int(count[b]) == len(rows) == min(n, keep)
+        assert kept[b].tolist() == rows + [-1] * (keep - len(rows)), b
+
+
+@pytest.mark.parametrize("n,keep,nsink,recent", [
+    (1, 1, 0, 0), (2, 1, 0, 0), (5, 8, 2, 2), (64, 64, 4, 16), (65, 64, 4, 16), (1000, 100, 4, 96), (1000, 100, 0, 100),
+    (1000, 100, 100, 0), (4095, 512, 4, 64), (4096, 1, 0, 0), (4097, 4096, 0, 0), (8193, 1024, 4, 128), (20011, 5000, 7, 33),
+])
+def test_tier(ctx, n, keep, nsink, recent):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(n)
+    w = torch.exp(3 * torch.randn(3, n + 3, generator=g, device=DEV))
+    check_tier(ctx, w, [n, max(n - 1, 0), n // 2], keep, nsink, recent)
+
+
+def test_tier_of_ties_and_odd_values(ctx):
+    w = torch.zeros(6, 3000, device=DEV)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1)
+    w[1] = torch.randint(0, 3, (3000,), generator=g, device=DEV).float()      # few values
+    w[2] = torch.randn(3000, generator=g, device=DEV)
+    w[2, 5:900:7], w[2, 100:2000:13], w[2, 50:2900:11] = math.nan, math.inf, -math.inf
+    w[3, ::2] = -0.0
+    w[3, 2000:] = -1.0
+    w[4] = 1.0 + torch.randint(0, 4, (3000,), generator=g, device=DEV) * 2.0 ** -23   # neighbours
+    w[5] = math.nan
+    w[5, 1500] = -5.0
+    for keep, nsink, recent in ((200, 4, 50), (1, 0, 0), (2999, 0, 0), (1700, 0, 3)):
+        check_tier(ctx, w, [3000] * 6, keep, nsink, recent)
+
+
+def test_tier_of_long_contexts(ctx):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(2)
+    w = torch.exp(2 * torch.randn(2, 131072, generator=g, device=DEV))
+    w[1] = (w[1] * 4).round() / 4                                              # ties in numbers
+    check_tier(ctx, w, [131072, 100003], 4096, 4, 512)
+
+
+def test_tier_lengths_out_of_range(ctx):
+    w = torch.rand(3, 50, device=DEV)
+    check_tier(ctx, w, [-3, 1 << 30, 0], 20, 2, 3)
+
+
+# ---------------------------------------------------------------------- move
+
+def evict(ctx, x, kept, count, weight=None):
+    K = kept.shape[1]
+    origin = torch.full((kept.shape[0], K), 55, dtype=torch.int32, device=DEV)
+    out = None if weight is None else torch.full((kept.shape[0], K), 55.0, device=DEV)
+    vkv.cache_evict(ctx, vkv.Pages(x.cache, x.table, x.kv_len, x.max_kv), kept, count, origin, weight, out)
+    return origin, out
+
+
+def table_of(lists, K):
+    kept = torch.full((len(lists), K), -1, dtype=torch.int32)
+    for b, rows in enumerate(lists):
+        kept[b, :len(rows)] = torch.tensor(rows, dtype=torch.int32)
+    return kept.to(DEV), torch.tensor([len(r) for r in lists], dtype=torch.int32, device=DEV)
+
+
+def check_move(ctx, x, lists, K):
+    before = [x.rows(b).clone() for b in range(len(lists))]
+    whole = x.cache.clone()
+    kept, count = table_of(lists, K)
+    weight = torch.rand(len(lists), x.max_kv + 1, device=DEV)
+    origin, out = evict(ctx, x, kept, count, weight)
+    after = [x.rows(b).clone() for b in range(len(lists))]
+    for b, rows in enumerate(lists):
+        n, o = len(rows), origin[b].tolist()
+        below = [u for u in rows if u < n]
+        holes = [j for j in range(n) if j not in set(below)]
+        want = {**{u: u for u in below}, **dict(zip(holes, [u for u in rows if u >= n]))}
+        assert o == [want[j] for j in range(n)] + [-1] * (K - n), b
+        assert torch.equal(after[b][:n], before[b][torch.tensor(o[:n], dtype=torch.long, device=DEV)])
+        assert torch.equal(after[b][n:], before[b][n:])          # rows behind are as they were
+        assert torch.equal(out[b, :n], weight[b, torch.tensor(o[:n], dtype=torch.long, device=DEV)])
+        assert bool((out[b, n:] == 0).all())
+    # nothing else of the buffer is touched
+    for b, rows in enumerate(lists):
+        pages, r = x.where[b]
+        n = len(rows)
+        whole[pages[:n], r[:n]] = after[b][:n]
+    assert torch.equal(whole.view(torch.int16), x.cache.view(torch.int16))
+    again, out2 = evict(ctx, x, kept, count, weight)             # the same call once more changes nothing
+    assert torch.equal(again, origin) and torch.equal(out2, out)
+    assert torch.equal(whole.view(torch.int16), x.cache.view(torch.int16))
+
+
+@pytest.mark.parametrize("page", [1, 16, 256])
+def test_move(ctx, page):
+    g = torch.Generator()
+    g.manual_seed(page)
+
+    def some(n, k):
+        return sorted(torch.randperm(n, generator=g)[:k].tolist())
+
+    lens = [300, 65, 1, 700, 64, 500, 40, 0]
+    x = Case(lens, [1] * 8, 1, page=page, seed=6)
+    lists = [some(300, 64), some(65, 64), [0], list(range(636, 700)), list(range(64)), list(range(0, 500, 8)), [39], []]
+    check_move(ctx, x, lists, 64)
+
+
+def test_move_of_large_tiers(ctx):
+    g = torch.Generator()
+    g.manual_seed(3)
+    x = Case([9000, 5000], [1, 1], 1, page=64, seed=7)
+    check_move(ctx, x, [sorted(torch.randperm(9000, generator=g)[:4111].tolist()), sorted(torch.randperm(5000, generator=g)[:4999].tolist())],
+               4999)
+
+
+def test_move_refuses_what_is_no_tier(ctx):
+    """Entries out of range, out of order or repeated, counts out of range, absent pages: nothing outside the
+    sequence's own rows is read or written, and what is a row of the table still moves."""
+    x = Case([100, 100, 100, 50], [1] * 4, 1, page=16, seed=8)
+    whole = x.cache.clone()
+    kept, count = table_of([[5, 90, 1 << 30], [-7, 3, 95], [99, 98, 97, 96], [49]], 8)
+    count.copy_(torch.tensor([3, 3, 1 << 30, -2], dtype=torch.int32))
+    origin, _ = evict(ctx, x, kept, count)
+    own = torch.zeros(x.cache.shape[:2], dtype=torch.bool, device=DEV)
+    for b in range(4):
+        own[x.where[b][0], x.where[b][1]] = True
+    assert torch.equal(x.cache.view(torch.int16)[~own], whole.view(torch.int16)[~own])
+    o = origin.cpu()
+    assert bool(((o >= -1) & (o < 100)).all()) and bool((o[3] == -1).all())
+    assert torch.equal(x.cache.view(torch.int16)[x.where[3]], whole.view(torch.int16)[x.where[3]])
+    y = Case([64], [1], 1, page=16, seed=9)
+    rows = y.rows(0).clone()
+    y.table[0, 3] = -1
+    kept, count = table_of([[40, 41, 50, 63]], 4)
+    evict(ctx, y, kept, count)
+    assert torch.equal(y.rows(0)[:2], rows[40:42]) and torch.equal(y.rows(0)[2:], rows[2:])
+
+
+# --------------------------------------------------------------- used together
+
+def test_prompt_heads_and_latent_rows_agree(ctx):
+    """A prompt attended with expanded heads equals the same prompt attended over its latent rows with
+    absorbed queries, up to the up-projection of the outputs."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1)
+    n, H = 150, 4
+    c = torch.randn(n, 512, generator=g, device=DEV).double()
+    kr = torch.randn(n, 64, generator=g, device=DEV).to(torch.bfloat16)
+    # projections that pick dims and double or halve them: expanded keys, values and absorbed queries are
+    # exact in bf16, so both calls compute the same attention
+    pick = torch.randint(0, 512, (H, 128), generator=g, device=DEV)
+    pickv = torch.randint(0, 512, (H, 128), generator=g, device=DEV)
+    c = c.to(torch.bfloat16)
+    k = torch.stack([c[:, pick[h]] for h in range(H)], 1)
+    v = torch.stack([c[:, pickv[h]] for h in range(H)], 1)
+    q = torch.randint(-8, 9, (n, H, 128), generator=g, device=DEV).double() / 8
+    qr = torch.randn(n, H, 64, generator=g, device=DEV).to(torch.bfloat16)
+    ql = torch.zeros(n, H, 512, dtype=torch.float64, device=DEV)
+    ql.scatter_add_(2, pick[None].expand(n, H, 128), q)          # sums of a few eighths: exact in bf16
+    assert torch.equal(ql.to(torch.bfloat16).double(), ql)
+    cu = torch.tensor([0, n], dtype=torch.int32, device=DEV)
+    pr = vkv.Prompt(torch.cat([q.to(torch.bfloat16), qr], 2), k, v, cu, n, k_rope=kr)
+    out, lse = torch.empty(n, H, 128, dtype=torch.bfloat16, device=DEV), torch.empty(n, H, device=DEV)
+    vkv.prompt_attend(ctx, pr, SCALE, out, lse)
+    x = Case([n], [n], H, seed=1)
+    x.cache[x.where[0]] = torch.cat([c, kr], 1)
+    pages, chunk = vkv.Pages(x.cache, x.table, x.kv_len, n), vkv.Chunk(ql.to(torch.bfloat16), qr, cu, n)
+    ws = torch.empty(max(vkv.chunk_workspace_size(pages, chunk), 256), dtype=torch.uint8, device=DEV)
+    out2, lse2 = torch.empty(n, H, 512, dtype=torch.bfloat16, device=DEV), torch.empty(n, H, device=DEV)
+    vkv.chunk_attend(ctx, pages, chunk, ws, SCALE, out2, lse2)
+    up = torch.stack([out2[:, h][:, pickv[h]] for h in range(H)], 1)
+    seen = torch.ones(n, n, dtype=torch.bool).tril()
+    for h in range(H):
+        kk = torch.cat([k[:, h], kr], 1)
+        qq = torch.cat([q[:, h].to(torch.bfloat16), qr[:, h]], 1)
+        o, l, ot, lt = attention(qq, kk, v[:, h], seen, SCALE)
+        check("expanded", out[:, h], o, ot), check("latent", up[:, h], o, ot * 576 / 192)
+        check("lse", lse[:, h], l, lt), check("latent lse", lse2[:, h], l, lt * 576 / 192)
+
+
+def test_serving_run(ctx):
+    """Prompt into the cache, weights of its tokens, the tier, the cache cut to it, then decode steps that
+    append rows: every step's output is the attention over exactly the rows that are left."""
+    B, H, page, n0, K = 3, 16, 16, [90, 64, 130], 48
+    x = Case(n0, n0, H, page=page, seed=20, max_kv=160)
+    # pages for the rows to come
+    total = x.cache.shape[0]
+    extra = torch.randn(3 * 4, page, 576, device=DEV).to(torch.bfloat16)
+    x.cache = torch.cat([x.cache, extra])
+    for b in range(B):
+        used = -(-n0[b] // page)
+        x.table[b, used:used + 4] = torch.arange(total + 4 * b, total + 4 * b + 4, dtype=torch.int32, device=DEV)[:x.table.shape[1] - used]
+    pages, chunk = vkv.Pages(x.cache, x.table, x.kv_len, 160), vkv.Chunk(x.q_lat, x.q_rope, x.cu, x.max_q)
+    out, lse = torch.empty(x.n_tok, H, 512, dtype=torch.bfloat16, device=DEV), torch.empty(x.n_tok, H, device=DEV)
+    ws = torch.empty(max(vkv.chunk_workspace_size(pages, chunk), 256), dtype=torch.uint8, device=DEV)
+    ww = torch.empty(max(vkv.weight_workspace_size(pages, chunk), 256), dtype=torch.uint8, device=DEV)
+    weight = torch.full((B, 160), math.nan, device=DEV)
+    vkv.chunk_attend(ctx, pages, chunk, ws, SCALE, out, lse)
+    vkv.weight_accumulate(ctx, pages, chunk, lse, ww, SCALE, 0.9, None, weight)
+    want, tol = expected(x, lse, 0.9, None)
+    for b in range(B):
+        check("weights of the prompt", weight[b, :n0[b]], want[b], tol[b])
+    kept, count = torch.empty(B, K, dtype=torch.int32, device=DEV), torch.empty(B, dtype=torch.int32, device=DEV)
+    vkv.weight_select(ctx, weight, x.kv_len, 160, 4, 8, kept, count)
+    left = [x.rows(b)[kept[b].long()].clone() for b in range(B)]          # the rows that stay, as a set
+    for b in range(B):
+        assert kept[b].tolist() == expected_tier(weight[b], n0[b], K, 4, 8)
+    moved, origin = torch.empty(B, K, device=DEV), torch.empty(B, K, dtype=torch.int32, device=DEV)
+    vkv.cache_evict(ctx, pages, kept, count, origin, weight, moved)
+    x.kv_len.copy_(count)
+    weight[:, :K] = moved
+    g = torch.Generator(device=DEV)
+    g.manual_seed(5)
+    cu = torch.arange(B + 1, dtype=torch.int32, device=DEV)
+    for step in range(3):
+        new = torch.randn(B, 576, generator=g, device=DEV).to(torch.bfloat16)
+        q = torch.randn(B, H, 576, generator=g, device=DEV).to(torch.bfloat16)
+        u = x.kv_len.long()
+        at = x.table.long().gather(1, (u // page)[:, None])[:, 0]
+        x.cache[at, u % page] = new
+        x.kv_len += 1
+        one = vkv.Chunk(q[..., :512], q[..., 512:], cu, 1)
+        ws1 = torch.empty(max(vkv.chunk_workspace_size(pages, one), 256), dtype=torch.uint8, device=DEV)
+        o, l = torch.empty(B, H, 512, dtype=torch.bfloat16, device=DEV), torch.empty(B, H, device=DEV)
+        vkv.chunk_attend(ctx, pages, one, ws1, SCALE, o, l)
+        vkv.weight_accumulate(ctx, pages, one, l, None, SCALE, 0.9, weight, weight)
+        for b in range(B):
+            left[b] = torch.cat([left[b], new[b:b + 1]])
+            kv = left[b].cpu()
+            oo, ll, ot, lt = attention(q[b].cpu(), kv, kv[:, :512], torch.ones(H, kv.shape[0], dtype=torch.bool), SCALE)
+            check("decode lse", l[b], ll, lt), check("decode out", o[b], oo, ot)
+            assert bool(torch.isfinite(weight[b, :K + step + 1]).all())
+
+
+def test_tier_feeds_the_kept_step(ctx):
+    """The weight tier as a kept table of the decode step's gather-attend on a dense cache, and the same
+    tier moved to the front and attended whole: the same rows, the same result."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(2)
+    B, T, W, H, K = 2, 512, 64, 16, 100
+    cache = torch.randn(B, T, 576, generator=g, device=DEV).to(torch.bfloat16)
+    q = torch.randn(B, H, 576, generator=g, device=DEV).to(torch.bfloat16)
+    ql, qr = q[..., :512].contiguous(), q[..., 512:].contiguous()
+    A = T - W
+    weight = torch.rand(B, T, generator=g, device=DEV)
+    kept, count = torch.empty(B, K, dtype=torch.int32, device=DEV), torch.empty(B, dtype=torch.int32, device=DEV)
+    vkv.weight_select(ctx, weight, torch.full((B,), A, dtype=torch.int32, device=DEV), T, 4, 0, kept, count)
+    step = vkv.Step(cache, ql, qr, W, vkv.VKV_MODE_ROPE)
+    ws = vkv.alloc_workspace(step, K)
+    out, lse = torch.empty(B, H, 512, dtype=torch.bfloat16, device=DEV), torch.empty(B, H, device=DEV)
+    vkv.attend(ctx, step, ws, K, kept, None, None, 0, SCALE, out, lse)
+    tier = torch.cat([kept, torch.arange(A, T, dtype=torch.int32, device=DEV)[None].expand(B, W)], 1).contiguous()
+    full = torch.full((B,), T, dtype=torch.int32, device=DEV)
+    n = torch.full((B,), K + W, dtype=torch.int32, device=DEV)
+    moved = cache.clone()
+    vkv.cache_evict(ctx, vkv.Pages.of_cache(moved, full), tier, n)
+    pages = vkv.Pages.of_cache(moved, n)
+    chunk = vkv.Chunk(ql, qr, torch.arange(B + 1, dtype=torch.int32, device=DEV), 1)
+    w2 = torch.empty(vkv.chunk_workspace_size(pages, chunk), dtype=torch.uint8, device=DEV)
+    out2, lse2 = torch.empty_like(out), torch.empty_like(lse)
+    vkv.chunk_attend(ctx, pages, chunk, w2, SCALE, out2, lse2)
+    for b in range(B):
+        rows = cache[b, tier[b].long()].cpu()
+        o, l, ot, lt = attention(q[b].cpu(), rows, rows[:, :512], torch.ones(H, K + W, dtype=torch.bool), SCALE)
+        check("moved out", out2[b], o, ot), check("moved lse", lse2[b], l, lt)
+        check("gathered lse", lse[b], l, lt)
+
+
+def test_graph_of_the_whole_step(ctx):
+    """Attention, weights, tier and move captured together and replayed, against the eager calls."""
+    B, H, K = 2, 16, 64
+    x = Case([200, 333], [2, 1], H, page=16, seed=30, max_q=2, max_kv=400)
+    backup, lens = x.cache.clone(), x.kv_len.clone()
+    pages, chunk = vkv.Pages(x.cache, x.table, x.kv_len, 400), vkv.Chunk(x.q_lat, x.q_rope, x.cu, 2)
+    ws = torch.empty(max(vkv.chunk_workspace_size(pages, chunk), 256), dtype=torch.uint8, device=DEV)
+    ww = torch.empty(max(vkv.weight_workspace_size(pages, chunk), 256), dtype=torch.uint8, device=DEV)
+    prev = torch.rand(B, 400, device=DEV)
+
+    def buffers():
+        return dict(out=torch.zeros(x.n_tok, H, 512, dtype=torch.bfloat16, device=DEV), lse=torch.zeros(x.n_tok, H, device=DEV),
+                    weight=torch.zeros(B, 400, device=DEV), kept=torch.zeros(B, K, dtype=torch.int32, device=DEV),
+                    count=torch.zeros(B, dtype=torch.int32, device=DEV), origin=torch.zeros(B, K, dtype=torch.int32, device=DEV),
+                    moved=torch.zeros(B, K, device=DEV))
+
+    def step(t):
+        vkv.chunk_attend(ctx, pages, chunk, ws, SCALE, t["out"], t["lse"])
+        vkv.weight_accumulate(ctx, pages, chunk, t["lse"], ww, SCALE, 0.9, prev, t["weight"])
+        vkv.weight_select(ctx, t["weight"], x.kv_len, 400, 4, 8, t["kept"], t["count"])
+        vkv.cache_evict(ctx, pages, t["kept"], t["count"], t["origin"], t["weight"], t["moved"])
+
+    eager, held = buffers(), buffers()
+    step(eager)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step(held)
+    for rep in range(3):
+        gen = torch.Generator(device=DEV)
+        gen.manual_seed(rep)
+        x.q_lat.copy_(torch.randn(x.q_lat.shape, generator=gen, device=DEV).to(torch.bfloat16))
+        x.kv_len.copy_(lens - 10 * rep)
+        x.cache.copy_(backup)
+        g.replay()
+        torch.cuda.synchronize()
+        after = x.cache.clone()
+        (torch.randn(300, 300, device=DEV) @ torch.randn(300, 300, device=DEV)).sum().item()
+        x.cache.copy_(backup)
+        step(eager)
+        torch.cuda.synchronize()
+        assert torch.equal(after.view(torch.int16), x.cache.view(torch.int16))
+        for name in eager:
+            assert torch.equal(eager[name], held[name]), (rep, name)
