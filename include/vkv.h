@@ -535,8 +535,8 @@ int vkv_prompt_attend(vkv_ctx* ctx, const vkv_prompt* pr, float scale, uint16_t*
  *   kv_len  [B] int32 (device): rows of each sequence; values outside
  *           [0, max_kv] are taken as the nearest bound
  * page: a power of two in [1, 65536].  1 <= B <= 65535, 0 <= max_kv <= 2^30,
- * 1 <= n_pages < 2^31; strides multiples of 8, row_stride >= 576, cache
- * 16-byte aligned.  Rows on a page outside [0, n_pages) do not exist: they are
+ * 1 <= n_pages < 2^31; strides multiples of 8 and below 2^35, row_stride >= 576,
+ * cache 16-byte aligned.  Rows on a page outside [0, n_pages) do not exist: they are
  * not read, have no weight and are not written.
  */
 typedef struct vkv_pages {

@@ -15,9 +15,12 @@
 // and 2 (few rows: decode) they split into 8 / QG streams that take the tiles in
 // turn, each in its own LDS stages, and join at the end through LDS.
 //
-// Cache rows go to LDS by direct loads; their pages' table entries, too, several
-// tiles ahead (per wave, so that they need no barrier).  Stage layout: row-major,
-// piece p (16 B) of tile row r at slot 72 r + (p ^ (r & 7)).
+// Cache rows go to LDS by direct loads, a row's 512 latent dims by one instruction whose
+// address is scalar but for the lane; so are the table entries, a tile ahead.  (Row
+// addresses per lane took 1100 vector cycles of a wave and tile, half its time.)
+// Stage layout: [32 rows][512 dims], then [32 rows][64 dims], 16-byte pieces permuted
+// within a row by an XOR with a function of the row that spreads the operand reads over
+// the LDS banks.
 //
 // Work split: up to CK_MAX_UNITS units, the tiles of all units are laid end to end
 // and cut into equal runs, one per CU, however the lengths differ; a run that
@@ -33,17 +36,16 @@ namespace vkv {
 constexpr int CK_WAVES = 8;
 constexpr int CK_THREADS = 64 * CK_WAVES;
 constexpr int CK_TILE = 32;                              // cache rows of a tile
-constexpr int CK_PIECES = D_ROW / 8;                     // 72 pieces of 16 B per row
-constexpr int CK_ROW_BYTES = 2 * D_ROW;
-constexpr int CK_STAGE = CK_TILE * CK_ROW_BYTES;         // 36 KB
-constexpr int CK_LOADS = CK_STAGE / 1024;                // loads of 1 KB
+constexpr int CK_LAT_BYTES = 2 * D_LAT, CK_ROPE_BYTES = 2 * D_ROPE;
+constexpr int CK_OFF_ROPE = CK_TILE * CK_LAT_BYTES;
+constexpr int CK_STAGE = CK_TILE * 2 * D_ROW;            // 36 KB
 constexpr int CK_STAGES = 4;
-constexpr int CK_ENT = 8;                                // table entries of this many tiles per wave
 constexpr int CK_KS = D_ROW / 32, CK_DT = D_LAT / 16;
 constexpr float CK_SLACK = 8.0f;   // lag allowed to the softmax reference maximum (log2 units)
 constexpr float CK_ROOM = 0x1p-40f;   // careful passes and joins: a factor of the weights, so that no sum of finite values overflows
-constexpr int CK_ENT_BYTES = CK_TILE * 4;
-constexpr int CK_SMEM = CK_STAGES * CK_STAGE + CK_WAVES * CK_ENT * CK_ENT_BYTES;
+constexpr int CK_OFF_ML = CK_STAGES * CK_STAGE;          // (m, l) of the waves' rows
+constexpr int CK_OFF_GONE = CK_OFF_ML + CK_WAVES * 16 * 8;   // per stage and wave: which of its tile rows do not exist
+constexpr int CK_SMEM = CK_OFF_GONE + CK_STAGES * CK_WAVES * 4;
 
 // ------------------------------------------------------------ units and runs
 
@@ -81,9 +83,108 @@ __device__ __forceinline__ int run_count(const ChunkArgs& a, int total) {
 }
 __device__ __forceinline__ int run_start(int g, int n, int total) { return (int)((int64_t)g * total / n); }
 
+// ------------------------------------------------------------------ tiles
+
+// XOR of the piece index of tile row r.  LDS serves a 128-bit read sixteen lanes at a
+// time, lanes {0-3, 12-15, 20-23, 24-27} and {4-11, 16-19, 28-31} of each half wave, and a
+// 64-bit one a half wave at a time; each such group has to touch 16 pieces that differ
+// modulo 16 (64 banks).  Latent panel (rows 1 KB apart, so the XOR alone decides): the
+// transposing V reads of a half wave take rows 4 a .. 4 a + 3 of four adjacent pieces
+// (32x32 products), or of two pieces and the next four rows (16x16): the row within
+// the four chooses a block of four pieces, the four's number y(b) the place in it, with
+// y = 0, 2, 3, 1, which also keeps the K reads apart (a group has all of r mod 16 in
+// 32x32 products; b = 0, 3 of one piece and b = 1, 2 of its neighbour, or the reverse, in
+// 16x16 ones).  Branch panel (128 bytes a row: odd rows in the other half of the
+// banks): r / 2 mod 8.
+__device__ __forceinline__ int lat_xor(int r) {
+    const int b = r >> 2;
+    return ((r & 3) << 2) | (((b ^ (b >> 1)) & 1) << 1) | ((b >> 1) & 1);
+}
+__device__ __forceinline__ int rope_xor(int r) { return (r >> 1) & 7; }
+
+typedef __attribute__((address_space(4))) const int32_t const_i32_t;
+
+// One wave's share of the tiles of a stream of WPT waves: NR rows of each.
+template <int WPT>
+struct TileLoader {
+    static constexpr int NR = CK_TILE / WPT;
+    static constexpr int LOADS = NR + (NR + 7) / 8;
+    const ChunkArgs& a;
+    const_i32_t* table;
+    int kv, wt, lane;       // rows of the sequence, wave of the stream, lane
+    int32_t e[NR];          // the fetched tile's table entries (scalar)
+
+    __device__ __forceinline__ int row(int t, int i) const { return min(CK_TILE * t + NR * wt + i, kv - 1); }
+    // rows past the end: the last row's
+    __device__ __forceinline__ void fetch(int t) {
+        e[0] = table[row(t, 0) >> a.shift];
+        if (a.page_mask < NR - 1)
+#pragma unroll
+            for (int i = 1; i < NR; ++i) e[i] = table[row(t, i) >> a.shift];
+    }
+    // the loads of the fetched tile t into stage st; gone: where its rows that do not exist are noted
+    __device__ __forceinline__ void issue(int t, uint8_t* st, uint32_t gone) const {
+        const char* base[NR];
+        uint32_t none = 0;
+        // on a page that does not exist: the first rows of the cache in place of its own, masked later
+        const bool whole = a.page_mask >= NR - 1;   // the rows lie on one page
+        if (whole) {
+            const int u = row(t, 0), last = min(kv - 1 - u, NR - 1);
+            const bool there = (uint32_t)e[0] < (uint32_t)a.n_pages;
+            const uint64_t at = (uint64_t)(uint32_t)(there ? e[0] : 0) * a.ps16 + (uint64_t)(uint32_t)(there ? u & a.page_mask : 0) * a.rs16;
+            base[0] = reinterpret_cast<const char*>(a.cache) + 16 * at;
+#pragma unroll
+            for (int i = 1; i < NR; ++i) base[i] = base[i - 1] + (i <= last ? 16 * (uint64_t)a.rs16 : 0);
+            none = there ? 0u : (1u << NR) - 1u;
+        } else {
+#pragma unroll
+            for (int i = 0; i < NR; ++i) {
+                const bool there = (uint32_t)e[i] < (uint32_t)a.n_pages;
+                const uint64_t at = (uint64_t)(uint32_t)(there ? e[i] : 0) * a.ps16 +
+                                    (uint64_t)(uint32_t)(there ? row(t, i) & a.page_mask : 0) * a.rs16;
+                base[i] = reinterpret_cast<const char*>(a.cache) + 16 * at;
+                none |= there ? 0u : 1u << i;
+            }
+        }
+        int ln = lane;
+        asm volatile("" : "+v"(ln));   // keeps the lane arithmetic out of registers across the loop
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            const int r = NR * wt + i;
+            const uint32_t off = (uint32_t)(16 * ln) ^ (uint32_t)(16 * lat_xor(r));
+            __builtin_amdgcn_global_load_lds((gbl_void_t*)(base[i] + off), (lds_void_t*)(st + CK_LAT_BYTES * r), 16, 0, 0);
+        }
+#pragma unroll
+        for (int j = 0; j < NR; j += 8) {      // eight rows, eight lanes each
+            const char* b = base[j];
+#pragma unroll
+            for (int i = 1; i < (NR < 8 ? NR : 8); ++i) b = (ln >> 3) == i ? base[j + i] : b;
+            const int r = NR * wt + j + (ln >> 3);
+            if (NR >= 8 || ln < 8 * NR)
+                __builtin_amdgcn_global_load_lds((gbl_void_t*)(b + CK_LAT_BYTES + 16 * ((ln & 7) ^ rope_xor(r))),
+                                                 (lds_void_t*)(st + CK_OFF_ROPE + CK_ROPE_BYTES * (NR * wt + j)), 16, 0, 0);
+        }
+        asm volatile("ds_write_b32 %0, %1" ::"v"(gone + 4 * wt), "v"(none) : "memory");
+    }
+    // where this lane reads the notes of a tile, and the mask they make (bit r: tile row r does not exist)
+    __device__ __forceinline__ static uint32_t note(uint32_t gone, int ln) { return gone + 4 * (ln % WPT); }
+    __device__ __forceinline__ static uint32_t absent(uint32_t w) {
+        uint32_t all = 0;
+        if (__ballot(w != 0))
+#pragma unroll
+            for (int i = 0; i < WPT; ++i) all |= (uint32_t)__builtin_amdgcn_readlane(w, i) << (NR * i);
+        return all;
+    }
+};
+
 // ------------------------------------------------------------------ a segment
 
 typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+
+// natural-log lse from the reference (log2 units) and the sum; nothing seen: -inf
+__device__ __forceinline__ float lse_of(float m, float l) {
+    return m == -INFINITY && l == 0.f ? -INFINITY : ((m == -INFINITY ? 0.f : m) + log2f(l)) * 0.69314718055994530942f;
+}
 
 // this lane's dims 16 dt + 4 g .. +3 of output row `row` from f times what o holds, and
 // its lse; rows that see nothing: 0, -inf
@@ -98,7 +199,7 @@ __device__ __forceinline__ void store_row(const ChunkArgs& a, int64_t row, int g
                             (__bf16)(o[dt][3] * inv)};
         *reinterpret_cast<bf16x4_t*>(out + 16 * dt) = v;
     }
-    if (g == 0) a.lse[row] = none ? -INFINITY : ((m == -INFINITY ? 0.f : m) + log2f(l)) * 0.69314718055994530942f;
+    if (g == 0) a.lse[row] = lse_of(m, l);
 }
 
 // Tiles [t0, t1) of unit x by one workgroup.  part: where an incomplete unit's
@@ -112,9 +213,8 @@ template <int QG, bool SAFE>
 __device__ __forceinline__ bool chunk_segment(const ChunkArgs& a, const CkUnit& x, int t0, int t1, float* part_o,
                                               float* part_ml, uint8_t* smem) {
     constexpr int KSTR = CK_WAVES / QG;          // streams of tiles
-    constexpr int PD = CK_STAGES / KSTR - 1;     // tiles loaded ahead: 3, 1, 0
-    constexpr int NL = (CK_LOADS + QG - 1) / QG; // loads of a tile per wave, at most
-    constexpr int NL_MIN = CK_LOADS / QG;        // and at least
+    constexpr int PD = CK_STAGES / KSTR - 1;     // tiles loaded ahead: 1, 0
+    static_assert(PD == 0 || PD == 1, "what the waits below assume");
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int qg = wave % QG, ks0 = wave / QG;
@@ -127,61 +227,18 @@ __device__ __forceinline__ bool chunk_segment(const ChunkArgs& a, const CkUnit& 
     const int nt = x.kv > 0 ? t1 - t0 : 0;
     const int nit = (nt + KSTR - 1) / KSTR;                     // tiles of each stream, the last ones perhaps past t1
 
-    const int32_t* table = a.table + (int64_t)x.b * a.tstride;
-    uint8_t* ents = smem + CK_STAGES * CK_STAGE + wave * (CK_ENT * CK_ENT_BYTES);
-    const uint32_t ents_lds = lds_addr(ents);
+    const uint32_t lds0 = lds_addr(smem);
+    TileLoader<QG> loader{a, (const_i32_t*)(a.table + (int64_t)x.b * a.tstride), x.kv, qg, lane, {}};
     auto tile_of = [&](int k) { return t0 + ks0 + KSTR * k; };
-    auto stage_of = [&](int k) { return (ks0 * (PD + 1) + k % (PD + 1)) * CK_STAGE; };
-    // table entries of the stream's tile k, one per tile row (rows past the end: of the last row)
-    auto issue_ent = [&](int k) {
-        const int u = min(CK_TILE * tile_of(k) + lane, x.kv - 1);
-        if (lane < CK_TILE)
-            __builtin_amdgcn_global_load_lds((gbl_void_t*)(table + (u >> a.shift)),
-                                             (lds_void_t*)(ents + (k % CK_ENT) * CK_ENT_BYTES), 4, 0, 0);
+    auto stage_of = [&](int k) { return ks0 * (PD + 1) + k % (PD + 1); };
+    auto gone_of = [&](int k) { return lds0 + CK_OFF_GONE + stage_of(k) * (CK_WAVES * 4); };
+    auto issue = [&](int k) {   // tile k of the stream, and the table entries of the next one
+        loader.issue(tile_of(k), smem + stage_of(k) * CK_STAGE, gone_of(k));
+        loader.fetch(tile_of(k + 1));
     };
-    // this wave's loads of the stream's tile k: slots 64 j .. 64 j + 63, j = qg + QG i
-    auto issue = [&](int k) {
-        const int t = tile_of(k);
-        uint8_t* st = smem + stage_of(k);
-        const uint32_t ent0 = ents_lds + (k % CK_ENT) * CK_ENT_BYTES;
-        int ln = lane;
-        asm volatile("" : "+v"(ln));   // keeps the slot arithmetic out of registers across the loop
-        constexpr int BATCH = NL < 9 ? NL : 9;
-#pragma unroll
-        for (int i0 = 0; i0 < NL; i0 += BATCH) {
-            int32_t e[BATCH];
-#pragma unroll
-            for (int i = 0; i < BATCH; ++i) {
-                const int r = min((64 * (qg + QG * (i0 + i)) + ln) / CK_PIECES, CK_TILE - 1);
-                asm volatile("ds_read_b32 %0, %1" : "=v"(e[i]) : "v"(ent0 + 4 * r));
-            }
-            if constexpr (BATCH == 9)
-                asm volatile("s_waitcnt lgkmcnt(0)"
-                             : "+v"(e[0]), "+v"(e[1]), "+v"(e[2]), "+v"(e[3]), "+v"(e[4]), "+v"(e[5]), "+v"(e[6]), "+v"(e[7]), "+v"(e[8]));
-            else
-                asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(e[0]), "+v"(e[1]), "+v"(e[2]), "+v"(e[3]), "+v"(e[4]));
-            static_assert(BATCH == 9 || BATCH == 5, "entries tied above");
-#pragma unroll
-            for (int i = 0; i < BATCH; ++i) {
-                const int j = qg + QG * (i0 + i);
-                const int q = 64 * j + ln, r = q / CK_PIECES;
-                const int u = min(CK_TILE * t + r, x.kv - 1);
-                // a page that does not exist: any row of the cache in its place, masked below
-                const bool there = (uint32_t)e[i] < (uint32_t)a.n_pages;
-                const int64_t at = there ? (int64_t)e[i] * a.ps + (int64_t)(u & a.page_mask) * a.rs : 0;
-                const uint16_t* src = a.cache + at + 8 * ((q - CK_PIECES * r) ^ (r & 7));
-                if (j < CK_LOADS)
-                    __builtin_amdgcn_global_load_lds((gbl_void_t*)src, (lds_void_t*)(st + 1024 * j), 16, 0, 0);
-            }
-        }
-    };
-
     if (nt > 0) {
-        for (int k = 0; k < max(2 * PD, 1); ++k) issue_ent(k);
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        if (PD == 0) issue_ent(1);
-        for (int k = 0; k < max(PD, 1); ++k)
-            if (k < nit) issue(k);
+        loader.fetch(tile_of(0));
+        issue(0);
     }
 
     // Q^T operand: row R, dims 32 ks + 8 g .. +8
@@ -197,18 +254,14 @@ __device__ __forceinline__ bool chunk_segment(const ChunkArgs& a, const CkUnit& 
         for (int ks = 0; ks < CK_KS; ++ks) asm volatile("" : "+v"(qf[ks]));   // no wait for them inside the tile loop
     }
 
-    // K operand of (row 16 mt + c, piece 4 ks + g), the piece's low three bits permuted; V operand
+    // K operand of (row 16 mt + c, piece 4 ks + g), the piece's low bits permuted; V operand
     // (transposing reads): lane 4 e + q of 16-lane group g reads rows 4 g + e and 16 + 4 g + e,
     // dims 16 dt + 4 q .. +3, i.e. piece 2 dt + q / 2, half q mod 2
-    const uint32_t lds0 = lds_addr(smem);
-    uint32_t kaddr[2], vaddr[4];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) kaddr[i] = c * CK_ROW_BYTES + 16 * ((4 * i + g) ^ (c & 7));
-    {
-        const int e = c >> 2, q = c & 3, row = 4 * g + e;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) vaddr[i] = row * CK_ROW_BYTES + 16 * ((2 * i + (q >> 1)) ^ (row & 7)) + 8 * (q & 1);
-    }
+    // (k-steps and dim blocks only flip bits of the permuted piece)
+    const int vrow = 4 * g + (c >> 2);
+    const uint32_t kaddr = c * CK_LAT_BYTES + 16 * (g ^ lat_xor(c));
+    const uint32_t raddr = CK_OFF_ROPE + c * CK_ROPE_BYTES + 16 * (g ^ rope_xor(c));
+    const uint32_t vaddr = vrow * CK_LAT_BYTES + 16 * (((c & 3) >> 1) ^ lat_xor(vrow)) + 8 * (c & 1);
 
     f32x4_t o[CK_DT];
 #pragma unroll
@@ -216,35 +269,35 @@ __device__ __forceinline__ bool chunk_segment(const ChunkArgs& a, const CkUnit& 
     float m_run = -INFINITY, l_run = 0.f;
 
     for (int k = 0; k < nit; ++k) {
-        // tile k has landed: at most the loads of the PD - 1 tiles behind it (and the table
-        // entries issued with them) are still in flight
-        if (PD > 1 && k + PD - 1 < nit)
-            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(PD > 1 ? (PD - 1) * (NL_MIN + 1) : 0) : "memory");
-        else
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        wg_barrier();   // every wave's share has, and the stage loaded next is free
-        if (PD > 0 && k + PD < nit) {
-            issue_ent(k + 2 * PD);
-            issue(k + PD);
-        }
+        // this wave's share of tile k has landed (nothing else is in flight), and every wave's;
+        // the stage loaded next is free
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        wg_barrier();
+        if (PD > 0 && k + PD < nit) issue(k + PD);
         const int t = tile_of(k), u0 = CK_TILE * t;
         if (t < t1 && !idle && u0 <= lim_hi) {
-            const uint32_t st = lds0 + stage_of(k);
-            int32_t ent;
-            asm volatile("ds_read_b32 %0, %1\n\ts_waitcnt lgkmcnt(0)"
-                         : "=&v"(ent)
-                         : "v"(ents_lds + (k % CK_ENT) * CK_ENT_BYTES + 4 * (lane & 31)));
-            const uint32_t absent = (uint32_t)__ballot((uint32_t)ent >= (uint32_t)a.n_pages);   // tile rows on no page
+            const uint32_t st = lds0 + stage_of(k) * CK_STAGE;
+            uint32_t note;
+            asm volatile("ds_read_b32 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(note) : "v"(loader.note(gone_of(k), lane)) : "memory");
+            const uint32_t absent = loader.absent(note);   // tile rows on no page
             const bool masked = u0 + CK_TILE - 1 > lim_lo || absent != 0;
             f32x4_t s[2] = {f32x4_t{0.f, 0.f, 0.f, 0.f}, f32x4_t{0.f, 0.f, 0.f, 0.f}};
             {
                 constexpr int SD = 3;   // operands read ahead of the matrix cores
                 bf16x8_t kf[SD + 1][2];
-                const uint32_t ka[2] = {st + kaddr[0], st + kaddr[1]};
+                uint32_t ka[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) ka[i] = st + (kaddr ^ (64 * i));
+                const uint32_t ra[2] = {st + raddr, st + (raddr ^ 64)};
                 auto kload = [&](auto kc) {
                     constexpr int ks = decltype(kc)::value;
-                    kf[ks % (SD + 1)][0] = lds_read128<128 * (ks >> 1)>(ka[ks & 1]);
-                    kf[ks % (SD + 1)][1] = lds_read128<128 * (ks >> 1) + 16 * CK_ROW_BYTES>(ka[ks & 1]);
+                    if constexpr (ks < D_LAT / 32) {
+                        kf[ks % (SD + 1)][0] = lds_read128<256 * (ks >> 2)>(ka[ks & 3]);
+                        kf[ks % (SD + 1)][1] = lds_read128<256 * (ks >> 2) + 16 * CK_LAT_BYTES>(ka[ks & 3]);
+                    } else {
+                        kf[ks % (SD + 1)][0] = lds_read128<0>(ra[ks & 1]);
+                        kf[ks % (SD + 1)][1] = lds_read128<16 * CK_ROPE_BYTES>(ra[ks & 1]);
+                    }
                 };
                 static_for<0, SD>(kload);
                 static_for<0, CK_KS>([&](auto kc) {
@@ -295,9 +348,6 @@ __device__ __forceinline__ bool chunk_segment(const ChunkArgs& a, const CkUnit& 
             }
             // the softmax's cross-lane reads complete before the V reads are issued
             asm volatile("" : "+v"(l_run), "+v"(pf));
-            uint32_t va[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) va[i] = st + vaddr[i];
             if (SAFE && masked) {
                 bf16x8_t seen;
 #pragma unroll
@@ -307,8 +357,8 @@ __device__ __forceinline__ bool chunk_segment(const ChunkArgs& a, const CkUnit& 
                 }
 #pragma unroll
                 for (int dt = 0; dt < CK_DT; ++dt) {
-                    i16x4_t lo = lds_read_tr16<0>(va[dt & 3] + 128 * (dt >> 2));
-                    i16x4_t hi = lds_read_tr16<16 * CK_ROW_BYTES>(va[dt & 3] + 128 * (dt >> 2));
+                    const uint32_t va = st + (vaddr ^ (32 * (dt & 7))) + 256 * (dt >> 3);
+                    i16x4_t lo = lds_read_tr16<0>(va), hi = lds_read_tr16<16 * CK_LAT_BYTES>(va);
                     lds_wait<0>(lo, hi);
                     bf16x8_t v = join(lo, hi);
                     const bf16x8_t code = split_nonfinite(v);
@@ -319,37 +369,38 @@ __device__ __forceinline__ bool chunk_segment(const ChunkArgs& a, const CkUnit& 
                     for (int i = 0; i < 4; ++i) o[dt][i] = add_nonfinite(o[dt][i], codes[i]);
                 }
             } else {
+                // dim blocks in the order dt = e + 8 f, f inner: one address per e
                 constexpr int VD = 4;
                 i16x4_t vv[VD + 1][2];
+                uint32_t va;
                 auto vload = [&](auto ic) {
-                    constexpr int dt = decltype(ic)::value;
-                    vv[dt % (VD + 1)][0] = lds_read_tr16<128 * (dt >> 2)>(va[dt & 3]);
-                    vv[dt % (VD + 1)][1] = lds_read_tr16<128 * (dt >> 2) + 16 * CK_ROW_BYTES>(va[dt & 3]);
+                    constexpr int i = decltype(ic)::value;
+                    if constexpr ((i & 3) == 0) va = st + (vaddr ^ (32 * (i >> 2)));
+                    vv[i % (VD + 1)][0] = lds_read_tr16<256 * (i & 3)>(va);
+                    vv[i % (VD + 1)][1] = lds_read_tr16<256 * (i & 3) + 16 * CK_LAT_BYTES>(va);
                 };
                 static_for<0, VD>(vload);
                 static_for<0, CK_DT>([&](auto ic) {
-                    constexpr int dt = decltype(ic)::value;
-                    if constexpr (dt + VD < CK_DT) vload(std::integral_constant<int, dt + VD>{});
-                    lds_wait<2 * ((dt + VD < CK_DT) ? VD : (CK_DT - 1 - dt))>(vv[dt % (VD + 1)][0], vv[dt % (VD + 1)][1]);
-                    o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(join(vv[dt % (VD + 1)][0], vv[dt % (VD + 1)][1]), pf, o[dt],
+                    constexpr int i = decltype(ic)::value, dt = (i >> 2) + 8 * (i & 3);
+                    if constexpr (i + VD < CK_DT) vload(std::integral_constant<int, i + VD>{});
+                    lds_wait<2 * ((i + VD < CK_DT) ? VD : (CK_DT - 1 - i))>(vv[i % (VD + 1)][0], vv[i % (VD + 1)][1]);
+                    o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(join(vv[i % (VD + 1)][0], vv[i % (VD + 1)][1]), pf, o[dt],
                                                                     0, 0, 0);
                 });
             }
         }
         if (PD == 0 && k + 1 < nit) {   // the stream's waves are done with its only stage
             wg_barrier();
-            issue_ent(k + 2);
             issue(k + 1);
         }
     }
     l_run = allreduce_groups(l_run, [](float p, float q) { return p + q; });
 
     // ---- the streams of a row join in the first one's wave, through the stages
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // table entries issued past the end have landed
     __syncthreads();
     float* fl = reinterpret_cast<float*>(smem);
     if constexpr (KSTR > 1) {
-        float* sml = fl + CK_STAGES * CK_STAGE / 4;   // the table entries' place: (m, l) of every wave's rows
+        float* sml = fl + CK_OFF_ML / 4;
         if (g == 0) {
             sml[2 * (16 * wave + c)] = m_run;
             sml[2 * (16 * wave + c) + 1] = l_run;
@@ -427,12 +478,300 @@ __device__ __forceinline__ bool chunk_segment(const ChunkArgs& a, const CkUnit& 
     return false;
 }
 
-// a call, so that the rare segment's registers are not the ordinary one's; by value, so
-// that nothing of the ordinary one has an address
-template <int QG>
-__device__ __attribute__((noinline)) void chunk_segment_again(ChunkArgs a, int u, int t0, int t1, float* part_o,
-                                                              float* part_ml, uint8_t* smem) {
-    (void)chunk_segment<QG, true>(a, chunk_unit(a, u, 16 * QG), t0, t1, part_o, part_ml, smem);
+// ------------------------------------------------- a segment of 128 rows
+//
+// With 64 rows and more the LDS reads of operands bound the segment above, in which a
+// wave reads every tile twice for 16 rows (557 KB a tile).  Here a wave has 32 rows,
+// shared with one other wave: each takes half of the 576 dims of S^T = K Q^T and half of
+// the 512 dims of O^T = V^T P^T, and the two exchange their halves of the sum S^T through LDS
+// (378 KB a tile, with the loads themselves).  Both then have all of S, the same softmax, and P in
+// registers as before (32x32x16 products).
+//
+// The waves form two groups (0-3 and 4-7, one of each on a SIMD) half a tile apart:
+// while one multiplies by K, the other does the softmax and multiplies by V, so that a
+// SIMD's vector and matrix instructions run beside each other.  Half-step h: group
+// e works on tile (h - e) / 2, on S where h - e is even, on P and O where it is odd.
+// Three tile stages: tile n is loaded from half-step 2 n - 3 on and first read at 2 n.
+
+constexpr int WD_STAGES = 3;
+constexpr int WD_KS = CK_KS, WD_DT = D_LAT / 64;   // 18 products of 16 dims, 8 blocks of 32 dims a wave
+constexpr int WD_XCH = 4096;                       // bytes of a wave's half sums
+constexpr int WD_OFF_XCH = WD_STAGES * CK_STAGE, WD_OFF_GONE = WD_OFF_XCH + CK_WAVES * WD_XCH;
+static_assert(WD_OFF_GONE + WD_STAGES * CK_WAVES * 4 <= CK_SMEM, "the wide segment's LDS");
+
+template <bool SAFE>
+__device__ __forceinline__ bool wide_segment(const ChunkArgs& a, const CkUnit& x, int t0, int t1, float* part_o,
+                                             float* part_ml, uint8_t* smem) {
+    const int tid = threadIdx.x, lane = tid & 63, c = lane & 31, hh = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int grp = wave >> 2, ch = wave & 1, rb = wave >> 1;   // group, half of the dims, block of 32 rows
+    const int R = x.row0 + 32 * rb + c;                         // this lane's row
+    const int Rc = min(R, x.nrow - 1);                          // rows past the end repeat the last one, never stored
+    const int lim = min(x.kv - x.nq + Rc / a.H, x.kv - 1);      // the last cache row it sees
+    const int lim_lo = __builtin_amdgcn_readfirstlane(lim);     // of the wave's rows
+    const bool idle = x.row0 + 32 * rb >= x.nrow;
+    const int nt = x.kv > 0 ? t1 - t0 : 0;
+
+    const uint32_t lds0 = lds_addr(smem);
+    TileLoader<CK_WAVES> loader{a, (const_i32_t*)(a.table + (int64_t)x.b * a.tstride), x.kv, wave, lane, {}};
+    auto gone_of = [&](int k) { return lds0 + WD_OFF_GONE + (k % WD_STAGES) * (CK_WAVES * 4); };
+    auto issue = [&](int k) {   // tile t0 + k, and the table entries of the next one
+        loader.issue(t0 + k, smem + (k % WD_STAGES) * CK_STAGE, gone_of(k));
+        loader.fetch(t0 + k + 1);
+    };
+    if (nt > 0) {
+        loader.fetch(t0);
+        issue(0);
+        if (nt > 1) issue(1);
+    }
+
+    // Q^T operand: row R, k-step j: latent dims 256 ch + 16 j + 8 hh .. +8 (j < 16), then branch dims
+    // 32 ch + 16 (j - 16) + 8 hh .. +8
+    bf16x8_t qf[WD_KS];
+    {
+        const int64_t row = x.tok0 * a.H + Rc;
+        const uint16_t* ql = a.q_lat + row * a.qls + 8 * hh;
+        const uint16_t* qr = a.q_rope + row * a.qrs + 8 * hh;
+#pragma unroll
+        for (int j = 0; j < WD_KS; ++j) {
+            qf[j] = *reinterpret_cast<const bf16x8_t*>(j < 16 ? ql + D_LAT / 2 * ch + 16 * j : qr + D_ROPE / 2 * ch + 16 * (j - 16));
+        }
+#pragma unroll
+        for (int j = 0; j < WD_KS; ++j) asm volatile("" : "+v"(qf[j]));   // no wait for them inside the loop
+    }
+
+    // Operand and exchange addresses are recomputed from an opaque copy of the lane index, so
+    // that no registers hold them across the loop.
+    auto opaque_lane = [&]() {
+        int ln = lane;
+        asm volatile("" : "+v"(ln));
+        return ln;
+    };
+
+    f32x16_t o[WD_DT], s;
+#pragma unroll
+    for (int dt = 0; dt < WD_DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
+    float m_run = -INFINITY, l_run = 0.f;
+
+    // the beginning of half-step h
+    auto half_step = [&](int h) {
+        // before an even one tile h / 2 has landed: at most the next tile's loads are still in flight
+        if ((h & 1) == 0) {
+            if (h / 2 + 1 < nt)
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(loader.LOADS) : "memory");
+            else
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        }
+        wg_barrier();   // every wave's loads have, the half sums of the last half-step are written, its stage is free
+        if ((h & 1) == 1 && (h + 3) / 2 < nt) issue((h + 3) / 2);
+    };
+    // Rows past the end and tiles that none of a wave's rows sees are computed like the others (no
+    // branches around the products), and masked.
+    if (nt > 0 && grp == 1) half_step(0);
+    for (int k = 0; k < nt; ++k) {
+        half_step(2 * k + grp);
+        const int u0 = CK_TILE * (t0 + k);
+        const uint32_t st = lds0 + (k % WD_STAGES) * CK_STAGE;
+        {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = 0.f;
+            constexpr int SD = 2;   // operands read ahead of the matrix cores
+            bf16x8_t kf[SD + 1];
+            // K operand of row c: latent piece 32 ch + 2 j + hh, branch piece 4 ch + 2 (j - 16) + hh, permuted
+            const int ln = opaque_lane(), r = ln & 31;
+            const uint32_t kaddr = r * CK_LAT_BYTES + 16 * ((ln >> 5) ^ lat_xor(r));
+            const uint32_t raddr = st + CK_OFF_ROPE + r * CK_ROPE_BYTES + 16 * (((ln >> 5) + 4 * ch) ^ rope_xor(r));
+            auto kload = [&](auto jc) {
+                constexpr int j = decltype(jc)::value;
+                if constexpr (j < 16)
+                    kf[j % (SD + 1)] = lds_read128<256 * (j >> 3)>((kaddr ^ (32 * (j & 7))) + (st + 512 * ch));
+                else
+                    kf[j % (SD + 1)] = lds_read128<0>(raddr ^ (32 * (j - 16)));
+            };
+            static_for<0, SD>(kload);
+            static_for<0, WD_KS>([&](auto jc) {
+                constexpr int j = decltype(jc)::value;
+                if constexpr (j + SD < WD_KS) kload(std::integral_constant<int, j + SD>{});
+                lds_wait<(j + SD < WD_KS) ? SD : (WD_KS - 1 - j)>(kf[j % (SD + 1)]);
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[j % (SD + 1)], qf[j], s, 0, 0, 0);
+            });
+            // this half of the sum to the other wave (the matrix results are read by explicit
+            // instructions, so the wait for the last product, at least 18 wait states, is explicit too)
+            asm volatile("s_nop 15\n\ts_nop 7" : "+v"(s));
+            const f32x4_t s0 = {s[0], s[1], s[2], s[3]}, s1 = {s[4], s[5], s[6], s[7]};
+            const f32x4_t s2 = {s[8], s[9], s[10], s[11]}, s3 = {s[12], s[13], s[14], s[15]};
+            asm volatile("ds_write_b128 %0, %1\n\tds_write_b128 %0, %2 offset:1024\n\tds_write_b128 %0, %3 offset:2048\n\t"
+                         "ds_write_b128 %0, %4 offset:3072\n\ts_waitcnt lgkmcnt(0)" ::"v"(lds0 + WD_OFF_XCH + wave * WD_XCH + 16 * ln),
+                         "v"(s0), "v"(s1), "v"(s2), "v"(s3)
+                         : "memory");
+        }
+        half_step(2 * k + grp + 1);
+        const int ln = opaque_lane();
+        uint32_t note;
+        {
+            f32x4_t y[4];
+            asm volatile("ds_read_b32 %4, %6\n\tds_read_b128 %0, %5\n\tds_read_b128 %1, %5 offset:1024\n\t"
+                         "ds_read_b128 %2, %5 offset:2048\n\tds_read_b128 %3, %5 offset:3072\n\ts_waitcnt lgkmcnt(0)"
+                         : "=&v"(y[0]), "=&v"(y[1]), "=&v"(y[2]), "=&v"(y[3]), "=&v"(note)
+                         : "v"(lds0 + WD_OFF_XCH + (wave ^ 1) * WD_XCH + 16 * ln), "v"(loader.note(gone_of(k), ln))
+                         : "memory");
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] += y[i >> 2][i & 3];
+        }
+        const uint32_t absent = loader.absent(note);   // tile rows on no page
+        const bool masked = u0 + CK_TILE - 1 > lim_lo || absent != 0;
+        // s[i] = score of tile row 8 (i / 4) + 4 hh + i % 4 for row R
+        if (masked) {
+            const int last = lim - u0 - 4 * hh;
+            const uint32_t gone = absent >> (4 * hh);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int r = 8 * (i >> 2) + (i & 3);
+                if (r > last || ((gone >> r) & 1u)) s[i] = -INFINITY;
+            }
+        }
+        float cmax = s[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) cmax = fmaxf(cmax, s[i]);
+        cmax = half_max(cmax) * a.scale_log2;
+        const bool move = cmax > m_run + CK_SLACK;
+        const float alpha = move ? __builtin_amdgcn_exp2f(m_run - cmax) : 1.0f;
+        if (move) m_run = cmax;
+        const float ref = m_run == -INFINITY ? 0.f : m_run;   // nothing but masked scores so far
+        bf16x8_t pf[2];
+        float psum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.scale_log2, -ref));
+            psum += p;
+            pf[i >> 3][i & 7] = (__bf16)(SAFE ? p * CK_ROOM : p);
+        }
+        l_run = l_run * alpha + psum;   // this lane's share of the sum
+        if (__ballot(move)) {
+#pragma unroll
+            for (int dt = 0; dt < WD_DT; ++dt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[dt][i] *= alpha;
+        }
+        // the softmax's cross-lane reads complete before the V reads are issued
+        asm volatile("" : "+v"(l_run), "+v"(pf[0]), "+v"(pf[1]));
+        // V operand (transposing reads): lane 4 e + q of a 16-lane group reads row 16 s + 8 u + 4 hh + e,
+        // dims 256 ch + 32 dt + 16 gi + 4 q .. +3, i.e. piece 32 ch + 4 dt + 2 gi + q / 2; 8 rows on, the
+        // permutation differs by 3 (y(b + 2) = y(b) ^ 3)
+        const int vrow = 4 * (ln >> 5) + ((ln >> 2) & 3);
+        const uint32_t vaddr = vrow * CK_LAT_BYTES + 16 * ((2 * ((ln >> 4) & 1) + ((ln >> 1) & 1)) ^ lat_xor(vrow)) + 8 * (ln & 1);
+        const uint32_t vst = st + 512 * ch;
+        if (SAFE && masked) {
+            bf16x8_t seen[2];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int r = 8 * (i >> 2) + 4 * hh + (i & 3);
+                seen[i >> 3][i & 7] = (u0 + r <= lim && !((absent >> r) & 1u)) ? (__bf16)1.0f : (__bf16)0.0f;
+            }
+#pragma unroll
+            for (int dt = 0; dt < WD_DT; ++dt) {
+                f32x16_t codes;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) codes[i] = 0.f;
+#pragma unroll
+                for (int s2 = 0; s2 < 2; ++s2) {
+                    const uint32_t at = vst + 256 * (dt >> 2) + 16 * CK_LAT_BYTES * s2;
+                    i16x4_t lo = lds_read_tr16<0>(at + (vaddr ^ (64 * (dt & 3))));
+                    i16x4_t hi = lds_read_tr16<8 * CK_LAT_BYTES>(at + (vaddr ^ (64 * (dt & 3) + 48)));
+                    lds_wait<0>(lo, hi);
+                    bf16x8_t v = join(lo, hi);
+                    const bf16x8_t code = split_nonfinite(v);
+                    o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pf[s2], o[dt], 0, 0, 0);
+                    codes = __builtin_amdgcn_mfma_f32_32x32x16_bf16(code, seen[s2], codes, 0, 0, 0);
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[dt][i] = add_nonfinite(o[dt][i], codes[i]);
+            }
+        } else {
+            // products in the order dt = e + 4 f, (f, s) inner: two addresses per e
+            constexpr int VD = 4, N = 2 * WD_DT;
+            i16x4_t vv[VD + 1][2];
+            uint32_t va[2];
+            auto vload = [&](auto ic) {
+                constexpr int i = decltype(ic)::value, f = (i >> 1) & 1, s2 = i & 1;
+                if constexpr ((i & 3) == 0) {
+                    va[0] = vst + (vaddr ^ (64 * (i >> 2)));
+                    va[1] = vst + (vaddr ^ (64 * (i >> 2) + 48));
+                }
+                vv[i % (VD + 1)][0] = lds_read_tr16<256 * f + 16 * CK_LAT_BYTES * s2>(va[0]);
+                vv[i % (VD + 1)][1] = lds_read_tr16<256 * f + 16 * CK_LAT_BYTES * s2 + 8 * CK_LAT_BYTES>(va[1]);
+            };
+            static_for<0, VD>(vload);
+            static_for<0, N>([&](auto ic) {
+                constexpr int i = decltype(ic)::value, dt = (i >> 2) + 4 * ((i >> 1) & 1), s2 = i & 1;
+                if constexpr (i + VD < N) vload(std::integral_constant<int, i + VD>{});
+                lds_wait<2 * ((i + VD < N) ? VD : (N - 1 - i))>(vv[i % (VD + 1)][0], vv[i % (VD + 1)][1]);
+                o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(join(vv[i % (VD + 1)][0], vv[i % (VD + 1)][1]), pf[s2], o[dt],
+                                                                0, 0, 0);
+            });
+        }
+    }
+    if (nt > 0 && grp == 0) half_step(2 * nt);
+    l_run = half_sum(l_run);
+
+    __syncthreads();
+    if constexpr (!SAFE) {
+        float top = 0.f;
+        if (!idle)
+#pragma unroll
+            for (int dt = 0; dt < WD_DT; ++dt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) top += fabsf(o[dt][i]) * 0x1p-40f;   // not finite where an output is not
+        uint32_t* flag = reinterpret_cast<uint32_t*>(smem);   // in the stages, which nobody reads any more
+        if (tid == 0) *flag = 0;
+        __syncthreads();
+        if (!(top < INFINITY)) *flag = 1;
+        __syncthreads();
+        const bool again = *flag != 0;
+        __syncthreads();
+        if (again) return true;
+    }
+    if (idle) return false;
+    if (part_o) {
+        float* po = part_o + wave * (32 * D_LAT / 2);
+#pragma unroll
+        for (int dt = 0; dt < WD_DT; ++dt)
+#pragma unroll
+            for (int i4 = 0; i4 < 4; ++i4)
+                *reinterpret_cast<f32x4_t*>(po + ((dt * 4 + i4) * 64 + lane) * 4) =
+                    f32x4_t{o[dt][4 * i4], o[dt][4 * i4 + 1], o[dt][4 * i4 + 2], o[dt][4 * i4 + 3]};
+        if (hh == 0 && ch == 0) {
+            part_ml[2 * (32 * rb + c)] = m_run;
+            part_ml[2 * (32 * rb + c) + 1] = SAFE ? -l_run : l_run;
+        }
+        return false;
+    }
+    if (R >= x.nrow) return false;
+    const int64_t row = x.tok0 * a.H + R;
+    const bool none = m_run == -INFINITY && l_run == 0.f;
+    const float inv = none ? 0.f : (1.0f / l_run) * (SAFE ? 1.0f / CK_ROOM : 1.0f);
+    uint16_t* out = a.out + row * D_LAT + D_LAT / 2 * ch + 4 * hh;
+#pragma unroll
+    for (int dt = 0; dt < WD_DT; ++dt)
+#pragma unroll
+        for (int i4 = 0; i4 < 4; ++i4) {
+            const bf16x4_t v = {(__bf16)(o[dt][4 * i4] * inv), (__bf16)(o[dt][4 * i4 + 1] * inv),
+                                (__bf16)(o[dt][4 * i4 + 2] * inv), (__bf16)(o[dt][4 * i4 + 3] * inv)};
+            *reinterpret_cast<bf16x4_t*>(out + 32 * dt + 8 * i4) = v;
+        }
+    if (hh == 0 && ch == 0) a.lse[row] = lse_of(m_run, l_run);
+    return false;
+}
+
+template <int QG, bool SAFE>
+__device__ __forceinline__ bool segment(const ChunkArgs& a, const CkUnit& x, int t0, int t1, float* part_o, float* part_ml,
+                                        uint8_t* smem) {
+    if constexpr (QG == CK_WAVES)
+        return wide_segment<SAFE>(a, x, t0, t1, part_o, part_ml, smem);
+    else
+        return chunk_segment<QG, SAFE>(a, x, t0, t1, part_o, part_ml, smem);
 }
 
 // ------------------------------------------------------------------- kernels
@@ -468,21 +807,17 @@ __device__ __forceinline__ int scan_units(const ChunkArgs& a, int rows, int* pre
     return total;
 }
 
-template <int QG>
-__global__ __launch_bounds__(CK_THREADS, 2) void chunk_run_kernel(ChunkArgs a) {
-    __shared__ __align__(256) uint8_t smem[CK_SMEM];
+// The segments of run g of n, one after another; returns whether one is to go again.
+template <int QG, bool SAFE>
+__device__ __forceinline__ bool chunk_run(const ChunkArgs& a, int g, int n, int total, const int* pre, uint8_t* smem) {
     constexpr int ROWS = 16 * QG;
-    __shared__ int pre[CK_MAX_UNITS];
-    const int total = scan_units(a, ROWS, pre), U = a.B * a.mb;
-    const int n = run_count(a, total), g = blockIdx.x;
-    if (g == 0)
-        for (int u = threadIdx.x; u <= U; u += CK_THREADS) a.first[u] = u < U ? pre[u] : total;
-    if (g >= n) return;
+    const int U = a.B * a.mb;
     const int beg = run_start(g, n, total), end = run_start(g + 1, n, total);
     int u = 0;   // the last unit that starts at or before beg
     for (int step = CK_MAX_UNITS / 2; step > 0; step /= 2)
         if (u + step < U && pre[u + step] <= beg) u += step;
     int at = beg;
+    bool again = false;
     while (at < end) {
         u = __builtin_amdgcn_readfirstlane(u);
         at = __builtin_amdgcn_readfirstlane(at);
@@ -498,33 +833,65 @@ __global__ __launch_bounds__(CK_THREADS, 2) void chunk_run_kernel(ChunkArgs a) {
         const int slot = 2 * g + (at > beg ? 1 : 0);
         float* po = whole ? nullptr : a.part_o + (int64_t)slot * (ROWS * D_LAT);
         float* pml = a.part_ml + (int64_t)slot * (ROWS * 2);
-        if (chunk_segment<QG, false>(a, x, t0, t1, po, pml, smem)) chunk_segment_again<QG>(a, u, t0, t1, po, pml, smem);
+        again |= segment<QG, SAFE>(a, x, t0, t1, po, pml, smem);
         __syncthreads();   // the stages are free
         at = base + t1;
         ++u;
     }
+    return again;
+}
+
+// Calls, so that the rare segments' registers are not the ordinary ones'; by value, so that
+// nothing of those has an address.
+template <int QG>
+__device__ __attribute__((noinline)) void chunk_run_again(ChunkArgs a, int g, int n, int total, const int* pre, uint8_t* smem) {
+    (void)chunk_run<QG, true>(a, g, n, total, pre, smem);
+}
+template <int QG>
+__device__ __attribute__((noinline)) void chunk_unit_again(ChunkArgs a, int u, int tiles, uint8_t* smem) {
+    (void)segment<QG, true>(a, chunk_unit(a, u, 16 * QG), 0, tiles, nullptr, nullptr, smem);
+}
+
+template <int QG>
+__global__ __launch_bounds__(CK_THREADS, 2) void chunk_run_kernel(ChunkArgs a) {
+    __shared__ __align__(256) uint8_t smem[CK_SMEM];
+    __shared__ int pre[CK_MAX_UNITS];
+    const int total = scan_units(a, 16 * QG, pre), U = a.B * a.mb;
+    const int n = run_count(a, total), g = blockIdx.x;
+    if (g == 0)
+        for (int u = threadIdx.x; u <= U; u += CK_THREADS) a.first[u] = u < U ? pre[u] : total;
+    if (g >= n) return;
+    if (chunk_run<QG, false>(a, g, n, total, pre, smem)) chunk_run_again<QG>(a, g, n, total, pre, smem);
 }
 
 template <int QG>
 __global__ __launch_bounds__(CK_THREADS, 2) void chunk_unit_kernel(ChunkArgs a) {
     __shared__ __align__(256) uint8_t smem[CK_SMEM];
-    constexpr int ROWS = 16 * QG;
     const int b = blockIdx.x / a.mb, j = a.mb - 1 - (int)(blockIdx.x % a.mb);
     const int u = b * a.mb + j;
-    const CkUnit x = chunk_unit(a, u, ROWS);
-    const int n = unit_tiles(a, x, ROWS);
+    const CkUnit x = chunk_unit(a, u, 16 * QG);
+    const int n = unit_tiles(a, x, 16 * QG);
     if (n == 0) return;
-    if (chunk_segment<QG, false>(a, x, 0, n, nullptr, nullptr, smem)) chunk_segment_again<QG>(a, u, 0, n, nullptr, nullptr, smem);
+    if (segment<QG, false>(a, x, 0, n, nullptr, nullptr, smem)) chunk_unit_again<QG>(a, u, n, smem);
 }
 
-// Joins the parts of a unit that several runs cover: block = (unit, 16 rows, 8 of the
-// 32 blocks of 16 dims), thread = 4 dims of a row.
-constexpr int CKJ_DT = 8, CKJ_BATCH = 8;
+// Joins the parts of a unit that several runs cover: block = (unit, 8 KB of a part),
+// thread = 4 dims of a row: float4 f of a part, in the order the segments leave them.
+constexpr int CKJ_THREADS = 512, CKJ_BATCH = 8;
 
-__global__ __launch_bounds__(64 * CKJ_DT) void chunk_join_kernel(ChunkArgs a, int QG) {
-    const int rows = 16 * QG;
-    constexpr int DP = CK_DT / CKJ_DT;
-    const int dp = blockIdx.x % DP, qg = blockIdx.x / DP % QG, u = blockIdx.x / (DP * QG);
+__global__ __launch_bounds__(CKJ_THREADS) void chunk_join_kernel(ChunkArgs a, int QG) {
+    const int rows = 16 * QG, per = rows * (D_LAT / 4) / CKJ_THREADS;
+    const int u = blockIdx.x / per, f = (blockIdx.x % per) * CKJ_THREADS + threadIdx.x, lane = f & 63;
+    int r, d;   // row of the unit and first dim
+    if (QG == CK_WAVES) {
+        const int i = (f >> 6) & 31, wave = f >> 11;   // [wave][32-dim block, 8 dims][lane]
+        r = 32 * (wave >> 1) + (lane & 31);
+        d = D_LAT / 2 * (wave & 1) + 8 * i + 4 * (lane >> 5);
+    } else {
+        const int dt = (f >> 6) & 31, qg = f >> 11;    // [16 rows][16-dim block][lane]
+        r = 16 * qg + (lane & 15);
+        d = 16 * dt + 4 * (lane >> 4);
+    }
     const int U = a.B * a.mb, total = a.first[U], base = a.first[u], next = a.first[u + 1];
     if (next == base) return;
     const int n = run_count(a, total);
@@ -538,9 +905,8 @@ __global__ __launch_bounds__(64 * CKJ_DT) void chunk_join_kernel(ChunkArgs a, in
     const int g0 = run_of(base), g1 = run_of(next - 1);
     if (g0 == g1) return;
     const CkUnit x = chunk_unit(a, u, rows);
-    const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
-    const int R = x.row0 + 16 * qg + c;
-    const int dt = dp * CKJ_DT + (threadIdx.x >> 6);
+    const int R = x.row0 + r;
+    if (R >= x.nrow) return;
     const bool late = run_start(g0, n, total) < base;   // the unit is its first run's last segment, not its first
     float M = -INFINITY, L = 0.f;
     f32x4_t acc = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -551,10 +917,10 @@ __global__ __launch_bounds__(64 * CKJ_DT) void chunk_join_kernel(ChunkArgs a, in
         for (int j = 0; j < CKJ_BATCH; ++j) {
             const int run = min(s0 + j, g1);
             const int64_t slot = 2 * run + (run == g0 && late ? 1 : 0);
-            const float* ml = a.part_ml + slot * (rows * 2) + 2 * (16 * qg + c);
+            const float* ml = a.part_ml + slot * (rows * 2) + 2 * r;
             m[j] = ml[0];
             l[j] = ml[1];
-            v[j] = *reinterpret_cast<const f32x4_t*>(a.part_o + slot * (rows * D_LAT) + qg * (16 * D_LAT) + (dt * 64 + lane) * 4);
+            v[j] = *reinterpret_cast<const f32x4_t*>(a.part_o + slot * (rows * D_LAT) + 4 * f);
         }
         float top = M;
 #pragma unroll
@@ -577,13 +943,12 @@ __global__ __launch_bounds__(64 * CKJ_DT) void chunk_join_kernel(ChunkArgs a, in
             for (int i = 0; i < 4; ++i) acc[i] += wo * v[j][i];
         }
     }
-    if (R >= x.nrow) return;
     const int64_t row = x.tok0 * a.H + R;
     const bool none = M == -INFINITY && L == 0.f;
     const float inv = none ? 0.f : (1.0f / L) * (1.0f / CK_ROOM);
-    const bf16x4_t r = {(__bf16)(acc[0] * inv), (__bf16)(acc[1] * inv), (__bf16)(acc[2] * inv), (__bf16)(acc[3] * inv)};
-    *reinterpret_cast<bf16x4_t*>(a.out + row * D_LAT + 16 * dt + 4 * g) = r;
-    if (g == 0 && dt == 0) a.lse[row] = none ? -INFINITY : ((M == -INFINITY ? 0.f : M) + log2f(L)) * 0.69314718055994530942f;
+    const bf16x4_t v4 = {(__bf16)(acc[0] * inv), (__bf16)(acc[1] * inv), (__bf16)(acc[2] * inv), (__bf16)(acc[3] * inv)};
+    *reinterpret_cast<bf16x4_t*>(a.out + row * D_LAT + d) = v4;
+    if (d == 0) a.lse[row] = lse_of(M, L);
 }
 
 ChunkSplit chunk_split(int64_t B, int64_t H, int64_t max_q, int64_t max_kv) {
@@ -613,7 +978,7 @@ hipError_t launch_chunk(const ChunkArgs& a, const ChunkSplit& sp, hipStream_t s)
         else hipLaunchKernelGGL((chunk_run_kernel<4>), grid, block, 0, s, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess || sp.runs == 1) return e;
-        hipLaunchKernelGGL(chunk_join_kernel, dim3((unsigned)(sp.units * sp.qg * (CK_DT / CKJ_DT))), dim3(64 * CKJ_DT), 0, s, a, (int)sp.qg);
+        hipLaunchKernelGGL(chunk_join_kernel, dim3((unsigned)(sp.units * 16 * sp.qg * (D_LAT / 4) / CKJ_THREADS)), dim3(CKJ_THREADS), 0, s, a, (int)sp.qg);
         return hipGetLastError();
     }
     const dim3 grid((unsigned)sp.units);

@@ -34,8 +34,14 @@ constexpr int prompt_stage_bytes() {
     return PR_KEYS * 2 * (DN + DR + DV);
 }
 
-// K panels: the b128 operand reads take eight rows of one piece at a time
-__device__ __forceinline__ int kpiece_xor(int r) { return r & 7; }
+// K panels: LDS serves a 128-bit read sixteen lanes (rows of one piece) at a time, rows
+// {0-3, 12-15, 20-27} and the others; each such group has all of r mod 16, and the even
+// rows of it all of r / 2 mod 8 (a 64-wide panel's odd rows lie in the other half of
+// the banks), so these spread it over all 16 pieces of a 256-byte sweep
+template <int D>
+__device__ __forceinline__ int kpiece_xor(int r) {
+    return D == 128 ? r & 15 : (r >> 1) & 7;
+}
 // V panels: the transposing reads take four rows (4 a .. 4 a + 3) of 2 or 4 adjacent
 // pieces; the row within the four picks a group of four pieces, so that they cover
 // every bank (a 64-wide panel has 8 pieces a row, and odd rows lie in the other half)
@@ -102,8 +108,8 @@ __device__ __forceinline__ bool prompt_block(const PromptArgs& a, uint8_t* smem)
     const uint16_t* vb = a.v + start * a.vts + (int64_t)g * a.vhs;
     auto issue = [&](int t) {
         uint8_t* st = smem + (t & 1) * STAGE;
-        load_panel<DN>(kb, a.kts, PR_KEYS * t, len, st, wave, lane, kpiece_xor);
-        if constexpr (DR > 0) load_panel<DR>(rb, a.rts, PR_KEYS * t, len, st + OFF_R, wave, lane, kpiece_xor);
+        load_panel<DN>(kb, a.kts, PR_KEYS * t, len, st, wave, lane, kpiece_xor<DN>);
+        if constexpr (DR > 0) load_panel<DR>(rb, a.rts, PR_KEYS * t, len, st + OFF_R, wave, lane, kpiece_xor<DR>);
         load_panel<DV>(vb, a.vts, PR_KEYS * t, len, st + OFF_V, wave, lane, vpiece_xor<DV>);
     };
 
@@ -119,14 +125,9 @@ __device__ __forceinline__ bool prompt_block(const PromptArgs& a, uint8_t* smem)
     for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[ks]));
 
     const uint32_t lds0 = lds_addr(smem);
-    // K operand of (row 32 mt + c, piece 2 ks + hh): the piece's low three bits are permuted
-    uint32_t kaddr[4], raddr[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int low = (2 * i + hh) ^ kpiece_xor(c);
-        kaddr[i] = c * (2 * DN) + 16 * low;
-        raddr[i] = OFF_R + c * (2 * DR) + 16 * low;
-    }
+    // K operand of (row 32 mt + c, piece 2 ks + hh): a k-step flips bits of the permuted piece
+    const uint32_t kaddr = c * (2 * DN) + 16 * (hh ^ kpiece_xor<DN>(c));
+    const uint32_t raddr = DR ? OFF_R + c * (2 * DR) + 16 * (hh ^ kpiece_xor<DR ? DR : 64>(c)) : 0;
     // V operand (transposing reads): lane 4 e + q of a 16-lane group reads row
     // 16 s + 8 u + 4 hh + e, dims 32 dt + 16 gi + 4 q .. +3
     uint32_t vaddr[DT][2];
@@ -169,20 +170,12 @@ __device__ __forceinline__ bool prompt_block(const PromptArgs& a, uint8_t* smem)
             {
                 constexpr int SD = 3;   // operands read ahead of the matrix cores
                 bf16x8_t kf[SD + 1][2];
-                uint32_t ka[4], ra[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) ka[i] = st + kaddr[i], ra[i] = st + raddr[i];
                 auto kload = [&](auto kc) {
                     constexpr int ks = decltype(kc)::value;
-                    if constexpr (ks < KSN) {
-                        kf[ks % (SD + 1)][0] = lds_read128<128 * (ks >> 2)>(ka[ks & 3]);
-                        kf[ks % (SD + 1)][1] = lds_read128<128 * (ks >> 2) + 32 * 2 * DN>(ka[ks & 3]);
-                    } else {
-                        kf[ks % (SD + 1)][0] = lds_read128<0>(ra[ks - KSN]);
-                        kf[ks % (SD + 1)][1] = lds_read128<32 * 2 * DR>(ra[ks - KSN]);
-                    }
+                    const uint32_t at = st + (ks < KSN ? kaddr ^ (32 * ks) : raddr ^ (32 * (ks - KSN)));
+                    kf[ks % (SD + 1)][0] = lds_read128<0>(at);
+                    kf[ks % (SD + 1)][1] = lds_read128<32 * 2 * (ks < KSN ? DN : DR)>(at);
                 };
-                static_assert(KSR <= 4, "one group of pieces in the second panel");
                 static_for<0, SD>(kload);
                 static_for<0, KS>([&](auto kc) {
                     constexpr int ks = decltype(kc)::value;

@@ -54,14 +54,16 @@ __global__ __launch_bounds__(WT_THREADS, 2) void weight_kernel(WeightArgs w) {
     const uint16_t* ql = a.q_lat + tok0 * a.H * a.qls;
     const uint16_t* qr = a.q_rope + tok0 * a.H * a.qrs;
     const float* lse = w.lse + tok0 * a.H;
-    // this wave's loads of tile t: slot q = 72 r + p' holds piece p' ^ (r & 7) of tile row r
+    // this wave's loads of tile t: slot q = 72 r + p' holds piece p' ^ (r / 2 mod 8) of tile row r (LDS serves a
+    // 128-bit read 16 lanes at a time, lanes {0-3, 12-15, 20-27} or the others of a half wave: their slots differ
+    // modulo 16, odd rows lying 8 slots on)
     auto issue = [&](int t, int s) {
         uint8_t* st = smem + s * WT_STAGE;
         int ln = lane;
         asm volatile("" : "+v"(ln));   // keeps the slot arithmetic out of registers across the loop
 #pragma unroll
         for (int i = 0; i < WT_LOADS; ++i) {
-            const int j = wave + WT_WAVES * i, q = 64 * j + ln, r = q / WT_PIECES, p = (q - WT_PIECES * r) ^ (r & 7);
+            const int j = wave + WT_WAVES * i, q = 64 * j + ln, r = q / WT_PIECES, p = (q - WT_PIECES * r) ^ ((r >> 1) & 7);
             const int64_t R = min(WT_TILE * t + r, nrow - 1);   // rows past the end repeat the last one, not counted
             const uint16_t* src = p < D_LAT / 8 ? ql + R * a.qls + 8 * p : qr + R * a.qrs + 8 * (p - D_LAT / 8);
             __builtin_amdgcn_global_load_lds((gbl_void_t*)src, (lds_void_t*)(st + 1024 * j), 16, 0, 0);
@@ -77,7 +79,7 @@ __global__ __launch_bounds__(WT_THREADS, 2) void weight_kernel(WeightArgs w) {
     const int uc = min(u, kv - 1);
     const int32_t page = a.table[(int64_t)b * a.tstride + (uc >> a.shift)];
     const bool there = (uint32_t)page < (uint32_t)a.n_pages;
-    const uint16_t* row = a.cache + (there ? (int64_t)page * a.ps + (int64_t)(uc & a.page_mask) * a.rs : 0) + 8 * hh;
+    const uint16_t* row = a.cache + (there ? 8 * ((int64_t)page * a.ps16 + (int64_t)(uc & a.page_mask) * a.rs16) : 0) + 8 * hh;
     float sum = 0.f;
     if (t0 < t1) {
         issue(t0, 0);
@@ -90,7 +92,7 @@ __global__ __launch_bounds__(WT_THREADS, 2) void weight_kernel(WeightArgs w) {
         const uint32_t lds0 = lds_addr(smem);
         uint32_t qaddr[4];   // Q operand of (tile row c, piece 2 ks + hh), the piece's low three bits permuted
 #pragma unroll
-        for (int i = 0; i < 4; ++i) qaddr[i] = c * WT_ROW_BYTES + 16 * ((2 * i + hh) ^ (c & 7));
+        for (int i = 0; i < 4; ++i) qaddr[i] = c * WT_ROW_BYTES + 16 * ((2 * i + hh) ^ ((c >> 1) & 7));
         for (int t = t0; t < t1; ++t) {
             const int s = (t - t0) & 1;
             // this wave's loads of tile t have landed (nothing else is in flight), every wave's

@@ -750,6 +750,9 @@ static int check_pages(vkv_ctx* ctx, const vkv_pages* pg) {
         return fail(ctx, VKV_E_ALIGN, "row_stride=%lld: need >= 576 and a multiple of 8", (long long)pg->row_stride);
     if (pg->page_stride < 0 || pg->page_stride % 8)
         return fail(ctx, VKV_E_ALIGN, "page_stride=%lld: need a multiple of 8, at least 0", (long long)pg->page_stride);
+    if (pg->row_stride / 8 >= (1ll << 32) || pg->page_stride / 8 >= (1ll << 32))
+        return fail(ctx, VKV_E_SHAPE, "row_stride=%lld or page_stride=%lld not below 2^35", (long long)pg->row_stride,
+                    (long long)pg->page_stride);
     if (pg->table_stride < (pg->max_kv + pg->page - 1) / pg->page)
         return fail(ctx, VKV_E_SHAPE, "table_stride=%lld holds fewer than max_kv=%lld rows", (long long)pg->table_stride,
                     (long long)pg->max_kv);
@@ -777,8 +780,8 @@ static int check_chunk(vkv_ctx* ctx, const vkv_pages* pg, const vkv_chunk* ch) {
 static ChunkArgs chunk_args(const vkv_pages* pg, const vkv_chunk* ch) {
     ChunkArgs a{};
     a.cache = pg->cache;
-    a.rs = pg->row_stride;
-    a.ps = pg->page_stride;
+    a.rs16 = (uint32_t)(pg->row_stride / 8);
+    a.ps16 = (uint32_t)(pg->page_stride / 8);
     while ((1 << a.shift) < pg->page) ++a.shift;
     a.page_mask = pg->page - 1;
     a.n_pages = (int)pg->n_pages;
@@ -937,8 +940,8 @@ int vkv_cache_evict(vkv_ctx* ctx, const vkv_pages* pg, const int32_t* kept, cons
     const ChunkArgs c = chunk_args(pg, &none);
     EvictArgs a{};
     a.cache = pg->cache;
-    a.rs = c.rs;
-    a.ps = c.ps;
+    a.rs = pg->row_stride;
+    a.ps = pg->page_stride;
     a.shift = c.shift;
     a.page_mask = c.page_mask;
     a.n_pages = c.n_pages;

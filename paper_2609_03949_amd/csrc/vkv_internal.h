@@ -312,7 +312,7 @@ struct PromptArgs {
 // the queries of a chunk over a paged cache (attention and attention weights)
 struct ChunkArgs {
     const uint16_t* cache;
-    int64_t rs, ps;        // row and page strides, elements
+    uint32_t rs16, ps16;   // row and page strides, 16 bytes
     int shift, page_mask;  // log2 of the rows of a page, rows - 1
     int n_pages;
     const int32_t* table;  // [B, tstride]

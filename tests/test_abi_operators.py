@@ -82,7 +82,7 @@ PAGES_BAD = [
     (dict(n_pages=1 << 31), -2), (dict(page=0), -4), (dict(page=48), -4), (dict(page=1 << 17), -4), (dict(page=-64), -4),
     (dict(cache=None), -1), (dict(table=None), -1), (dict(kv_len=None), -1), (dict(cache=FAKE + 8), -3), (dict(table=FAKE + 2), -3),
     (dict(kv_len=FAKE + 1), -3), (dict(row_stride=568), -3), (dict(row_stride=580), -3), (dict(page_stride=-8), -3),
-    (dict(page_stride=4), -3), (dict(table_stride=15), -2),
+    (dict(page_stride=4), -3), (dict(table_stride=15), -2), (dict(page_stride=1 << 35), -2), (dict(row_stride=1 << 35), -2),
 ]
 CHUNK_BAD = [
     (dict(H=0), -2), (dict(H=129), -2), (dict(n_tok=-1), -2), (dict(n_tok=1 << 31), -2), (dict(max_q=-1), -2),
