@@ -213,8 +213,7 @@ template <int QG, bool SAFE>
 __device__ __forceinline__ bool chunk_segment(const ChunkArgs& a, const CkUnit& x, int t0, int t1, float* part_o,
                                               float* part_ml, uint8_t* smem) {
     constexpr int KSTR = CK_WAVES / QG;          // streams of tiles
-    constexpr int PD = CK_STAGES / KSTR - 1;     // tiles loaded ahead: 1, 0
-    static_assert(PD == 0 || PD == 1, "what the waits below assume");
+    constexpr int PD = CK_STAGES / KSTR - 1;     // tiles loaded ahead: 3, 1, 0
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int qg = wave % QG, ks0 = wave / QG;
@@ -236,11 +235,6 @@ __device__ __forceinline__ bool chunk_segment(const ChunkArgs& a, const CkUnit& 
         loader.issue(tile_of(k), smem + stage_of(k) * CK_STAGE, gone_of(k));
         loader.fetch(tile_of(k + 1));
     };
-    if (nt > 0) {
-        loader.fetch(tile_of(0));
-        issue(0);
-    }
-
     // Q^T operand: row R, dims 32 ks + 8 g .. +8
     bf16x8_t qf[CK_KS];
     {
@@ -250,18 +244,23 @@ __device__ __forceinline__ bool chunk_segment(const ChunkArgs& a, const CkUnit& 
 #pragma unroll
         for (int ks = 0; ks < CK_KS; ++ks)
             qf[ks] = *reinterpret_cast<const bf16x8_t*>(ks < D_LAT / 32 ? ql + 32 * ks : qr + 32 * ks - D_LAT);
-#pragma unroll
-        for (int ks = 0; ks < CK_KS; ++ks) asm volatile("" : "+v"(qf[ks]));   // no wait for them inside the tile loop
     }
+    if (nt > 0) {
+        loader.fetch(tile_of(0));
+        issue(0);
+        if (PD > 1 && nit > 1) issue(1);
+        if (PD > 2 && nit > 2) issue(2);
+    }
+#pragma unroll
+    for (int ks = 0; ks < CK_KS; ++ks) asm volatile("" : "+v"(qf[ks]));   // no wait for them inside the tile loop
 
-    // K operand of (row 16 mt + c, piece 4 ks + g), the piece's low bits permuted; V operand
-    // (transposing reads): lane 4 e + q of 16-lane group g reads rows 4 g + e and 16 + 4 g + e,
-    // dims 16 dt + 4 q .. +3, i.e. piece 2 dt + q / 2, half q mod 2
-    // (k-steps and dim blocks only flip bits of the permuted piece)
-    const int vrow = 4 * g + (c >> 2);
-    const uint32_t kaddr = c * CK_LAT_BYTES + 16 * (g ^ lat_xor(c));
-    const uint32_t raddr = CK_OFF_ROPE + c * CK_ROPE_BYTES + 16 * (g ^ rope_xor(c));
-    const uint32_t vaddr = vrow * CK_LAT_BYTES + 16 * (((c & 3) >> 1) ^ lat_xor(vrow)) + 8 * (c & 1);
+    // Operand addresses are recomputed from an opaque copy of the lane index, so that no
+    // registers hold them across the loop.
+    auto opaque_lane = [&]() {
+        int ln = lane;
+        asm volatile("" : "+v"(ln));
+        return ln;
+    };
 
     f32x4_t o[CK_DT];
 #pragma unroll
@@ -269,22 +268,27 @@ __device__ __forceinline__ bool chunk_segment(const ChunkArgs& a, const CkUnit& 
     float m_run = -INFINITY, l_run = 0.f;
 
     for (int k = 0; k < nit; ++k) {
-        // this wave's share of tile k has landed (nothing else is in flight), and every wave's;
-        // the stage loaded next is free
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        // this wave's share of tile k has landed (at most the loads of the PD - 1 tiles behind it are
+        // still in flight), and every wave's; the stage loaded next is free
+        if (PD > 1 && k + PD - 1 < nit)
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(PD > 1 ? (PD - 1) * loader.LOADS : 0) : "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         wg_barrier();
         if (PD > 0 && k + PD < nit) issue(k + PD);
         const int t = tile_of(k), u0 = CK_TILE * t;
         if (t < t1 && !idle && u0 <= lim_hi) {
             const uint32_t st = lds0 + stage_of(k) * CK_STAGE;
-            uint32_t note;
-            asm volatile("ds_read_b32 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(note) : "v"(loader.note(gone_of(k), lane)) : "memory");
-            const uint32_t absent = loader.absent(note);   // tile rows on no page
-            const bool masked = u0 + CK_TILE - 1 > lim_lo || absent != 0;
+            uint32_t note;   // arrives ahead of the K operands
+            asm volatile("ds_read_b32 %0, %1" : "=v"(note) : "v"(loader.note(gone_of(k), lane)) : "memory");
             f32x4_t s[2] = {f32x4_t{0.f, 0.f, 0.f, 0.f}, f32x4_t{0.f, 0.f, 0.f, 0.f}};
             {
-                constexpr int SD = 3;   // operands read ahead of the matrix cores
+                constexpr int SD = 2;   // operands read ahead of the matrix cores
                 bf16x8_t kf[SD + 1][2];
+                // K operand of (row 16 mt + c, piece 4 ks + g), the piece's low bits permuted
+                const int ln = opaque_lane(), r = ln & 15;
+                const uint32_t kaddr = r * CK_LAT_BYTES + 16 * ((ln >> 4) ^ lat_xor(r));
+                const uint32_t raddr = CK_OFF_ROPE + r * CK_ROPE_BYTES + 16 * ((ln >> 4) ^ rope_xor(r));
                 uint32_t ka[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) ka[i] = st + (kaddr ^ (64 * i));
@@ -308,7 +312,10 @@ __device__ __forceinline__ bool chunk_segment(const ChunkArgs& a, const CkUnit& 
                     for (int mt = 0; mt < 2; ++mt)
                         s[mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[ks % (SD + 1)][mt], qf[ks], s[mt], 0, 0, 0);
                 });
+                lds_wait<0>(note);
             }
+            const uint32_t absent = loader.absent(note);   // tile rows on no page
+            const bool masked = u0 + CK_TILE - 1 > lim_lo || absent != 0;
             // s[mt][i] = score of tile row 16 mt + 4 g + i for row R
             if (masked) {
                 const int last = lim - u0 - 4 * g;
@@ -348,6 +355,10 @@ __device__ __forceinline__ bool chunk_segment(const ChunkArgs& a, const CkUnit& 
             }
             // the softmax's cross-lane reads complete before the V reads are issued
             asm volatile("" : "+v"(l_run), "+v"(pf));
+            // V operand (transposing reads): lane 4 e + q of 16-lane group g reads rows 4 g + e and 16 + 4 g + e,
+            // dims 16 dt + 4 q .. +3, i.e. piece 2 dt + q / 2, half q mod 2
+            const int vl = opaque_lane(), vrow = vl >> 2;
+            const uint32_t vaddr = vrow * CK_LAT_BYTES + 16 * (((vl >> 1) & 1) ^ lat_xor(vrow)) + 8 * (vl & 1);
             if (SAFE && masked) {
                 bf16x8_t seen;
 #pragma unroll
@@ -478,308 +489,26 @@ __device__ __forceinline__ bool chunk_segment(const ChunkArgs& a, const CkUnit& 
     return false;
 }
 
-// ------------------------------------------------- a segment of 128 rows
-//
-// With 64 rows and more the LDS reads of operands bound the segment above, in which a
-// wave reads every tile twice for 16 rows (557 KB a tile).  Here a wave has 32 rows,
-// shared with one other wave: each takes half of the 576 dims of S^T = K Q^T and half of
-// the 512 dims of O^T = V^T P^T, and the two exchange their halves of the sum S^T through LDS
-// (378 KB a tile, with the loads themselves).  Both then have all of S, the same softmax, and P in
-// registers as before (32x32x16 products).
-//
-// The waves form two groups (0-3 and 4-7, one of each on a SIMD) half a tile apart:
-// while one multiplies by K, the other does the softmax and multiplies by V, so that a
-// SIMD's vector and matrix instructions run beside each other.  Half-step h: group
-// e works on tile (h - e) / 2, on S where h - e is even, on P and O where it is odd.
-// Three tile stages: tile n is loaded from half-step 2 n - 3 on and first read at 2 n.
-
-constexpr int WD_STAGES = 3;
-constexpr int WD_KS = CK_KS, WD_DT = D_LAT / 64;   // 18 products of 16 dims, 8 blocks of 32 dims a wave
-constexpr int WD_XCH = 4096;                       // bytes of a wave's half sums
-constexpr int WD_OFF_XCH = WD_STAGES * CK_STAGE, WD_OFF_GONE = WD_OFF_XCH + CK_WAVES * WD_XCH;
-static_assert(WD_OFF_GONE + WD_STAGES * CK_WAVES * 4 <= CK_SMEM, "the wide segment's LDS");
-
-template <bool SAFE>
-__device__ __forceinline__ bool wide_segment(const ChunkArgs& a, const CkUnit& x, int t0, int t1, float* part_o,
-                                             float* part_ml, uint8_t* smem) {
-    const int tid = threadIdx.x, lane = tid & 63, c = lane & 31, hh = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int grp = wave >> 2, ch = wave & 1, rb = wave >> 1;   // group, half of the dims, block of 32 rows
-    const int R = x.row0 + 32 * rb + c;                         // this lane's row
-    const int Rc = min(R, x.nrow - 1);                          // rows past the end repeat the last one, never stored
-    const int lim = min(x.kv - x.nq + Rc / a.H, x.kv - 1);      // the last cache row it sees
-    const int lim_lo = __builtin_amdgcn_readfirstlane(lim);     // of the wave's rows
-    const bool idle = x.row0 + 32 * rb >= x.nrow;
-    const int nt = x.kv > 0 ? t1 - t0 : 0;
-
-    const uint32_t lds0 = lds_addr(smem);
-    TileLoader<CK_WAVES> loader{a, (const_i32_t*)(a.table + (int64_t)x.b * a.tstride), x.kv, wave, lane, {}};
-    auto gone_of = [&](int k) { return lds0 + WD_OFF_GONE + (k % WD_STAGES) * (CK_WAVES * 4); };
-    auto issue = [&](int k) {   // tile t0 + k, and the table entries of the next one
-        loader.issue(t0 + k, smem + (k % WD_STAGES) * CK_STAGE, gone_of(k));
-        loader.fetch(t0 + k + 1);
-    };
-    if (nt > 0) {
-        loader.fetch(t0);
-        issue(0);
-        if (nt > 1) issue(1);
-    }
-
-    // Q^T operand: row R, k-step j: latent dims 256 ch + 16 j + 8 hh .. +8 (j < 16), then branch dims
-    // 32 ch + 16 (j - 16) + 8 hh .. +8
-    bf16x8_t qf[WD_KS];
-    {
-        const int64_t row = x.tok0 * a.H + Rc;
-        const uint16_t* ql = a.q_lat + row * a.qls + 8 * hh;
-        const uint16_t* qr = a.q_rope + row * a.qrs + 8 * hh;
-#pragma unroll
-        for (int j = 0; j < WD_KS; ++j) {
-            qf[j] = *reinterpret_cast<const bf16x8_t*>(j < 16 ? ql + D_LAT / 2 * ch + 16 * j : qr + D_ROPE / 2 * ch + 16 * (j - 16));
-        }
-#pragma unroll
-        for (int j = 0; j < WD_KS; ++j) asm volatile("" : "+v"(qf[j]));   // no wait for them inside the loop
-    }
-
-    // Operand and exchange addresses are recomputed from an opaque copy of the lane index, so
-    // that no registers hold them across the loop.
-    auto opaque_lane = [&]() {
-        int ln = lane;
-        asm volatile("" : "+v"(ln));
-        return ln;
-    };
-
-    f32x16_t o[WD_DT], s;
-#pragma unroll
-    for (int dt = 0; dt < WD_DT; ++dt)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
-    float m_run = -INFINITY, l_run = 0.f;
-
-    // the beginning of half-step h
-    auto half_step = [&](int h) {
-        // before an even one tile h / 2 has landed: at most the next tile's loads are still in flight
-        if ((h & 1) == 0) {
-            if (h / 2 + 1 < nt)
-                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(loader.LOADS) : "memory");
-            else
-                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        }
-        wg_barrier();   // every wave's loads have, the half sums of the last half-step are written, its stage is free
-        if ((h & 1) == 1 && (h + 3) / 2 < nt) issue((h + 3) / 2);
-    };
-    // Rows past the end and tiles that none of a wave's rows sees are computed like the others (no
-    // branches around the products), and masked.
-    if (nt > 0 && grp == 1) half_step(0);
-    for (int k = 0; k < nt; ++k) {
-        half_step(2 * k + grp);
-        const int u0 = CK_TILE * (t0 + k);
-        const uint32_t st = lds0 + (k % WD_STAGES) * CK_STAGE;
-        {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = 0.f;
-            constexpr int SD = 2;   // operands read ahead of the matrix cores
-            bf16x8_t kf[SD + 1];
-            // K operand of row c: latent piece 32 ch + 2 j + hh, branch piece 4 ch + 2 (j - 16) + hh, permuted
-            const int ln = opaque_lane(), r = ln & 31;
-            const uint32_t kaddr = r * CK_LAT_BYTES + 16 * ((ln >> 5) ^ lat_xor(r));
-            const uint32_t raddr = st + CK_OFF_ROPE + r * CK_ROPE_BYTES + 16 * (((ln >> 5) + 4 * ch) ^ rope_xor(r));
-            auto kload = [&](auto jc) {
-                constexpr int j = decltype(jc)::value;
-                if constexpr (j < 16)
-                    kf[j % (SD + 1)] = lds_read128<256 * (j >> 3)>((kaddr ^ (32 * (j & 7))) + (st + 512 * ch));
-                else
-                    kf[j % (SD + 1)] = lds_read128<0>(raddr ^ (32 * (j - 16)));
-            };
-            static_for<0, SD>(kload);
-            static_for<0, WD_KS>([&](auto jc) {
-                constexpr int j = decltype(jc)::value;
-                if constexpr (j + SD < WD_KS) kload(std::integral_constant<int, j + SD>{});
-                lds_wait<(j + SD < WD_KS) ? SD : (WD_KS - 1 - j)>(kf[j % (SD + 1)]);
-                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[j % (SD + 1)], qf[j], s, 0, 0, 0);
-            });
-            // this half of the sum to the other wave (the matrix results are read by explicit
-            // instructions, so the wait for the last product, at least 18 wait states, is explicit too)
-            asm volatile("s_nop 15\n\ts_nop 7" : "+v"(s));
-            const f32x4_t s0 = {s[0], s[1], s[2], s[3]}, s1 = {s[4], s[5], s[6], s[7]};
-            const f32x4_t s2 = {s[8], s[9], s[10], s[11]}, s3 = {s[12], s[13], s[14], s[15]};
-            asm volatile("ds_write_b128 %0, %1\n\tds_write_b128 %0, %2 offset:1024\n\tds_write_b128 %0, %3 offset:2048\n\t"
-                         "ds_write_b128 %0, %4 offset:3072\n\ts_waitcnt lgkmcnt(0)" ::"v"(lds0 + WD_OFF_XCH + wave * WD_XCH + 16 * ln),
-                         "v"(s0), "v"(s1), "v"(s2), "v"(s3)
-                         : "memory");
-        }
-        half_step(2 * k + grp + 1);
-        const int ln = opaque_lane();
-        uint32_t note;
-        {
-            f32x4_t y[4];
-            asm volatile("ds_read_b32 %4, %6\n\tds_read_b128 %0, %5\n\tds_read_b128 %1, %5 offset:1024\n\t"
-                         "ds_read_b128 %2, %5 offset:2048\n\tds_read_b128 %3, %5 offset:3072\n\ts_waitcnt lgkmcnt(0)"
-                         : "=&v"(y[0]), "=&v"(y[1]), "=&v"(y[2]), "=&v"(y[3]), "=&v"(note)
-                         : "v"(lds0 + WD_OFF_XCH + (wave ^ 1) * WD_XCH + 16 * ln), "v"(loader.note(gone_of(k), ln))
-                         : "memory");
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] += y[i >> 2][i & 3];
-        }
-        const uint32_t absent = loader.absent(note);   // tile rows on no page
-        const bool masked = u0 + CK_TILE - 1 > lim_lo || absent != 0;
-        // s[i] = score of tile row 8 (i / 4) + 4 hh + i % 4 for row R
-        if (masked) {
-            const int last = lim - u0 - 4 * hh;
-            const uint32_t gone = absent >> (4 * hh);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int r = 8 * (i >> 2) + (i & 3);
-                if (r > last || ((gone >> r) & 1u)) s[i] = -INFINITY;
-            }
-        }
-        float cmax = s[0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i) cmax = fmaxf(cmax, s[i]);
-        cmax = half_max(cmax) * a.scale_log2;
-        const bool move = cmax > m_run + CK_SLACK;
-        const float alpha = move ? __builtin_amdgcn_exp2f(m_run - cmax) : 1.0f;
-        if (move) m_run = cmax;
-        const float ref = m_run == -INFINITY ? 0.f : m_run;   // nothing but masked scores so far
-        bf16x8_t pf[2];
-        float psum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], a.scale_log2, -ref));
-            psum += p;
-            pf[i >> 3][i & 7] = (__bf16)(SAFE ? p * CK_ROOM : p);
-        }
-        l_run = l_run * alpha + psum;   // this lane's share of the sum
-        if (__ballot(move)) {
-#pragma unroll
-            for (int dt = 0; dt < WD_DT; ++dt)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[dt][i] *= alpha;
-        }
-        // the softmax's cross-lane reads complete before the V reads are issued
-        asm volatile("" : "+v"(l_run), "+v"(pf[0]), "+v"(pf[1]));
-        // V operand (transposing reads): lane 4 e + q of a 16-lane group reads row 16 s + 8 u + 4 hh + e,
-        // dims 256 ch + 32 dt + 16 gi + 4 q .. +3, i.e. piece 32 ch + 4 dt + 2 gi + q / 2; 8 rows on, the
-        // permutation differs by 3 (y(b + 2) = y(b) ^ 3)
-        const int vrow = 4 * (ln >> 5) + ((ln >> 2) & 3);
-        const uint32_t vaddr = vrow * CK_LAT_BYTES + 16 * ((2 * ((ln >> 4) & 1) + ((ln >> 1) & 1)) ^ lat_xor(vrow)) + 8 * (ln & 1);
-        const uint32_t vst = st + 512 * ch;
-        if (SAFE && masked) {
-            bf16x8_t seen[2];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int r = 8 * (i >> 2) + 4 * hh + (i & 3);
-                seen[i >> 3][i & 7] = (u0 + r <= lim && !((absent >> r) & 1u)) ? (__bf16)1.0f : (__bf16)0.0f;
-            }
-#pragma unroll
-            for (int dt = 0; dt < WD_DT; ++dt) {
-                f32x16_t codes;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) codes[i] = 0.f;
-#pragma unroll
-                for (int s2 = 0; s2 < 2; ++s2) {
-                    const uint32_t at = vst + 256 * (dt >> 2) + 16 * CK_LAT_BYTES * s2;
-                    i16x4_t lo = lds_read_tr16<0>(at + (vaddr ^ (64 * (dt & 3))));
-                    i16x4_t hi = lds_read_tr16<8 * CK_LAT_BYTES>(at + (vaddr ^ (64 * (dt & 3) + 48)));
-                    lds_wait<0>(lo, hi);
-                    bf16x8_t v = join(lo, hi);
-                    const bf16x8_t code = split_nonfinite(v);
-                    o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pf[s2], o[dt], 0, 0, 0);
-                    codes = __builtin_amdgcn_mfma_f32_32x32x16_bf16(code, seen[s2], codes, 0, 0, 0);
-                }
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[dt][i] = add_nonfinite(o[dt][i], codes[i]);
-            }
-        } else {
-            // products in the order dt = e + 4 f, (f, s) inner: two addresses per e
-            constexpr int VD = 4, N = 2 * WD_DT;
-            i16x4_t vv[VD + 1][2];
-            uint32_t va[2];
-            auto vload = [&](auto ic) {
-                constexpr int i = decltype(ic)::value, f = (i >> 1) & 1, s2 = i & 1;
-                if constexpr ((i & 3) == 0) {
-                    va[0] = vst + (vaddr ^ (64 * (i >> 2)));
-                    va[1] = vst + (vaddr ^ (64 * (i >> 2) + 48));
-                }
-                vv[i % (VD + 1)][0] = lds_read_tr16<256 * f + 16 * CK_LAT_BYTES * s2>(va[0]);
-                vv[i % (VD + 1)][1] = lds_read_tr16<256 * f + 16 * CK_LAT_BYTES * s2 + 8 * CK_LAT_BYTES>(va[1]);
-            };
-            static_for<0, VD>(vload);
-            static_for<0, N>([&](auto ic) {
-                constexpr int i = decltype(ic)::value, dt = (i >> 2) + 4 * ((i >> 1) & 1), s2 = i & 1;
-                if constexpr (i + VD < N) vload(std::integral_constant<int, i + VD>{});
-                lds_wait<2 * ((i + VD < N) ? VD : (N - 1 - i))>(vv[i % (VD + 1)][0], vv[i % (VD + 1)][1]);
-                o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(join(vv[i % (VD + 1)][0], vv[i % (VD + 1)][1]), pf[s2], o[dt],
-                                                                0, 0, 0);
-            });
-        }
-    }
-    if (nt > 0 && grp == 0) half_step(2 * nt);
-    l_run = half_sum(l_run);
-
-    __syncthreads();
-    if constexpr (!SAFE) {
-        float top = 0.f;
-        if (!idle)
-#pragma unroll
-            for (int dt = 0; dt < WD_DT; ++dt)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) top += fabsf(o[dt][i]) * 0x1p-40f;   // not finite where an output is not
-        uint32_t* flag = reinterpret_cast<uint32_t*>(smem);   // in the stages, which nobody reads any more
-        if (tid == 0) *flag = 0;
-        __syncthreads();
-        if (!(top < INFINITY)) *flag = 1;
-        __syncthreads();
-        const bool again = *flag != 0;
-        __syncthreads();
-        if (again) return true;
-    }
-    if (idle) return false;
-    if (part_o) {
-        float* po = part_o + wave * (32 * D_LAT / 2);
-#pragma unroll
-        for (int dt = 0; dt < WD_DT; ++dt)
-#pragma unroll
-            for (int i4 = 0; i4 < 4; ++i4)
-                *reinterpret_cast<f32x4_t*>(po + ((dt * 4 + i4) * 64 + lane) * 4) =
-                    f32x4_t{o[dt][4 * i4], o[dt][4 * i4 + 1], o[dt][4 * i4 + 2], o[dt][4 * i4 + 3]};
-        if (hh == 0 && ch == 0) {
-            part_ml[2 * (32 * rb + c)] = m_run;
-            part_ml[2 * (32 * rb + c) + 1] = SAFE ? -l_run : l_run;
-        }
-        return false;
-    }
-    if (R >= x.nrow) return false;
-    const int64_t row = x.tok0 * a.H + R;
-    const bool none = m_run == -INFINITY && l_run == 0.f;
-    const float inv = none ? 0.f : (1.0f / l_run) * (SAFE ? 1.0f / CK_ROOM : 1.0f);
-    uint16_t* out = a.out + row * D_LAT + D_LAT / 2 * ch + 4 * hh;
-#pragma unroll
-    for (int dt = 0; dt < WD_DT; ++dt)
-#pragma unroll
-        for (int i4 = 0; i4 < 4; ++i4) {
-            const bf16x4_t v = {(__bf16)(o[dt][4 * i4] * inv), (__bf16)(o[dt][4 * i4 + 1] * inv),
-                                (__bf16)(o[dt][4 * i4 + 2] * inv), (__bf16)(o[dt][4 * i4 + 3] * inv)};
-            *reinterpret_cast<bf16x4_t*>(out + 32 * dt + 8 * i4) = v;
-        }
-    if (hh == 0 && ch == 0) a.lse[row] = lse_of(m_run, l_run);
-    return false;
-}
-
-template <int QG, bool SAFE>
-__device__ __forceinline__ bool segment(const ChunkArgs& a, const CkUnit& x, int t0, int t1, float* part_o, float* part_ml,
-                                        uint8_t* smem) {
-    if constexpr (QG == CK_WAVES)
-        return wide_segment<SAFE>(a, x, t0, t1, part_o, part_ml, smem);
-    else
-        return chunk_segment<QG, SAFE>(a, x, t0, t1, part_o, part_ml, smem);
-}
-
 // ------------------------------------------------------------------- kernels
 
 // first tile of every unit in the run of all tiles, and their number, into LDS
 __device__ __forceinline__ int scan_units(const ChunkArgs& a, int rows, int* pre) {
+    const int tid = threadIdx.x, lane = tid & 63, U = a.B * a.mb;
+    auto wave_prefix = [&](int v) {
+        for (int d = 1; d < 64; d *= 2) {
+            const int t = __shfl_up(v, d);
+            if (lane >= d) v += t;
+        }
+        return v;
+    };
+    if (U <= 64) {   // every wave for itself, the same values: no barrier
+        const int n = lane < U ? unit_tiles(a, chunk_unit(a, lane, rows), rows) : 0;
+        const int upto = wave_prefix(n);
+        pre[lane] = upto - n;
+        return __builtin_amdgcn_readlane(upto, 63);
+    }
     constexpr int PER = CK_MAX_UNITS / CK_THREADS;
-    const int tid = threadIdx.x, U = a.B * a.mb;
+    __shared__ int waves[CK_WAVES];
     int n[PER], sum = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
@@ -787,24 +516,22 @@ __device__ __forceinline__ int scan_units(const ChunkArgs& a, int rows, int* pre
         n[i] = u < U ? unit_tiles(a, chunk_unit(a, u, rows), rows) : 0;
         sum += n[i];
     }
-    pre[tid] = sum;
+    const int upto = wave_prefix(sum);
+    if (lane == 63) waves[tid >> 6] = upto;
     __syncthreads();
-    for (int d = 1; d < CK_THREADS; d *= 2) {
-        const int v = tid >= d ? pre[tid - d] : 0;
-        __syncthreads();
-        pre[tid] += v;
-        __syncthreads();
+    int at = upto - sum, total = 0;
+#pragma unroll
+    for (int i = 0; i < CK_WAVES; ++i) {
+        if (i < (tid >> 6)) at += waves[i];
+        total += waves[i];
     }
-    const int total = __builtin_amdgcn_readfirstlane(pre[CK_THREADS - 1]);
-    int at = pre[tid] - sum;
-    __syncthreads();
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         pre[PER * tid + i] = at;
         at += n[i];
     }
     __syncthreads();
-    return total;
+    return __builtin_amdgcn_readfirstlane(total);
 }
 
 // The segments of run g of n, one after another; returns whether one is to go again.
@@ -830,10 +557,14 @@ __device__ __forceinline__ bool chunk_run(const ChunkArgs& a, int g, int n, int 
         const CkUnit x = chunk_unit(a, u, ROWS);
         const int t0 = at - base, t1 = min(end, next) - base;
         const bool whole = t0 == 0 && t1 == next - base;
+        if (threadIdx.x == 0) {   // for the join: the unit's first and last run, and which of its slots the first one fills
+            if (t0 == 0) a.span[3 * u] = g, a.span[3 * u + 2] = at > beg;
+            if (t1 == next - base) a.span[3 * u + 1] = g;
+        }
         const int slot = 2 * g + (at > beg ? 1 : 0);
         float* po = whole ? nullptr : a.part_o + (int64_t)slot * (ROWS * D_LAT);
         float* pml = a.part_ml + (int64_t)slot * (ROWS * 2);
-        again |= segment<QG, SAFE>(a, x, t0, t1, po, pml, smem);
+        again |= chunk_segment<QG, SAFE>(a, x, t0, t1, po, pml, smem);
         __syncthreads();   // the stages are free
         at = base + t1;
         ++u;
@@ -849,7 +580,7 @@ __device__ __attribute__((noinline)) void chunk_run_again(ChunkArgs a, int g, in
 }
 template <int QG>
 __device__ __attribute__((noinline)) void chunk_unit_again(ChunkArgs a, int u, int tiles, uint8_t* smem) {
-    (void)segment<QG, true>(a, chunk_unit(a, u, 16 * QG), 0, tiles, nullptr, nullptr, smem);
+    (void)chunk_segment<QG, true>(a, chunk_unit(a, u, 16 * QG), 0, tiles, nullptr, nullptr, smem);
 }
 
 template <int QG>
@@ -858,8 +589,9 @@ __global__ __launch_bounds__(CK_THREADS, 2) void chunk_run_kernel(ChunkArgs a) {
     __shared__ int pre[CK_MAX_UNITS];
     const int total = scan_units(a, 16 * QG, pre), U = a.B * a.mb;
     const int n = run_count(a, total), g = blockIdx.x;
-    if (g == 0)
-        for (int u = threadIdx.x; u <= U; u += CK_THREADS) a.first[u] = u < U ? pre[u] : total;
+    if (g == 0)   // units without rows: nothing to join
+        for (int u = threadIdx.x; u < U; u += CK_THREADS)
+            if ((u + 1 < U ? pre[u + 1] : total) == pre[u]) a.span[3 * u] = a.span[3 * u + 1] = 0;
     if (g >= n) return;
     if (chunk_run<QG, false>(a, g, n, total, pre, smem)) chunk_run_again<QG>(a, g, n, total, pre, smem);
 }
@@ -872,83 +604,76 @@ __global__ __launch_bounds__(CK_THREADS, 2) void chunk_unit_kernel(ChunkArgs a) 
     const CkUnit x = chunk_unit(a, u, 16 * QG);
     const int n = unit_tiles(a, x, 16 * QG);
     if (n == 0) return;
-    if (segment<QG, false>(a, x, 0, n, nullptr, nullptr, smem)) chunk_unit_again<QG>(a, u, n, smem);
+    if (chunk_segment<QG, false>(a, x, 0, n, nullptr, nullptr, smem)) chunk_unit_again<QG>(a, u, n, smem);
 }
 
-// Joins the parts of a unit that several runs cover: block = (unit, 8 KB of a part),
-// thread = 4 dims of a row: float4 f of a part, in the order the segments leave them.
-constexpr int CKJ_THREADS = 512, CKJ_BATCH = 8;
+// Joins the parts of a unit that several runs cover: block = (unit, 128 float4 of a
+// part, in the order the segments leave them), thread = one of them in every CKJ_GROUPS-th
+// part; then the groups join through LDS, in order.
+constexpr int CKJ_F = 128, CKJ_GROUPS = 4, CKJ_THREADS = CKJ_F * CKJ_GROUPS, CKJ_BATCH = 4;
+
+struct JoinSum {
+    float M, L;
+    f32x4_t acc;
+};
+// x += w y, and the references: weights exp2(m - M), m = -inf where nothing was seen (then 0, or NaN)
+__device__ __forceinline__ void join_add(JoinSum& x, float m, float l, const f32x4_t& v, float f) {
+    if (m > x.M) {
+        const float w = x.M == -INFINITY ? 1.0f : exp2f(x.M - m);
+        x.L *= w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x.acc[i] *= w;
+        x.M = m;
+    }
+    const float w = m == -INFINITY ? 1.0f : exp2f(m - x.M);
+    x.L += w * l;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x.acc[i] += w * f * v[i];
+}
 
 __global__ __launch_bounds__(CKJ_THREADS) void chunk_join_kernel(ChunkArgs a, int QG) {
-    const int rows = 16 * QG, per = rows * (D_LAT / 4) / CKJ_THREADS;
-    const int u = blockIdx.x / per, f = (blockIdx.x % per) * CKJ_THREADS + threadIdx.x, lane = f & 63;
-    int r, d;   // row of the unit and first dim
-    if (QG == CK_WAVES) {
-        const int i = (f >> 6) & 31, wave = f >> 11;   // [wave][32-dim block, 8 dims][lane]
-        r = 32 * (wave >> 1) + (lane & 31);
-        d = D_LAT / 2 * (wave & 1) + 8 * i + 4 * (lane >> 5);
-    } else {
-        const int dt = (f >> 6) & 31, qg = f >> 11;    // [16 rows][16-dim block][lane]
-        r = 16 * qg + (lane & 15);
-        d = 16 * dt + 4 * (lane >> 4);
-    }
-    const int U = a.B * a.mb, total = a.first[U], base = a.first[u], next = a.first[u + 1];
-    if (next == base) return;
-    const int n = run_count(a, total);
-    // the runs that hold the unit's first and last tile
-    auto run_of = [&](int tile) {
-        int g = (int)min((int64_t)tile * n / total, (int64_t)n - 1);
-        while (run_start(g + 1, n, total) <= tile) ++g;
-        while (run_start(g, n, total) > tile) --g;
-        return g;
-    };
-    const int g0 = run_of(base), g1 = run_of(next - 1);
+    __shared__ JoinSum sums[CKJ_GROUPS - 1][CKJ_F];
+    const int rows = 16 * QG, per = rows * (D_LAT / 4) / CKJ_F;
+    const int u = blockIdx.x / per, grp = threadIdx.x / CKJ_F;
+    const int f = (blockIdx.x % per) * CKJ_F + threadIdx.x % CKJ_F, lane = f & 63;
+    const int r = 16 * (f >> 11) + (lane & 15), d = 16 * ((f >> 6) & 31) + 4 * (lane >> 4);   // row of the unit, first dim
+    const int g0 = a.span[3 * u], g1 = a.span[3 * u + 1], late = a.span[3 * u + 2];
     if (g0 == g1) return;
     const CkUnit x = chunk_unit(a, u, rows);
     const int R = x.row0 + r;
-    if (R >= x.nrow) return;
-    const bool late = run_start(g0, n, total) < base;   // the unit is its first run's last segment, not its first
-    float M = -INFINITY, L = 0.f;
-    f32x4_t acc = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    for (int s0 = g0; s0 <= g1; s0 += CKJ_BATCH) {
-        float m[CKJ_BATCH], l[CKJ_BATCH];
-        f32x4_t v[CKJ_BATCH];
+    const bool live = R < x.nrow;
+    JoinSum t{-INFINITY, 0.f, f32x4_t{0.f, 0.f, 0.f, 0.f}};
+    if (live)
+        for (int s0 = g0 + grp; s0 <= g1; s0 += CKJ_GROUPS * CKJ_BATCH) {
+            float m[CKJ_BATCH], l[CKJ_BATCH];
+            f32x4_t v[CKJ_BATCH];
 #pragma unroll
-        for (int j = 0; j < CKJ_BATCH; ++j) {
-            const int run = min(s0 + j, g1);
-            const int64_t slot = 2 * run + (run == g0 && late ? 1 : 0);
-            const float* ml = a.part_ml + slot * (rows * 2) + 2 * r;
-            m[j] = ml[0];
-            l[j] = ml[1];
-            v[j] = *reinterpret_cast<const f32x4_t*>(a.part_o + slot * (rows * D_LAT) + 4 * f);
+            for (int j = 0; j < CKJ_BATCH; ++j) {   // all loads in flight
+                const int run = min(s0 + CKJ_GROUPS * j, g1);
+                const int64_t slot = 2 * run + (run == g0 ? late : 0);
+                const float* ml = a.part_ml + slot * (rows * 2) + 2 * r;
+                m[j] = ml[0];
+                l[j] = ml[1];
+                v[j] = *reinterpret_cast<const f32x4_t*>(a.part_o + slot * (rows * D_LAT) + 4 * f);
+            }
+#pragma unroll
+            for (int j = 0; j < CKJ_BATCH; ++j)   // acc carries the factor; parts with l < 0 do already
+                if (s0 + CKJ_GROUPS * j <= g1) join_add(t, m[j], fabsf(l[j]), v[j], l[j] < 0.f ? 1.0f : CK_ROOM);
         }
-        float top = M;
+    if (grp > 0) sums[grp - 1][threadIdx.x % CKJ_F] = t;
+    __syncthreads();
+    if (grp > 0 || !live) return;
 #pragma unroll
-        for (int j = 0; j < CKJ_BATCH; ++j)
-            if (s0 + j <= g1) top = fmaxf(top, m[j]);
-        if (top != M && M != -INFINITY) {
-            const float w = exp2f(M - top);
-            L *= w;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[i] *= w;
-        }
-        M = top;
-#pragma unroll
-        for (int j = 0; j < CKJ_BATCH; ++j) {
-            if (s0 + j > g1) break;
-            const float w = m[j] == -INFINITY ? 1.0f : exp2f(m[j] - M);   // nothing seen: 0, or NaN
-            L += w * fabsf(l[j]);
-            const float wo = w * (l[j] < 0.f ? 1.0f : CK_ROOM);   // acc carries the factor
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[i] += wo * v[j][i];
-        }
+    for (int i = 0; i < CKJ_GROUPS - 1; ++i) {
+        const JoinSum y = sums[i][threadIdx.x];
+        join_add(t, y.M, y.L, y.acc, 1.0f);
     }
     const int64_t row = x.tok0 * a.H + R;
-    const bool none = M == -INFINITY && L == 0.f;
-    const float inv = none ? 0.f : (1.0f / L) * (1.0f / CK_ROOM);
-    const bf16x4_t v4 = {(__bf16)(acc[0] * inv), (__bf16)(acc[1] * inv), (__bf16)(acc[2] * inv), (__bf16)(acc[3] * inv)};
+    const bool none = t.M == -INFINITY && t.L == 0.f;
+    const float inv = none ? 0.f : (1.0f / t.L) * (1.0f / CK_ROOM);
+    const bf16x4_t v4 = {(__bf16)(t.acc[0] * inv), (__bf16)(t.acc[1] * inv), (__bf16)(t.acc[2] * inv), (__bf16)(t.acc[3] * inv)};
     *reinterpret_cast<bf16x4_t*>(a.out + row * D_LAT + d) = v4;
-    if (d == 0) a.lse[row] = lse_of(M, L);
+    if (d == 0) a.lse[row] = lse_of(t.M, t.L);
 }
 
 ChunkSplit chunk_split(int64_t B, int64_t H, int64_t max_q, int64_t max_kv) {
@@ -959,12 +684,12 @@ ChunkSplit chunk_split(int64_t B, int64_t H, int64_t max_q, int64_t max_kv) {
     s.units = B * s.mb;
     const int64_t tiles = s.units * std::max<int64_t>(1, (max_kv + CK_TILE - 1) / CK_TILE);
     s.runs = s.units <= CK_MAX_UNITS && tiles < (1ll << 31) ? CK_RUNS : 0;
-    s.min_run = 2 * CK_WAVES / s.qg;
+    s.min_run = CK_WAVES / s.qg;
     if (s.runs) {
         s.runs = std::max<int64_t>(1, std::min<int64_t>(s.runs, tiles / s.min_run));
         s.part_o = (size_t)(2 * s.runs) * 16 * s.qg * D_LAT * 4;
         s.part_ml = (size_t)(2 * s.runs) * 16 * s.qg * 2 * 4;
-        s.first = (size_t)(s.units + 1) * 4;
+        s.span = (size_t)s.units * 3 * 4;
     }
     return s;
 }
@@ -978,7 +703,7 @@ hipError_t launch_chunk(const ChunkArgs& a, const ChunkSplit& sp, hipStream_t s)
         else hipLaunchKernelGGL((chunk_run_kernel<4>), grid, block, 0, s, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess || sp.runs == 1) return e;
-        hipLaunchKernelGGL(chunk_join_kernel, dim3((unsigned)(sp.units * 16 * sp.qg * (D_LAT / 4) / CKJ_THREADS)), dim3(CKJ_THREADS), 0, s, a, (int)sp.qg);
+        hipLaunchKernelGGL(chunk_join_kernel, dim3((unsigned)(sp.units * 16 * sp.qg * (D_LAT / 4) / CKJ_F)), dim3(CKJ_THREADS), 0, s, a, (int)sp.qg);
         return hipGetLastError();
     }
     const dim3 grid((unsigned)sp.units);

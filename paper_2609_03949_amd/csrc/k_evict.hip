@@ -1,120 +1,366 @@
 // k_evict.hip -- the tier of the rows of largest accumulated attention weight, and
 // the move of a tier's rows to the front of a paged cache (gfx950).
+#include <algorithm>
+
 #include "vkv_internal.h"
 
 namespace vkv {
 
 // ------------------------------------------------------------- the selection
 //
-// Rows [0, nsink) and [n - recent, n) are kept in any case; of the others the m of
-// largest weight, ties to the lower row.  Order by an integer key that grows with the
-// weight (NaN below everything, -0 equal to 0).
+// Rows [0, nsink) and [n - recent, n) are kept in any case; of the others (those that
+// compete) the m of largest weight, ties to the lower row.  Order by an integer key that
+// grows with the weight (NaN below everything, -0 equal to 0).
+//
+// One launch, up to WS_MAX_PARTS workgroups a sequence; each finds the m-th largest key for
+// itself and writes its part of the rows.  Up to WS_CAP competing rows lie in LDS; of more,
+// a sample of WS_SAMPLE rows brackets the m-th key within 4.5 standard deviations of its
+// rank, one pass over all weights counts what lies above the bracket and lists what lies
+// in it, and the key is selected among those.  Where the bracket misses (which the
+// counts tell) or holds too many, the selection passes over all weights.  The pass is
+// what the time goes to: two comparisons and, at 5% of the rows listed, a list write in
+// most waves, about 8 us for 131072 rows; more workgroups a sequence would not shorten it.
 
-constexpr int WS_THREADS = 1024, WS_PER = 4;
+constexpr int WS_THREADS = 1024, WS_WAVES = WS_THREADS / 64;
+constexpr int WS_CAP = 16384, WS_SEG = WS_CAP / WS_WAVES;   // listed rows, and of one wave
+constexpr int WS_SAMPLE = 2048, WS_BINS = 2048;
+constexpr int WS_MAX_PARTS = 8;
+constexpr int WS_LOADS = 16;                                // loads of a thread in flight
 
 __device__ __forceinline__ uint32_t weight_key(float w) {
     if (w != w) return 0u;
     return key_to_ord(w + 0.0f);
 }
 
-// inclusive prefix sum over the block's threads; `total` of all of them
-__device__ __forceinline__ int block_prefix(int v, int* s_wave, int& total) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+struct SelShared {
+    float w[WS_CAP];          // listed weights, a segment for each wave, and their rows
+    int32_t row[WS_CAP];
+    int hist[2][WS_BINS];     // one is cleared while the other is read
+    int wave[WS_WAVES];
+    uint32_t lo[WS_WAVES], hi[WS_WAVES];
+    int seg[WS_WAVES];        // rows listed by each wave
+    uint32_t edge[2];
+    int bin, left;
+};
+
+__device__ __forceinline__ int wave_prefix(int v) {
+    const int lane = threadIdx.x & 63;
     for (int d = 1; d < 64; d *= 2) {
         const int t = __shfl_up(v, d);
         if (lane >= d) v += t;
     }
+    return v;
+}
+
+// sum over the block's threads (two barriers)
+__device__ __forceinline__ int block_sum(int v, SelShared& sh) {
+    v = wave_prefix(v);
     __syncthreads();
-    if (lane == 63) s_wave[wave] = v;
+    if ((threadIdx.x & 63) == 63) sh.wave[threadIdx.x >> 6] = v;
     __syncthreads();
-    int before = 0;
-    total = 0;
-    for (int i = 0; i < WS_THREADS / 64; ++i) {
-        const int t = s_wave[i];
-        if (i < wave) before += t;
-        total += t;
+    int total = 0;
+#pragma unroll
+    for (int i = 0; i < WS_WAVES; ++i) total += sh.wave[i];
+    return total;
+}
+
+// smallest and largest of the threads' values (two barriers)
+__device__ __forceinline__ void block_range(uint32_t& lo, uint32_t& hi, SelShared& sh) {
+    for (int d = 32; d > 0; d /= 2) {
+        lo = min(lo, (uint32_t)__shfl_xor((int)lo, d));
+        hi = max(hi, (uint32_t)__shfl_xor((int)hi, d));
     }
-    return v + before;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) sh.lo[threadIdx.x >> 6] = lo, sh.hi[threadIdx.x >> 6] = hi;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < WS_WAVES; ++i) lo = min(lo, sh.lo[i]), hi = max(hi, sh.hi[i]);
+}
+
+// After the threads' atomics on hist[which] (the other one is cleared here): each thread's two
+// bins, counted from the top (bins - 1 - 2 t and the next one down), and what lies above them.
+struct TopBins {
+    int i1, c1, c0, above;
+};
+__device__ __forceinline__ TopBins top_bins(int bins, int which, SelShared& sh) {
+    const int tid = threadIdx.x, wave = tid >> 6;
+    __syncthreads();
+    TopBins t;
+    t.i1 = bins - 1 - 2 * tid;
+    t.c1 = t.i1 >= 0 ? sh.hist[which][t.i1] : 0;
+    t.c0 = t.i1 >= 1 ? sh.hist[which][t.i1 - 1] : 0;
+    const int upto = wave_prefix(t.c1 + t.c0);
+    if ((tid & 63) == 63) sh.wave[wave] = upto;
+#pragma unroll
+    for (int i = tid; i < WS_BINS; i += WS_THREADS) sh.hist[which ^ 1][i] = 0;
+    __syncthreads();
+    t.above = upto - t.c1 - t.c0;
+#pragma unroll
+    for (int i = 0; i < WS_WAVES; ++i) t.above += i < wave ? sh.wave[i] : 0;
+    return t;
+}
+
+// The rank-th largest (from 1) of the keys that each(f) hands to f, every thread its own ones,
+// all in [lo, hi]; `left` of the keys equal to it are among the rank largest.  hist[which] is clear.
+template <typename Each>
+__device__ __forceinline__ uint32_t radix_select(Each each, uint32_t lo, uint32_t hi, int rank, int& which, SelShared& sh,
+                                                 int& left) {
+    uint32_t prefix = 0, mask = 0;
+    int shift = hi == lo ? 0 : 32 - __clz((int)(hi - lo));   // the digits are those of key - lo
+    left = rank;
+    while (shift > 0) {
+        const int bits = min(shift, 11), bins = 1 << bits;
+        shift -= bits;
+        each([&](uint32_t k) {
+            const uint32_t x = k - lo;
+            if ((x & mask) == prefix) atomicAdd(&sh.hist[which][(x >> shift) & (bins - 1)], 1);
+        });
+        const TopBins t = top_bins(bins, which, sh);
+        if (t.above < left && left <= t.above + t.c1 + t.c0) {
+            const bool first = left <= t.above + t.c1;
+            sh.bin = first ? t.i1 : t.i1 - 1;
+            sh.left = left - (first ? t.above : t.above + t.c1);
+        }
+        __syncthreads();
+        prefix |= (uint32_t)sh.bin << shift;
+        mask |= (uint32_t)(bins - 1) << shift;
+        left = sh.left;
+        which ^= 1;
+    }
+    return lo + prefix;
 }
 
 __global__ __launch_bounds__(WS_THREADS) void weight_select_kernel(WeightSelArgs a) {
-    __shared__ int hist[2048];
-    __shared__ int s_wave[WS_THREADS / 64];
-    __shared__ int s_bin, s_left;
-    const int b = blockIdx.x, tid = threadIdx.x;
+    __shared__ SelShared sh;
+    // a sequence's workgroups on one XCD (they go there in turn), whose L2 then holds its weights
+    const int b = (int)(blockIdx.x / (8u * a.parts)) * 8 + (int)(blockIdx.x % 8u), part = (int)(blockIdx.x / 8u) % a.parts;
+    if (b >= a.B) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = min(max(a.kv_len[b], 0), a.max_kv), K = a.keep;
     int32_t* kept = a.kept + (int64_t)b * K;
-    if (tid == 0) a.count[b] = min(n, K);
+    if (part == 0 && tid == 0) a.count[b] = min(n, K);
     if (n <= K) {
-        for (int j = tid; j < K; j += WS_THREADS) kept[j] = j < n ? j : -1;
+        for (int64_t j = (int64_t)part * WS_THREADS + tid; j < K; j += (int64_t)a.parts * WS_THREADS) kept[j] = j < n ? (int)j : -1;
         return;
     }
     const float* w = a.weight + (int64_t)b * a.stride;
-    const int lo = a.nsink, hi = n - a.recent;   // the rows that compete
-    int left = K - a.nsink - a.recent;           // how many of them are kept
-    // the left-th largest key, 11 + 11 + 10 bits at a time
-    uint32_t prefix = 0, mask = 0;
-    const int shifts[3] = {21, 10, 0};
-    if (left > 0)
-        for (int pass = 0; pass < 3; ++pass) {
-            const int shift = shifts[pass], bins = pass == 2 ? 1024 : 2048;
-            for (int i = tid; i < bins; i += WS_THREADS) hist[i] = 0;
-            __syncthreads();
-            for (int u = lo + tid; u < hi; u += WS_THREADS) {
-                const uint32_t key = weight_key(w[u]);
-                if ((key & mask) == prefix) atomicAdd(&hist[(key >> shift) & (bins - 1)], 1);
+    const int lo = a.nsink, hi = n - a.recent, N = hi - lo;   // the rows that compete
+    const int m = K - a.nsink - a.recent;                     // how many of them are kept (fewer than N)
+    // this workgroup's rows (max_kv is at most 2^30: no overflow below)
+    const int size = (n + a.parts - 1) / a.parts;
+    const int r0 = min(part * size, n), r1 = min(r0 + size, n);
+    const int s0 = min(max(r0, lo), hi);                      // competing rows before r0 are [lo, s0)
+
+    // kept: key > T, or key = T and row <= cut;  before: the competing rows kept before s0
+    uint32_t T = 0xFFFFFFFFu;
+    int cut = 0x7FFFFFFF, before = 0;
+    if (m > 0) {
+        constexpr int PER = WS_SEG / 64;      // listed keys of a thread, in registers
+        uint32_t key[PER];
+        int cnt = 0, rank = m, which = 0, ties, unused;
+        bool listed = true;
+        uint32_t ka = 0xFFFFFFFFu, kb = 0;    // the listed keys' range
+        for (int i = tid; i < WS_BINS; i += WS_THREADS) sh.hist[0][i] = 0;
+        // rows of the listed keys: consecutive ones for each wave, or those in sh.row
+        const bool whole = N <= WS_CAP;
+        const int seg = (N + WS_WAVES - 1) / WS_WAVES;
+        const int beg = min(wave * seg, N);
+        auto row_of = [&](int i) { return whole ? lo + beg + 64 * i + lane : sh.row[wave * WS_SEG + 64 * i + lane]; };
+        if (whole) {
+            cnt = min(seg, N - beg);
+            float v[PER];
+#pragma unroll
+            for (int i = 0; i < PER; ++i) v[i] = 64 * i < cnt ? w[lo + beg + min(64 * i + lane, cnt - 1)] : 0.f;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                key[i] = weight_key(v[i]);
+                if (64 * i + lane < cnt) {
+                    ka = min(ka, key[i]);
+                    kb = max(kb, key[i]);
+                }
+            }
+            block_range(ka, kb, sh);
+        } else {
+            // the sample: one row of each of WS_SAMPLE equal pieces, at a place in it that a hash picks
+            uint32_t sample[WS_SAMPLE / WS_THREADS];
+#pragma unroll
+            for (int i = 0; i < WS_SAMPLE / WS_THREADS; ++i) {
+                const uint32_t j = tid + WS_THREADS * i;
+                const uint32_t h = (j * 2654435761u) ^ (j * 40503u >> 3);
+                const int p0 = (int)((int64_t)N * j / WS_SAMPLE), p1 = (int)((int64_t)N * (j + 1) / WS_SAMPLE);
+                sample[i] = weight_key(w[lo + p0 + (int)(h % (uint32_t)(p1 - p0))]);
+                ka = min(ka, sample[i]);
+                kb = max(kb, sample[i]);
+            }
+            block_range(ka, kb, sh);
+            // by a histogram over the sample's range: the bins of the ranks that bracket the m-th key
+            const int shift = max(kb == ka ? 0 : 32 - __clz((int)(kb - ka)) - 11, 0);
+#pragma unroll
+            for (int i = 0; i < WS_SAMPLE / WS_THREADS; ++i) atomicAdd(&sh.hist[0][(sample[i] - ka) >> shift], 1);
+            const float p = (float)m / (float)N, e = WS_SAMPLE * p, d = 4.5f * sqrtf(e * (1.0f - p)) + 2.0f;
+            const int top = (int)(e - d), low = (int)(e + d) + 1;
+            if (tid == 0) sh.edge[0] = 0u, sh.edge[1] = 0xFF800000u;   // no lower one; +inf
+            const TopBins t = top_bins(WS_BINS, 0, sh);
+            which = 1;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int above = t.above + (i ? t.c1 : 0), c = i ? t.c0 : t.c1;
+                const uint32_t bin = ka + ((uint32_t)(t.i1 - i) << shift);
+                if (above < low && low <= above + c) sh.edge[0] = bin;
+                if (above < top && top <= above + c) sh.edge[1] = min(bin + (1u << shift) - 1u, kb);
             }
             __syncthreads();
-            // bins from the top: thread t takes bins - 1 - 2 t and the next one down
-            const int i1 = bins - 1 - 2 * tid, c1 = i1 >= 0 ? hist[i1] : 0, c0 = i1 >= 1 ? hist[i1 - 1] : 0;
-            int total;
-            const int upto = block_prefix(c1 + c0, s_wave, total), above = upto - c1 - c0;
-            if (above < left && left <= upto) {
-                const bool first = left <= above + c1;
-                s_bin = first ? i1 : i1 - 1;
-                s_left = left - (first ? above : above + c1);
+            ka = sh.edge[0];
+            kb = sh.edge[1];
+            listed = ka != 0u;    // (0: NaN, which compares with nothing, or everything)
+            int above = 0;
+            if (listed) {
+                const float fb = ord_to_key(kb), fa = ord_to_key(ka);
+                auto look = [&](float v, int u, uint64_t in) __attribute__((always_inline)) {
+                    const uint64_t gt = __ballot(v > fb) & in;
+                    const uint64_t ge = __ballot(v >= fa) & in & ~gt;
+                    above += __popcll(gt);
+                    if (ge) {
+                        const int c = __popcll(ge);
+                        if (cnt + c <= WS_SEG && (ge >> lane & 1ull)) {
+                            const int at = wave * WS_SEG + cnt + __builtin_amdgcn_mbcnt_hi((uint32_t)(ge >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)ge, 0));
+                            sh.w[at] = v;
+                            sh.row[at] = u;
+                        }
+                        cnt += c;
+                    }
+                };
+                int above_before = 0;
+                for (int half = 0; half < 2; ++half) {        // the rows before s0, then the others
+                    const int e1 = half ? hi : s0;
+                    int i0 = half ? s0 : lo;
+                    above_before = half ? above : 0;
+                    for (; e1 - i0 >= WS_THREADS * WS_LOADS; i0 += WS_THREADS * WS_LOADS) {
+                        float v[WS_LOADS];
+                        const int u = i0 + tid;
+#pragma unroll
+                        for (int i = 0; i < WS_LOADS; ++i) v[i] = w[u + WS_THREADS * i];
+#pragma unroll
+                        for (int i = 0; i < WS_LOADS; ++i) look(v[i], u + WS_THREADS * i, ~0ull);
+                    }
+                    for (; i0 < e1; i0 += WS_THREADS) {
+                        const int u = i0 + tid;
+                        const float v = w[min(u, e1 - 1)];
+                        look(v, u, __ballot(u < e1));
+                    }
+                }
+                // over the waves: rows above, rows above before s0, rows listed
+                if (lane == 0) sh.lo[wave] = (uint32_t)above, sh.hi[wave] = (uint32_t)above_before, sh.seg[wave] = cnt;
+                __syncthreads();
+                int in = 0;
+                above = 0;
+#pragma unroll
+                for (int i = 0; i < WS_WAVES; ++i) {
+                    above += (int)sh.lo[i];
+                    before += (int)sh.hi[i];
+                    in += sh.seg[i];
+                    listed = listed && sh.seg[i] <= WS_SEG;
+                }
+                listed = listed && above < m && m <= above + in;
+                rank = m - above;
+                cnt = listed ? cnt : 0;
+#pragma unroll
+                for (int i = 0; i < PER; ++i)
+                    if (64 * i + lane < cnt) key[i] = key_to_ord(sh.w[wave * WS_SEG + 64 * i + lane] + 0.0f);
             }
-            __syncthreads();
-            prefix |= (uint32_t)s_bin << shift;
-            mask |= (uint32_t)(bins - 1) << shift;
-            left = s_left;
-            __syncthreads();
         }
-    // rows above the key, and the first `left` rows that have it, in order
-    const bool none = K - a.nsink - a.recent == 0;
-    int out = 0, ties = 0;
-    for (int u0 = 0; u0 < n; u0 += WS_THREADS * WS_PER) {
-        uint32_t key[WS_PER];
-        int eq = 0;
+        if (listed) {
+            auto each = [&](auto f) {
 #pragma unroll
-        for (int i = 0; i < WS_PER; ++i) {
-            const int u = u0 + WS_PER * tid + i;
-            key[i] = u >= lo && u < hi ? weight_key(w[u]) : 0u;
-            eq += u >= lo && u < hi && key[i] == prefix && !none;
+                for (int i = 0; i < PER; ++i)
+                    if (64 * i < cnt && 64 * i + lane < cnt) f(key[i]);
+            };
+            T = radix_select(each, ka, kb, rank, which, sh, ties);
+            // all rows of that key, as a rule; else the ties-th lowest of them
+            int c = 0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+                if (64 * i + lane < cnt) c += key[i] == T;
+            if (block_sum(c, sh) > ties) {
+                auto rows = [&](auto f) {
+#pragma unroll
+                    for (int i = 0; i < PER; ++i)
+                        if (64 * i + lane < cnt && key[i] == T) f(~(uint32_t)row_of(i));
+                };
+                cut = (int)~radix_select(rows, ~(uint32_t)hi, ~(uint32_t)lo, ties, which, sh, unused);
+            }
+            if (r0 > lo) {
+                c = 0;
+#pragma unroll
+                for (int i = 0; i < PER; ++i)
+                    if (64 * i + lane < cnt) {
+                        const int u = row_of(i);
+                        c += u < s0 && (key[i] > T || (key[i] == T && u <= cut));
+                    }
+                before += block_sum(c, sh);
+            }
+        } else {
+            // over all weights
+            auto all = [&](int e0, int e1, auto f) {
+                for (int i0 = e0 + tid; i0 < e1; i0 += WS_THREADS * WS_LOADS) {
+                    float v[WS_LOADS];
+#pragma unroll
+                    for (int i = 0; i < WS_LOADS; ++i) v[i] = w[min(i0 + WS_THREADS * i, e1 - 1)];
+#pragma unroll
+                    for (int i = 0; i < WS_LOADS; ++i)
+                        if (i0 + WS_THREADS * i < e1) f(weight_key(v[i]), i0 + WS_THREADS * i);
+                }
+            };
+            T = radix_select([&](auto f) { all(lo, hi, [&](uint32_t k, int) { f(k); }); }, 0u, 0xFFFFFFFFu, m, which, sh, ties);
+            cut = (int)~radix_select([&](auto f) { all(lo, hi, [&](uint32_t k, int u) { if (k == T) f(~(uint32_t)u); }); },
+                                     ~(uint32_t)hi, ~(uint32_t)lo, ties, which, sh, unused);
+            int c = 0;
+            all(lo, s0, [&](uint32_t k, int u) { c += k > T || (k == T && u <= cut); });
+            before = block_sum(c, sh);
         }
-        int total_eq, total;
-        int at_eq = ties + block_prefix(eq, s_wave, total_eq) - eq;
-        bool take[WS_PER];
-        int cnt = 0;
+    }
+    // the kept rows of [r0, r1), in order: each wave 512 consecutive rows at a time
+    int out = min(r0, lo) + before + max(r0 - hi, 0);
+    constexpr int G = 8;
+    for (int u0 = r0; u0 < r1; u0 += WS_THREADS * G) {
+        float v[G];
+        uint64_t take[G];
+        int c = 0;
+        const int w0 = u0 + 64 * G * wave;
 #pragma unroll
-        for (int i = 0; i < WS_PER; ++i) {
-            const int u = u0 + WS_PER * tid + i;
-            const bool in = u >= lo && u < hi;
-            take[i] = u < n && (!in || (!none && (key[i] > prefix || (key[i] == prefix && at_eq < left))));
-            if (in && !none && key[i] == prefix) ++at_eq;
-            cnt += take[i];
+        for (int i = 0; i < G; ++i) v[i] = w[min(w0 + 64 * i + lane, r1 - 1)];
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+            const int u = w0 + 64 * i + lane;
+            const uint32_t k = weight_key(v[i]);
+            take[i] = __ballot(u < r1 && (u < lo || u >= hi || (m > 0 && (k > T || (k == T && u <= cut)))));
+            c += __popcll(take[i]);
         }
-        int at = out + block_prefix(cnt, s_wave, total) - cnt;
+        __syncthreads();
+        if (lane == 0) sh.wave[wave] = c;
+        __syncthreads();
+        int at = out;
 #pragma unroll
-        for (int i = 0; i < WS_PER; ++i)
-            if (take[i]) kept[at++] = u0 + WS_PER * tid + i;
-        ties += total_eq;
-        out += total;
+        for (int i = 0; i < WS_WAVES; ++i) {
+            const int t = sh.wave[i];
+            if (i < wave) at += t;
+            out += t;
+        }
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+            if (take[i] >> lane & 1ull) kept[at + __popcll(take[i] & ((1ull << lane) - 1ull))] = w0 + 64 * i + lane;
+            at += __popcll(take[i]);
+        }
     }
 }
 
+// workgroups of a sequence: each passes over all its weights, so more only divide the writing
+int weight_select_parts(int64_t B, int64_t max_kv) {
+    return (int)std::max<int64_t>(1, std::min<int64_t>({WS_MAX_PARTS, 256 / B, (max_kv + WS_CAP - 1) / WS_CAP}));
+}
+
 hipError_t launch_weight_select(const WeightSelArgs& a, hipStream_t s) {
-    hipLaunchKernelGGL(weight_select_kernel, dim3((unsigned)a.B), dim3(WS_THREADS), 0, s, a);
+    hipLaunchKernelGGL(weight_select_kernel, dim3((unsigned)((a.B + 7) / 8 * 8 * a.parts)), dim3(WS_THREADS), 0, s, a);
     return hipGetLastError();
 }
 

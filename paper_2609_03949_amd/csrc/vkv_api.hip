@@ -802,19 +802,19 @@ static ChunkArgs chunk_args(const vkv_pages* pg, const vkv_chunk* ch) {
 }
 
 // the workspace's arrays
-static size_t chunk_layout(const ChunkSplit& sp, size_t* part_o, size_t* part_ml, size_t* first) {
+static size_t chunk_layout(const ChunkSplit& sp, size_t* part_o, size_t* part_ml, size_t* span) {
     *part_o = 0;
     *part_ml = up256(sp.part_o);
-    *first = *part_ml + up256(sp.part_ml);
-    return *first + up256(sp.first);
+    *span = *part_ml + up256(sp.part_ml);
+    return *span + up256(sp.span);
 }
 
 int vkv_chunk_workspace_size(const vkv_pages* pg, const vkv_chunk* ch, size_t* bytes) {
     if (!bytes) return fail(nullptr, VKV_E_ARG, "bytes is NULL");
     int rc = check_chunk(nullptr, pg, ch);
     if (rc) return rc;
-    size_t po, pml, first;
-    *bytes = chunk_layout(chunk_split(pg->B, ch->H, ch->max_q, pg->max_kv), &po, &pml, &first);
+    size_t po, pml, span;
+    *bytes = chunk_layout(chunk_split(pg->B, ch->H, ch->max_q, pg->max_kv), &po, &pml, &span);
     return VKV_OK;
 }
 
@@ -827,8 +827,8 @@ int vkv_chunk_attend(vkv_ctx* ctx, const vkv_pages* pg, const vkv_chunk* ch, voi
     if (!out || !lse) return fail(ctx, VKV_E_ARG, "out and lse are required");
     if (!al16(out)) return fail(ctx, VKV_E_ALIGN, "out must be 16-byte aligned");
     const ChunkSplit sp = chunk_split(pg->B, ch->H, ch->max_q, pg->max_kv);
-    size_t po, pml, first;
-    const size_t need = chunk_layout(sp, &po, &pml, &first);
+    size_t po, pml, span;
+    const size_t need = chunk_layout(sp, &po, &pml, &span);
     if (need > 0 && (rc = check_ws(ctx, ws, ws_bytes, need))) return rc;
     if (ch->n_tok == 0 || ch->max_q == 0) return VKV_OK;
     ChunkArgs a = chunk_args(pg, ch);
@@ -842,7 +842,7 @@ int vkv_chunk_attend(vkv_ctx* ctx, const vkv_pages* pg, const vkv_chunk* ch, voi
     if (sp.runs) {
         a.part_o = reinterpret_cast<float*>(w + po);
         a.part_ml = reinterpret_cast<float*>(w + pml);
-        a.first = reinterpret_cast<int32_t*>(w + first);
+        a.span = reinterpret_cast<int32_t*>(w + span);
     }
     DeviceGuard dev(ctx);
     HIP_TRY(ctx, dev.err);
@@ -916,6 +916,7 @@ int vkv_weight_select(vkv_ctx* ctx, const float* weight, int64_t B, int64_t max_
     a.nsink = (int)nsink;
     a.recent = (int)recent;
     a.keep = (int)keep;
+    a.parts = weight_select_parts(B, max_kv);
     a.kept = kept;
     a.count = count;
     DeviceGuard dev(ctx);

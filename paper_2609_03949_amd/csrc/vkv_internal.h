@@ -330,7 +330,7 @@ struct ChunkArgs {
     float scale_log2;
     uint16_t* out;         // [n_tok, H, 512]
     float* lse;            // [n_tok, H]
-    int32_t* first;        // [units + 1] first tile of each unit in the run of all tiles
+    int32_t* span;         // [units][3] first and last run that hold tiles of the unit, and which slot of the first
     float* part_o;         // [2 runs][16 qg rows x 512], accumulator order
     float* part_ml;        // [2 runs][16 qg rows][2]
 };
@@ -339,7 +339,7 @@ constexpr int CK_RUNS = 256;         // one per CU
 // how a chunk is cut: waves by rows (16 qg rows a unit), units, runs (0: a workgroup per unit), workspace bytes
 struct ChunkSplit {
     int64_t qg, mb, units, runs, min_run;
-    size_t part_o, part_ml, first;
+    size_t part_o, part_ml, span;
 };
 ChunkSplit chunk_split(int64_t B, int64_t H, int64_t max_q, int64_t max_kv);
 hipError_t launch_chunk(const ChunkArgs& a, const ChunkSplit& sp, hipStream_t s);
@@ -364,9 +364,11 @@ struct WeightSelArgs {
     int64_t stride;
     const int32_t* kv_len; // [B]
     int B, max_kv, nsink, recent, keep;
+    int parts;             // workgroups of a sequence
     int32_t* kept;         // [B, keep]
     int32_t* count;        // [B]
 };
+int weight_select_parts(int64_t B, int64_t max_kv);
 hipError_t launch_weight_select(const WeightSelArgs& a, hipStream_t s);
 
 struct EvictArgs {

@@ -207,6 +207,45 @@ def test_tier_of_long_contexts(ctx):
     check_tier(ctx, w, [131072, 100003], 4096, 4, 512)
 
 
+def sampled_rows(N):
+    """Where the selection samples the N competing rows of a long sequence."""
+    j = torch.arange(2048, dtype=torch.int64)
+    h = ((j * 2654435761) & 0xFFFFFFFF) ^ ((j * 40503 & 0xFFFFFFFF) >> 3)
+    p0, p1 = N * j // 2048, N * (j + 1) // 2048
+    return p0 + h % (p1 - p0)
+
+
+@pytest.mark.parametrize("n", [16383, 16384, 16385, 16392, 40000])
+@pytest.mark.parametrize("share", [0.0001, 0.03, 0.5, 0.97])
+def test_tier_of_listed_and_sampled_rows(ctx, n, share):
+    """Lengths around the number of rows that lie in LDS, few to nearly all of them kept."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(n)
+    w = torch.exp(2 * torch.randn(2, n, generator=g, device=DEV))
+    w[1] = w[1].sort().values
+    check_tier(ctx, w, [n, n], max(int(n * share), 1), 0, 0)
+
+
+def test_tier_where_the_sample_misleads(ctx):
+    """The sampled rows hold the largest weights, or the smallest: the bracket misses the wanted key; ties and NaN
+    in numbers that no list holds."""
+    N = 50000
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1)
+    w = torch.rand(6, N, generator=g, device=DEV)
+    at = sampled_rows(N).to(DEV)
+    w[0, at] += 10.0
+    w[1, at] -= 10.0
+    w[2, :] = 0.5
+    w[2, ::3] = 0.25
+    w[3, ::2] = math.nan
+    w[4] = (w[4] * 8).round()
+    w[5, 1000:30000] = math.nan
+    for keep in (100, 5000, 25000, 40000):
+        check_tier(ctx, w, [N, N, N, N, N - 1, N], keep, 0, 0)
+    check_tier(ctx, w, [N] * 6, 5000, 4, 4000)
+
+
 def test_tier_lengths_out_of_range(ctx):
     w = torch.rand(3, 50, device=DEV)
     check_tier(ctx, w, [-3, 1 << 30, 0], 20, 2, 3)
