@@ -186,17 +186,19 @@ def _stream(stream) -> ctypes.c_void_p:
 
 
 def _typed(t: Optional[torch.Tensor], dtype, name: str, shape=None, contiguous: bool = True):
-    """The pointer of an argument after its type, its shape (None: any size) and its layout are checked
+    """The address of an argument after its type, its shape (None: any size) and its layout are checked
     (not contiguous: any strides, neighbouring elements in the last dimension)."""
     if t is None:
         return None
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-    if shape is not None and (t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape))):
-        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    if contiguous and not t.is_contiguous() or t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1:
+    s = t.shape
+    if shape is not None and s != shape and (
+            len(s) != len(shape) or any(n is not None and n != m for n, m in zip(shape, s))):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(s)}")
+    if not t.is_contiguous() and (contiguous or s[-1] > 1 and t.stride(-1) != 1):
         raise ValueError(f"{name} must be contiguous" + ("" if contiguous else " in its last dimension"))
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def _stride(t: torch.Tensor, dim: int) -> int:
@@ -204,9 +206,9 @@ def _stride(t: torch.Tensor, dim: int) -> int:
     return t.stride(dim) if t.shape[dim] > 1 else 0
 
 
-def _call_stream(ctx: "Context", stream) -> ctypes.c_void_p:
+def _call_stream(ctx: "Context", stream) -> int:
     """The stream of a call: the given one, else the current one of the context's device."""
-    return _stream(torch.cuda.current_stream(ctx.device) if stream is None else stream)
+    return (torch.cuda.current_stream(ctx.device) if stream is None else stream).cuda_stream
 
 
 class Context:
@@ -609,7 +611,7 @@ def chunk_attend(ctx: Context, pages: Pages, chunk: Chunk, ws: torch.Tensor, sca
     _sequences(pages, chunk)
     n, H = chunk.n_tok, chunk.H
     ctx.check(ctx.lib.vkv_chunk_attend(
-        ctx.handle, pages.ref, chunk.ref, _ptr(ws), ws.numel() * ws.element_size(), float(scale),
+        ctx.handle, pages.ref, chunk.ref, _ptr(ws), ws.nbytes, float(scale),
         _typed(out, torch.bfloat16, "out", (n, H, D_LAT)), _typed(lse, torch.float32, "lse", (n, H)),
         _call_stream(ctx, stream)))
 
@@ -632,8 +634,8 @@ def weight_accumulate(ctx: Context, pages: Pages, chunk: Chunk, lse: torch.Tenso
     f = torch.float32
     ctx.check(ctx.lib.vkv_weight_accumulate(
         ctx.handle, pages.ref, chunk.ref, _typed(lse, f, "lse", (chunk.n_tok, chunk.H)), _ptr(ws),
-        0 if ws is None else ws.numel() * ws.element_size(), float(scale), float(decay),
-        _typed(prev, f, "prev", tuple(weight.shape)), _typed(weight, f, "weight", (pages.B, None)), weight.shape[1],
+        0 if ws is None else ws.nbytes, float(scale), float(decay),
+        _typed(prev, f, "prev", weight.shape), _typed(weight, f, "weight", (pages.B, None)), weight.shape[1],
         _call_stream(ctx, stream)))
 
 

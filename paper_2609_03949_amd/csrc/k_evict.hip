@@ -17,13 +17,18 @@ namespace vkv {
 // a sample of WS_SAMPLE rows brackets the m-th key within 4.5 standard deviations of its
 // rank, one pass over all weights counts what lies above the bracket and lists what lies
 // in it, and the key is selected among those.  Where the bracket misses (which the
-// counts tell) or holds too many, the selection passes over all weights.  The pass is
-// what the time goes to: two comparisons and, at 5% of the rows listed, a list write in
-// most waves, about 8 us for 131072 rows; more workgroups a sequence would not shorten it.
+// counts tell) or holds too many, the selection passes over all weights.
+//
+// Measured at 32 sequences of 131072 rows, m = 4096: 36 us, of which the sample and its
+// bracket 7, the pass over the weights 16, the selection among the listed rows 4 and the
+// writing 5.  The pass is bound by what one compute unit does for its sequence's rows: two
+// comparisons a row and, with a bracket that holds 5% of them, a list write in most waves
+// (written without the branch it took as long).  More workgroups a sequence only divide the
+// writing: each has to know the key, and joining their counts would take a second launch.
 
 constexpr int WS_THREADS = 1024, WS_WAVES = WS_THREADS / 64;
-constexpr int WS_CAP = 16384, WS_SEG = WS_CAP / WS_WAVES;   // listed rows, and of one wave
-constexpr int WS_SAMPLE = 2048, WS_BINS = 2048;
+constexpr int WS_PER = 16, WS_CAP = WS_THREADS * WS_PER;    // listed rows of a thread, and of all
+constexpr int WS_SAMPLE = 8192, WS_BINS = 2048;
 constexpr int WS_MAX_PARTS = 8;
 constexpr int WS_LOADS = 16;                                // loads of a thread in flight
 
@@ -33,23 +38,29 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 }
 
 struct SelShared {
-    float w[WS_CAP];          // listed weights, a segment for each wave, and their rows
-    int32_t row[WS_CAP];
+    uint2 list[WS_PER + 1][WS_THREADS];   // listed rows and their weights, each thread its own (the last place: too many)
     int hist[2][WS_BINS];     // one is cleared while the other is read
     int wave[WS_WAVES];
     uint32_t lo[WS_WAVES], hi[WS_WAVES];
-    int seg[WS_WAVES];        // rows listed by each wave
+    int in[WS_WAVES], most[WS_WAVES];     // rows listed by each wave; whether one of its threads found too many
     uint32_t edge[2];
-    int bin, left;
+    int bin, left, size;
 };
 
-__device__ __forceinline__ int wave_prefix(int v) {
-    const int lane = threadIdx.x & 63;
-    for (int d = 1; d < 64; d *= 2) {
-        const int t = __shfl_up(v, d);
-        if (lane >= d) v += t;
-    }
+// v combined with that of other lanes by op, in steps within the rows of 16 lanes and then over
+// them, without LDS: lane l ends with all of lanes 0 .. l.  zero: op's neutral value.
+template <typename Op>
+__device__ __forceinline__ int wave_scan(int v, int zero, Op op) {
+    v = op(v, __builtin_amdgcn_update_dpp(zero, v, 0x111, 0xF, 0xF, false));   // row_shr:1
+    v = op(v, __builtin_amdgcn_update_dpp(zero, v, 0x112, 0xF, 0xF, false));   // row_shr:2
+    v = op(v, __builtin_amdgcn_update_dpp(zero, v, 0x114, 0xF, 0xF, false));   // row_shr:4
+    v = op(v, __builtin_amdgcn_update_dpp(zero, v, 0x118, 0xF, 0xF, false));   // row_shr:8
+    v = op(v, __builtin_amdgcn_update_dpp(zero, v, 0x142, 0xA, 0xF, false));   // row_bcast:15 to rows 1 and 3
+    v = op(v, __builtin_amdgcn_update_dpp(zero, v, 0x143, 0xC, 0xF, false));   // row_bcast:31 to rows 2 and 3
     return v;
+}
+__device__ __forceinline__ int wave_prefix(int v) {
+    return wave_scan(v, 0, [](int x, int y) { return x + y; });
 }
 
 // sum over the block's threads (two barriers)
@@ -66,12 +77,10 @@ __device__ __forceinline__ int block_sum(int v, SelShared& sh) {
 
 // smallest and largest of the threads' values (two barriers)
 __device__ __forceinline__ void block_range(uint32_t& lo, uint32_t& hi, SelShared& sh) {
-    for (int d = 32; d > 0; d /= 2) {
-        lo = min(lo, (uint32_t)__shfl_xor((int)lo, d));
-        hi = max(hi, (uint32_t)__shfl_xor((int)hi, d));
-    }
+    lo = (uint32_t)wave_scan((int)lo, -1, [](int x, int y) { return (int)min((uint32_t)x, (uint32_t)y); });
+    hi = (uint32_t)wave_scan((int)hi, 0, [](int x, int y) { return (int)max((uint32_t)x, (uint32_t)y); });
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) sh.lo[threadIdx.x >> 6] = lo, sh.hi[threadIdx.x >> 6] = hi;
+    if ((threadIdx.x & 63) == 63) sh.lo[threadIdx.x >> 6] = lo, sh.hi[threadIdx.x >> 6] = hi;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < WS_WAVES; ++i) lo = min(lo, sh.lo[i]), hi = max(hi, sh.hi[i]);
@@ -101,7 +110,8 @@ __device__ __forceinline__ TopBins top_bins(int bins, int which, SelShared& sh) 
 }
 
 // The rank-th largest (from 1) of the keys that each(f) hands to f, every thread its own ones,
-// all in [lo, hi]; `left` of the keys equal to it are among the rank largest.  hist[which] is clear.
+// all in [lo, hi]: returns T such that the rank largest are the keys above T and `left` of those
+// equal to T (0 where a digit's bin ends the selection: T is then below the bin).  hist[which] is clear.
 template <typename Each>
 __device__ __forceinline__ uint32_t radix_select(Each each, uint32_t lo, uint32_t hi, int rank, int& which, SelShared& sh,
                                                  int& left) {
@@ -120,12 +130,17 @@ __device__ __forceinline__ uint32_t radix_select(Each each, uint32_t lo, uint32_
             const bool first = left <= t.above + t.c1;
             sh.bin = first ? t.i1 : t.i1 - 1;
             sh.left = left - (first ? t.above : t.above + t.c1);
+            sh.size = first ? t.c1 : t.c0;
         }
         __syncthreads();
         prefix |= (uint32_t)sh.bin << shift;
         mask |= (uint32_t)(bins - 1) << shift;
         left = sh.left;
         which ^= 1;
+        if (sh.size == left && lo + prefix != 0u) {   // all keys of the bin
+            left = 0;
+            return lo + prefix - 1u;
+        }
     }
     return lo + prefix;
 }
@@ -155,26 +170,28 @@ __global__ __launch_bounds__(WS_THREADS) void weight_select_kernel(WeightSelArgs
     uint32_t T = 0xFFFFFFFFu;
     int cut = 0x7FFFFFFF, before = 0;
     if (m > 0) {
-        constexpr int PER = WS_SEG / 64;      // listed keys of a thread, in registers
-        uint32_t key[PER];
-        int cnt = 0, rank = m, which = 0, ties, unused;
+        uint32_t key[WS_PER];                 // this thread's listed keys, cnt of them
+        int cnt = 0, rank = m, which = 0, ties;
+        // the count-th lowest of the rows whose complements each(f) hands out
+        auto last_row = [&](auto each, int count) {
+            int left;
+            const uint32_t t = radix_select(each, ~(uint32_t)hi, ~(uint32_t)lo, count, which, sh, left);
+            return (int)~t - (left == 0 ? 1 : 0);   // (below the bin: the rows before ~t)
+        };
         bool listed = true;
         uint32_t ka = 0xFFFFFFFFu, kb = 0;    // the listed keys' range
         for (int i = tid; i < WS_BINS; i += WS_THREADS) sh.hist[0][i] = 0;
-        // rows of the listed keys: consecutive ones for each wave, or those in sh.row
         const bool whole = N <= WS_CAP;
-        const int seg = (N + WS_WAVES - 1) / WS_WAVES;
-        const int beg = min(wave * seg, N);
-        auto row_of = [&](int i) { return whole ? lo + beg + 64 * i + lane : sh.row[wave * WS_SEG + 64 * i + lane]; };
+        auto row_of = [&](int i) { return whole ? lo + tid + WS_THREADS * i : (int)sh.list[i][tid].x; };
         if (whole) {
-            cnt = min(seg, N - beg);
-            float v[PER];
+            cnt = max((N - tid + WS_THREADS - 1) / WS_THREADS, 0);
+            float v[WS_PER];
 #pragma unroll
-            for (int i = 0; i < PER; ++i) v[i] = 64 * i < cnt ? w[lo + beg + min(64 * i + lane, cnt - 1)] : 0.f;
+            for (int i = 0; i < WS_PER; ++i) v[i] = WS_THREADS * i < N ? w[lo + min(tid + WS_THREADS * i, N - 1)] : 0.f;
 #pragma unroll
-            for (int i = 0; i < PER; ++i) {
+            for (int i = 0; i < WS_PER; ++i) {
                 key[i] = weight_key(v[i]);
-                if (64 * i + lane < cnt) {
+                if (i < cnt) {
                     ka = min(ka, key[i]);
                     kb = max(kb, key[i]);
                 }
@@ -216,84 +233,91 @@ __global__ __launch_bounds__(WS_THREADS) void weight_select_kernel(WeightSelArgs
             int above = 0;
             if (listed) {
                 const float fb = ord_to_key(kb), fa = ord_to_key(ka);
-                auto look = [&](float v, int u, uint64_t in) __attribute__((always_inline)) {
-                    const uint64_t gt = __ballot(v > fb) & in;
-                    const uint64_t ge = __ballot(v >= fa) & in & ~gt;
-                    above += __popcll(gt);
-                    if (ge) {
-                        const int c = __popcll(ge);
-                        if (cnt + c <= WS_SEG && (ge >> lane & 1ull)) {
-                            const int at = wave * WS_SEG + cnt + __builtin_amdgcn_mbcnt_hi((uint32_t)(ge >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)ge, 0));
-                            sh.w[at] = v;
-                            sh.row[at] = u;
-                        }
-                        cnt += c;
+                int gt = 0;   // this thread's count
+                auto look = [&](float v, int u) __attribute__((always_inline)) {
+                    const bool over = v > fb;
+                    gt += over;
+                    if (v >= fa && !over) {
+                        sh.list[min(cnt, WS_PER)][tid] = make_uint2((uint32_t)u, __float_as_uint(v));
+                        ++cnt;
                     }
                 };
                 int above_before = 0;
                 for (int half = 0; half < 2; ++half) {        // the rows before s0, then the others
                     const int e1 = half ? hi : s0;
                     int i0 = half ? s0 : lo;
-                    above_before = half ? above : 0;
-                    for (; e1 - i0 >= WS_THREADS * WS_LOADS; i0 += WS_THREADS * WS_LOADS) {
-                        float v[WS_LOADS];
-                        const int u = i0 + tid;
+                    above_before = gt;
+                    // the next batch's loads are in flight while one is looked at
+                    float v[WS_LOADS], next[WS_LOADS];
+                    auto load = [&](float (&x)[WS_LOADS]) __attribute__((always_inline)) {
 #pragma unroll
-                        for (int i = 0; i < WS_LOADS; ++i) v[i] = w[u + WS_THREADS * i];
+                        for (int i = 0; i < WS_LOADS; ++i) x[i] = w[i0 + tid + WS_THREADS * i];
+                    };
+                    constexpr int STEP = WS_THREADS * WS_LOADS;
+                    if (e1 - i0 >= STEP) load(next);
+                    while (e1 - i0 >= STEP) {
 #pragma unroll
-                        for (int i = 0; i < WS_LOADS; ++i) look(v[i], u + WS_THREADS * i, ~0ull);
-                    }
-                    for (; i0 < e1; i0 += WS_THREADS) {
+                        for (int i = 0; i < WS_LOADS; ++i) v[i] = next[i];
                         const int u = i0 + tid;
-                        const float v = w[min(u, e1 - 1)];
-                        look(v, u, __ballot(u < e1));
+                        i0 += STEP;
+                        if (e1 - i0 >= STEP) load(next);
+#pragma unroll
+                        for (int i = 0; i < WS_LOADS; ++i) look(v[i], u + WS_THREADS * i);
                     }
+                    for (int u = i0 + tid; u < e1; u += WS_THREADS) look(w[u], u);
                 }
-                // over the waves: rows above, rows above before s0, rows listed
-                if (lane == 0) sh.lo[wave] = (uint32_t)above, sh.hi[wave] = (uint32_t)above_before, sh.seg[wave] = cnt;
+                // over the block: rows above, rows above before s0, rows listed
+                gt = wave_prefix(gt);
+                above_before = wave_prefix(above_before);
+                const int listing = wave_prefix(cnt);
+                const bool full = __ballot(cnt > WS_PER) != 0;
+                if (lane == 63) {
+                    sh.lo[wave] = (uint32_t)gt;
+                    sh.hi[wave] = (uint32_t)above_before;
+                    sh.in[wave] = listing;
+                    sh.most[wave] = full;
+                }
                 __syncthreads();
                 int in = 0;
-                above = 0;
 #pragma unroll
                 for (int i = 0; i < WS_WAVES; ++i) {
                     above += (int)sh.lo[i];
                     before += (int)sh.hi[i];
-                    in += sh.seg[i];
-                    listed = listed && sh.seg[i] <= WS_SEG;
+                    in += sh.in[i];
+                    listed = listed && !sh.most[i];
                 }
                 listed = listed && above < m && m <= above + in;
                 rank = m - above;
                 cnt = listed ? cnt : 0;
 #pragma unroll
-                for (int i = 0; i < PER; ++i)
-                    if (64 * i + lane < cnt) key[i] = key_to_ord(sh.w[wave * WS_SEG + 64 * i + lane] + 0.0f);
+                for (int i = 0; i < WS_PER; ++i)
+                    if (i < cnt) key[i] = key_to_ord(__uint_as_float(sh.list[i][tid].y) + 0.0f);
             }
         }
         if (listed) {
             auto each = [&](auto f) {
 #pragma unroll
-                for (int i = 0; i < PER; ++i)
-                    if (64 * i < cnt && 64 * i + lane < cnt) f(key[i]);
+                for (int i = 0; i < WS_PER; ++i)
+                    if (i < cnt) f(key[i]);
             };
             T = radix_select(each, ka, kb, rank, which, sh, ties);
-            // all rows of that key, as a rule; else the ties-th lowest of them
+            // rows whose key is T: the ties-th lowest of them
             int c = 0;
-#pragma unroll
-            for (int i = 0; i < PER; ++i)
-                if (64 * i + lane < cnt) c += key[i] == T;
-            if (block_sum(c, sh) > ties) {
+            if (ties == 0) {
+                cut = -1;
+            } else {
                 auto rows = [&](auto f) {
 #pragma unroll
-                    for (int i = 0; i < PER; ++i)
-                        if (64 * i + lane < cnt && key[i] == T) f(~(uint32_t)row_of(i));
+                    for (int i = 0; i < WS_PER; ++i)
+                        if (i < cnt && key[i] == T) f(~(uint32_t)row_of(i));
                 };
-                cut = (int)~radix_select(rows, ~(uint32_t)hi, ~(uint32_t)lo, ties, which, sh, unused);
+                cut = last_row(rows, ties);
             }
             if (r0 > lo) {
                 c = 0;
 #pragma unroll
-                for (int i = 0; i < PER; ++i)
-                    if (64 * i + lane < cnt) {
+                for (int i = 0; i < WS_PER; ++i)
+                    if (i < cnt) {
                         const int u = row_of(i);
                         c += u < s0 && (key[i] > T || (key[i] == T && u <= cut));
                     }
@@ -312,16 +336,15 @@ __global__ __launch_bounds__(WS_THREADS) void weight_select_kernel(WeightSelArgs
                 }
             };
             T = radix_select([&](auto f) { all(lo, hi, [&](uint32_t k, int) { f(k); }); }, 0u, 0xFFFFFFFFu, m, which, sh, ties);
-            cut = (int)~radix_select([&](auto f) { all(lo, hi, [&](uint32_t k, int u) { if (k == T) f(~(uint32_t)u); }); },
-                                     ~(uint32_t)hi, ~(uint32_t)lo, ties, which, sh, unused);
+            cut = ties == 0 ? -1 : last_row([&](auto f) { all(lo, hi, [&](uint32_t k, int u) { if (k == T) f(~(uint32_t)u); }); }, ties);
             int c = 0;
             all(lo, s0, [&](uint32_t k, int u) { c += k > T || (k == T && u <= cut); });
             before = block_sum(c, sh);
         }
     }
-    // the kept rows of [r0, r1), in order: each wave 512 consecutive rows at a time
+    // the kept rows of [r0, r1), in order: each wave 1024 consecutive rows at a time
     int out = min(r0, lo) + before + max(r0 - hi, 0);
-    constexpr int G = 8;
+    constexpr int G = 16;
     for (int u0 = r0; u0 < r1; u0 += WS_THREADS * G) {
         float v[G];
         uint64_t take[G];

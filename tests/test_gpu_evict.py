@@ -209,9 +209,10 @@ def test_tier_of_long_contexts(ctx):
 
 def sampled_rows(N):
     """Where the selection samples the N competing rows of a long sequence."""
-    j = torch.arange(2048, dtype=torch.int64)
+    S = 8192
+    j = torch.arange(S, dtype=torch.int64)
     h = ((j * 2654435761) & 0xFFFFFFFF) ^ ((j * 40503 & 0xFFFFFFFF) >> 3)
-    p0, p1 = N * j // 2048, N * (j + 1) // 2048
+    p0, p1 = N * j // S, N * (j + 1) // S
     return p0 + h % (p1 - p0)
 
 
