@@ -4,16 +4,12 @@
 //   weight[u] = decay * prev[u] + sum_{i, h: u seen} exp(scale * (q_lat . c_u + q_rope . r_u) - lse_ih)
 //
 // The attention's log-sum-exp is given, so one product S = Q K^T and one
-// exponential per score are left.  Work split: workgroup = 128 cache rows, two of
-// them per CU (one loads its rows while the other computes); each of 4 waves
-// holds 32 rows (576 dims) in its registers as the B operand and the queries pass by: tiles
-// of 32 (token, head) rows through two LDS stages by direct loads, one barrier per
-// tile.  A lane then has one cache row (its column) and 16 queries: the sum over
-// the queries is in-lane but for one swap of the lane halves at the end.  Every
-// row's sum belongs to one workgroup; where there are few cache rows the queries
-// are cut into parts as well, and a second kernel adds those in order.  Nothing
-// is added atomically: the same inputs give the same bits.
-// Sums: fp32, 16 terms of a tile first, then over the tiles.
+// exponential per score are left.  Cache rows lie in a wave's registers as the B
+// operand and the queries pass by, tiles of 32 (token, head) rows through LDS
+// stages: a lane then has one cache row (its column) and 16 queries a tile, and
+// the sum over the queries is in-lane but for one swap of the lane halves at the
+// end.  Sums: fp32, 16 terms of a tile first, then over the tiles.  Nothing is
+// added atomically: the same inputs give the same bits.
 #include <algorithm>
 
 #include "vkv_tile.h"
@@ -21,20 +17,35 @@
 namespace vkv {
 
 constexpr int WT_WAVES = 4, WT_THREADS = 64 * WT_WAVES;
-constexpr int WT_ROWS = 32 * WT_WAVES;                   // cache rows of a workgroup
 constexpr int WT_TILE = 32;                              // queries of a tile
-constexpr int WT_PIECES = D_ROW / 8;
-constexpr int WT_ROW_BYTES = 2 * D_ROW;
-constexpr int WT_STAGE = WT_TILE * WT_ROW_BYTES;
-constexpr int WT_LOADS = WT_STAGE / 1024 / WT_WAVES;     // 9 loads of 1 KB per wave
+constexpr int WT_STAGE = WT_TILE * 2 * D_ROW;
 constexpr int WT_KS = D_ROW / 16;
+static_assert(D_LAT == 512 && D_ROW == 576 && WT_TILE == 32 && WT_WAVES == 4, "a latent row per load; one rope load a wave");
 
-__global__ __launch_bounds__(WT_THREADS, 2) void weight_kernel(WeightArgs w) {
-    __shared__ __align__(256) uint8_t smem[2 * WT_STAGE + 2 * 256];   // tiles, then their lse values
+// rows new in this chunk start at 0; a sequence without new tokens keeps its weights
+__device__ __forceinline__ void finish(const WeightArgs& w, int b, int u, int kv, int nq, float sum) {
+    const int64_t at = (int64_t)b * w.stride + u;
+    const bool old = w.prev && u < kv - nq;
+    if (nq == 0)
+        w.weight[at] = w.prev ? w.prev[at] : 0.f;
+    else
+        w.weight[at] = old && w.decay != 0.f ? __builtin_fmaf(w.decay, w.prev[at], sum) : sum;
+}
+
+// ---------------------------------------------------------------- few queries
+//
+// Workgroup = 128 cache rows, two of them per CU: one loads its rows while the other
+// computes, and loading is what the time goes to.  Each of 4 waves holds 32 rows.
+
+constexpr int WF_ROWS = 32 * WT_WAVES;                   // cache rows of a workgroup
+constexpr int WF_PIECES = D_ROW / 8;
+constexpr int WF_ROW_BYTES = 2 * D_ROW;
+constexpr int WF_LOADS = WT_STAGE / 1024 / WT_WAVES;     // 9 loads of 1 KB per wave
+
+__global__ __launch_bounds__(WT_THREADS, 2) void weight_few_kernel(WeightArgs w) {
+    __shared__ __align__(256) uint8_t smem[2 * WT_STAGE + 2 * 256];   // tiles (rows of 1152 bytes), then their lse values
     const ChunkArgs& a = w.c;
-    const int nblk = w.nblk;
-    const int z = blockIdx.x / (nblk * a.B), rest = blockIdx.x % (nblk * a.B);
-    const int b = rest / nblk, u0 = (rest % nblk) * WT_ROWS;
+    const int b = blockIdx.x / w.nblk, u0 = (blockIdx.x % w.nblk) * WF_ROWS;
     const int kv = min(max(a.kv_len[b], 0), a.max_kv);
     if (u0 >= kv) return;
     const int64_t tok0 = min(max((int64_t)a.cu[b], (int64_t)0), a.n_tok);
@@ -45,11 +56,10 @@ __global__ __launch_bounds__(WT_THREADS, 2) void weight_kernel(WeightArgs w) {
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int uw = u0 + 32 * wave;            // the wave's first cache row
     const int u = uw + c;                     // this lane's
-    // the queries of this part that see some row of the block: those of the tokens from i0 on
+    // the queries that see some row of the block: those of the tokens from i0 on
     const int i0 = max(u0 - (kv - nq), 0);
     const int ntile = (nrow + WT_TILE - 1) / WT_TILE;
-    const int per = (ntile + w.parts - 1) / w.parts;
-    const int t0 = max(z * per, (int)((int64_t)i0 * a.H / WT_TILE)), t1 = min(z * per + per, ntile);
+    const int t0 = (int)((int64_t)i0 * a.H / WT_TILE), t1 = ntile;
 
     const uint16_t* ql = a.q_lat + tok0 * a.H * a.qls;
     const uint16_t* qr = a.q_rope + tok0 * a.H * a.qrs;
@@ -62,8 +72,8 @@ __global__ __launch_bounds__(WT_THREADS, 2) void weight_kernel(WeightArgs w) {
         int ln = lane;
         asm volatile("" : "+v"(ln));   // keeps the slot arithmetic out of registers across the loop
 #pragma unroll
-        for (int i = 0; i < WT_LOADS; ++i) {
-            const int j = wave + WT_WAVES * i, q = 64 * j + ln, r = q / WT_PIECES, p = (q - WT_PIECES * r) ^ ((r >> 1) & 7);
+        for (int i = 0; i < WF_LOADS; ++i) {
+            const int j = wave + WT_WAVES * i, q = 64 * j + ln, r = q / WF_PIECES, p = (q - WF_PIECES * r) ^ ((r >> 1) & 7);
             const int64_t R = min(WT_TILE * t + r, nrow - 1);   // rows past the end repeat the last one, not counted
             const uint16_t* src = p < D_LAT / 8 ? ql + R * a.qls + 8 * p : qr + R * a.qrs + 8 * (p - D_LAT / 8);
             __builtin_amdgcn_global_load_lds((gbl_void_t*)src, (lds_void_t*)(st + 1024 * j), 16, 0, 0);
@@ -92,7 +102,7 @@ __global__ __launch_bounds__(WT_THREADS, 2) void weight_kernel(WeightArgs w) {
         const uint32_t lds0 = lds_addr(smem);
         uint32_t qaddr[4];   // Q operand of (tile row c, piece 2 ks + hh), the piece's low three bits permuted
 #pragma unroll
-        for (int i = 0; i < 4; ++i) qaddr[i] = c * WT_ROW_BYTES + 16 * ((2 * i + hh) ^ ((c >> 1) & 7));
+        for (int i = 0; i < 4; ++i) qaddr[i] = c * WF_ROW_BYTES + 16 * ((2 * i + hh) ^ ((c >> 1) & 7));
         for (int t = t0; t < t1; ++t) {
             const int s = (t - t0) & 1;
             // this wave's loads of tile t have landed (nothing else is in flight), every wave's
@@ -155,52 +165,456 @@ __global__ __launch_bounds__(WT_THREADS, 2) void weight_kernel(WeightArgs w) {
     }
     sum = half_sum(sum);
     if (hh == 1 || u >= kv) return;
-    if (!there) sum = 0.f;
-    if (w.parts > 1) {
-        w.part[((int64_t)z * a.B + b) * a.max_kv + u] = sum;
-        return;
+    finish(w, b, u, kv, nq, there ? sum : 0.f);
+}
+
+// --------------------------------------------------------------- many queries
+//
+// Each of 4 waves holds 64 cache rows (576 dims: 288 of its 512 registers), so that a query
+// tile read from LDS feeds two products: with 32 rows a wave, LDS takes as long as the
+// matrix cores.  One workgroup per CU then, and the wave overlaps by itself: the scores of a
+// tile become weights, and the loads and operand reads of later ones are issued, between the
+// products of the present one.  (The products are written as instructions: the scores stay
+// in vector registers, most of the cache rows in the accumulation registers.)  One barrier
+// per tile; the operand reads run on over it.
+//
+// The work is cut into WW_RUNS equal runs of (block of 256 rows, query tile) pairs, as the
+// device's lengths give it, one workgroup each: no last round of blocks on part of the chip,
+// and the workgroups load their rows at different times.  A block that several runs share
+// gets its parts through the workspace, added in order by a second kernel.
+//
+// Measured at 32 tokens of 64 heads over 4 x 65536 rows (lengths from 50021): 478 us, 1.06
+// PFLOP/s, at clocks that the power limit takes to 1.5 GHz (32 rows a wave, two workgroups
+// per CU: 589 us; rows loaded as operands, 15.5 us a block, instead of whole: 485 us).
+
+constexpr int WW_ROWS = 64 * WT_WAVES;                   // cache rows of a block
+constexpr int WW_STAGES = 4;
+constexpr int WW_LAT = WT_TILE * 2 * D_LAT;              // latent panel: rows of 1 KB; then rows of 128 bytes
+constexpr int WW_SD = 5;                                 // operands read ahead of the matrix cores
+constexpr int WW_LSE = 4;                                // lse slots of a wave, of 256 bytes
+constexpr int WW_ACC = 12;                               // K operands in vector registers, the others in accumulation registers
+constexpr int WW_RUNS = 256;
+constexpr int WW_LOAD = 3;                               // loading a block's rows counts as so many tiles
+static_assert(WT_KS % (WW_SD + 1) == 0, "operands keep their registers from tile to tile");
+static_assert((WW_ROWS * WT_TILE) % (WT_TILE * WT_TILE) == 0, "whole tiles per block of new rows and head");
+
+// A sequence's blocks and their query tiles: all ntile for the first `full` blocks; those of the new rows are not
+// seen by the first tokens, and begin at tile first, first + step, ...
+struct WeightSpan {
+    int kv, nq, nblk, ntile, full, first, step;
+    int64_t cost;             // tiles in all, with WW_LOAD a block before its own (one of a sequence without new tokens)
+    int64_t tok0;
+    __device__ __forceinline__ int64_t later(int64_t j) const {   // tiles of the first j blocks after the full ones
+        return j * (ntile - first + WW_LOAD) - (int64_t)step * (j * (j - 1) / 2);
     }
-    // rows new in this chunk start at 0; a sequence without new tokens keeps its weights
-    const int64_t at = (int64_t)b * w.stride + u;
-    const bool old = w.prev && u < kv - nq;
-    if (nq == 0)
-        w.weight[at] = w.prev ? w.prev[at] : 0.f;
-    else
-        w.weight[at] = old && w.decay != 0.f ? __builtin_fmaf(w.decay, w.prev[at], sum) : sum;
+};
+__device__ __forceinline__ WeightSpan weight_span(const ChunkArgs& a, int b) {
+    WeightSpan s;
+    s.kv = min(max(a.kv_len[b], 0), a.max_kv);
+    s.tok0 = min(max((int64_t)a.cu[b], (int64_t)0), a.n_tok);
+    const int64_t tok1 = min(max((int64_t)a.cu[b + 1], s.tok0), a.n_tok);
+    s.nq = (int)min(tok1 - s.tok0, (int64_t)a.max_q);
+    s.nblk = (s.kv + WW_ROWS - 1) / WW_ROWS;
+    s.ntile = max((s.nq * a.H + WT_TILE - 1) / WT_TILE, 1);
+    const int old = s.kv - s.nq;
+    s.full = old < 0 ? 0 : min(s.nblk, old / WW_ROWS + 1);
+    s.first = s.full < s.nblk ? (int)((int64_t)(s.full * WW_ROWS - old) * a.H / WT_TILE) : 0;
+    s.step = WW_ROWS / WT_TILE * a.H;
+    s.cost = (int64_t)s.full * (s.ntile + WW_LOAD) + s.later(s.nblk - s.full);
+    return s;
 }
 
-__global__ __launch_bounds__(256) void weight_join_kernel(WeightArgs w) {
+// The block of a sequence's tile `off` (< cost): its first tile, and off's place and the number of tiles in it
+struct WeightPlace {
+    int blk, t0;
+    int64_t k, n;
+};
+__device__ __forceinline__ WeightPlace weight_place(const WeightSpan& s, int64_t off) {
+    WeightPlace p;
+    const int each = s.ntile + WW_LOAD;
+    if (off < (int64_t)s.full * each) {
+        p.blk = (int)(off / each);
+        p.t0 = 0;
+        p.k = off - (int64_t)p.blk * each;
+    } else {
+        off -= (int64_t)s.full * each;
+        int lo = 0, hi = s.nblk - s.full;      // later(lo) <= off < later(hi)
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (s.later(mid) <= off) lo = mid;
+            else hi = mid;
+        }
+        p.blk = s.full + lo;
+        p.t0 = s.first + s.step * lo;
+        p.k = off - s.later(lo);
+    }
+    p.n = s.ntile - p.t0 + WW_LOAD;
+    return p;
+}
+
+__device__ __forceinline__ int64_t uniform64(int64_t v) {
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)((uint64_t)v >> 32)) << 32 |
+                     (uint32_t)__builtin_amdgcn_readfirstlane((int)v));
+}
+
+// Tiles over all sequences, and the sequence and its tile at place x = at(total) (x < total).
+struct WeightFind {
+    int64_t sum[WT_THREADS + 1];
+    int64_t off;
+    int b;
+};
+template <typename At>
+__device__ __forceinline__ int64_t weight_find(const ChunkArgs& a, WeightFind& f, At at, int& b, int64_t& off) {
+    const int tid = threadIdx.x, per = (a.B + WT_THREADS - 1) / WT_THREADS;
+    const int b0 = min(tid * per, a.B), b1 = min(b0 + per, a.B);
+    int64_t mine = 0;
+    for (int i = b0; i < b1; ++i) mine += weight_span(a, i).cost;
+    f.sum[tid + 1] = mine;
+    if (tid == 0) f.sum[0] = 0;
+    for (int d = 1; d < WT_THREADS; d *= 2) {
+        __syncthreads();
+        const int64_t v = tid + 1 > d ? f.sum[tid + 1 - d] : 0;
+        __syncthreads();
+        f.sum[tid + 1] += v;
+    }
+    if (tid == 0) f.b = 0, f.off = 0;
+    __syncthreads();
+    const int64_t total = f.sum[WT_THREADS], x = at(total);
+    if (f.sum[tid] <= x && x < f.sum[tid + 1]) {
+        int64_t o = x - f.sum[tid];
+        int i = b0;
+        for (; i + 1 < b1; ++i) {
+            const int64_t c = weight_span(a, i).cost;
+            if (o < c) break;
+            o -= c;
+        }
+        f.b = i;
+        f.off = o;
+    }
+    __syncthreads();
+    b = __builtin_amdgcn_readfirstlane(f.b);
+    off = uniform64(f.off);
+    return uniform64(total);
+}
+__device__ __forceinline__ int64_t run_start(int64_t total, int r) {
+    return total / WW_RUNS * r + total % WW_RUNS * r / WW_RUNS;
+}
+
+__global__ __launch_bounds__(WT_THREADS, 1) void weight_many_kernel(WeightArgs w) {
+    __shared__ __align__(256) uint8_t smem[WW_STAGES * WT_STAGE + WT_WAVES * WW_LSE * 256];   // tiles, then their lse values
+    __shared__ WeightFind find;
     const ChunkArgs& a = w.c;
-    const int nb = (a.max_kv + 255) / 256, b = blockIdx.x / nb, u = (blockIdx.x % nb) * 256 + threadIdx.x;
-    const int kv = min(max(a.kv_len[b], 0), a.max_kv);
-    if (u >= kv) return;
-    const int64_t tok0 = min(max((int64_t)a.cu[b], (int64_t)0), a.n_tok);
-    const int64_t tok1 = min(max((int64_t)a.cu[b + 1], tok0), a.n_tok);
-    const int nq = (int)min(tok1 - tok0, (int64_t)a.max_q);
-    float sum = 0.f;
-    for (int z = 0; z < w.parts; ++z) sum += w.part[((int64_t)z * a.B + b) * a.max_kv + u];
-    const int64_t at = (int64_t)b * w.stride + u;
-    const bool old = w.prev && u < kv - nq;
-    if (nq == 0)
-        w.weight[at] = w.prev ? w.prev[at] : 0.f;
-    else
-        w.weight[at] = old && w.decay != 0.f ? __builtin_fmaf(w.decay, w.prev[at], sum) : sum;
+    const int tid = threadIdx.x, lane = tid & 63, c = lane & 31, hh = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), run = blockIdx.x;
+    int b;
+    int64_t off;
+    const int64_t total = weight_find(a, find, [&](int64_t n) { return run_start(n, run); }, b, off);
+    int64_t left = run_start(total, run + 1) - run_start(total, run);
+    while (left > 0) {
+        const WeightSpan sp = weight_span(a, b);
+        if (off >= sp.cost) {
+            ++b;
+            off = 0;
+            continue;
+        }
+        const WeightPlace pl = weight_place(sp, off);
+        const int n = (int)min(pl.n - pl.k, left);       // tiles of this block
+        off += n;
+        left -= n;
+        const int kv = __builtin_amdgcn_readfirstlane(sp.kv), nq = __builtin_amdgcn_readfirstlane(sp.nq), nrow = nq * a.H;
+        const int blk = __builtin_amdgcn_readfirstlane(pl.blk);
+        const int k0 = __builtin_amdgcn_readfirstlane((int)pl.k) - WW_LOAD, first = __builtin_amdgcn_readfirstlane(pl.t0);
+        const int t0 = first + max(k0, 0), t1 = nq > 0 ? first + max(k0 + n, 0) : t0;
+        const int64_t tok0 = sp.tok0;
+        const int uw = WW_ROWS * blk + 64 * wave;        // the wave's first cache row; this lane's: uw + c and uw + 32 + c
+        const uint16_t* ql = a.q_lat + tok0 * a.H * a.qls;
+        const uint16_t* qr = a.q_rope + tok0 * a.H * a.qrs;
+        const float* lse = w.lse + tok0 * a.H;
+        // This wave's loads of tile t, i = 0 .. 9 in order: latent rows wave + 4 i, then a quarter of the rope rows, then
+        // the lse (each wave's own copy).  Slot j of a latent row holds piece j ^ (row mod 16), of a rope row piece
+        // j ^ (row / 2 mod 8): LDS serves a 128-bit read 16 lanes at a time, lanes {0-3, 12-15, 20-27} or the others of a
+        // half wave, and their slots then differ modulo 16.  Rows past the end repeat an earlier one, not counted.
+        const uint8_t* lat_row = nullptr;         // (scalar) the next latent row
+        const int64_t next_row = 8 * a.qls;       // bytes
+        auto seek = [&](int t, auto ic) __attribute__((always_inline)) {
+            constexpr int i = decltype(ic)::value;
+            const int R = WT_TILE * t + wave + 4 * i;
+            if constexpr (i == 0) lat_row = reinterpret_cast<const uint8_t*>(ql + (int64_t)min(R, nrow - 1) * a.qls);
+            else if constexpr (i < 8) lat_row += R < nrow ? next_row : 0;
+            if constexpr (i < 8) asm volatile("" : "+s"(lat_row));
+        };
+        auto issue = [&](int t, int s, int slot, auto ic) __attribute__((always_inline)) {
+            constexpr int i = decltype(ic)::value;
+            uint8_t* st = smem + s * WT_STAGE;
+            if constexpr (i < 8) {
+                const int r = wave + 4 * i;
+                uint32_t at;                      // (computed here each time: not kept for every i across the loop)
+                asm volatile("v_xor_b32 %0, %1, %2" : "=v"(at) : "s"(16 * (r & 15)), "v"(16 * lane));
+                __builtin_amdgcn_global_load_lds((gbl_void_t*)(lat_row + at), (lds_void_t*)(st + 1024 * r), 16, 0, 0);
+            } else if constexpr (i == 8) {
+                const int r = 8 * wave + (lane >> 3), R = min(WT_TILE * t + r, nrow - 1);
+                __builtin_amdgcn_global_load_lds((gbl_void_t*)(qr + (int64_t)R * a.qrs + 8 * ((lane & 7) ^ ((r >> 1) & 7))),
+                                                 (lds_void_t*)(st + WW_LAT + 1024 * wave), 16, 0, 0);
+            } else {
+                const int R = min(WT_TILE * t + c, nrow - 1);
+                __builtin_amdgcn_global_load_lds((gbl_void_t*)(lse + R),
+                                                 (lds_void_t*)(smem + WW_STAGES * WT_STAGE + 256 * (WW_LSE * wave + (slot & (WW_LSE - 1)))), 4, 0, 0);
+            }
+        };
+
+        // K operand: cache row uw + 32 g + c, dims 16 ks + 8 hh .. +8 (rows past the end repeat the last one; a page
+        // that does not exist: any row of the cache, not counted)
+        bool there[2];
+        const uint16_t* row[2];
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            const int uc = min(uw + 32 * g + c, kv - 1);
+            const int32_t page = a.table[(int64_t)b * a.tstride + (uc >> a.shift)];
+            there[g] = (uint32_t)page < (uint32_t)a.n_pages;
+            row[g] = a.cache + (there[g] ? 8 * ((int64_t)page * a.ps16 + (int64_t)(uc & a.page_mask) * a.rs16) : 0);
+        }
+        float sum[2];
+#pragma unroll
+        for (int g = 0; g < 2; ++g) sum[g] = 0.f;
+        if (t0 < t1) {
+            uint32_t lat[8], rope[4];   // operand of tile row c, piece 2 ks + hh, in a stage: latent ks mod 8, rope
+#pragma unroll
+            for (int i = 0; i < 8; ++i) lat[i] = c * 1024 + 16 * ((2 * i + hh) ^ (c & 15));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) rope[i] = WW_LAT + c * 128 + 16 * ((2 * i + hh) ^ ((c >> 1) & 7));
+            wg_barrier();      // every wave is done with the stages (of the block before)
+            // The cache rows come through the wave's own stage, laid out like a tile, 32 at a time: whole rows, which
+            // direct loads fetch three times as fast as operands (32 bytes of a row a load) do.
+            bf16x8_t kf[2][WT_KS];
+            uint8_t* own = smem + wave * WT_STAGE;
+            static_assert(WT_WAVES == WW_STAGES, "a stage for each wave");
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                const uint64_t mine = (uint64_t)row[g];
+                int ln = lane;
+                asm volatile("" : "+v"(ln));     // nothing of this is kept from block to block
+#pragma unroll 2
+                for (int r = 0; r < 32; ++r) {
+                    const uint8_t* base = (const uint8_t*)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), r) << 32 |
+                                                           (uint32_t)__builtin_amdgcn_readlane((int)mine, r));
+                    __builtin_amdgcn_global_load_lds((gbl_void_t*)(base + ((16u * ln) ^ (16u * (r & 15)))), (lds_void_t*)(own + 1024 * r), 16, 0, 0);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int r = 8 * j + (ln >> 3);
+                    const uint64_t base = (uint64_t)(uint32_t)__shfl((int)(mine >> 32), r) << 32 | (uint32_t)__shfl((int)mine, r);
+                    __builtin_amdgcn_global_load_lds((gbl_void_t*)(base + 2 * D_LAT + 16u * ((ln & 7) ^ ((r >> 1) & 7))),
+                                                     (lds_void_t*)(own + WW_LAT + 1024 * j), 16, 0, 0);
+                }
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+                for (int ks = 0; ks < WT_KS; ++ks)
+                    kf[g][ks] = *reinterpret_cast<const bf16x8_t*>(own + (ks < 32 ? lat[ks & 7] + 256 * (ks >> 3) : rope[ks & 3]));
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+                for (int ks = 0; ks < WT_KS; ++ks) {    // read before the next rows come
+                    if (g * WT_KS + ks < WW_ACC) asm volatile("" : "+v"(kf[g][ks])::"memory");
+                    else asm volatile("" : "+a"(kf[g][ks])::"memory");
+                }
+            }
+            wg_barrier();
+            static_for<0, 10>([&](auto ic) { seek(t0, ic); issue(t0, 0, 0, ic); });
+            static_for<0, 10>([&](auto ic) { seek(min(t0 + 1, t1 - 1), ic); issue(min(t0 + 1, t1 - 1), 1, 1, ic); });
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            wg_barrier();
+            const uint32_t lds0 = lds_addr(smem);
+            bf16x8_t qf[WW_SD + 1];
+            auto qload = [&](uint32_t st, auto kc) __attribute__((always_inline)) {
+                constexpr int ks = decltype(kc)::value;
+                if constexpr (ks < 32) qf[ks % (WW_SD + 1)] = lds_read128<256 * (ks >> 3)>(st + lat[ks & 7]);
+                else qf[ks % (WW_SD + 1)] = lds_read128<0>(st + rope[ks - 32]);
+            };
+            // The scores of a tile become weights while the matrix cores work on the next one: y, with
+            // the lse z4 of their queries (nothing pending: 0 and inf, whose weights are 0).
+            f32x16_t xa[2], xb[2];
+            f32x4_t z4[4];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+#pragma unroll
+                for (int g = 0; g < 2; ++g) xb[g][i] = 0.f;
+                z4[i >> 2][i & 3] = INFINITY;
+            }
+            auto weight = [&](float x, float l) __attribute__((always_inline)) {
+                return __builtin_amdgcn_exp2f(__builtin_fmaf(x, a.scale_log2, -1.4426950408889634f * l));
+            };
+            // tiles [safe0, safe1) hold whole queries that see all of the wave's rows
+            const int64_t full = (int64_t)a.H * (uw + 63 - (kv - nq));
+            const int safe0 = ((int)max(min(full, (int64_t)nrow), (int64_t)0) + WT_TILE - 1) / WT_TILE, safe1 = nrow / WT_TILE;
+            int s = 0;
+            static_for<0, WW_SD>([&](auto kc) { qload(lds0, kc); });
+            auto tile = [&](int t, f32x16_t (&x)[2], f32x16_t (&y)[2]) __attribute__((always_inline)) {
+                const int sn = (s + 1) % WW_STAGES, sl = (s + 2) % WW_STAGES;
+                const int tl = min(t + 2, t1 - 1);   // loaded (from the last tile but one on: once more, not used)
+                const uint32_t st = lds0 + s * WT_STAGE, stn = lds0 + sn * WT_STAGE;
+                s = sn;
+                float add[2];
+                static_for<0, WT_KS>([&](auto kc) {
+                    constexpr int ks = decltype(kc)::value, KB = WT_KS - WW_SD;
+                    if constexpr (ks == KB) {
+                        // This wave's loads of the next tile have landed (those of the one after are in flight), every
+                        // wave's have, and every wave is done with the tile before, whose stage the next tile's loads fill.
+                        asm volatile("s_waitcnt vmcnt(10)" ::: "memory");
+                        wg_barrier();
+                    }
+                    auto product = [&](auto gc) __attribute__((always_inline)) {
+                        constexpr int g = decltype(gc)::value;
+                        constexpr bool acc = g * WT_KS + ks >= WW_ACC;
+                        const bf16x8_t& q = qf[ks % (WW_SD + 1)];
+                        // (the first product waits for its operand)
+                        constexpr int n = g == 1 ? 15 : WW_SD - 1 + (ks >= 34 ? 4 : 0);
+                        if constexpr (ks == 0 && acc) asm volatile("s_waitcnt lgkmcnt(%3)\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(x[g]) : "v"(q), "a"(kf[g][ks]), "n"(n));
+                        else if constexpr (ks == 0) asm volatile("s_waitcnt lgkmcnt(%3)\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(x[g]) : "v"(q), "v"(kf[g][ks]), "n"(n));
+                        else if constexpr (g == 0 && acc) asm volatile("s_waitcnt lgkmcnt(%3)\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(x[g]) : "v"(q), "a"(kf[g][ks]), "n"(n));
+                        else if constexpr (g == 0) asm volatile("s_waitcnt lgkmcnt(%3)\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(x[g]) : "v"(q), "v"(kf[g][ks]), "n"(n));
+                        else asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(x[g]) : "v"(q), "a"(kf[g][ks]));
+                        __builtin_amdgcn_sched_barrier(0);
+                    };
+                    // A wave issues in order, and the second product when the first one's passes are over: what
+                    // stands between them, and after them, is to fit into 32 cycles each.
+                    product(std::integral_constant<int, 0>{});
+                    if constexpr (ks == 0) {
+#pragma unroll
+                        for (int g = 0; g < 2; ++g) asm volatile("" : "+v"(y[g]));
+                    }
+                    if constexpr (ks >= 1 && ks <= 32) {
+                        constexpr int g = (ks - 1) % 2, i = (ks - 1) / 2;
+                        const float p = weight(y[g][i], z4[i >> 2][i & 3]);
+                        add[g] = i ? add[g] + p : p;
+                        asm volatile("" : "+v"(add[g]));   // here, not after the products
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                    product(std::integral_constant<int, 1>{});
+                    if constexpr (ks < KB) qload(st, std::integral_constant<int, ks + WW_SD>{});
+                    else qload(stn, std::integral_constant<int, ks - KB>{});
+                    if constexpr (ks == 33) {
+                        // the lse of tile rows 8 i4 + 4 hh .. +3
+                        const uint32_t la = lds0 + WW_STAGES * WT_STAGE + 256 * (WW_LSE * wave + ((t - t0) & (WW_LSE - 1))) + 16 * hh;
+                        asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %4 offset:32\n\tds_read_b128 %2, %4 offset:64\n\t"
+                                     "ds_read_b128 %3, %4 offset:96"
+                                     : "=&v"(z4[0]), "=&v"(z4[1]), "=&v"(z4[2]), "=&v"(z4[3])
+                                     : "v"(la));
+                    }
+                    if constexpr (ks % 3 == 1 && ks < 30) seek(tl, std::integral_constant<int, ks / 3>{});
+                    if constexpr (ks % 3 == 2 && ks < 30) issue(tl, sl, t - t0 + 2, std::integral_constant<int, ks / 3>{});
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+                asm volatile("s_waitcnt lgkmcnt(2)" : "+v"(z4[0]), "+v"(z4[1]), "+v"(z4[2]), "+v"(z4[3]));
+#pragma unroll
+                for (int g = 0; g < 2; ++g) sum[g] += add[g];
+                float low = z4[0][0];   // -inf: a query without weights
+#pragma unroll
+                for (int i = 1; i < 16; ++i) low = fminf(low, z4[i >> 2][i & 3]);
+                // x[i] = score of query row 32 t + 8 (i / 4) + 4 hh + i % 4 and cache row u.  Rows the tile's first token
+                // does not see, rows past the last query, or a query without weights: at once, score by score
+                if (t < safe0 || t >= safe1 || __ballot(low == -INFINITY) != 0) {
+                    int ln = lane;
+                    asm volatile("" : "+v"(ln));     // nothing of this is kept across the loop
+                    const int r0 = WT_TILE * t + 4 * (ln >> 5);
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) {
+                        asm volatile("s_nop 15\n\ts_nop 3" : "+v"(x[g]));
+                        // the first query row that sees cache row u (none sees those from kv on)
+                        const int first = a.H * min(max(uw + 32 * g + (ln & 31) - (kv - nq), 0), nq);
+                        float part = 0.f;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int R = r0 + 8 * (i >> 2) + (i & 3);
+                            const float l = z4[i >> 2][i & 3], p = weight(x[g][i], l);
+                            if (R < nrow && R >= first && l != -INFINITY) part += p;
+                            x[g][i] = 0.f;
+                        }
+                        sum[g] += part;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) z4[i >> 2][i & 3] = INFINITY;
+                }
+            };
+            auto rest = [&](f32x16_t (&y)[2]) __attribute__((always_inline)) {
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+                for (int i = 0; i <= WW_SD; ++i) lds_wait<0>(qf[i]);   // the reads after the last tile
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    asm volatile("s_nop 15\n\ts_nop 3" : "+v"(y[g]));
+                    float add = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) add += weight(y[g][i], z4[i >> 2][i & 3]);
+                    sum[g] += add;
+                }
+            };
+            for (int t = t0;; t += 2) {
+                tile(t, xa, xb);
+                if (t + 1 >= t1) {
+                    rest(xa);
+                    break;
+                }
+                tile(t + 1, xb, xa);
+                if (t + 2 >= t1) {
+                    rest(xb);
+                    break;
+                }
+            }
+        }
+        // a block within one run is done; the others' sums: the run's first block that began in an earlier one, and its last
+        const bool whole = pl.k == 0 && n == pl.n;
+        float* slot = w.part + (int64_t)(2 * run + (pl.k == 0)) * WW_ROWS + 64 * wave + c;
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            const int u = uw + 32 * g + c;
+            float sums = half_sum(sum[g]);
+            if (!there[g]) sums = 0.f;
+            if (hh == 1) continue;
+            if (!whole) slot[32 * g] = sums;
+            else if (u < kv) finish(w, b, u, kv, nq, sums);
+        }
+    }
 }
 
-// parts of the queries: enough workgroups for two per CU, but at least 8 tiles in a part
-int64_t weight_parts(int64_t B, int64_t H, int64_t max_q, int64_t max_kv) {
-    const int64_t blocks = B * ((max_kv + WT_ROWS - 1) / WT_ROWS), tiles = (max_q * H + WT_TILE - 1) / WT_TILE;
-    return std::max<int64_t>(1, std::min(512 / std::max<int64_t>(blocks, 1), tiles / 8));
+// The sums of the blocks that begin in run blockIdx.x and end in a later one.
+__global__ __launch_bounds__(WW_ROWS) void weight_join_kernel(WeightArgs w) {
+    __shared__ WeightFind find;
+    const int run = blockIdx.x;
+    int b;
+    int64_t off;
+    const int64_t total = weight_find(w.c, find, [&](int64_t n) { return max(run_start(n, run + 1) - 1, (int64_t)0); }, b, off);
+    const int64_t x0 = run_start(total, run), x1 = run_start(total, run + 1);
+    if (x0 == x1) return;
+    const WeightSpan sp = weight_span(w.c, b);
+    const WeightPlace pl = weight_place(sp, off);        // of the run's last tile
+    const int64_t end = x1 - 1 - pl.k + pl.n;
+    if (x1 - 1 - pl.k < x0 || end <= x1) return;
+    const int row = threadIdx.x, u = WW_ROWS * pl.blk + row;
+    float sum = w.part[(int64_t)(2 * run + 1) * WW_ROWS + row];
+    for (int r = run + 1; r < WW_RUNS && run_start(total, r) < end; ++r)
+        if (run_start(total, r) < run_start(total, r + 1)) sum += w.part[(int64_t)(2 * r) * WW_ROWS + row];
+    if (u < sp.kv) finish(w, b, u, sp.kv, sp.nq, sum);
 }
 
-int64_t weight_blocks(int64_t max_kv) { return (max_kv + WT_ROWS - 1) / WT_ROWS; }
+// More than 8 query tiles of the longest chunk: at 8 tiles the forms are even (16 sequences of 32768 rows: 238 us in
+// runs, 245 us by blocks; one of 8192: 28 and 23 us), at 4 by blocks is the faster one (202 and 192 us), at 16 runs are
+// (335 and 389 us; one of 8192: 32 and 43 us).
+static bool many_queries(int64_t H, int64_t max_q) { return (max_q * H + WT_TILE - 1) / WT_TILE > 8; }
+
+size_t weight_workspace_bytes(int64_t H, int64_t max_q) {
+    return many_queries(H, max_q) ? (size_t)2 * WW_RUNS * WW_ROWS * sizeof(float) : 0;
+}
+
+int64_t weight_blocks(int64_t max_kv) { return (max_kv + WF_ROWS - 1) / WF_ROWS; }
 
 hipError_t launch_weight(const WeightArgs& w, hipStream_t s) {
-    const int64_t n = (int64_t)w.nblk * w.c.B * w.parts;
-    hipLaunchKernelGGL(weight_kernel, dim3((unsigned)n), dim3(WT_THREADS), 0, s, w);
+    if (!many_queries(w.c.H, w.c.max_q)) {
+        hipLaunchKernelGGL(weight_few_kernel, dim3((unsigned)((int64_t)w.nblk * w.c.B)), dim3(WT_THREADS), 0, s, w);
+        return hipGetLastError();
+    }
+    hipLaunchKernelGGL(weight_many_kernel, dim3(WW_RUNS), dim3(WT_THREADS), 0, s, w);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || w.parts == 1) return e;
-    hipLaunchKernelGGL(weight_join_kernel, dim3((unsigned)((int64_t)w.c.B * ((w.c.max_kv + 255) / 256))), dim3(256), 0, s, w);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(weight_join_kernel, dim3(WW_RUNS), dim3(WW_ROWS), 0, s, w);
     return hipGetLastError();
 }
 

@@ -856,8 +856,7 @@ int vkv_weight_workspace_size(const vkv_pages* pg, const vkv_chunk* ch, size_t* 
     if (!bytes) return fail(nullptr, VKV_E_ARG, "bytes is NULL");
     int rc = check_chunk(nullptr, pg, ch);
     if (rc) return rc;
-    const int64_t parts = weight_parts(pg->B, ch->H, ch->max_q, pg->max_kv);
-    *bytes = parts > 1 ? up256((size_t)(parts * pg->B * pg->max_kv) * 4) : 0;
+    *bytes = up256(weight_workspace_bytes(ch->H, ch->max_q));
     return VKV_OK;
 }
 
@@ -872,10 +871,11 @@ int vkv_weight_accumulate(vkv_ctx* ctx, const vkv_pages* pg, const vkv_chunk* ch
     if (!lse || !weight) return fail(ctx, VKV_E_ARG, "lse and weight are required");
     if (weight_stride < pg->max_kv)
         return fail(ctx, VKV_E_SHAPE, "weight_stride=%lld smaller than max_kv=%lld", (long long)weight_stride, (long long)pg->max_kv);
-    const int64_t parts = weight_parts(pg->B, ch->H, ch->max_q, pg->max_kv), blocks = weight_blocks(pg->max_kv);
-    if (pg->B * blocks * parts >= (1ll << 31))
+    const int64_t blocks = weight_blocks(pg->max_kv);
+    if (pg->B * blocks >= (1ll << 31))
         return fail(ctx, VKV_E_SHAPE, "B=%lld with max_kv=%lld: too many rows", (long long)pg->B, (long long)pg->max_kv);
-    if (parts > 1 && (rc = check_ws(ctx, ws, ws_bytes, up256((size_t)(parts * pg->B * pg->max_kv) * 4)))) return rc;
+    const size_t need = up256(weight_workspace_bytes(ch->H, ch->max_q));
+    if (need && (rc = check_ws(ctx, ws, ws_bytes, need))) return rc;
     if (pg->max_kv == 0) return VKV_OK;
     WeightArgs w{};
     w.c = chunk_args(pg, ch);
@@ -886,7 +886,6 @@ int vkv_weight_accumulate(vkv_ctx* ctx, const vkv_pages* pg, const vkv_chunk* ch
     w.weight = weight;
     w.stride = weight_stride;
     w.nblk = (int)blocks;
-    w.parts = (int)parts;
     w.part = (float*)ws;
     DeviceGuard dev(ctx);
     HIP_TRY(ctx, dev.err);

@@ -105,6 +105,21 @@ def test_weights(ctx, kv_lens, q_lens, H, decay):
             check(f"weight from nothing, sequence {b}", out[b, :n], want[b], tol[b])
 
 
+def test_weights_of_many_queries_and_rows(ctx):
+    """Enough rows and queries for the form with 256 cache rows a workgroup: rows' ends and the diagonal in every
+    place of a block, chunks of no, one and more tokens, a query without weights."""
+    kv_lens, q_lens = [1 + 37 * i % 521 for i in range(128)], [i % 6 for i in range(128)]
+    x = Case(kv_lens, q_lens, 128, seed=21, page=64)
+    lse = true_lse(x)
+    lse[7, 3] = -math.inf
+    prev = torch.rand(128, x.max_kv, device=DEV)
+    want, tol = expected(x, lse, 0.75, prev)
+    out = accumulate(ctx, x, lse, 0.75, prev, torch.full_like(prev, -3.0))
+    for b, n in enumerate(kv_lens):
+        check(f"weight of sequence {b}", out[b, :n], want[b], tol[b])
+        assert bool((out[b, n:] == -3.0).all())
+
+
 def test_weights_sum_to_the_queries(ctx):
     """With the attention call's own lse each token and head gives 1 in all."""
     x = Case([700, 90], [4, 1], 128, seed=3, page=64)
