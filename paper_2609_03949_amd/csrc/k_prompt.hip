@@ -50,22 +50,42 @@ __device__ __forceinline__ int vpiece_xor(int r) {
     return DV == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
 }
 
-// one panel of a tile: D columns of PR_KEYS rows, this wave's share (1 KB per load)
-template <int D, typename XOR>
-__device__ __forceinline__ void load_panel(const uint16_t* base, int64_t ts, int t0, int len, uint8_t* st, int wave,
-                                           int lane, XOR xr) {
-    constexpr int PC = D / 8;                     // pieces per row
-    constexpr int RPL = 64 / PC;                  // rows per load
-    constexpr int NL = PR_KEYS * PC / 64 / PR_WAVES;
-    const int r0 = RPL * wave + lane / PC;        // row of the first load; the i-th one RPL * PR_WAVES * i on
-    const int piece = (lane % PC) ^ xr(r0);       // the same for every i: xr has a period of RPL * PR_WAVES rows
-#pragma unroll
-    for (int i = 0; i < NL; ++i) {
-        const int row = min(t0 + r0 + RPL * PR_WAVES * i, len - 1);   // rows past the end repeat the last one
-        const uint16_t* src = base + row * ts + 8 * piece;
-        __builtin_amdgcn_global_load_lds((gbl_void_t*)src, (lds_void_t*)(st + 1024 * (wave + PR_WAVES * i)), 16, 0, 0);
+// One panel of a tile: D columns of PR_KEYS rows, this wave's share (1 KB per load).  A lane
+// keeps the offset of its row and piece of the first load; the rest of the address is scalar
+// but in a sequence's last tile, whose rows past the end repeat the last one (address
+// arithmetic in the lanes took as long as the exponentials).
+template <int D>
+struct PanelLoader {
+    static constexpr int PC = D / 8;              // pieces per row
+    static constexpr int RPL = 64 / PC;           // rows per load
+    static constexpr int NL = PR_KEYS * PC / 64 / PR_WAVES;
+    const uint8_t* base;
+    int64_t row_bytes, off;
+    int r0, wave;                                 // row of the first load; the i-th one RPL * PR_WAVES * i on
+    template <typename XOR>
+    __device__ __forceinline__ PanelLoader(const uint16_t* b, int64_t ts, int wave_, int lane, XOR xr)
+        : base(reinterpret_cast<const uint8_t*>(b)), row_bytes(2 * ts), r0(RPL * wave_ + lane / PC), wave(wave_) {
+        off = r0 * row_bytes + 16 * ((lane % PC) ^ xr(r0));   // the piece is the same for every i: xr has a period of RPL * PR_WAVES rows
     }
-}
+    __device__ __forceinline__ void load(int t0, int len, uint8_t* st) const {
+        const uint8_t* tile = base + t0 * row_bytes;
+        if (t0 + PR_KEYS <= len) {
+#pragma unroll
+            for (int i = 0; i < NL; ++i)
+                __builtin_amdgcn_global_load_lds((gbl_void_t*)(tile + RPL * PR_WAVES * i * row_bytes + off),
+                                                 (lds_void_t*)(st + 1024 * (wave + PR_WAVES * i)), 16, 0, 0);
+        } else {
+            int first = r0;
+            asm volatile("" : "+v"(first));       // nothing of this is kept across the tiles
+#pragma unroll 1
+            for (int i = 0; i < NL; ++i) {
+                const int row = first + RPL * PR_WAVES * i;
+                __builtin_amdgcn_global_load_lds((gbl_void_t*)(tile + off + (int64_t)(min(row, len - 1 - t0) - first) * row_bytes),
+                                                 (lds_void_t*)(st + 1024 * (wave + PR_WAVES * i)), 16, 0, 0);
+            }
+        }
+    }
+};
 
 // One block: SAFE false is the ordinary pass.  A masked key has weight 0, and 0 times
 // a value that is not finite is not 0, so such a value would reach rows that do not see
@@ -104,13 +124,15 @@ __device__ __forceinline__ bool prompt_block(const PromptArgs& a, uint8_t* smem)
     const int ntile = (min(len, q0 + PR_ROWS) + PR_KEYS - 1) / PR_KEYS;
 
     const uint16_t* kb = a.k + start * a.kts + (int64_t)g * a.khs;
-    const uint16_t* rb = DR ? a.kr + start * a.rts : nullptr;
     const uint16_t* vb = a.v + start * a.vts + (int64_t)g * a.vhs;
+    const PanelLoader<DN> kpanel(kb, a.kts, wave, lane, kpiece_xor<DN>);
+    const PanelLoader<DR ? DR : 64> rpanel(DR ? a.kr + start * a.rts : kb, a.rts, wave, lane, kpiece_xor<DR ? DR : 64>);
+    const PanelLoader<DV> vpanel(vb, a.vts, wave, lane, vpiece_xor<DV>);
     auto issue = [&](int t) {
         uint8_t* st = smem + (t & 1) * STAGE;
-        load_panel<DN>(kb, a.kts, PR_KEYS * t, len, st, wave, lane, kpiece_xor<DN>);
-        if constexpr (DR > 0) load_panel<DR>(rb, a.rts, PR_KEYS * t, len, st + OFF_R, wave, lane, kpiece_xor<DR>);
-        load_panel<DV>(vb, a.vts, PR_KEYS * t, len, st + OFF_V, wave, lane, vpiece_xor<DV>);
+        kpanel.load(PR_KEYS * t, len, st);
+        if constexpr (DR > 0) rpanel.load(PR_KEYS * t, len, st + OFF_R);
+        vpanel.load(PR_KEYS * t, len, st + OFF_V);
     };
 
     // Q^T operand: query qi, dims 16 ks + 8 hh .. +8 (rows past the end repeat the last one, never stored)
