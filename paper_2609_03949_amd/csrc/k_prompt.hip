@@ -89,8 +89,8 @@ struct PanelLoader {
 
 // One block: SAFE false is the ordinary pass.  A masked key has weight 0, and 0 times
 // a value that is not finite is not 0, so such a value would reach rows that do not see
-// it.  That shows in the result: the block then stores nothing and returns true, and
-// goes again with SAFE, which takes the values that are not finite apart in the tiles
+// it.  That shows in the result: the block then returns true and goes again with SAFE,
+// over what it stored, which takes the values that are not finite apart in the tiles
 // that hold masked keys, and keeps the weights small (by a power of two: all else has
 // the same bits), as those above 1 may have made a sum overflow.
 template <int DN, int DR, int DV, bool SAFE>
@@ -101,7 +101,7 @@ __device__ __forceinline__ bool prompt_block(const PromptArgs& a, uint8_t* smem)
 
     // the longest blocks first; with 8 | H every XCD takes H / 8 neighbouring heads of
     // each sequence (workgroups go to the XCDs in turn), which share K and V in its L2
-    const int64_t npair = (int64_t)a.n_seq * a.H;
+    const uint32_t npair = (uint32_t)a.n_seq * (uint32_t)a.H;     // (the grid is below 2^31)
     const int qb = a.nqb - 1 - (int)(blockIdx.x / npair);
     const int p = (int)(blockIdx.x % npair);
     int b = p / a.H, h = p % a.H;
@@ -142,6 +142,8 @@ __device__ __forceinline__ bool prompt_block(const PromptArgs& a, uint8_t* smem)
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8_t*>(src + 16 * ks);
     }
+    if constexpr (SAFE) wg_barrier();   // every wave has read the others' words (below)
+    issue(0);
     // consume the query loads here, so no wait for them lands inside the tile loop
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[ks]));
@@ -173,7 +175,6 @@ __device__ __forceinline__ bool prompt_block(const PromptArgs& a, uint8_t* smem)
             for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
         m_run = -INFINITY;
         l_run = 0.f;
-        issue(0);
         for (int t = 0; t < ntile; ++t) {
             // this wave's loads of tile t have landed (nothing else is in flight), every wave's
             // have, and every wave is done with tile t - 1, whose stage is loaded next
@@ -293,39 +294,41 @@ __device__ __forceinline__ bool prompt_block(const PromptArgs& a, uint8_t* smem)
         }
         l_run = half_sum(l_run);
     }
+    // the workgroup's waves share the tiles, so they go again together; each one's word lies in
+    // the stage of the last tile but one, which every wave was done with before the last
+    const uint32_t word = lds0 + (ntile & 1) * STAGE;
     if constexpr (!SAFE) {
         float top = 0.f;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) top += fabsf(o[dt][i]) * 0x1p-40f;   // not finite where an output is not
-        // the workgroup's waves share the tiles, so they go again together; the flag lies
-        // in the stages, which nobody reads any more
-        __syncthreads();
-        uint32_t* flag = reinterpret_cast<uint32_t*>(smem);
-        if (tid == 0) *flag = 0;
-        __syncthreads();
-        if (!(top < INFINITY)) *flag = 1;
-        __syncthreads();
-        const bool again = *flag != 0;
-        __syncthreads();
-        if (again) return true;
+            for (int i = 0; i < 16; ++i) top = __builtin_fmaf(fabsf(o[dt][i]), 0x1p-40f, top);   // not finite where an output is not
+        const uint32_t again = __ballot(!(top < INFINITY)) != 0;
+        asm volatile("ds_write_b32 %0, %1" ::"v"(word + 4 * wave), "v"(again) : "memory");
     }
-    if (qi >= len) return false;
-    const float inv = (1.0f / l_run) * (SAFE ? 1.0f / PR_ROOM : 1.0f);
-    uint16_t* out = a.out + ((start + qi) * a.H + h) * DV + 4 * hh;
+    if (qi < len) {
+        const float inv = (1.0f / l_run) * (SAFE ? 1.0f / PR_ROOM : 1.0f);
+        uint16_t* out = a.out + ((start + qi) * a.H + h) * DV + 4 * hh;
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
+        for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-        for (int i4 = 0; i4 < 4; ++i4) {
-            typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
-            const bf16x4_t v = {(__bf16)(o[dt][4 * i4] * inv), (__bf16)(o[dt][4 * i4 + 1] * inv),
-                                (__bf16)(o[dt][4 * i4 + 2] * inv), (__bf16)(o[dt][4 * i4 + 3] * inv)};
-            *reinterpret_cast<bf16x4_t*>(out + 32 * dt + 8 * i4) = v;
-        }
-    if (hh == 0) a.lse[(start + qi) * a.H + h] = (m_run + log2f(l_run)) * 0.69314718055994530942f;
-    return false;
+            for (int i4 = 0; i4 < 4; ++i4) {
+                typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+                const bf16x4_t v = {(__bf16)(o[dt][4 * i4] * inv), (__bf16)(o[dt][4 * i4 + 1] * inv),
+                                    (__bf16)(o[dt][4 * i4 + 2] * inv), (__bf16)(o[dt][4 * i4 + 3] * inv)};
+                *reinterpret_cast<bf16x4_t*>(out + 32 * dt + 8 * i4) = v;
+            }
+        if (hh == 0) a.lse[(start + qi) * a.H + h] = (m_run + log2f(l_run)) * 0.69314718055994530942f;
+    }
+    if constexpr (SAFE) return false;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");    // (no wait for the stores)
+    wg_barrier();
+    f32x4_t words;
+    asm volatile("ds_read_b128 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(words) : "v"(word) : "memory");
+    const uint32_t any = __float_as_uint(words[0]) | __float_as_uint(words[1]) | __float_as_uint(words[2]) | __float_as_uint(words[3]);
+    return __builtin_amdgcn_readfirstlane(any) != 0;
 }
+static_assert(PR_WAVES == 4, "four words");
 
 // a call, so that the rare block's registers are not the ordinary one's; by value, so
 // that nothing of the ordinary one has an address
