@@ -186,20 +186,21 @@ __device__ __forceinline__ float lse_of(float m, float l) {
     return m == -INFINITY && l == 0.f ? -INFINITY : ((m == -INFINITY ? 0.f : m) + log2f(l)) * 0.69314718055994530942f;
 }
 
-// this lane's dims 16 dt + 4 g .. +3 of output row `row` from f times what o holds, and
-// its lse; rows that see nothing: 0, -inf
+// this lane's dims 16 dt + 4 g .. +3 of output row `row` (dt = at(0) .. at(N - 1)) from f times what
+// o holds, and its lse if `first`; rows that see nothing: 0, -inf
+template <int N, typename At>
 __device__ __forceinline__ void store_row(const ChunkArgs& a, int64_t row, int g, float m, float l, float f,
-                                          const f32x4_t* o) {
+                                          const f32x4_t (&o)[N], At at, bool first) {
     const bool none = m == -INFINITY && l == 0.f;
     const float inv = none ? 0.f : (1.0f / l) * f;
     uint16_t* out = a.out + row * D_LAT + 4 * g;
 #pragma unroll
-    for (int dt = 0; dt < CK_DT; ++dt) {
-        const bf16x4_t v = {(__bf16)(o[dt][0] * inv), (__bf16)(o[dt][1] * inv), (__bf16)(o[dt][2] * inv),
-                            (__bf16)(o[dt][3] * inv)};
-        *reinterpret_cast<bf16x4_t*>(out + 16 * dt) = v;
+    for (int i = 0; i < N; ++i) {
+        const bf16x4_t v = {(__bf16)(o[i][0] * inv), (__bf16)(o[i][1] * inv), (__bf16)(o[i][2] * inv),
+                            (__bf16)(o[i][3] * inv)};
+        *reinterpret_cast<bf16x4_t*>(out + 16 * at(i)) = v;
     }
-    if (g == 0) a.lse[row] = lse_of(m, l);
+    if (g == 0 && first) a.lse[row] = lse_of(m, l);
 }
 
 // Tiles [t0, t1) of unit x by one workgroup.  part: where an incomplete unit's
@@ -407,10 +408,47 @@ __device__ __forceinline__ bool chunk_segment(const ChunkArgs& a, const CkUnit& 
     }
     l_run = allreduce_groups(l_run, [](float p, float q) { return p + q; });
 
-    // ---- the streams of a row join in the first one's wave, through the stages
+    // ---- the streams of a row join, each wave a part of the dims: its dim blocks of the first half, then of the second
     __syncthreads();
-    float* fl = reinterpret_cast<float*>(smem);
-    if constexpr (KSTR > 1) {
+    constexpr int NO = CK_DT / KSTR;             // dim blocks of a wave in the end
+    auto block_of = [&](int i) { return KSTR == 1 ? i : 16 * (i / (NO / 2)) + NO / 2 * ks0 + i % (NO / 2); };
+    auto finish = [&](const f32x4_t (&o)[NO]) __attribute__((always_inline)) {
+        if constexpr (!SAFE) {
+            float top = 0.f;
+#pragma unroll
+            for (int j = 0; j < NO; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top = __builtin_fmaf(fabsf(o[j][i]), 0x1p-40f, top);   // not finite where an output is not
+            uint32_t* words = reinterpret_cast<uint32_t*>(smem);   // in the stages, which nobody reads any more
+            const bool bad = __ballot(!idle && !(top < INFINITY)) != 0;
+            if (lane == 0) words[wave] = bad;
+            __syncthreads();
+            uint32_t any = 0;
+#pragma unroll
+            for (int i = 0; i < CK_WAVES; ++i) any |= words[i];
+            if (__builtin_amdgcn_readfirstlane(any) != 0) {
+                __syncthreads();   // every wave has read the words
+                return true;
+            }
+        }
+        if (idle) return false;
+        if (part_o) {
+            float* po = part_o + qg * (16 * D_LAT);
+#pragma unroll
+            for (int j = 0; j < NO; ++j) *reinterpret_cast<f32x4_t*>(po + (block_of(j) * 64 + lane) * 4) = o[j];
+            if (g == 0 && ks0 == 0) {
+                part_ml[2 * (16 * qg + c)] = m_run;
+                part_ml[2 * (16 * qg + c) + 1] = SAFE ? -l_run : l_run;
+            }
+        } else if (R < x.nrow) {
+            store_row(a, x.tok0 * a.H + R, g, m_run, l_run, SAFE ? 1.0f / CK_ROOM : 1.0f, o, block_of, ks0 == 0);
+        }
+        return false;
+    };
+    if constexpr (KSTR == 1) {
+        return finish(o);
+    } else {
+        float* fl = reinterpret_cast<float*>(smem);
         float* sml = fl + CK_OFF_ML / 4;
         if (g == 0) {
             sml[2 * (16 * wave + c)] = m_run;
@@ -426,67 +464,42 @@ __device__ __forceinline__ bool chunk_segment(const ChunkArgs& a, const CkUnit& 
             const float m = sml[2 * (16 * (qg + QG * j) + c)], l = sml[2 * (16 * (qg + QG * j) + c) + 1];
             L += m == -INFINITY ? l : weight(m) * l;   // nothing seen: l is 0, or NaN from a score that is NaN
         }
-        if (m_run != -INFINITY) {   // (without one, o is 0, or NaN)
-            const float w = weight(m_run);
-#pragma unroll
-            for (int dt = 0; dt < CK_DT; ++dt)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) o[dt][i] *= w;
-        }
+        const float w = m_run == -INFINITY ? 1.0f : weight(m_run);   // (without a maximum, o is 0, or NaN)
         m_run = M;
         l_run = L;
-        constexpr int WO = 16 * D_LAT;   // floats of a wave's O
-        auto put = [&](float* dst) {
+        // blocks of 1 KB: [row group][stream][16 dim blocks]
+        f32x4_t sum[NO];
+        float* rows = fl + qg * (KSTR * 16 * 256) + lane * 4;
 #pragma unroll
-            for (int dt = 0; dt < CK_DT; ++dt) *reinterpret_cast<f32x4_t*>(dst + (dt * 64 + lane) * 4) = o[dt];
-        };
-        auto add = [&](const float* src) {
+        for (int half = 0; half < 2; ++half) {
+            if (!idle) {
 #pragma unroll
-            for (int dt = 0; dt < CK_DT; ++dt) {
-                const f32x4_t v = *reinterpret_cast<const f32x4_t*>(src + (dt * 64 + lane) * 4);
+                for (int d = 0; d < 16; ++d) {
+                    f32x4_t v = o[16 * half + d];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) o[dt][i] += v[i];
+                    for (int i = 0; i < 4; ++i) v[i] *= w;
+                    *reinterpret_cast<f32x4_t*>(rows + (ks0 * 16 + d) * 256) = v;
+                }
             }
-        };
-#pragma unroll
-        for (int half = CK_WAVES / 2; half >= QG; half /= 2) {
-            if (wave >= half && wave < 2 * half) put(fl + (wave - half) * WO);
             __syncthreads();
-            if (wave < half) add(fl + wave * WO);
+            if (!idle) {
+#pragma unroll
+                for (int k = 0; k < NO / 2; ++k) {
+                    f32x4_t v[KSTR];
+#pragma unroll
+                    for (int j = 0; j < KSTR; ++j)
+                        v[j] = *reinterpret_cast<const f32x4_t*>(rows + (j * 16 + NO / 2 * ks0 + k) * 256);
+#pragma unroll
+                    for (int j = 1; j < KSTR; ++j)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) v[0][i] += v[j][i];
+                    sum[NO / 2 * half + k] = v[0];
+                }
+            }
             __syncthreads();
         }
+        return finish(sum);
     }
-    const bool mine = ks0 == 0 && !idle;
-    if constexpr (!SAFE) {
-        float top = 0.f;
-        if (mine)
-#pragma unroll
-            for (int dt = 0; dt < CK_DT; ++dt)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) top += fabsf(o[dt][i]) * 0x1p-40f;   // not finite where an output is not
-        uint32_t* flag = reinterpret_cast<uint32_t*>(smem);   // in the stages, which nobody reads any more
-        if (tid == 0) *flag = 0;
-        __syncthreads();
-        if (!(top < INFINITY)) *flag = 1;
-        __syncthreads();
-        const bool again = *flag != 0;
-        __syncthreads();
-        if (again) return true;
-    }
-    if (!mine) return false;
-    if (part_o) {
-        float* po = part_o + qg * (16 * D_LAT);
-#pragma unroll
-        for (int dt = 0; dt < CK_DT; ++dt) *reinterpret_cast<f32x4_t*>(po + (dt * 64 + lane) * 4) = o[dt];
-        if (g == 0) {
-            part_ml[2 * (16 * qg + c)] = m_run;
-            part_ml[2 * (16 * qg + c) + 1] = SAFE ? -l_run : l_run;
-        }
-        return false;
-    }
-    if (R >= x.nrow) return false;
-    store_row(a, x.tok0 * a.H + R, g, m_run, l_run, SAFE ? 1.0f / CK_ROOM : 1.0f, o);
-    return false;
 }
 
 // ------------------------------------------------------------------- kernels
