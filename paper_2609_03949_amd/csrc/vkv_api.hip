@@ -49,6 +49,7 @@ static int fail(vkv_ctx* ctx, int code, const char* fmt, ...) {
     } while (0)
 
 static inline bool al16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+static inline bool al4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
 static inline size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
 
 // Makes the context's device the current one for a call and puts the caller's back.
@@ -697,6 +698,7 @@ int vkv_prompt_attend(vkv_ctx* ctx, const vkv_prompt* pr, float scale, uint16_t*
         return fail(ctx, VKV_E_ARG, "q, k, v, cu, out and lse are required, and k_rope iff dr > 0");
     if (!al16(pr->q) || !al16(pr->k) || !al16(pr->v) || !al16(pr->k_rope) || !al16(out))
         return fail(ctx, VKV_E_ALIGN, "q, k, k_rope, v and out must be 16-byte aligned");
+    if (!al4(pr->cu) || !al4(lse)) return fail(ctx, VKV_E_ALIGN, "cu and lse must be 4-byte aligned");
     for (int64_t st : {pr->q_tok_stride, pr->q_head_stride, pr->k_tok_stride, pr->k_head_stride, pr->v_tok_stride,
                        pr->v_head_stride, pr->dr > 0 ? pr->k_rope_tok_stride : (int64_t)0})
         if (st < 0 || st % 8) return fail(ctx, VKV_E_ALIGN, "stride %lld: need a multiple of 8, at least 0", (long long)st);
@@ -744,7 +746,7 @@ static int check_pages(vkv_ctx* ctx, const vkv_pages* pg) {
         return fail(ctx, VKV_E_UNSUPPORTED, "page=%d: need a power of two in [1, 65536]", pg->page);
     if (!pg->cache || !pg->table || !pg->kv_len) return fail(ctx, VKV_E_ARG, "cache, table and kv_len are required");
     if (!al16(pg->cache)) return fail(ctx, VKV_E_ALIGN, "cache must be 16-byte aligned");
-    if (((uintptr_t)pg->table & 3u) || ((uintptr_t)pg->kv_len & 3u))
+    if (!al4(pg->table) || !al4(pg->kv_len))
         return fail(ctx, VKV_E_ALIGN, "table and kv_len must be 4-byte aligned");
     if (pg->row_stride < D_ROW || pg->row_stride % 8)
         return fail(ctx, VKV_E_ALIGN, "row_stride=%lld: need >= 576 and a multiple of 8", (long long)pg->row_stride);
@@ -771,6 +773,7 @@ static int check_chunk(vkv_ctx* ctx, const vkv_pages* pg, const vkv_chunk* ch) {
                     (long long)ch->H, (long long)pg->B);
     if (!ch->q_lat || !ch->q_rope || !ch->cu) return fail(ctx, VKV_E_ARG, "q_lat, q_rope and cu are required");
     if (!al16(ch->q_lat) || !al16(ch->q_rope)) return fail(ctx, VKV_E_ALIGN, "q_lat and q_rope must be 16-byte aligned");
+    if (!al4(ch->cu)) return fail(ctx, VKV_E_ALIGN, "cu must be 4-byte aligned");
     if (ch->q_lat_stride < 0 || ch->q_lat_stride % 8 || ch->q_rope_stride < 0 || ch->q_rope_stride % 8)
         return fail(ctx, VKV_E_ALIGN, "query strides %lld, %lld: need multiples of 8, at least 0", (long long)ch->q_lat_stride,
                     (long long)ch->q_rope_stride);
@@ -825,7 +828,7 @@ int vkv_chunk_attend(vkv_ctx* ctx, const vkv_pages* pg, const vkv_chunk* ch, voi
     if (rc) return rc;
     if (bad_scale(scale)) return fail(ctx, VKV_E_ARG, "scale must be positive and finite");
     if (!out || !lse) return fail(ctx, VKV_E_ARG, "out and lse are required");
-    if (!al16(out)) return fail(ctx, VKV_E_ALIGN, "out must be 16-byte aligned");
+    if (!al16(out) || !al4(lse)) return fail(ctx, VKV_E_ALIGN, "out must be 16-byte aligned, lse 4-byte");
     const ChunkSplit sp = chunk_split(pg->B, ch->H, ch->max_q, pg->max_kv);
     size_t po, pml, span;
     const size_t need = chunk_layout(sp, &po, &pml, &span);
@@ -869,6 +872,7 @@ int vkv_weight_accumulate(vkv_ctx* ctx, const vkv_pages* pg, const vkv_chunk* ch
     if (bad_scale(scale)) return fail(ctx, VKV_E_ARG, "scale must be positive and finite");
     if (!(decay >= 0.f) || !(decay < 1e30f)) return fail(ctx, VKV_E_ARG, "decay must be finite and >= 0");
     if (!lse || !weight) return fail(ctx, VKV_E_ARG, "lse and weight are required");
+    if (!al4(lse) || !al4(prev) || !al4(weight)) return fail(ctx, VKV_E_ALIGN, "lse, prev and weight must be 4-byte aligned");
     if (weight_stride < pg->max_kv)
         return fail(ctx, VKV_E_SHAPE, "weight_stride=%lld smaller than max_kv=%lld", (long long)weight_stride, (long long)pg->max_kv);
     const int64_t blocks = weight_blocks(pg->max_kv);
@@ -906,6 +910,8 @@ int vkv_weight_select(vkv_ctx* ctx, const float* weight, int64_t B, int64_t max_
         return fail(ctx, VKV_E_ARG, "nsink=%lld and recent=%lld: need >= 0 and at most keep=%lld together", (long long)nsink,
                     (long long)recent, (long long)keep);
     if (!weight || !kv_len || !kept || !count) return fail(ctx, VKV_E_ARG, "weight, kv_len, kept and count are required");
+    if (!al4(weight) || !al4(kv_len) || !al4(kept) || !al4(count))
+        return fail(ctx, VKV_E_ALIGN, "weight, kv_len, kept and count must be 4-byte aligned");
     WeightSelArgs a{};
     a.weight = weight;
     a.stride = weight_stride;
@@ -931,6 +937,8 @@ int vkv_cache_evict(vkv_ctx* ctx, const vkv_pages* pg, const int32_t* kept, cons
     if (rc) return rc;
     if (keep < 1 || keep > (1ll << 30)) return fail(ctx, VKV_E_ARG, "keep=%lld outside [1, 2^30]", (long long)keep);
     if (!kept || !count) return fail(ctx, VKV_E_ARG, "kept and count are required");
+    if (!al4(kept) || !al4(count) || !al4(origin) || !al4(weight) || !al4(weight_out))
+        return fail(ctx, VKV_E_ALIGN, "kept, count, origin, weight and weight_out must be 4-byte aligned");
     if ((weight != nullptr) != (weight_out != nullptr)) return fail(ctx, VKV_E_ARG, "weight and weight_out go together");
     if (weight && weight_stride < pg->max_kv)
         return fail(ctx, VKV_E_SHAPE, "weight_stride=%lld smaller than max_kv=%lld", (long long)weight_stride, (long long)pg->max_kv);

@@ -226,3 +226,22 @@ def test_evict_refusals(vkv, ctx, change, code):
     assert vkv.load().vkv_cache_evict(ctx, ctypes.byref(pg), a["kept"], a["count"], a["keep"], a["origin"], a["weight"],
                                       a["weight_stride"], a["weight_out"], None) == code
     assert vkv.load().vkv_cache_evict(None, None, None, None, 1, None, None, 0, None, None) == -1
+
+
+def test_misaligned_words_are_refused(vkv, ctx):
+    """Offsets, lengths, statistics and tables that do not lie on a multiple of 4 bytes."""
+    odd = FAKE + 2
+    assert prompt(vkv, ctx, cu=odd) == -3 and prompt(vkv, ctx, lse=odd) == -3
+    assert chunk(vkv, ctx, dict(cu=odd)) == -3 and chunk(vkv, ctx, {}, lse=odd) == -3
+    assert chunk(vkv, ctx, dict(table=odd)) == -3 and chunk(vkv, ctx, dict(kv_len=odd)) == -3
+    for k in ("lse", "prev", "weight"):
+        assert weights(vkv, ctx, {}, **{k: odd}) == -3
+    for k in ("weight", "kv_len", "kept", "count"):
+        a = dict(SELECT, **{k: odd})
+        assert vkv.load().vkv_weight_select(ctx, a["weight"], a["B"], a["max_kv"], a["weight_stride"], a["kv_len"], a["keep"],
+                                            a["nsink"], a["recent"], a["kept"], a["count"], None) == -3
+    pg = make(vkv._Pages, PAGES)
+    for k in ("kept", "count", "origin", "weight", "weight_out"):
+        a = dict(EVICT, **{k: odd})
+        assert vkv.load().vkv_cache_evict(ctx, ctypes.byref(pg), a["kept"], a["count"], a["keep"], a["origin"], a["weight"],
+                                          a["weight_stride"], a["weight_out"], None) == -3

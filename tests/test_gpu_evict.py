@@ -120,6 +120,27 @@ def test_weights_of_many_queries_and_rows(ctx):
         assert bool((out[b, n:] == -3.0).all())
 
 
+@pytest.mark.parametrize("kv_lens,q_lens,H", [
+    ([1, 0, 255, 256, 257, 0, 512, 513], [40, 3, 0, 33, 1, 0, 17, 64], 16),     # around the blocks of 256 rows
+    ([1], [300], 1),                                                            # one row, seen by the last token alone
+    ([700], [700], 5),                                                          # a whole prompt, blocks of fewer and fewer tiles
+    ([2049, 1, 300], [9, 1, 0], 128),                                           # blocks shared by many runs
+    ([600] * 3, [0, 300, 0], 1),
+])
+def test_weights_in_runs(ctx, kv_lens, q_lens, H):
+    """More than 8 tiles of queries: equal runs over blocks of 256 cache rows, blocks shared by several runs."""
+    x = Case(kv_lens, q_lens, H, seed=H + 3, page=16)
+    lse = true_lse(x)
+    prev = torch.rand(len(kv_lens), x.max_kv + 3, device=DEV)
+    want, tol = expected(x, lse, 0.5, prev)
+    first = accumulate(ctx, x, lse, 0.5, prev, torch.full_like(prev, -3.0))
+    for b, n in enumerate(kv_lens):
+        check(f"weight of sequence {b}", first[b, :n], want[b], tol[b])
+        assert bool((first[b, n:] == -3.0).all())
+    again = accumulate(ctx, x, lse, 0.5, prev, torch.full_like(prev, -3.0))
+    assert torch.equal(first, again)
+
+
 def test_weights_sum_to_the_queries(ctx):
     """With the attention call's own lse each token and head gives 1 in all."""
     x = Case([700, 90], [4, 1], 128, seed=3, page=64)
@@ -155,6 +176,78 @@ def test_weights_ignore_what_is_not_seen(ctx):
     x.cache[pages[149], r[149]] = math.nan
     out = accumulate(ctx, x, lse, 0.0, None, torch.zeros(1, 150, device=DEV))
     assert torch.equal(out[0, :149], clean[0, :149]) and bool(torch.isnan(out[0, 149]))
+
+
+def test_weights_in_runs_of_absent_pages_and_dead_queries(ctx):
+    """The same in blocks of 256 rows: pages that do not exist (their rows' place holds NaN), queries without weights."""
+    x = Case([600, 64], [30, 12], 16, seed=6, page=16)
+    lse = true_lse(x)
+    lse[0, 3], lse[29, 15], lse[31] = -math.inf, -math.inf, -math.inf
+    x.table[0, 2], x.table[0, 20], x.table[1, 1] = -1, 1 << 28, x.cache.shape[0]
+    x.cache[0] = math.nan
+    absent = [torch.zeros(600, dtype=torch.bool), torch.zeros(64, dtype=torch.bool)]
+    absent[0][32:48] = absent[0][320:336] = absent[1][16:32] = True
+    for b, n in enumerate((600, 64)):      # the sequence that has page 0 of the cache loses it too
+        absent[b] |= (x.where[b][0] == 0).cpu()
+        x.table[b][x.table[b] == 0] = -1
+    prev = torch.rand(2, 600, device=DEV)
+    for b in range(2):
+        pages, r = x.where[b]
+        x.cache[pages[absent[b].to(DEV)], r[absent[b].to(DEV)]] = 0.0      # for the reference; the kernel does not read them
+    want, tol = expected(x, lse, 0.5, prev, absent)
+    x.cache[0] = math.nan
+    out = accumulate(ctx, x, lse, 0.5, prev, torch.zeros_like(prev))
+    for b, n in enumerate((600, 64)):
+        check(f"weight of sequence {b}", out[b, :n], want[b], tol[b])
+
+
+def test_weights_in_runs_ignore_what_is_not_seen(ctx):
+    """NaN in later tokens' rows and behind the end stays there; queries that are parts of wider rows; pages far apart."""
+    x = Case([400], [40], 16, seed=7)
+    lse = true_lse(x)
+    clean = accumulate(ctx, x, lse, 0.0, None, torch.zeros(1, 400, device=DEV))
+    pages, r = x.where[0]
+    x.cache[pages[399], r[399]] = math.nan
+    out = accumulate(ctx, x, lse, 0.0, None, torch.zeros(1, 400, device=DEV))
+    assert torch.equal(out[0, :399], clean[0, :399]) and bool(torch.isnan(out[0, 399]))
+    x.q_lat, x.q_rope = x.q[..., :512], x.q[..., 512:]
+    n = x.cache.shape[0]
+    step = (1 << 32) // (n - 1) // 8 * 8 + 8
+    far = torch.empty(step * (n - 1) + 16 * 576, dtype=torch.bfloat16, device=DEV).as_strided((n, 16, 576), (step, 576, 1))
+    far.copy_(x.cache)
+    x.cache = far
+    out = accumulate(ctx, x, lse, 0.0, None, torch.zeros(1, 400, device=DEV))
+    assert torch.equal(out[0, :399], clean[0, :399])
+
+
+def test_weights_in_runs_captured(ctx):
+    """Two graphs of the runs, a workspace each, replayed with other queries and lengths, against the eager call."""
+    x = Case([700, 300, 90], [24, 3, 0], 16, seed=8, max_q=24, max_kv=800)
+    lse = torch.randn(x.n_tok, 16, device=DEV) + 5.0
+    prev = torch.rand(3, 800, device=DEV)
+    pages, chunk = vkv.Pages(x.cache, x.table, x.kv_len, 800), vkv.Chunk(x.q_lat, x.q_rope, x.cu, 24)
+    graphs = []
+    accumulate(ctx, x, lse, 0.9, prev, torch.zeros(3, 800, device=DEV))
+    torch.cuda.synchronize()
+    for _ in range(2):
+        ws = torch.empty(vkv.weight_workspace_size(pages, chunk), dtype=torch.uint8, device=DEV)
+        out = torch.zeros(3, 800, device=DEV)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            vkv.weight_accumulate(ctx, pages, chunk, lse, ws, SCALE, 0.9, prev, out)
+        graphs.append((g, ws, out))
+    for rep in range(3):
+        gen = torch.Generator(device=DEV)
+        gen.manual_seed(70 + rep)
+        x.q_lat.copy_(torch.randn(x.q_lat.shape, generator=gen, device=DEV).to(torch.bfloat16))
+        x.kv_len.copy_(torch.tensor([700 - 150 * rep, 300 - rep, 90], dtype=torch.int32))
+        for g, _, out in graphs:
+            out.zero_()
+            g.replay()
+        torch.cuda.synchronize()
+        want = accumulate(ctx, x, lse, 0.9, prev, torch.zeros(3, 800, device=DEV))
+        for _, _, out in graphs:
+            assert torch.equal(out, want), rep
 
 
 # ----------------------------------------------------------------- selection
