@@ -4,15 +4,14 @@
 //   weight[u] = decay * prev[u] + sum_{i, h: u seen} exp(scale * (q_lat . c_u + q_rope . r_u) - lse_ih)
 //
 // The attention's log-sum-exp is given, so one product S = Q K^T and one
-// exponential per score are left.  Cache rows lie in a wave's registers as the B
-// operand and the queries pass by, tiles of 32 (token, head) rows through LDS
-// stages: a lane then has one cache row (its column) and 16 queries a tile, and
-// the sum over the queries is in-lane but for one swap of the lane halves at the
-// end.  Sums: fp32, 16 terms of a tile first, then over the tiles.  Nothing is
-// added atomically: the same inputs give the same bits.
+// exponential per score are left: a lane has one cache row (its column of the product) and
+// 16 queries a tile, so the sum over the queries is in-lane but for one swap of the lane
+// halves, and over tiles or waves.  With many queries the cache rows stay in registers and
+// the queries pass by, with few the other way round.  Sums: fp32, 16 terms of a tile first.
+// Nothing is added atomically: the same inputs give the same bits.
 #include <algorithm>
 
-#include "vkv_tile.h"
+#include "vkv_pages.h"
 
 namespace vkv {
 
@@ -25,147 +24,10 @@ static_assert(D_LAT == 512 && D_ROW == 576 && WT_TILE == 32 && WT_WAVES == 4, "a
 // rows new in this chunk start at 0; a sequence without new tokens keeps its weights
 __device__ __forceinline__ void finish(const WeightArgs& w, int b, int u, int kv, int nq, float sum) {
     const int64_t at = (int64_t)b * w.stride + u;
-    const bool old = w.prev && u < kv - nq;
     if (nq == 0)
         w.weight[at] = w.prev ? w.prev[at] : 0.f;
     else
-        w.weight[at] = old && w.decay != 0.f ? __builtin_fmaf(w.decay, w.prev[at], sum) : sum;
-}
-
-// ---------------------------------------------------------------- few queries
-//
-// Workgroup = 128 cache rows, two of them per CU: one loads its rows while the other
-// computes, and loading is what the time goes to.  Each of 4 waves holds 32 rows.
-
-constexpr int WF_ROWS = 32 * WT_WAVES;                   // cache rows of a workgroup
-constexpr int WF_PIECES = D_ROW / 8;
-constexpr int WF_ROW_BYTES = 2 * D_ROW;
-constexpr int WF_LOADS = WT_STAGE / 1024 / WT_WAVES;     // 9 loads of 1 KB per wave
-
-__global__ __launch_bounds__(WT_THREADS, 2) void weight_few_kernel(WeightArgs w) {
-    __shared__ __align__(256) uint8_t smem[2 * WT_STAGE + 2 * 256];   // tiles (rows of 1152 bytes), then their lse values
-    const ChunkArgs& a = w.c;
-    const int b = blockIdx.x / w.nblk, u0 = (blockIdx.x % w.nblk) * WF_ROWS;
-    const int kv = min(max(a.kv_len[b], 0), a.max_kv);
-    if (u0 >= kv) return;
-    const int64_t tok0 = min(max((int64_t)a.cu[b], (int64_t)0), a.n_tok);
-    const int64_t tok1 = min(max((int64_t)a.cu[b + 1], tok0), a.n_tok);
-    const int nq = (int)min(tok1 - tok0, (int64_t)a.max_q), nrow = nq * a.H;
-
-    const int tid = threadIdx.x, lane = tid & 63, c = lane & 31, hh = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int uw = u0 + 32 * wave;            // the wave's first cache row
-    const int u = uw + c;                     // this lane's
-    // the queries that see some row of the block: those of the tokens from i0 on
-    const int i0 = max(u0 - (kv - nq), 0);
-    const int ntile = (nrow + WT_TILE - 1) / WT_TILE;
-    const int t0 = (int)((int64_t)i0 * a.H / WT_TILE), t1 = ntile;
-
-    const uint16_t* ql = a.q_lat + tok0 * a.H * a.qls;
-    const uint16_t* qr = a.q_rope + tok0 * a.H * a.qrs;
-    const float* lse = w.lse + tok0 * a.H;
-    // this wave's loads of tile t: slot q = 72 r + p' holds piece p' ^ (r / 2 mod 8) of tile row r (LDS serves a
-    // 128-bit read 16 lanes at a time, lanes {0-3, 12-15, 20-27} or the others of a half wave: their slots differ
-    // modulo 16, odd rows lying 8 slots on)
-    auto issue = [&](int t, int s) {
-        uint8_t* st = smem + s * WT_STAGE;
-        int ln = lane;
-        asm volatile("" : "+v"(ln));   // keeps the slot arithmetic out of registers across the loop
-#pragma unroll
-        for (int i = 0; i < WF_LOADS; ++i) {
-            const int j = wave + WT_WAVES * i, q = 64 * j + ln, r = q / WF_PIECES, p = (q - WF_PIECES * r) ^ ((r >> 1) & 7);
-            const int64_t R = min(WT_TILE * t + r, nrow - 1);   // rows past the end repeat the last one, not counted
-            const uint16_t* src = p < D_LAT / 8 ? ql + R * a.qls + 8 * p : qr + R * a.qrs + 8 * (p - D_LAT / 8);
-            __builtin_amdgcn_global_load_lds((gbl_void_t*)src, (lds_void_t*)(st + 1024 * j), 16, 0, 0);
-        }
-        if (wave == 0) {
-            const int R = min(WT_TILE * t + c, nrow - 1);
-            __builtin_amdgcn_global_load_lds((gbl_void_t*)(lse + R), (lds_void_t*)(smem + 2 * WT_STAGE + 256 * s), 4, 0, 0);
-        }
-    };
-
-    // K operand: cache row u, dims 16 ks + 8 hh .. +8 (rows past the end repeat the last one; a page that
-    // does not exist: any row of the cache, not counted)
-    const int uc = min(u, kv - 1);
-    const int32_t page = a.table[(int64_t)b * a.tstride + (uc >> a.shift)];
-    const bool there = (uint32_t)page < (uint32_t)a.n_pages;
-    const uint16_t* row = a.cache + (there ? 8 * ((int64_t)page * a.ps16 + (int64_t)(uc & a.page_mask) * a.rs16) : 0) + 8 * hh;
-    float sum = 0.f;
-    if (t0 < t1) {
-        issue(t0, 0);
-        bf16x8_t kf[WT_KS];
-#pragma unroll
-        for (int ks = 0; ks < WT_KS; ++ks) kf[ks] = *reinterpret_cast<const bf16x8_t*>(row + 16 * ks);
-#pragma unroll
-        for (int ks = 0; ks < WT_KS; ++ks) asm volatile("" : "+v"(kf[ks]));   // no wait for them inside the tile loop
-
-        const uint32_t lds0 = lds_addr(smem);
-        uint32_t qaddr[4];   // Q operand of (tile row c, piece 2 ks + hh), the piece's low three bits permuted
-#pragma unroll
-        for (int i = 0; i < 4; ++i) qaddr[i] = c * WF_ROW_BYTES + 16 * ((2 * i + hh) ^ ((c >> 1) & 7));
-        for (int t = t0; t < t1; ++t) {
-            const int s = (t - t0) & 1;
-            // this wave's loads of tile t have landed (nothing else is in flight), every wave's
-            // have, and every wave is done with the stage loaded next
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            wg_barrier();
-            if (t + 1 < t1) issue(t + 1, s ^ 1);
-            const uint32_t st = lds0 + s * WT_STAGE;
-            f32x16_t x;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = 0.f;
-            // the lse of tile rows 8 i4 + 4 hh .. +3
-            f32x4_t z4[4];
-            const uint32_t la = lds0 + 2 * WT_STAGE + 256 * s + 16 * hh;
-            asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %4 offset:32\n\tds_read_b128 %2, %4 offset:64\n\t"
-                         "ds_read_b128 %3, %4 offset:96\n\ts_waitcnt lgkmcnt(0)"
-                         : "=&v"(z4[0]), "=&v"(z4[1]), "=&v"(z4[2]), "=&v"(z4[3])
-                         : "v"(la));
-            {
-                constexpr int SD = 4;   // operands read ahead of the matrix cores
-                bf16x8_t qf[SD + 1];
-                uint32_t qa[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) qa[i] = st + qaddr[i];
-                auto qload = [&](auto kc) {
-                    constexpr int ks = decltype(kc)::value;
-                    qf[ks % (SD + 1)] = lds_read128<128 * (ks >> 2)>(qa[ks & 3]);
-                };
-                static_for<0, SD>(qload);
-                static_for<0, WT_KS>([&](auto kc) {
-                    constexpr int ks = decltype(kc)::value;
-                    if constexpr (ks + SD < WT_KS) qload(std::integral_constant<int, ks + SD>{});
-                    lds_wait<(ks + SD < WT_KS) ? SD : (WT_KS - 1 - ks)>(qf[ks % (SD + 1)]);
-                    x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[ks % (SD + 1)], kf[ks], x, 0, 0, 0);
-                });
-            }
-            // x[i] = score of query row 32 t + 8 (i / 4) + 4 hh + i % 4 and cache row u
-            bool dead = false;   // a query without weights (its lse is -inf)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) dead |= z4[i >> 2][i & 3] == -INFINITY;
-            // rows the tile's first token does not see, rows past the last query, or such a query
-            const bool masked = uw + 31 > kv - nq + WT_TILE * t / a.H || WT_TILE * t + WT_TILE > nrow || __ballot(dead) != 0;
-            float add = 0.f;
-            if (masked) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int R = WT_TILE * t + 8 * (i >> 2) + 4 * hh + (i & 3);
-                    const float l = z4[i >> 2][i & 3];
-                    const bool seen = R < nrow && u <= kv - nq + R / a.H && l != -INFINITY;
-                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale_log2, -l * 1.4426950408889634f));
-                    if (seen) add += p;
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    add += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale_log2, -z4[i >> 2][i & 3] * 1.4426950408889634f));
-            }
-            sum += add;
-        }
-    }
-    sum = half_sum(sum);
-    if (hh == 1 || u >= kv) return;
-    finish(w, b, u, kv, nq, there ? sum : 0.f);
+        w.weight[at] = w.prev && w.decay != 0.f && u < kv - nq ? __builtin_fmaf(w.decay, w.prev[at], sum) : sum;
 }
 
 // --------------------------------------------------------------- many queries
@@ -257,21 +119,22 @@ __device__ __forceinline__ int64_t uniform64(int64_t v) {
                      (uint32_t)__builtin_amdgcn_readfirstlane((int)v));
 }
 
-// Tiles over all sequences, and the sequence and its tile at place x = at(total) (x < total).
+// The sum of cost(b) over all sequences; the sequence that holds place x = at(sum) (x < sum), and x's place in it.
+template <int THREADS>
 struct WeightFind {
-    int64_t sum[WT_THREADS + 1];
+    int64_t sum[THREADS + 1];
     int64_t off;
     int b;
 };
-template <typename At>
-__device__ __forceinline__ int64_t weight_find(const ChunkArgs& a, WeightFind& f, At at, int& b, int64_t& off) {
-    const int tid = threadIdx.x, per = (a.B + WT_THREADS - 1) / WT_THREADS;
-    const int b0 = min(tid * per, a.B), b1 = min(b0 + per, a.B);
+template <int THREADS, typename Cost, typename At>
+__device__ __forceinline__ int64_t weight_find(int B, WeightFind<THREADS>& f, Cost cost, At at, int& b, int64_t& off) {
+    const int tid = threadIdx.x, per = (B + THREADS - 1) / THREADS;
+    const int b0 = min(tid * per, B), b1 = min(b0 + per, B);
     int64_t mine = 0;
-    for (int i = b0; i < b1; ++i) mine += weight_span(a, i).cost;
+    for (int i = b0; i < b1; ++i) mine += cost(i);
     f.sum[tid + 1] = mine;
     if (tid == 0) f.sum[0] = 0;
-    for (int d = 1; d < WT_THREADS; d *= 2) {
+    for (int d = 1; d < THREADS; d *= 2) {
         __syncthreads();
         const int64_t v = tid + 1 > d ? f.sum[tid + 1 - d] : 0;
         __syncthreads();
@@ -279,12 +142,12 @@ __device__ __forceinline__ int64_t weight_find(const ChunkArgs& a, WeightFind& f
     }
     if (tid == 0) f.b = 0, f.off = 0;
     __syncthreads();
-    const int64_t total = f.sum[WT_THREADS], x = at(total);
+    const int64_t total = f.sum[THREADS], x = at(total);
     if (f.sum[tid] <= x && x < f.sum[tid + 1]) {
         int64_t o = x - f.sum[tid];
         int i = b0;
         for (; i + 1 < b1; ++i) {
-            const int64_t c = weight_span(a, i).cost;
+            const int64_t c = cost(i);
             if (o < c) break;
             o -= c;
         }
@@ -302,13 +165,14 @@ __device__ __forceinline__ int64_t run_start(int64_t total, int r) {
 
 __global__ __launch_bounds__(WT_THREADS, 1) void weight_many_kernel(WeightArgs w) {
     __shared__ __align__(256) uint8_t smem[WW_STAGES * WT_STAGE + WT_WAVES * WW_LSE * 256];   // tiles, then their lse values
-    __shared__ WeightFind find;
+    __shared__ WeightFind<WT_THREADS> find;
     const ChunkArgs& a = w.c;
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 31, hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), run = blockIdx.x;
     int b;
     int64_t off;
-    const int64_t total = weight_find(a, find, [&](int64_t n) { return run_start(n, run); }, b, off);
+    const int64_t total = weight_find<WT_THREADS>(
+        a.B, find, [&](int i) { return weight_span(a, i).cost; }, [&](int64_t n) { return run_start(n, run); }, b, off);
     int64_t left = run_start(total, run + 1) - run_start(total, run);
     while (left > 0) {
         const WeightSpan sp = weight_span(a, b);
@@ -577,11 +441,13 @@ __global__ __launch_bounds__(WT_THREADS, 1) void weight_many_kernel(WeightArgs w
 
 // The sums of the blocks that begin in run blockIdx.x and end in a later one.
 __global__ __launch_bounds__(WW_ROWS) void weight_join_kernel(WeightArgs w) {
-    __shared__ WeightFind find;
+    __shared__ WeightFind<WW_ROWS> find;
     const int run = blockIdx.x;
     int b;
     int64_t off;
-    const int64_t total = weight_find(w.c, find, [&](int64_t n) { return max(run_start(n, run + 1) - 1, (int64_t)0); }, b, off);
+    const int64_t total = weight_find<WW_ROWS>(
+        w.c.B, find, [&](int i) { return weight_span(w.c, i).cost; },
+        [&](int64_t n) { return max(run_start(n, run + 1) - 1, (int64_t)0); }, b, off);
     const int64_t x0 = run_start(total, run), x1 = run_start(total, run + 1);
     if (x0 == x1) return;
     const WeightSpan sp = weight_span(w.c, b);
@@ -595,20 +461,204 @@ __global__ __launch_bounds__(WW_ROWS) void weight_join_kernel(WeightArgs w) {
     if (u < sp.kv) finish(w, b, u, sp.kv, sp.nq, sum);
 }
 
-// More than 8 query tiles of the longest chunk: at 8 tiles the forms are even (16 sequences of 32768 rows: 238 us in
-// runs, 245 us by blocks; one of 8192: 28 and 23 us), at 4 by blocks is the faster one (202 and 192 us), at 16 runs are
-// (335 and 389 us; one of 8192: 32 and 43 us).
-static bool many_queries(int64_t H, int64_t max_q) { return (max_q * H + WT_TILE - 1) / WT_TILE > 8; }
+// ---------------------------------------------------------------- few queries
+//
+// Up to 256 (token, head) rows, 32 of them in the registers of each wave (the A operand),
+// and the cache passes by once: tiles of 32 rows through LDS stages by direct loads, three
+// tiles ahead where all 8 waves hold queries; with up to 128 rows two streams of 4 waves
+// take the tiles in turn, one tile ahead each.  Reading the cache is the bound: every CU
+// takes an equal run of all sequences' tiles.  A wave's sums over its queries meet those of
+// the others through LDS, one tile later.
+//
+// Measured at one token of 128 heads over 16 x 32768 rows: 119 us, 5.1 TB/s.  (Rows held in
+// registers as with many queries, two workgroups of 128 rows per CU: 157 us, 3.8 TB/s.)
+
+constexpr int WF_WAVES = 8, WF_THREADS = 64 * WF_WAVES, WF_STAGES = 4;
+constexpr int WF_OFF_SUM = WF_STAGES * CK_STAGE;                      // [2][wave][32]: sums of the waves' queries
+constexpr int WF_OFF_GONE = WF_OFF_SUM + 2 * WF_WAVES * 32 * 4;       // per stage and wave: which of its tile rows do not exist
+constexpr int WF_OFF_PREV = WF_OFF_GONE + WF_STAGES * WF_WAVES * 4;   // the old weights of the rows of 8 tiles: a tile's are read after
+constexpr int WF_SMEM = WF_OFF_PREV + 2 * WF_STAGES * 256;            // its stage is loaded again
+
+template <int QW>   // waves of a stream
+__global__ __launch_bounds__(WF_THREADS, 2) void weight_few_kernel(WeightArgs w) {
+    __shared__ __align__(256) uint8_t smem[WF_SMEM];
+    __shared__ WeightFind<WF_THREADS> find;
+    constexpr int KSTR = WF_WAVES / QW, PD = WF_STAGES / KSTR - 1;   // streams; tiles loaded ahead
+    const ChunkArgs& a = w.c;
+    const int tid = threadIdx.x, lane = tid & 63, c = lane & 31, hh = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), run = blockIdx.x;
+    const int qw = wave % QW, ks0 = wave / QW;
+    const uint32_t lds0 = lds_addr(smem);
+    auto rows_of = [&](int b) { return min(max(a.kv_len[b], 0), a.max_kv); };
+    auto tiles_of = [&](int b) { return (int64_t)((rows_of(b) + CK_TILE - 1) / CK_TILE); };
+    int b;
+    int64_t off;
+    const int64_t total = weight_find<WF_THREADS>(a.B, find, tiles_of, [&](int64_t n) { return run_start(n, run); }, b, off);
+    int64_t left = run_start(total, run + 1) - run_start(total, run);
+    while (left > 0) {
+        const int kv = rows_of(b), tiles = (kv + CK_TILE - 1) / CK_TILE;
+        if (off >= tiles) {
+            ++b;
+            off = 0;
+            continue;
+        }
+        const int t0 = (int)off, t1 = (int)min((int64_t)tiles, off + left);
+        left -= t1 - t0;
+        off = t1;
+        const int64_t tok0 = min(max((int64_t)a.cu[b], (int64_t)0), a.n_tok);
+        const int64_t tok1 = min(max((int64_t)a.cu[b + 1], tok0), a.n_tok);
+        const int nq = (int)min(tok1 - tok0, (int64_t)a.max_q), nrow = nq * a.H;
+        if (nq == 0) {
+            for (int u = CK_TILE * t0 + tid; u < min(CK_TILE * t1, kv); u += WF_THREADS) finish(w, b, u, kv, 0, 0.f);
+            continue;
+        }
+        const int nw = (nrow + 31) / 32;             // waves of a stream that have queries
+        const int row0 = 32 * qw;
+        const bool idle = row0 >= nrow;
+        const int nit = (t1 - t0 + KSTR - 1) / KSTR;   // tiles of each stream, the last ones perhaps past t1
+        auto tile_of = [&](int k) { return t0 + ks0 + KSTR * k; };
+        auto stage_of = [&](int k) { return ks0 * (PD + 1) + k % (PD + 1); };
+        auto gone_of = [&](int k) { return lds0 + WF_OFF_GONE + stage_of(k) * (WF_WAVES * 4); };
+        TileLoader<QW> loader{a, (const_i32_t*)(a.table + (int64_t)b * a.tstride), kv, qw, lane, {}};
+        auto prev_of = [&](int k) { return smem + WF_OFF_PREV + 256 * (ks0 * 2 * (PD + 1) + k % (2 * (PD + 1))); };
+        const bool old = w.prev && w.decay != 0.f;
+        auto issue = [&](int k) {   // tile k of the stream, and the table entries of the next one
+            if (old && qw == 0) {
+                const int u = min(CK_TILE * tile_of(k) + c, kv - 1);
+                __builtin_amdgcn_global_load_lds((gbl_void_t*)(w.prev + (int64_t)b * w.stride + u), (lds_void_t*)prev_of(k), 4, 0, 0);
+            }
+            loader.issue(tile_of(k), smem + stage_of(k) * CK_STAGE, gone_of(k));
+            loader.fetch(tile_of(k + 1));
+        };
+        // Q operand: query row row0 + c, dims 16 ks + 8 hh .. +8; rows past the end repeat the last one, not counted
+        bf16x8_t qf[WT_KS];
+        {
+            const int64_t row = tok0 * a.H + min(row0 + c, nrow - 1);
+            const uint16_t* ql = a.q_lat + row * a.qls + 8 * hh;
+            const uint16_t* qr = a.q_rope + row * a.qrs + 8 * hh;
+#pragma unroll
+            for (int ks = 0; ks < WT_KS; ++ks)
+                qf[ks] = *reinterpret_cast<const bf16x8_t*>(ks < D_LAT / 16 ? ql + 16 * ks : qr + 16 * ks - D_LAT);
+        }
+        // -lse log2 e of this lane's query rows row0 + 8 (i / 4) + 4 hh + i % 4 (-inf: none, or one without weights)
+        float z[16];
+        bool odd = row0 + 32 > nrow;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int R = row0 + 8 * (i >> 2) + 4 * hh + (i & 3);
+            const float l = w.lse[tok0 * a.H + min(R, nrow - 1)];
+            odd |= l == -INFINITY;
+            z[i] = R < nrow && l != -INFINITY ? -1.4426950408889634f * l : -INFINITY;
+        }
+        const bool some = __ballot(odd) != 0;
+        loader.fetch(tile_of(0));
+        issue(0);
+        if (PD > 1 && nit > 1) issue(1);
+        if (PD > 2 && nit > 2) issue(2);
+#pragma unroll
+        for (int ks = 0; ks < WT_KS; ++ks) asm volatile("" : "+v"(qf[ks]));   // no wait for them inside the tile loop
+#pragma unroll
+        for (int i = 0; i < 16; ++i) asm volatile("" : "+v"(z[i]));
+
+        // a tile's sums, over the waves in order (explicit LDS reads: the compiler would make its own wait for the
+        // direct loads in flight)
+        auto sum_of = [&](int k, int wv) { return lds0 + WF_OFF_SUM + 4 * (((k & 1) * WF_WAVES + wv) * 32 + c); };
+        auto close = [&](int k) {
+            const int u = CK_TILE * tile_of(k) + c;
+            if (qw != k % QW || tile_of(k) >= t1) return;
+            const uint32_t at = sum_of(k, ks0 * QW);
+            float s[QW];
+            static_for<0, QW>([&](auto ic) { s[decltype(ic)::value] = lds_read32<128 * decltype(ic)::value>(at); });
+            float pv = lds_read32<0>(lds_addr(prev_of(k)) + 4 * c);
+#pragma unroll
+            for (int i = 0; i < QW; ++i) lds_wait<0>(s[i]);
+            lds_wait<0>(pv);
+            float sum = s[0];
+#pragma unroll
+            for (int i = 1; i < QW; ++i) sum += i < nw ? s[i] : 0.f;
+            if (old && u < kv - nq) sum = __builtin_fmaf(w.decay, pv, sum);
+            if (lane < 32 && u < kv) w.weight[(int64_t)b * w.stride + u] = sum;
+        };
+        for (int k = 0; k < nit; ++k) {
+            // this wave's share of tile k has landed (at most the loads of the PD - 1 tiles behind it are still
+            // in flight), and every wave's; the stage loaded next is free
+            if (PD > 1 && k + PD - 1 < nit)
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(PD > 1 ? (PD - 1) * loader.LOADS : 0) : "memory");
+            else
+                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            wg_barrier();
+            if (k + PD < nit) issue(k + PD);
+            if (k > 0) close(k - 1);
+            const int t = tile_of(k), u0 = CK_TILE * t;
+            if (t < t1 && !idle) {
+                const uint32_t st = lds0 + stage_of(k) * CK_STAGE;
+                uint32_t note;   // arrives ahead of the operands
+                asm volatile("ds_read_b32 %0, %1" : "=v"(note) : "v"(loader.note(gone_of(k), lane)) : "memory");
+                f32x16_t x;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[i] = 0.f;
+                {
+                    constexpr int SD = 3;   // operands read ahead of the matrix cores
+                    bf16x8_t kf[SD + 1];
+                    int ln = lane;
+                    asm volatile("" : "+v"(ln));   // nothing of the addresses is kept across the tiles
+                    // K operand of (tile row c, piece 2 ks + hh), the piece's low bits permuted
+                    const uint32_t ka = st + (ln & 31) * CK_LAT_BYTES + 16 * ((ln >> 5) ^ lat_xor(ln & 31));
+                    const uint32_t ra = st + CK_OFF_ROPE + (ln & 31) * CK_ROPE_BYTES + 16 * ((ln >> 5) ^ rope_xor(ln & 31));
+                    auto kload = [&](auto kc) {
+                        constexpr int ks = decltype(kc)::value;
+                        if constexpr (ks < D_LAT / 16) kf[ks % (SD + 1)] = lds_read128<256 * (ks >> 3)>(ka ^ (32 * (ks & 7)));
+                        else kf[ks % (SD + 1)] = lds_read128<0>(ra ^ (32 * (ks - D_LAT / 16)));
+                    };
+                    static_for<0, SD>(kload);
+                    static_for<0, WT_KS>([&](auto kc) {
+                        constexpr int ks = decltype(kc)::value;
+                        if constexpr (ks + SD < WT_KS) kload(std::integral_constant<int, ks + SD>{});
+                        lds_wait<(ks + SD < WT_KS) ? SD : (WT_KS - 1 - ks)>(kf[ks % (SD + 1)]);
+                        x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[ks], kf[ks % (SD + 1)], x, 0, 0, 0);
+                    });
+                    lds_wait<0>(note);
+                }
+                const uint32_t absent = loader.absent(note);   // tile rows on no page
+                float sum = 0.f;
+                if (some || u0 + CK_TILE - 1 > kv - nq + row0 / a.H) {   // rows that a query does not see, or odd ones
+                    // the first query row that sees cache row u0 + c (none sees those from kv on)
+                    const int first = a.H * min(max(u0 + c - (kv - nq), 0), nq);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale_log2, z[i]));
+                        if (row0 + 8 * (i >> 2) + 4 * hh + (i & 3) >= first && z[i] != -INFINITY) sum += p;
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale_log2, z[i]));
+                }
+                sum = half_sum(sum);
+                if ((absent >> c) & 1u) sum = 0.f;
+                if (hh == 0) asm volatile("ds_write_b32 %0, %1" ::"v"(sum_of(k, wave)), "v"(sum) : "memory");
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        wg_barrier();
+        close(nit - 1);
+        wg_barrier();      // the sums and the stages are free
+    }
+}
+
+// More than 256 query rows of the longest chunk, which the few-queries form cannot hold.  At 256 it takes 184 us where
+// runs take 238 (16 sequences of 32768 rows), 16 where they take 28 (one of 8192), 53 and 68 (64 of 2048).
+static bool many_queries(int64_t H, int64_t max_q) { return max_q * H > 32 * WF_WAVES; }
 
 size_t weight_workspace_bytes(int64_t H, int64_t max_q) {
     return many_queries(H, max_q) ? (size_t)2 * WW_RUNS * WW_ROWS * sizeof(float) : 0;
 }
 
-int64_t weight_blocks(int64_t max_kv) { return (max_kv + WF_ROWS - 1) / WF_ROWS; }
-
 hipError_t launch_weight(const WeightArgs& w, hipStream_t s) {
     if (!many_queries(w.c.H, w.c.max_q)) {
-        hipLaunchKernelGGL(weight_few_kernel, dim3((unsigned)((int64_t)w.nblk * w.c.B)), dim3(WT_THREADS), 0, s, w);
+        if ((int64_t)w.c.max_q * w.c.H > 128)
+            hipLaunchKernelGGL((weight_few_kernel<8>), dim3(WW_RUNS), dim3(WF_THREADS), 0, s, w);
+        else
+            hipLaunchKernelGGL((weight_few_kernel<4>), dim3(WW_RUNS), dim3(WF_THREADS), 0, s, w);
         return hipGetLastError();
     }
     hipLaunchKernelGGL(weight_many_kernel, dim3(WW_RUNS), dim3(WT_THREADS), 0, s, w);

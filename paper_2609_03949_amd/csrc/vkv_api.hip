@@ -875,9 +875,6 @@ int vkv_weight_accumulate(vkv_ctx* ctx, const vkv_pages* pg, const vkv_chunk* ch
     if (!al4(lse) || !al4(prev) || !al4(weight)) return fail(ctx, VKV_E_ALIGN, "lse, prev and weight must be 4-byte aligned");
     if (weight_stride < pg->max_kv)
         return fail(ctx, VKV_E_SHAPE, "weight_stride=%lld smaller than max_kv=%lld", (long long)weight_stride, (long long)pg->max_kv);
-    const int64_t blocks = weight_blocks(pg->max_kv);
-    if (pg->B * blocks >= (1ll << 31))
-        return fail(ctx, VKV_E_SHAPE, "B=%lld with max_kv=%lld: too many rows", (long long)pg->B, (long long)pg->max_kv);
     const size_t need = up256(weight_workspace_bytes(ch->H, ch->max_q));
     if (need && (rc = check_ws(ctx, ws, ws_bytes, need))) return rc;
     if (pg->max_kv == 0) return VKV_OK;
@@ -889,7 +886,6 @@ int vkv_weight_accumulate(vkv_ctx* ctx, const vkv_pages* pg, const vkv_chunk* ch
     w.prev = prev;
     w.weight = weight;
     w.stride = weight_stride;
-    w.nblk = (int)blocks;
     w.part = (float*)ws;
     DeviceGuard dev(ctx);
     HIP_TRY(ctx, dev.err);

@@ -351,10 +351,8 @@ struct WeightArgs {
     const float* prev;     // [B, stride] or null (may be weight)
     float* weight;         // [B, stride]
     int64_t stride;
-    int nblk;              // blocks of cache rows of the longest sequence (few queries)
     float* part;           // workspace (many queries): sums of the blocks that several runs share
 };
-int64_t weight_blocks(int64_t max_kv);
 size_t weight_workspace_bytes(int64_t H, int64_t max_q);
 hipError_t launch_weight(const WeightArgs& w, hipStream_t s);
 

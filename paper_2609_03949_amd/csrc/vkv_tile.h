@@ -40,6 +40,12 @@ __device__ __forceinline__ bf16x8_t lds_read128(uint32_t addr) {
     asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFF));
     return v;
 }
+template <int OFF>
+__device__ __forceinline__ float lds_read32(uint32_t addr) {
+    float v;
+    asm volatile("ds_read_b32 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFF));
+    return v;
+}
 // transposing read: within each 16-lane group, lane j supplies the address of
 // 4 consecutive 16-bit elements D[j][0..3], and lane i receives D[4e + i/4][i % 4]
 // for e = 0..3

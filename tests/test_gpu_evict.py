@@ -141,6 +141,31 @@ def test_weights_in_runs(ctx, kv_lens, q_lens, H):
     assert torch.equal(first, again)
 
 
+@pytest.mark.parametrize("H,most", [(128, 2), (17, 15), (32, 4), (1, 200), (128, 1)])
+@pytest.mark.parametrize("page", [1, 4, 64])
+def test_weights_of_few_queries(ctx, H, most, page):
+    """Up to 8 tiles of queries, in one and in two streams: rows and tokens of every number, pages smaller than a wave's
+    rows, absent ones, a query without weights, in place."""
+    kv_lens = [1, 0, 31, 32, 33, 64, 65, 100, 1000, 257, 6]
+    q_lens = [most - i % (most + 1) for i in range(len(kv_lens))]
+    x = Case(kv_lens, q_lens, H, seed=H + page, page=page)
+    lse = true_lse(x)
+    lse[0, 0] = -math.inf
+    absent = [torch.zeros(n, dtype=torch.bool) for n in kv_lens]
+    absent[8][640:704] = True
+    x.table[8, 640 // page:704 // page] = -5
+    prev = torch.rand(len(kv_lens), x.max_kv + 1, device=DEV)
+    want, tol = expected(x, lse, 0.8, prev, absent)
+    out = accumulate(ctx, x, lse, 0.8, prev, torch.full_like(prev, -3.0))
+    for b, n in enumerate(kv_lens):
+        check(f"weight of sequence {b}", out[b, :n], want[b], tol[b])
+        assert bool((out[b, n:] == -3.0).all())
+    same = prev.clone()
+    accumulate(ctx, x, lse, 0.8, same, same)
+    for b, n in enumerate(kv_lens):
+        assert torch.equal(same[b, :n], out[b, :n]) and torch.equal(same[b, n:], prev[b, n:])
+
+
 def test_weights_sum_to_the_queries(ctx):
     """With the attention call's own lse each token and head gives 1 in all."""
     x = Case([700, 90], [4, 1], 128, seed=3, page=64)
