@@ -54,7 +54,7 @@ constexpr int WW_STAGES = 4;
 constexpr int WW_LAT = WT_TILE * 2 * D_LAT;              // latent panel: rows of 1 KB; then rows of 128 bytes
 constexpr int WW_SD = 5;                                 // operands read ahead of the matrix cores
 constexpr int WW_LSE = 4;                                // lse slots of a wave, of 256 bytes
-constexpr int WW_ACC = 12;                               // K operands in vector registers, the others in accumulation registers
+constexpr int WW_ACC = 8;                                // K operands in vector registers, the others in accumulation registers
 constexpr int WW_RUNS = 256;
 constexpr int WW_LOAD = 3;                               // loading a block's rows counts as so many tiles
 static_assert(WT_KS % (WW_SD + 1) == 0, "operands keep their registers from tile to tile");
@@ -367,6 +367,8 @@ __global__ __launch_bounds__(WT_THREADS, 1) void weight_many_kernel(WeightArgs w
                     if constexpr (ks % 3 == 2 && ks < 30) issue(tl, sl, t - t0 + 2, std::integral_constant<int, ks / 3>{});
                     __builtin_amdgcn_sched_barrier(0);
                 });
+                // the last product of each group is through before anything reads a result, copies of the compiler's included
+                asm volatile("s_nop 13" : "+v"(x[0]), "+v"(x[1]));
                 asm volatile("s_waitcnt lgkmcnt(2)" : "+v"(z4[0]), "+v"(z4[1]), "+v"(z4[2]), "+v"(z4[3]));
 #pragma unroll
                 for (int g = 0; g < 2; ++g) sum[g] += add[g];
