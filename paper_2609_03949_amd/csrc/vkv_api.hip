@@ -838,7 +838,7 @@ int vkv_chunk_attend(vkv_ctx* ctx, const vkv_pages* pg, const vkv_chunk* ch, voi
     char* w = (char*)ws;
     a.mb = (int)sp.mb;
     a.runs = (int)sp.runs;
-    a.min_run = (int)sp.min_run;
+    a.streams = (int)sp.streams;
     a.scale_log2 = scale * 1.4426950408889634f;
     a.out = out;
     a.lse = lse;

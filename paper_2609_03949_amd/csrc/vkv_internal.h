@@ -326,7 +326,7 @@ struct ChunkArgs {
     int64_t n_tok;
     int B, H, max_q;
     int mb;                // blocks of rows of a sequence
-    int runs, min_run;     // most runs the tiles are cut into, fewest tiles of one
+    int runs, streams;     // most runs the tiles are cut into; streams of tiles of a workgroup
     float scale_log2;
     uint16_t* out;         // [n_tok, H, 512]
     float* lse;            // [n_tok, H]
@@ -338,7 +338,7 @@ constexpr int CK_MAX_UNITS = 1024;   // units up to which the tiles are cut into
 constexpr int CK_RUNS = 256;         // one per CU
 // how a chunk is cut: waves by rows (16 qg rows a unit), units, runs (0: a workgroup per unit), workspace bytes
 struct ChunkSplit {
-    int64_t qg, mb, units, runs, min_run;
+    int64_t qg, mb, units, runs, streams;
     size_t part_o, part_ml, span;
 };
 ChunkSplit chunk_split(int64_t B, int64_t H, int64_t max_q, int64_t max_kv);
