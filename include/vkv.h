@@ -640,13 +640,15 @@ int vkv_weight_select(vkv_ctx* ctx, const float* weight, int64_t B, int64_t max_
  * row from count[b] on.
  *   kept   [B, keep] int32: count[b] rows of [0, kv_len[b]), ascending (from
  *          vkv_weight_select or vkv_sigma_select); count [B] int32
- *   origin [B, keep] int32 (may be NULL): the row that lies in slot j now, -1 from
- *          count[b] on
+ *   origin [B, keep] int32 (may be NULL): the row that lies in slot j now; -1 from
+ *          count[b] on, and for a slot that holds no row of the tier (below)
  *   weight, weight_out (may both be NULL): weight_out[b*keep + j] = weight[b*weight_stride
- *          + origin[b,j]], 0 from count[b] on; the buffers may not overlap
+ *          + origin[b,j]], 0 where origin is -1; the buffers may not overlap
  * Rows below kv_len[b] must not lie on pages that another sequence (or another entry of
- * the table) uses.  Entries that are not rows of an ascending table are not moved
- * (origin -1); a row is not moved from or to an absent page.  Only slots
+ * the table) uses.  Entries that are not rows of an ascending table are not moved, nor
+ * is a row from or to an absent page: its slot keeps what it held, which is no row of
+ * the tier, and has origin -1, as has a kept row's own slot on an absent page.  A caller
+ * that keeps rows on absent pages looks at origin before it attends the slots.  Only slots
  * below count[b] are written, so a call on the same table and tier may be
  * repeated.  1 <= keep <= 2^30.
  */

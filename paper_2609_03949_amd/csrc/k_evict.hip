@@ -445,19 +445,22 @@ __global__ __launch_bounds__(64) void evict_kernel(EvictArgs a) {
             if (src != j && (src < n || src >= kv)) src = -1;   // not a table of ascending rows: nothing is moved
         }
     }
-    if (lane < EV_SLOTS && j0 + lane < a.keep) {
-        const int64_t at = (int64_t)b * a.keep + j0 + lane;
-        if (a.origin) a.origin[at] = src;
-        if (a.weight_out) a.weight_out[at] = src >= 0 ? a.weight[(int64_t)b * a.wstride + src] : 0.f;
-    }
-    // where the rows lie (a row on a page that does not exist stays)
+    const float weight = a.weight_out && src >= 0 ? a.weight[(int64_t)b * a.wstride + src] : 0.f;
+    // where the rows lie; one whose page, or whose slot's page, does not exist is in no slot
     int64_t from = -1, to = -1;
-    if (src >= 0 && src != j0 + lane) {
+    if (src >= 0) {
         const int32_t ps = table[src >> a.shift], pd = table[(j0 + lane) >> a.shift];
-        if ((uint32_t)ps < (uint32_t)a.n_pages && (uint32_t)pd < (uint32_t)a.n_pages) {
+        if ((uint32_t)ps >= (uint32_t)a.n_pages || (uint32_t)pd >= (uint32_t)a.n_pages) {
+            src = -1;
+        } else if (src != j0 + lane) {
             from = (int64_t)ps * a.ps + (int64_t)(src & a.page_mask) * a.rs;
             to = (int64_t)pd * a.ps + (int64_t)((j0 + lane) & a.page_mask) * a.rs;
         }
+    }
+    if (lane < EV_SLOTS && j0 + lane < a.keep) {
+        const int64_t at = (int64_t)b * a.keep + j0 + lane;
+        if (a.origin) a.origin[at] = src;
+        if (a.weight_out) a.weight_out[at] = src >= 0 ? weight : 0.f;
     }
     if (__ballot(from >= 0) == 0) return;
     u32x4_t piece[EV_LOADS];
