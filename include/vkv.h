@@ -645,9 +645,9 @@ int vkv_weight_select(vkv_ctx* ctx, const float* weight, int64_t B, int64_t max_
  *   weight, weight_out (may both be NULL): weight_out[b*keep + j] = weight[b*weight_stride
  *          + origin[b,j]], 0 where origin is -1; the buffers may not overlap
  * Rows below kv_len[b] must not lie on pages that another sequence (or another entry of
- * the table) uses.  Entries that are not rows of an ascending table are not moved, nor
- * is a row from or to an absent page: its slot keeps what it held, which is no row of
- * the tier, and has origin -1, as has a kept row's own slot on an absent page.  A caller
+ * the table) uses.  An entry that is not a row or not above the entry before it is not
+ * moved, nor is a row from or to an absent page: its slot keeps what it held, which is no
+ * row of the tier, and has origin -1, as has a kept row's own slot on an absent page.  A caller
  * that keeps rows on absent pages looks at origin before it attends the slots.  Only slots
  * below count[b] are written, so a call on the same table and tier may be
  * repeated.  1 <= keep <= 2^30.

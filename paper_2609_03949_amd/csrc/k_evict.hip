@@ -442,7 +442,8 @@ __global__ __launch_bounds__(64) void evict_kernel(EvictArgs a) {
             const int hole = j - i0 - __popc(held & ((1u << lane) - 1));   // its rank, if slot j is one
             const int p = below + hole;
             src = (held >> lane) & 1u ? j : p >= 0 && p < n ? kept[p] : -1;
-            if (src != j && (src < n || src >= kv)) src = -1;   // not a table of ascending rows: nothing is moved
+            // not a row, or not above the entry before it: nothing is moved
+            if (src != j && (src < n || src >= kv || (p > 0 && kept[p - 1] >= src))) src = -1;
         }
     }
     const float weight = a.weight_out && src >= 0 ? a.weight[(int64_t)b * a.wstride + src] : 0.f;

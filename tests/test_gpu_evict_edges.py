@@ -59,3 +59,14 @@ def test_rows_on_absent_pages(ctx, entry):
     # slots 0..29: 10..15 stay, 16..19 would; the holes 0..9 take 30, 31 (absent), 32..39, and 20..29 lie on the absent page
     check(x, 2, origin, out, weight, before, [-1, -1] + list(range(32, 40)) + list(range(10, 16)) + [-1] * 14, 64)
     check(x, 3, origin, out, weight, before, [33, 1, 34], 64)
+
+
+def test_entries_that_are_not_ascending_do_not_move(ctx):
+    """Descending and repeated entries, and rows that are none between rows that are."""
+    x = Case([100] * 4, [1] * 4, 1, page=16, seed=10)
+    tiers = [[99, 98, 97, 96], [5, 5, 70, 70], [60, 1 << 30, 70, 71], [0, 2, 50, 49, 51]]
+    origin, out, weight, before = evict(ctx, x, tiers, 8)
+    check(x, 0, origin, out, weight, before, [99, -1, -1, -1], 100)
+    check(x, 1, origin, out, weight, before, [5, -1, 70, -1], 100)
+    check(x, 2, origin, out, weight, before, [60, -1, -1, 71], 100)
+    check(x, 3, origin, out, weight, before, [0, 50, 2, -1, 51], 100)
