@@ -531,7 +531,8 @@ int vkv_prompt_attend(vkv_ctx* ctx, const vkv_prompt* pr, float scale, uint16_t*
  * u % page of page table[b*table_stride + u/page]; row r of page p is at
  * cache + p*page_stride + r*row_stride (elements).  A cache [B, T, 576] is one
  * whose page j of sequence b is page b*T/page + j.
- *   table   [B, table_stride] int32 (device), table_stride >= ceil(max_kv / page)
+ *   table   [B, table_stride] int32 (device), table_stride >= ceil(max_kv / page);
+ *           may be NULL with max_kv = 0
  *   kv_len  [B] int32 (device): rows of each sequence; values outside
  *           [0, max_kv] are taken as the nearest bound
  * page: a power of two in [1, 65536].  1 <= B <= 65535, 0 <= max_kv <= 2^30,
@@ -556,7 +557,8 @@ typedef struct vkv_pages {
  * nq = cu[b+1] - cu[b] sees the rows u <= kv_len[b] - nq + i (their own rows are
  * in the cache already).
  *   q_lat   (token, head) row t*H + h at q_lat + (t*H + h)*q_lat_stride: 512 bf16
- *   q_rope  likewise, 64 bf16
+ *   q_rope  likewise, 64 bf16 (with n_tok = 0 these, and what the calls below read or
+ *           write per token, may be NULL)
  *   cu      [B + 1] int32 (device), ascending, cu[0] = 0; offsets outside
  *           [0, n_tok] are taken as the nearest bound, a sequence's tokens past
  *           its first max_q are left out
@@ -607,6 +609,7 @@ int vkv_chunk_attend(vkv_ctx* ctx, const vkv_pages* pg, const vkv_chunk* ch, voi
  *   lse           [n_tok, H] fp32, as vkv_chunk_attend wrote it
  *   prev, weight  row u of sequence b at b*weight_stride + u, fp32; the same
  *                 buffer or buffers that do not overlap; weight_stride >= max_kv
+ *                 (weight may be NULL with max_kv = 0, here and below)
  *   decay         finite, >= 0
  * bf16 MFMA, fp32 accumulation; no atomics: the same inputs give the same bits.
  * ws: vkv_weight_workspace_size bytes (0 is possible), 256-byte aligned; the rules

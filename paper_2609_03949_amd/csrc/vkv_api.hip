@@ -744,7 +744,8 @@ static int check_pages(vkv_ctx* ctx, const vkv_pages* pg) {
         return fail(ctx, VKV_E_SHAPE, "n_pages=%lld outside [1, 2^31)", (long long)pg->n_pages);
     if (pg->page < 1 || pg->page > 65536 || (pg->page & (pg->page - 1)))
         return fail(ctx, VKV_E_UNSUPPORTED, "page=%d: need a power of two in [1, 65536]", pg->page);
-    if (!pg->cache || !pg->table || !pg->kv_len) return fail(ctx, VKV_E_ARG, "cache, table and kv_len are required");
+    if (!pg->cache || (!pg->table && pg->max_kv > 0) || !pg->kv_len)
+        return fail(ctx, VKV_E_ARG, "cache, table and kv_len are required");
     if (!al16(pg->cache)) return fail(ctx, VKV_E_ALIGN, "cache must be 16-byte aligned");
     if (!al4(pg->table) || !al4(pg->kv_len))
         return fail(ctx, VKV_E_ALIGN, "table and kv_len must be 4-byte aligned");
@@ -771,7 +772,8 @@ static int check_chunk(vkv_ctx* ctx, const vkv_pages* pg, const vkv_chunk* ch) {
     if (ch->max_q * ch->H > (1ll << 30) || pg->B * chunk_split(pg->B, ch->H, ch->max_q, pg->max_kv).mb >= (1ll << 31))
         return fail(ctx, VKV_E_SHAPE, "max_q=%lld with H=%lld and B=%lld: too many rows", (long long)ch->max_q,
                     (long long)ch->H, (long long)pg->B);
-    if (!ch->q_lat || !ch->q_rope || !ch->cu) return fail(ctx, VKV_E_ARG, "q_lat, q_rope and cu are required");
+    if (((!ch->q_lat || !ch->q_rope) && ch->n_tok > 0) || !ch->cu)
+        return fail(ctx, VKV_E_ARG, "q_lat, q_rope and cu are required");
     if (!al16(ch->q_lat) || !al16(ch->q_rope)) return fail(ctx, VKV_E_ALIGN, "q_lat and q_rope must be 16-byte aligned");
     if (!al4(ch->cu)) return fail(ctx, VKV_E_ALIGN, "cu must be 4-byte aligned");
     if (ch->q_lat_stride < 0 || ch->q_lat_stride % 8 || ch->q_rope_stride < 0 || ch->q_rope_stride % 8)
@@ -827,7 +829,7 @@ int vkv_chunk_attend(vkv_ctx* ctx, const vkv_pages* pg, const vkv_chunk* ch, voi
     int rc = check_chunk(ctx, pg, ch);
     if (rc) return rc;
     if (bad_scale(scale)) return fail(ctx, VKV_E_ARG, "scale must be positive and finite");
-    if (!out || !lse) return fail(ctx, VKV_E_ARG, "out and lse are required");
+    if ((!out || !lse) && ch->n_tok > 0) return fail(ctx, VKV_E_ARG, "out and lse are required");
     if (!al16(out) || !al4(lse)) return fail(ctx, VKV_E_ALIGN, "out must be 16-byte aligned, lse 4-byte");
     const ChunkSplit sp = chunk_split(pg->B, ch->H, ch->max_q, pg->max_kv);
     size_t po, pml, span;
@@ -871,7 +873,7 @@ int vkv_weight_accumulate(vkv_ctx* ctx, const vkv_pages* pg, const vkv_chunk* ch
     if (rc) return rc;
     if (bad_scale(scale)) return fail(ctx, VKV_E_ARG, "scale must be positive and finite");
     if (!(decay >= 0.f) || !(decay < 1e30f)) return fail(ctx, VKV_E_ARG, "decay must be finite and >= 0");
-    if (!lse || !weight) return fail(ctx, VKV_E_ARG, "lse and weight are required");
+    if ((!lse && ch->n_tok > 0) || (!weight && pg->max_kv > 0)) return fail(ctx, VKV_E_ARG, "lse and weight are required");
     if (!al4(lse) || !al4(prev) || !al4(weight)) return fail(ctx, VKV_E_ALIGN, "lse, prev and weight must be 4-byte aligned");
     if (weight_stride < pg->max_kv)
         return fail(ctx, VKV_E_SHAPE, "weight_stride=%lld smaller than max_kv=%lld", (long long)weight_stride, (long long)pg->max_kv);
@@ -905,7 +907,8 @@ int vkv_weight_select(vkv_ctx* ctx, const float* weight, int64_t B, int64_t max_
     if (nsink < 0 || recent < 0 || nsink > keep || recent > keep - nsink)
         return fail(ctx, VKV_E_ARG, "nsink=%lld and recent=%lld: need >= 0 and at most keep=%lld together", (long long)nsink,
                     (long long)recent, (long long)keep);
-    if (!weight || !kv_len || !kept || !count) return fail(ctx, VKV_E_ARG, "weight, kv_len, kept and count are required");
+    if ((!weight && max_kv > 0) || !kv_len || !kept || !count)
+        return fail(ctx, VKV_E_ARG, "weight, kv_len, kept and count are required");
     if (!al4(weight) || !al4(kv_len) || !al4(kept) || !al4(count))
         return fail(ctx, VKV_E_ALIGN, "weight, kv_len, kept and count must be 4-byte aligned");
     WeightSelArgs a{};
@@ -935,7 +938,8 @@ int vkv_cache_evict(vkv_ctx* ctx, const vkv_pages* pg, const int32_t* kept, cons
     if (!kept || !count) return fail(ctx, VKV_E_ARG, "kept and count are required");
     if (!al4(kept) || !al4(count) || !al4(origin) || !al4(weight) || !al4(weight_out))
         return fail(ctx, VKV_E_ALIGN, "kept, count, origin, weight and weight_out must be 4-byte aligned");
-    if ((weight != nullptr) != (weight_out != nullptr)) return fail(ctx, VKV_E_ARG, "weight and weight_out go together");
+    if (pg->max_kv > 0 ? (weight != nullptr) != (weight_out != nullptr) : weight && !weight_out)   // (without rows weight is empty)
+        return fail(ctx, VKV_E_ARG, "weight and weight_out go together");
     if (weight && weight_stride < pg->max_kv)
         return fail(ctx, VKV_E_SHAPE, "weight_stride=%lld smaller than max_kv=%lld", (long long)weight_stride, (long long)pg->max_kv);
     if (pg->B * evict_waves(keep) >= (1ll << 31))
