@@ -228,7 +228,9 @@ __global__ __launch_bounds__(WS_THREADS) void weight_select_kernel(WeightSelArgs
             }
             __syncthreads();
             ka = sh.edge[0];
-            kb = sh.edge[1];
+            // the key between the negative numbers and 0 is no weight's (-0 has that of 0), and as a number it is -0, which
+            // 0 is not above: rows of weight 0 would be listed with keys outside the bracket
+            kb = sh.edge[1] == 0x7FFFFFFFu ? 0x7FFFFFFEu : sh.edge[1];
             listed = ka != 0u;    // (0: NaN, which compares with nothing, or everything)
             int above = 0;
             if (listed) {
