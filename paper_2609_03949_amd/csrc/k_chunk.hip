@@ -527,7 +527,9 @@ __global__ __launch_bounds__(CK_THREADS, 2) void chunk_run_kernel(ChunkArgs a) {
 template <int QG>
 __global__ __launch_bounds__(CK_THREADS, 2) void chunk_unit_kernel(ChunkArgs a) {
     __shared__ __align__(256) uint8_t smem[CK_SMEM];
-    const int b = blockIdx.x / a.mb, j = a.mb - 1 - (int)(blockIdx.x % a.mb);
+    const uint32_t wg = workgroup_id();
+    if (wg >= (uint32_t)a.B * (uint32_t)a.mb) return;
+    const int b = (int)(wg / (uint32_t)a.mb), j = a.mb - 1 - (int)(wg % (uint32_t)a.mb);
     const int u = b * a.mb + j;
     const CkUnit x = chunk_unit(a, u, 16 * QG);
     const int n = unit_tiles(a, x, 16 * QG);
@@ -634,7 +636,7 @@ hipError_t launch_chunk(const ChunkArgs& a, const ChunkSplit& sp, hipStream_t s)
         hipLaunchKernelGGL(chunk_join_kernel, dim3((unsigned)(sp.units * 16 * sp.qg * (D_LAT / 4) / CKJ_F)), dim3(CKJ_THREADS), 0, s, a, (int)sp.qg);
         return hipGetLastError();
     }
-    const dim3 grid((unsigned)sp.units);
+    const dim3 grid = grid_of(sp.units);
     if (sp.qg == 8) hipLaunchKernelGGL((chunk_unit_kernel<8>), grid, block, 0, s, a);
     else if (sp.qg == 2) hipLaunchKernelGGL((chunk_unit_kernel<2>), grid, block, 0, s, a);
     else hipLaunchKernelGGL((chunk_unit_kernel<4>), grid, block, 0, s, a);

@@ -421,8 +421,9 @@ __device__ __forceinline__ int kept_below(const int32_t* kept, int n, int x) {
 }
 
 __global__ __launch_bounds__(64) void evict_kernel(EvictArgs a) {
-    const int nw = (a.keep + EV_SLOTS - 1) / EV_SLOTS;
-    const int b = blockIdx.x / nw, j0 = (blockIdx.x % nw) * EV_SLOTS;
+    const uint32_t nw = (uint32_t)(a.keep + EV_SLOTS - 1) / EV_SLOTS, wg = workgroup_id();
+    if (wg >= (uint32_t)a.B * nw) return;
+    const int b = (int)(wg / nw), j0 = (int)(wg % nw) * EV_SLOTS;
     const int lane = threadIdx.x;
     const int kv = min(max(a.kv_len[b], 0), a.max_kv);
     const int32_t* kept = a.kept + (int64_t)b * a.keep;
@@ -483,7 +484,7 @@ __global__ __launch_bounds__(64) void evict_kernel(EvictArgs a) {
 int64_t evict_waves(int64_t keep) { return (keep + EV_SLOTS - 1) / EV_SLOTS; }
 
 hipError_t launch_evict(const EvictArgs& a, hipStream_t s) {
-    hipLaunchKernelGGL(evict_kernel, dim3((unsigned)(a.B * evict_waves(a.keep))), dim3(64), 0, s, a);
+    hipLaunchKernelGGL(evict_kernel, grid_of(a.B * evict_waves(a.keep)), dim3(64), 0, s, a);
     return hipGetLastError();
 }
 

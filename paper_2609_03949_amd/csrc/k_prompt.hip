@@ -110,8 +110,9 @@ __device__ __forceinline__ bool prompt_block(const PromptArgs& a, uint8_t* smem)
     // the longest blocks first; with 8 | H every XCD takes H / 8 neighbouring heads of
     // each sequence (workgroups go to the XCDs in turn), which share K and V in its L2
     const uint32_t npair = (uint32_t)a.n_seq * (uint32_t)a.H;     // (the grid is below 2^31)
-    const int qb = a.nqb - 1 - (int)(blockIdx.x / npair);
-    const int p = (int)(blockIdx.x % npair);
+    const uint32_t wg = workgroup_id();
+    const int qb = a.nqb - 1 - (int)(wg / npair);                 // (below 0: none)
+    const int p = (int)(wg % npair);
     int b = p / a.H, h = p % a.H;
     if (a.H % 8 == 0) {
         const int hx = a.H / 8, i = p / 8;
@@ -123,7 +124,7 @@ __device__ __forceinline__ bool prompt_block(const PromptArgs& a, uint8_t* smem)
     const int64_t end = min(max((int64_t)a.cu[b + 1], start), a.n_tok);
     const int len = (int)min(end - start, (int64_t)a.max_len);
     const int q0 = qb * PR_ROWS;
-    if (q0 >= len) return false;
+    if (q0 >= len || qb < 0) return false;
 
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 31, hh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -354,7 +355,7 @@ __global__ __launch_bounds__(64 * PR_WAVES, 2) void prompt_kernel(PromptArgs a) 
 int64_t prompt_blocks(int64_t len) { return (len + PR_ROWS - 1) / PR_ROWS; }
 
 hipError_t launch_prompt(const PromptArgs& a, int dn, int dr, hipStream_t s) {
-    const dim3 grid((unsigned)((int64_t)a.n_seq * a.H * a.nqb)), block(64 * PR_WAVES);
+    const dim3 grid = grid_of((int64_t)a.n_seq * a.H * a.nqb), block(64 * PR_WAVES);
     if (dn == 128 && dr == 64)
         hipLaunchKernelGGL((prompt_kernel<128, 64, 128>), grid, block, 0, s, a);
     else if (dn == 128)

@@ -293,6 +293,12 @@ struct AttendArgs {
     float* lse;            // [B,H]
 };
 
+// Workgroups of a launch: HIP takes fewer than 2^32 work-items in a dimension, so n of them (below 2^31, of up to 512
+// work-items) lie in rows of GRID_ROW where they are many; the last row has some past the end.
+constexpr int64_t GRID_ROW = 1ll << 22;
+inline dim3 grid_of(int64_t n) { return dim3((unsigned)(n < GRID_ROW ? n : GRID_ROW), (unsigned)((n + GRID_ROW - 1) / GRID_ROW)); }
+__device__ __forceinline__ uint32_t workgroup_id() { return blockIdx.y * (uint32_t)GRID_ROW + blockIdx.x; }
+
 struct PromptArgs {
     const uint16_t* q;     // [n_tok, H, dn + dr]
     const uint16_t* k;     // [n_tok, Hk, dn]
