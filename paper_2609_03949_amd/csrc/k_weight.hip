@@ -338,9 +338,18 @@ __global__ __launch_bounds__(WT_THREADS, 1) void weight_many_kernel(WeightArgs w
                         else asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(x[g]) : "v"(q), "a"(kf[g][ks]));
                         __builtin_amdgcn_sched_barrier(0);
                     };
+                    // The compiler does not see that results are in flight and would not wait before it reads or copies
+                    // them: the statement of the last products ends when they are through (12 wait states after 8 passes).
+                    // Between products nothing names their results (a test of the generated code holds it to that).
+                    auto last_products = [&]() __attribute__((always_inline)) {
+                        static_assert(WT_KS > WW_ACC, "their operands are in accumulation registers");
+                        asm volatile("s_waitcnt lgkmcnt(%5)\n\tv_mfma_f32_32x32x16_bf16 %0, %2, %3, %0\n\tv_mfma_f32_32x32x16_bf16 %1, %2, %4, %1\n\ts_nop 13"
+                                     : "+v"(x[0]), "+v"(x[1]) : "v"(qf[(WT_KS - 1) % (WW_SD + 1)]), "a"(kf[0][WT_KS - 1]), "a"(kf[1][WT_KS - 1]), "n"(WW_SD - 1 + 4));
+                        __builtin_amdgcn_sched_barrier(0);
+                    };
                     // A wave issues in order, and the second product when the first one's passes are over: what
                     // stands between them, and after them, is to fit into 32 cycles each.
-                    product(std::integral_constant<int, 0>{});
+                    if constexpr (ks < WT_KS - 1) product(std::integral_constant<int, 0>{});
                     if constexpr (ks == 0) {
 #pragma unroll
                         for (int g = 0; g < 2; ++g) asm volatile("" : "+v"(y[g]));
@@ -352,7 +361,8 @@ __global__ __launch_bounds__(WT_THREADS, 1) void weight_many_kernel(WeightArgs w
                         asm volatile("" : "+v"(add[g]));   // here, not after the products
                     }
                     __builtin_amdgcn_sched_barrier(0);
-                    product(std::integral_constant<int, 1>{});
+                    if constexpr (ks < WT_KS - 1) product(std::integral_constant<int, 1>{});
+                    else last_products();
                     if constexpr (ks < KB) qload(st, std::integral_constant<int, ks + WW_SD>{});
                     else qload(stn, std::integral_constant<int, ks - KB>{});
                     if constexpr (ks == 33) {
@@ -367,8 +377,6 @@ __global__ __launch_bounds__(WT_THREADS, 1) void weight_many_kernel(WeightArgs w
                     if constexpr (ks % 3 == 2 && ks < 30) issue(tl, sl, t - t0 + 2, std::integral_constant<int, ks / 3>{});
                     __builtin_amdgcn_sched_barrier(0);
                 });
-                // the last product of each group is through before anything reads a result, copies of the compiler's included
-                asm volatile("s_nop 13" : "+v"(x[0]), "+v"(x[1]));
                 asm volatile("s_waitcnt lgkmcnt(2)" : "+v"(z4[0]), "+v"(z4[1]), "+v"(z4[2]), "+v"(z4[3]));
 #pragma unroll
                 for (int g = 0; g < 2; ++g) sum[g] += add[g];
@@ -383,7 +391,6 @@ __global__ __launch_bounds__(WT_THREADS, 1) void weight_many_kernel(WeightArgs w
                     const int r0 = WT_TILE * t + 4 * (ln >> 5);
 #pragma unroll
                     for (int g = 0; g < 2; ++g) {
-                        asm volatile("s_nop 15\n\ts_nop 3" : "+v"(x[g]));
                         // the first query row that sees cache row u (none sees those from kv on)
                         const int first = a.H * min(max(uw + 32 * g + (ln & 31) - (kv - nq), 0), nq);
                         float part = 0.f;
@@ -406,7 +413,6 @@ __global__ __launch_bounds__(WT_THREADS, 1) void weight_many_kernel(WeightArgs w
                 for (int i = 0; i <= WW_SD; ++i) lds_wait<0>(qf[i]);   // the reads after the last tile
 #pragma unroll
                 for (int g = 0; g < 2; ++g) {
-                    asm volatile("s_nop 15\n\ts_nop 3" : "+v"(y[g]));
                     float add = 0.f;
 #pragma unroll
                     for (int i = 0; i < 16; ++i) add += weight(y[g][i], z4[i >> 2][i & 3]);
