@@ -461,12 +461,6 @@ __global__ __launch_bounds__(64) void evict_kernel(EvictArgs a) {
             to = (int64_t)pd * a.ps + (int64_t)((j0 + lane) & a.page_mask) * a.rs;
         }
     }
-    if (lane < EV_SLOTS && j0 + lane < a.keep) {
-        const int64_t at = (int64_t)b * a.keep + j0 + lane;
-        if (a.origin) a.origin[at] = src;
-        if (a.weight_out) a.weight_out[at] = src >= 0 ? weight : 0.f;
-    }
-    if (__ballot(from >= 0) == 0) return;
     u32x4_t piece[EV_LOADS];
     int64_t dst[EV_LOADS];
 #pragma unroll
@@ -475,6 +469,11 @@ __global__ __launch_bounds__(64) void evict_kernel(EvictArgs a) {
         const int64_t f = __shfl(from, r), t = __shfl(to, r);
         dst[i] = f >= 0 ? t + 8 * p : -1;
         piece[i] = f >= 0 ? *reinterpret_cast<const u32x4_t*>(a.cache + f + 8 * p) : u32x4_t{0, 0, 0, 0};
+    }
+    if (lane < EV_SLOTS && j0 + lane < a.keep) {
+        const int64_t at = (int64_t)b * a.keep + j0 + lane;
+        if (a.origin) a.origin[at] = src;
+        if (a.weight_out) a.weight_out[at] = src >= 0 ? weight : 0.f;
     }
 #pragma unroll
     for (int i = 0; i < EV_LOADS; ++i)
