@@ -206,9 +206,28 @@ def _stride(t: torch.Tensor, dim: int) -> int:
     return t.stride(dim) if t.shape[dim] > 1 else 0
 
 
-def _call_stream(ctx: "Context", stream) -> int:
-    """The stream of a call: the given one, else the current one of the context's device."""
-    return (torch.cuda.current_stream(ctx.device) if stream is None else stream).cuda_stream
+def _one_device(*tensors) -> int:
+    """The device index of tensors that have to lie on one (-1: in host memory, which no call takes)."""
+    at = {t.get_device() for t in tensors if t is not None}
+    if len(at) > 1:
+        raise ValueError("tensors on different devices: " + ", ".join(sorted({str(t.device) for t in tensors if t is not None})))
+    return at.pop()
+
+
+def _call_stream(ctx: "Context", stream, held: int, *tensors) -> int:
+    """The stream of a call, the given one or else the current one of the context's device, after what is given is found to
+    lie there: the device of a description's tensors, the call's own tensors, the stream."""
+    here = ctx.device
+    if held != here:
+        raise ValueError(f"tensors on {'cuda:%d' % held if held >= 0 else 'cpu'}, the context's device is cuda:{here}")
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError(f"a tensor on {t.device}, the context's device is cuda:{here}")
+    if stream is None:
+        return torch.cuda.current_stream(here).cuda_stream
+    if stream.device.index != here:
+        raise ValueError(f"a stream of {stream.device}, the context's device is cuda:{here}")
+    return stream.cuda_stream
 
 
 class Context:
@@ -499,6 +518,7 @@ class Prompt:
     def __init__(self, q, k, v, cu, max_len: int, k_rope=None):
         bf = torch.bfloat16
         self.tensors = (q, k, v, cu, k_rope)  # keep alive
+        self.device = _one_device(*self.tensors)
         s = _Prompt()
         s.q = _typed(q, bf, "q", (None, None, None), False)
         n, s.H = q.shape[0], q.shape[1]
@@ -526,7 +546,7 @@ def prompt_attend(ctx: Context, prompt: Prompt, scale: float, out: torch.Tensor,
     ctx.check(ctx.lib.vkv_prompt_attend(
         ctx.handle, prompt.ref, float(scale),
         _typed(out, torch.bfloat16, "out", (prompt.n_tok, prompt.H, prompt.dv)),
-        _typed(lse, torch.float32, "lse", (prompt.n_tok, prompt.H)), _call_stream(ctx, stream)))
+        _typed(lse, torch.float32, "lse", (prompt.n_tok, prompt.H)), _call_stream(ctx, stream, prompt.device, out, lse)))
 
 
 class Pages:
@@ -535,6 +555,7 @@ class Pages:
 
     def __init__(self, cache, table, kv_len, max_kv: int):
         self.tensors = (cache, table, kv_len)  # keep alive
+        self.device = _one_device(*self.tensors)
         s = _Pages()
         s.cache = _typed(cache, torch.bfloat16, "cache", (None, None, D_ROW), False)
         s.table = _typed(table, torch.int32, "table", (None, None), False)
@@ -572,6 +593,7 @@ class Chunk:
 
     def __init__(self, q_lat, q_rope, cu, max_q: int):
         self.tensors = (q_lat, q_rope, cu)  # keep alive
+        self.device = _one_device(*self.tensors)
         n, H = q_lat.shape[0], q_lat.shape[1]
         s = _Chunk()
         for name, t, d in (("q_lat", q_lat, D_LAT), ("q_rope", q_rope, D_ROPE)):
@@ -593,6 +615,8 @@ class Chunk:
 def _sequences(pages: Pages, chunk: Chunk):
     if pages.B != chunk.B:
         raise ValueError(f"{pages.B} sequences in the pages, {chunk.B} in the chunk")
+    if pages.device != chunk.device:
+        raise ValueError("the pages and the chunk lie on different devices")
 
 
 def chunk_workspace_size(pages: Pages, chunk: Chunk) -> int:
@@ -613,7 +637,7 @@ def chunk_attend(ctx: Context, pages: Pages, chunk: Chunk, ws: torch.Tensor, sca
     ctx.check(ctx.lib.vkv_chunk_attend(
         ctx.handle, pages.ref, chunk.ref, _ptr(ws), ws.nbytes, float(scale),
         _typed(out, torch.bfloat16, "out", (n, H, D_LAT)), _typed(lse, torch.float32, "lse", (n, H)),
-        _call_stream(ctx, stream)))
+        _call_stream(ctx, stream, pages.device, ws, out, lse)))
 
 
 def weight_workspace_size(pages: Pages, chunk: Chunk) -> int:
@@ -636,7 +660,7 @@ def weight_accumulate(ctx: Context, pages: Pages, chunk: Chunk, lse: torch.Tenso
         ctx.handle, pages.ref, chunk.ref, _typed(lse, f, "lse", (chunk.n_tok, chunk.H)), _ptr(ws),
         0 if ws is None else ws.nbytes, float(scale), float(decay),
         _typed(prev, f, "prev", weight.shape), _typed(weight, f, "weight", (pages.B, None)), weight.shape[1],
-        _call_stream(ctx, stream)))
+        _call_stream(ctx, stream, pages.device, lse, ws, prev, weight)))
 
 
 def weight_select(ctx: Context, weight: torch.Tensor, kv_len: torch.Tensor, max_kv: int, nsink: int, recent: int,
@@ -647,7 +671,7 @@ def weight_select(ctx: Context, weight: torch.Tensor, kv_len: torch.Tensor, max_
     ctx.check(ctx.lib.vkv_weight_select(
         ctx.handle, _typed(weight, torch.float32, "weight", (None, None)), B, int(max_kv), weight.shape[1],
         _typed(kv_len, i32, "kv_len", (B,)), kept.shape[-1], int(nsink), int(recent), _typed(kept, i32, "kept", (B, None)),
-        _typed(count, i32, "count", (B,)), _call_stream(ctx, stream)))
+        _typed(count, i32, "count", (B,)), _call_stream(ctx, stream, weight.get_device(), kv_len, kept, count)))
 
 
 def cache_evict(ctx: Context, pages: Pages, kept: torch.Tensor, count: torch.Tensor,
@@ -660,7 +684,8 @@ def cache_evict(ctx: Context, pages: Pages, kept: torch.Tensor, count: torch.Ten
     ctx.check(ctx.lib.vkv_cache_evict(
         ctx.handle, pages.ref, _typed(kept, i32, "kept", (B, K)), _typed(count, i32, "count", (B,)), K,
         _typed(origin, i32, "origin", (B, K)), _typed(weight, f, "weight", (B, None)),
-        0 if weight is None else weight.shape[1], _typed(weight_out, f, "weight_out", (B, K)), _call_stream(ctx, stream)))
+        0 if weight is None else weight.shape[1], _typed(weight_out, f, "weight_out", (B, K)),
+        _call_stream(ctx, stream, pages.device, kept, count, origin, weight, weight_out)))
 
 
 def check_rows(ctx: Context, step: Step, k: int, sel: Optional[torch.Tensor],
