@@ -560,8 +560,9 @@ typedef struct vkv_pages {
  *   q_rope  likewise, 64 bf16 (with n_tok = 0 these, and what the calls below read or
  *           write per token, may be NULL)
  *   cu      [B + 1] int32 (device), ascending, cu[0] = 0; offsets outside
- *           [0, n_tok] are taken as the nearest bound, a sequence's tokens past
- *           its first max_q are left out
+ *           [0, n_tok] are taken as the nearest bound; a sequence's tokens past
+ *           its first max_q are left out (nq, and so the rows that the others see,
+ *           stay those of the whole chunk)
  * 1 <= H <= 128, 0 <= n_tok < 2^31, 0 <= max_q, max_q*H <= 2^30; strides multiples of
  * 8, at least 0, pointers 16-byte aligned.
  */

@@ -54,7 +54,8 @@ constexpr int CK_SMEM = CK_OFF_GONE + CK_STAGES * CK_WAVES * 4;
 struct CkUnit {
     int b, row0, nrow;      // sequence, first row of the block, rows of the sequence
     int64_t tok0;           // first token of the sequence among the packed ones
-    int nq, kv;             // new tokens and cache rows of the sequence
+    int nq, kv;             // new tokens (max_q at most) and cache rows of the sequence
+    int old;                // its rows before the new tokens' (below 0: more tokens than rows)
 };
 
 __device__ __forceinline__ CkUnit chunk_unit(const ChunkArgs& a, int u, int rows) {
@@ -67,6 +68,7 @@ __device__ __forceinline__ CkUnit chunk_unit(const ChunkArgs& a, int u, int rows
     x.nq = (int)min(e - s, (int64_t)a.max_q);
     x.nrow = x.nq * a.H;
     x.kv = min(max(a.kv_len[x.b], 0), a.max_kv);
+    x.old = rows_before(x.kv, e - s, a.max_q);
     return x;
 }
 
@@ -75,7 +77,7 @@ __device__ __forceinline__ CkUnit chunk_unit(const ChunkArgs& a, int u, int rows
 __device__ __forceinline__ int unit_tiles(const ChunkArgs& a, const CkUnit& x, int rows) {
     if (x.row0 >= x.nrow) return 0;
     const int last = min(x.row0 + rows, x.nrow) - 1;
-    const int seen = max(x.kv - x.nq + last / a.H + 1, 0);
+    const int seen = max(x.old + last / a.H + 1, 0);
     return max((seen + CK_TILE - 1) / CK_TILE, 1);
 }
 
@@ -135,7 +137,7 @@ __device__ __forceinline__ bool chunk_segment(const ChunkArgs& a, const CkUnit& 
     const int qg = wave % QG, ks0 = wave / QG;
     const int R = x.row0 + 16 * qg + c;                         // this lane's row
     const int Rc = min(R, x.nrow - 1);                          // rows past the end repeat the last one, never stored
-    const int lim = min(x.kv - x.nq + Rc / a.H, x.kv - 1);      // the last cache row it sees
+    const int lim = min(x.old + Rc / a.H, x.kv - 1);            // the last cache row it sees
     const int lim_lo = __builtin_amdgcn_readfirstlane(lim);     // of the wave's rows
     const int lim_hi = __builtin_amdgcn_readlane(lim, 15);
     const bool idle = x.row0 + 16 * qg >= x.nrow;

@@ -22,12 +22,12 @@ constexpr int WT_KS = D_ROW / 16;
 static_assert(D_LAT == 512 && D_ROW == 576 && WT_TILE == 32 && WT_WAVES == 4, "a latent row per load; one rope load a wave");
 
 // rows new in this chunk start at 0; a sequence without new tokens keeps its weights
-__device__ __forceinline__ void finish(const WeightArgs& w, int b, int u, int kv, int nq, float sum) {
+__device__ __forceinline__ void finish(const WeightArgs& w, int b, int u, int kv, int old, float sum) {
     const int64_t at = (int64_t)b * w.stride + u;
-    if (nq == 0)
+    if (old == kv)
         w.weight[at] = w.prev ? w.prev[at] : 0.f;
     else
-        w.weight[at] = w.prev && w.decay != 0.f && u < kv - nq ? __builtin_fmaf(w.decay, w.prev[at], sum) : sum;
+        w.weight[at] = w.prev && w.decay != 0.f && u < old ? __builtin_fmaf(w.decay, w.prev[at], sum) : sum;
 }
 
 // --------------------------------------------------------------- many queries
@@ -61,13 +61,15 @@ static_assert(WT_KS % (WW_SD + 1) == 0, "operands keep their registers from tile
 static_assert((WW_ROWS * WT_TILE) % (WT_TILE * WT_TILE) == 0, "whole tiles per block of new rows and head");
 
 // A sequence's blocks and their query tiles: all ntile for the first `full` blocks; those of the new rows are not
-// seen by the first tokens, and begin at tile first, first + step, ...
+// seen by the first tokens, and begin at tile first, first + step, ... (`some` of them; the rows of tokens past the
+// first max_q are seen by none)
 struct WeightSpan {
-    int kv, nq, nblk, ntile, full, first, step;
+    int kv, nq, old, nblk, ntile, full, first, step, some;
     int64_t cost;             // tiles in all, with WW_LOAD a block before its own (one of a sequence without new tokens)
     int64_t tok0;
     __device__ __forceinline__ int64_t later(int64_t j) const {   // tiles of the first j blocks after the full ones
-        return j * (ntile - first + WW_LOAD) - (int64_t)step * (j * (j - 1) / 2);
+        const int64_t i = min(j, (int64_t)some);
+        return j * WW_LOAD + i * (ntile - first) - (int64_t)step * (i * (i - 1) / 2);
     }
 };
 __device__ __forceinline__ WeightSpan weight_span(const ChunkArgs& a, int b) {
@@ -78,10 +80,11 @@ __device__ __forceinline__ WeightSpan weight_span(const ChunkArgs& a, int b) {
     s.nq = (int)min(tok1 - s.tok0, (int64_t)a.max_q);
     s.nblk = (s.kv + WW_ROWS - 1) / WW_ROWS;
     s.ntile = max((s.nq * a.H + WT_TILE - 1) / WT_TILE, 1);
-    const int old = s.kv - s.nq;
-    s.full = old < 0 ? 0 : min(s.nblk, old / WW_ROWS + 1);
-    s.first = s.full < s.nblk ? (int)((int64_t)(s.full * WW_ROWS - old) * a.H / WT_TILE) : 0;
+    s.old = rows_before(s.kv, tok1 - s.tok0, a.max_q);
+    s.full = s.old < 0 ? 0 : min(s.nblk, s.old / WW_ROWS + 1);
+    s.first = s.full < s.nblk ? (int)((int64_t)(s.full * WW_ROWS - s.old) * a.H / WT_TILE) : 0;
     s.step = WW_ROWS / WT_TILE * a.H;
+    s.some = min(s.nblk - s.full, (max(s.ntile - s.first, 0) + s.step - 1) / s.step);
     s.cost = (int64_t)s.full * (s.ntile + WW_LOAD) + s.later(s.nblk - s.full);
     return s;
 }
@@ -107,10 +110,10 @@ __device__ __forceinline__ WeightPlace weight_place(const WeightSpan& s, int64_t
             else hi = mid;
         }
         p.blk = s.full + lo;
-        p.t0 = s.first + s.step * lo;
+        p.t0 = s.first + s.step * min(lo, s.some);     // (behind the last tile: none)
         p.k = off - s.later(lo);
     }
-    p.n = s.ntile - p.t0 + WW_LOAD;
+    p.n = max(s.ntile - p.t0, 0) + WW_LOAD;
     return p;
 }
 
@@ -186,6 +189,7 @@ __global__ __launch_bounds__(WT_THREADS, 1) void weight_many_kernel(WeightArgs w
         off += n;
         left -= n;
         const int kv = __builtin_amdgcn_readfirstlane(sp.kv), nq = __builtin_amdgcn_readfirstlane(sp.nq), nrow = nq * a.H;
+        const int old = __builtin_amdgcn_readfirstlane(sp.old);
         const int blk = __builtin_amdgcn_readfirstlane(pl.blk);
         const int k0 = __builtin_amdgcn_readfirstlane((int)pl.k) - WW_LOAD, first = __builtin_amdgcn_readfirstlane(pl.t0);
         const int t0 = first + max(k0, 0), t1 = nq > 0 ? first + max(k0 + n, 0) : t0;
@@ -307,7 +311,7 @@ __global__ __launch_bounds__(WT_THREADS, 1) void weight_many_kernel(WeightArgs w
                 return __builtin_amdgcn_exp2f(__builtin_fmaf(x, a.scale_log2, -1.4426950408889634f * l));
             };
             // tiles [safe0, safe1) hold whole queries that see all of the wave's rows
-            const int64_t full = (int64_t)a.H * (uw + 63 - (kv - nq));
+            const int64_t full = a.H * ((int64_t)(uw + 63) - old);
             const int safe0 = ((int)max(min(full, (int64_t)nrow), (int64_t)0) + WT_TILE - 1) / WT_TILE, safe1 = nrow / WT_TILE;
             int s = 0;
             static_for<0, WW_SD>([&](auto kc) { qload(lds0, kc); });
@@ -392,7 +396,7 @@ __global__ __launch_bounds__(WT_THREADS, 1) void weight_many_kernel(WeightArgs w
 #pragma unroll
                     for (int g = 0; g < 2; ++g) {
                         // the first query row that sees cache row u (none sees those from kv on)
-                        const int first = a.H * min(max(uw + 32 * g + (ln & 31) - (kv - nq), 0), nq);
+                        const int first = a.H * min(max(uw + 32 * g + (ln & 31) - old, 0), nq);
                         float part = 0.f;
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
@@ -442,7 +446,7 @@ __global__ __launch_bounds__(WT_THREADS, 1) void weight_many_kernel(WeightArgs w
             if (!there[g]) sums = 0.f;
             if (hh == 1) continue;
             if (!whole) slot[32 * g] = sums;
-            else if (u < kv) finish(w, b, u, kv, nq, sums);
+            else if (u < kv) finish(w, b, u, kv, old, sums);
         }
     }
 }
@@ -466,7 +470,7 @@ __global__ __launch_bounds__(WW_ROWS) void weight_join_kernel(WeightArgs w) {
     float sum = w.part[(int64_t)(2 * run + 1) * WW_ROWS + row];
     for (int r = run + 1; r < WW_RUNS && run_start(total, r) < end; ++r)
         if (run_start(total, r) < run_start(total, r + 1)) sum += w.part[(int64_t)(2 * r) * WW_ROWS + row];
-    if (u < sp.kv) finish(w, b, u, sp.kv, sp.nq, sum);
+    if (u < sp.kv) finish(w, b, u, sp.kv, sp.old, sum);
 }
 
 // ---------------------------------------------------------------- few queries
@@ -515,9 +519,9 @@ __global__ __launch_bounds__(WF_THREADS, 2) void weight_few_kernel(WeightArgs w)
         off = t1;
         const int64_t tok0 = min(max((int64_t)a.cu[b], (int64_t)0), a.n_tok);
         const int64_t tok1 = min(max((int64_t)a.cu[b + 1], tok0), a.n_tok);
-        const int nq = (int)min(tok1 - tok0, (int64_t)a.max_q), nrow = nq * a.H;
+        const int nq = (int)min(tok1 - tok0, (int64_t)a.max_q), nrow = nq * a.H, before = rows_before(kv, tok1 - tok0, a.max_q);
         if (nq == 0) {
-            for (int u = CK_TILE * t0 + tid; u < min(CK_TILE * t1, kv); u += WF_THREADS) finish(w, b, u, kv, 0, 0.f);
+            for (int u = CK_TILE * t0 + tid; u < min(CK_TILE * t1, kv); u += WF_THREADS) finish(w, b, u, kv, before, 0.f);
             continue;
         }
         const int nw = (nrow + 31) / 32;             // waves of a stream that have queries
@@ -584,7 +588,7 @@ __global__ __launch_bounds__(WF_THREADS, 2) void weight_few_kernel(WeightArgs w)
             float sum = s[0];
 #pragma unroll
             for (int i = 1; i < QW; ++i) sum += i < nw ? s[i] : 0.f;
-            if (old && u < kv - nq) sum = __builtin_fmaf(w.decay, pv, sum);
+            if (old && u < before) sum = __builtin_fmaf(w.decay, pv, sum);
             if (lane < 32 && u < kv) w.weight[(int64_t)b * w.stride + u] = sum;
         };
         for (int k = 0; k < nit; ++k) {
@@ -629,9 +633,9 @@ __global__ __launch_bounds__(WF_THREADS, 2) void weight_few_kernel(WeightArgs w)
                 }
                 const uint32_t absent = loader.absent(note);   // tile rows on no page
                 float sum = 0.f;
-                if (some || u0 + CK_TILE - 1 > kv - nq + row0 / a.H) {   // rows that a query does not see, or odd ones
+                if (some || u0 + CK_TILE - 1 > before + row0 / a.H) {   // rows that a query does not see, or odd ones
                     // the first query row that sees cache row u0 + c (none sees those from kv on)
-                    const int first = a.H * min(max(u0 + c - (kv - nq), 0), nq);
+                    const int first = a.H * min(max(u0 + c - before, 0), nq);
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.scale_log2, z[i]));

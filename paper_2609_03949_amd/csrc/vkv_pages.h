@@ -28,6 +28,12 @@ __device__ __forceinline__ int lat_xor(int r) {
 }
 __device__ __forceinline__ int rope_xor(int r) { return (r >> 1) & 7; }
 
+// The cache rows before those of a sequence's new tokens: token i sees the rows up to rows_before + i.  (Below -max_q no
+// token that is computed sees a row, and no row is older than the tokens: cut there, within 32 bits.)
+__device__ __forceinline__ int rows_before(int kv, int64_t tokens, int max_q) {
+    return (int)(kv - min(tokens, (int64_t)kv + max_q));
+}
+
 typedef __attribute__((address_space(4))) const int32_t const_i32_t;
 
 // One wave's share of the tiles of a stream of WPT waves: NR rows of each.
