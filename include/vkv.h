@@ -628,8 +628,9 @@ int vkv_weight_accumulate(vkv_ctx* ctx, const vkv_pages* pg, const vkv_chunk* ch
  * all, or every row where n <= keep.
  *   kept [B, keep] int32, ascending, -1 from count[b] on;  count [B] int32 = min(n, keep)
  * 1 <= keep <= 2^30, nsink, recent >= 0, nsink + recent <= keep,
- * weight_stride >= max_kv.  A tier for vkv_step_run_kept (with kept rows of the
- * archive) or vkv_cache_evict.
+ * weight_stride >= max_kv.  A tier for vkv_cache_evict, or, with kv_len the archive's
+ * rows, for vkv_step_run_kept and vkv_attend, which take whole tables only: every
+ * count[b] = keep, no -1.
  */
 int vkv_weight_select(vkv_ctx* ctx, const float* weight, int64_t B, int64_t max_kv, int64_t weight_stride,
                       const int32_t* kv_len, int64_t keep, int64_t nsink, int64_t recent, int32_t* kept,

@@ -29,8 +29,8 @@
 // themselves: one workgroup each, the later rows (more tiles) first.
 //
 // Measured: 512 new tokens of 128 heads behind up to 16384 rows, 3 sequences: 4.43 ms, 1.12
-// PFLOP/s (bound: LDS returns, 557 KB a tile, and the power limit); one token of 128 heads
-// over 32 x 32768 rows 295 us, 0.8 PFLOP/s (the run 275, the join 20); one token of 16
+// PFLOP/s (bound: LDS returns, 557 KB a tile at 128 bytes a cycle, 95% of the cycles); one token
+// of 128 heads over 32 x 32768 rows 293 us, 0.8 PFLOP/s (the run 275, the join 18); one token of 16
 // heads over 8192 rows 20.2 us: launches, and in the run 3 us before the loads are under
 // way, 3 us for them and the tile, 4 us for the streams' join, 1 us of stores.
 #include <algorithm>
@@ -125,8 +125,9 @@ __device__ __forceinline__ void store_row(const ChunkArgs& a, int64_t row, int g
 // false and a result is not finite: a masked row has weight 0 and 0 times a value
 // that is not finite is not 0, so with SAFE the tiles that hold masked rows take
 // those values apart; and weights above 1 may have made a sum overflow, so with
-// SAFE they are small (by a power of two: all else has the same bits).  Parts whose O
-// carries that factor have a negative l.
+// SAFE they are small (by a power of two: the same bits but for weights and sums below
+// 2^-86, whose roundings are of absolute size).  Parts whose O carries that factor have a
+// negative l.
 template <int QG, bool SAFE>
 __device__ __forceinline__ bool chunk_segment(const ChunkArgs& a, const CkUnit& x, int t0, int t1, float* part_o,
                                               float* part_ml, uint8_t* smem) {

@@ -19,7 +19,7 @@ namespace vkv {
 // in it, and the key is selected among those.  Where the bracket misses (which the
 // counts tell) or holds too many, the selection passes over all weights.
 //
-// Measured at 32 sequences of 131072 rows, m = 4096: 36 us, of which the sample and its
+// Measured at 32 sequences of 131072 rows, m = 4096: 34 us, of which the sample and its
 // bracket 7, the pass over the weights 16, the selection among the listed rows 4 and the
 // writing 5.  The pass is bound by what one compute unit does for its sequence's rows: two
 // comparisons a row and, with a bracket that holds 5% of them, a list write in most waves

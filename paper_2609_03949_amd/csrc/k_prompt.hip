@@ -18,9 +18,9 @@
 // type of V); the sum of the weights is taken before that rounding, in fp32.
 //
 // Bound: LDS, the matrix cores and the vector units each are busy half of a tile's time,
-// and long prompts run at the power limit (1.8 GHz).  Measured: 16384 tokens, 16 heads of
+// and long prompts run at the power limit (1.9 GHz).  Measured: 16384 tokens, 16 heads of
 // 192/128 dims 1217 us, 1.13 PFLOP/s; 16 prompts of 17 to 2048 tokens, 32 heads of 128 dims
-// 266 us, 0.72 PFLOP/s (more than a quarter of a workgroup's time lies before its
+// 260 to 266 us, 0.72 PFLOP/s (more than a quarter of a workgroup's time lies before its
 // second tile and after its last one).  No faster: the weights between the products of the values
 // (1256 and 268 us); the next tile's scores ahead of them, which needs registers for
 // two tiles' scores (more than 100 spilled).
@@ -99,8 +99,9 @@ struct PanelLoader {
 // a value that is not finite is not 0, so such a value would reach rows that do not see
 // it.  That shows in the result: the block then returns true and goes again with SAFE,
 // over what it stored, which takes the values that are not finite apart in the tiles
-// that hold masked keys, and keeps the weights small (by a power of two: all else has
-// the same bits), as those above 1 may have made a sum overflow.
+// that hold masked keys, and keeps the weights small (by a power of two: the same bits
+// but for weights and sums below 2^-86, whose roundings are of absolute size), as those
+// above 1 may have made a sum overflow.
 template <int DN, int DR, int DV, bool SAFE>
 __device__ __forceinline__ bool prompt_block(const PromptArgs& a, uint8_t* smem) {
     constexpr int STAGE = prompt_stage_bytes<DN, DR, DV>();

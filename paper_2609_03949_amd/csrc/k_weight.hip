@@ -45,9 +45,9 @@ __device__ __forceinline__ void finish(const WeightArgs& w, int b, int u, int kv
 // and the workgroups load their rows at different times.  A block that several runs share
 // gets its parts through the workspace, added in order by a second kernel.
 //
-// Measured at 32 tokens of 64 heads over 4 x 65536 rows (lengths from 50021): 478 us, 1.06
-// PFLOP/s, at clocks that the power limit takes to 1.5 GHz (32 rows a wave, two workgroups
-// per CU: 589 us; rows loaded as operands, 15.5 us a block, instead of whole: 485 us).
+// Measured at 32 tokens of 64 heads over 4 x 65536 rows (lengths from 50021): 451 to 478 us by
+// card, 1.06 to 1.13 PFLOP/s, at 2.0 GHz with the matrix cores busy for 53% of the cycles (32 rows a
+// wave, two workgroups per CU: 589 us; rows loaded as operands, 15.5 us a block, instead of whole: 485 us).
 
 constexpr int WW_ROWS = 64 * WT_WAVES;                   // cache rows of a block
 constexpr int WW_STAGES = 4;
@@ -482,7 +482,7 @@ __global__ __launch_bounds__(WW_ROWS) void weight_join_kernel(WeightArgs w) {
 // takes an equal run of all sequences' tiles.  A wave's sums over its queries meet those of
 // the others through LDS, one tile later.
 //
-// Measured at one token of 128 heads over 16 x 32768 rows: 119 us, 5.1 TB/s.  (Rows held in
+// Measured at one token of 128 heads over 16 x 32768 rows: 117 us, 5.2 TB/s.  (Rows held in
 // registers as with many queries, two workgroups of 128 rows per CU: 157 us, 3.8 TB/s.)
 
 constexpr int WF_WAVES = 8, WF_THREADS = 64 * WF_WAVES, WF_STAGES = 4;

@@ -28,9 +28,10 @@ __device__ __forceinline__ void static_for(F&& f) {
 // compiler sees no LDS read of a stage, so it never makes them wait for the
 // direct loads still in flight into the other stages, and the lgkmcnt waits
 // before each use are explicit (lds_wait: at most N of this wave's LDS
-// operations outstanding; LDS operations complete in order).  The kernel
-// issues no scalar memory loads inside the tile loop, so lgkmcnt counts LDS
-// operations only there.
+// operations outstanding; LDS operations complete in order).  Scalar memory
+// loads count in lgkmcnt too and end in any order; where a tile loop issues some
+// (table entries of a paged cache), one still in flight only makes a counted wait
+// longer: of the N operations that may be outstanding, fewer are LDS reads then.
 __device__ __forceinline__ uint32_t lds_addr(const void* p) {
     return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
 }
