@@ -657,8 +657,9 @@ __global__ __launch_bounds__(WF_THREADS, 2) void weight_few_kernel(WeightArgs w)
     }
 }
 
-// More than 256 query rows of the longest chunk, which the few-queries form cannot hold.  At 256 it takes 184 us where
-// runs take 238 (16 sequences of 32768 rows), 16 where they take 28 (one of 8192), 53 and 68 (64 of 2048).
+// More than 256 query rows of the longest chunk, which the few-queries form cannot hold.  At 256 (two tokens of 128 heads,
+// one in every third sequence) it takes 162 us where runs take 215 (16 sequences of 32768 rows), 16 where they take 26 (one
+// of 8192), 47 and 63 (64 of 2048).
 static bool many_queries(int64_t H, int64_t max_q) { return max_q * H > 32 * WF_WAVES; }
 
 size_t weight_workspace_bytes(int64_t H, int64_t max_q) {
