@@ -54,13 +54,22 @@ def test_runs_on_the_given_stream(ctx, name):     # noqa: F811
     call, fresh = operators(ctx)[name]
     want, blank, got = fresh(), fresh(), fresh()
     call(want, None)
+    given, other = torch.cuda.Stream(), torch.cuda.Stream()
     torch.cuda.synchronize()
-    s = torch.cuda.Stream()
-    with torch.cuda.stream(s):
-        torch.cuda._sleep(50_000_000)          # some tens of ms, behind which the call waits
-    call(got, s)
-    torch.cuda.current_stream().synchronize()
-    assert all(torch.equal(bits(a), bits(b)) for a, b in zip(got, blank)) and not s.query()
-    s.synchronize()
+    # what is launched on a stream that is being captured is recorded and does not run; the current stream runs what it gets
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=given, capture_error_mode="relaxed"):
+        with torch.cuda.stream(other):
+            call(got, given)
+    torch.cuda.synchronize()
+    assert all(torch.equal(bits(a), bits(b)) for a, b in zip(got, blank))
+    graph.replay()
+    torch.cuda.synchronize()
     assert all(torch.equal(bits(a), bits(b)) for a, b in zip(got, want))
     assert not all(torch.equal(bits(a), bits(b)) for a, b in zip(got, blank))
+    # and without a capture
+    again = fresh()
+    given.wait_stream(torch.cuda.current_stream())
+    call(again, given)
+    given.synchronize()
+    assert all(torch.equal(bits(a), bits(b)) for a, b in zip(again, want))
