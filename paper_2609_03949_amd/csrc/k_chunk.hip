@@ -35,7 +35,7 @@
 // way, 3 us for them and the tile, 4 us for the streams' join, 1 us of stores.
 #include <algorithm>
 
-#include "vkv_pages.h"
+#include "vkv_runs.h"
 
 namespace vkv {
 
@@ -49,37 +49,7 @@ constexpr int CK_OFF_ML = CK_STAGES * CK_STAGE;          // (m, l) of the waves'
 constexpr int CK_OFF_GONE = CK_OFF_ML + CK_WAVES * 16 * 8;   // per stage and wave: which of its tile rows do not exist
 constexpr int CK_SMEM = CK_OFF_GONE + CK_STAGES * CK_WAVES * 4;
 
-// ------------------------------------------------------------ units and runs
-
-struct CkUnit {
-    int b, row0, nrow;      // sequence, first row of the block, rows of the sequence
-    int64_t tok0;           // first token of the sequence among the packed ones
-    int nq, kv;             // new tokens (max_q at most) and cache rows of the sequence
-    int old;                // its rows before the new tokens' (below 0: more tokens than rows)
-};
-
-__device__ __forceinline__ CkUnit chunk_unit(const ChunkArgs& a, int u, int rows) {
-    CkUnit x;
-    x.b = u / a.mb;
-    x.row0 = (u - x.b * a.mb) * rows;
-    const int64_t s = min(max((int64_t)a.cu[x.b], (int64_t)0), a.n_tok);
-    const int64_t e = min(max((int64_t)a.cu[x.b + 1], s), a.n_tok);
-    x.tok0 = s;
-    x.nq = (int)min(e - s, (int64_t)a.max_q);
-    x.nrow = x.nq * a.H;
-    x.kv = min(max(a.kv_len[x.b], 0), a.max_kv);
-    x.old = rows_before(x.kv, e - s, a.max_q);
-    return x;
-}
-
-// tiles that some row of the block sees; a block of rows that see nothing counts
-// one, so that its outputs are written; 0: no rows
-__device__ __forceinline__ int unit_tiles(const ChunkArgs& a, const CkUnit& x, int rows) {
-    if (x.row0 >= x.nrow) return 0;
-    const int last = min(x.row0 + rows, x.nrow) - 1;
-    const int seen = max(x.old + last / a.H + 1, 0);
-    return max((seen + CK_TILE - 1) / CK_TILE, 1);
-}
+// ---------------------------------------------------------------------- runs
 
 // Runs the tiles of all units are cut into: at most one per CU, and as a run costs its tiles
 // (1.2 us each, or each round of one per stream) and its parts (written and read again: 256 KB,
@@ -92,16 +62,8 @@ __device__ __forceinline__ int run_count(const ChunkArgs& a, int total) {
     while (2.0f * (float)len <= 0.3525f * sqrtf((float)total)) len *= 2;
     return min(max((total + len - 1) / len, 1), a.runs);
 }
-__device__ __forceinline__ int run_start(int g, int n, int total) { return (int)((int64_t)g * total / n); }
 
 // ------------------------------------------------------------------ a segment
-
-typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
-
-// natural-log lse from the reference (log2 units) and the sum; nothing seen: -inf
-__device__ __forceinline__ float lse_of(float m, float l) {
-    return m == -INFINITY && l == 0.f ? -INFINITY : ((m == -INFINITY ? 0.f : m) + log2f(l)) * 0.69314718055994530942f;
-}
 
 // this lane's dims 16 dt + 4 g .. +3 of output row `row` (dt = at(0) .. at(N - 1)) from f times what
 // o holds, and its lse if `first`; rows that see nothing: 0, -inf
@@ -422,49 +384,6 @@ __device__ __forceinline__ bool chunk_segment(const ChunkArgs& a, const CkUnit& 
 
 // ------------------------------------------------------------------- kernels
 
-// first tile of every unit in the run of all tiles, and their number, into LDS
-__device__ __forceinline__ int scan_units(const ChunkArgs& a, int rows, int* pre) {
-    const int tid = threadIdx.x, lane = tid & 63, U = a.B * a.mb;
-    auto wave_prefix = [&](int v) {
-        for (int d = 1; d < 64; d *= 2) {
-            const int t = __shfl_up(v, d);
-            if (lane >= d) v += t;
-        }
-        return v;
-    };
-    if (U <= 64) {   // every wave for itself, the same values: no barrier
-        const int n = lane < U ? unit_tiles(a, chunk_unit(a, lane, rows), rows) : 0;
-        const int upto = wave_prefix(n);
-        pre[lane] = upto - n;
-        return __builtin_amdgcn_readlane(upto, 63);
-    }
-    constexpr int PER = CK_MAX_UNITS / CK_THREADS;
-    __shared__ int waves[CK_WAVES];
-    int n[PER], sum = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int u = PER * tid + i;
-        n[i] = u < U ? unit_tiles(a, chunk_unit(a, u, rows), rows) : 0;
-        sum += n[i];
-    }
-    const int upto = wave_prefix(sum);
-    if (lane == 63) waves[tid >> 6] = upto;
-    __syncthreads();
-    int at = upto - sum, total = 0;
-#pragma unroll
-    for (int i = 0; i < CK_WAVES; ++i) {
-        if (i < (tid >> 6)) at += waves[i];
-        total += waves[i];
-    }
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        pre[PER * tid + i] = at;
-        at += n[i];
-    }
-    __syncthreads();
-    return __builtin_amdgcn_readfirstlane(total);
-}
-
 // The segments of run g of n, one after another; returns whether one is to go again.
 template <int QG, bool SAFE>
 __device__ __forceinline__ bool chunk_run(const ChunkArgs& a, int g, int n, int total, const int* pre, uint8_t* smem) {
@@ -518,7 +437,7 @@ template <int QG>
 __global__ __launch_bounds__(CK_THREADS, 2) void chunk_run_kernel(ChunkArgs a) {
     __shared__ __align__(256) uint8_t smem[CK_SMEM];
     __shared__ int pre[CK_MAX_UNITS];
-    const int total = scan_units(a, 16 * QG, pre), U = a.B * a.mb;
+    const int total = scan_units<CK_TILE, CK_THREADS>(a, 16 * QG, pre), U = a.B * a.mb;
     const int n = run_count(a, total), g = blockIdx.x;
     if (g == 0)   // units without rows: nothing to join
         for (int u = threadIdx.x; u < U; u += CK_THREADS)
@@ -535,7 +454,7 @@ __global__ __launch_bounds__(CK_THREADS, 2) void chunk_unit_kernel(ChunkArgs a) 
     const int b = (int)(wg / (uint32_t)a.mb), j = a.mb - 1 - (int)(wg % (uint32_t)a.mb);
     const int u = b * a.mb + j;
     const CkUnit x = chunk_unit(a, u, 16 * QG);
-    const int n = unit_tiles(a, x, 16 * QG);
+    const int n = unit_tiles<CK_TILE>(a, x, 16 * QG);
     if (n == 0) return;
     if (chunk_segment<QG, false>(a, x, 0, n, nullptr, nullptr, smem)) chunk_unit_again<QG>(a, u, n, smem);
 }
@@ -544,25 +463,6 @@ __global__ __launch_bounds__(CK_THREADS, 2) void chunk_unit_kernel(ChunkArgs a) 
 // part, in the order the segments leave them), thread = one of them in every CKJ_GROUPS-th
 // part; then the groups join through LDS, in order.
 constexpr int CKJ_F = 128, CKJ_GROUPS = 4, CKJ_THREADS = CKJ_F * CKJ_GROUPS, CKJ_BATCH = 4;
-
-struct JoinSum {
-    float M, L;
-    f32x4_t acc;
-};
-// x += w y, and the references: weights exp2(m - M), m = -inf where nothing was seen (then 0, or NaN)
-__device__ __forceinline__ void join_add(JoinSum& x, float m, float l, const f32x4_t& v, float f) {
-    if (m > x.M) {
-        const float w = x.M == -INFINITY ? 1.0f : exp2f(x.M - m);
-        x.L *= w;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x.acc[i] *= w;
-        x.M = m;
-    }
-    const float w = m == -INFINITY ? 1.0f : exp2f(m - x.M);
-    x.L += w * l;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x.acc[i] += w * f * v[i];
-}
 
 __global__ __launch_bounds__(CKJ_THREADS) void chunk_join_kernel(ChunkArgs a, int QG) {
     __shared__ JoinSum sums[CKJ_GROUPS - 1][CKJ_F];
