@@ -24,7 +24,10 @@
  *
  * Around it: causal attention over the prompt (vkv_prompt_attend), attention of one
  * or more new tokens over a paged cache (vkv_chunk_attend), and eviction by accumulated
- * attention weight (vkv_weight_accumulate, vkv_weight_select, vkv_cache_evict).
+ * attention weight (vkv_weight_accumulate, vkv_weight_select, vkv_cache_evict).  For a cache
+ * held in 8 bits: rotary positions (vkv_rope_apply), the write of new rows (vkv_cache8_write),
+ * attention over them (vkv_chunk8_attend), and its pages, shared, reserved and moved
+ * (vkv_pages_fork, vkv_pages_reserve, vkv_pages_compact).
  *
  * Conventions (all entry points):
  *   - Pointers are DEVICE pointers unless stated.  The caller owns every
@@ -659,6 +662,175 @@ int vkv_weight_select(vkv_ctx* ctx, const float* weight, int64_t B, int64_t max_
  */
 int vkv_cache_evict(vkv_ctx* ctx, const vkv_pages* pg, const int32_t* kept, const int32_t* count, int64_t keep,
                     int32_t* origin, const float* weight, int64_t weight_stride, float* weight_out, void* stream);
+
+/* ------------------------------------------------------ rotary positions */
+
+/*
+ * Rotary positions: what q_rope and the branch r_u have been through before they meet
+ * (Sec. 3, Eq. (setup)).  `dims` dims of each row, from `first` on, are pairs (a_i, b_i),
+ * i < dims / 2: neighbours (2i, 2i + 1) if interleaved, else the halves (i, i + dims / 2).
+ * At position p
+ *   a_i' = m (a_i cos t - b_i sin t),  b_i' = m (b_i cos t + a_i sin t),  t = p f_i,
+ * m = magnitude.  With theta_i = base^(-2i/dims) the frequencies are
+ *   VKV_ROPE_PLAIN   f_i = theta_i
+ *   VKV_ROPE_LINEAR  f_i = theta_i / factor                         (positions pressed together)
+ *   VKV_ROPE_BASE    theta_i of the base  base * factor^(dims / (dims - 2))
+ *   VKV_ROPE_PARTS   f_i = theta_i ((1 - g) / factor + g),  g = clamp((n_i - slow) / (fast - slow), 0, 1),
+ *                    n_i = original theta_i / 2 pi, the turns over the original context
+ * dims: even, in [2, 256]; base > 1, factor > 0, magnitude > 0, all finite; BASE: dims >= 4;
+ * PARTS: original >= 1 and fast > slow >= 0, finite (they are ignored elsewhere; factor by PLAIN); no f_i above 1024.
+ */
+#define VKV_ROPE_PLAIN 0
+#define VKV_ROPE_LINEAR 1
+#define VKV_ROPE_BASE 2
+#define VKV_ROPE_PARTS 3
+#define VKV_ROPE_MAX_DIMS 256
+typedef struct vkv_rope {
+    int32_t dims, interleaved, scaling, reserved0;
+    double base, factor, original, fast, slow, magnitude;
+} vkv_rope;
+/* The frequencies f_i into freq[0 .. dims/2) (HOST pointer, fp64).  No device work. */
+int vkv_rope_frequencies(const vkv_rope* rope, double* freq);
+/*
+ * out = x with its pairs turned.  Row (t, h) of n_tok x H has `width` dims and lies at
+ * x + t*x_tok_stride + h*x_head_stride (elements, bf16), in out likewise; pos [n_tok] int32
+ * (device; any value, negative ones turn back).  transposed != 0 applies the transposed map
+ * (t -> -t): with the gradient of out as x, out is the gradient of x.  x and out may be the
+ * same buffer with the same strides, else they may not overlap; dims outside
+ * [first, first + dims) are copied to another out, and not touched in place.  Rows of out may not
+ * overlap each other (rows of x may: strides of 0 are a broadcast input).
+ * 1 <= H <= 65535, n_tok*H < 2^31, first >= 0, first + dims <= width <= 65536, strides at least 0.  Any
+ * alignment of 2 bytes; 16-byte aligned rows with first, dims / 2 and width multiples of 8 are fastest.
+ * The angle is the fp64 product p f_i, reduced to one turn in fp64; its sine and cosine are fp32;
+ * the products are fp32, rounded once to bf16.  Allocates nothing; fit for graph capture (replays use the
+ * frequencies of the captured call and the then current pos).
+ */
+int vkv_rope_apply(vkv_ctx* ctx, const vkv_rope* rope, const uint16_t* x, int64_t n_tok, int64_t H, int64_t width,
+                   int64_t first, int64_t x_tok_stride, int64_t x_head_stride, const int32_t* pos,
+                   int32_t transposed, uint16_t* out, int64_t out_tok_stride, int64_t out_head_stride, void* stream);
+
+/* ------------------------------------------------- the cache held in 8 bits */
+
+/*
+ * A paged latent cache held in 8 bits.  A row has VKV_ROW8 bytes: 512 codes of the latent c_u
+ * (8-bit floating point: sign, 4 exponent bits of bias 7, 3 fraction bits, largest value 448, no
+ * infinities, 0x7F and 0xFF NaN), then the branch r_u as 64 bf16, as the cache of vkv_pages holds it
+ * (with whole contexts in one stretch the index scan of VKV_MODE_ROPE reads it there).
+ * `block` consecutive rows of a page share a scale: row r of page p stands for
+ *   c_u = 2^(s - 127) * code,  s = scale[p*scale_stride + r/block],
+ * one for each block of tokens, as all heads read the one latent.  Bytes s outside [VKV_SCALE_MIN,
+ * VKV_SCALE_MAX] are taken as the nearest bound.
+ * Row r of page p is at cache + p*page_stride + r*row_stride (BYTES); table, kv_len, B,
+ * max_kv, n_pages and page are those of vkv_pages.  block: a power of two in [1, 64], at most page.
+ * Strides multiples of 16 and below 2^36, row_stride >= 640, cache 16-byte aligned; scale_stride >= page / block and
+ * below 2^31, scale at any byte.
+ */
+#define VKV_ROW8 640
+#define VKV_SCALE_MIN 63
+#define VKV_SCALE_MAX 191
+typedef struct vkv_pages8 {
+    int64_t B, max_kv, n_pages;
+    int32_t page, block;
+    uint8_t* cache;
+    int64_t row_stride, page_stride;
+    uint8_t* scale;
+    int64_t scale_stride;
+    const int32_t* table;
+    int64_t table_stride;
+    const int32_t* kv_len;
+} vkv_pages8;
+
+/*
+ * Writes the rows of the newest tokens: sequence b's tokens [cu[b], cu[b+1]) of the n_tok packed ones are
+ * its rows kv_len[b] - nq + i, nq = cu[b+1] - cu[b] (kv_len counts them already, as in vkv_chunk).
+ *   lat [n_tok, 512], rope [n_tok, 64] bf16: token t at lat + t*lat_stride, rope + t*rope_stride
+ * A block's scale is 2^e with the least e such that no new latent of it exceeds 448 * 2^e, and no less
+ * than the scale the block has, if it holds rows before the new ones; where that grows, the codes of those
+ * rows are coded again (which changes only values below 2^-6 of the new scale).  Codes are rounded to
+ * nearest, ties to even.  Values that are not finite or above 448 * 2^64 are stored as NaN and have no
+ * say in the scale; e is kept within [-64, 64].
+ * The rows behind the new ones and every other block keep their bytes.  Tokens past the first max_q of a
+ * sequence, tokens whose row would be below 0, and rows on absent pages are not written (the rows that the others take stay
+ * those of the whole chunk).  A page that is written may be in one place of one table only (vkv_pages_reserve sees to it).
+ * 0 <= n_tok < 2^31, 0 <= max_q <= 2^30; strides multiples of 8, at least 0, pointers 16-byte aligned (cu 4).
+ * No atomics: the same inputs give the same bytes.  Allocates nothing; fit for graph capture.
+ */
+int vkv_cache8_write(vkv_ctx* ctx, const vkv_pages8* pg, const uint16_t* lat, int64_t lat_stride, const uint16_t* rope,
+                     int64_t rope_stride, const int32_t* cu, int64_t n_tok, int64_t max_q, void* stream);
+
+/*
+ * vkv_chunk_attend on a cache held in 8 bits: the same chunk, scores, outputs and rules, on the rows
+ * that the codes stand for.  bf16 MFMA on the exact values of the codes (every one is a bf16 value), fp32
+ * accumulation; the weights are rounded to bf16, times the row's power of two, for the product with the codes.
+ * Rows that a token does not see do not reach it, whatever they hold.
+ * ws: vkv_chunk8_workspace_size bytes; the rules of vkv_chunk_attend's.
+ */
+int vkv_chunk8_workspace_size(const vkv_pages8* pg, const vkv_chunk* ch, size_t* bytes);
+int vkv_chunk8_attend(vkv_ctx* ctx, const vkv_pages8* pg, const vkv_chunk* ch, void* ws, size_t ws_bytes, float scale,
+                      uint16_t* out, float* lse, void* stream);
+
+/* ------------------------------------------------------ the pages' life */
+
+/*
+ * Pages that sequences hold, share and give back.  The pool's bytes lie in up to VKV_MAX_PLANES planes
+ * (the rows, their scales, an index of them; a cache of vkv_pages is one plane), each of `layers` equal layers
+ * that one table serves: page p of layer l is the `bytes` bytes at base + l*layer_stride + p*page_stride.
+ *   table   [B, table_stride] int32: entries [0, width) of each row are in use; values outside
+ *           [0, n_pages) name no page
+ *   kv_len  [B] int32: rows of each sequence
+ *   refs    [n_pages] int32: how many entries of the table name each page; a page with none is free.  The
+ *           calls below keep it so; a pool starts with refs = 0 and a table of -1 (or any state that agrees)
+ * 1 <= B <= 65535, 1 <= n_pages < 2^31, page a power of two in [1, 65536], 1 <= width <= 2^30, width*page <= 2^30,
+ * table_stride >= width, 0 <= n_planes <= VKV_MAX_PLANES; a plane: 1 <= bytes <= page_stride < 2^31,
+ * 1 <= layers <= 65535, layer_stride below 2^46 (ignored for one layer); the pages of a plane, over all its
+ * layers, may not overlap.
+ * All calls: no atomics whose order shows, so the same inputs give the same result; asynchronous, allocate
+ * nothing, fit for graph capture (replays act on the then current tables).  ws: vkv_pool_workspace_size bytes,
+ * 256-byte aligned, holds nothing between calls, may not be shared by calls that overlap; nor may two calls on one pool.
+ */
+#define VKV_MAX_PLANES 4
+typedef struct vkv_plane {
+    void* base;
+    int64_t bytes, page_stride, layers, layer_stride;
+} vkv_plane;
+typedef struct vkv_pool {
+    int64_t B, n_pages, width;
+    int32_t page, n_planes;
+    int32_t* table;
+    int64_t table_stride;
+    int32_t* kv_len;
+    int32_t* refs;
+    vkv_plane plane[VKV_MAX_PLANES];
+} vkv_pool;
+int vkv_pool_workspace_size(const vkv_pool* pool, size_t* bytes);
+
+/*
+ * Every sequence b becomes a fork of sequence from[b] as it was before the call, all at once: the same
+ * length, and the pages of its rows, shared (pages that were reserved beyond them stay with their holder).
+ * from[b] = b leaves b as it is, and any value outside [0, B) leaves it empty: its pages are given back.
+ * Beams that change places, a prompt with several answers, requests that end: one call.
+ * No bytes of a page move.  from [B] int32 (device).
+ */
+int vkv_pages_fork(vkv_ctx* ctx, const vkv_pool* pool, const int32_t* from, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Gets every sequence ready for its rows [kv_len[b], want[b]) (want taken into [0, width*page]; nothing
+ * where want[b] <= kv_len[b]): entries from kv_len/page on that name no page take a free one, and a page
+ * that holds rows below kv_len, is to take more and is shared is replaced by a copy (every plane and layer) that the sequence
+ * has for itself.  Each sharer that asks gets its own; a page that none is left to hold becomes free when
+ * the call is over.  Free pages are given lowest first, sequence by sequence, the copy first, then entry by entry.
+ * missing [B] int32: the pages that could not be had; their entries are left as they were (no page, or the shared
+ * one), and rows may not be written there.  An absent page that should hold rows below kv_len stays absent and counts as missing.
+ * kv_len is not changed.  want [B] int32 (device).
+ */
+int vkv_pages_reserve(vkv_ctx* ctx, const vkv_pool* pool, const int32_t* want, int32_t* missing, void* ws,
+                      size_t ws_bytes, void* stream);
+
+/*
+ * Moves pages so that the n in use (refs > 0) are the pages [0, n): the highest one in use goes to the lowest
+ * free one, and so on; table and refs follow.  used [1] int32 (device) = n: what lies behind can be given back.
+ */
+int vkv_pages_compact(vkv_ctx* ctx, const vkv_pool* pool, int32_t* used, void* ws, size_t ws_bytes, void* stream);
 
 /* enable != 0: vkv_step_run records a pair of HIP events around its score
  * scan, on the call's stream, for up to 512 calls; vkv_score_timing reads

@@ -23,11 +23,16 @@ __all__ = [
     "step_run_trigger", "sketch_workspace_size", "sketch_basis", "sigma_workspace_size", "sigma_close",
     "sigma_tier_size", "sigma_select", "step_run_kept", "pack_rows", "page_box", "page_bound", "SIGMA_BLOCK",
     "Prompt", "prompt_attend", "Pages", "Chunk", "chunk_workspace_size", "chunk_attend",
-    "weight_workspace_size", "weight_accumulate", "weight_select", "cache_evict", "exported_symbols",
+    "weight_workspace_size", "weight_accumulate", "weight_select", "cache_evict",
+    "VKV_ROPE_PLAIN", "VKV_ROPE_LINEAR", "VKV_ROPE_BASE", "VKV_ROPE_PARTS", "Rope", "rope_apply",
+    "Pages8", "cache8_write", "chunk8_workspace_size", "chunk8_attend",
+    "Pool", "pool_workspace_size", "pages_fork", "pages_reserve", "pages_compact", "exported_symbols",
 ]
 
 VKV_MODE_ROPE, VKV_MODE_DIGEST, VKV_MODE_ROPE_DIGEST = 1, 2, 3
+VKV_ROPE_PLAIN, VKV_ROPE_LINEAR, VKV_ROPE_BASE, VKV_ROPE_PARTS = 0, 1, 2, 3
 D_LAT, D_ROPE, D_ROW = 512, 64, 576
+ROW8, MAX_PLANES = 640, 4
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libvkv.so")
@@ -41,6 +46,8 @@ exported_symbols = (
     "vkv_sigma_select", "vkv_step_run_kept", "vkv_pack_rows", "vkv_page_box", "vkv_page_bound",
     "vkv_prompt_attend", "vkv_chunk_workspace_size", "vkv_chunk_attend", "vkv_weight_workspace_size",
     "vkv_weight_accumulate", "vkv_weight_select", "vkv_cache_evict",
+    "vkv_rope_frequencies", "vkv_rope_apply", "vkv_cache8_write", "vkv_chunk8_workspace_size", "vkv_chunk8_attend",
+    "vkv_pool_workspace_size", "vkv_pages_fork", "vkv_pages_reserve", "vkv_pages_compact",
 )
 SIGMA_BLOCK = 4096
 
@@ -93,6 +100,41 @@ class _Chunk(ctypes.Structure):
         ("n_tok", ctypes.c_int64), ("H", ctypes.c_int64), ("max_q", ctypes.c_int64),
         ("q_lat", ctypes.c_void_p), ("q_lat_stride", ctypes.c_int64),
         ("q_rope", ctypes.c_void_p), ("q_rope_stride", ctypes.c_int64), ("cu", ctypes.c_void_p),
+    ]
+
+
+class _Rope(ctypes.Structure):
+    _fields_ = [
+        ("dims", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("scaling", ctypes.c_int32),
+        ("reserved0", ctypes.c_int32), ("base", ctypes.c_double), ("factor", ctypes.c_double),
+        ("original", ctypes.c_double), ("fast", ctypes.c_double), ("slow", ctypes.c_double),
+        ("magnitude", ctypes.c_double),
+    ]
+
+
+class _Pages8(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int64), ("max_kv", ctypes.c_int64), ("n_pages", ctypes.c_int64),
+        ("page", ctypes.c_int32), ("block", ctypes.c_int32),
+        ("cache", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("page_stride", ctypes.c_int64),
+        ("scale", ctypes.c_void_p), ("scale_stride", ctypes.c_int64),
+        ("table", ctypes.c_void_p), ("table_stride", ctypes.c_int64), ("kv_len", ctypes.c_void_p),
+    ]
+
+
+class _Plane(ctypes.Structure):
+    _fields_ = [
+        ("base", ctypes.c_void_p), ("bytes", ctypes.c_int64), ("page_stride", ctypes.c_int64),
+        ("layers", ctypes.c_int64), ("layer_stride", ctypes.c_int64),
+    ]
+
+
+class _Pool(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int64), ("n_pages", ctypes.c_int64), ("width", ctypes.c_int64),
+        ("page", ctypes.c_int32), ("n_planes", ctypes.c_int32),
+        ("table", ctypes.c_void_p), ("table_stride", ctypes.c_int64), ("kv_len", ctypes.c_void_p),
+        ("refs", ctypes.c_void_p), ("plane", _Plane * MAX_PLANES),
     ]
 
 
@@ -156,6 +198,16 @@ def load():
     lib.vkv_weight_accumulate.argtypes = [P, pg, ch, P, P, sz, f32, f32, P, P, i64, P]
     lib.vkv_weight_select.argtypes = [P, P, i64, i64, i64, P, i64, i64, i64, P, P, P]
     lib.vkv_cache_evict.argtypes = [P, pg, P, P, i64, P, P, i64, P, P]
+    rp, p8, po = ctypes.POINTER(_Rope), ctypes.POINTER(_Pages8), ctypes.POINTER(_Pool)
+    lib.vkv_rope_frequencies.argtypes = [rp, P]
+    lib.vkv_rope_apply.argtypes = [P, rp, P, i64, i64, i64, i64, i64, i64, P, i32, P, i64, i64, P]
+    lib.vkv_cache8_write.argtypes = [P, p8, P, i64, P, i64, P, i64, i64, P]
+    lib.vkv_chunk8_workspace_size.argtypes = [p8, ch, ctypes.POINTER(sz)]
+    lib.vkv_chunk8_attend.argtypes = [P, p8, ch, P, sz, f32, P, P, P]
+    lib.vkv_pool_workspace_size.argtypes = [po, ctypes.POINTER(sz)]
+    lib.vkv_pages_fork.argtypes = [P, po, P, P, sz, P]
+    lib.vkv_pages_reserve.argtypes = [P, po, P, P, P, sz, P]
+    lib.vkv_pages_compact.argtypes = [P, po, P, P, sz, P]
     lib.vkv_set_timing.argtypes = [P, ctypes.c_int]
     lib.vkv_score_timing.argtypes = [P, ctypes.POINTER(ctypes.c_float), ctypes.c_int]
     for name in exported_symbols:
@@ -686,6 +738,184 @@ def cache_evict(ctx: Context, pages: Pages, kept: torch.Tensor, count: torch.Ten
         _typed(origin, i32, "origin", (B, K)), _typed(weight, f, "weight", (B, None)),
         0 if weight is None else weight.shape[1], _typed(weight_out, f, "weight_out", (B, K)),
         _call_stream(ctx, stream, pages.device, kept, count, origin, weight, weight_out)))
+
+
+class Rope:
+    """Rotary positions (``vkv_rope``): `dims` dims in pairs, neighbours if interleaved, else the two halves;
+    scaling one of VKV_ROPE_*."""
+
+    def __init__(self, dims: int, base: float = 10000.0, interleaved: bool = False, scaling: int = VKV_ROPE_PLAIN,
+                 factor: float = 1.0, original: float = 4096.0, fast: float = 32.0, slow: float = 1.0,
+                 magnitude: float = 1.0):
+        s = _Rope()
+        s.dims, s.interleaved, s.scaling = int(dims), 1 if interleaved else 0, int(scaling)
+        s.base, s.factor, s.original = float(base), float(factor), float(original)
+        s.fast, s.slow, s.magnitude = float(fast), float(slow), float(magnitude)
+        self.c = s
+        self.dims = int(dims)
+        self.frequencies()   # refuses what the calls would
+
+    def frequencies(self) -> list:
+        """vkv_rope_frequencies: the angle of each pair at position 1."""
+        lib = load()
+        f = (ctypes.c_double * max(self.dims // 2, 1))()
+        rc = lib.vkv_rope_frequencies(self.ref, f)
+        if rc != 0:
+            raise VkvError(rc, lib.vkv_last_error(None).decode())
+        return list(f)
+
+    @property
+    def ref(self):
+        return ctypes.byref(self.c)
+
+
+def rope_apply(ctx: Context, rope: Rope, x: torch.Tensor, pos: torch.Tensor, out: torch.Tensor, first: int = 0,
+               transposed: bool = False, stream=None):
+    """vkv_rope_apply: out = x with dims [first, first + rope.dims) turned by the tokens' positions pos [n] int32; x, out
+    [n,H,D] or [n,D] bf16 (any strides but the last), out may be x."""
+    bf = torch.bfloat16
+    if x.dim() not in (2, 3):
+        raise ValueError(f"x must be [n, H, D] or [n, D], got {tuple(x.shape)}")
+    px, po = _typed(x, bf, "x", None, False), _typed(out, bf, "out", x.shape, False)
+    n, H, D = x.shape[0], x.shape[1] if x.dim() == 3 else 1, x.shape[-1]
+    xs, os_ = [_stride(x, 0), _stride(x, 1) if x.dim() == 3 else 0], [_stride(out, 0), _stride(out, 1) if x.dim() == 3 else 0]
+    ctx.check(ctx.lib.vkv_rope_apply(
+        ctx.handle, rope.ref, px, n, H, D, int(first), xs[0], xs[1], _typed(pos, torch.int32, "pos", (n,)),
+        1 if transposed else 0, po, os_[0], os_[1], _call_stream(ctx, stream, x.get_device(), pos, out)))
+
+
+class Pages8:
+    """A paged latent cache held in 8 bits (``vkv_pages8``): cache [n_pages, page, 640] uint8 (any page and row strides of
+    whole 16 bytes), scale [n_pages, page / block] uint8, table [B, ceil(max_kv / page) or more] int32, kv_len [B] int32."""
+
+    def __init__(self, cache, scale, table, kv_len, max_kv: int):
+        self.tensors = (cache, scale, table, kv_len)  # keep alive
+        self.device = _one_device(*self.tensors)
+        s = _Pages8()
+        s.cache = _typed(cache, torch.uint8, "cache", (None, None, ROW8), False)
+        s.scale = _typed(scale, torch.uint8, "scale", (cache.shape[0], None), False)
+        s.table = _typed(table, torch.int32, "table", (None, None), False)
+        s.kv_len = _typed(kv_len, torch.int32, "kv_len", (table.shape[0],))
+        s.n_pages, s.page = cache.shape[0], cache.shape[1]
+        if scale.shape[1] < 1 or s.page % scale.shape[1]:
+            raise ValueError(f"{scale.shape[1]} scales for a page of {s.page} rows")
+        s.block = s.page // scale.shape[1]
+        s.page_stride = _stride(cache, 0)
+        s.row_stride = cache.stride(1) if cache.shape[1] > 1 else ROW8
+        s.scale_stride = scale.stride(0) if scale.shape[0] > 1 else scale.shape[1]
+        s.B, s.max_kv, s.table_stride = table.shape[0], int(max_kv), table.shape[1]
+        if table.shape[0] > 1:   # rows of the table may lie further apart than they are wide
+            if table.stride(0) < table.shape[1]:
+                raise ValueError("table rows overlap")
+            s.table_stride = table.stride(0)
+        if table.shape[1] * cache.shape[1] < int(max_kv):
+            raise ValueError(f"table of {table.shape[1]} pages of {cache.shape[1]} rows holds fewer than {max_kv} rows")
+        self.c = s
+        self.B, self.max_kv, self.block = s.B, s.max_kv, s.block
+
+    @property
+    def ref(self):
+        return ctypes.byref(self.c)
+
+
+def cache8_write(ctx: Context, pages: Pages8, lat: torch.Tensor, rope: torch.Tensor, cu: torch.Tensor, max_q: int, stream=None):
+    """vkv_cache8_write: the newest tokens' rows, lat [n,512] and rope [n,64] bf16 (any token stride), cu [B+1] int32, at
+    most max_q tokens a sequence, into the cache."""
+    bf = torch.bfloat16
+    n = lat.shape[0]
+    ctx.check(ctx.lib.vkv_cache8_write(
+        ctx.handle, pages.ref, _typed(lat, bf, "lat", (None, D_LAT), False), _stride(lat, 0),
+        _typed(rope, bf, "rope", (n, D_ROPE), False), _stride(rope, 0), _typed(cu, torch.int32, "cu", (pages.B + 1,)), n,
+        int(max_q), _call_stream(ctx, stream, pages.device, lat, rope, cu)))
+
+
+def chunk8_workspace_size(pages: Pages8, chunk: Chunk) -> int:
+    _sequences(pages, chunk)
+    lib = load()
+    n = ctypes.c_size_t(0)
+    rc = lib.vkv_chunk8_workspace_size(pages.ref, chunk.ref, ctypes.byref(n))
+    if rc != 0:
+        raise VkvError(rc, lib.vkv_last_error(None).decode())
+    return int(n.value)
+
+
+def chunk8_attend(ctx: Context, pages: Pages8, chunk: Chunk, ws: torch.Tensor, scale: float, out: torch.Tensor,
+                  lse: torch.Tensor, stream=None):
+    """vkv_chunk8_attend: out [n,H,512] bf16, lse [n,H] fp32."""
+    _sequences(pages, chunk)
+    n, H = chunk.n_tok, chunk.H
+    ctx.check(ctx.lib.vkv_chunk8_attend(
+        ctx.handle, pages.ref, chunk.ref, _ptr(ws), ws.nbytes, float(scale),
+        _typed(out, torch.bfloat16, "out", (n, H, D_LAT)), _typed(lse, torch.float32, "lse", (n, H)),
+        _call_stream(ctx, stream, pages.device, ws, out, lse)))
+
+
+class Pool:
+    """The pages that sequences share (``vkv_pool``): table [B, width] int32, kv_len [B] int32, refs [n_pages] int32,
+    pages of `page` rows, and the planes that hold their bytes, each [layers, n_pages, ...] of any type, a page's bytes in one
+    piece (a cache of ``Pages`` is cache[None])."""
+
+    def __init__(self, table, kv_len, refs, page: int, planes):
+        planes = list(planes)
+        self.tensors = (table, kv_len, refs, *planes)  # keep alive
+        self.device = _one_device(*self.tensors)
+        if len(planes) > MAX_PLANES:
+            raise ValueError(f"{len(planes)} planes, at most {MAX_PLANES}")
+        i32 = torch.int32
+        s = _Pool()
+        s.table = _typed(table, i32, "table", (None, None), False)
+        s.B, s.width = table.shape
+        s.table_stride = table.stride(0) if s.B > 1 else s.width
+        s.kv_len = _typed(kv_len, i32, "kv_len", (s.B,))
+        s.refs = _typed(refs, i32, "refs", (None,))
+        s.n_pages, s.page, s.n_planes = refs.shape[0], int(page), len(planes)
+        for k, t in enumerate(planes):
+            if t.dim() < 3 or t.shape[1] != s.n_pages or t.shape[0] < 1:
+                raise ValueError(f"plane {k} must be [layers, {s.n_pages}, ...], got {tuple(t.shape)}")
+            if not t[0, 0].is_contiguous():
+                raise ValueError(f"plane {k}: a page must be contiguous")
+            size, d = t.element_size(), s.plane[k]
+            d.base, d.layers, d.bytes = t.data_ptr(), t.shape[0], t[0, 0].numel() * size
+            d.page_stride = t.stride(1) * size if s.n_pages > 1 else d.bytes
+            d.layer_stride = t.stride(0) * size if t.shape[0] > 1 else 0
+        self.c = s
+        self.B, self.n_pages = s.B, s.n_pages
+
+    @property
+    def ref(self):
+        return ctypes.byref(self.c)
+
+
+def pool_workspace_size(pool: Pool) -> int:
+    lib = load()
+    n = ctypes.c_size_t(0)
+    rc = lib.vkv_pool_workspace_size(pool.ref, ctypes.byref(n))
+    if rc != 0:
+        raise VkvError(rc, lib.vkv_last_error(None).decode())
+    return int(n.value)
+
+
+def pages_fork(ctx: Context, pool: Pool, source: torch.Tensor, ws: torch.Tensor, stream=None):
+    """vkv_pages_fork: sequence b becomes a fork of sequence source[b] ([B] int32; b itself: stays, outside [0, B): empty)."""
+    ctx.check(ctx.lib.vkv_pages_fork(
+        ctx.handle, pool.ref, _typed(source, torch.int32, "source", (pool.B,)), _ptr(ws), ws.nbytes,
+        _call_stream(ctx, stream, pool.device, source, ws)))
+
+
+def pages_reserve(ctx: Context, pool: Pool, want: torch.Tensor, missing: torch.Tensor, ws: torch.Tensor, stream=None):
+    """vkv_pages_reserve: pages for the rows up to want [B] int32, and a copy of a last page that is shared; missing [B]
+    int32 <- the pages that could not be had."""
+    i32 = torch.int32
+    ctx.check(ctx.lib.vkv_pages_reserve(
+        ctx.handle, pool.ref, _typed(want, i32, "want", (pool.B,)), _typed(missing, i32, "missing", (pool.B,)), _ptr(ws),
+        ws.nbytes, _call_stream(ctx, stream, pool.device, want, missing, ws)))
+
+
+def pages_compact(ctx: Context, pool: Pool, used: torch.Tensor, ws: torch.Tensor, stream=None):
+    """vkv_pages_compact: the pages in use become the first ones; used [1] int32 <- how many they are."""
+    ctx.check(ctx.lib.vkv_pages_compact(
+        ctx.handle, pool.ref, _typed(used, torch.int32, "used", (1,)), _ptr(ws), ws.nbytes,
+        _call_stream(ctx, stream, pool.device, used, ws)))
 
 
 def check_rows(ctx: Context, step: Step, k: int, sel: Optional[torch.Tensor],

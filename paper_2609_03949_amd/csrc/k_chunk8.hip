@@ -1,0 +1,615 @@
+// k_chunk8.hip -- attention of a chunk of new tokens over a paged latent cache held in 8 bits
+// (gfx950).
+//
+//   s_u = scale * (q_lat . c_u + q_rope . r_u),  c_u = 2^e code_u,  u <= kv_len - nq + i,
+//   o_i = sum_u softmax_u(s) c_u   (512 dims)
+//
+// Units of (token, head) rows and the runs of cache tiles they are cut into are those of the bf16
+// cache's kernel.  A tile is 64 rows of 640 bytes, three of them in LDS (direct loads); a workgroup is
+// four waves, one a SIMD.  Every 8-bit value is a bf16 value, so the products take bf16 operands that are
+// exact: the conversion of the keys multiplies by their power of two, and the weights carry it for
+// the product with the values.  The conversions are what the vector units do, so each code is converted
+// once a workgroup for either product: wave w takes the scores of its 16 of the tile's rows against all
+// the unit's queries (held in registers), the weights go through LDS, and it takes the 128 dims from 128 w on
+// of the outputs.
+#include <algorithm>
+
+#include "vkv_runs.h"
+
+namespace vkv {
+
+constexpr int C8_TILE = 64, C8_WAVES = 4, C8_THREADS = 64 * C8_WAVES, C8_STAGES = 3;
+constexpr int C8_OFF_ROPE = C8_TILE * D_LAT;                    // of a stage: [64][512] codes, [64][64] bf16
+constexpr int C8_STAGE = C8_TILE * VKV_ROW8;                    // 40 KB
+// what is read at constant offsets lies first (they have 16 bits), the stages after it
+constexpr int C8_OFF_WORD = 0;                                  // per stage and row: the word that holds its scale byte
+constexpr int C8_OFF_NOTE = C8_OFF_WORD + C8_STAGES * C8_TILE * 4;   // how far to shift it, or C8_ABSENT
+constexpr int C8_OFF_TOP = C8_OFF_NOTE + C8_STAGES * C8_TILE * 4;    // per row of the unit: the waves' largest scores
+constexpr int C8_OFF_BAD = C8_OFF_TOP + 64 * 16;                // per wave: whether a score that a mask hides is NaN
+constexpr int C8_OFF_P = C8_OFF_BAD + 512;                      // weights: [rows of the unit][64] bf16
+constexpr int C8_OFF_STAGE = C8_OFF_P + 64 * 2 * C8_TILE;       // 1 KB aligned, as pieces are chosen by XORs of the address
+constexpr int C8_SMEM = C8_OFF_STAGE + C8_STAGES * C8_STAGE;
+static_assert(C8_OFF_STAGE % 1024 == 0 && C8_OFF_P % 1024 == 0, "");
+constexpr uint32_t C8_ABSENT = 255;
+constexpr float C8_SLACK = 8.0f;   // lag allowed to the softmax reference maximum (log2 units)
+
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+
+// XOR of the 16-byte piece index within the 512 bytes of tile row r, so that what a group of lanes
+// reads at a time lies in 16 pieces that differ modulo 16: the keys' 128-bit reads (16 rows, in two sets
+// of 8 whose pieces differ by 9: closed under it, as bits 0 and 3 of this are bits 2 and 3 of r) and the
+// values' transposing reads (16 rows of one piece, or rows {0-3, 8-11} or {4-7, 12-15} of two neighbours).
+__host__ __device__ constexpr int code_xor(int r) { return ((r & 3) << 1) | (r & 8) | ((r >> 2) & 1); }
+
+template <int OFF>
+__device__ __forceinline__ u32x2_t lds_read_tr8(uint32_t addr) {
+    u32x2_t v;
+    asm volatile("ds_read_b64_tr_b8 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFF));
+    return v;
+}
+template <int OFF>
+__device__ __forceinline__ u32x4_t lds_read_u4(uint32_t addr) {
+    u32x4_t v;
+    asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFF));
+    return v;
+}
+__device__ __forceinline__ uint32_t lds_read_u1(uint32_t addr) {
+    uint32_t v;
+    asm volatile("ds_read_b32 %0, %1" : "=v"(v) : "v"(addr));
+    return v;
+}
+__device__ __forceinline__ void lds_write_u1(uint32_t addr, uint32_t v) {
+    asm volatile("ds_write_b32 %0, %1" ::"v"(addr), "v"(v) : "memory");
+}
+__device__ __forceinline__ void lds_write_u2(uint32_t addr, const u32x2_t& v) {
+    asm volatile("ds_write_b64 %0, %1" ::"v"(addr), "v"(v) : "memory");
+}
+// every LDS operation of this wave is through, then every wave's
+__device__ __forceinline__ void lds_barrier() {
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// eight codes times sc (a power of two), exact
+__device__ __forceinline__ bf16x8_t decode8(uint32_t lo, uint32_t hi, float sc) {
+    bf16x2_t v[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, sc, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, sc, true),
+                     __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, sc, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, sc, true)};
+    bf16x8_t r;
+    __builtin_memcpy(&r, v, 16);
+    return r;
+}
+// NaN codes become 0: in the values of a tile where a mask hides a row that holds one (a token that sees
+// such a row has a score that is NaN, whatever its values are)
+__device__ __forceinline__ uint32_t drop_nan(uint32_t w) {
+    const uint32_t n = (((w & 0x7F7F7F7Fu) + 0x01010101u) >> 7) & 0x01010101u;
+    return w & ~((n << 8) - n);
+}
+__device__ __forceinline__ float scale_of(uint32_t word, uint32_t note) {
+    const uint32_t s = min(max((word >> (note & 31u)) & 255u, (uint32_t)VKV_SCALE_MIN), (uint32_t)VKV_SCALE_MAX);
+    return note == C8_ABSENT ? 0.f : __uint_as_float(s << 23);
+}
+
+// One wave's share of a tile: 16 of its rows, their codes, branch and scale words.
+struct Loader8 {
+    static constexpr int NR = 16;
+    const Chunk8Args& a;
+    const_i32_t* table;
+    int kv, wt, lane;
+    int32_t e[NR];          // the fetched tile's table entries (scalar)
+
+    __device__ __forceinline__ int row(int t, int i) const { return min(C8_TILE * t + NR * wt + i, kv - 1); }
+    __device__ __forceinline__ void fetch(int t) {
+        e[0] = table[row(t, 0) >> a.shift];
+        if (a.page_mask < NR - 1)
+#pragma unroll
+            for (int i = 1; i < NR; ++i) e[i] = table[row(t, i) >> a.shift];
+    }
+    // the loads of the fetched tile t into stage st (its number in LDS: sg)
+    __device__ __forceinline__ void issue(int t, uint8_t* smem, uint32_t lds0, int sg) const {
+        uint8_t* st = smem + C8_OFF_STAGE + sg * C8_STAGE;
+        const char* base[NR];
+        const uint8_t* word;     // this lane's (of 16) scale byte
+        uint32_t absent;
+        int ln = lane;
+        asm volatile("" : "+v"(ln));   // keeps the lane arithmetic out of registers across the loop
+        const int i16 = ln & 15;
+        if (a.page_mask >= NR - 1) {   // the rows lie on one page; rows past the end: the last row's
+            const int u = row(t, 0), last = min(kv - 1 - u, NR - 1);
+            const bool there = (uint32_t)e[0] < (uint32_t)a.n_pages;
+            const uint32_t p = there ? e[0] : 0, r = there ? u & a.page_mask : 0;
+            base[0] = reinterpret_cast<const char*>(a.cache8) + 16 * ((uint64_t)p * a.ps16 + (uint64_t)r * a.rs16);
+#pragma unroll
+            for (int i = 1; i < NR; ++i) base[i] = base[i - 1] + (there && i <= last ? 16 * (uint64_t)a.rs16 : 0);
+            word = a.scale + (uint64_t)p * (uint64_t)a.sstride + (there ? (r + (uint32_t)min(i16, last)) >> a.bshift : 0);
+            absent = there ? 0 : C8_ABSENT;
+        } else {
+            uint64_t pl = 0;
+            uint32_t rl = 0;
+            absent = 0;
+#pragma unroll
+            for (int i = 0; i < NR; ++i) {
+                const bool there = (uint32_t)e[i] < (uint32_t)a.n_pages;
+                const uint32_t p = there ? e[i] : 0, r = there ? row(t, i) & a.page_mask : 0;
+                base[i] = reinterpret_cast<const char*>(a.cache8) + 16 * ((uint64_t)p * a.ps16 + (uint64_t)r * a.rs16);
+                const bool mine = i16 == i;
+                pl = mine ? (uint64_t)p * (uint64_t)a.sstride : pl;
+                rl = mine ? r : rl;
+                absent = mine ? (there ? 0 : C8_ABSENT) : absent;
+            }
+            word = a.scale + pl + (rl >> a.bshift);
+        }
+        const int hb = ln >> 5;
+#pragma unroll
+        for (int i = 0; i < NR; i += 2) {
+            const char* b = hb ? base[i + 1] : base[i];
+            const uint32_t off = 16 * ((uint32_t)(ln & 31) ^ (uint32_t)code_xor(i) ^ (uint32_t)(2 * hb));
+            __builtin_amdgcn_global_load_lds((gbl_void_t*)(b + off), (lds_void_t*)(st + D_LAT * (NR * wt + i)), 16, 0, 0);
+        }
+#pragma unroll
+        for (int j = 0; j < NR; j += 8) {      // eight rows, eight lanes each
+            const char* b = base[j];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) b = (ln >> 3) == i ? base[j + i] : b;
+            const int r = j + (ln >> 3);
+            __builtin_amdgcn_global_load_lds((gbl_void_t*)(b + D_LAT + 16 * ((ln & 7) ^ rope_xor(r))),
+                                             (lds_void_t*)(st + C8_OFF_ROPE + 2 * D_ROPE * (NR * wt + j)), 16, 0, 0);
+        }
+        if (ln < NR) {   // the aligned word around the byte
+            const uint64_t at = (uint64_t)(uintptr_t)word;
+            __builtin_amdgcn_global_load_lds((gbl_void_t*)(uintptr_t)(at & ~3ull),
+                                             (lds_void_t*)(smem + C8_OFF_WORD + (sg * C8_TILE + NR * wt) * 4), 4, 0, 0);
+            lds_write_u1(lds0 + C8_OFF_NOTE + (sg * C8_TILE + NR * wt + ln) * 4, absent ? C8_ABSENT : 8u * (uint32_t)(at & 3u));
+        }
+    }
+    static constexpr int LOADS = NR / 2 + NR / 8 + 1;
+};
+
+// ------------------------------------------------------------------ a segment
+
+// Tiles [t0, t1) of unit x (16 RG rows) by one workgroup.  part: where an incomplete unit's
+// (O, m, l) go, or null (outputs).
+template <int RG>
+__device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit& x, int t0, int t1, float* part_o,
+                                               float* part_ml, uint8_t* smem) {
+    constexpr bool WIDE = RG > 1;                 // 32x32 products for the outputs
+    constexpr int RB = WIDE ? RG / 2 : 1;         // their blocks of rows
+    constexpr int NO = WIDE ? 4 : 8;              // their blocks of dims
+    constexpr int KS = WIDE ? 4 : 2;              // their steps along the tile
+    typedef typename std::conditional<WIDE, f32x16_t, f32x4_t>::type acc_t;
+    const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t lds0 = lds_addr(smem);
+    int lim[RG];                                                // the last cache row that this lane's rows see
+#pragma unroll
+    for (int i = 0; i < RG; ++i) lim[i] = min(x.old + min(x.row0 + 16 * i + c, x.nrow - 1) / a.H, x.kv - 1);   // rows past the end repeat the last one
+    const int lim_lo = __builtin_amdgcn_readfirstlane(min(x.old + x.row0 / a.H, x.kv - 1));
+    const int nt = x.kv > 0 ? t1 - t0 : 0;
+
+    Loader8 loader{a, (const_i32_t*)(a.table + (int64_t)x.b * a.tstride), x.kv, w, lane, {}};
+    // pieces of a key's codes that this lane reads: step s takes piece s ^ 9 (g & 1) ^ 16 (g >> 1), half after half
+    const int pg = 9 * (g & 1) ^ 16 * (g >> 1);
+    bf16x8_t qf[RG][18];
+#pragma unroll
+    for (int i = 0; i < RG; ++i) {
+        const int64_t row = x.tok0 * a.H + min(x.row0 + 16 * i + c, x.nrow - 1);
+        const uint16_t* ql = a.q_lat + row * a.qls;
+        const uint16_t* qr = a.q_rope + row * a.qrs + 8 * g;
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            qf[i][2 * s] = *reinterpret_cast<const bf16x8_t*>(ql + 16 * (s ^ pg));
+            qf[i][2 * s + 1] = *reinterpret_cast<const bf16x8_t*>(ql + 16 * (s ^ pg) + 8);
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s) qf[i][16 + s] = *reinterpret_cast<const bf16x8_t*>(qr + 32 * s);
+    }
+    if (nt > 0) {
+        loader.fetch(t0);
+        loader.issue(t0, smem, lds0, 0);
+        loader.fetch(t0 + 1);
+        if (nt > 1) {
+            loader.issue(t0 + 1, smem, lds0, 1);
+            loader.fetch(t0 + 2);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < RG; ++i)
+#pragma unroll
+        for (int s = 0; s < 18; ++s) asm volatile("" : "+v"(qf[i][s]));   // no wait for them inside the tile loop
+
+    acc_t o[NO][RB];
+#pragma unroll
+    for (int d = 0; d < NO; ++d)
+#pragma unroll
+        for (int r = 0; r < RB; ++r)
+#pragma unroll
+            for (int i = 0; i < (WIDE ? 16 : 4); ++i) o[d][r][i] = 0.f;
+    float m_run[RG], l_run[RG];
+#pragma unroll
+    for (int i = 0; i < RG; ++i) m_run[i] = -INFINITY, l_run[i] = 0.f;
+
+    int sg = 0;   // the stage of tile k
+    for (int k = 0; k < nt; ++k) {
+        // this wave's share of tile k has landed, and every wave's; what was read of tile k - 1 and its weights has been used
+        if (k + 1 < nt)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(Loader8::LOADS) : "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        lds_barrier();
+        if (k + 2 < nt) {
+            loader.issue(t0 + k + 2, smem, lds0, sg == 0 ? 2 : sg - 1);
+            loader.fetch(t0 + k + 3);
+        }
+        const int u0 = C8_TILE * (t0 + k);
+        const uint32_t st = lds0 + C8_OFF_STAGE + sg * C8_STAGE;
+        const uint32_t wn = lds0 + C8_OFF_WORD + (sg * C8_TILE + lane) * 4;
+        sg = sg == 2 ? 0 : sg + 1;
+
+        // ---- scores of rows 16 w .. + 15 of the tile
+        uint32_t word = lds_read_u1(wn), note = lds_read_u1(wn + (C8_OFF_NOTE - C8_OFF_WORD));
+        const int kx = 16 * code_xor(c);
+        const uint32_t ka = st + (16 * w + c) * D_LAT + ((16 * pg) ^ kx);
+        const uint32_t ra = st + C8_OFF_ROPE + (16 * w + c) * (2 * D_ROPE) + 16 * (g ^ rope_xor(c));
+        constexpr int SD = 3;          // operands read ahead of the matrix cores: 8 of codes, 2 of the branch
+        u32x4_t kc[SD + 1];
+        auto kload = [&](auto sc_) {
+            constexpr int s = decltype(sc_)::value;
+            kc[s % (SD + 1)] = lds_read_u4<0>(s < 8 ? ka ^ (16 * s) : ra ^ (64 * (s - 8)));
+        };
+        static_for<0, SD>(kload);
+        lds_wait<SD>(word, note);
+        const float sc = scale_of(word, note);                  // of tile row `lane`
+        const uint64_t absent = __ballot(sc == 0.f);
+        const float sk = __shfl(sc, 16 * w + c);                // of the key this lane decodes
+        float sp[4];                                            // of those whose scores it gets: 16 w + 4 g + i
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sp[i] = __shfl(sc, 16 * w + 4 * g + i);
+        f32x4_t s4[RG];
+#pragma unroll
+        for (int i = 0; i < RG; ++i) s4[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        static_for<0, 10>([&](auto sc_) {
+            constexpr int s = decltype(sc_)::value;
+            if constexpr (s + SD < 10) kload(std::integral_constant<int, s + SD>{});
+            u32x4_t& v = kc[s % (SD + 1)];
+            lds_wait<(s + SD < 10) ? SD : 9 - s>(v);
+            if constexpr (s < 8) {
+                const bf16x8_t k0 = decode8(v[0], v[1], sk), k1 = decode8(v[2], v[3], sk);
+#pragma unroll
+                for (int i = 0; i < RG; ++i) s4[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qf[i][2 * s], s4[i], 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < RG; ++i) s4[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, qf[i][2 * s + 1], s4[i], 0, 0, 0);
+            } else {
+#pragma unroll
+                for (int i = 0; i < RG; ++i)
+                    s4[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, v), qf[i][8 + s], s4[i], 0, 0, 0);
+            }
+        });
+
+        // ---- masks, the waves' maxima
+        bool bad = false;
+        if (u0 + C8_TILE - 1 > lim_lo || absent != 0) {
+            const uint32_t gone = (uint32_t)(absent >> (16 * w + 4 * g));
+#pragma unroll
+            for (int j = 0; j < RG; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (u0 + 16 * w + 4 * g + i > lim[j] || ((gone >> i) & 1u)) {
+                        bad |= s4[j][i] != s4[j][i];
+                        s4[j][i] = -INFINITY;
+                    }
+        }
+        float top[RG];
+#pragma unroll
+        for (int j = 0; j < RG; ++j) {
+            float m = fmaxf(fmaxf(s4[j][0], s4[j][1]), fmaxf(s4[j][2], s4[j][3]));
+            top[j] = allreduce_groups(m, [](float p, float q) { return fmaxf(p, q); }) * a.scale_log2;
+        }
+        const bool wave_bad = __ballot(bad) != 0;
+        // the weights against the reference that every wave has; they are written again where it moves
+        float ps[RG];
+        auto weights = [&]() __attribute__((always_inline)) {
+#pragma unroll
+            for (int j = 0; j < RG; ++j) {
+                const float ref = m_run[j] == -INFINITY ? 0.f : m_run[j];
+                bf16x4_t p4;
+                ps[j] = 0.f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s4[j][i], a.scale_log2, -ref));
+                    ps[j] += p;
+                    p4[i] = (__bf16)(p * sp[i]);
+                }
+                // slots of a row: as they are (16x16 products), or in each 16 of them rows 4 h + (0..3, 8..11) for half h
+                const int row = 16 * j + c, piece = WIDE ? 2 * w + (g & 1) : 2 * w + (g >> 1), half = WIDE ? g >> 1 : g & 1;
+                lds_write_u2(lds0 + C8_OFF_P + row * (2 * C8_TILE) + 16 * (piece ^ rope_xor(row)) + 8 * half,
+                             __builtin_bit_cast(u32x2_t, p4));
+            }
+        };
+        weights();
+        if (g == 0)
+#pragma unroll
+            for (int j = 0; j < RG; ++j) lds_write_u1(lds0 + C8_OFF_TOP + (16 * j + c) * 16 + 4 * w, __float_as_uint(top[j]));
+        if (lane == 0) lds_write_u1(lds0 + C8_OFF_BAD + 4 * w, wave_bad ? 1u : 0u);
+        lds_barrier();
+        u32x4_t tops[RG], bads = lds_read_u4<C8_OFF_BAD>(lds0);
+#pragma unroll
+        for (int j = 0; j < RG; ++j) tops[j] = lds_read_u4<C8_OFF_TOP>(lds0 + (16 * j + c) * 16);
+        lds_wait<0>(bads);
+        bool move = false;
+        float next[RG];
+#pragma unroll
+        for (int j = 0; j < RG; ++j) {
+            lds_wait<0>(tops[j]);
+            const float m = fmaxf(fmaxf(__uint_as_float(tops[j][0]), __uint_as_float(tops[j][1])),
+                                  fmaxf(__uint_as_float(tops[j][2]), __uint_as_float(tops[j][3])));
+            const bool up = m > m_run[j] + C8_SLACK;
+            next[j] = up ? m : m_run[j];
+            move |= up;
+        }
+        if (__ballot(move)) {   // the same in every wave
+            float al[RG];
+#pragma unroll
+            for (int j = 0; j < RG; ++j) {
+                al[j] = next[j] == m_run[j] ? 1.0f : __builtin_amdgcn_exp2f(m_run[j] - next[j]);
+                l_run[j] *= al[j];
+                m_run[j] = next[j];
+            }
+#pragma unroll
+            for (int r = 0; r < RB; ++r) {
+                float f = al[0];
+                if constexpr (WIDE) f = (lane & 16) ? al[2 * r + 1] : al[2 * r];
+#pragma unroll
+                for (int d = 0; d < NO; ++d)
+#pragma unroll
+                    for (int i = 0; i < (WIDE ? 16 : 4); ++i) o[d][r][i] *= f;
+            }
+            weights();
+            lds_barrier();
+        }
+#pragma unroll
+        for (int j = 0; j < RG; ++j) l_run[j] += ps[j];   // this lane's share of the sum
+
+        // ---- outputs, dims 128 w .. + 127
+        u32x4_t pf[KS][RB];
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int r = 0; r < RB; ++r) {
+                const int row = WIDE ? 32 * r + (lane & 31) : c, piece = WIDE ? 2 * s + (lane >> 5) : 4 * s + g;
+                pf[s][r] = lds_read_u4<C8_OFF_P>(lds0 + row * (2 * C8_TILE) + 16 * (piece ^ rope_xor(row)));
+            }
+        const int e = c >> 1;       // the row within a lane group's eight, its place among the tile's
+        const int vr = WIDE ? 4 * (lane >> 5) + (e & 3) + 8 * (e >> 2) : 8 * g + e;
+        const int vp = WIDE ? 8 * w + (g & 1) : 8 * w;
+        const uint32_t va = st + vr * D_LAT + 16 * (vp ^ code_xor(vr)) + 8 * (lane & 1);
+        auto product = [&](auto clean) __attribute__((always_inline)) {
+            constexpr int N = KS * NO, VD = 6;
+            u32x2_t vv[VD + 1];
+            auto vload = [&](auto ic) {
+                constexpr int i = decltype(ic)::value, s = i / NO, d = i % NO;
+                vv[i % (VD + 1)] = lds_read_tr8<(WIDE ? 16 : 32) * D_LAT * s>(va ^ (WIDE ? 32 * d : 16 * d));
+            };
+            static_for<0, VD>(vload);
+            static_for<0, N>([&](auto ic) {
+                constexpr int i = decltype(ic)::value, s = i / NO, d = i % NO;
+                if constexpr (i + VD < N) vload(std::integral_constant<int, i + VD>{});
+                if constexpr (i == 0)
+#pragma unroll
+                    for (int q = 0; q < KS * RB; ++q) lds_wait<VD + 1>(pf[q / RB][q % RB]);
+                lds_wait<(i + VD < N) ? VD : N - 1 - i>(vv[i % (VD + 1)]);
+                uint32_t lo = vv[i % (VD + 1)][0], hi = vv[i % (VD + 1)][1];
+                if constexpr (decltype(clean)::value) lo = drop_nan(lo), hi = drop_nan(hi);
+                const bf16x8_t v = decode8(lo, hi, 1.0f);
+#pragma unroll
+                for (int r = 0; r < RB; ++r) {
+                    const bf16x8_t p = __builtin_bit_cast(bf16x8_t, pf[s][r]);
+                    if constexpr (WIDE) o[d][r] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p, o[d][r], 0, 0, 0);
+                    else o[d][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p, o[d][r], 0, 0, 0);
+                }
+            });
+        };
+        if (bads[0] | bads[1] | bads[2] | bads[3]) product(std::true_type{});
+        else product(std::false_type{});
+    }
+
+    // ---- the sums of the waves' rows
+    __syncthreads();
+    float* sums = reinterpret_cast<float*>(smem + C8_OFF_TOP);   // [row][wave]
+#pragma unroll
+    for (int j = 0; j < RG; ++j) {
+        const float l = allreduce_groups(l_run[j], [](float p, float q) { return p + q; });
+        if (g == 0) sums[4 * (16 * j + c) + w] = l;
+    }
+    float* ref = reinterpret_cast<float*>(smem + C8_OFF_P);      // [row]
+    if (w == 0 && g == 0)
+#pragma unroll
+        for (int j = 0; j < RG; ++j) ref[16 * j + c] = m_run[j];
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+        const int row = WIDE ? 32 * r + (lane & 31) : c, R = x.row0 + row;
+        const float m = ref[row], l = (sums[4 * row] + sums[4 * row + 1]) + (sums[4 * row + 2] + sums[4 * row + 3]);
+        if (part_o) {
+            // accumulator order: [wave][dim block][row block][4][64 lanes][4], or [wave][dim block][64 lanes][4]
+#pragma unroll
+            for (int d = 0; d < NO; ++d)
+#pragma unroll
+                for (int q = 0; q < (WIDE ? 4 : 1); ++q) {
+                    const f32x4_t v = {o[d][r][4 * q], o[d][r][4 * q + 1], o[d][r][4 * q + 2], o[d][r][4 * q + 3]};
+                    *reinterpret_cast<f32x4_t*>(part_o + ((((w * NO + d) * RB + r) * (WIDE ? 4 : 1) + q) * 64 + lane) * 4) = v;
+                }
+            if (w == 0 && lane < (WIDE ? 32 : 16)) {
+                part_ml[2 * row] = m;
+                part_ml[2 * row + 1] = l;
+            }
+        } else if (R < x.nrow) {
+            const int64_t at = x.tok0 * a.H + R;
+            const bool none = m == -INFINITY && l == 0.f;
+            const float inv = none ? 0.f : 1.0f / l;
+            uint16_t* out = a.out + at * D_LAT + 128 * w + (WIDE ? 4 * (lane >> 5) : 4 * g);
+#pragma unroll
+            for (int d = 0; d < NO; ++d)
+#pragma unroll
+                for (int q = 0; q < (WIDE ? 4 : 1); ++q) {
+                    const bf16x4_t v = {(__bf16)(o[d][r][4 * q] * inv), (__bf16)(o[d][r][4 * q + 1] * inv),
+                                        (__bf16)(o[d][r][4 * q + 2] * inv), (__bf16)(o[d][r][4 * q + 3] * inv)};
+                    *reinterpret_cast<bf16x4_t*>(out + (WIDE ? 32 * d + 8 * q : 16 * d)) = v;
+                }
+            if (w == 0 && lane < (WIDE ? 32 : 16)) a.lse[at] = lse_of(m, l);
+        }
+    }
+}
+
+// ------------------------------------------------------------------- kernels
+
+// Runs the tiles of all units are cut into: at most one per CU, and no shorter than `streams` tiles.
+__device__ __forceinline__ int run_count8(const Chunk8Args& a, int total) {
+    int len = 1;
+    while (2.0f * (float)len <= 0.25f * sqrtf((float)total)) len *= 2;
+    return min(max((total + len - 1) / len, 1), a.runs);
+}
+
+template <int RG>
+__global__ __launch_bounds__(C8_THREADS, 1) void chunk8_run_kernel(Chunk8Args a) {
+    constexpr int ROWS = 16 * RG;
+    __shared__ __align__(1024) uint8_t smem[C8_SMEM];
+    __shared__ int pre[CK_MAX_UNITS];
+    const int total = scan_units<C8_TILE, C8_THREADS>(a, ROWS, pre), U = a.B * a.mb;
+    const int n = run_count8(a, total), g = blockIdx.x;
+    if (g == 0)   // units without rows: nothing to join
+        for (int u = threadIdx.x; u < U; u += C8_THREADS)
+            if ((u + 1 < U ? pre[u + 1] : total) == pre[u]) a.span[3 * u] = a.span[3 * u + 1] = 0;
+    if (g >= n) return;
+    const int beg = run_start(g, n, total), end = run_start(g + 1, n, total);
+    int u = 0;   // the last unit that starts at or before beg
+    for (int step = CK_MAX_UNITS / 2; step > 0; step /= 2)
+        if (u + step < U && pre[u + step] <= beg) u += step;
+    int at = beg;
+    while (at < end) {
+        u = __builtin_amdgcn_readfirstlane(u);
+        at = __builtin_amdgcn_readfirstlane(at);
+        const int base = __builtin_amdgcn_readfirstlane(pre[u]);
+        const int next = __builtin_amdgcn_readfirstlane(u + 1 < U ? pre[u + 1] : total);
+        if (next <= at) {   // a unit without rows
+            ++u;
+            continue;
+        }
+        const CkUnit x = chunk_unit(a, u, ROWS);
+        const int t0 = at - base, t1 = min(end, next) - base;
+        const bool whole = t0 == 0 && t1 == next - base;
+        if (threadIdx.x == 0) {   // for the join: the unit's first and last run, and which of its slots the first one fills
+            if (t0 == 0) a.span[3 * u] = g, a.span[3 * u + 2] = at > beg;
+            if (t1 == next - base) a.span[3 * u + 1] = g;
+        }
+        const int64_t slot = 2 * g + (at > beg ? 1 : 0);
+        chunk8_segment<RG>(a, x, t0, t1, whole ? nullptr : a.part_o + slot * (ROWS * D_LAT), a.part_ml + slot * (ROWS * 2), smem);
+        __syncthreads();   // the stages are free
+        at = base + t1;
+        ++u;
+    }
+}
+
+template <int RG>
+__global__ __launch_bounds__(C8_THREADS, 1) void chunk8_unit_kernel(Chunk8Args a) {
+    __shared__ __align__(1024) uint8_t smem[C8_SMEM];
+    const uint32_t wg = workgroup_id();
+    if (wg >= (uint32_t)a.B * (uint32_t)a.mb) return;
+    const int b = (int)(wg / (uint32_t)a.mb), j = a.mb - 1 - (int)(wg % (uint32_t)a.mb);   // the later rows (more tiles) first
+    const CkUnit x = chunk_unit(a, b * a.mb + j, 16 * RG);
+    const int n = unit_tiles<C8_TILE>(a, x, 16 * RG);
+    if (n == 0) return;
+    chunk8_segment<RG>(a, x, 0, n, nullptr, nullptr, smem);
+}
+
+// Joins the parts of a unit that several runs cover: block = (unit, 128 float4 of a part, in the order the
+// segments leave them), thread = one of them in every C8J_GROUPS-th part; then the groups join through LDS, in order.
+constexpr int C8J_F = 128, C8J_GROUPS = 4, C8J_THREADS = C8J_F * C8J_GROUPS, C8J_BATCH = 4;
+
+__global__ __launch_bounds__(C8J_THREADS) void chunk8_join_kernel(Chunk8Args a, int RG) {
+    __shared__ JoinSum sums[C8J_GROUPS - 1][C8J_F];
+    const int rows = 16 * RG, per = rows * (D_LAT / 4) / C8J_F;
+    const int u = blockIdx.x / per, grp = threadIdx.x / C8J_F;
+    const int f = (blockIdx.x % per) * C8J_F + threadIdx.x % C8J_F, lane = f & 63;
+    int r, d;   // row of the unit, first dim
+    if (RG == 1) {
+        r = lane & 15;
+        d = 16 * (f >> 6) + 4 * (lane >> 4);
+    } else {
+        const int rb = RG / 2, q = (f >> 6) & 3, blk = f >> 8;
+        r = 32 * (blk % rb) + (lane & 31);
+        d = 32 * (blk / rb) + 8 * q + 4 * (lane >> 5);
+    }
+    const int g0 = a.span[3 * u], g1 = a.span[3 * u + 1], late = a.span[3 * u + 2];
+    if (g0 == g1) return;
+    const CkUnit x = chunk_unit(a, u, rows);
+    const int R = x.row0 + r;
+    const bool live = R < x.nrow;
+    JoinSum t{-INFINITY, 0.f, f32x4_t{0.f, 0.f, 0.f, 0.f}};
+    if (live)
+        for (int s0 = g0 + grp; s0 <= g1; s0 += C8J_GROUPS * C8J_BATCH) {
+            float m[C8J_BATCH], l[C8J_BATCH];
+            f32x4_t v[C8J_BATCH];
+#pragma unroll
+            for (int j = 0; j < C8J_BATCH; ++j) {   // all loads in flight
+                const int run = min(s0 + C8J_GROUPS * j, g1);
+                const int64_t slot = 2 * run + (run == g0 ? late : 0);
+                const float* ml = a.part_ml + slot * (rows * 2) + 2 * r;
+                m[j] = ml[0];
+                l[j] = ml[1];
+                v[j] = *reinterpret_cast<const f32x4_t*>(a.part_o + slot * (rows * D_LAT) + 4 * f);
+            }
+#pragma unroll
+            for (int j = 0; j < C8J_BATCH; ++j)
+                if (s0 + C8J_GROUPS * j <= g1) join_add(t, m[j], l[j], v[j], 1.0f);
+        }
+    if (grp > 0) sums[grp - 1][threadIdx.x % C8J_F] = t;
+    __syncthreads();
+    if (grp > 0 || !live) return;
+#pragma unroll
+    for (int i = 0; i < C8J_GROUPS - 1; ++i) {
+        const JoinSum y = sums[i][threadIdx.x];
+        join_add(t, y.M, y.L, y.acc, 1.0f);
+    }
+    const int64_t row = x.tok0 * a.H + R;
+    const bool none = t.M == -INFINITY && t.L == 0.f;
+    const float inv = none ? 0.f : 1.0f / t.L;
+    const bf16x4_t v4 = {(__bf16)(t.acc[0] * inv), (__bf16)(t.acc[1] * inv), (__bf16)(t.acc[2] * inv), (__bf16)(t.acc[3] * inv)};
+    *reinterpret_cast<bf16x4_t*>(a.out + row * D_LAT + d) = v4;
+    if (d == 0) a.lse[row] = lse_of(t.M, t.L);
+}
+
+ChunkSplit chunk8_split(int64_t B, int64_t H, int64_t max_q, int64_t max_kv) {
+    ChunkSplit s{};
+    const int64_t rows = max_q * H;
+    s.qg = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    s.mb = (rows + 16 * s.qg - 1) / (16 * s.qg);
+    s.units = B * s.mb;
+    const int64_t tiles = s.units * std::max<int64_t>(1, (max_kv + C8_TILE - 1) / C8_TILE);
+    s.runs = s.units <= CK_MAX_UNITS && tiles < (1ll << 31) ? CK_RUNS : 0;
+    s.streams = 1;
+    if (s.runs) {
+        s.runs = std::max<int64_t>(1, std::min<int64_t>(s.runs, tiles));
+        s.part_o = (size_t)(2 * s.runs) * 16 * s.qg * D_LAT * 4;
+        s.part_ml = (size_t)(2 * s.runs) * 16 * s.qg * 2 * 4;
+        s.span = (size_t)s.units * 3 * 4;
+    }
+    return s;
+}
+
+template <int RG>
+static hipError_t launch_chunk8_rows(const Chunk8Args& a, const ChunkSplit& sp, hipStream_t s) {
+    if (!sp.runs) {
+        hipLaunchKernelGGL((chunk8_unit_kernel<RG>), grid_of(sp.units), dim3(C8_THREADS), 0, s, a);
+        return hipGetLastError();
+    }
+    hipLaunchKernelGGL((chunk8_run_kernel<RG>), dim3((unsigned)sp.runs), dim3(C8_THREADS), 0, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || sp.runs == 1) return e;
+    hipLaunchKernelGGL(chunk8_join_kernel, dim3((unsigned)(sp.units * 16 * RG * (D_LAT / 4) / C8J_F)), dim3(C8J_THREADS), 0, s, a, RG);
+    return hipGetLastError();
+}
+
+hipError_t launch_chunk8(const Chunk8Args& a, const ChunkSplit& sp, hipStream_t s) {
+    return sp.qg == 1 ? launch_chunk8_rows<1>(a, sp, s) : sp.qg == 2 ? launch_chunk8_rows<2>(a, sp, s) : launch_chunk8_rows<4>(a, sp, s);
+}
+
+}  // namespace vkv

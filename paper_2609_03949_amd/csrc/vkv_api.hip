@@ -5,6 +5,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <cmath>
 #include <vector>
 
 #include "vkv_internal.h"
@@ -762,16 +763,15 @@ static int check_pages(vkv_ctx* ctx, const vkv_pages* pg) {
     return VKV_OK;
 }
 
-static int check_chunk(vkv_ctx* ctx, const vkv_pages* pg, const vkv_chunk* ch) {
-    int rc = check_pages(ctx, pg);
-    if (rc) return rc;
+// the queries; mb: blocks of rows of a sequence, as the call cuts them
+static int check_queries(vkv_ctx* ctx, int64_t B, const vkv_chunk* ch, int64_t (*mb)(int64_t rows)) {
     if (!ch) return fail(ctx, VKV_E_ARG, "chunk is NULL");
     if (ch->H < 1 || ch->H > 128) return fail(ctx, VKV_E_SHAPE, "H=%lld outside [1, 128]", (long long)ch->H);
     if (ch->n_tok < 0 || ch->n_tok >= (1ll << 31) || ch->max_q < 0 || ch->max_q >= (1ll << 31))
         return fail(ctx, VKV_E_SHAPE, "n_tok=%lld or max_q=%lld outside [0, 2^31)", (long long)ch->n_tok, (long long)ch->max_q);
-    if (ch->max_q * ch->H > (1ll << 30) || pg->B * chunk_split(pg->B, ch->H, ch->max_q, pg->max_kv).mb >= (1ll << 31))
+    if (ch->max_q * ch->H > (1ll << 30) || B * mb(ch->max_q * ch->H) >= (1ll << 31))
         return fail(ctx, VKV_E_SHAPE, "max_q=%lld with H=%lld and B=%lld: too many rows", (long long)ch->max_q,
-                    (long long)ch->H, (long long)pg->B);
+                    (long long)ch->H, (long long)B);
     if (((!ch->q_lat || !ch->q_rope) && ch->n_tok > 0) || !ch->cu)
         return fail(ctx, VKV_E_ARG, "q_lat, q_rope and cu are required");
     if (!al16(ch->q_lat) || !al16(ch->q_rope)) return fail(ctx, VKV_E_ALIGN, "q_lat and q_rope must be 16-byte aligned");
@@ -780,6 +780,23 @@ static int check_chunk(vkv_ctx* ctx, const vkv_pages* pg, const vkv_chunk* ch) {
         return fail(ctx, VKV_E_ALIGN, "query strides %lld, %lld: need multiples of 8, at least 0", (long long)ch->q_lat_stride,
                     (long long)ch->q_rope_stride);
     return VKV_OK;
+}
+
+static int check_chunk(vkv_ctx* ctx, const vkv_pages* pg, const vkv_chunk* ch) {
+    int rc = check_pages(ctx, pg);
+    if (rc) return rc;
+    return check_queries(ctx, pg->B, ch, [](int64_t rows) { return chunk_split(1, 1, rows, 0).mb; });
+}
+
+static void query_args(ChunkArgs& a, const vkv_chunk* ch) {
+    a.q_lat = ch->q_lat;
+    a.q_rope = ch->q_rope;
+    a.qls = ch->q_lat_stride;
+    a.qrs = ch->q_rope_stride;
+    a.cu = ch->cu;
+    a.n_tok = ch->n_tok;
+    a.H = (int)ch->H;
+    a.max_q = (int)ch->max_q;
 }
 
 static ChunkArgs chunk_args(const vkv_pages* pg, const vkv_chunk* ch) {
@@ -794,16 +811,25 @@ static ChunkArgs chunk_args(const vkv_pages* pg, const vkv_chunk* ch) {
     a.tstride = pg->table_stride;
     a.kv_len = pg->kv_len;
     a.max_kv = (int)pg->max_kv;
-    a.q_lat = ch->q_lat;
-    a.q_rope = ch->q_rope;
-    a.qls = ch->q_lat_stride;
-    a.qrs = ch->q_rope_stride;
-    a.cu = ch->cu;
-    a.n_tok = ch->n_tok;
     a.B = (int)pg->B;
-    a.H = (int)ch->H;
-    a.max_q = (int)ch->max_q;
+    query_args(a, ch);
     return a;
+}
+
+// how the chunk is cut, its outputs and the workspace's arrays
+static void split_args(ChunkArgs& a, const ChunkSplit& sp, char* w, size_t po, size_t pml, size_t span, float scale, uint16_t* out,
+                       float* lse) {
+    a.mb = (int)sp.mb;
+    a.runs = (int)sp.runs;
+    a.streams = (int)sp.streams;
+    a.scale_log2 = scale * 1.4426950408889634f;
+    a.out = out;
+    a.lse = lse;
+    if (sp.runs) {
+        a.part_o = reinterpret_cast<float*>(w + po);
+        a.part_ml = reinterpret_cast<float*>(w + pml);
+        a.span = reinterpret_cast<int32_t*>(w + span);
+    }
 }
 
 // the workspace's arrays
@@ -837,21 +863,340 @@ int vkv_chunk_attend(vkv_ctx* ctx, const vkv_pages* pg, const vkv_chunk* ch, voi
     if (need > 0 && (rc = check_ws(ctx, ws, ws_bytes, need))) return rc;
     if (ch->n_tok == 0 || ch->max_q == 0) return VKV_OK;
     ChunkArgs a = chunk_args(pg, ch);
-    char* w = (char*)ws;
-    a.mb = (int)sp.mb;
-    a.runs = (int)sp.runs;
-    a.streams = (int)sp.streams;
-    a.scale_log2 = scale * 1.4426950408889634f;
-    a.out = out;
-    a.lse = lse;
-    if (sp.runs) {
-        a.part_o = reinterpret_cast<float*>(w + po);
-        a.part_ml = reinterpret_cast<float*>(w + pml);
-        a.span = reinterpret_cast<int32_t*>(w + span);
-    }
+    split_args(a, sp, (char*)ws, po, pml, span, scale, out, lse);
     DeviceGuard dev(ctx);
     HIP_TRY(ctx, dev.err);
     HIP_TRY(ctx, launch_chunk(a, sp, (hipStream_t)stream));
+    return VKV_OK;
+}
+
+// ------------------------------------------------- the cache held in 8 bits
+
+static int check_pages8(vkv_ctx* ctx, const vkv_pages8* pg) {
+    if (!pg) return fail(ctx, VKV_E_ARG, "pages is NULL");
+    if (pg->B < 1 || pg->B > 65535) return fail(ctx, VKV_E_SHAPE, "B=%lld outside [1, 65535]", (long long)pg->B);
+    if (pg->max_kv < 0 || pg->max_kv > (1ll << 30))
+        return fail(ctx, VKV_E_SHAPE, "max_kv=%lld outside [0, 2^30]", (long long)pg->max_kv);
+    if (pg->n_pages < 1 || pg->n_pages >= (1ll << 31))
+        return fail(ctx, VKV_E_SHAPE, "n_pages=%lld outside [1, 2^31)", (long long)pg->n_pages);
+    if (pg->page < 1 || pg->page > 65536 || (pg->page & (pg->page - 1)))
+        return fail(ctx, VKV_E_UNSUPPORTED, "page=%d: need a power of two in [1, 65536]", pg->page);
+    if (pg->block < 1 || pg->block > 64 || pg->block > pg->page || (pg->block & (pg->block - 1)))
+        return fail(ctx, VKV_E_UNSUPPORTED, "block=%d: need a power of two in [1, 64], at most page=%d", pg->block, pg->page);
+    if (!pg->cache || !pg->scale || (!pg->table && pg->max_kv > 0) || !pg->kv_len)
+        return fail(ctx, VKV_E_ARG, "cache, scale, table and kv_len are required");
+    if (!al16(pg->cache)) return fail(ctx, VKV_E_ALIGN, "cache must be 16-byte aligned");
+    if (!al4(pg->table) || !al4(pg->kv_len))
+        return fail(ctx, VKV_E_ALIGN, "table and kv_len must be 4-byte aligned");
+    if (pg->row_stride < VKV_ROW8 || pg->row_stride % 16)
+        return fail(ctx, VKV_E_ALIGN, "row_stride=%lld: need >= 640 and a multiple of 16", (long long)pg->row_stride);
+    if (pg->page_stride < 0 || pg->page_stride % 16)
+        return fail(ctx, VKV_E_ALIGN, "page_stride=%lld: need a multiple of 16, at least 0", (long long)pg->page_stride);
+    if (pg->row_stride / 16 >= (1ll << 32) || pg->page_stride / 16 >= (1ll << 32))
+        return fail(ctx, VKV_E_SHAPE, "row_stride=%lld or page_stride=%lld not below 2^36", (long long)pg->row_stride,
+                    (long long)pg->page_stride);
+    if (pg->scale_stride < pg->page / pg->block || pg->scale_stride >= (1ll << 31))
+        return fail(ctx, VKV_E_SHAPE, "scale_stride=%lld outside [page / block, 2^31)", (long long)pg->scale_stride);
+    if (pg->table_stride < (pg->max_kv + pg->page - 1) / pg->page)
+        return fail(ctx, VKV_E_SHAPE, "table_stride=%lld holds fewer than max_kv=%lld rows", (long long)pg->table_stride,
+                    (long long)pg->max_kv);
+    return VKV_OK;
+}
+
+static Chunk8Args pages8_args(const vkv_pages8* pg) {
+    Chunk8Args a{};
+    a.cache8 = pg->cache;
+    a.rs16 = (uint32_t)(pg->row_stride / 16);
+    a.ps16 = (uint32_t)(pg->page_stride / 16);
+    while ((1 << a.shift) < pg->page) ++a.shift;
+    a.page_mask = pg->page - 1;
+    a.n_pages = (int)pg->n_pages;
+    a.scale = pg->scale;
+    a.sstride = pg->scale_stride;
+    while ((1 << a.bshift) < pg->block) ++a.bshift;
+    a.table = pg->table;
+    a.tstride = pg->table_stride;
+    a.kv_len = pg->kv_len;
+    a.max_kv = (int)pg->max_kv;
+    a.B = (int)pg->B;
+    return a;
+}
+
+int vkv_cache8_write(vkv_ctx* ctx, const vkv_pages8* pg, const uint16_t* lat, int64_t lat_stride, const uint16_t* rope,
+                     int64_t rope_stride, const int32_t* cu, int64_t n_tok, int64_t max_q, void* stream) {
+    if (!ctx) return fail(nullptr, VKV_E_ARG, "ctx is NULL");
+    int rc = check_pages8(ctx, pg);
+    if (rc) return rc;
+    if (n_tok < 0 || n_tok >= (1ll << 31)) return fail(ctx, VKV_E_SHAPE, "n_tok=%lld outside [0, 2^31)", (long long)n_tok);
+    if (max_q < 0 || max_q > (1ll << 30)) return fail(ctx, VKV_E_SHAPE, "max_q=%lld outside [0, 2^30]", (long long)max_q);
+    if (((!lat || !rope) && n_tok > 0) || !cu) return fail(ctx, VKV_E_ARG, "lat, rope and cu are required");
+    if (!al16(lat) || !al16(rope)) return fail(ctx, VKV_E_ALIGN, "lat and rope must be 16-byte aligned");
+    if (!al4(cu)) return fail(ctx, VKV_E_ALIGN, "cu must be 4-byte aligned");
+    if (lat_stride < 0 || lat_stride % 8 || rope_stride < 0 || rope_stride % 8)
+        return fail(ctx, VKV_E_ALIGN, "strides %lld, %lld: need multiples of 8, at least 0", (long long)lat_stride, (long long)rope_stride);
+    const int64_t q = std::min(std::min(max_q, n_tok), pg->max_kv);   // rows that a sequence can take
+    if (q == 0) return VKV_OK;
+    Write8Args a{};
+    a.c = pages8_args(pg);
+    a.cache = pg->cache;
+    a.scale = pg->scale;
+    a.lat = lat;
+    a.ls = lat_stride;
+    a.rope = rope;
+    a.rs = rope_stride;
+    a.c.cu = cu;
+    a.c.n_tok = n_tok;
+    a.c.max_q = (int)max_q;
+    if (pg->B * write8_blocks(q, pg->block) >= (1ll << 31))
+        return fail(ctx, VKV_E_SHAPE, "max_q=%lld with B=%lld: too many blocks", (long long)max_q, (long long)pg->B);
+    DeviceGuard dev(ctx);
+    HIP_TRY(ctx, dev.err);
+    HIP_TRY(ctx, launch_write8(a, q, (hipStream_t)stream));
+    return VKV_OK;
+}
+
+static int check_chunk8(vkv_ctx* ctx, const vkv_pages8* pg, const vkv_chunk* ch) {
+    int rc = check_pages8(ctx, pg);
+    if (rc) return rc;
+    return check_queries(ctx, pg->B, ch, [](int64_t rows) { return chunk8_split(1, 1, rows, 0).mb; });
+}
+
+int vkv_chunk8_workspace_size(const vkv_pages8* pg, const vkv_chunk* ch, size_t* bytes) {
+    if (!bytes) return fail(nullptr, VKV_E_ARG, "bytes is NULL");
+    int rc = check_chunk8(nullptr, pg, ch);
+    if (rc) return rc;
+    size_t po, pml, span;
+    *bytes = chunk_layout(chunk8_split(pg->B, ch->H, ch->max_q, pg->max_kv), &po, &pml, &span);
+    return VKV_OK;
+}
+
+int vkv_chunk8_attend(vkv_ctx* ctx, const vkv_pages8* pg, const vkv_chunk* ch, void* ws, size_t ws_bytes, float scale,
+                      uint16_t* out, float* lse, void* stream) {
+    if (!ctx) return fail(nullptr, VKV_E_ARG, "ctx is NULL");
+    int rc = check_chunk8(ctx, pg, ch);
+    if (rc) return rc;
+    if (bad_scale(scale)) return fail(ctx, VKV_E_ARG, "scale must be positive and finite");
+    if ((!out || !lse) && ch->n_tok > 0) return fail(ctx, VKV_E_ARG, "out and lse are required");
+    if (!al16(out) || !al4(lse)) return fail(ctx, VKV_E_ALIGN, "out must be 16-byte aligned, lse 4-byte");
+    const ChunkSplit sp = chunk8_split(pg->B, ch->H, ch->max_q, pg->max_kv);
+    size_t po, pml, span;
+    const size_t need = chunk_layout(sp, &po, &pml, &span);
+    if (need > 0 && (rc = check_ws(ctx, ws, ws_bytes, need))) return rc;
+    if (ch->n_tok == 0 || ch->max_q == 0) return VKV_OK;
+    Chunk8Args a = pages8_args(pg);
+    query_args(a, ch);
+    split_args(a, sp, (char*)ws, po, pml, span, scale, out, lse);
+    DeviceGuard dev(ctx);
+    HIP_TRY(ctx, dev.err);
+    HIP_TRY(ctx, launch_chunk8(a, sp, (hipStream_t)stream));
+    return VKV_OK;
+}
+
+// ------------------------------------------------------ rotary positions
+
+static int check_rope(vkv_ctx* ctx, const vkv_rope* r) {
+    if (!r) return fail(ctx, VKV_E_ARG, "rope is NULL");
+    if (r->dims < 2 || r->dims > VKV_ROPE_MAX_DIMS || r->dims % 2)
+        return fail(ctx, VKV_E_SHAPE, "dims=%d: need an even number in [2, %d]", r->dims, VKV_ROPE_MAX_DIMS);
+    if (r->scaling < VKV_ROPE_PLAIN || r->scaling > VKV_ROPE_PARTS) return fail(ctx, VKV_E_ARG, "scaling=%d", r->scaling);
+    if (!(r->base > 1.0) || !std::isfinite(r->base) || !(r->magnitude > 0.0) || !(r->magnitude <= 3e38))
+        return fail(ctx, VKV_E_ARG, "base=%g must be above 1 and magnitude=%g above 0, both finite", r->base, r->magnitude);
+    if (r->scaling != VKV_ROPE_PLAIN && (!(r->factor > 0.0) || !std::isfinite(r->factor)))
+        return fail(ctx, VKV_E_ARG, "factor=%g must be above 0 and finite", r->factor);
+    if (r->scaling == VKV_ROPE_BASE && r->dims < 4) return fail(ctx, VKV_E_SHAPE, "VKV_ROPE_BASE needs at least 4 dims");
+    if (r->scaling == VKV_ROPE_PARTS &&
+        (!(r->original >= 1.0) || !std::isfinite(r->original) || !(r->slow >= 0.0) || !(r->fast > r->slow) || !std::isfinite(r->fast)))
+        return fail(ctx, VKV_E_ARG, "original=%g, fast=%g, slow=%g: need original >= 1 and fast > slow >= 0, finite", r->original,
+                    r->fast, r->slow);
+    return VKV_OK;
+}
+
+static bool rope_frequencies(const vkv_rope* r, double* f) {
+    const double base = r->scaling == VKV_ROPE_BASE ? r->base * std::pow(r->factor, r->dims / (r->dims - 2.0)) : r->base;
+    for (int i = 0; i < r->dims / 2; ++i) {
+        double t = std::pow(base, -2.0 * i / r->dims);
+        if (r->scaling == VKV_ROPE_LINEAR) t /= r->factor;
+        if (r->scaling == VKV_ROPE_PARTS) {
+            const double turns = r->original * t / 6.283185307179586477;
+            const double g = std::min(std::max((turns - r->slow) / (r->fast - r->slow), 0.0), 1.0);
+            t *= (1.0 - g) / r->factor + g;
+        }
+        if (!(t <= 1024.0)) return false;   // the angle of a far position would have no digit left
+        f[i] = t;
+    }
+    return true;
+}
+
+int vkv_rope_frequencies(const vkv_rope* rope, double* freq) {
+    int rc = check_rope(nullptr, rope);
+    if (rc) return rc;
+    if (!freq) return fail(nullptr, VKV_E_ARG, "freq is NULL");
+    double f[VKV_ROPE_MAX_DIMS / 2];
+    if (!rope_frequencies(rope, f)) return fail(nullptr, VKV_E_ARG, "a frequency above 1024");
+    std::copy(f, f + rope->dims / 2, freq);
+    return VKV_OK;
+}
+
+int vkv_rope_apply(vkv_ctx* ctx, const vkv_rope* rope, const uint16_t* x, int64_t n_tok, int64_t H, int64_t width,
+                   int64_t first, int64_t x_tok_stride, int64_t x_head_stride, const int32_t* pos, int32_t transposed,
+                   uint16_t* out, int64_t out_tok_stride, int64_t out_head_stride, void* stream) {
+    if (!ctx) return fail(nullptr, VKV_E_ARG, "ctx is NULL");
+    int rc = check_rope(ctx, rope);
+    if (rc) return rc;
+    if (H < 1 || H > 65535 || n_tok < 0 || n_tok >= (1ll << 31) || n_tok * H >= (1ll << 31))
+        return fail(ctx, VKV_E_SHAPE, "n_tok=%lld, H=%lld: need 1 <= H <= 65535 and n_tok * H below 2^31", (long long)n_tok, (long long)H);
+    if (width < 2 || width > 65536 || first < 0 || first + rope->dims > width)
+        return fail(ctx, VKV_E_SHAPE, "dims [%lld, %lld) outside rows of %lld (at most 65536)", (long long)first,
+                    (long long)(first + rope->dims), (long long)width);
+    if (n_tok == 0) return VKV_OK;
+    if (!x || !pos || !out) return fail(ctx, VKV_E_ARG, "x, pos and out are required");
+    if (((uintptr_t)x & 1u) || ((uintptr_t)out & 1u) || !al4(pos))
+        return fail(ctx, VKV_E_ALIGN, "x and out must be 2-byte aligned, pos 4-byte");
+    if (x_tok_stride < 0 || x_head_stride < 0 || out_tok_stride < 0 || out_head_stride < 0)
+        return fail(ctx, VKV_E_ALIGN, "strides must be at least 0");
+    const int64_t ts = n_tok > 1 ? out_tok_stride : 0, hs = H > 1 ? out_head_stride : 0;
+    if ((n_tok > 1 && out_tok_stride < width) || (H > 1 && out_head_stride < width) ||
+        (n_tok > 1 && H > 1 && out_tok_stride < (H - 1) * hs + width && out_head_stride < (n_tok - 1) * ts + width))
+        return fail(ctx, VKV_E_SHAPE, "rows of out overlap");
+    if (x == out && ((n_tok > 1 && x_tok_stride != out_tok_stride) || (H > 1 && x_head_stride != out_head_stride)))
+        return fail(ctx, VKV_E_ARG, "in place, x and out need the same strides");
+    RopeArgs a{};
+    if (!rope_frequencies(rope, a.freq)) return fail(ctx, VKV_E_ARG, "a frequency above 1024");
+    a.x = x;
+    a.out = out;
+    a.pos = pos;
+    a.n_tok = n_tok;
+    a.H = (int)H;
+    a.xts = n_tok > 1 ? x_tok_stride : 0;
+    a.xhs = H > 1 ? x_head_stride : 0;
+    a.ots = ts;
+    a.ohs = hs;
+    a.width = (int)width;
+    a.first = (int)first;
+    a.dims = rope->dims;
+    a.interleaved = rope->interleaved != 0;
+    a.transposed = transposed != 0;
+    a.magnitude = (float)rope->magnitude;
+    DeviceGuard dev(ctx);
+    HIP_TRY(ctx, dev.err);
+    HIP_TRY(ctx, launch_rope(a, (hipStream_t)stream));
+    return VKV_OK;
+}
+
+// ------------------------------------------------------ the pages' life
+
+static int check_pool(vkv_ctx* ctx, const vkv_pool* po) {
+    if (!po) return fail(ctx, VKV_E_ARG, "pool is NULL");
+    if (po->B < 1 || po->B > 65535) return fail(ctx, VKV_E_SHAPE, "B=%lld outside [1, 65535]", (long long)po->B);
+    if (po->n_pages < 1 || po->n_pages >= (1ll << 31))
+        return fail(ctx, VKV_E_SHAPE, "n_pages=%lld outside [1, 2^31)", (long long)po->n_pages);
+    if (po->page < 1 || po->page > 65536 || (po->page & (po->page - 1)))
+        return fail(ctx, VKV_E_UNSUPPORTED, "page=%d: need a power of two in [1, 65536]", po->page);
+    if (po->width < 1 || po->width > (1ll << 30) || po->width * po->page > (1ll << 30))
+        return fail(ctx, VKV_E_SHAPE, "width=%lld pages of %d rows: need 1 to 2^30 rows", (long long)po->width, po->page);
+    if (po->table_stride < po->width)
+        return fail(ctx, VKV_E_SHAPE, "table_stride=%lld below width=%lld", (long long)po->table_stride, (long long)po->width);
+    if (!po->table || !po->kv_len || !po->refs) return fail(ctx, VKV_E_ARG, "table, kv_len and refs are required");
+    if (!al4(po->table) || !al4(po->kv_len) || !al4(po->refs))
+        return fail(ctx, VKV_E_ALIGN, "table, kv_len and refs must be 4-byte aligned");
+    if (po->n_planes < 0 || po->n_planes > VKV_MAX_PLANES)
+        return fail(ctx, VKV_E_ARG, "n_planes=%d outside [0, %d]", po->n_planes, VKV_MAX_PLANES);
+    for (int k = 0; k < po->n_planes; ++k) {
+        const vkv_plane& p = po->plane[k];
+        if (!p.base) return fail(ctx, VKV_E_ARG, "plane %d has no base", k);
+        if (p.bytes < 1 || p.bytes >= (1ll << 31) || p.layers < 1 || p.layers > 65535)
+            return fail(ctx, VKV_E_SHAPE, "plane %d: %lld bytes a page in %lld layers, need [1, 2^31) and [1, 65535]", k,
+                        (long long)p.bytes, (long long)p.layers);
+        // the pages of a layer, and the layers, lie one behind another or one within the other's gaps
+        const int64_t pages = (po->n_pages - 1) * p.page_stride + p.bytes, layers = (p.layers - 1) * p.layer_stride + p.bytes;
+        if ((po->n_pages > 1 && p.page_stride < p.bytes) || p.page_stride < 0 || p.page_stride >= (1ll << 31) ||
+            (p.layers > 1 && (p.layer_stride < 0 || p.layer_stride >= (1ll << 46))) ||
+            (p.layers > 1 && po->n_pages > 1 && p.layer_stride < pages && p.page_stride < layers) ||
+            (p.layers > 1 && p.layer_stride < p.bytes))
+            return fail(ctx, VKV_E_SHAPE, "plane %d: pages overlap (strides %lld, %lld)", k, (long long)p.page_stride,
+                        (long long)p.layer_stride);
+    }
+    return VKV_OK;
+}
+
+static PoolArgs pool_args(const vkv_pool* po, void* ws) {
+    PoolArgs a{};
+    a.B = (int)po->B;
+    a.n_pages = (int)po->n_pages;
+    a.width = (int)po->width;
+    a.page = po->page;
+    a.table = po->table;
+    a.tstride = po->table_stride;
+    a.kv_len = po->kv_len;
+    a.refs = po->refs;
+    a.n_planes = po->n_planes;
+    for (int k = 0; k < po->n_planes; ++k) {
+        const vkv_plane& p = po->plane[k];
+        PoolPlane& q = a.plane[k];
+        q.base = (uint8_t*)p.base;
+        q.bytes = p.bytes;
+        q.ps = p.page_stride;
+        q.ls = p.layers > 1 ? p.layer_stride : 0;
+        q.layers = (int)p.layers;
+        const uint64_t all = (uint64_t)(uintptr_t)p.base | (uint64_t)q.bytes | (uint64_t)q.ps | (uint64_t)q.ls;
+        q.unit = all % 16 == 0 ? 16 : all % 4 == 0 ? 4 : 1;
+        q.pieces = (int)((q.bytes + 16 * 1024 - 1) / (16 * 1024));
+    }
+    a.nb = (int)((po->n_pages + POOL_BLOCK - 1) / POOL_BLOCK);
+    const PoolLayout L = pool_layout(po->B, po->n_pages, po->width);
+    char* w = (char*)ws;
+    a.head = reinterpret_cast<int32_t*>(w + L.head);
+    a.block = reinterpret_cast<int32_t*>(w + L.block);
+    a.need = reinterpret_cast<int32_t*>(w + L.need);
+    a.list = reinterpret_cast<int32_t*>(w + L.list);
+    a.from = reinterpret_cast<int32_t*>(w + L.from);
+    a.to = reinterpret_cast<int32_t*>(w + L.to);
+    a.rows = reinterpret_cast<int32_t*>(w + L.rows);
+    return a;
+}
+
+int vkv_pool_workspace_size(const vkv_pool* pool, size_t* bytes) {
+    if (!bytes) return fail(nullptr, VKV_E_ARG, "bytes is NULL");
+    int rc = check_pool(nullptr, pool);
+    if (rc) return rc;
+    *bytes = pool_layout(pool->B, pool->n_pages, pool->width).total;
+    return VKV_OK;
+}
+
+static int check_pool_call(vkv_ctx* ctx, const vkv_pool* pool, const void* in, const void* out, void* ws, size_t ws_bytes) {
+    if (!ctx) return fail(nullptr, VKV_E_ARG, "ctx is NULL");
+    int rc = check_pool(ctx, pool);
+    if (rc) return rc;
+    if (!in || !out) return fail(ctx, VKV_E_ARG, "from, want, missing and used are required");
+    if (!al4(in) || !al4(out)) return fail(ctx, VKV_E_ALIGN, "from, want, missing and used must be 4-byte aligned");
+    return check_ws(ctx, ws, ws_bytes, pool_layout(pool->B, pool->n_pages, pool->width).total);
+}
+
+int vkv_pages_fork(vkv_ctx* ctx, const vkv_pool* pool, const int32_t* from, void* ws, size_t ws_bytes, void* stream) {
+    int rc = check_pool_call(ctx, pool, from, from, ws, ws_bytes);
+    if (rc) return rc;
+    DeviceGuard dev(ctx);
+    HIP_TRY(ctx, dev.err);
+    HIP_TRY(ctx, launch_fork(pool_args(pool, ws), from, (hipStream_t)stream));
+    return VKV_OK;
+}
+
+int vkv_pages_reserve(vkv_ctx* ctx, const vkv_pool* pool, const int32_t* want, int32_t* missing, void* ws, size_t ws_bytes,
+                      void* stream) {
+    int rc = check_pool_call(ctx, pool, want, missing, ws, ws_bytes);
+    if (rc) return rc;
+    DeviceGuard dev(ctx);
+    HIP_TRY(ctx, dev.err);
+    HIP_TRY(ctx, launch_reserve(pool_args(pool, ws), want, missing, (hipStream_t)stream));
+    return VKV_OK;
+}
+
+int vkv_pages_compact(vkv_ctx* ctx, const vkv_pool* pool, int32_t* used, void* ws, size_t ws_bytes, void* stream) {
+    int rc = check_pool_call(ctx, pool, used, used, ws, ws_bytes);
+    if (rc) return rc;
+    DeviceGuard dev(ctx);
+    HIP_TRY(ctx, dev.err);
+    HIP_TRY(ctx, launch_compact(pool_args(pool, ws), used, (hipStream_t)stream));
     return VKV_OK;
 }
 

@@ -350,6 +350,75 @@ struct ChunkSplit {
 ChunkSplit chunk_split(int64_t B, int64_t H, int64_t max_q, int64_t max_kv);
 hipError_t launch_chunk(const ChunkArgs& a, const ChunkSplit& sp, hipStream_t s);
 
+// the same over a cache held in 8 bits (rs16, ps16: strides of its rows of VKV_ROW8 bytes)
+struct Chunk8Args : ChunkArgs {
+    const uint8_t* cache8;
+    const uint8_t* scale;
+    int64_t sstride;       // scale bytes from page to page
+    int bshift;            // log2 of the rows that share one
+};
+ChunkSplit chunk8_split(int64_t B, int64_t H, int64_t max_q, int64_t max_kv);
+hipError_t launch_chunk8(const Chunk8Args& a, const ChunkSplit& sp, hipStream_t s);
+
+struct Write8Args {
+    Chunk8Args c;          // the pages; cu, n_tok, max_q
+    uint8_t* cache;
+    uint8_t* scale;
+    const uint16_t* lat;   // [n_tok] rows of 512
+    const uint16_t* rope;  // [n_tok] rows of 64
+    int64_t ls, rs;        // their strides, elements
+    int mb;                // workgroups of a sequence
+};
+int64_t write8_blocks(int64_t q, int64_t block);   // workgroups of a sequence of up to q new rows
+hipError_t launch_write8(Write8Args a, int64_t q, hipStream_t s);
+
+struct RopeArgs {
+    const uint16_t* x;
+    uint16_t* out;
+    const int32_t* pos;    // [n_tok]
+    int64_t n_tok;
+    int64_t xts, xhs, ots, ohs;   // token and head strides, elements
+    int H, width, first, dims, interleaved, transposed;
+    int parts;             // workgroups of a token
+    float magnitude;
+    double freq[VKV_ROPE_MAX_DIMS / 2];
+};
+hipError_t launch_rope(RopeArgs a, hipStream_t s);
+
+struct PoolPlane {
+    uint8_t* base;
+    int64_t bytes, ps, ls; // of a page; strides of pages and layers
+    int layers;
+    int unit;              // bytes moved at a time: 16, 4 or 1
+    int pieces;            // workgroups' shares of a page of a layer
+};
+struct PoolArgs {
+    int B, n_pages, width, page;
+    int32_t* table;
+    int64_t tstride;
+    int32_t* kv_len;
+    int32_t* refs;
+    int n_planes;
+    PoolPlane plane[VKV_MAX_PLANES];
+    int nb;                // blocks of POOL_BLOCK pages
+    // workspace
+    int32_t* head;         // a few words: how many pages are copied, and the like
+    int32_t* block;        // [nb] pages of each block that are free, or in use
+    int32_t* need;         // [B] pages that a sequence needs
+    int32_t* list;         // [n_pages] free pages; or the holes that pages move into
+    int32_t* from;         // [max(n_pages, B)] pages that are copied, and
+    int32_t* to;           // where to
+    int32_t* rows;         // [B, width + 1] forks' table rows and lengths
+};
+struct PoolLayout {
+    size_t head, block, need, list, from, to, rows, total;
+};
+constexpr int POOL_BLOCK = 4096;
+PoolLayout pool_layout(int64_t B, int64_t n_pages, int64_t width);
+hipError_t launch_fork(const PoolArgs& a, const int32_t* from, hipStream_t s);
+hipError_t launch_reserve(const PoolArgs& a, const int32_t* want, int32_t* missing, hipStream_t s);
+hipError_t launch_compact(const PoolArgs& a, int32_t* used, hipStream_t s);
+
 struct WeightArgs {
     ChunkArgs c;           // cache and queries
     const float* lse;      // [n_tok, H]

@@ -1,0 +1,245 @@
+"""vkv_chunk8_attend against plain attention in 64 bits on what the codes stand for: contexts around the tiles of 64
+rows, single tokens and chunks, every split of the rows and of the work, pages and blocks of every size, tokens that
+see nothing, NaN where a token does not look, scales at their bounds, strides, graphs, streams.
+
+The bounds are those of the bf16 cache's test: the operands are exact (every code times its power of two is a bf16
+value), so the same roundings remain: fp32 sums of 576 products, the weights' rounding to bf16 (times a power of two,
+which is exact), fp32 sums over the rows, the output's rounding to bf16."""
+import math
+
+import pytest
+import torch
+
+import paper_2609_03949_amd as vkv
+
+from _attention import attention, check
+from _paged8 import Case8
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+SCALE = 1.0 / math.sqrt(192.0)
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    c = vkv.Context(0)
+    yield c
+    c.close()
+
+
+def handles(x):
+    return vkv.Pages8(x.cache, x.scale, x.table, x.kv_len, x.max_kv), vkv.Chunk(x.q_lat, x.q_rope, x.cu, x.max_q)
+
+
+def run(ctx, x, fill=7.0, stream=None):
+    pages, chunk = handles(x)
+    ws = torch.full((max(vkv.chunk8_workspace_size(pages, chunk), 256),), 0xFF, dtype=torch.uint8, device=DEV)
+    out = torch.full((x.n_tok, x.H, 512), fill, dtype=torch.bfloat16, device=DEV)
+    lse = torch.full((x.n_tok, x.H), fill, device=DEV)
+    vkv.chunk8_attend(ctx, pages, chunk, ws, SCALE, out, lse, stream)
+    return out, lse
+
+
+def compare(x, out, lse, seen=None, only=None, scale=SCALE):
+    at = 0
+    for b, nq in enumerate(x.q_lens):
+        if nq and (only is None or b in only):
+            kv = x.rows(b)
+            vis = (x.seen(b) if seen is None else seen[b])[:, None, :].expand(nq, x.H, kv.shape[0]).reshape(nq * x.H, -1)
+            kv = torch.where(vis.any(0)[:, None], kv, 0.0)      # what no token sees has no say
+            q = x.q[at:at + nq].reshape(nq * x.H, 576)
+            o, l, ot, lt = attention(q, kv, kv[:, :512], vis, scale)
+            check(f"lse of sequence {b}", lse[at:at + nq].reshape(-1), l, lt)
+            check(f"out of sequence {b}", out[at:at + nq].reshape(-1, 512), o, ot)
+        at += nq
+
+
+@pytest.mark.parametrize("H", [1, 16, 17, 32, 33, 64, 65, 128])
+def test_single_tokens(ctx, H):
+    x = Case8([1, 15, 16, 17, 63, 64, 65, 0, 129, 500], [1] * 10, H, seed=H)
+    compare(x, *run(ctx, x))
+
+
+@pytest.mark.parametrize("page,block", [(1, 1), (2, 1), (4, 4), (8, 2), (16, 1), (32, 8), (64, 16), (64, 64), (512, 32)])
+def test_pages(ctx, page, block):
+    x = Case8([300, 77, 1, 513], [1, 4, 1, 2], 16, page=page, block=block, seed=page + block, spread=3.0)
+    compare(x, *run(ctx, x))
+
+
+@pytest.mark.parametrize("H,q_lens,kv_lens", [
+    (16, [2, 1, 0, 3], [100, 40, 50, 3]),            # 32 rows and 48
+    (8, [5, 16, 1], [5, 16, 1]),                     # a prompt: every token new
+    (128, [3, 1, 2], [70, 33, 1000]),                # blocks of one token or half of one
+    (3, [50, 7, 0, 90], [50, 100, 10, 89]),          # blocks that cut a token's heads; a first token that sees nothing
+    (128, [4], [2]),                                 # tokens that see nothing
+    (40, [9, 33], [0, 40]),                          # an empty cache
+    (1, [1], [3]), (2, [1, 3], [64, 65]),
+])
+def test_chunks(ctx, H, q_lens, kv_lens):
+    x = Case8(kv_lens, q_lens, H, seed=H + len(q_lens))
+    out, lse = run(ctx, x)
+    compare(x, out, lse)
+    at = 0
+    for nq, kv in zip(q_lens, kv_lens):
+        none = max(nq - kv, 0)
+        assert bool((out[at:at + none] == 0).all()) and bool((lse[at:at + none] == -math.inf).all())
+        at += nq
+
+
+@pytest.mark.parametrize("H,q,kv,page", [(16, [1, 1, 1], [20011, 3, 9000], 64), (128, [3], [12345], 128), (32, [1, 2], [7000, 5], 16)])
+def test_long_context_is_split_and_joined(ctx, H, q, kv, page):
+    x = Case8(kv, q, H, page=page, seed=2)
+    compare(x, *run(ctx, x))
+
+
+def test_many_units(ctx):
+    """A bound on the chunk that gives more units than are cut into runs: a workgroup per unit."""
+    q_lens = [1, 0, 3, 17, 130] + [1] * 28
+    kv = [200 + 7 * b for b in range(33)]
+    x = Case8(kv, q_lens, 8, seed=4, max_q=512)
+    compare(x, *run(ctx, x), only=[0, 2, 3, 4, 20, 32])
+    for H, most in ((1, 16), (4, 8)):                # units of 16 and 32 rows, many sequences
+        y = Case8([5 + b % 90 for b in range(1100)], [1] * 1100, H, seed=H, max_q=most)
+        compare(y, *run(ctx, y), only=[0, 7, 500, 1099])
+
+
+def test_steep_scores(ctx):
+    """Scores that rise along the context by far more than the reference maximum's slack, and equal rows."""
+    x = Case8([700], [2], 16, seed=5)
+    p, r = x.where[0]
+    x.scale[p, r // 16] = (117 + torch.arange(700, device=DEV) // 64).to(torch.uint8)
+    same = p[200:300], r[200:300]
+    x.cache[same] = x.cache[p[200], r[200]].expand(100, 640)
+    compare(x, *run(ctx, x))
+
+
+def test_absent_pages(ctx):
+    """Rows on pages outside the cache do not exist, whatever the entry says; the rest is attended."""
+    for page in (16, 4):
+        x = Case8([300, 64, 40], [2, 1, 1], 16, page=page, block=4, seed=6)
+        gone = [3, 7, 18 * 16 // page]
+        x.table[0, 3], x.table[0, 7], x.table[0, gone[2]] = -1, 1 << 30, x.cache.shape[0]
+        x.table[1, :] = -5
+        seen = [x.seen(b).clone() for b in range(3)]
+        for p in gone:
+            seen[0][:, page * p:page * p + page] = False
+        seen[1][:] = False
+        out, lse = run(ctx, x)
+        compare(x, out, lse, seen=seen)
+        assert bool((out[2] == 0).all()) and bool((lse[2] == -math.inf).all())
+
+
+def test_lengths_out_of_range_are_cut(ctx):
+    x = Case8([100, 50], [1, 1], 16, seed=7)
+    x.kv_len.copy_(torch.tensor([1 << 30, -4], dtype=torch.int32))
+    out, lse = run(ctx, x)
+    compare(x, out, lse, only=[0])
+    assert bool((out[1] == 0).all()) and bool((lse[1] == -math.inf).all())
+
+
+def test_chunk_past_its_bound_and_rows_behind(ctx):
+    x = Case8([90, 60], [10, 6], 5, seed=8, behind=4)
+    out, lse = run(ctx, x, fill=3.0)
+    compare(x, out, lse)
+    assert bool((out[16:] == 3.0).all()) and bool((lse[16:] == 3.0).all())
+    x.max_q = 4                                      # the first four tokens see what they see in the whole chunk
+    o, l = run(ctx, x, fill=3.0)
+    for at, n in ((0, 10), (10, 6)):
+        assert bool((o[at + 4:at + n] == 3.0).all()) and bool((l[at + 4:at + n] == 3.0).all())
+        assert torch.allclose(l[at:at + 4], lse[at:at + 4], rtol=1e-5, atol=1e-5)
+
+
+@pytest.mark.parametrize("H,q_lens,kv_lens", [(16, [1, 40], [90, 100]), (128, [3, 20], [3000, 70]), (8, [2, 4], [30, 64])])
+def test_what_a_token_does_not_see_does_not_reach_it(ctx, H, q_lens, kv_lens):
+    """NaN codes and a branch that is not finite in the rows of later tokens."""
+    x = Case8(kv_lens, q_lens, H, seed=9)
+    clean = run(ctx, x)
+    nq, n, at = q_lens[1], kv_lens[1], q_lens[0]
+    p, r = x.where[1]
+    tok = nq - 2                                     # the last two tokens' rows
+    for t, dim in ((tok, 0), (tok, 511), (tok, 130), (tok + 1, 77)):
+        u = n - nq + t
+        x.cache[p[u], r[u], dim] = 0x7F if dim else 0xFF
+    u = n - 1
+    x.cache[p[u], r[u], 512:516].copy_(torch.tensor([math.inf, math.nan], dtype=torch.bfloat16, device=DEV).view(torch.uint8))
+    out, lse = run(ctx, x)
+    assert torch.equal(out[:at + tok], clean[0][:at + tok]) and torch.equal(lse[:at + tok], clean[1][:at + tok])
+    assert bool(out[at + tok:at + nq].isnan().all()) and bool(lse[at + tok:at + nq].isnan().all())
+
+
+def test_queries_that_are_not_finite_stay_with_themselves(ctx):
+    x = Case8([100, 300], [3, 1], 16, seed=10)
+    clean = run(ctx, x)
+    x.q_lat[1, 5, 3] = math.nan
+    x.q_rope[0, 2, 1] = math.inf
+    out, lse = run(ctx, x)
+    same = torch.ones(4, 16, dtype=torch.bool, device=DEV)
+    same[1, 5] = same[0, 2] = False
+    assert torch.equal(out[same], clean[0][same]) and torch.equal(lse[same], clean[1][same])
+    assert bool(out[1, 5].isnan().all()) and bool(lse[1, 5].isnan())
+
+
+def test_scales_at_their_bounds(ctx):
+    """Bytes outside the range count as its bounds; rows of very different scale side by side."""
+    x = Case8([96, 64], [1, 2], 16, seed=11, block=16)
+    q = x.q_lat
+    for b, bytes_ in ((0, [0, 62, 63, 64, 63, 0]), (1, [190, 191, 192, 255])):
+        p, r = x.where[b]
+        x.scale[p, r // 16] = torch.tensor(bytes_, dtype=torch.uint8, device=DEV).repeat_interleave(16)
+    q[1:] *= 2.0 ** -70
+    x.q[..., :512] = q
+    compare(x, *run(ctx, x))
+
+
+def test_padded_rows_and_strides(ctx):
+    x = Case8([130, 70], [2, 5], 24, page=32, block=8, seed=12, pad=48)
+    wide = torch.full((2, 9), -1, dtype=torch.int32, device=DEV)
+    wide[:, :x.table.shape[1]] = x.table
+    x.table = wide[:, :x.table.shape[1]]
+    big = torch.zeros(x.cache.shape[0], 7, dtype=torch.uint8, device=DEV)
+    big[:, 1:5] = x.scale
+    x.scale = big[:, 1:5]                            # scales at odd addresses
+    x.q_lat, x.q_rope = x.q[..., :512], x.q[..., 512:]
+    compare(x, *run(ctx, x))
+
+
+def test_same_bits_again(ctx):
+    x = Case8([9000, 5000, 800], [1, 1, 1], 16, page=64, seed=13)
+    a, b = run(ctx, x), run(ctx, x)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_captured_and_replayed(ctx):
+    """Replays read the then current lengths, table, scales and queries; eager work between them."""
+    x = Case8([2000, 700], [2, 1], 16, seed=14, max_kv=2048)
+    y = Case8([1500, 2047], [1, 2], 16, seed=15, max_kv=2048, max_q=2, spare=200)
+    pages, chunk = handles(x)
+    ws = torch.empty(vkv.chunk8_workspace_size(pages, chunk), dtype=torch.uint8, device=DEV)
+    out, lse = torch.empty(3, 16, 512, dtype=torch.bfloat16, device=DEV), torch.empty(3, 16, device=DEV)
+    vkv.chunk8_attend(ctx, pages, chunk, ws, SCALE, out, lse)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        vkv.chunk8_attend(ctx, pages, chunk, ws, SCALE, out, lse)
+    keep = {k: getattr(x, k).clone() for k in ("cache", "scale", "table", "kv_len", "cu", "q_lat", "q_rope")}
+    for turn in range(3):
+        for src in (keep, {k: getattr(y, k) for k in keep}):
+            for k, v in src.items():
+                getattr(x, k)[:min(v.shape[0], getattr(x, k).shape[0])].copy_(v[:getattr(x, k).shape[0]])
+            out.fill_(5.0)
+            g.replay()
+            torch.cuda.synchronize()
+            got = out.clone(), lse.clone()
+            want = run(ctx, x)
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_on_another_stream(ctx):
+    x = Case8([3000], [1], 16, seed=16)
+    want = run(ctx, x)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    got = run(ctx, x, stream=s)
+    s.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])

@@ -1,0 +1,173 @@
+"""vkv_cache8_write against its definition in 64 bits: the codes and scales bit for bit (a scale is a power of two, so the
+one rounding is the code's), every other byte as it was."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2609_03949_amd as vkv
+
+from _paged8 import Case8, TOP, decode, encode, least_byte, same_codes
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    c = vkv.Context(0)
+    yield c
+    c.close()
+
+
+def rows(n, seed, size=1.0):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    x = torch.randn(n, 512, generator=g, device=DEV) * torch.exp(torch.randn(n, 1, generator=g, device=DEV)) * size
+    return x.to(torch.bfloat16), torch.randn(n, 64, generator=g, device=DEV).to(torch.bfloat16)
+
+
+def want(x, lat, rope, max_q):
+    """cache and scale as they should be after the write, on the CPU."""
+    cache, scale = x.cache.cpu().numpy().copy(), x.scale.cpu().numpy().copy()
+    new, branch = lat.double().cpu().numpy(), rope.cpu().view(torch.uint8).numpy()
+    table, R, page, cu = x.table.cpu().numpy(), x.block, x.page, x.cu.tolist()
+    for b, kv in enumerate(x.kv_len.tolist()):
+        kv = min(max(kv, 0), x.max_kv)
+        n = cu[b + 1] - cu[b]
+        at = {kv - n + i: cu[b] + i for i in range(min(n, max_q)) if kv - n + i >= 0}
+        for u0 in sorted({u - u % R for u in at}):
+            p = table[b, u0 // page]
+            if not 0 <= p < cache.shape[0]:
+                continue
+            r0, j = u0 % page, u0 % page // R
+            mine = [u for u in range(u0, u0 + R) if u in at]
+            s = least_byte(np.concatenate([new[at[u]] for u in mine]))
+            older = range(u0, mine[0])
+            if len(older):
+                was = int(np.clip(scale[p, j], 63, 191))
+                if s > was:
+                    for u in older:
+                        v = decode(torch.from_numpy(cache[p, r0 + u - u0, :512]), torch.tensor(was)).numpy()
+                        cache[p, r0 + u - u0, :512] = encode(v * 2.0 ** (127 - s))
+                s = max(s, was)
+            scale[p, j] = s
+            for u in mine:
+                v = new[at[u]]
+                v = np.where(np.abs(v) <= TOP * 2.0 ** 64, v, np.nan)
+                cache[p, r0 + u - u0, :512] = encode(v * 2.0 ** (127 - s))
+                cache[p, r0 + u - u0, 512:] = branch[at[u]]
+    return cache, scale
+
+
+def check(ctx, x, lat, rope, max_q=None, **kw):
+    max_q = x.max_q if max_q is None else max_q
+    cache, scale = want(x, lat, rope, max_q)
+    rest = x.whole[..., 640:].clone()
+    vkv.cache8_write(ctx, vkv.Pages8(x.cache, x.scale, x.table, x.kv_len, x.max_kv), lat, rope, x.cu, max_q, **kw)
+    torch.cuda.synchronize()
+    got = x.cache.cpu().numpy()
+    assert np.array_equal(x.scale.cpu().numpy(), scale)
+    assert same_codes(got[..., :512], cache[..., :512])
+    assert np.array_equal(got[..., 512:], cache[..., 512:])
+    assert torch.equal(x.whole[..., 640:], rest)
+
+
+@pytest.mark.parametrize("page,block", [(1, 1), (16, 1), (16, 2), (16, 4), (64, 8), (16, 16), (64, 16), (32, 32), (64, 64), (256, 64)])
+@pytest.mark.parametrize("size", [1.0, 40.0])
+def test_blocks(ctx, page, block, size):
+    """Single tokens and chunks from every place of a block; larger rows make the scales of older ones grow."""
+    kv = [1, 16, 17, 65, 64, 200, 40, 3, 300]
+    q = [1, 1, 1, 1, 64, 33, 0, 3, 129]
+    x = Case8(kv, q, 1, page=page, block=block, seed=page + block)
+    check(ctx, x, *rows(sum(q), 3, size))
+
+
+def test_one_token_after_another_is_the_same_as_its_block(ctx):
+    """Rows that grow: a block filled row by row has the codes of its largest row's scale, but for what fell below its step."""
+    x = Case8([48], [1], 1, page=16, block=16, seed=1)
+    lat, rope = rows(48, 5)
+    lat = (lat.float() * torch.linspace(0.5, 3.0, 48, device=DEV)[:, None]).to(torch.bfloat16)
+    for u in range(48):
+        x.kv_len.fill_(u + 1)
+        check(ctx, x, lat[u:u + 1], rope[u:u + 1])
+    one = x.scale.clone()
+    x.kv_len.fill_(48)
+    x.cu = torch.tensor([0, 48], dtype=torch.int32, device=DEV)
+    check(ctx, x, lat, rope, 48)
+    assert torch.equal(one, x.scale)
+
+
+def test_magnitudes(ctx):
+    """Zeros, the smallest and the largest values, halfway values, what is not finite."""
+    x = Case8([32, 16, 16, 16], [32, 16, 16, 16], 1, page=16, block=16, seed=2)
+    lat, rope = rows(80, 7)
+    lat[:16] = 0
+    lat[16:32] = (torch.arange(512, device=DEV).float() * 0.0625 - 15).to(torch.bfloat16)       # ties of the coding
+    lat[32:48] *= 2.0 ** -100
+    lat[48:64] *= 2.0 ** 66
+    lat[49, :8] = torch.tensor([math.inf, -math.inf, math.nan, 448 * 2.0 ** 64, 450 * 2.0 ** 64, 3e38, -3e38, 0], device=DEV).to(torch.bfloat16)
+    lat[64:80, 1:] = 0
+    lat[64:80, 0] = torch.tensor([2.0 ** (k - 8) * 1.75 for k in range(16)], device=DEV).to(torch.bfloat16)
+    check(ctx, x, lat, rope)
+
+
+def test_scales_out_of_range_and_nan_among_older_rows(ctx):
+    for byte in (0, 62, 192, 255):
+        x = Case8([24], [2], 1, page=16, block=16, seed=3)
+        x.scale[x.where[0][0][20], 0] = byte
+        x.cache[x.where[0][0][17], 1, 5] = 0xFF
+        check(ctx, x, *rows(2, 9))
+
+
+def test_chunk_past_its_bound_short_sequences_and_absent_pages(ctx):
+    x = Case8([90, 3, 40], [10, 6, 20], 1, page=16, block=4, seed=4, behind=3)
+    x.table[2, 1] = -1
+    check(ctx, x, *rows(39, 11))
+    y = Case8([90, 60], [40, 6], 1, page=16, block=16, seed=5)
+    check(ctx, y, *rows(46, 12), max_q=7)
+    z = Case8([90, 60], [40, 6], 1, page=16, block=16, seed=5)
+    z.kv_len.copy_(torch.tensor([1 << 30, -7], dtype=torch.int32))
+    check(ctx, z, *rows(46, 13))
+
+
+def test_strides(ctx):
+    x = Case8([90, 61], [40, 6], 1, page=32, block=8, seed=6, pad=16)
+    both = torch.cat(rows(46, 14), 1)                 # rows of 576, as the model makes them
+    big = torch.zeros(x.cache.shape[0], 7, dtype=torch.uint8, device=DEV)
+    big[:, 1:5] = x.scale
+    x.scale = big[:, 1:5]
+    check(ctx, x, both[:, :512], both[:, 512:])
+    assert bool((big[:, 0] == 0).all()) and bool((big[:, 5:] == 0).all())
+    y = Case8([20], [12], 1, page=16, block=16, seed=7)
+    lat, rope = rows(1, 15)
+    check(ctx, y, lat.expand(12, 512), rope.expand(12, 64))
+
+
+def test_captured_and_on_another_stream(ctx):
+    x = Case8([90, 61], [3, 1], 1, page=16, block=16, seed=8)
+    lat, rope = rows(4, 16)
+    pages = vkv.Pages8(x.cache, x.scale, x.table, x.kv_len, x.max_kv)
+    before = x.cache.clone(), x.scale.clone()
+    vkv.cache8_write(ctx, pages, lat, rope, x.cu, 3)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        vkv.cache8_write(ctx, pages, lat, rope, x.cu, 3)
+    for k in range(3):
+        x.cache.copy_(before[0])
+        x.scale.copy_(before[1])
+        a, r = rows(4, 20 + k, 1.0 + 30 * k)
+        lat.copy_(a)
+        rope.copy_(r)
+        x.kv_len.copy_(torch.tensor([90 - k, 61 - 7 * k], dtype=torch.int32))
+        cache, scale = want(x, lat, rope, 3)
+        g.replay()
+        torch.cuda.synchronize()
+        assert np.array_equal(x.scale.cpu().numpy(), scale)
+        assert same_codes(x.cache.cpu().numpy()[..., :512], cache[..., :512])
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    check(ctx, x, *rows(4, 30), stream=s)
