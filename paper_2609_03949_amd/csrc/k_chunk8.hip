@@ -78,11 +78,21 @@ __device__ __forceinline__ bf16x8_t decode8(uint32_t lo, uint32_t hi, float sc) 
     __builtin_memcpy(&r, v, 16);
     return r;
 }
-// NaN codes become 0: in the values of a tile where a mask hides a row that holds one (a token that sees
-// such a row has a score that is NaN, whatever its values are)
-__device__ __forceinline__ uint32_t drop_nan(uint32_t w) {
+__device__ __forceinline__ uint32_t drop_nan(uint32_t w) {   // NaN codes become 0
     const uint32_t n = (((w & 0x7F7F7F7Fu) + 0x01010101u) >> 7) & 0x01010101u;
     return w & ~((n << 8) - n);
+}
+// Wave w's 16 rows of a tile (at st in LDS) without NaN codes, where a mask hides a row that holds one: 0 times it would
+// not be 0.  (A token that sees such a row has a score that is NaN, whatever its values are.)  Rare.
+__device__ __attribute__((noinline)) void clean_tile(uint32_t st, int w, int lane) {
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t at = st + (16 * w + 2 * i) * D_LAT + 16 * lane;
+        u32x4_t v = lds_read_u4<0>(at);
+        lds_wait<0>(v);
+        for (int q = 0; q < 4; ++q) v[q] = drop_nan(v[q]);
+        asm volatile("ds_write_b128 %0, %1" ::"v"(at), "v"(v) : "memory");
+    }
+    lds_barrier();
 }
 __device__ __forceinline__ float scale_of(uint32_t word, uint32_t note) {
     const uint32_t s = min(max((word >> (note & 31u)) & 255u, (uint32_t)VKV_SCALE_MIN), (uint32_t)VKV_SCALE_MAX);
@@ -105,8 +115,8 @@ struct Loader8 {
             for (int i = 1; i < NR; ++i) e[i] = table[row(t, i) >> a.shift];
     }
     // the loads of the fetched tile t into stage st (its number in LDS: sg)
-    __device__ __forceinline__ void issue(int t, uint8_t* smem, uint32_t lds0, int sg) const {
-        uint8_t* st = smem + C8_OFF_STAGE + sg * C8_STAGE;
+    __device__ __forceinline__ void issue(int t, uint8_t* smem, uint32_t lds0, int sg, int stages = C8_OFF_STAGE) const {
+        uint8_t* st = smem + stages + sg * C8_STAGE;
         const char* base[NR];
         const uint8_t* word;     // this lane's (of 16) scale byte
         uint32_t absent;
@@ -165,6 +175,14 @@ struct Loader8 {
 };
 
 // ------------------------------------------------------------------ a segment
+
+// v *= f for an accumulator register: said so that the compiler keeps the outputs where the products add to them (with
+// a plain product it copies all of them to the other registers and back around every tile).  The products that wrote v and
+// those that read it next are a barrier away, as far as their wait states go.
+__device__ __forceinline__ void scale_acc(float& v, float f) {
+    float t;
+    asm volatile("v_accvgpr_read_b32 %1, %0\n\tv_mul_f32 %1, %1, %2\n\tv_accvgpr_write_b32 %0, %1" : "+a"(v), "=&v"(t) : "v"(f));
+}
 
 // Tiles [t0, t1) of unit x (16 RG rows) by one workgroup.  part: where an incomplete unit's
 // (O, m, l) go, or null (outputs).
@@ -360,7 +378,11 @@ __device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit
 #pragma unroll
                 for (int d = 0; d < NO; ++d)
 #pragma unroll
-                    for (int i = 0; i < (WIDE ? 16 : 4); ++i) o[d][r][i] *= f;
+                    for (int i = 0; i < (WIDE ? 16 : 4); ++i) {
+                        float v = o[d][r][i];
+                        scale_acc(v, f);
+                        o[d][r][i] = v;
+                    }
             }
             weights();
             lds_barrier();
@@ -381,7 +403,8 @@ __device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit
         const int vr = WIDE ? 4 * (lane >> 5) + (e & 3) + 8 * (e >> 2) : 8 * g + e;
         const int vp = WIDE ? 8 * w + (g & 1) : 8 * w;
         const uint32_t va = st + vr * D_LAT + 16 * (vp ^ code_xor(vr)) + 8 * (lane & 1);
-        auto product = [&](auto clean) __attribute__((always_inline)) {
+        if (bads[0] | bads[1] | bads[2] | bads[3]) clean_tile(st, w, lane);
+        {
             constexpr int N = KS * NO, VD = 6;
             u32x2_t vv[VD + 1];
             auto vload = [&](auto ic) {
@@ -396,9 +419,7 @@ __device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit
 #pragma unroll
                     for (int q = 0; q < KS * RB; ++q) lds_wait<VD + 1>(pf[q / RB][q % RB]);
                 lds_wait<(i + VD < N) ? VD : N - 1 - i>(vv[i % (VD + 1)]);
-                uint32_t lo = vv[i % (VD + 1)][0], hi = vv[i % (VD + 1)][1];
-                if constexpr (decltype(clean)::value) lo = drop_nan(lo), hi = drop_nan(hi);
-                const bf16x8_t v = decode8(lo, hi, 1.0f);
+                const bf16x8_t v = decode8(vv[i % (VD + 1)][0], vv[i % (VD + 1)][1], 1.0f);
 #pragma unroll
                 for (int r = 0; r < RB; ++r) {
                     const bf16x8_t p = __builtin_bit_cast(bf16x8_t, pf[s][r]);
@@ -406,9 +427,7 @@ __device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit
                     else o[d][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p, o[d][r], 0, 0, 0);
                 }
             });
-        };
-        if (bads[0] | bads[1] | bads[2] | bads[3]) product(std::true_type{});
-        else product(std::false_type{});
+        }
     }
 
     // ---- the sums of the waves' rows
@@ -459,6 +478,289 @@ __device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit
     }
 }
 
+// ------------------------------------------------- a segment of a unit of 128 rows
+
+// As above, but the queries of 128 rows do not fit in every wave: wave w takes the scores of rows 32 w .. + 31 of the unit
+// against all of the tile's rows, and 128 dims of all rows' outputs.  It has its rows' scores to itself, so
+// their reference moves before the weights are written; the other waves learn by how much.
+constexpr int B8_OFF_SCALE = C8_OFF_TOP;                        // [wave][64] the tile's scales, each wave's own copy
+constexpr int B8_OFF_P = C8_OFF_P;                              // [128][64] bf16
+constexpr int B8_OFF_STAGE = B8_OFF_P + 128 * 2 * C8_TILE;
+constexpr int B8_OFF_ALPHA = B8_OFF_STAGE + C8_STAGES * C8_STAGE;   // [128] by what a row's outputs are to be multiplied
+constexpr int B8_SMEM = B8_OFF_ALPHA + 512;
+static_assert(B8_OFF_STAGE % 1024 == 0 && C8_OFF_P - C8_OFF_BAD >= 64, "");
+
+__device__ __forceinline__ void chunk8_big_segment(const Chunk8Args& a, const CkUnit& x, int t0, int t1, float* part_o,
+                                                   float* part_ml, uint8_t* smem) {
+    const int tid = threadIdx.x, lane = tid & 63, c = lane & 31, h = lane >> 5;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t lds0 = lds_addr(smem);
+    const int first = min(x.row0 + 32 * w, x.nrow - 1);
+    const int Rc = min(x.row0 + 32 * w + c, x.nrow - 1);        // rows past the end repeat the last one, never stored
+    const int lim = min(x.old + Rc / a.H, x.kv - 1);            // the last cache row that this lane's row sees
+    const int lim_lo = __builtin_amdgcn_readfirstlane(min(x.old + first / a.H, x.kv - 1));
+    const int nt = x.kv > 0 ? t1 - t0 : 0;
+
+    Loader8 loader{a, (const_i32_t*)(a.table + (int64_t)x.b * a.tstride), x.kv, w, lane, {}};
+    // Q^T operand: step 2 s + i (i < 2) has dims 32 s + 16 h + 8 i .. + 7, as a 16-byte piece of codes holds them
+    bf16x8_t qf[36];
+    {
+        const int64_t row = x.tok0 * a.H + Rc;
+        const uint16_t* ql = a.q_lat + row * a.qls + 16 * h;
+        const uint16_t* qr = a.q_rope + row * a.qrs + 8 * h;
+#pragma unroll
+        for (int s = 0; s < 32; ++s) qf[s] = *reinterpret_cast<const bf16x8_t*>(ql + 32 * (s >> 1) + 8 * (s & 1));
+#pragma unroll
+        for (int s = 0; s < 4; ++s) qf[32 + s] = *reinterpret_cast<const bf16x8_t*>(qr + 16 * s);
+    }
+    if (nt > 0) {
+        loader.fetch(t0);
+        loader.issue(t0, smem, lds0, 0, B8_OFF_STAGE);
+        loader.fetch(t0 + 1);
+        if (nt > 1) {
+            loader.issue(t0 + 1, smem, lds0, 1, B8_OFF_STAGE);
+            loader.fetch(t0 + 2);
+        }
+    }
+#pragma unroll
+    for (int s = 0; s < 36; ++s) asm volatile("" : "+v"(qf[s]));   // no wait for them inside the tile loop
+
+    f32x16_t o[4][4];   // [dim block][row block]
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][r][i] = 0.f;
+    float m_run = -INFINITY, l_run = 0.f;
+    auto opaque_lane = [&]() {   // operand addresses are found anew from it, so that no registers hold them across the loop
+        int ln = lane;
+        asm volatile("" : "+v"(ln));
+        return ln;
+    };
+
+    int sg = 0;   // the stage of tile k
+    for (int k = 0; k < nt; ++k) {
+        if (k + 1 < nt)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(Loader8::LOADS) : "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        lds_barrier();
+        if (k + 2 < nt) {
+            loader.issue(t0 + k + 2, smem, lds0, sg == 0 ? 2 : sg - 1, B8_OFF_STAGE);
+            loader.fetch(t0 + k + 3);
+        }
+        const int u0 = C8_TILE * (t0 + k);
+        const uint32_t st = lds0 + B8_OFF_STAGE + sg * C8_STAGE;
+        const uint32_t wn = lds0 + C8_OFF_WORD + (sg * C8_TILE + lane) * 4;
+        sg = sg == 2 ? 0 : sg + 1;
+
+        // ---- scores of the 64 rows of the tile: s[b][i] is row 32 b + 8 (i / 4) + 4 h + i % 4
+        uint32_t word = lds_read_u1(wn), note = lds_read_u1(wn + (C8_OFF_NOTE - C8_OFF_WORD));
+        const int ln = opaque_lane(), r = ln & 31;
+        uint32_t ka[2];    // pieces 2 s + h of rows r and 32 + r
+        ka[0] = st + r * D_LAT + 16 * ((ln >> 5) ^ code_xor(r & 15));
+        ka[1] = ka[0] + 32 * D_LAT;
+        const uint32_t ra = st + C8_OFF_ROPE + r * (2 * D_ROPE) + 16 * ((ln >> 5) ^ rope_xor(r));
+        constexpr int SD = 3;          // operands read ahead of the matrix cores, of either half of the tile: 16 of codes, 4 of the branch
+        u32x4_t kc[SD + 1][2];
+        auto kload = [&](auto sc_) {
+            constexpr int s = decltype(sc_)::value;
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                if constexpr (s < 16) kc[s % (SD + 1)][b] = lds_read_u4<0>(ka[b] ^ (32 * s));
+                else kc[s % (SD + 1)][b] = b ? lds_read_u4<32 * 2 * D_ROPE>(ra ^ (32 * (s - 16))) : lds_read_u4<0>(ra ^ (32 * (s - 16)));
+            }
+        };
+        static_for<0, SD>(kload);
+        lds_wait<2 * SD>(word, note);
+        const float sc = scale_of(word, note);                  // of tile row `lane`
+        const uint64_t absent = __ballot(sc == 0.f);
+        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(sc), __float_as_uint(sc), false, false);
+        const float sk[2] = {__uint_as_float(sw[0]), __uint_as_float(sw[1])};   // of rows r and 32 + r
+        lds_write_u1(lds0 + B8_OFF_SCALE + 256 * w + 4 * ln, __float_as_uint(sc));
+        f32x16_t s2[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s2[b][i] = 0.f;
+        static_for<0, 20>([&](auto sc_) {
+            constexpr int s = decltype(sc_)::value;
+            if constexpr (s + SD < 20) kload(std::integral_constant<int, s + SD>{});
+            lds_wait<2 * ((s + SD < 20) ? SD : 19 - s)>(kc[s % (SD + 1)][0], kc[s % (SD + 1)][1]);
+            if constexpr (s < 16) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        const u32x4_t& v = kc[s % (SD + 1)][b];
+                        s2[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode8(v[2 * i], v[2 * i + 1], sk[b]), qf[2 * s + i], s2[b], 0, 0, 0);
+                    }
+            } else {
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+                    s2[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kc[s % (SD + 1)][b]), qf[16 + s], s2[b], 0, 0, 0);
+            }
+        });
+
+        // ---- weights
+        bool bad = false;
+        if (u0 + C8_TILE - 1 > lim_lo || absent != 0) {
+            const int last = lim - u0 - 4 * h;
+            const uint64_t gone = absent >> (4 * h);
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int row = 32 * b + 8 * (i >> 2) + (i & 3);
+                    if (row > last || ((gone >> row) & 1u)) {
+                        bad |= s2[b][i] != s2[b][i];
+                        s2[b][i] = -INFINITY;
+                    }
+                }
+        }
+        float top = s2[0][0];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, s2[b][i]);
+        top = half_max(top) * a.scale_log2;
+        const bool move = top > m_run + C8_SLACK;
+        const float alpha = move ? __builtin_amdgcn_exp2f(m_run - top) : 1.0f;
+        if (move) m_run = top;
+        l_run *= alpha;
+        const float ref = m_run == -INFINITY ? 0.f : m_run;
+        const uint32_t flags = (__ballot(move) ? 1u : 0u) | (__ballot(bad) ? 2u : 0u);
+        const uint32_t pa = lds0 + B8_OFF_P + (32 * w + c) * (2 * C8_TILE);
+        const uint32_t px = rope_xor(c);
+        float psum = 0.f;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {      // 16 rows of the tile, eight of them this lane's
+                u32x4_t f[2] = {lds_read_u4<B8_OFF_SCALE>(lds0 + 256 * w + 128 * b + 64 * q + 16 * h),
+                                lds_read_u4<B8_OFF_SCALE + 32>(lds0 + 256 * w + 128 * b + 64 * q + 16 * h)};
+                lds_wait<0>(f[0], f[1]);
+                bf16x8_t p8;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s2[b][8 * q + i], a.scale_log2, -ref));
+                    psum += p;
+                    p8[i] = (__bf16)(p * __uint_as_float(f[i >> 2][i & 3]));
+                }
+                const u32x4_t v = __builtin_bit_cast(u32x4_t, p8);
+                asm volatile("ds_write_b128 %0, %1" ::"v"(pa + 16 * ((2 * (2 * b + q) + h) ^ px)), "v"(v) : "memory");
+            }
+        l_run += psum;   // this lane's share of the sum
+        if (h == 0) lds_write_u1(lds0 + B8_OFF_ALPHA + (32 * w + c) * 4, __float_as_uint(alpha));
+        if (lane == 0) lds_write_u1(lds0 + C8_OFF_BAD + 4 * w, flags);
+        lds_barrier();
+
+        // ---- outputs, dims 128 w .. + 127
+        u32x4_t fl = lds_read_u4<C8_OFF_BAD>(lds0);
+        lds_wait<0>(fl);
+        const uint32_t all = __builtin_amdgcn_readfirstlane(fl[0] | fl[1] | fl[2] | fl[3]);
+        if (all & 1u) {
+#pragma unroll
+            for (int rb = 0; rb < 4; ++rb) {
+                uint32_t f = lds_read_u1(lds0 + B8_OFF_ALPHA + (32 * rb + c) * 4);
+                lds_wait<0>(f);
+#pragma unroll
+                for (int d = 0; d < 4; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        float v = o[d][rb][i];
+                        scale_acc(v, __uint_as_float(f));
+                        o[d][rb][i] = v;
+                    }
+            }
+        }
+        const int vl = opaque_lane(), e = (vl >> 1) & 7, vr = 4 * (vl >> 5) + (e & 3) + 8 * (e >> 2);
+        const uint32_t va = st + vr * D_LAT + 16 * ((8 * w + ((vl >> 4) & 1)) ^ code_xor(vr)) + 8 * (vl & 1);
+        const uint32_t pr = lds0 + B8_OFF_P + (vl & 31) * (2 * C8_TILE) + 16 * ((vl >> 5) ^ rope_xor(vl & 31));
+        if (all & 2u) clean_tile(st, w, lane);
+        {
+            constexpr int N = 16, VD = 4;
+            u32x2_t vv[VD + 1];
+            u32x4_t pf[4];
+            auto vload = [&](auto ic) {
+                constexpr int i = decltype(ic)::value, s = i >> 2, d = i & 3;
+                vv[i % (VD + 1)] = lds_read_tr8<16 * D_LAT * s>(va ^ (32 * d));
+            };
+            auto pload = [&](auto sc_) {
+                constexpr int s = decltype(sc_)::value;
+#pragma unroll
+                for (int rb = 0; rb < 4; ++rb) pf[rb] = rb == 0 ? lds_read_u4<0>(pr ^ (32 * s)) : rb == 1 ? lds_read_u4<4096>(pr ^ (32 * s))
+                                                      : rb == 2 ? lds_read_u4<8192>(pr ^ (32 * s)) : lds_read_u4<12288>(pr ^ (32 * s));
+            };
+            static_for<0, VD>(vload);
+            static_for<0, N>([&](auto ic) {
+                constexpr int i = decltype(ic)::value, s = i >> 2, d = i & 3;
+                if constexpr (d == 0) {
+                    pload(std::integral_constant<int, s>{});
+                    lds_wait<2>(pf[0], pf[1]);
+                    lds_wait<0>(pf[2], pf[3]);
+                }
+                if constexpr (i + VD < N) vload(std::integral_constant<int, i + VD>{});
+                lds_wait<(i + VD < N) ? VD : N - 1 - i>(vv[i % (VD + 1)]);
+                const bf16x8_t v = decode8(vv[i % (VD + 1)][0], vv[i % (VD + 1)][1], 1.0f);
+#pragma unroll
+                for (int rb = 0; rb < 4; ++rb)
+                    o[d][rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8_t, pf[rb]), o[d][rb], 0, 0, 0);
+            });
+        }
+    }
+
+    // ---- the rows' references and sums, for every wave
+    __syncthreads();
+    float* ml = reinterpret_cast<float*>(smem + B8_OFF_P);   // [row][2]
+    const float l = half_sum(l_run);
+    if (h == 0) {
+        ml[2 * (32 * w + c)] = m_run;
+        ml[2 * (32 * w + c) + 1] = l;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int rb = 0; rb < 4; ++rb) {
+        const int row = 32 * rb + c, R = x.row0 + row;
+        const float m = ml[2 * row], sum = ml[2 * row + 1];
+        if (part_o) {
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const f32x4_t v = {o[d][rb][4 * q], o[d][rb][4 * q + 1], o[d][rb][4 * q + 2], o[d][rb][4 * q + 3]};
+                    *reinterpret_cast<f32x4_t*>(part_o + ((((w * 4 + d) * 4 + rb) * 4 + q) * 64 + lane) * 4) = v;
+                }
+            if (w == 0 && h == 0) {
+                part_ml[2 * row] = m;
+                part_ml[2 * row + 1] = sum;
+            }
+        } else if (R < x.nrow) {
+            const int64_t at = x.tok0 * a.H + R;
+            const bool none = m == -INFINITY && sum == 0.f;
+            const float inv = none ? 0.f : 1.0f / sum;
+            uint16_t* out = a.out + at * D_LAT + 128 * w + 4 * h;
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const bf16x4_t v = {(__bf16)(o[d][rb][4 * q] * inv), (__bf16)(o[d][rb][4 * q + 1] * inv),
+                                        (__bf16)(o[d][rb][4 * q + 2] * inv), (__bf16)(o[d][rb][4 * q + 3] * inv)};
+                    *reinterpret_cast<bf16x4_t*>(out + 32 * d + 8 * q) = v;
+                }
+            if (w == 0 && h == 0) a.lse[at] = lse_of(m, sum);
+        }
+    }
+}
+
+template <int RG>
+__device__ __forceinline__ void segment8(const Chunk8Args& a, const CkUnit& x, int t0, int t1, float* part_o, float* part_ml,
+                                         uint8_t* smem) {
+    if constexpr (RG == 8) chunk8_big_segment(a, x, t0, t1, part_o, part_ml, smem);
+    else chunk8_segment<RG>(a, x, t0, t1, part_o, part_ml, smem);
+}
+
 // ------------------------------------------------------------------- kernels
 
 // Runs the tiles of all units are cut into: at most one per CU, and no shorter than `streams` tiles.
@@ -471,7 +773,7 @@ __device__ __forceinline__ int run_count8(const Chunk8Args& a, int total) {
 template <int RG>
 __global__ __launch_bounds__(C8_THREADS, 1) void chunk8_run_kernel(Chunk8Args a) {
     constexpr int ROWS = 16 * RG;
-    __shared__ __align__(1024) uint8_t smem[C8_SMEM];
+    __shared__ __align__(1024) uint8_t smem[RG == 8 ? B8_SMEM : C8_SMEM];
     __shared__ int pre[CK_MAX_UNITS];
     const int total = scan_units<C8_TILE, C8_THREADS>(a, ROWS, pre), U = a.B * a.mb;
     const int n = run_count8(a, total), g = blockIdx.x;
@@ -501,7 +803,7 @@ __global__ __launch_bounds__(C8_THREADS, 1) void chunk8_run_kernel(Chunk8Args a)
             if (t1 == next - base) a.span[3 * u + 1] = g;
         }
         const int64_t slot = 2 * g + (at > beg ? 1 : 0);
-        chunk8_segment<RG>(a, x, t0, t1, whole ? nullptr : a.part_o + slot * (ROWS * D_LAT), a.part_ml + slot * (ROWS * 2), smem);
+        segment8<RG>(a, x, t0, t1, whole ? nullptr : a.part_o + slot * (ROWS * D_LAT), a.part_ml + slot * (ROWS * 2), smem);
         __syncthreads();   // the stages are free
         at = base + t1;
         ++u;
@@ -510,14 +812,14 @@ __global__ __launch_bounds__(C8_THREADS, 1) void chunk8_run_kernel(Chunk8Args a)
 
 template <int RG>
 __global__ __launch_bounds__(C8_THREADS, 1) void chunk8_unit_kernel(Chunk8Args a) {
-    __shared__ __align__(1024) uint8_t smem[C8_SMEM];
+    __shared__ __align__(1024) uint8_t smem[RG == 8 ? B8_SMEM : C8_SMEM];
     const uint32_t wg = workgroup_id();
     if (wg >= (uint32_t)a.B * (uint32_t)a.mb) return;
     const int b = (int)(wg / (uint32_t)a.mb), j = a.mb - 1 - (int)(wg % (uint32_t)a.mb);   // the later rows (more tiles) first
     const CkUnit x = chunk_unit(a, b * a.mb + j, 16 * RG);
     const int n = unit_tiles<C8_TILE>(a, x, 16 * RG);
     if (n == 0) return;
-    chunk8_segment<RG>(a, x, 0, n, nullptr, nullptr, smem);
+    segment8<RG>(a, x, 0, n, nullptr, nullptr, smem);
 }
 
 // Joins the parts of a unit that several runs cover: block = (unit, 128 float4 of a part, in the order the
@@ -580,7 +882,7 @@ __global__ __launch_bounds__(C8J_THREADS) void chunk8_join_kernel(Chunk8Args a, 
 ChunkSplit chunk8_split(int64_t B, int64_t H, int64_t max_q, int64_t max_kv) {
     ChunkSplit s{};
     const int64_t rows = max_q * H;
-    s.qg = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    s.qg = rows <= 16 ? 1 : rows <= 32 ? 2 : rows <= 64 ? 4 : 8;
     s.mb = (rows + 16 * s.qg - 1) / (16 * s.qg);
     s.units = B * s.mb;
     const int64_t tiles = s.units * std::max<int64_t>(1, (max_kv + C8_TILE - 1) / C8_TILE);
@@ -609,7 +911,8 @@ static hipError_t launch_chunk8_rows(const Chunk8Args& a, const ChunkSplit& sp, 
 }
 
 hipError_t launch_chunk8(const Chunk8Args& a, const ChunkSplit& sp, hipStream_t s) {
-    return sp.qg == 1 ? launch_chunk8_rows<1>(a, sp, s) : sp.qg == 2 ? launch_chunk8_rows<2>(a, sp, s) : launch_chunk8_rows<4>(a, sp, s);
+    return sp.qg == 1 ? launch_chunk8_rows<1>(a, sp, s) : sp.qg == 2 ? launch_chunk8_rows<2>(a, sp, s)
+         : sp.qg == 4 ? launch_chunk8_rows<4>(a, sp, s) : launch_chunk8_rows<8>(a, sp, s);
 }
 
 }  // namespace vkv
