@@ -31,7 +31,10 @@ constexpr int C8_OFF_STAGE = C8_OFF_P + 64 * 2 * C8_TILE;       // 1 KB aligned,
 constexpr int C8_SMEM = C8_OFF_STAGE + C8_STAGES * C8_STAGE;
 static_assert(C8_OFF_STAGE % 1024 == 0 && C8_OFF_P % 1024 == 0, "");
 constexpr uint32_t C8_ABSENT = 255;
-constexpr float C8_SLACK = 8.0f;   // lag allowed to the softmax reference maximum (log2 units)
+// Lag allowed to the softmax reference maximum (log2 units): weights up to 2^16, so that outputs are seldom multiplied; a sum
+// over 2^30 rows of 448 * 2^64 stays below 2^119.  (What lies 2^126 below the reference is 0.)
+constexpr float C8_SLACK = 16.0f;
+constexpr float C8_ROOM = 24.0f;   // and a new reference is that far above the maximum, so that it lasts for scores up to 2^40 times as heavy
 
 typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
@@ -65,6 +68,9 @@ __device__ __forceinline__ void lds_write_u1(uint32_t addr, uint32_t v) {
 __device__ __forceinline__ void lds_write_u2(uint32_t addr, const u32x2_t& v) {
     asm volatile("ds_write_b64 %0, %1" ::"v"(addr), "v"(v) : "memory");
 }
+__device__ __forceinline__ void lds_write_u4(uint32_t addr, const u32x4_t& v) {
+    asm volatile("ds_write_b128 %0, %1" ::"v"(addr), "v"(v) : "memory");
+}
 // every LDS operation of this wave is through, then every wave's
 __device__ __forceinline__ void lds_barrier() {
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -90,7 +96,7 @@ __device__ __attribute__((noinline)) void clean_tile(uint32_t st, int w, int lan
         u32x4_t v = lds_read_u4<0>(at);
         lds_wait<0>(v);
         for (int q = 0; q < 4; ++q) v[q] = drop_nan(v[q]);
-        asm volatile("ds_write_b128 %0, %1" ::"v"(at), "v"(v) : "memory");
+        lds_write_u4(at, v);
     }
     lds_barrier();
 }
@@ -114,9 +120,45 @@ struct Loader8 {
 #pragma unroll
             for (int i = 1; i < NR; ++i) e[i] = table[row(t, i) >> a.shift];
     }
-    // the loads of the fetched tile t into stage st (its number in LDS: sg)
-    __device__ __forceinline__ void issue(int t, uint8_t* smem, uint32_t lds0, int sg, int stages = C8_OFF_STAGE) const {
+    // Are tile t's rows of this wave all there and on one page?  Then scalar row addresses and 32 bits of offset a lane do, and
+    // the loads can be issued one by one.
+    __device__ __forceinline__ bool plain(int t) const {
+        return a.page_mask >= NR - 1 && row(t, 0) + NR <= kv && (uint32_t)e[0] < (uint32_t)a.n_pages && a.rs16 < (1u << 24);
+    }
+    static constexpr int LOADS = NR / 2 + NR / 8 + 1;
+    template <int J>
+    __device__ __forceinline__ void part(int t, uint8_t* smem, uint32_t lds0, int sg, int stages) const {
         uint8_t* st = smem + stages + sg * C8_STAGE;
+        int ln = lane;
+        asm volatile("" : "+v"(ln));   // keeps the lane arithmetic out of registers across the loop
+        const uint32_t r = row(t, 0) & a.page_mask, rs = 16 * a.rs16;
+        const char* b = reinterpret_cast<const char*>(a.cache8) + 16 * ((uint64_t)(uint32_t)e[0] * a.ps16 + (uint64_t)r * a.rs16);
+        if constexpr (J < NR / 2) {             // two rows' codes, half a wave each
+            constexpr int i = 2 * J;
+            const uint32_t p16 = (16 * (ln & 31)) ^ (32 * (ln >> 5));
+            __builtin_amdgcn_global_load_lds((gbl_void_t*)(b + (uint64_t)rs * i + ((p16 ^ (16 * code_xor(i))) + (ln >> 5) * rs)),
+                                             (lds_void_t*)(st + D_LAT * (NR * wt + i)), 16, 0, 0);
+        } else if constexpr (J < LOADS - 1) {   // eight rows' branch, eight lanes each
+            constexpr int i = 8 * (J - NR / 2);
+            const uint32_t q16 = 16 * ((ln & 7) ^ ((ln >> 4) & 3));
+            __builtin_amdgcn_global_load_lds((gbl_void_t*)(b + (uint64_t)rs * i + ((q16 ^ (8 * i)) + (ln >> 3) * rs + D_LAT)),
+                                             (lds_void_t*)(st + C8_OFF_ROPE + 2 * D_ROPE * (NR * wt + i)), 16, 0, 0);
+        } else if (ln < NR) {                   // the aligned words around the scale bytes
+            const uint64_t s0 = (uint64_t)(uintptr_t)(a.scale + (uint64_t)(uint32_t)e[0] * (uint64_t)a.sstride);
+            const uint32_t at = (uint32_t)(s0 & 3) + ((r + ln) >> a.bshift);
+            __builtin_amdgcn_global_load_lds((gbl_void_t*)(uintptr_t)((s0 & ~3ull) + (at & ~3u)),
+                                             (lds_void_t*)(smem + C8_OFF_WORD + (sg * C8_TILE + NR * wt) * 4), 4, 0, 0);
+            lds_write_u1(lds0 + C8_OFF_NOTE + (sg * C8_TILE + NR * wt + ln) * 4, 8u * (at & 3u));
+        }
+    }
+    // the loads of the fetched tile t into stage sg
+    __device__ __forceinline__ void issue(int t, uint8_t* smem, uint32_t lds0, int sg, int stages = C8_OFF_STAGE) const {
+        if (plain(t)) static_for<0, LOADS>([&](auto ic) { part<decltype(ic)::value>(t, smem, lds0, sg, stages); });
+        else issue_any(t, smem, lds0, sg, stages);
+    }
+    __device__ __forceinline__ void issue_any(int t, uint8_t* smem, uint32_t lds0, int sg, int stages) const {
+        uint8_t* st = smem + stages + sg * C8_STAGE;
+        const int u = row(t, 0);
         const char* base[NR];
         const uint8_t* word;     // this lane's (of 16) scale byte
         uint32_t absent;
@@ -124,7 +166,7 @@ struct Loader8 {
         asm volatile("" : "+v"(ln));   // keeps the lane arithmetic out of registers across the loop
         const int i16 = ln & 15;
         if (a.page_mask >= NR - 1) {   // the rows lie on one page; rows past the end: the last row's
-            const int u = row(t, 0), last = min(kv - 1 - u, NR - 1);
+            const int last = min(kv - 1 - u, NR - 1);
             const bool there = (uint32_t)e[0] < (uint32_t)a.n_pages;
             const uint32_t p = there ? e[0] : 0, r = there ? u & a.page_mask : 0;
             base[0] = reinterpret_cast<const char*>(a.cache8) + 16 * ((uint64_t)p * a.ps16 + (uint64_t)r * a.rs16);
@@ -171,7 +213,6 @@ struct Loader8 {
             lds_write_u1(lds0 + C8_OFF_NOTE + (sg * C8_TILE + NR * wt + ln) * 4, absent ? C8_ABSENT : 8u * (uint32_t)(at & 3u));
         }
     }
-    static constexpr int LOADS = NR / 2 + NR / 8 + 1;
 };
 
 // ------------------------------------------------------------------ a segment
@@ -255,7 +296,6 @@ __device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit
         lds_barrier();
         if (k + 2 < nt) {
             loader.issue(t0 + k + 2, smem, lds0, sg == 0 ? 2 : sg - 1);
-            loader.fetch(t0 + k + 3);
         }
         const int u0 = C8_TILE * (t0 + k);
         const uint32_t st = lds0 + C8_OFF_STAGE + sg * C8_STAGE;
@@ -360,7 +400,7 @@ __device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit
             const float m = fmaxf(fmaxf(__uint_as_float(tops[j][0]), __uint_as_float(tops[j][1])),
                                   fmaxf(__uint_as_float(tops[j][2]), __uint_as_float(tops[j][3])));
             const bool up = m > m_run[j] + C8_SLACK;
-            next[j] = up ? m : m_run[j];
+            next[j] = up ? m + C8_ROOM : m_run[j];
             move |= up;
         }
         if (__ballot(move)) {   // the same in every wave
@@ -389,6 +429,9 @@ __device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit
         }
 #pragma unroll
         for (int j = 0; j < RG; ++j) l_run[j] += ps[j];   // this lane's share of the sum
+
+        // after the waits for every LDS operation, which would be waits for these scalar loads too
+        if (k + 2 < nt) loader.fetch(t0 + k + 3);
 
         // ---- outputs, dims 128 w .. + 127
         u32x4_t pf[KS][RB];
@@ -483,12 +526,191 @@ __device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit
 // As above, but the queries of 128 rows do not fit in every wave: wave w takes the scores of rows 32 w .. + 31 of the unit
 // against all of the tile's rows, and 128 dims of all rows' outputs.  It has its rows' scores to itself, so
 // their reference moves before the weights are written; the other waves learn by how much.
-constexpr int B8_OFF_SCALE = C8_OFF_TOP;                        // [wave][64] the tile's scales, each wave's own copy
-constexpr int B8_OFF_P = C8_OFF_P;                              // [128][64] bf16
-constexpr int B8_OFF_STAGE = B8_OFF_P + 128 * 2 * C8_TILE;
-constexpr int B8_OFF_ALPHA = B8_OFF_STAGE + C8_STAGES * C8_STAGE;   // [128] by what a row's outputs are to be multiplied
-constexpr int B8_SMEM = B8_OFF_ALPHA + 512;
-static_assert(B8_OFF_STAGE % 1024 == 0 && C8_OFF_P - C8_OFF_BAD >= 64, "");
+//
+// A wave has its SIMD to itself, so what keeps the matrix cores busy while codes are converted (vector instructions,
+// about as long as the products that they feed) has to be in the same instruction stream: the scores of tile k + 1 are
+// taken between the outputs of tile k, four products of either at a time.
+constexpr int B8_P = 128 * 2 * C8_TILE;                         // weights of a tile, [128][64] bf16; two of them
+constexpr int B8_OFF_SCALE = C8_OFF_TOP;                        // [64] the tile's scales (every wave writes the same ones)
+constexpr int B8_OFF_ALPHA = B8_OFF_SCALE + 4 * C8_TILE;        // two of [128]: by what a row's outputs are to be multiplied
+constexpr int B8_OFF_BAD = B8_OFF_ALPHA + 2 * 512;              // two of [4]: the waves' flags, outputs to multiply, a hidden NaN
+constexpr int B8_OFF_P = C8_OFF_P;
+constexpr int B8_OFF_STAGE = B8_OFF_P + 2 * B8_P;
+constexpr int B8_SMEM = B8_OFF_STAGE + C8_STAGES * C8_STAGE;
+static_assert(B8_OFF_BAD + 32 <= B8_OFF_P && B8_OFF_STAGE % 1024 == 0, "");
+
+// The products of the scores are written as instructions: their results have to lie in the registers that the vector
+// units read (the compiler takes accumulators for every product of a kernel that needs some, where these do not fit
+// beside the outputs).  It does not see them, so the wait states are here: two from an operand's conversion to the
+// product, and after the last products, in their own statement, what a reader of the result has to wait (12 from the
+// last one's issue, 8 passes).
+__device__ __forceinline__ void score_first(f32x16_t& s, const bf16x8_t& k, const bf16x8_t& q) {
+    asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(k), "v"(q));
+}
+template <bool NEAR>   // the conversion is right before (else an output's product and a conversion lie between)
+__device__ __forceinline__ void score_next(f32x16_t& s, const bf16x8_t& k, const bf16x8_t& q) {
+    if constexpr (NEAR) asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(k), "v"(q));
+    else asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(k), "v"(q));
+}
+__device__ __forceinline__ void score_last(f32x16_t& s0, f32x16_t& s1, const bf16x8_t& k0, const bf16x8_t& k1, const bf16x8_t& q) {
+    asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %2, %4, %0\n\tv_mfma_f32_32x32x16_bf16 %1, %3, %4, %1\n\ts_nop 15\n\ts_nop 7"
+                 : "+v"(s0), "+v"(s1) : "v"(k0), "v"(k1), "v"(q));
+}
+
+// What the fused loop has in flight of LDS reads: in step j (from -AHEAD: before the loop) the keys of step j + AHEAD (two
+// reads), the values of step j + AHEAD (one), and at the end of every fourth step the weights of the next four (four).
+constexpr int B8_AHEAD = 2, B8_STEPS = 20, B8_OUT = 16;
+template <bool SCORES, bool OUT>
+constexpr int reads_keys(int j) { return SCORES && j + B8_AHEAD < B8_STEPS ? 2 : 0; }
+template <bool SCORES, bool OUT>
+constexpr int reads_values(int j) { return OUT && j + B8_AHEAD < B8_OUT ? 1 : 0; }
+template <bool SCORES, bool OUT>
+constexpr int reads_weights(int j) { return OUT && j >= 0 && j % 4 == 3 && j + 1 < B8_OUT ? 4 : 0; }
+// reads behind those of a step's keys or values, at the place where they are waited for
+template <bool SCORES, bool OUT>
+constexpr int reads_step(int j) { return reads_keys<SCORES, OUT>(j) + reads_values<SCORES, OUT>(j); }
+template <bool SCORES, bool OUT>
+constexpr int reads_between(int i) {   // of the steps i - AHEAD + 1 .. i - 1, and the weights of step i - AHEAD
+    int n = reads_weights<SCORES, OUT>(i - B8_AHEAD);
+    for (int j = i - B8_AHEAD + 1; j < i; ++j) n += reads_step<SCORES, OUT>(j) + reads_weights<SCORES, OUT>(j);
+    return n;
+}
+template <bool SCORES, bool OUT>
+constexpr int behind_keys(int i) {     // step i's keys, in step i after its reads
+    return reads_values<SCORES, OUT>(i - B8_AHEAD) + reads_between<SCORES, OUT>(i) + reads_step<SCORES, OUT>(i);
+}
+template <bool SCORES, bool OUT>
+constexpr int behind_next(int i) {     // step i + 1's keys, in step i before its last product for the outputs (and the read behind it)
+    const int w = reads_weights<SCORES, OUT>(i);
+    return reads_values<SCORES, OUT>(i + 1 - B8_AHEAD) + reads_between<SCORES, OUT>(i + 1) - w + (w ? 3 : 0);
+}
+template <bool SCORES, bool OUT>
+constexpr int behind_values(int i) {   // step i + 1's values, in step i after its reads
+    return reads_between<SCORES, OUT>(i + 1) - reads_weights<SCORES, OUT>(i);
+}
+static_assert(B8_AHEAD == 2, "");
+
+struct Big8 {
+    bf16x8_t qf[36];     // Q^T operand: step 2 s + i (i < 2) has dims 32 s + 16 h + 8 i .. + 7, as a 16-byte piece of codes holds them
+    f32x16_t o[4][4];    // outputs, [dim block][row block]
+    f32x16_t s[2];       // scores: s[b][i] is tile row 32 b + 8 (i / 4) + 4 h + i % 4
+};
+
+// Outputs of the tile in stage sv with the weights at pw, and scores of the tile in stage sk.  Returns this lane's scale (of
+// tile row `lane` of the latter).
+template <bool SCORES, bool OUT>
+__device__ __forceinline__ float fused8(Big8& z, uint32_t lds0, uint32_t sv, uint32_t pw, uint32_t sk, uint32_t wn, int w, int lane) {
+    int ln = lane;
+    asm volatile("" : "+v"(ln));   // operand addresses are found anew from it, so that no registers hold them across the loop
+    const int r = ln & 31, hh = ln >> 5;
+    // values: a lane group's eight rows of 16, its place among the dims; weights: row r, piece 2 step + h
+    const int e = (ln >> 1) & 7, vr = 4 * hh + (e & 3) + 8 * (e >> 2);
+    const uint32_t va = sv + vr * D_LAT + 16 * ((8 * w + ((ln >> 4) & 1)) ^ code_xor(vr)) + 8 * (ln & 1);
+    const uint32_t pr = pw + r * (2 * C8_TILE) + 16 * (hh ^ rope_xor(r));
+    // keys: pieces 2 s + h of rows r and 32 + r
+    const uint32_t ka = sk + r * D_LAT + 16 * (hh ^ code_xor(r & 15)), kb = ka + 32 * D_LAT;
+    const uint32_t ra = sk + C8_OFF_ROPE + r * (2 * D_ROPE) + 16 * (hh ^ rope_xor(r));
+    constexpr int NB = B8_AHEAD + 1;
+    u32x4_t kc[NB][2], pf[4];
+    u32x2_t vv[NB];
+    float sc = 0.f, sk2[2] = {0.f, 0.f};
+    auto kload = [&](auto ic) {
+        constexpr int i = decltype(ic)::value;
+        if constexpr (SCORES && i < B8_STEPS) {
+            if constexpr (i < 16) {
+                kc[i % NB][0] = lds_read_u4<0>(ka ^ (32 * i));
+                kc[i % NB][1] = lds_read_u4<0>(kb ^ (32 * i));
+            } else {
+                kc[i % NB][0] = lds_read_u4<0>(ra ^ (32 * (i - 16)));
+                kc[i % NB][1] = lds_read_u4<32 * 2 * D_ROPE>(ra ^ (32 * (i - 16)));
+            }
+        }
+    };
+    auto vload = [&](auto ic) {
+        constexpr int i = decltype(ic)::value;
+        if constexpr (OUT && i < B8_OUT) vv[i % NB] = lds_read_tr8<16 * D_LAT * (i >> 2)>(va ^ (32 * (i & 3)));
+    };
+    auto pload = [&](auto sc_, auto rc) {
+        constexpr int s = decltype(sc_)::value, rb = decltype(rc)::value;
+        pf[rb] = lds_read_u4<rb * 32 * 2 * C8_TILE>(pr ^ (32 * s));
+    };
+    uint32_t word = 0, note = C8_ABSENT;
+    if constexpr (SCORES) {
+        word = lds_read_u1(wn);
+        note = lds_read_u1(wn + (C8_OFF_NOTE - C8_OFF_WORD));
+    }
+    if constexpr (OUT) static_for<0, 4>([&](auto rc) { pload(std::integral_constant<int, 0>{}, rc); });
+    static_for<0, B8_AHEAD>([&](auto ic) {
+        kload(ic);
+        vload(ic);
+    });
+    if constexpr (SCORES) {
+        lds_wait<(OUT ? 4 + 3 * B8_AHEAD : 2 * B8_AHEAD)>(word, note);
+        sc = scale_of(word, note);
+        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(sc), __float_as_uint(sc), false, false);
+        sk2[0] = __uint_as_float(sw[0]);     // of rows r and 32 + r
+        sk2[1] = __uint_as_float(sw[1]);
+    }
+    // the operands of the next products: a key's is decoded while the product before it runs, a step's values during the last one
+    bf16x8_t kd, vd[2];
+    auto vwait = [&](auto ic, auto n) {
+        lds_wait<decltype(n)::value>(vv[decltype(ic)::value % NB]);
+    };
+    auto kdecode = [&](auto ic, auto qc) {
+        constexpr int i = decltype(ic)::value, q = decltype(qc)::value;
+        const u32x4_t& k4 = kc[i % NB][q & 1];
+        kd = decode8(k4[2 * (q >> 1)], k4[2 * (q >> 1) + 1], sk2[q & 1]);
+    };
+    if constexpr (SCORES) {
+        lds_wait<(OUT ? 1 : 0) + (B8_AHEAD - 1) * (OUT ? 3 : 2)>(kc[0][0], kc[0][1]);
+        kdecode(std::integral_constant<int, 0>{}, std::integral_constant<int, 0>{});
+    }
+    if constexpr (OUT) {
+        vwait(std::integral_constant<int, 0>{}, std::integral_constant<int, (B8_AHEAD - 1) * (SCORES ? 3 : 1)>{});
+        vd[0] = decode8(vv[0][0], vv[0][1], 1.0f);
+    }
+    static_for<0, (SCORES ? B8_STEPS : B8_OUT)>([&](auto ic) {
+        constexpr int i = decltype(ic)::value;
+        constexpr bool out = OUT && i < B8_OUT, more = OUT && i + 1 < B8_OUT;
+        kload(std::integral_constant<int, i + B8_AHEAD>{});
+        vload(std::integral_constant<int, i + B8_AHEAD>{});
+        if constexpr (SCORES && i >= 16) lds_wait<behind_keys<SCORES, OUT>(i)>(kc[i % NB][0], kc[i % NB][1]);
+        if constexpr (more) lds_wait<behind_values<SCORES, OUT>(i)>(vv[(i + 1) % NB]);
+        static_for<0, 4>([&](auto rc) {      // a product of either kind, and conversions behind each
+            constexpr int q = decltype(rc)::value, half = q >> 1, b = q & 1;
+            if constexpr (SCORES && i < 16) {
+                if constexpr (i == 0 && half == 0) score_first(z.s[b], kd, z.qf[0]);
+                else score_next<!more>(z.s[b], kd, z.qf[2 * i + half]);
+                if constexpr (q < 3) {
+                    kdecode(ic, std::integral_constant<int, q + 1>{});
+                } else if constexpr (i + 1 < 16) {
+                    lds_wait<behind_next<SCORES, OUT>(i)>(kc[(i + 1) % NB][0], kc[(i + 1) % NB][1]);
+                    kdecode(std::integral_constant<int, i + 1>{}, std::integral_constant<int, 0>{});
+                }
+            } else if constexpr (SCORES && i < B8_STEPS - 1) {
+                if constexpr (half == 0) score_next<true>(z.s[b], __builtin_bit_cast(bf16x8_t, kc[i % NB][b]), z.qf[16 + i]);
+            } else if constexpr (SCORES && q == 0) {
+                score_last(z.s[0], z.s[1], __builtin_bit_cast(bf16x8_t, kc[i % NB][0]), __builtin_bit_cast(bf16x8_t, kc[i % NB][1]), z.qf[16 + i]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (out) {
+                constexpr int s = i >> 2, d = i & 3;
+                // the weights came at the end of the last step: behind each are the later ones, and this step's keys and values
+                if constexpr (d == 0) lds_wait<3 - q + reads_keys<SCORES, OUT>(i) + reads_values<SCORES, OUT>(i)>(pf[q]);
+                z.o[d][q] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vd[i & 1], __builtin_bit_cast(bf16x8_t, pf[q]), z.o[d][q], 0, 0, 0);
+                if constexpr (d == 3 && more) pload(std::integral_constant<int, s + 1>{}, rc);
+                if constexpr (more) {        // a quarter of the next step's values
+                    const uint32_t word = vv[(i + 1) % NB][q >> 1];
+                    const bf16x2_t two = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(word, 1.0f, q & 1);
+                    vd[(i + 1) & 1][2 * q] = two[0];
+                    vd[(i + 1) & 1][2 * q + 1] = two[1];
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    });
+    return sc;
+}
 
 __device__ __forceinline__ void chunk8_big_segment(const Chunk8Args& a, const CkUnit& x, int t0, int t1, float* part_o,
                                                    float* part_ml, uint8_t* smem) {
@@ -502,16 +724,15 @@ __device__ __forceinline__ void chunk8_big_segment(const Chunk8Args& a, const Ck
     const int nt = x.kv > 0 ? t1 - t0 : 0;
 
     Loader8 loader{a, (const_i32_t*)(a.table + (int64_t)x.b * a.tstride), x.kv, w, lane, {}};
-    // Q^T operand: step 2 s + i (i < 2) has dims 32 s + 16 h + 8 i .. + 7, as a 16-byte piece of codes holds them
-    bf16x8_t qf[36];
+    Big8 z;
     {
         const int64_t row = x.tok0 * a.H + Rc;
         const uint16_t* ql = a.q_lat + row * a.qls + 16 * h;
         const uint16_t* qr = a.q_rope + row * a.qrs + 8 * h;
 #pragma unroll
-        for (int s = 0; s < 32; ++s) qf[s] = *reinterpret_cast<const bf16x8_t*>(ql + 32 * (s >> 1) + 8 * (s & 1));
+        for (int s = 0; s < 32; ++s) z.qf[s] = *reinterpret_cast<const bf16x8_t*>(ql + 32 * (s >> 1) + 8 * (s & 1));
 #pragma unroll
-        for (int s = 0; s < 4; ++s) qf[32 + s] = *reinterpret_cast<const bf16x8_t*>(qr + 16 * s);
+        for (int s = 0; s < 4; ++s) z.qf[32 + s] = *reinterpret_cast<const bf16x8_t*>(qr + 16 * s);
     }
     if (nt > 0) {
         loader.fetch(t0);
@@ -523,87 +744,22 @@ __device__ __forceinline__ void chunk8_big_segment(const Chunk8Args& a, const Ck
         }
     }
 #pragma unroll
-    for (int s = 0; s < 36; ++s) asm volatile("" : "+v"(qf[s]));   // no wait for them inside the tile loop
-
-    f32x16_t o[4][4];   // [dim block][row block]
+    for (int s = 0; s < 36; ++s) asm volatile("" : "+v"(z.qf[s]));   // no wait for them inside the tile loop
 #pragma unroll
     for (int d = 0; d < 4; ++d)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[d][r][i] = 0.f;
+            for (int i = 0; i < 16; ++i) z.o[d][r][i] = 0.f;
     float m_run = -INFINITY, l_run = 0.f;
-    auto opaque_lane = [&]() {   // operand addresses are found anew from it, so that no registers hold them across the loop
-        int ln = lane;
-        asm volatile("" : "+v"(ln));
-        return ln;
-    };
 
-    int sg = 0;   // the stage of tile k
-    for (int k = 0; k < nt; ++k) {
-        if (k + 1 < nt)
-            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(Loader8::LOADS) : "memory");
-        else
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        lds_barrier();
-        if (k + 2 < nt) {
-            loader.issue(t0 + k + 2, smem, lds0, sg == 0 ? 2 : sg - 1, B8_OFF_STAGE);
-            loader.fetch(t0 + k + 3);
-        }
-        const int u0 = C8_TILE * (t0 + k);
-        const uint32_t st = lds0 + B8_OFF_STAGE + sg * C8_STAGE;
-        const uint32_t wn = lds0 + C8_OFF_WORD + (sg * C8_TILE + lane) * 4;
-        sg = sg == 2 ? 0 : sg + 1;
-
-        // ---- scores of the 64 rows of the tile: s[b][i] is row 32 b + 8 (i / 4) + 4 h + i % 4
-        uint32_t word = lds_read_u1(wn), note = lds_read_u1(wn + (C8_OFF_NOTE - C8_OFF_WORD));
-        const int ln = opaque_lane(), r = ln & 31;
-        uint32_t ka[2];    // pieces 2 s + h of rows r and 32 + r
-        ka[0] = st + r * D_LAT + 16 * ((ln >> 5) ^ code_xor(r & 15));
-        ka[1] = ka[0] + 32 * D_LAT;
-        const uint32_t ra = st + C8_OFF_ROPE + r * (2 * D_ROPE) + 16 * ((ln >> 5) ^ rope_xor(r));
-        constexpr int SD = 3;          // operands read ahead of the matrix cores, of either half of the tile: 16 of codes, 4 of the branch
-        u32x4_t kc[SD + 1][2];
-        auto kload = [&](auto sc_) {
-            constexpr int s = decltype(sc_)::value;
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                if constexpr (s < 16) kc[s % (SD + 1)][b] = lds_read_u4<0>(ka[b] ^ (32 * s));
-                else kc[s % (SD + 1)][b] = b ? lds_read_u4<32 * 2 * D_ROPE>(ra ^ (32 * (s - 16))) : lds_read_u4<0>(ra ^ (32 * (s - 16)));
-            }
-        };
-        static_for<0, SD>(kload);
-        lds_wait<2 * SD>(word, note);
-        const float sc = scale_of(word, note);                  // of tile row `lane`
+    // the weights of the tile whose scores are there (rows from u0 on), into buffer k & 1
+    auto weights = [&](int k, int u0, float sc) __attribute__((always_inline)) {
+        const uint32_t own = lds0 + B8_OFF_SCALE;
+        lds_write_u1(own + 4 * lane, __float_as_uint(sc));
         const uint64_t absent = __ballot(sc == 0.f);
-        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(sc), __float_as_uint(sc), false, false);
-        const float sk[2] = {__uint_as_float(sw[0]), __uint_as_float(sw[1])};   // of rows r and 32 + r
-        lds_write_u1(lds0 + B8_OFF_SCALE + 256 * w + 4 * ln, __float_as_uint(sc));
-        f32x16_t s2[2];
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s2[b][i] = 0.f;
-        static_for<0, 20>([&](auto sc_) {
-            constexpr int s = decltype(sc_)::value;
-            if constexpr (s + SD < 20) kload(std::integral_constant<int, s + SD>{});
-            lds_wait<2 * ((s + SD < 20) ? SD : 19 - s)>(kc[s % (SD + 1)][0], kc[s % (SD + 1)][1]);
-            if constexpr (s < 16) {
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int b = 0; b < 2; ++b) {
-                        const u32x4_t& v = kc[s % (SD + 1)][b];
-                        s2[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(decode8(v[2 * i], v[2 * i + 1], sk[b]), qf[2 * s + i], s2[b], 0, 0, 0);
-                    }
-            } else {
-#pragma unroll
-                for (int b = 0; b < 2; ++b)
-                    s2[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kc[s % (SD + 1)][b]), qf[16 + s], s2[b], 0, 0, 0);
-            }
-        });
-
-        // ---- weights
+        u32x4_t f[8];                         // of the rows whose scores this lane has, in their order
+        static_for<0, 8>([&](auto ic) { f[decltype(ic)::value] = lds_read_u4<32 * decltype(ic)::value>(own + 16 * h); });
         bool bad = false;
         if (u0 + C8_TILE - 1 > lim_lo || absent != 0) {
             const int last = lim - u0 - 4 * h;
@@ -614,101 +770,95 @@ __device__ __forceinline__ void chunk8_big_segment(const Chunk8Args& a, const Ck
                 for (int i = 0; i < 16; ++i) {
                     const int row = 32 * b + 8 * (i >> 2) + (i & 3);
                     if (row > last || ((gone >> row) & 1u)) {
-                        bad |= s2[b][i] != s2[b][i];
-                        s2[b][i] = -INFINITY;
+                        bad |= z.s[b][i] != z.s[b][i];
+                        z.s[b][i] = -INFINITY;
                     }
                 }
         }
-        float top = s2[0][0];
+        float top = z.s[0][0];
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, s2[b][i]);
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, z.s[b][i]);
         top = half_max(top) * a.scale_log2;
         const bool move = top > m_run + C8_SLACK;
+        top += C8_ROOM;
         const float alpha = move ? __builtin_amdgcn_exp2f(m_run - top) : 1.0f;
         if (move) m_run = top;
         l_run *= alpha;
         const float ref = m_run == -INFINITY ? 0.f : m_run;
         const uint32_t flags = (__ballot(move) ? 1u : 0u) | (__ballot(bad) ? 2u : 0u);
-        const uint32_t pa = lds0 + B8_OFF_P + (32 * w + c) * (2 * C8_TILE);
+        const uint32_t pa = lds0 + B8_OFF_P + (k & 1) * B8_P + (32 * w + c) * (2 * C8_TILE);
         const uint32_t px = rope_xor(c);
         float psum = 0.f;
+        static_for<0, 4>([&](auto ic) { lds_wait<0>(f[2 * decltype(ic)::value], f[2 * decltype(ic)::value + 1]); });
+        static_for<0, 4>([&](auto ic) {        // 16 rows of the tile, eight of them this lane's
+            constexpr int q = decltype(ic)::value, b = q >> 1;
+            bf16x8_t p8;
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {      // 16 rows of the tile, eight of them this lane's
-                u32x4_t f[2] = {lds_read_u4<B8_OFF_SCALE>(lds0 + 256 * w + 128 * b + 64 * q + 16 * h),
-                                lds_read_u4<B8_OFF_SCALE + 32>(lds0 + 256 * w + 128 * b + 64 * q + 16 * h)};
-                lds_wait<0>(f[0], f[1]);
-                bf16x8_t p8;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s2[b][8 * q + i], a.scale_log2, -ref));
-                    psum += p;
-                    p8[i] = (__bf16)(p * __uint_as_float(f[i >> 2][i & 3]));
-                }
-                const u32x4_t v = __builtin_bit_cast(u32x4_t, p8);
-                asm volatile("ds_write_b128 %0, %1" ::"v"(pa + 16 * ((2 * (2 * b + q) + h) ^ px)), "v"(v) : "memory");
+            for (int i = 0; i < 8; ++i) {
+                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(z.s[b][8 * (q & 1) + i], a.scale_log2, -ref));
+                psum += p;
+                p8[i] = (__bf16)(p * __uint_as_float(f[2 * q + (i >> 2)][i & 3]));
             }
+            const u32x4_t v = __builtin_bit_cast(u32x4_t, p8);
+            lds_write_u4(pa + 16 * ((2 * q + h) ^ px), v);
+        });
         l_run += psum;   // this lane's share of the sum
-        if (h == 0) lds_write_u1(lds0 + B8_OFF_ALPHA + (32 * w + c) * 4, __float_as_uint(alpha));
-        if (lane == 0) lds_write_u1(lds0 + C8_OFF_BAD + 4 * w, flags);
-        lds_barrier();
+        if (h == 0) lds_write_u1(lds0 + B8_OFF_ALPHA + 512 * (k & 1) + (32 * w + c) * 4, __float_as_uint(alpha));
+        if (lane == 0) lds_write_u1(lds0 + B8_OFF_BAD + 16 * (k & 1) + 4 * w, flags);
+    };
+    auto stage = [&](int sg) { return lds0 + B8_OFF_STAGE + sg * C8_STAGE; };
+    auto words = [&](int sg) { return lds0 + C8_OFF_WORD + (sg * C8_TILE + lane) * 4; };
 
-        // ---- outputs, dims 128 w .. + 127
-        u32x4_t fl = lds_read_u4<C8_OFF_BAD>(lds0);
+    if (nt > 0) {
+        if (nt > 1)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(Loader8::LOADS) : "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        lds_barrier();
+        const float sc = fused8<true, false>(z, lds0, 0, 0, stage(0), words(0), w, lane);
+        weights(0, C8_TILE * t0, sc);
+    }
+    int sg = 0;   // the stage of tile k
+    // tile k + 1 has landed, every wave's share; the weights of tile k are there, and nobody reads tile k - 1 any more
+    auto turn = [&](int k, auto more) __attribute__((always_inline)) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        lds_barrier();
+        u32x4_t fl = lds_read_u4<B8_OFF_BAD>(lds0 + 16 * (k & 1));
+        if (decltype(more)::value && k + 2 < nt) loader.issue(t0 + k + 2, smem, lds0, sg == 0 ? 2 : sg - 1, B8_OFF_STAGE);
         lds_wait<0>(fl);
-        const uint32_t all = __builtin_amdgcn_readfirstlane(fl[0] | fl[1] | fl[2] | fl[3]);
+        const uint32_t all = __builtin_amdgcn_readfirstlane((fl[0] | fl[1]) | (fl[2] | fl[3]));
         if (all & 1u) {
 #pragma unroll
-            for (int rb = 0; rb < 4; ++rb) {
-                uint32_t f = lds_read_u1(lds0 + B8_OFF_ALPHA + (32 * rb + c) * 4);
+            for (int rb = 0; rb < 4; ++rb) {      // a wave's rows are a row block
+                if (!(__builtin_amdgcn_readfirstlane(fl[rb]) & 1u)) continue;
+                uint32_t f = lds_read_u1(lds0 + B8_OFF_ALPHA + 512 * (k & 1) + (32 * rb + c) * 4);
                 lds_wait<0>(f);
 #pragma unroll
                 for (int d = 0; d < 4; ++d)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        float v = o[d][rb][i];
+                        float v = z.o[d][rb][i];
                         scale_acc(v, __uint_as_float(f));
-                        o[d][rb][i] = v;
+                        z.o[d][rb][i] = v;
                     }
             }
         }
-        const int vl = opaque_lane(), e = (vl >> 1) & 7, vr = 4 * (vl >> 5) + (e & 3) + 8 * (e >> 2);
-        const uint32_t va = st + vr * D_LAT + 16 * ((8 * w + ((vl >> 4) & 1)) ^ code_xor(vr)) + 8 * (vl & 1);
-        const uint32_t pr = lds0 + B8_OFF_P + (vl & 31) * (2 * C8_TILE) + 16 * ((vl >> 5) ^ rope_xor(vl & 31));
-        if (all & 2u) clean_tile(st, w, lane);
-        {
-            constexpr int N = 16, VD = 4;
-            u32x2_t vv[VD + 1];
-            u32x4_t pf[4];
-            auto vload = [&](auto ic) {
-                constexpr int i = decltype(ic)::value, s = i >> 2, d = i & 3;
-                vv[i % (VD + 1)] = lds_read_tr8<16 * D_LAT * s>(va ^ (32 * d));
-            };
-            auto pload = [&](auto sc_) {
-                constexpr int s = decltype(sc_)::value;
-#pragma unroll
-                for (int rb = 0; rb < 4; ++rb) pf[rb] = rb == 0 ? lds_read_u4<0>(pr ^ (32 * s)) : rb == 1 ? lds_read_u4<4096>(pr ^ (32 * s))
-                                                      : rb == 2 ? lds_read_u4<8192>(pr ^ (32 * s)) : lds_read_u4<12288>(pr ^ (32 * s));
-            };
-            static_for<0, VD>(vload);
-            static_for<0, N>([&](auto ic) {
-                constexpr int i = decltype(ic)::value, s = i >> 2, d = i & 3;
-                if constexpr (d == 0) {
-                    pload(std::integral_constant<int, s>{});
-                    lds_wait<2>(pf[0], pf[1]);
-                    lds_wait<0>(pf[2], pf[3]);
-                }
-                if constexpr (i + VD < N) vload(std::integral_constant<int, i + VD>{});
-                lds_wait<(i + VD < N) ? VD : N - 1 - i>(vv[i % (VD + 1)]);
-                const bf16x8_t v = decode8(vv[i % (VD + 1)][0], vv[i % (VD + 1)][1], 1.0f);
-#pragma unroll
-                for (int rb = 0; rb < 4; ++rb)
-                    o[d][rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8_t, pf[rb]), o[d][rb], 0, 0, 0);
-            });
-        }
+        if (all & 2u) clean_tile(stage(sg), w, lane);
+        // after the waits for every LDS operation, which would be waits for these scalar loads too
+        if (decltype(more)::value && k + 2 < nt) loader.fetch(t0 + k + 3);
+    };
+    for (int k = 0; k + 1 < nt; ++k) {
+        turn(k, std::true_type{});
+        const int next = sg == 2 ? 0 : sg + 1;
+        const float sc = fused8<true, true>(z, lds0, stage(sg), lds0 + B8_OFF_P + (k & 1) * B8_P, stage(next), words(next), w, lane);
+        weights(k + 1, C8_TILE * (t0 + k + 1), sc);
+        sg = next;
+    }
+    if (nt > 0) {
+        turn(nt - 1, std::false_type{});
+        (void)fused8<false, true>(z, lds0, stage(sg), lds0 + B8_OFF_P + ((nt - 1) & 1) * B8_P, 0, 0, w, lane);
     }
 
     // ---- the rows' references and sums, for every wave
@@ -729,7 +879,7 @@ __device__ __forceinline__ void chunk8_big_segment(const Chunk8Args& a, const Ck
             for (int d = 0; d < 4; ++d)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const f32x4_t v = {o[d][rb][4 * q], o[d][rb][4 * q + 1], o[d][rb][4 * q + 2], o[d][rb][4 * q + 3]};
+                    const f32x4_t v = {z.o[d][rb][4 * q], z.o[d][rb][4 * q + 1], z.o[d][rb][4 * q + 2], z.o[d][rb][4 * q + 3]};
                     *reinterpret_cast<f32x4_t*>(part_o + ((((w * 4 + d) * 4 + rb) * 4 + q) * 64 + lane) * 4) = v;
                 }
             if (w == 0 && h == 0) {
@@ -745,8 +895,8 @@ __device__ __forceinline__ void chunk8_big_segment(const Chunk8Args& a, const Ck
             for (int d = 0; d < 4; ++d)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const bf16x4_t v = {(__bf16)(o[d][rb][4 * q] * inv), (__bf16)(o[d][rb][4 * q + 1] * inv),
-                                        (__bf16)(o[d][rb][4 * q + 2] * inv), (__bf16)(o[d][rb][4 * q + 3] * inv)};
+                    const bf16x4_t v = {(__bf16)(z.o[d][rb][4 * q] * inv), (__bf16)(z.o[d][rb][4 * q + 1] * inv),
+                                        (__bf16)(z.o[d][rb][4 * q + 2] * inv), (__bf16)(z.o[d][rb][4 * q + 3] * inv)};
                     *reinterpret_cast<bf16x4_t*>(out + 32 * d + 8 * q) = v;
                 }
             if (w == 0 && h == 0) a.lse[at] = lse_of(m, sum);
