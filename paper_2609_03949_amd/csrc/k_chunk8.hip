@@ -588,7 +588,7 @@ template <bool SCORES, bool OUT>
 constexpr int behind_values(int i) {   // step i + 1's values, in step i after its reads
     return reads_between<SCORES, OUT>(i + 1) - reads_weights<SCORES, OUT>(i);
 }
-static_assert(B8_AHEAD == 2, "");
+static_assert(B8_AHEAD == 2, "");   // (the values' registers are two)
 
 struct Big8 {
     bf16x8_t qf[36];     // Q^T operand: step 2 s + i (i < 2) has dims 32 s + 16 h + 8 i .. + 7, as a 16-byte piece of codes holds them
@@ -608,18 +608,18 @@ __device__ __forceinline__ float fused8(Big8& z, uint32_t lds0, uint32_t sv, uin
     const uint32_t va = sv + vr * D_LAT + 16 * ((8 * w + ((ln >> 4) & 1)) ^ code_xor(vr)) + 8 * (ln & 1);
     const uint32_t pr = pw + r * (2 * C8_TILE) + 16 * (hh ^ rope_xor(r));
     // keys: pieces 2 s + h of rows r and 32 + r
-    const uint32_t ka = sk + r * D_LAT + 16 * (hh ^ code_xor(r & 15)), kb = ka + 32 * D_LAT;
+    const uint32_t ka = sk + r * D_LAT + 16 * (hh ^ code_xor(r & 15));
     const uint32_t ra = sk + C8_OFF_ROPE + r * (2 * D_ROPE) + 16 * (hh ^ rope_xor(r));
     constexpr int NB = B8_AHEAD + 1;
     u32x4_t kc[NB][2], pf[4];
-    u32x2_t vv[NB];
+    u32x2_t vv[2];
     float sc = 0.f, sk2[2] = {0.f, 0.f};
     auto kload = [&](auto ic) {
         constexpr int i = decltype(ic)::value;
         if constexpr (SCORES && i < B8_STEPS) {
             if constexpr (i < 16) {
                 kc[i % NB][0] = lds_read_u4<0>(ka ^ (32 * i));
-                kc[i % NB][1] = lds_read_u4<0>(kb ^ (32 * i));
+                kc[i % NB][1] = lds_read_u4<32 * D_LAT>(ka ^ (32 * i));
             } else {
                 kc[i % NB][0] = lds_read_u4<0>(ra ^ (32 * (i - 16)));
                 kc[i % NB][1] = lds_read_u4<32 * 2 * D_ROPE>(ra ^ (32 * (i - 16)));
@@ -628,7 +628,7 @@ __device__ __forceinline__ float fused8(Big8& z, uint32_t lds0, uint32_t sv, uin
     };
     auto vload = [&](auto ic) {
         constexpr int i = decltype(ic)::value;
-        if constexpr (OUT && i < B8_OUT) vv[i % NB] = lds_read_tr8<16 * D_LAT * (i >> 2)>(va ^ (32 * (i & 3)));
+        if constexpr (OUT && i < B8_OUT) vv[i % 2] = lds_read_tr8<16 * D_LAT * (i >> 2)>(va ^ (32 * (i & 3)));
     };
     auto pload = [&](auto sc_, auto rc) {
         constexpr int s = decltype(sc_)::value, rb = decltype(rc)::value;
@@ -654,7 +654,7 @@ __device__ __forceinline__ float fused8(Big8& z, uint32_t lds0, uint32_t sv, uin
     // the operands of the next products: a key's is decoded while the product before it runs, a step's values during the last one
     bf16x8_t kd, vd[2];
     auto vwait = [&](auto ic, auto n) {
-        lds_wait<decltype(n)::value>(vv[decltype(ic)::value % NB]);
+        lds_wait<decltype(n)::value>(vv[decltype(ic)::value % 2]);
     };
     auto kdecode = [&](auto ic, auto qc) {
         constexpr int i = decltype(ic)::value, q = decltype(qc)::value;
@@ -675,7 +675,7 @@ __device__ __forceinline__ float fused8(Big8& z, uint32_t lds0, uint32_t sv, uin
         kload(std::integral_constant<int, i + B8_AHEAD>{});
         vload(std::integral_constant<int, i + B8_AHEAD>{});
         if constexpr (SCORES && i >= 16) lds_wait<behind_keys<SCORES, OUT>(i)>(kc[i % NB][0], kc[i % NB][1]);
-        if constexpr (more) lds_wait<behind_values<SCORES, OUT>(i)>(vv[(i + 1) % NB]);
+        if constexpr (more) lds_wait<behind_values<SCORES, OUT>(i)>(vv[(i + 1) % 2]);
         static_for<0, 4>([&](auto rc) {      // a product of either kind, and conversions behind each
             constexpr int q = decltype(rc)::value, half = q >> 1, b = q & 1;
             if constexpr (SCORES && i < 16) {
@@ -700,7 +700,7 @@ __device__ __forceinline__ float fused8(Big8& z, uint32_t lds0, uint32_t sv, uin
                 z.o[d][q] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vd[i & 1], __builtin_bit_cast(bf16x8_t, pf[q]), z.o[d][q], 0, 0, 0);
                 if constexpr (d == 3 && more) pload(std::integral_constant<int, s + 1>{}, rc);
                 if constexpr (more) {        // a quarter of the next step's values
-                    const uint32_t word = vv[(i + 1) % NB][q >> 1];
+                    const uint32_t word = vv[(i + 1) % 2][q >> 1];
                     const bf16x2_t two = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(word, 1.0f, q & 1);
                     vd[(i + 1) & 1][2 * q] = two[0];
                     vd[(i + 1) & 1][2 * q + 1] = two[1];
@@ -755,8 +755,11 @@ __device__ __forceinline__ void chunk8_big_segment(const Chunk8Args& a, const Ck
 
     // the weights of the tile whose scores are there (rows from u0 on), into buffer k & 1
     auto weights = [&](int k, int u0, float sc) __attribute__((always_inline)) {
+        int ln = lane;
+        asm volatile("" : "+v"(ln));          // (as above)
+        const int c = ln & 31, h = ln >> 5;
         const uint32_t own = lds0 + B8_OFF_SCALE;
-        lds_write_u1(own + 4 * lane, __float_as_uint(sc));
+        lds_write_u1(own + 4 * ln, __float_as_uint(sc));
         const uint64_t absent = __ballot(sc == 0.f);
         u32x4_t f[8];                         // of the rows whose scores this lane has, in their order
         static_for<0, 8>([&](auto ic) { f[decltype(ic)::value] = lds_read_u4<32 * decltype(ic)::value>(own + 16 * h); });
@@ -806,7 +809,7 @@ __device__ __forceinline__ void chunk8_big_segment(const Chunk8Args& a, const Ck
         });
         l_run += psum;   // this lane's share of the sum
         if (h == 0) lds_write_u1(lds0 + B8_OFF_ALPHA + 512 * (k & 1) + (32 * w + c) * 4, __float_as_uint(alpha));
-        if (lane == 0) lds_write_u1(lds0 + B8_OFF_BAD + 16 * (k & 1) + 4 * w, flags);
+        if (ln == 0) lds_write_u1(lds0 + B8_OFF_BAD + 16 * (k & 1) + 4 * w, flags);
     };
     auto stage = [&](int sg) { return lds0 + B8_OFF_STAGE + sg * C8_STAGE; };
     auto words = [&](int sg) { return lds0 + C8_OFF_WORD + (sg * C8_TILE + lane) * 4; };
@@ -904,6 +907,10 @@ __device__ __forceinline__ void chunk8_big_segment(const Chunk8Args& a, const Ck
     }
 }
 
+// Floats from one run's part to the next: 1280 bytes more than a part has.  At a run's end every workgroup stores its part at about
+// the same pace; parts a power of two apart would keep all of them at the same few memory channels.
+constexpr int64_t part_stride(int rows) { return (int64_t)rows * D_LAT + 320; }
+
 template <int RG>
 __device__ __forceinline__ void segment8(const Chunk8Args& a, const CkUnit& x, int t0, int t1, float* part_o, float* part_ml,
                                          uint8_t* smem) {
@@ -953,7 +960,7 @@ __global__ __launch_bounds__(C8_THREADS, 1) void chunk8_run_kernel(Chunk8Args a)
             if (t1 == next - base) a.span[3 * u + 1] = g;
         }
         const int64_t slot = 2 * g + (at > beg ? 1 : 0);
-        segment8<RG>(a, x, t0, t1, whole ? nullptr : a.part_o + slot * (ROWS * D_LAT), a.part_ml + slot * (ROWS * 2), smem);
+        segment8<RG>(a, x, t0, t1, whole ? nullptr : a.part_o + slot * part_stride(ROWS), a.part_ml + slot * (ROWS * 2), smem);
         __syncthreads();   // the stages are free
         at = base + t1;
         ++u;
@@ -1007,7 +1014,7 @@ __global__ __launch_bounds__(C8J_THREADS) void chunk8_join_kernel(Chunk8Args a, 
                 const float* ml = a.part_ml + slot * (rows * 2) + 2 * r;
                 m[j] = ml[0];
                 l[j] = ml[1];
-                v[j] = *reinterpret_cast<const f32x4_t*>(a.part_o + slot * (rows * D_LAT) + 4 * f);
+                v[j] = *reinterpret_cast<const f32x4_t*>(a.part_o + slot * part_stride(rows) + 4 * f);
             }
 #pragma unroll
             for (int j = 0; j < C8J_BATCH; ++j)
@@ -1040,7 +1047,7 @@ ChunkSplit chunk8_split(int64_t B, int64_t H, int64_t max_q, int64_t max_kv) {
     s.streams = 1;
     if (s.runs) {
         s.runs = std::max<int64_t>(1, std::min<int64_t>(s.runs, tiles));
-        s.part_o = (size_t)(2 * s.runs) * 16 * s.qg * D_LAT * 4;
+        s.part_o = (size_t)(2 * s.runs) * part_stride(16 * s.qg) * 4;
         s.part_ml = (size_t)(2 * s.runs) * 16 * s.qg * 2 * 4;
         s.span = (size_t)s.units * 3 * 4;
     }
