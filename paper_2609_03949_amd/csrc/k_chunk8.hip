@@ -225,7 +225,7 @@ __device__ __forceinline__ void scale_acc(float& v, float f) {
     asm volatile("v_accvgpr_read_b32 %1, %0\n\tv_mul_f32 %1, %1, %2\n\tv_accvgpr_write_b32 %0, %1" : "+a"(v), "=&v"(t) : "v"(f));
 }
 
-// Tiles [t0, t1) of unit x (16 RG rows) by one workgroup.  part: where an incomplete unit's
+// Tiles [t0, t1) of unit x (16 RG rows, RG 1 or 2) by one workgroup.  part: where an incomplete unit's
 // (O, m, l) go, or null (outputs).
 template <int RG>
 __device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit& x, int t0, int t1, float* part_o,
@@ -518,6 +518,40 @@ __device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit
                 }
             if (w == 0 && lane < (WIDE ? 32 : 16)) a.lse[at] = lse_of(m, l);
         }
+    }
+}
+
+// What becomes of a row block's outputs (the dims 128 w .. + 127 of row R of a unit of 32 RB rows, 32x32 layout): a part, or the outputs
+// at row `at` of the call's if it is one.
+template <int RB, typename Out>
+__device__ __forceinline__ void finish_rows(const Chunk8Args& a, int64_t at, bool live, int row, int rb, int w, int lane, float m, float l,
+                                            Out&& o, float* part_o, float* part_ml) {
+    if (part_o) {
+        // accumulator order: [wave][dim block][row block][4][64 lanes][4]
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const f32x4_t v = {o(d)[4 * q], o(d)[4 * q + 1], o(d)[4 * q + 2], o(d)[4 * q + 3]};
+                *reinterpret_cast<f32x4_t*>(part_o + ((((w * 4 + d) * RB + rb) * 4 + q) * 64 + lane) * 4) = v;
+            }
+        if (w == 0 && lane < 32) {
+            part_ml[2 * row] = m;
+            part_ml[2 * row + 1] = l;
+        }
+    } else if (live) {
+        const bool none = m == -INFINITY && l == 0.f;
+        const float inv = none ? 0.f : 1.0f / l;
+        uint16_t* out = a.out + at * D_LAT + 128 * w + 4 * (lane >> 5);
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const bf16x4_t v = {(__bf16)(o(d)[4 * q] * inv), (__bf16)(o(d)[4 * q + 1] * inv), (__bf16)(o(d)[4 * q + 2] * inv),
+                                    (__bf16)(o(d)[4 * q + 3] * inv)};
+                *reinterpret_cast<bf16x4_t*>(out + 32 * d + 8 * q) = v;
+            }
+        if (w == 0 && lane < 32) a.lse[at] = lse_of(m, l);
     }
 }
 
@@ -876,34 +910,226 @@ __device__ __forceinline__ void chunk8_big_segment(const Chunk8Args& a, const Ck
 #pragma unroll
     for (int rb = 0; rb < 4; ++rb) {
         const int row = 32 * rb + c, R = x.row0 + row;
-        const float m = ml[2 * row], sum = ml[2 * row + 1];
-        if (part_o) {
+        finish_rows<4>(a, x.tok0 * a.H + R, R < x.nrow, row, rb, w, lane, ml[2 * row], ml[2 * row + 1], [&](int d) -> const f32x16_t& { return z.o[d][rb]; }, part_o, part_ml);
+    }
+}
+
+// ------------------------------------------------- a segment of a unit of 64 rows
+
+// Scores by rows as for 128, 16 of them a wave; there are registers enough for the compiler to hold everything, and a tile's
+// scores and outputs follow each other.
+constexpr int M8_OFF_SCALE = C8_OFF_TOP, M8_OFF_ALPHA = M8_OFF_SCALE + 4 * C8_TILE;   // [64] scales, [64] factors of the outputs
+
+__device__ __forceinline__ void chunk8_mid_segment(const Chunk8Args& a, const CkUnit& x, int t0, int t1, float* part_o,
+                                                   float* part_ml, uint8_t* smem) {
+    const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t lds0 = lds_addr(smem);
+    const int Rc = min(x.row0 + 16 * w + c, x.nrow - 1);        // rows past the end repeat the last one, never stored
+    const int lim = min(x.old + Rc / a.H, x.kv - 1);            // the last cache row that this lane's row sees
+    const int lim_lo = __builtin_amdgcn_readfirstlane(min(x.old + min(x.row0 + 16 * w, x.nrow - 1) / a.H, x.kv - 1));
+    const int nt = x.kv > 0 ? t1 - t0 : 0;
+
+    Loader8 loader{a, (const_i32_t*)(a.table + (int64_t)x.b * a.tstride), x.kv, w, lane, {}};
+    const int pg = 9 * (g & 1) ^ 16 * (g >> 1);                 // pieces of a key, as for fewer rows
+    bf16x8_t qf[18];
+    {
+        const int64_t row = x.tok0 * a.H + Rc;
+        const uint16_t* ql = a.q_lat + row * a.qls;
+        const uint16_t* qr = a.q_rope + row * a.qrs + 8 * g;
 #pragma unroll
-            for (int d = 0; d < 4; ++d)
+        for (int s = 0; s < 16; ++s) qf[s] = *reinterpret_cast<const bf16x8_t*>(ql + 16 * ((s >> 1) ^ pg) + 8 * (s & 1));
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const f32x4_t v = {z.o[d][rb][4 * q], z.o[d][rb][4 * q + 1], z.o[d][rb][4 * q + 2], z.o[d][rb][4 * q + 3]};
-                    *reinterpret_cast<f32x4_t*>(part_o + ((((w * 4 + d) * 4 + rb) * 4 + q) * 64 + lane) * 4) = v;
-                }
-            if (w == 0 && h == 0) {
-                part_ml[2 * row] = m;
-                part_ml[2 * row + 1] = sum;
-            }
-        } else if (R < x.nrow) {
-            const int64_t at = x.tok0 * a.H + R;
-            const bool none = m == -INFINITY && sum == 0.f;
-            const float inv = none ? 0.f : 1.0f / sum;
-            uint16_t* out = a.out + at * D_LAT + 128 * w + 4 * h;
-#pragma unroll
-            for (int d = 0; d < 4; ++d)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const bf16x4_t v = {(__bf16)(z.o[d][rb][4 * q] * inv), (__bf16)(z.o[d][rb][4 * q + 1] * inv),
-                                        (__bf16)(z.o[d][rb][4 * q + 2] * inv), (__bf16)(z.o[d][rb][4 * q + 3] * inv)};
-                    *reinterpret_cast<bf16x4_t*>(out + 32 * d + 8 * q) = v;
-                }
-            if (w == 0 && h == 0) a.lse[at] = lse_of(m, sum);
+        for (int s = 0; s < 2; ++s) qf[16 + s] = *reinterpret_cast<const bf16x8_t*>(qr + 32 * s);
+    }
+    if (nt > 0) {
+        loader.fetch(t0);
+        loader.issue(t0, smem, lds0, 0);
+        loader.fetch(t0 + 1);
+        if (nt > 1) {
+            loader.issue(t0 + 1, smem, lds0, 1);
+            loader.fetch(t0 + 2);
         }
+    }
+#pragma unroll
+    for (int s = 0; s < 18; ++s) asm volatile("" : "+v"(qf[s]));   // no wait for them inside the tile loop
+
+    f32x16_t o[4][2];   // [dim block][row block]
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][r][i] = 0.f;
+    float m_run = -INFINITY, l_run = 0.f;
+
+    int sg = 0;   // the stage of tile k
+    for (int k = 0; k < nt; ++k) {
+        if (k + 1 < nt)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(Loader8::LOADS) : "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        lds_barrier();
+        if (k + 2 < nt) loader.issue(t0 + k + 2, smem, lds0, sg == 0 ? 2 : sg - 1);
+        const int u0 = C8_TILE * (t0 + k);
+        const uint32_t st = lds0 + C8_OFF_STAGE + sg * C8_STAGE;
+        const uint32_t wn = lds0 + C8_OFF_WORD + (sg * C8_TILE + lane) * 4;
+        sg = sg == 2 ? 0 : sg + 1;
+
+        // ---- scores of the 64 rows of the tile: s4[b][i] is row 16 b + 4 g + i
+        uint32_t word = lds_read_u1(wn), note = lds_read_u1(wn + (C8_OFF_NOTE - C8_OFF_WORD));
+        const uint32_t ka = st + c * D_LAT + ((16 * pg) ^ (16 * code_xor(c)));
+        const uint32_t ra = st + C8_OFF_ROPE + c * (2 * D_ROPE) + 16 * (g ^ rope_xor(c));
+        constexpr int SD = 2;          // operands read ahead of the matrix cores, of the tile's four row blocks: 8 of codes, 2 of the branch
+        u32x4_t kc[SD + 1][4];
+        auto kload = [&](auto sc_) {
+            constexpr int s = decltype(sc_)::value;
+            static_for<0, 4>([&](auto bc) {
+                constexpr int b = decltype(bc)::value;
+                if constexpr (s < 8) kc[s % (SD + 1)][b] = lds_read_u4<16 * D_LAT * b>(ka ^ (16 * s));
+                else kc[s % (SD + 1)][b] = lds_read_u4<16 * 2 * D_ROPE * b>(ra ^ (64 * (s - 8)));
+            });
+        };
+        static_for<0, SD>(kload);
+        lds_wait<4 * SD>(word, note);
+        const float sc = scale_of(word, note);                  // of tile row `lane`
+        const uint64_t absent = __ballot(sc == 0.f);
+        lds_write_u1(lds0 + M8_OFF_SCALE + 4 * lane, __float_as_uint(sc));   // (every wave writes the same ones)
+        float sk[4];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) sk[b] = __shfl(sc, 16 * b + c);
+        f32x4_t s4[4];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) s4[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        static_for<0, 10>([&](auto sc_) {
+            constexpr int s = decltype(sc_)::value;
+            if constexpr (s + SD < 10) kload(std::integral_constant<int, s + SD>{});
+            constexpr int N = 4 * ((s + SD < 10) ? SD : 9 - s);
+            lds_wait<N>(kc[s % (SD + 1)][0], kc[s % (SD + 1)][1]);
+            lds_wait<N>(kc[s % (SD + 1)][2], kc[s % (SD + 1)][3]);
+#pragma unroll
+            for (int i = 0; i < (s < 8 ? 2 : 1); ++i)
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    const u32x4_t& v = kc[s % (SD + 1)][b];
+                    if constexpr (s < 8)
+                        s4[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8(v[2 * i], v[2 * i + 1], sk[b]), qf[2 * s + i], s4[b], 0, 0, 0);
+                    else
+                        s4[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, v), qf[8 + s], s4[b], 0, 0, 0);
+                }
+        });
+
+        // ---- weights
+        u32x4_t f[4];                 // the scales of this lane's scores
+        static_for<0, 4>([&](auto bc) { f[decltype(bc)::value] = lds_read_u4<M8_OFF_SCALE + 64 * decltype(bc)::value>(lds0 + 16 * g); });
+        bool bad = false;
+        if (u0 + C8_TILE - 1 > lim_lo || absent != 0) {
+            const int last = lim - u0 - 4 * g;
+            const uint64_t gone = absent >> (4 * g);
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (16 * b + i > last || ((gone >> (16 * b + i)) & 1u)) {
+                        bad |= s4[b][i] != s4[b][i];
+                        s4[b][i] = -INFINITY;
+                    }
+        }
+        float top = s4[0][0];
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top = fmaxf(top, s4[b][i]);
+        top = allreduce_groups(top, [](float p, float q) { return fmaxf(p, q); }) * a.scale_log2;
+        const bool move = top > m_run + C8_SLACK;
+        top += C8_ROOM;
+        const float alpha = move ? __builtin_amdgcn_exp2f(m_run - top) : 1.0f;
+        if (move) m_run = top;
+        l_run *= alpha;
+        const float ref = m_run == -INFINITY ? 0.f : m_run;
+        const uint32_t flags = (__ballot(move) ? 1u : 0u) | (__ballot(bad) ? 2u : 0u);
+        static_for<0, 4>([&](auto bc) { lds_wait<0>(f[decltype(bc)::value]); });
+        static_for<0, 4>([&](auto bc) {
+            constexpr int b = decltype(bc)::value;
+            bf16x4_t p4;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s4[b][i], a.scale_log2, -ref));
+                l_run += p;           // this lane's share of the sum
+                p4[i] = (__bf16)(p * __uint_as_float(f[b][i]));
+            }
+            const int row = 16 * w + c;   // slots of a row: in each 16 of them rows 4 h + (0..3, 8..11) for half h
+            lds_write_u2(lds0 + C8_OFF_P + row * (2 * C8_TILE) + 16 * ((2 * b + (g & 1)) ^ rope_xor(row)) + 8 * (g >> 1),
+                         __builtin_bit_cast(u32x2_t, p4));
+        });
+        if (g == 0) lds_write_u1(lds0 + M8_OFF_ALPHA + (16 * w + c) * 4, __float_as_uint(alpha));
+        if (lane == 0) lds_write_u1(lds0 + C8_OFF_BAD + 4 * w, flags);
+        lds_barrier();
+
+        // ---- outputs, dims 128 w .. + 127
+        u32x4_t fl = lds_read_u4<C8_OFF_BAD>(lds0);
+        lds_wait<0>(fl);
+        const uint32_t any = __builtin_amdgcn_readfirstlane((fl[0] | fl[1]) | (fl[2] | fl[3]));
+        if (any & 1u) {
+#pragma unroll
+            for (int rb = 0; rb < 2; ++rb) {
+                uint32_t al = lds_read_u1(lds0 + M8_OFF_ALPHA + (32 * rb + (lane & 31)) * 4);
+                lds_wait<0>(al);
+#pragma unroll
+                for (int d = 0; d < 4; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        float v = o[d][rb][i];
+                        scale_acc(v, __uint_as_float(al));
+                        o[d][rb][i] = v;
+                    }
+            }
+        }
+        if (any & 2u) clean_tile(st, w, lane);
+        // after the waits for every LDS operation, which would be waits for these scalar loads too
+        if (k + 2 < nt) loader.fetch(t0 + k + 3);
+        u32x4_t pf[4][2];
+        static_for<0, 4>([&](auto sc_) {
+            static_for<0, 2>([&](auto rc) {
+                constexpr int s = decltype(sc_)::value, rb = decltype(rc)::value;
+                pf[s][rb] = lds_read_u4<C8_OFF_P + rb * 32 * 2 * C8_TILE>(lds0 + (lane & 31) * (2 * C8_TILE) +
+                                                                         16 * ((2 * s + (lane >> 5)) ^ rope_xor(lane & 31)));
+            });
+        });
+        const int e = c >> 1, vr = 4 * (lane >> 5) + (e & 3) + 8 * (e >> 2);
+        const uint32_t va = st + vr * D_LAT + 16 * ((8 * w + (g & 1)) ^ code_xor(vr)) + 8 * (lane & 1);
+        constexpr int N = 16, VD = 6;
+        u32x2_t vv[VD + 1];
+        auto vload = [&](auto ic) {
+            constexpr int i = decltype(ic)::value;
+            vv[i % (VD + 1)] = lds_read_tr8<16 * D_LAT * (i >> 2)>(va ^ (32 * (i & 3)));
+        };
+        static_for<0, VD>(vload);
+        static_for<0, N>([&](auto ic) {
+            constexpr int i = decltype(ic)::value, s = i >> 2, d = i & 3;
+            if constexpr (i + VD < N) vload(std::integral_constant<int, i + VD>{});
+            if constexpr (i == 0) static_for<0, 8>([&](auto q) { lds_wait<VD + 1>(pf[decltype(q)::value / 2][decltype(q)::value % 2]); });
+            lds_wait<(i + VD < N) ? VD : N - 1 - i>(vv[i % (VD + 1)]);
+            const bf16x8_t v = decode8(vv[i % (VD + 1)][0], vv[i % (VD + 1)][1], 1.0f);
+#pragma unroll
+            for (int rb = 0; rb < 2; ++rb)
+                o[d][rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8_t, pf[s][rb]), o[d][rb], 0, 0, 0);
+        });
+    }
+
+    // ---- the rows' references and sums, for every wave
+    __syncthreads();
+    float* ml = reinterpret_cast<float*>(smem + C8_OFF_P);   // [row][2]
+    const float l = allreduce_groups(l_run, [](float p, float q) { return p + q; });
+    if (g == 0) {
+        ml[2 * (16 * w + c)] = m_run;
+        ml[2 * (16 * w + c) + 1] = l;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int rb = 0; rb < 2; ++rb) {
+        const int row = 32 * rb + (lane & 31), R = x.row0 + row;
+        finish_rows<2>(a, x.tok0 * a.H + R, R < x.nrow, row, rb, w, lane, ml[2 * row], ml[2 * row + 1], [&](int d) -> const f32x16_t& { return o[d][rb]; }, part_o, part_ml);
     }
 }
 
@@ -915,15 +1141,19 @@ template <int RG>
 __device__ __forceinline__ void segment8(const Chunk8Args& a, const CkUnit& x, int t0, int t1, float* part_o, float* part_ml,
                                          uint8_t* smem) {
     if constexpr (RG == 8) chunk8_big_segment(a, x, t0, t1, part_o, part_ml, smem);
+    else if constexpr (RG == 4) chunk8_mid_segment(a, x, t0, t1, part_o, part_ml, smem);
     else chunk8_segment<RG>(a, x, t0, t1, part_o, part_ml, smem);
 }
 
 // ------------------------------------------------------------------- kernels
 
-// Runs the tiles of all units are cut into: at most one per CU, and no shorter than `streams` tiles.
+// Runs the tiles of all units are cut into: at most one per CU, and as a run costs its tiles and the writing and reading of its
+// part, some sqrt(tiles) of them, twice as many where parts are small.  16 heads over 4 x 8192 rows 20.6 us, 25.0 with half as many
+// runs; 128 heads over 32768 rows 49.1 us, 55.0 with twice as many.
+template <int RG>
 __device__ __forceinline__ int run_count8(const Chunk8Args& a, int total) {
     int len = 1;
-    while (2.0f * (float)len <= 0.25f * sqrtf((float)total)) len *= 2;
+    while (2.0f * (float)len <= (RG <= 2 ? 0.12f : 0.25f) * sqrtf((float)total)) len *= 2;
     return min(max((total + len - 1) / len, 1), a.runs);
 }
 
@@ -933,7 +1163,7 @@ __global__ __launch_bounds__(C8_THREADS, 1) void chunk8_run_kernel(Chunk8Args a)
     __shared__ __align__(1024) uint8_t smem[RG == 8 ? B8_SMEM : C8_SMEM];
     __shared__ int pre[CK_MAX_UNITS];
     const int total = scan_units<C8_TILE, C8_THREADS>(a, ROWS, pre), U = a.B * a.mb;
-    const int n = run_count8(a, total), g = blockIdx.x;
+    const int n = run_count8<RG>(a, total), g = blockIdx.x;
     if (g == 0)   // units without rows: nothing to join
         for (int u = threadIdx.x; u < U; u += C8_THREADS)
             if ((u + 1 < U ? pre[u + 1] : total) == pre[u]) a.span[3 * u] = a.span[3 * u + 1] = 0;
@@ -979,21 +1209,24 @@ __global__ __launch_bounds__(C8_THREADS, 1) void chunk8_unit_kernel(Chunk8Args a
     segment8<RG>(a, x, 0, n, nullptr, nullptr, smem);
 }
 
-// Joins the parts of a unit that several runs cover: block = (unit, 128 float4 of a part, in the order the
-// segments leave them), thread = one of them in every C8J_GROUPS-th part; then the groups join through LDS, in order.
-constexpr int C8J_F = 128, C8J_GROUPS = 4, C8J_THREADS = C8J_F * C8J_GROUPS, C8J_BATCH = 4;
+// Joins the parts of a unit that several runs cover: block = (unit, F float4 of a part, in the order the segments leave them),
+// thread = one of them in every GROUPS-th part; then the groups join through LDS, in order.  Few rows: more groups, as a
+// part is small and the loads' latency what counts.
+constexpr int C8J_THREADS = 512, C8J_BATCH = 4;
 
-__global__ __launch_bounds__(C8J_THREADS) void chunk8_join_kernel(Chunk8Args a, int RG) {
-    __shared__ JoinSum sums[C8J_GROUPS - 1][C8J_F];
-    const int rows = 16 * RG, per = rows * (D_LAT / 4) / C8J_F;
-    const int u = blockIdx.x / per, grp = threadIdx.x / C8J_F;
-    const int f = (blockIdx.x % per) * C8J_F + threadIdx.x % C8J_F, lane = f & 63;
+template <int RG, int F>
+__global__ __launch_bounds__(C8J_THREADS) void chunk8_join_kernel(Chunk8Args a) {
+    constexpr int GROUPS = C8J_THREADS / F, rows = 16 * RG, per = rows * (D_LAT / 4) / F;
+    __shared__ JoinSum sums[GROUPS - 1][F];
+    const int u = blockIdx.x / per, grp = threadIdx.x / F;
+    const int f = (blockIdx.x % per) * F + threadIdx.x % F, lane = f & 63;
     int r, d;   // row of the unit, first dim
-    if (RG == 1) {
+    if constexpr (RG == 1) {
         r = lane & 15;
         d = 16 * (f >> 6) + 4 * (lane >> 4);
     } else {
-        const int rb = RG / 2, q = (f >> 6) & 3, blk = f >> 8;
+        constexpr int rb = RG / 2;
+        const int q = (f >> 6) & 3, blk = f >> 8;
         r = 32 * (blk % rb) + (lane & 31);
         d = 32 * (blk / rb) + 8 * q + 4 * (lane >> 5);
     }
@@ -1004,12 +1237,12 @@ __global__ __launch_bounds__(C8J_THREADS) void chunk8_join_kernel(Chunk8Args a, 
     const bool live = R < x.nrow;
     JoinSum t{-INFINITY, 0.f, f32x4_t{0.f, 0.f, 0.f, 0.f}};
     if (live)
-        for (int s0 = g0 + grp; s0 <= g1; s0 += C8J_GROUPS * C8J_BATCH) {
+        for (int s0 = g0 + grp; s0 <= g1; s0 += GROUPS * C8J_BATCH) {
             float m[C8J_BATCH], l[C8J_BATCH];
             f32x4_t v[C8J_BATCH];
 #pragma unroll
             for (int j = 0; j < C8J_BATCH; ++j) {   // all loads in flight
-                const int run = min(s0 + C8J_GROUPS * j, g1);
+                const int run = min(s0 + GROUPS * j, g1);
                 const int64_t slot = 2 * run + (run == g0 ? late : 0);
                 const float* ml = a.part_ml + slot * (rows * 2) + 2 * r;
                 m[j] = ml[0];
@@ -1018,13 +1251,13 @@ __global__ __launch_bounds__(C8J_THREADS) void chunk8_join_kernel(Chunk8Args a, 
             }
 #pragma unroll
             for (int j = 0; j < C8J_BATCH; ++j)
-                if (s0 + C8J_GROUPS * j <= g1) join_add(t, m[j], l[j], v[j], 1.0f);
+                if (s0 + GROUPS * j <= g1) join_add(t, m[j], l[j], v[j], 1.0f);
         }
-    if (grp > 0) sums[grp - 1][threadIdx.x % C8J_F] = t;
+    if (grp > 0) sums[grp - 1][threadIdx.x % F] = t;
     __syncthreads();
     if (grp > 0 || !live) return;
 #pragma unroll
-    for (int i = 0; i < C8J_GROUPS - 1; ++i) {
+    for (int i = 0; i < GROUPS - 1; ++i) {
         const JoinSum y = sums[i][threadIdx.x];
         join_add(t, y.M, y.L, y.acc, 1.0f);
     }
@@ -1063,7 +1296,11 @@ static hipError_t launch_chunk8_rows(const Chunk8Args& a, const ChunkSplit& sp, 
     hipLaunchKernelGGL((chunk8_run_kernel<RG>), dim3((unsigned)sp.runs), dim3(C8_THREADS), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || sp.runs == 1) return e;
-    hipLaunchKernelGGL(chunk8_join_kernel, dim3((unsigned)(sp.units * 16 * RG * (D_LAT / 4) / C8J_F)), dim3(C8J_THREADS), 0, s, a, RG);
+    // a part in many pieces where few units share the chip (many parts of each), fewer pieces where there are units enough
+    const int F = sp.units * RG <= 16 ? 32 : 128;
+    const dim3 grid((unsigned)(sp.units * 16 * RG * (D_LAT / 4) / F));
+    if (F == 32) hipLaunchKernelGGL((chunk8_join_kernel<RG, 32>), grid, dim3(C8J_THREADS), 0, s, a);
+    else hipLaunchKernelGGL((chunk8_join_kernel<RG, 128>), grid, dim3(C8J_THREADS), 0, s, a);
     return hipGetLastError();
 }
 
