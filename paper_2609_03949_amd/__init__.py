@@ -773,15 +773,17 @@ def rope_apply(ctx: Context, rope: Rope, x: torch.Tensor, pos: torch.Tensor, out
                transposed: bool = False, stream=None):
     """vkv_rope_apply: out = x with dims [first, first + rope.dims) turned by the tokens' positions pos [n] int32; x, out
     [n,H,D] or [n,D] bf16 (any strides but the last), out may be x."""
-    bf = torch.bfloat16
-    if x.dim() not in (2, 3):
-        raise ValueError(f"x must be [n, H, D] or [n, D], got {tuple(x.shape)}")
-    px, po = _typed(x, bf, "x", None, False), _typed(out, bf, "out", x.shape, False)
-    n, H, D = x.shape[0], x.shape[1] if x.dim() == 3 else 1, x.shape[-1]
-    xs, os_ = [_stride(x, 0), _stride(x, 1) if x.dim() == 3 else 0], [_stride(out, 0), _stride(out, 1) if x.dim() == 3 else 0]
+    bf, shape = torch.bfloat16, x.shape
+    heads = len(shape) == 3
+    if not heads and len(shape) != 2:
+        raise ValueError(f"x must be [n, H, D] or [n, D], got {tuple(shape)}")
+    px, po = _typed(x, bf, "x", None, False), _typed(out, bf, "out", shape, False)
+    n, H, D = shape if heads else (shape[0], 1, shape[1])
+    xs, os_ = x.stride(), out.stride()
     ctx.check(ctx.lib.vkv_rope_apply(
-        ctx.handle, rope.ref, px, n, H, D, int(first), xs[0], xs[1], _typed(pos, torch.int32, "pos", (n,)),
-        1 if transposed else 0, po, os_[0], os_[1], _call_stream(ctx, stream, x.get_device(), pos, out)))
+        ctx.handle, rope.ref, px, n, H, D, first, xs[0] if n > 1 else 0, xs[1] if H > 1 else 0,
+        _typed(pos, torch.int32, "pos", (n,)), 1 if transposed else 0, po, os_[0] if n > 1 else 0, os_[1] if H > 1 else 0,
+        _call_stream(ctx, stream, x.get_device(), pos, out)))
 
 
 class Pages8:

@@ -93,6 +93,42 @@ __global__ __launch_bounds__(PO_THREADS) void fork_put_kernel(PoolArgs a, const 
     if (threadIdx.x == 0) a.kv_len[b] = n;
 }
 
+// Both in one workgroup, for few entries (launches are what such a call costs): the sequences' sources and lengths in LDS, then
+// the entries of all of them, thread by thread.
+constexpr int PS_THREADS = 1024, PS_WAVES = PS_THREADS / 64, PS_EACH = POOL_SMALL / PS_THREADS, PS_SEQS = PS_THREADS;
+
+__global__ __launch_bounds__(PS_THREADS) void fork_small_kernel(PoolArgs a, const int32_t* from) {
+    __shared__ int src[PS_SEQS], len[PS_SEQS];      // (src[b] = b: stays)
+    const int tid = threadIdx.x, entries = a.B * a.width;
+    if (tid < a.B) {
+        const int s = from[tid];
+        const bool some = s >= 0 && s < a.B;
+        src[tid] = some ? s : -1;
+        len[tid] = some ? rows_of(a, a.kv_len[s]) : 0;
+    }
+    __syncthreads();
+#pragma unroll 4
+    for (int i = tid; i < entries; i += PS_THREADS) {
+        const int b = i / a.width, j = i - b * a.width, s = src[b];
+        if (s == b) continue;
+        int e = j < (len[b] + a.page - 1) / a.page ? a.table[(int64_t)s * a.tstride + j] : -1;
+        if (names(a, e)) atomicAdd(a.refs + e, 1);
+        else e = -1;
+        a.rows[i] = e;
+    }
+    __syncthreads();
+#pragma unroll 4
+    for (int i = tid; i < entries; i += PS_THREADS) {      // (each thread the entries that it wrote)
+        const int b = i / a.width, j = i - b * a.width;
+        if (src[b] == b) continue;
+        int32_t* t = a.table + (int64_t)b * a.tstride + j;
+        const int e = *t;
+        if (names(a, e)) atomicAdd(a.refs + e, -1);
+        *t = a.rows[i];
+    }
+    if (tid < a.B && src[tid] != tid) a.kv_len[tid] = len[tid];
+}
+
 // -------------------------------------------------------------------- reserve
 
 struct Ask {
@@ -116,11 +152,21 @@ __device__ __forceinline__ Ask ask(const PoolArgs& a, const int32_t* want, int b
     return q;
 }
 
+// what a wave's sequence needs: pages, and whether one of them is for a copy
+__device__ __forceinline__ int needs(const PoolArgs& a, const int32_t* want, int b, bool* shares) {
+    const Ask q = ask(a, want, b);
+    int n = 0;
+    for (int j = q.j0 + (int)(threadIdx.x & 63); j < q.j1; j += 64) n += !names(a, a.table[(int64_t)b * a.tstride + j]);
+    *shares = q.shared >= 0;
+    return wave_sum(n) + *shares;
+}
+
 // pages of each block that are free (or in use, if used), and what each sequence needs
 __global__ __launch_bounds__(PO_THREADS) void pool_count_kernel(PoolArgs a, const int32_t* want, int used) {
     __shared__ int lds[PO_WAVES];
     if ((int)blockIdx.x < a.nb) {
         int n = 0;
+#pragma unroll
         for (int i = 0; i < PO_EACH; ++i) {
             const int64_t p = (int64_t)blockIdx.x * POOL_BLOCK + PO_THREADS * i + threadIdx.x;
             if (p < a.n_pages) n += (a.refs[p] > 0) == (used != 0);
@@ -132,13 +178,11 @@ __global__ __launch_bounds__(PO_THREADS) void pool_count_kernel(PoolArgs a, cons
     }
     const int b = ((int)blockIdx.x - a.nb) * PO_WAVES + (threadIdx.x >> 6), lane = threadIdx.x & 63;
     if (b >= a.B) return;
-    const Ask q = ask(a, want, b);
-    int n = 0;
-    for (int j = q.j0 + lane; j < q.j1; j += 64) n += !names(a, a.table[(int64_t)b * a.tstride + j]);
-    n = wave_sum(n) + (q.shared >= 0);
+    bool shares;
+    const int n = needs(a, want, b, &shares);
     if (lane == 0) {
         a.need[2 * b] = n;
-        a.need[2 * b + 1] = q.shared >= 0;
+        a.need[2 * b + 1] = shares;
     }
 }
 
@@ -163,33 +207,24 @@ __global__ __launch_bounds__(PO_THREADS) void reserve_list_kernel(PoolArgs a) {
     if ((int)blockIdx.x == a.nb - 1 && threadIdx.x == 0) a.head[PO_FREE] = before + a.block[blockIdx.x];
 }
 
-// a wave a sequence: its requests are those from the sum of the sequences' before it on
-__global__ __launch_bounds__(PO_THREADS) void reserve_give_kernel(PoolArgs a, const int32_t* want, int32_t* missing) {
-    const int b = (int)blockIdx.x * PO_WAVES + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (b >= a.B) return;
-    const int have = a.head[PO_FREE];
-    int64_t at = 0;
-    int copy = 0;
-    for (int i = lane; i < b; i += 64) {
-        at += a.need[2 * i];
-        copy += a.need[2 * i + 1];
-    }
-    at = wave_sum(at);
-    copy = wave_sum(copy);
-    Ask q = ask(a, want, b);
-    q.shared = a.need[2 * b + 1] ? q.kv / a.page : -1;   // its entry: the counts change while the call runs
+// One wave's sequence b takes its requests, those from `at` on of all, and its copy, the copy-th; list: the free pages in order.
+__device__ __forceinline__ void give(const PoolArgs& a, const int32_t* want, int b, int64_t at, int copy, bool shares, int have,
+                                     const int32_t* list, int32_t* missing, bool count) {
+    const int lane = threadIdx.x & 63;
+    const Ask q = ask(a, want, b);      // (its shared is not looked at: the counts change while the call runs)
     int lacks = q.absent;
     int32_t* t = a.table + (int64_t)b * a.tstride;
-    if (q.shared >= 0) {
+    if (shares) {
         if (at < have) {
             if (lane == 0) {
-                const int e = t[q.shared], to = a.list[at];
+                int32_t* entry = t + q.kv / a.page;
+                const int e = *entry, to = list[at];
                 a.from[copy] = e;
                 a.to[copy] = to;
-                atomicMax(a.head + PO_PAIRS, copy + 1);
+                if (count) atomicMax(a.head + PO_PAIRS, copy + 1);
                 atomicAdd(a.refs + e, -1);
                 a.refs[to] = 1;
-                t[q.shared] = to;
+                *entry = to;
             }
         } else {
             ++lacks;
@@ -202,7 +237,7 @@ __global__ __launch_bounds__(PO_THREADS) void reserve_give_kernel(PoolArgs a, co
         const int64_t r = at + __popcll(all & ((1ull << lane) - 1));
         const bool got = open && r < have;
         if (got) {
-            const int to = a.list[r];
+            const int to = list[r];
             a.refs[to] = 1;
             t[j + lane] = to;
         }
@@ -210,6 +245,119 @@ __global__ __launch_bounds__(PO_THREADS) void reserve_give_kernel(PoolArgs a, co
         lacks += __popcll(__ballot(open && !got));
     }
     if (lane == 0) missing[b] = lacks;
+}
+// a wave a sequence: its requests are those from the sum of the sequences' before it on
+__global__ __launch_bounds__(PO_THREADS) void reserve_give_kernel(PoolArgs a, const int32_t* want, int32_t* missing) {
+    const int b = (int)blockIdx.x * PO_WAVES + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (b >= a.B) return;
+    int64_t at = 0;
+    int copy = 0;
+    for (int i = lane; i < b; i += 64) {
+        at += a.need[2 * i];
+        copy += a.need[2 * i + 1];
+    }
+    give(a, want, b, wave_sum(at), wave_sum(copy), a.need[2 * b + 1] != 0, a.head[PO_FREE], a.list, missing, true);
+}
+
+// The three launches above in one workgroup, for pools of few pages: ranks in registers, needs and free pages in LDS (launches are
+// what such a call costs: fork and reserve of 4 beams over 2048 rows 26.6 us in six launches, 16.3 in three; of 64 beams over 8192
+// rows 26.1 and 20.1).
+constexpr int PS_SHORT = 8;      // entries up to which a thread looks through its sequence's by itself
+
+// the sum of v over the threads before this one, and over all
+__device__ __forceinline__ int small_before(int v, int* lds, int* total) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    int upto = v;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int t = __shfl_up(upto, d);
+        if (lane >= d) upto += t;
+    }
+    __syncthreads();
+    if (lane == 63) lds[w] = upto;
+    __syncthreads();
+    int s = upto - v, all = 0;
+#pragma unroll
+    for (int i = 0; i < PS_WAVES; ++i) {
+        if (i < w) s += lds[i];
+        all += lds[i];
+    }
+    *total = all;
+    return s;
+}
+
+__global__ __launch_bounds__(PS_THREADS) void reserve_small_kernel(PoolArgs a, const int32_t* want, int32_t* missing) {
+    __shared__ int32_t list[POOL_SMALL];
+    __shared__ int lds[PS_WAVES], need[PS_SEQS], share[PS_SEQS];
+    const int tid = threadIdx.x, w = tid >> 6, p0 = PS_EACH * tid;
+    int32_t refs[PS_EACH];
+#pragma unroll
+    for (int i = 0; i < PS_EACH; ++i) refs[i] = p0 + i < a.n_pages ? a.refs[p0 + i] : 1;
+    // a thread a sequence; those with many entries a wave each, after them
+    Ask q{};
+    q.shared = -1;
+    uint32_t open = 0;               // its entries that name no page
+    if (tid < a.B) {
+        q = ask(a, want, tid);
+        if (q.j1 - q.j0 <= PS_SHORT)
+            for (int j = 0; j < q.j1 - q.j0; ++j) open |= names(a, a.table[(int64_t)tid * a.tstride + q.j0 + j]) ? 0u : 1u << j;
+        need[tid] = __popc(open) + (q.shared >= 0);
+        share[tid] = q.j1 - q.j0 > PS_SHORT;
+    }
+    __syncthreads();
+    for (int b = w; b < a.B; b += PS_WAVES)
+        if (share[b]) {
+            bool shares;
+            const int n = needs(a, want, b, &shares);
+            if ((tid & 63) == 0) need[b] = min(n, POOL_SMALL + 1);   // (more than there are, and sums within 32 bits)
+        }
+    int free = 0, have, copies, most;
+#pragma unroll
+    for (int i = 0; i < PS_EACH; ++i) free += refs[i] <= 0;
+    int r = small_before(free, lds, &have);
+#pragma unroll
+    for (int i = 0; i < PS_EACH; ++i)
+        if (refs[i] <= 0) list[r++] = p0 + i;
+    // (the scan has waited for every wave)
+    const int at = small_before(tid < a.B ? need[tid] : 0, lds, &most), copy = small_before(q.shared >= 0, lds, &copies);
+    const bool wide = tid < a.B && share[tid];
+    __syncthreads();
+    if (tid < a.B) need[tid] = at, share[tid] = !wide ? INT32_MIN : q.shared >= 0 ? copy : -1 - copy;
+    int pairs;
+    (void)small_before(q.shared >= 0 && at < have, lds, &pairs);
+    if (tid == 0) a.head[PO_PAIRS] = pairs;
+    if (tid < a.B && !wide) {
+        int n = at, lacks = q.absent;
+        int32_t* t = a.table + (int64_t)tid * a.tstride;
+        if (q.shared >= 0) {
+            if (n < have) {
+                const int to = list[n];
+                a.from[copy] = q.shared;
+                a.to[copy] = to;
+                atomicAdd(a.refs + q.shared, -1);
+                a.refs[to] = 1;
+                t[q.j0 - 1] = to;
+            } else {
+                ++lacks;
+            }
+            ++n;
+        }
+        for (int j = 0; j < q.j1 - q.j0; ++j)
+            if ((open >> j) & 1u) {
+                if (n < have) {
+                    a.refs[list[n]] = 1;
+                    t[q.j0 + j] = list[n];
+                } else {
+                    ++lacks;
+                }
+                ++n;
+            }
+        missing[tid] = lacks;
+    }
+    for (int b = w; b < a.B; b += PS_WAVES) {
+        const int s = share[b];
+        if (s != INT32_MIN) give(a, want, b, need[b], s < 0 ? -1 - s : s, s >= 0, have, list, missing, false);
+    }
 }
 
 // -------------------------------------------------------------------- compact
@@ -239,6 +387,35 @@ __global__ __launch_bounds__(PO_THREADS) void compact_list_kernel(PoolArgs a, in
         r += u;
     }
     if (blockIdx.x == 0 && threadIdx.x == 0) *used = n;   // where every page is in use, the counting launch has left no pairs
+}
+
+// the count of the pages in use, and the list, in one workgroup, for few pages
+__global__ __launch_bounds__(PS_THREADS) void compact_small_kernel(PoolArgs a, int32_t* used) {
+    __shared__ int lds[PS_WAVES];
+    const int p0 = PS_EACH * threadIdx.x;
+    uint32_t in = 0;
+#pragma unroll
+    for (int i = 0; i < PS_EACH; ++i)
+        if (p0 + i < a.n_pages && a.refs[p0 + i] > 0) in |= 1u << i;
+    int n, r = small_before(__popc(in), lds, &n);   // pages in use, and before p
+#pragma unroll
+    for (int i = 0; i < PS_EACH; ++i) {
+        const int p = p0 + i;
+        if (p >= a.n_pages) break;
+        const bool u = (in >> i) & 1u;
+        if (p == n) a.head[PO_PAIRS] = n - r;
+        if (p >= n) {
+            a.list[p] = u ? n - 1 - r : -1;
+            if (u) a.from[n - 1 - r] = p;
+        } else if (!u) {
+            a.to[p - r] = p;
+        }
+        r += u;
+    }
+    if (threadIdx.x == 0) {
+        if (n >= a.n_pages) a.head[PO_PAIRS] = 0;
+        *used = n;
+    }
 }
 
 // ----------------------------------------------------------------------- copy
@@ -340,6 +517,10 @@ PoolLayout pool_layout(int64_t B, int64_t n_pages, int64_t width) {
 }
 
 hipError_t launch_fork(const PoolArgs& a, const int32_t* from, hipStream_t s) {
+    if (a.B <= PS_SEQS && (int64_t)a.B * a.width <= POOL_SMALL_TABLE) {
+        hipLaunchKernelGGL(fork_small_kernel, dim3(1), dim3(1024), 0, s, a, from);
+        return hipGetLastError();
+    }
     hipLaunchKernelGGL(fork_take_kernel, dim3((unsigned)a.B), dim3(PO_THREADS), 0, s, a, from);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -355,14 +536,19 @@ static int movers(const PoolArgs& a, int64_t pairs) {
 }
 
 hipError_t launch_reserve(const PoolArgs& a, const int32_t* want, int32_t* missing, hipStream_t s) {
-    const int seqs = (a.B + PO_WAVES - 1) / PO_WAVES;
-    hipLaunchKernelGGL(pool_count_kernel, dim3((unsigned)(a.nb + seqs)), dim3(PO_THREADS), 0, s, a, want, 0);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(reserve_list_kernel, dim3((unsigned)a.nb), dim3(PO_THREADS), 0, s, a);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    hipLaunchKernelGGL(reserve_give_kernel, dim3((unsigned)seqs), dim3(PO_THREADS), 0, s, a, want, missing);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+    hipError_t e;
+    if (a.n_pages <= POOL_SMALL && a.B <= PS_SEQS) {
+        hipLaunchKernelGGL(reserve_small_kernel, dim3(1), dim3(PS_THREADS), 0, s, a, want, missing);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    } else {
+        const int seqs = (a.B + PO_WAVES - 1) / PO_WAVES;
+        hipLaunchKernelGGL(pool_count_kernel, dim3((unsigned)(a.nb + seqs)), dim3(PO_THREADS), 0, s, a, want, 0);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+        hipLaunchKernelGGL(reserve_list_kernel, dim3((unsigned)a.nb), dim3(PO_THREADS), 0, s, a);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+        hipLaunchKernelGGL(reserve_give_kernel, dim3((unsigned)seqs), dim3(PO_THREADS), 0, s, a, want, missing);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
     const int n = movers(a, a.B);
     if (n == 0) return hipSuccess;
     hipLaunchKernelGGL(pool_copy_kernel, dim3((unsigned)n), dim3(PO_THREADS), 0, s, a);
@@ -370,11 +556,16 @@ hipError_t launch_reserve(const PoolArgs& a, const int32_t* want, int32_t* missi
 }
 
 hipError_t launch_compact(const PoolArgs& a, int32_t* used, hipStream_t s) {
-    hipLaunchKernelGGL(pool_count_kernel, dim3((unsigned)a.nb), dim3(PO_THREADS), 0, s, a, (const int32_t*)nullptr, 1);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(compact_list_kernel, dim3((unsigned)a.nb), dim3(PO_THREADS), 0, s, a, used);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+    hipError_t e;
+    if (a.n_pages <= POOL_SMALL) {
+        hipLaunchKernelGGL(compact_small_kernel, dim3(1), dim3(PS_THREADS), 0, s, a, used);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    } else {
+        hipLaunchKernelGGL(pool_count_kernel, dim3((unsigned)a.nb), dim3(PO_THREADS), 0, s, a, (const int32_t*)nullptr, 1);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+        hipLaunchKernelGGL(compact_list_kernel, dim3((unsigned)a.nb), dim3(PO_THREADS), 0, s, a, used);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
     const int n = movers(a, a.n_pages / 2);
     const int64_t words = std::max<int64_t>((int64_t)a.B * a.width, a.n_pages);
     const int tables = (int)std::min<int64_t>((words + 4 * PO_THREADS - 1) / (4 * PO_THREADS), 1024);

@@ -379,7 +379,7 @@ struct RopeArgs {
     int64_t n_tok;
     int64_t xts, xhs, ots, ohs;   // token and head strides, elements
     int H, width, first, dims, interleaved, transposed;
-    int parts;             // workgroups of a token
+    int parts, toks;       // workgroups of a token, or tokens of a workgroup
     float magnitude;
     double freq[VKV_ROPE_MAX_DIMS / 2];
 };
@@ -414,6 +414,8 @@ struct PoolLayout {
     size_t head, block, need, list, from, to, rows, total;
 };
 constexpr int POOL_BLOCK = 4096;
+constexpr int POOL_SMALL = 8192;             // pages, and
+constexpr int64_t POOL_SMALL_TABLE = 1 << 13;   // table entries up to which one workgroup does what is not a copy
 PoolLayout pool_layout(int64_t B, int64_t n_pages, int64_t width);
 hipError_t launch_fork(const PoolArgs& a, const int32_t* from, hipStream_t s);
 hipError_t launch_reserve(const PoolArgs& a, const int32_t* want, int32_t* missing, hipStream_t s);
