@@ -752,6 +752,7 @@ typedef struct vkv_pages8 {
  * The rows behind the new ones and every other block keep their bytes.  Tokens past the first max_q of a
  * sequence, tokens whose row would be below 0, and rows on absent pages are not written (the rows that the others take stay
  * those of the whole chunk).  A page that is written may be in one place of one table only (vkv_pages_reserve sees to it).
+ * Pages may not overlap (page_stride at least (page - 1)*row_stride + 640, or row_stride at least n_pages*page_stride).
  * 0 <= n_tok < 2^31, 0 <= max_q <= 2^30; strides multiples of 8, at least 0, pointers 16-byte aligned (cu 4).
  * No atomics: the same inputs give the same bytes.  Allocates nothing; fit for graph capture.
  */

@@ -100,7 +100,7 @@ __global__ __launch_bounds__(W8_THREADS) void write8_kernel(Write8Args a) {
             u32x2_t{code4(v[0], v[1], v[2], v[3]), code4(v[4], v[5], v[6], v[7])};
     }
     if (u0 < first && s > was) {                 // rows that were there before
-        const float g = power(was - s);
+        const float g = power(max(was - s, -126));   // (from 2^-20 on every code becomes 0)
         for (int i = 0; i < NR; ++i) {
             const int u = u0 + w % GW + GW * i;
             if (u >= first) break;

@@ -934,6 +934,10 @@ int vkv_cache8_write(vkv_ctx* ctx, const vkv_pages8* pg, const uint16_t* lat, in
     if (!al4(cu)) return fail(ctx, VKV_E_ALIGN, "cu must be 4-byte aligned");
     if (lat_stride < 0 || lat_stride % 8 || rope_stride < 0 || rope_stride % 8)
         return fail(ctx, VKV_E_ALIGN, "strides %lld, %lld: need multiples of 8, at least 0", (long long)lat_stride, (long long)rope_stride);
+    // the pages lie one behind another, or one within the other's gaps
+    if (pg->n_pages > 1 && (pg->page_stride < VKV_ROW8 || (pg->page_stride < (pg->page - 1) * pg->row_stride + VKV_ROW8 &&
+                                                           pg->row_stride / pg->page_stride < pg->n_pages)))
+        return fail(ctx, VKV_E_SHAPE, "page_stride=%lld: pages overlap", (long long)pg->page_stride);
     const int64_t q = std::min(std::min(max_q, n_tok), pg->max_kv);   // rows that a sequence can take
     if (q == 0) return VKV_OK;
     Write8Args a{};

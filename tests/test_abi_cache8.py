@@ -165,6 +165,8 @@ def test_chunk8_call_refusals(ctx):
 @pytest.mark.parametrize("change,code", PAGES8_BAD + [
     (dict(n_tok=-1), -2), (dict(n_tok=1 << 31), -2), (dict(max_q=-1), -2), (dict(max_q=(1 << 30) + 1), -2), (dict(lat=None), -1),
     (dict(rope=None), -1), (dict(cu=None), -1), (dict(lat=FAKE + 8), -3), (dict(rope=FAKE + 2), -3), (dict(cu=FAKE + 2), -3),
+    (dict(page_stride=0), -2), (dict(page_stride=63 * 640), -2), (dict(page_stride=640), -2), (dict(page_stride=640, row_stride=63 * 640), -2),
+    (dict(page=1, block=1, table_stride=1000, page_stride=624), -2),
     (dict(lat_stride=-8), -3), (dict(lat_stride=513), -3), (dict(rope_stride=68), -3),
     (dict(B=65535, max_kv=1 << 30, table_stride=1 << 24, n_tok=(1 << 31) - 1, max_q=1 << 30), -2),
 ])

@@ -122,6 +122,20 @@ def test_scales_out_of_range_and_nan_among_older_rows(ctx):
         check(ctx, x, *rows(2, 9))
 
 
+@pytest.mark.parametrize("old,new", [(63, 64), (64, 60), (0, 40), (100, 64)])
+def test_scales_that_grow_by_a_lot(ctx, old, new):
+    """From the lowest scale byte to the highest: the older rows' codes become zeros (of their sign), NaN stays."""
+    x = Case8([14], [1], 1, page=16, block=16, seed=10)
+    x.scale[:] = old
+    x.cache[x.where[0][0][2], 2, 7] = 0xFF
+    lat, rope = rows(1, 17)
+    lat[0, 3] = 447 * 2.0 ** new
+    check(ctx, x, lat, rope)
+    p, r = x.where[0]
+    was = x.cache[p[:13], r[:13], :512]
+    assert bool((was[2, 7] == 0xFF) | (was[2, 7] == 0x7F))
+
+
 def test_chunk_past_its_bound_short_sequences_and_absent_pages(ctx):
     x = Case8([90, 3, 40], [10, 6, 20], 1, page=16, block=4, seed=4, behind=3)
     x.table[2, 1] = -1
@@ -141,6 +155,9 @@ def test_strides(ctx):
     x.scale = big[:, 1:5]
     check(ctx, x, both[:, :512], both[:, 512:])
     assert bool((big[:, 0] == 0).all()) and bool((big[:, 5:] == 0).all())
+    z = Case8([90, 61], [40, 6], 1, page=32, block=8, seed=6)
+    z.cache = z.cache.transpose(0, 1).contiguous().transpose(0, 1)      # a page's rows among the other pages'
+    check(ctx, z, both[:, :512], both[:, 512:])
     y = Case8([20], [12], 1, page=16, block=16, seed=7)
     lat, rope = rows(1, 15)
     check(ctx, y, lat.expand(12, 512), rope.expand(12, 64))
