@@ -1133,10 +1133,6 @@ __device__ __forceinline__ void chunk8_mid_segment(const Chunk8Args& a, const Ck
     }
 }
 
-// Floats from one run's part to the next: 1280 bytes more than a part has.  At a run's end every workgroup stores its part at about
-// the same pace; parts a power of two apart would keep all of them at the same few memory channels.
-constexpr int64_t part_stride(int rows) { return (int64_t)rows * D_LAT + 320; }
-
 template <int RG>
 __device__ __forceinline__ void segment8(const Chunk8Args& a, const CkUnit& x, int t0, int t1, float* part_o, float* part_ml,
                                          uint8_t* smem) {
@@ -1190,7 +1186,7 @@ __global__ __launch_bounds__(C8_THREADS, 1) void chunk8_run_kernel(Chunk8Args a)
             if (t1 == next - base) a.span[3 * u + 1] = g;
         }
         const int64_t slot = 2 * g + (at > beg ? 1 : 0);
-        segment8<RG>(a, x, t0, t1, whole ? nullptr : a.part_o + slot * part_stride(ROWS), a.part_ml + slot * (ROWS * 2), smem);
+        segment8<RG>(a, x, t0, t1, whole ? nullptr : a.part_o + slot * (ROWS * D_LAT), a.part_ml + slot * (ROWS * 2), smem);
         __syncthreads();   // the stages are free
         at = base + t1;
         ++u;
@@ -1247,7 +1243,7 @@ __global__ __launch_bounds__(C8J_THREADS) void chunk8_join_kernel(Chunk8Args a) 
                 const float* ml = a.part_ml + slot * (rows * 2) + 2 * r;
                 m[j] = ml[0];
                 l[j] = ml[1];
-                v[j] = *reinterpret_cast<const f32x4_t*>(a.part_o + slot * part_stride(rows) + 4 * f);
+                v[j] = *reinterpret_cast<const f32x4_t*>(a.part_o + slot * (rows * D_LAT) + 4 * f);
             }
 #pragma unroll
             for (int j = 0; j < C8J_BATCH; ++j)
@@ -1280,7 +1276,7 @@ ChunkSplit chunk8_split(int64_t B, int64_t H, int64_t max_q, int64_t max_kv) {
     s.streams = 1;
     if (s.runs) {
         s.runs = std::max<int64_t>(1, std::min<int64_t>(s.runs, tiles));
-        s.part_o = (size_t)(2 * s.runs) * part_stride(16 * s.qg) * 4;
+        s.part_o = (size_t)(2 * s.runs) * 16 * s.qg * D_LAT * 4;
         s.part_ml = (size_t)(2 * s.runs) * 16 * s.qg * 2 * 4;
         s.span = (size_t)s.units * 3 * 4;
     }

@@ -243,3 +243,46 @@ def test_on_another_stream(ctx):
     got = run(ctx, x, stream=s)
     s.synchronize()
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_far_apart(ctx):
+    """Pages and rows whose offsets take more than 32 bits, among them rows too far apart for 32-bit offsets within eight."""
+    x = Case8([150, 64], [1, 3], 16, page=16, block=4, seed=17)
+    want = run(ctx, x)
+    n, page, near = x.cache.shape[0], x.page, x.cache
+    far = torch.empty(6 << 30, dtype=torch.uint8, device=DEV)
+    for rs, ps in ((640, 400 << 20), ((1 << 28) + 640, 1024)):
+        x.cache = far.as_strided((n, page, 640), (ps, rs, 1))
+        x.cache.copy_(near)
+        got = run(ctx, x)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_two_calls_at_once(ctx):
+    """On two streams, each with a workspace of its own."""
+    a, b = Case8([9000, 70], [1, 1], 16, page=64, seed=18), Case8([4000], [2], 128, page=64, seed=19)
+    want = run(ctx, a), run(ctx, b)
+    torch.cuda.synchronize()
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+    got = []
+    for _ in range(3):
+        for x, s in zip((a, b), streams):
+            with torch.cuda.stream(s):
+                got.append(run(ctx, x))
+    torch.cuda.synchronize()
+    for i, g in enumerate(got):
+        assert torch.equal(g[0], want[i % 2][0]) and torch.equal(g[1], want[i % 2][1])
+
+
+def test_very_many_sequences(ctx):
+    """65535 sequences x 257 blocks of rows: 16.8 million workgroups of 256, more than one grid dimension holds."""
+    many, H = 65535, 128
+    x = Case8([60, 33], [2, 1], H, page=64, seed=20)
+    want = run(ctx, x)
+    live = [70, many - 1]
+    table, kv, cu = (torch.full((many, 1), -1, dtype=torch.int32), torch.zeros(many, dtype=torch.int32), torch.zeros(many + 1, dtype=torch.int32))
+    table[live], kv[live] = x.table.cpu(), x.kv_len.cpu()
+    cu[71:], cu[many] = 2, 3
+    x.table, x.kv_len, x.cu, x.max_q = table.to(DEV), kv.to(DEV), cu.to(DEV), 257
+    got = run(ctx, x)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])

@@ -183,3 +183,20 @@ def test_captured_and_on_another_stream(ctx):
     s = torch.cuda.Stream()
     s.wait_stream(torch.cuda.current_stream())
     check(ctx, rope, (64, 10000.0, 0, 1.0, 0, 0, 0), x, pos, inter=True, stream=s)
+
+
+def test_very_many_tokens(ctx):
+    """67 million tokens, four a workgroup: more workgroups of 256 than one grid dimension holds; offsets past 32 bits."""
+    rope = vkv.Rope(256)
+    n = (1 << 26) + 77
+    x = torch.zeros(n, 256, dtype=torch.bfloat16, device=DEV)
+    pos = torch.arange(n, dtype=torch.int32, device=DEV)
+    at = torch.tensor([0, 1, 12345, n // 2, (1 << 23) - 1, 1 << 23, n - 2, n - 1], device=DEV)
+    some = data(8, 1, 256, 4, 99)[0][:, 0]
+    x[at] = some
+    vkv.rope_apply(ctx, rope, x, pos, x)
+    torch.cuda.synchronize()
+    want, tol = turned(some[:, None], pos[at], frequencies(256, 10000.0, vkv.VKV_ROPE_PLAIN, 1.0, 4096.0, 32.0, 1.0), 0, False, 1.0, False)
+    assert bool(((x[at][:, None].double().cpu() - want).abs() <= tol).all())
+    x[at] = 0
+    assert not any(bool(part.any()) for part in x.split(1 << 24))
