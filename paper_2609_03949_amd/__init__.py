@@ -823,12 +823,12 @@ class Pages8:
 def cache8_write(ctx: Context, pages: Pages8, lat: torch.Tensor, rope: torch.Tensor, cu: torch.Tensor, max_q: int, stream=None):
     """vkv_cache8_write: the newest tokens' rows, lat [n,512] and rope [n,64] bf16 (any token stride), cu [B+1] int32, at
     most max_q tokens a sequence, into the cache."""
-    bf = torch.bfloat16
-    n = lat.shape[0]
+    bf, n = torch.bfloat16, lat.shape[0]
+    pl, pr = _typed(lat, bf, "lat", (n, D_LAT), False), _typed(rope, bf, "rope", (n, D_ROPE), False)
+    ls, rs = (lat.stride(0), rope.stride(0)) if n > 1 else (0, 0)
     ctx.check(ctx.lib.vkv_cache8_write(
-        ctx.handle, pages.ref, _typed(lat, bf, "lat", (None, D_LAT), False), _stride(lat, 0),
-        _typed(rope, bf, "rope", (n, D_ROPE), False), _stride(rope, 0), _typed(cu, torch.int32, "cu", (pages.B + 1,)), n,
-        int(max_q), _call_stream(ctx, stream, pages.device, lat, rope, cu)))
+        ctx.handle, pages.ref, pl, ls, pr, rs, _typed(cu, torch.int32, "cu", (pages.B + 1,)), n, int(max_q),
+        _call_stream(ctx, stream, pages.device, lat, rope, cu)))
 
 
 def chunk8_workspace_size(pages: Pages8, chunk: Chunk) -> int:

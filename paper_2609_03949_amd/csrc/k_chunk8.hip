@@ -1268,10 +1268,17 @@ __global__ __launch_bounds__(C8J_THREADS) void chunk8_join_kernel(Chunk8Args a) 
 ChunkSplit chunk8_split(int64_t B, int64_t H, int64_t max_q, int64_t max_kv) {
     ChunkSplit s{};
     const int64_t rows = max_q * H;
-    s.qg = rows <= 16 ? 1 : rows <= 32 ? 2 : rows <= 64 ? 4 : 8;
+    // Rows of a unit.  Many rows: each code is converted once for all of them.  Few rows: more units where the cache alone does not
+    // give every CU some tiles to work through, a start and a part that take less time, and the cache is read again from
+    // nearby.  128 heads, a token each, units of 16, 64 and 128 rows: one sequence of 4096 rows 21, 27, 42 us, of 32768 rows 45,
+    // 36, 57 us; 16 of 32768 rows 426, 198, 179 us.  32 heads, units of 16 and 32 rows: one of 8192 rows 20, 28 us; 4 of 32768
+    // rows 48, 50 us, 16 of them 121, 96 us.
+    const int64_t cache = B * std::max<int64_t>(1, (max_kv + C8_TILE - 1) / C8_TILE);   // tiles
+    const int64_t of16 = (rows + 15) / 16 * cache, of64 = (rows + 63) / 64 * cache;
+    s.qg = rows <= 16 || of16 <= 2048 || (rows <= 32 && of16 <= 4096) ? 1 : rows <= 32 ? 2 : rows <= 64 || of64 <= 8192 ? 4 : 8;
     s.mb = (rows + 16 * s.qg - 1) / (16 * s.qg);
     s.units = B * s.mb;
-    const int64_t tiles = s.units * std::max<int64_t>(1, (max_kv + C8_TILE - 1) / C8_TILE);
+    const int64_t tiles = s.mb * cache;
     s.runs = s.units <= CK_MAX_UNITS && tiles < (1ll << 31) ? CK_RUNS : 0;
     s.streams = 1;
     if (s.runs) {
