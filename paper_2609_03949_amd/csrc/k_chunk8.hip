@@ -105,15 +105,20 @@ __device__ __forceinline__ float scale_of(uint32_t word, uint32_t note) {
     return note == C8_ABSENT ? 0.f : __uint_as_float(s << 23);
 }
 
-// One wave's share of a tile: 16 of its rows, their codes, branch and scale words.
+// One wave's share of a tile of 4 NR rows: NR of them, their codes, branch and scale words.  WORD, NOTE: where the words of all
+// stages are, and what is noted of each.
+template <int NR, int WORD, int NOTE>
 struct Loader8 {
-    static constexpr int NR = 16;
+    static constexpr int TILE = 4 * NR, STAGE = TILE * VKV_ROW8, OFF_ROPE = TILE * D_LAT;
     const Chunk8Args& a;
     const_i32_t* table;
     int kv, wt, lane;
     int32_t e[NR];          // the fetched tile's table entries (scalar)
 
-    __device__ __forceinline__ int row(int t, int i) const { return min(C8_TILE * t + NR * wt + i, kv - 1); }
+    // among 16 rows of the tile, which the XORs go by, NR = 8 are the first or the last
+    __device__ __forceinline__ uint32_t late() const { return NR == 8 ? wt & 1 : 0; }
+
+    __device__ __forceinline__ int row(int t, int i) const { return min(TILE * t + NR * wt + i, kv - 1); }
     __device__ __forceinline__ void fetch(int t) {
         e[0] = table[row(t, 0) >> a.shift];
         if (a.page_mask < NR - 1)
@@ -128,43 +133,43 @@ struct Loader8 {
     static constexpr int LOADS = NR / 2 + NR / 8 + 1;
     template <int J>
     __device__ __forceinline__ void part(int t, uint8_t* smem, uint32_t lds0, int sg, int stages) const {
-        uint8_t* st = smem + stages + sg * C8_STAGE;
+        uint8_t* st = smem + stages + sg * STAGE;
         int ln = lane;
         asm volatile("" : "+v"(ln));   // keeps the lane arithmetic out of registers across the loop
         const uint32_t r = row(t, 0) & a.page_mask, rs = 16 * a.rs16;
         const char* b = reinterpret_cast<const char*>(a.cache8) + 16 * ((uint64_t)(uint32_t)e[0] * a.ps16 + (uint64_t)r * a.rs16);
         if constexpr (J < NR / 2) {             // two rows' codes, half a wave each
             constexpr int i = 2 * J;
-            const uint32_t p16 = (16 * (ln & 31)) ^ (32 * (ln >> 5));
+            const uint32_t p16 = (16 * (ln & 31)) ^ (32 * (ln >> 5)) ^ (128 * late());
             __builtin_amdgcn_global_load_lds((gbl_void_t*)(b + (uint64_t)rs * i + ((p16 ^ (16 * code_xor(i))) + (ln >> 5) * rs)),
                                              (lds_void_t*)(st + D_LAT * (NR * wt + i)), 16, 0, 0);
         } else if constexpr (J < LOADS - 1) {   // eight rows' branch, eight lanes each
             constexpr int i = 8 * (J - NR / 2);
-            const uint32_t q16 = 16 * ((ln & 7) ^ ((ln >> 4) & 3));
+            const uint32_t q16 = 16 * ((ln & 7) ^ ((ln >> 4) & 3)) ^ (64 * late());
             __builtin_amdgcn_global_load_lds((gbl_void_t*)(b + (uint64_t)rs * i + ((q16 ^ (8 * i)) + (ln >> 3) * rs + D_LAT)),
-                                             (lds_void_t*)(st + C8_OFF_ROPE + 2 * D_ROPE * (NR * wt + i)), 16, 0, 0);
+                                             (lds_void_t*)(st + OFF_ROPE + 2 * D_ROPE * (NR * wt + i)), 16, 0, 0);
         } else if (ln < NR) {                   // the aligned words around the scale bytes
             const uint64_t s0 = (uint64_t)(uintptr_t)(a.scale + (uint64_t)(uint32_t)e[0] * (uint64_t)a.sstride);
             const uint32_t at = (uint32_t)(s0 & 3) + ((r + ln) >> a.bshift);
             __builtin_amdgcn_global_load_lds((gbl_void_t*)(uintptr_t)((s0 & ~3ull) + (at & ~3u)),
-                                             (lds_void_t*)(smem + C8_OFF_WORD + (sg * C8_TILE + NR * wt) * 4), 4, 0, 0);
-            lds_write_u1(lds0 + C8_OFF_NOTE + (sg * C8_TILE + NR * wt + ln) * 4, 8u * (at & 3u));
+                                             (lds_void_t*)(smem + WORD + (sg * TILE + NR * wt) * 4), 4, 0, 0);
+            lds_write_u1(lds0 + NOTE + (sg * TILE + NR * wt + ln) * 4, 8u * (at & 3u));
         }
     }
     // the loads of the fetched tile t into stage sg
-    __device__ __forceinline__ void issue(int t, uint8_t* smem, uint32_t lds0, int sg, int stages = C8_OFF_STAGE) const {
+    __device__ __forceinline__ void issue(int t, uint8_t* smem, uint32_t lds0, int sg, int stages) const {
         if (plain(t)) static_for<0, LOADS>([&](auto ic) { part<decltype(ic)::value>(t, smem, lds0, sg, stages); });
         else issue_any(t, smem, lds0, sg, stages);
     }
     __device__ __forceinline__ void issue_any(int t, uint8_t* smem, uint32_t lds0, int sg, int stages) const {
-        uint8_t* st = smem + stages + sg * C8_STAGE;
+        uint8_t* st = smem + stages + sg * STAGE;
         const int u = row(t, 0);
         const char* base[NR];
-        const uint8_t* word;     // this lane's (of 16) scale byte
+        const uint8_t* word;     // this lane's (of NR) scale byte
         uint32_t absent;
         int ln = lane;
         asm volatile("" : "+v"(ln));   // keeps the lane arithmetic out of registers across the loop
-        const int i16 = ln & 15;
+        const int mine = ln & (NR - 1);
         if (a.page_mask >= NR - 1) {   // the rows lie on one page; rows past the end: the last row's
             const int last = min(kv - 1 - u, NR - 1);
             const bool there = (uint32_t)e[0] < (uint32_t)a.n_pages;
@@ -172,7 +177,7 @@ struct Loader8 {
             base[0] = reinterpret_cast<const char*>(a.cache8) + 16 * ((uint64_t)p * a.ps16 + (uint64_t)r * a.rs16);
 #pragma unroll
             for (int i = 1; i < NR; ++i) base[i] = base[i - 1] + (there && i <= last ? 16 * (uint64_t)a.rs16 : 0);
-            word = a.scale + (uint64_t)p * (uint64_t)a.sstride + (there ? (r + (uint32_t)min(i16, last)) >> a.bshift : 0);
+            word = a.scale + (uint64_t)p * (uint64_t)a.sstride + (there ? (r + (uint32_t)min(mine, last)) >> a.bshift : 0);
             absent = there ? 0 : C8_ABSENT;
         } else {
             uint64_t pl = 0;
@@ -183,10 +188,11 @@ struct Loader8 {
                 const bool there = (uint32_t)e[i] < (uint32_t)a.n_pages;
                 const uint32_t p = there ? e[i] : 0, r = there ? row(t, i) & a.page_mask : 0;
                 base[i] = reinterpret_cast<const char*>(a.cache8) + 16 * ((uint64_t)p * a.ps16 + (uint64_t)r * a.rs16);
-                const bool mine = i16 == i;
-                pl = mine ? (uint64_t)p * (uint64_t)a.sstride : pl;
-                rl = mine ? r : rl;
-                absent = mine ? (there ? 0 : C8_ABSENT) : absent;
+                if (mine == i) {
+                    pl = (uint64_t)p * (uint64_t)a.sstride;
+                    rl = r;
+                    absent = there ? 0 : C8_ABSENT;
+                }
             }
             word = a.scale + pl + (rl >> a.bshift);
         }
@@ -194,7 +200,7 @@ struct Loader8 {
 #pragma unroll
         for (int i = 0; i < NR; i += 2) {
             const char* b = hb ? base[i + 1] : base[i];
-            const uint32_t off = 16 * ((uint32_t)(ln & 31) ^ (uint32_t)code_xor(i) ^ (uint32_t)(2 * hb));
+            const uint32_t off = 16 * ((uint32_t)(ln & 31) ^ (uint32_t)code_xor(i) ^ (uint32_t)(2 * hb) ^ (8 * late()));
             __builtin_amdgcn_global_load_lds((gbl_void_t*)(b + off), (lds_void_t*)(st + D_LAT * (NR * wt + i)), 16, 0, 0);
         }
 #pragma unroll
@@ -202,18 +208,20 @@ struct Loader8 {
             const char* b = base[j];
 #pragma unroll
             for (int i = 1; i < 8; ++i) b = (ln >> 3) == i ? base[j + i] : b;
-            const int r = j + (ln >> 3);
+            const int r = j + 8 * (int)late() + (ln >> 3);
             __builtin_amdgcn_global_load_lds((gbl_void_t*)(b + D_LAT + 16 * ((ln & 7) ^ rope_xor(r))),
-                                             (lds_void_t*)(st + C8_OFF_ROPE + 2 * D_ROPE * (NR * wt + j)), 16, 0, 0);
+                                             (lds_void_t*)(st + OFF_ROPE + 2 * D_ROPE * (NR * wt + j)), 16, 0, 0);
         }
         if (ln < NR) {   // the aligned word around the byte
             const uint64_t at = (uint64_t)(uintptr_t)word;
             __builtin_amdgcn_global_load_lds((gbl_void_t*)(uintptr_t)(at & ~3ull),
-                                             (lds_void_t*)(smem + C8_OFF_WORD + (sg * C8_TILE + NR * wt) * 4), 4, 0, 0);
-            lds_write_u1(lds0 + C8_OFF_NOTE + (sg * C8_TILE + NR * wt + ln) * 4, absent ? C8_ABSENT : 8u * (uint32_t)(at & 3u));
+                                             (lds_void_t*)(smem + WORD + (sg * TILE + NR * wt) * 4), 4, 0, 0);
+            lds_write_u1(lds0 + NOTE + (sg * TILE + NR * wt + ln) * 4, absent ? C8_ABSENT : 8u * (uint32_t)(at & 3u));
         }
     }
 };
+
+typedef Loader8<16, C8_OFF_WORD, C8_OFF_NOTE> Loader64;   // tiles of 64 rows
 
 // ------------------------------------------------------------------ a segment
 
@@ -244,7 +252,7 @@ __device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit
     const int lim_lo = __builtin_amdgcn_readfirstlane(min(x.old + x.row0 / a.H, x.kv - 1));
     const int nt = x.kv > 0 ? t1 - t0 : 0;
 
-    Loader8 loader{a, (const_i32_t*)(a.table + (int64_t)x.b * a.tstride), x.kv, w, lane, {}};
+    Loader64 loader{a, (const_i32_t*)(a.table + (int64_t)x.b * a.tstride), x.kv, w, lane, {}};
     // pieces of a key's codes that this lane reads: step s takes piece s ^ 9 (g & 1) ^ 16 (g >> 1), half after half
     const int pg = 9 * (g & 1) ^ 16 * (g >> 1);
     bf16x8_t qf[RG][18];
@@ -263,10 +271,10 @@ __device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit
     }
     if (nt > 0) {
         loader.fetch(t0);
-        loader.issue(t0, smem, lds0, 0);
+        loader.issue(t0, smem, lds0, 0, C8_OFF_STAGE);
         loader.fetch(t0 + 1);
         if (nt > 1) {
-            loader.issue(t0 + 1, smem, lds0, 1);
+            loader.issue(t0 + 1, smem, lds0, 1, C8_OFF_STAGE);
             loader.fetch(t0 + 2);
         }
     }
@@ -290,12 +298,12 @@ __device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit
     for (int k = 0; k < nt; ++k) {
         // this wave's share of tile k has landed, and every wave's; what was read of tile k - 1 and its weights has been used
         if (k + 1 < nt)
-            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(Loader8::LOADS) : "memory");
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(Loader64::LOADS) : "memory");
         else
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         lds_barrier();
         if (k + 2 < nt) {
-            loader.issue(t0 + k + 2, smem, lds0, sg == 0 ? 2 : sg - 1);
+            loader.issue(t0 + k + 2, smem, lds0, sg == 0 ? 2 : sg - 1, C8_OFF_STAGE);
         }
         const int u0 = C8_TILE * (t0 + k);
         const uint32_t st = lds0 + C8_OFF_STAGE + sg * C8_STAGE;
@@ -757,7 +765,7 @@ __device__ __forceinline__ void chunk8_big_segment(const Chunk8Args& a, const Ck
     const int lim_lo = __builtin_amdgcn_readfirstlane(min(x.old + first / a.H, x.kv - 1));
     const int nt = x.kv > 0 ? t1 - t0 : 0;
 
-    Loader8 loader{a, (const_i32_t*)(a.table + (int64_t)x.b * a.tstride), x.kv, w, lane, {}};
+    Loader64 loader{a, (const_i32_t*)(a.table + (int64_t)x.b * a.tstride), x.kv, w, lane, {}};
     Big8 z;
     {
         const int64_t row = x.tok0 * a.H + Rc;
@@ -850,7 +858,7 @@ __device__ __forceinline__ void chunk8_big_segment(const Chunk8Args& a, const Ck
 
     if (nt > 0) {
         if (nt > 1)
-            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(Loader8::LOADS) : "memory");
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(Loader64::LOADS) : "memory");
         else
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         lds_barrier();
@@ -914,23 +922,50 @@ __device__ __forceinline__ void chunk8_big_segment(const Chunk8Args& a, const Ck
     }
 }
 
-// ------------------------------------------------- a segment of a unit of 64 rows
+// --------------------------------------------- a segment of a unit of 32 or 64 rows
 
-// Scores by rows as for 128, 16 of them a wave; there are registers enough for the compiler to hold everything, and a tile's
-// scores and outputs follow each other.
-constexpr int M8_OFF_SCALE = C8_OFF_TOP, M8_OFF_ALPHA = M8_OFF_SCALE + 4 * C8_TILE;   // [64] scales, [64] factors of the outputs
+// Eight waves, two a SIMD: four take scores and weights, 16 rows of the unit each (and no others, so that a reference is one wave's
+// own), four the outputs, 128 dims each, of the tile before; so a SIMD's vector units convert and weigh for one while its
+// matrix cores work for the other.  Tiles of 32 rows, seven in LDS: five on their way while two are used.
+constexpr int M8_TILE = 32, M8_THREADS = 512, M8_STAGES = 7;
+constexpr int M8_OFF_WORD = 0, M8_OFF_NOTE = M8_OFF_WORD + M8_STAGES * M8_TILE * 4;
+constexpr int M8_OFF_SCALE = M8_OFF_NOTE + M8_STAGES * M8_TILE * 4;   // [32] the tile's scales (every wave writes the same ones)
+constexpr int M8_OFF_ALPHA = M8_OFF_SCALE + 4 * M8_TILE;              // two of [64]: by what a row's outputs are to be multiplied
+constexpr int M8_OFF_BAD = M8_OFF_ALPHA + 2 * 256;                    // two of [4]: the waves' flags, outputs to multiply, a hidden NaN
+constexpr int M8_OFF_P = 3072, M8_P = 64 * 2 * M8_TILE;               // weights of a tile, [64][32] bf16; two of them
+constexpr int M8_OFF_STAGE = M8_OFF_P + 2 * M8_P;
+typedef Loader8<8, M8_OFF_WORD, M8_OFF_NOTE> Loader32;
+constexpr int M8_SMEM = M8_OFF_STAGE + M8_STAGES * Loader32::STAGE;
+static_assert(M8_OFF_BAD + 32 <= M8_OFF_P && M8_OFF_STAGE % 1024 == 0 && Loader32::TILE == M8_TILE, "");
 
-__device__ __forceinline__ void chunk8_mid_segment(const Chunk8Args& a, const CkUnit& x, int t0, int t1, float* part_o,
-                                                   float* part_ml, uint8_t* smem) {
-    const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
-    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const uint32_t lds0 = lds_addr(smem);
+// XOR of the 16-byte piece index within the 64 bytes of a row's weights: 16 rows' reads of a piece differ modulo 256 bytes
+__device__ __forceinline__ int weight_xor(int r) { return (r >> 2) & 3; }
+
+// The dims 128 w .. + 127 of a tile (at st), which this wave alone reads any more, without NaN codes (as clean_tile).
+__device__ __attribute__((noinline)) void clean_dims(uint32_t st, int w, int lane) {
+    for (int i = 0; i < M8_TILE; i += 8) {
+        const int r = i + (lane >> 3);
+        const uint32_t at = st + r * D_LAT + 16 * ((8 * w + (lane & 7)) ^ code_xor(r & 15));
+        u32x4_t v = lds_read_u4<0>(at);
+        lds_wait<0>(v);
+        for (int q = 0; q < 4; ++q) v[q] = drop_nan(v[q]);
+        lds_write_u4(at, v);
+    }
+}
+
+// Scores and weights of a segment's tiles by the rows 16 w .. + 15 of unit x.
+template <int RG>
+__device__ __forceinline__ void mid_scores(const Chunk8Args& a, const CkUnit& x, int t0, int nt, uint32_t lds0, int w, int lane, float& m_run,
+                                           float& l_run) {
+    const int c = lane & 15, g = lane >> 4;
+    if (w >= RG || x.row0 + 16 * w >= x.nrow) {                 // no rows: nothing to say
+        if (lane < 2) lds_write_u1(lds0 + M8_OFF_BAD + 16 * lane + 4 * w, 0);
+        for (int k = -1; k < nt; ++k) lds_barrier();
+        return;
+    }
     const int Rc = min(x.row0 + 16 * w + c, x.nrow - 1);        // rows past the end repeat the last one, never stored
     const int lim = min(x.old + Rc / a.H, x.kv - 1);            // the last cache row that this lane's row sees
-    const int lim_lo = __builtin_amdgcn_readfirstlane(min(x.old + min(x.row0 + 16 * w, x.nrow - 1) / a.H, x.kv - 1));
-    const int nt = x.kv > 0 ? t1 - t0 : 0;
-
-    Loader8 loader{a, (const_i32_t*)(a.table + (int64_t)x.b * a.tstride), x.kv, w, lane, {}};
+    const int lim_lo = __builtin_amdgcn_readfirstlane(min(x.old + (x.row0 + 16 * w) / a.H, x.kv - 1));
     const int pg = 9 * (g & 1) ^ 16 * (g >> 1);                 // pieces of a key, as for fewer rows
     bf16x8_t qf[18];
     {
@@ -942,75 +977,51 @@ __device__ __forceinline__ void chunk8_mid_segment(const Chunk8Args& a, const Ck
 #pragma unroll
         for (int s = 0; s < 2; ++s) qf[16 + s] = *reinterpret_cast<const bf16x8_t*>(qr + 32 * s);
     }
-    if (nt > 0) {
-        loader.fetch(t0);
-        loader.issue(t0, smem, lds0, 0);
-        loader.fetch(t0 + 1);
-        if (nt > 1) {
-            loader.issue(t0 + 1, smem, lds0, 1);
-            loader.fetch(t0 + 2);
-        }
-    }
 #pragma unroll
-    for (int s = 0; s < 18; ++s) asm volatile("" : "+v"(qf[s]));   // no wait for them inside the tile loop
-
-    f32x16_t o[4][2];   // [dim block][row block]
-#pragma unroll
-    for (int d = 0; d < 4; ++d)
-#pragma unroll
-        for (int r = 0; r < 2; ++r)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[d][r][i] = 0.f;
-    float m_run = -INFINITY, l_run = 0.f;
+    for (int s = 0; s < 18; ++s) asm volatile("" : "+a"(qf[s]));   // no wait for them inside the tile loop
 
     int sg = 0;   // the stage of tile k
     for (int k = 0; k < nt; ++k) {
-        if (k + 1 < nt)
-            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(Loader8::LOADS) : "memory");
-        else
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         lds_barrier();
-        if (k + 2 < nt) loader.issue(t0 + k + 2, smem, lds0, sg == 0 ? 2 : sg - 1);
-        const int u0 = C8_TILE * (t0 + k);
-        const uint32_t st = lds0 + C8_OFF_STAGE + sg * C8_STAGE;
-        const uint32_t wn = lds0 + C8_OFF_WORD + (sg * C8_TILE + lane) * 4;
-        sg = sg == 2 ? 0 : sg + 1;
+        const int u0 = M8_TILE * (t0 + k);
+        const uint32_t st = lds0 + M8_OFF_STAGE + sg * Loader32::STAGE;
+        const uint32_t wn = lds0 + M8_OFF_WORD + (sg * M8_TILE + (lane & 31)) * 4;
+        sg = sg == M8_STAGES - 1 ? 0 : sg + 1;
 
-        // ---- scores of the 64 rows of the tile: s4[b][i] is row 16 b + 4 g + i
-        uint32_t word = lds_read_u1(wn), note = lds_read_u1(wn + (C8_OFF_NOTE - C8_OFF_WORD));
+        // ---- scores of the 32 rows of the tile: s4[b][i] is row 16 b + 4 g + i
+        uint32_t word = lds_read_u1(wn), note = lds_read_u1(wn + (M8_OFF_NOTE - M8_OFF_WORD));
         const uint32_t ka = st + c * D_LAT + ((16 * pg) ^ (16 * code_xor(c)));
-        const uint32_t ra = st + C8_OFF_ROPE + c * (2 * D_ROPE) + 16 * (g ^ rope_xor(c));
-        constexpr int SD = 2;          // operands read ahead of the matrix cores, of the tile's four row blocks: 8 of codes, 2 of the branch
-        u32x4_t kc[SD + 1][4];
+        const uint32_t ra = st + Loader32::OFF_ROPE + c * (2 * D_ROPE) + 16 * (g ^ rope_xor(c));
+        constexpr int SD = 3;          // operands read ahead of the matrix cores, of the tile's two row blocks: 8 of codes, 2 of the branch
+        u32x4_t kc[SD + 1][2];
         auto kload = [&](auto sc_) {
             constexpr int s = decltype(sc_)::value;
-            static_for<0, 4>([&](auto bc) {
+            static_for<0, 2>([&](auto bc) {
                 constexpr int b = decltype(bc)::value;
                 if constexpr (s < 8) kc[s % (SD + 1)][b] = lds_read_u4<16 * D_LAT * b>(ka ^ (16 * s));
                 else kc[s % (SD + 1)][b] = lds_read_u4<16 * 2 * D_ROPE * b>(ra ^ (64 * (s - 8)));
             });
         };
         static_for<0, SD>(kload);
-        lds_wait<4 * SD>(word, note);
-        const float sc = scale_of(word, note);                  // of tile row `lane`
-        const uint64_t absent = __ballot(sc == 0.f);
-        lds_write_u1(lds0 + M8_OFF_SCALE + 4 * lane, __float_as_uint(sc));   // (every wave writes the same ones)
-        float sk[4];
+        lds_wait<2 * SD>(word, note);
+        const float sc = scale_of(word, note);                  // of tile row `lane` & 31
+        const uint32_t absent = (uint32_t)__ballot(sc == 0.f);
+        if (lane < M8_TILE) lds_write_u1(lds0 + M8_OFF_SCALE + 4 * lane, __float_as_uint(sc));
+        float sk[2];
 #pragma unroll
-        for (int b = 0; b < 4; ++b) sk[b] = __shfl(sc, 16 * b + c);
-        f32x4_t s4[4];
+        for (int b = 0; b < 2; ++b) sk[b] = __shfl(sc, 16 * b + c);
+        f32x4_t s4[2];
 #pragma unroll
-        for (int b = 0; b < 4; ++b) s4[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int b = 0; b < 2; ++b) s4[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         static_for<0, 10>([&](auto sc_) {
             constexpr int s = decltype(sc_)::value;
             if constexpr (s + SD < 10) kload(std::integral_constant<int, s + SD>{});
-            constexpr int N = 4 * ((s + SD < 10) ? SD : 9 - s);
+            constexpr int N = 2 * ((s + SD < 10) ? SD : 9 - s);
             lds_wait<N>(kc[s % (SD + 1)][0], kc[s % (SD + 1)][1]);
-            lds_wait<N>(kc[s % (SD + 1)][2], kc[s % (SD + 1)][3]);
 #pragma unroll
             for (int i = 0; i < (s < 8 ? 2 : 1); ++i)
 #pragma unroll
-                for (int b = 0; b < 4; ++b) {
+                for (int b = 0; b < 2; ++b) {
                     const u32x4_t& v = kc[s % (SD + 1)][b];
                     if constexpr (s < 8)
                         s4[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8(v[2 * i], v[2 * i + 1], sk[b]), qf[2 * s + i], s4[b], 0, 0, 0);
@@ -1019,15 +1030,15 @@ __device__ __forceinline__ void chunk8_mid_segment(const Chunk8Args& a, const Ck
                 }
         });
 
-        // ---- weights
-        u32x4_t f[4];                 // the scales of this lane's scores
-        static_for<0, 4>([&](auto bc) { f[decltype(bc)::value] = lds_read_u4<M8_OFF_SCALE + 64 * decltype(bc)::value>(lds0 + 16 * g); });
+        // ---- weights, into buffer k & 1
+        u32x4_t f[2];                 // the scales of this lane's scores
+        static_for<0, 2>([&](auto bc) { f[decltype(bc)::value] = lds_read_u4<M8_OFF_SCALE + 64 * decltype(bc)::value>(lds0 + 16 * g); });
         bool bad = false;
-        if (u0 + C8_TILE - 1 > lim_lo || absent != 0) {
+        if (u0 + M8_TILE - 1 > lim_lo || absent != 0) {
             const int last = lim - u0 - 4 * g;
-            const uint64_t gone = absent >> (4 * g);
+            const uint32_t gone = absent >> (4 * g);
 #pragma unroll
-            for (int b = 0; b < 4; ++b)
+            for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     if (16 * b + i > last || ((gone >> (16 * b + i)) & 1u)) {
@@ -1037,7 +1048,7 @@ __device__ __forceinline__ void chunk8_mid_segment(const Chunk8Args& a, const Ck
         }
         float top = s4[0][0];
 #pragma unroll
-        for (int b = 0; b < 4; ++b)
+        for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int i = 0; i < 4; ++i) top = fmaxf(top, s4[b][i]);
         top = allreduce_groups(top, [](float p, float q) { return fmaxf(p, q); }) * a.scale_log2;
@@ -1048,8 +1059,9 @@ __device__ __forceinline__ void chunk8_mid_segment(const Chunk8Args& a, const Ck
         l_run *= alpha;
         const float ref = m_run == -INFINITY ? 0.f : m_run;
         const uint32_t flags = (__ballot(move) ? 1u : 0u) | (__ballot(bad) ? 2u : 0u);
-        static_for<0, 4>([&](auto bc) { lds_wait<0>(f[decltype(bc)::value]); });
-        static_for<0, 4>([&](auto bc) {
+        lds_wait<0>(f[0], f[1]);
+        const int row = 16 * w + c;
+        static_for<0, 2>([&](auto bc) {
             constexpr int b = decltype(bc)::value;
             bf16x4_t p4;
 #pragma unroll
@@ -1058,22 +1070,72 @@ __device__ __forceinline__ void chunk8_mid_segment(const Chunk8Args& a, const Ck
                 l_run += p;           // this lane's share of the sum
                 p4[i] = (__bf16)(p * __uint_as_float(f[b][i]));
             }
-            const int row = 16 * w + c;   // slots of a row: in each 16 of them rows 4 h + (0..3, 8..11) for half h
-            lds_write_u2(lds0 + C8_OFF_P + row * (2 * C8_TILE) + 16 * ((2 * b + (g & 1)) ^ rope_xor(row)) + 8 * (g >> 1),
+            // slots of a row: in each 16 of them rows 4 h + (0..3, 8..11) for half h
+            lds_write_u2(lds0 + M8_OFF_P + M8_P * (k & 1) + row * (2 * M8_TILE) + 16 * ((2 * b + (g & 1)) ^ weight_xor(row)) + 8 * (g >> 1),
                          __builtin_bit_cast(u32x2_t, p4));
         });
-        if (g == 0) lds_write_u1(lds0 + M8_OFF_ALPHA + (16 * w + c) * 4, __float_as_uint(alpha));
-        if (lane == 0) lds_write_u1(lds0 + C8_OFF_BAD + 4 * w, flags);
-        lds_barrier();
+        if (g == 0) lds_write_u1(lds0 + M8_OFF_ALPHA + 256 * (k & 1) + row * 4, __float_as_uint(alpha));
+        if (lane == 0) lds_write_u1(lds0 + M8_OFF_BAD + 16 * (k & 1) + 4 * w, flags);
+    }
+    lds_barrier();
+}
 
-        // ---- outputs, dims 128 w .. + 127
-        u32x4_t fl = lds_read_u4<C8_OFF_BAD>(lds0);
-        lds_wait<0>(fl);
-        const uint32_t any = __builtin_amdgcn_readfirstlane((fl[0] | fl[1]) | (fl[2] | fl[3]));
-        if (any & 1u) {
+// Loads of a segment's tiles, and the outputs' dims 128 w .. + 127 of all the unit's rows.
+template <int RB>
+__device__ __forceinline__ void mid_outputs(const Chunk8Args& a, const CkUnit& x, int t0, int nt, uint8_t* smem, uint32_t lds0, int w, int lane,
+                                            f32x16_t (&o)[4][RB]) {
+    Loader32 loader{a, (const_i32_t*)(a.table + (int64_t)x.b * a.tstride), x.kv, w, lane, {}};
+    constexpr int FIRST = M8_STAGES - 2;
+    {
+        Loader32 first[FIRST] = {loader, loader, loader, loader, loader};
+        static_assert(FIRST == 5, "");
 #pragma unroll
-            for (int rb = 0; rb < 2; ++rb) {
-                uint32_t al = lds_read_u1(lds0 + M8_OFF_ALPHA + (32 * rb + (lane & 31)) * 4);
+        for (int i = 0; i < FIRST; ++i)
+            if (i < nt) first[i].fetch(t0 + i);
+        loader.fetch(t0 + FIRST);
+#pragma unroll
+        for (int i = 0; i < FIRST; ++i)
+            if (i < nt) first[i].issue(t0 + i, smem, lds0, i, M8_OFF_STAGE);
+    }
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int r = 0; r < RB; ++r)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][r][i] = 0.f;
+
+    // tile k + 1 has landed; the weights of tile k are there, and nobody reads tile k - 1 any more: tile k + 6 goes into its place
+    auto turn = [&](int k, int sg) __attribute__((always_inline)) {
+        if (k + 5 < nt)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * Loader32::LOADS) : "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        lds_barrier();
+        if (k + 6 < nt) loader.issue(t0 + k + 6, smem, lds0, sg, M8_OFF_STAGE);
+    };
+    turn(-1, FIRST);
+    if (FIRST + 1 < nt) loader.fetch(t0 + FIRST + 1);
+    int sg = 0;   // the stage of tile k
+    for (int k = 0; k < nt; ++k) {
+        turn(k, sg == 0 ? M8_STAGES - 1 : sg - 1);
+        const uint32_t st = lds0 + M8_OFF_STAGE + sg * Loader32::STAGE;
+        sg = sg == M8_STAGES - 1 ? 0 : sg + 1;
+        const int r = lane & 31, hh = lane >> 5;
+        const uint32_t pr = lds0 + M8_OFF_P + M8_P * (k & 1) + r * (2 * M8_TILE) + 16 * (hh ^ weight_xor(r));
+        u32x4_t fl = lds_read_u4<M8_OFF_BAD>(lds0 + 16 * (k & 1));
+        u32x4_t pf[2][RB];
+        static_for<0, 2>([&](auto sc_) {
+            static_for<0, RB>([&](auto rc) {
+                constexpr int s = decltype(sc_)::value, rb = decltype(rc)::value;
+                pf[s][rb] = lds_read_u4<rb * 32 * 2 * M8_TILE>(pr ^ (32 * s));
+            });
+        });
+        lds_wait<2 * RB>(fl);
+        const uint32_t all = __builtin_amdgcn_readfirstlane((fl[0] | fl[1]) | (fl[2] | fl[3]));
+        if (all & 1u) {
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) {
+                uint32_t al = lds_read_u1(lds0 + M8_OFF_ALPHA + 256 * (k & 1) + (32 * rb + r) * 4);
                 lds_wait<0>(al);
 #pragma unroll
                 for (int d = 0; d < 4; ++d)
@@ -1085,20 +1147,10 @@ __device__ __forceinline__ void chunk8_mid_segment(const Chunk8Args& a, const Ck
                     }
             }
         }
-        if (any & 2u) clean_tile(st, w, lane);
-        // after the waits for every LDS operation, which would be waits for these scalar loads too
-        if (k + 2 < nt) loader.fetch(t0 + k + 3);
-        u32x4_t pf[4][2];
-        static_for<0, 4>([&](auto sc_) {
-            static_for<0, 2>([&](auto rc) {
-                constexpr int s = decltype(sc_)::value, rb = decltype(rc)::value;
-                pf[s][rb] = lds_read_u4<C8_OFF_P + rb * 32 * 2 * C8_TILE>(lds0 + (lane & 31) * (2 * C8_TILE) +
-                                                                         16 * ((2 * s + (lane >> 5)) ^ rope_xor(lane & 31)));
-            });
-        });
-        const int e = c >> 1, vr = 4 * (lane >> 5) + (e & 3) + 8 * (e >> 2);
-        const uint32_t va = st + vr * D_LAT + 16 * ((8 * w + (g & 1)) ^ code_xor(vr)) + 8 * (lane & 1);
-        constexpr int N = 16, VD = 6;
+        if (all & 2u) clean_dims(st, w, lane);
+        const int e = (lane >> 1) & 7, vr = 4 * hh + (e & 3) + 8 * (e >> 2);   // a lane group's eight rows of 16, its place among the dims
+        const uint32_t va = st + vr * D_LAT + 16 * ((8 * w + ((lane >> 4) & 1)) ^ code_xor(vr)) + 8 * (lane & 1);
+        constexpr int N = 8, VD = 5;
         u32x2_t vv[VD + 1];
         auto vload = [&](auto ic) {
             constexpr int i = decltype(ic)::value;
@@ -1108,36 +1160,73 @@ __device__ __forceinline__ void chunk8_mid_segment(const Chunk8Args& a, const Ck
         static_for<0, N>([&](auto ic) {
             constexpr int i = decltype(ic)::value, s = i >> 2, d = i & 3;
             if constexpr (i + VD < N) vload(std::integral_constant<int, i + VD>{});
-            if constexpr (i == 0) static_for<0, 8>([&](auto q) { lds_wait<VD + 1>(pf[decltype(q)::value / 2][decltype(q)::value % 2]); });
+            if constexpr (i == 0) static_for<0, 2 * RB>([&](auto q) { lds_wait<VD + 1>(pf[decltype(q)::value / RB][decltype(q)::value % RB]); });
             lds_wait<(i + VD < N) ? VD : N - 1 - i>(vv[i % (VD + 1)]);
             const bf16x8_t v = decode8(vv[i % (VD + 1)][0], vv[i % (VD + 1)][1], 1.0f);
 #pragma unroll
-            for (int rb = 0; rb < 2; ++rb)
+            for (int rb = 0; rb < RB; ++rb)
                 o[d][rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8_t, pf[s][rb]), o[d][rb], 0, 0, 0);
         });
-    }
-
-    // ---- the rows' references and sums, for every wave
-    __syncthreads();
-    float* ml = reinterpret_cast<float*>(smem + C8_OFF_P);   // [row][2]
-    const float l = allreduce_groups(l_run, [](float p, float q) { return p + q; });
-    if (g == 0) {
-        ml[2 * (16 * w + c)] = m_run;
-        ml[2 * (16 * w + c) + 1] = l;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int rb = 0; rb < 2; ++rb) {
-        const int row = 32 * rb + (lane & 31), R = x.row0 + row;
-        finish_rows<2>(a, x.tok0 * a.H + R, R < x.nrow, row, rb, w, lane, ml[2 * row], ml[2 * row + 1], [&](int d) -> const f32x16_t& { return o[d][rb]; }, part_o, part_ml);
+        // after the waits for every LDS operation, which would be waits for these scalar loads too
+        if (k + 7 < nt) loader.fetch(t0 + k + 7);
     }
 }
+
+template <int RG>
+__device__ __forceinline__ void chunk8_mid_segment(const Chunk8Args& a, const CkUnit& x, int t0, int t1, float* part_o,
+                                                   float* part_ml, uint8_t* smem) {
+    constexpr int RB = RG / 2;
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));   // keeps the lane arithmetic of the loops out of registers across the units
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = wave & 3;
+    const uint32_t lds0 = lds_addr(smem);
+    const int nt = x.kv > 0 ? t1 - t0 : 0;
+    float* ml = reinterpret_cast<float*>(smem + M8_OFF_P);   // [row][2]
+    if (wave < 4) {
+        float m_run = -INFINITY, l_run = 0.f;
+        if (nt > 0) mid_scores<RG>(a, x, t0, nt, lds0, w, lane, m_run, l_run);
+        // ---- the rows' references and sums, for every wave
+        __syncthreads();
+        const float l = allreduce_groups(l_run, [](float p, float q) { return p + q; });
+        if (w < RG && lane < 16) {
+            ml[2 * (16 * w + lane)] = m_run;
+            ml[2 * (16 * w + lane) + 1] = l;
+        }
+        __syncthreads();
+        return;
+    }
+    f32x16_t o[4][RB];   // [dim block][row block]
+    if (nt > 0) {
+        mid_outputs<RB>(a, x, t0, nt, smem, lds0, w, lane, o);
+    } else {
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int r = 0; r < RB; ++r)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[d][r][i] = 0.f;
+    }
+    __syncthreads();
+    __syncthreads();
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        const int row = 32 * rb + (lane & 31), R = x.row0 + row;
+        finish_rows<RB>(a, x.tok0 * a.H + R, R < x.nrow, row, rb, w, lane, ml[2 * row], ml[2 * row + 1], [&](int d) -> const f32x16_t& { return o[d][rb]; }, part_o, part_ml);
+    }
+}
+
+// how a unit of 16 RG rows is worked on
+template <int RG>
+struct Shape8 {
+    static constexpr int TILE = RG == 2 || RG == 4 ? M8_TILE : C8_TILE, THREADS = RG == 2 || RG == 4 ? M8_THREADS : C8_THREADS;
+    static constexpr int SMEM = RG == 8 ? B8_SMEM : RG == 1 ? C8_SMEM : M8_SMEM;
+};
 
 template <int RG>
 __device__ __forceinline__ void segment8(const Chunk8Args& a, const CkUnit& x, int t0, int t1, float* part_o, float* part_ml,
                                          uint8_t* smem) {
     if constexpr (RG == 8) chunk8_big_segment(a, x, t0, t1, part_o, part_ml, smem);
-    else if constexpr (RG == 4) chunk8_mid_segment(a, x, t0, t1, part_o, part_ml, smem);
+    else if constexpr (RG > 1) chunk8_mid_segment<RG>(a, x, t0, t1, part_o, part_ml, smem);
     else chunk8_segment<RG>(a, x, t0, t1, part_o, part_ml, smem);
 }
 
@@ -1149,19 +1238,19 @@ __device__ __forceinline__ void segment8(const Chunk8Args& a, const CkUnit& x, i
 template <int RG>
 __device__ __forceinline__ int run_count8(const Chunk8Args& a, int total) {
     int len = 1;
-    while (2.0f * (float)len <= (RG <= 2 ? 0.12f : 0.25f) * sqrtf((float)total)) len *= 2;
+    while (2.0f * (float)len <= (RG == 1 ? 0.12f : RG == 8 ? 0.25f : 0.35f) * sqrtf((float)total)) len *= 2;
     return min(max((total + len - 1) / len, 1), a.runs);
 }
 
 template <int RG>
-__global__ __launch_bounds__(C8_THREADS, 1) void chunk8_run_kernel(Chunk8Args a) {
-    constexpr int ROWS = 16 * RG;
-    __shared__ __align__(1024) uint8_t smem[RG == 8 ? B8_SMEM : C8_SMEM];
+__global__ __launch_bounds__(Shape8<RG>::THREADS, 1) void chunk8_run_kernel(Chunk8Args a) {
+    constexpr int ROWS = 16 * RG, TILE = Shape8<RG>::TILE, THREADS = Shape8<RG>::THREADS;
+    __shared__ __align__(1024) uint8_t smem[Shape8<RG>::SMEM];
     __shared__ int pre[CK_MAX_UNITS];
-    const int total = scan_units<C8_TILE, C8_THREADS>(a, ROWS, pre), U = a.B * a.mb;
+    const int total = scan_units<TILE, THREADS>(a, ROWS, pre), U = a.B * a.mb;
     const int n = run_count8<RG>(a, total), g = blockIdx.x;
     if (g == 0)   // units without rows: nothing to join
-        for (int u = threadIdx.x; u < U; u += C8_THREADS)
+        for (int u = threadIdx.x; u < U; u += THREADS)
             if ((u + 1 < U ? pre[u + 1] : total) == pre[u]) a.span[3 * u] = a.span[3 * u + 1] = 0;
     if (g >= n) return;
     const int beg = run_start(g, n, total), end = run_start(g + 1, n, total);
@@ -1194,13 +1283,13 @@ __global__ __launch_bounds__(C8_THREADS, 1) void chunk8_run_kernel(Chunk8Args a)
 }
 
 template <int RG>
-__global__ __launch_bounds__(C8_THREADS, 1) void chunk8_unit_kernel(Chunk8Args a) {
-    __shared__ __align__(1024) uint8_t smem[RG == 8 ? B8_SMEM : C8_SMEM];
+__global__ __launch_bounds__(Shape8<RG>::THREADS, 1) void chunk8_unit_kernel(Chunk8Args a) {
+    __shared__ __align__(1024) uint8_t smem[Shape8<RG>::SMEM];
     const uint32_t wg = workgroup_id();
     if (wg >= (uint32_t)a.B * (uint32_t)a.mb) return;
     const int b = (int)(wg / (uint32_t)a.mb), j = a.mb - 1 - (int)(wg % (uint32_t)a.mb);   // the later rows (more tiles) first
     const CkUnit x = chunk_unit(a, b * a.mb + j, 16 * RG);
-    const int n = unit_tiles<C8_TILE>(a, x, 16 * RG);
+    const int n = unit_tiles<Shape8<RG>::TILE>(a, x, 16 * RG);
     if (n == 0) return;
     segment8<RG>(a, x, 0, n, nullptr, nullptr, smem);
 }
@@ -1293,10 +1382,10 @@ ChunkSplit chunk8_split(int64_t B, int64_t H, int64_t max_q, int64_t max_kv) {
 template <int RG>
 static hipError_t launch_chunk8_rows(const Chunk8Args& a, const ChunkSplit& sp, hipStream_t s) {
     if (!sp.runs) {
-        hipLaunchKernelGGL((chunk8_unit_kernel<RG>), grid_of(sp.units), dim3(C8_THREADS), 0, s, a);
+        hipLaunchKernelGGL((chunk8_unit_kernel<RG>), grid_of(sp.units), dim3(Shape8<RG>::THREADS), 0, s, a);
         return hipGetLastError();
     }
-    hipLaunchKernelGGL((chunk8_run_kernel<RG>), dim3((unsigned)sp.runs), dim3(C8_THREADS), 0, s, a);
+    hipLaunchKernelGGL((chunk8_run_kernel<RG>), dim3((unsigned)sp.runs), dim3(Shape8<RG>::THREADS), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || sp.runs == 1) return e;
     // a part in many pieces where few units share the chip (many parts of each), fewer pieces where there are units enough
