@@ -5,13 +5,18 @@
 //   o_i = sum_u softmax_u(s) c_u   (512 dims)
 //
 // Units of (token, head) rows and the runs of cache tiles they are cut into are those of the bf16
-// cache's kernel.  A tile is 64 rows of 640 bytes, three of them in LDS (direct loads); a workgroup is
-// four waves, one a SIMD.  Every 8-bit value is a bf16 value, so the products take bf16 operands that are
-// exact: the conversion of the keys multiplies by their power of two, and the weights carry it for
-// the product with the values.  The conversions are what the vector units do, so each code is converted
-// once a workgroup for either product: wave w takes the scores of its 16 of the tile's rows against all
-// the unit's queries (held in registers), the weights go through LDS, and it takes the 128 dims from 128 w on
-// of the outputs.
+// cache's kernel.  A tile is 64 or 32 rows of 640 bytes, three or seven of them in LDS (direct loads).  Every 8-bit value is a
+// bf16 value, so the products take bf16 operands that are exact: the conversion of the keys multiplies by their power of
+// two, and the weights carry it for the product with the values.  (The 8-bit products of these matrix cores take half the
+// time, but lose 1e-5 of the sum of the magnitudes where bf16 products lose 1e-8.)  The queries stay in registers, so do the
+// outputs, 128 dims a wave; weights go through LDS.  What the vector units convert is as long as the products it is for, and
+// bounds units of many rows as much as these do; units of few rows are bound by HBM.  So there are three ways to work on a unit,
+// by its rows:
+//   16       four waves; scores by rows of the tile, so that each code is converted once for either product
+//   32, 64   four waves of scores, by rows of the unit, beside four of outputs
+//   128      four waves, both in one stream of instructions, the scores of a tile between the outputs of the one before
+// 16 sequences of up to 65536 rows, 16 heads: 127 us, 4.7 TB/s.  16 of 32768 rows, 32 and 64 heads: 85 and 112 us.  32 of 32768
+// rows, 128 heads: 275 us; 3 x 512 new tokens over 16384 rows, 128 heads: 4.28 ms, 1.16 PFLOP/s.
 #include <algorithm>
 
 #include "vkv_runs.h"
@@ -24,12 +29,12 @@ constexpr int C8_STAGE = C8_TILE * VKV_ROW8;                    // 40 KB
 // what is read at constant offsets lies first (they have 16 bits), the stages after it
 constexpr int C8_OFF_WORD = 0;                                  // per stage and row: the word that holds its scale byte
 constexpr int C8_OFF_NOTE = C8_OFF_WORD + C8_STAGES * C8_TILE * 4;   // how far to shift it, or C8_ABSENT
-constexpr int C8_OFF_TOP = C8_OFF_NOTE + C8_STAGES * C8_TILE * 4;    // per row of the unit: the waves' largest scores
-constexpr int C8_OFF_BAD = C8_OFF_TOP + 64 * 16;                // per wave: whether a score that a mask hides is NaN
-constexpr int C8_OFF_P = C8_OFF_BAD + 512;                      // weights: [rows of the unit][64] bf16
-constexpr int C8_OFF_STAGE = C8_OFF_P + 64 * 2 * C8_TILE;       // 1 KB aligned, as pieces are chosen by XORs of the address
+constexpr int C8_OFF_TOP = C8_OFF_NOTE + C8_STAGES * C8_TILE * 4;    // [16] per row of the unit: the waves' largest scores
+constexpr int C8_OFF_BAD = C8_OFF_TOP + 16 * 16;                // per wave: whether a score that a mask hides is NaN
+constexpr int C8_OFF_P = 2048;                                  // weights: [16][64] bf16
+constexpr int C8_OFF_STAGE = C8_OFF_P + 16 * 2 * C8_TILE;       // 1 KB aligned, as pieces are chosen by XORs of the address
 constexpr int C8_SMEM = C8_OFF_STAGE + C8_STAGES * C8_STAGE;
-static_assert(C8_OFF_STAGE % 1024 == 0 && C8_OFF_P % 1024 == 0, "");
+static_assert(C8_OFF_BAD + 16 <= C8_OFF_P && C8_OFF_STAGE % 1024 == 0 && C8_OFF_P % 1024 == 0, "");
 constexpr uint32_t C8_ABSENT = 255;
 // Lag allowed to the softmax reference maximum (log2 units): weights up to 2^16, so that outputs are seldom multiplied; a sum
 // over 2^30 rows of 448 * 2^64 stays below 2^119.  (What lies 2^126 below the reference is 0.)
@@ -106,14 +111,16 @@ __device__ __forceinline__ float scale_of(uint32_t word, uint32_t note) {
 }
 
 // One wave's share of a tile of 4 NR rows: NR of them, their codes, branch and scale words.  WORD, NOTE: where the words of all
-// stages are, and what is noted of each.
-template <int NR, int WORD, int NOTE>
+// stages are, and what is noted of each.  HOLD: a lane's offsets in registers of their own across the loop, not found anew for
+// every tile (some 60 cycles a load).
+template <int NR, int WORD, int NOTE, bool HOLD>
 struct Loader8 {
     static constexpr int TILE = 4 * NR, STAGE = TILE * VKV_ROW8, OFF_ROPE = TILE * D_LAT;
     const Chunk8Args& a;
     const_i32_t* table;
     int kv, wt, lane;
     int32_t e[NR];          // the fetched tile's table entries (scalar)
+    uint32_t off[HOLD ? NR / 2 + NR / 8 : 1];
 
     // among 16 rows of the tile, which the XORs go by, NR = 8 are the first or the last
     __device__ __forceinline__ uint32_t late() const { return NR == 8 ? wt & 1 : 0; }
@@ -131,23 +138,36 @@ struct Loader8 {
         return a.page_mask >= NR - 1 && row(t, 0) + NR <= kv && (uint32_t)e[0] < (uint32_t)a.n_pages && a.rs16 < (1u << 24);
     }
     static constexpr int LOADS = NR / 2 + NR / 8 + 1;
+    // this lane's place in load J from the wave's first row on: of two rows' codes, half a wave each, or of eight rows'
+    // branch, eight lanes each
+    template <int J>
+    __device__ __forceinline__ uint32_t place(int ln) const {
+        const uint32_t rs = 16 * a.rs16;
+        if constexpr (J < NR / 2) {
+            const uint32_t p16 = (16 * (ln & 31)) ^ (32 * (ln >> 5)) ^ (128 * late());
+            return (p16 ^ (16 * code_xor(2 * J))) + (2 * J + (ln >> 5)) * rs;
+        } else {
+            constexpr int i = 8 * (J - NR / 2);
+            const uint32_t q16 = 16 * ((ln & 7) ^ ((ln >> 4) & 3)) ^ (64 * late());
+            return (q16 ^ (8 * i)) + (i + (ln >> 3)) * rs + D_LAT;
+        }
+    }
+    __device__ __forceinline__ void prepare() {
+        if constexpr (HOLD) static_for<0, LOADS - 1>([&](auto ic) { off[decltype(ic)::value] = place<decltype(ic)::value>(lane); });
+    }
     template <int J>
     __device__ __forceinline__ void part(int t, uint8_t* smem, uint32_t lds0, int sg, int stages) const {
         uint8_t* st = smem + stages + sg * STAGE;
         int ln = lane;
-        asm volatile("" : "+v"(ln));   // keeps the lane arithmetic out of registers across the loop
-        const uint32_t r = row(t, 0) & a.page_mask, rs = 16 * a.rs16;
+        if constexpr (!HOLD) asm volatile("" : "+v"(ln));   // keeps the lane arithmetic out of registers across the loop
+        const uint32_t r = row(t, 0) & a.page_mask;
         const char* b = reinterpret_cast<const char*>(a.cache8) + 16 * ((uint64_t)(uint32_t)e[0] * a.ps16 + (uint64_t)r * a.rs16);
-        if constexpr (J < NR / 2) {             // two rows' codes, half a wave each
-            constexpr int i = 2 * J;
-            const uint32_t p16 = (16 * (ln & 31)) ^ (32 * (ln >> 5)) ^ (128 * late());
-            __builtin_amdgcn_global_load_lds((gbl_void_t*)(b + (uint64_t)rs * i + ((p16 ^ (16 * code_xor(i))) + (ln >> 5) * rs)),
-                                             (lds_void_t*)(st + D_LAT * (NR * wt + i)), 16, 0, 0);
-        } else if constexpr (J < LOADS - 1) {   // eight rows' branch, eight lanes each
-            constexpr int i = 8 * (J - NR / 2);
-            const uint32_t q16 = 16 * ((ln & 7) ^ ((ln >> 4) & 3)) ^ (64 * late());
-            __builtin_amdgcn_global_load_lds((gbl_void_t*)(b + (uint64_t)rs * i + ((q16 ^ (8 * i)) + (ln >> 3) * rs + D_LAT)),
-                                             (lds_void_t*)(st + OFF_ROPE + 2 * D_ROPE * (NR * wt + i)), 16, 0, 0);
+        if constexpr (J < LOADS - 1) {
+            const int at = J < NR / 2 ? D_LAT * (NR * wt + 2 * J) : OFF_ROPE + 2 * D_ROPE * (NR * wt + 8 * (J - NR / 2));
+            uint32_t o;
+            if constexpr (HOLD) o = off[J];
+            else o = place<J>(ln);
+            __builtin_amdgcn_global_load_lds((gbl_void_t*)(b + o), (lds_void_t*)(st + at), 16, 0, 0);
         } else if (ln < NR) {                   // the aligned words around the scale bytes
             const uint64_t s0 = (uint64_t)(uintptr_t)(a.scale + (uint64_t)(uint32_t)e[0] * (uint64_t)a.sstride);
             const uint32_t at = (uint32_t)(s0 & 3) + ((r + ln) >> a.bshift);
@@ -221,7 +241,8 @@ struct Loader8 {
     }
 };
 
-typedef Loader8<16, C8_OFF_WORD, C8_OFF_NOTE> Loader64;   // tiles of 64 rows
+typedef Loader8<16, C8_OFF_WORD, C8_OFF_NOTE, true> Loader64;   // tiles of 64 rows
+typedef Loader8<16, C8_OFF_WORD, C8_OFF_NOTE, false> Loader64Lean;
 
 // ------------------------------------------------------------------ a segment
 
@@ -233,41 +254,33 @@ __device__ __forceinline__ void scale_acc(float& v, float f) {
     asm volatile("v_accvgpr_read_b32 %1, %0\n\tv_mul_f32 %1, %1, %2\n\tv_accvgpr_write_b32 %0, %1" : "+a"(v), "=&v"(t) : "v"(f));
 }
 
-// Tiles [t0, t1) of unit x (16 RG rows, RG 1 or 2) by one workgroup.  part: where an incomplete unit's
-// (O, m, l) go, or null (outputs).
-template <int RG>
+// Tiles [t0, t1) of unit x (16 rows) by one workgroup.  part: where an incomplete unit's (O, m, l) go, or null (outputs).
+// Wave w takes the scores of rows 16 w .. + 15 of a tile and the output dims from 128 w on.  Weights are taken against the
+// reference that every wave has, while the waves' maxima are exchanged, and again where these move it.
 __device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit& x, int t0, int t1, float* part_o,
                                                float* part_ml, uint8_t* smem) {
-    constexpr bool WIDE = RG > 1;                 // 32x32 products for the outputs
-    constexpr int RB = WIDE ? RG / 2 : 1;         // their blocks of rows
-    constexpr int NO = WIDE ? 4 : 8;              // their blocks of dims
-    constexpr int KS = WIDE ? 4 : 2;              // their steps along the tile
-    typedef typename std::conditional<WIDE, f32x16_t, f32x4_t>::type acc_t;
+    constexpr int NO = 8, KS = 2;                 // the outputs' blocks of dims, and steps along the tile
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t lds0 = lds_addr(smem);
-    int lim[RG];                                                // the last cache row that this lane's rows see
-#pragma unroll
-    for (int i = 0; i < RG; ++i) lim[i] = min(x.old + min(x.row0 + 16 * i + c, x.nrow - 1) / a.H, x.kv - 1);   // rows past the end repeat the last one
+    const int Rc = min(x.row0 + c, x.nrow - 1);                 // rows past the end repeat the last one, never stored
+    const int lim = min(x.old + Rc / a.H, x.kv - 1);            // the last cache row that this lane's row sees
     const int lim_lo = __builtin_amdgcn_readfirstlane(min(x.old + x.row0 / a.H, x.kv - 1));
     const int nt = x.kv > 0 ? t1 - t0 : 0;
 
-    Loader64 loader{a, (const_i32_t*)(a.table + (int64_t)x.b * a.tstride), x.kv, w, lane, {}};
+    Loader64 loader{a, (const_i32_t*)(a.table + (int64_t)x.b * a.tstride), x.kv, w, lane, {}, {}};
+    loader.prepare();
     // pieces of a key's codes that this lane reads: step s takes piece s ^ 9 (g & 1) ^ 16 (g >> 1), half after half
     const int pg = 9 * (g & 1) ^ 16 * (g >> 1);
-    bf16x8_t qf[RG][18];
-#pragma unroll
-    for (int i = 0; i < RG; ++i) {
-        const int64_t row = x.tok0 * a.H + min(x.row0 + 16 * i + c, x.nrow - 1);
+    bf16x8_t qf[18];
+    {
+        const int64_t row = x.tok0 * a.H + Rc;
         const uint16_t* ql = a.q_lat + row * a.qls;
         const uint16_t* qr = a.q_rope + row * a.qrs + 8 * g;
 #pragma unroll
-        for (int s = 0; s < 8; ++s) {
-            qf[i][2 * s] = *reinterpret_cast<const bf16x8_t*>(ql + 16 * (s ^ pg));
-            qf[i][2 * s + 1] = *reinterpret_cast<const bf16x8_t*>(ql + 16 * (s ^ pg) + 8);
-        }
+        for (int s = 0; s < 16; ++s) qf[s] = *reinterpret_cast<const bf16x8_t*>(ql + 16 * ((s >> 1) ^ pg) + 8 * (s & 1));
 #pragma unroll
-        for (int s = 0; s < 2; ++s) qf[i][16 + s] = *reinterpret_cast<const bf16x8_t*>(qr + 32 * s);
+        for (int s = 0; s < 2; ++s) qf[16 + s] = *reinterpret_cast<const bf16x8_t*>(qr + 32 * s);
     }
     if (nt > 0) {
         loader.fetch(t0);
@@ -279,20 +292,12 @@ __device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit
         }
     }
 #pragma unroll
-    for (int i = 0; i < RG; ++i)
-#pragma unroll
-        for (int s = 0; s < 18; ++s) asm volatile("" : "+v"(qf[i][s]));   // no wait for them inside the tile loop
+    for (int s = 0; s < 18; ++s) asm volatile("" : "+v"(qf[s]));   // no wait for them inside the tile loop
 
-    acc_t o[NO][RB];
+    f32x4_t o[NO];
 #pragma unroll
-    for (int d = 0; d < NO; ++d)
-#pragma unroll
-        for (int r = 0; r < RB; ++r)
-#pragma unroll
-            for (int i = 0; i < (WIDE ? 16 : 4); ++i) o[d][r][i] = 0.f;
-    float m_run[RG], l_run[RG];
-#pragma unroll
-    for (int i = 0; i < RG; ++i) m_run[i] = -INFINITY, l_run[i] = 0.f;
+    for (int d = 0; d < NO; ++d) o[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    float m_run = -INFINITY, l_run = 0.f;
 
     int sg = 0;   // the stage of tile k
     for (int k = 0; k < nt; ++k) {
@@ -302,9 +307,7 @@ __device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit
         else
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         lds_barrier();
-        if (k + 2 < nt) {
-            loader.issue(t0 + k + 2, smem, lds0, sg == 0 ? 2 : sg - 1, C8_OFF_STAGE);
-        }
+        if (k + 2 < nt) loader.issue(t0 + k + 2, smem, lds0, sg == 0 ? 2 : sg - 1, C8_OFF_STAGE);
         const int u0 = C8_TILE * (t0 + k);
         const uint32_t st = lds0 + C8_OFF_STAGE + sg * C8_STAGE;
         const uint32_t wn = lds0 + C8_OFF_WORD + (sg * C8_TILE + lane) * 4;
@@ -312,8 +315,7 @@ __device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit
 
         // ---- scores of rows 16 w .. + 15 of the tile
         uint32_t word = lds_read_u1(wn), note = lds_read_u1(wn + (C8_OFF_NOTE - C8_OFF_WORD));
-        const int kx = 16 * code_xor(c);
-        const uint32_t ka = st + (16 * w + c) * D_LAT + ((16 * pg) ^ kx);
+        const uint32_t ka = st + (16 * w + c) * D_LAT + ((16 * pg) ^ (16 * code_xor(c)));
         const uint32_t ra = st + C8_OFF_ROPE + (16 * w + c) * (2 * D_ROPE) + 16 * (g ^ rope_xor(c));
         constexpr int SD = 3;          // operands read ahead of the matrix cores: 8 of codes, 2 of the branch
         u32x4_t kc[SD + 1];
@@ -329,9 +331,7 @@ __device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit
         float sp[4];                                            // of those whose scores it gets: 16 w + 4 g + i
 #pragma unroll
         for (int i = 0; i < 4; ++i) sp[i] = __shfl(sc, 16 * w + 4 * g + i);
-        f32x4_t s4[RG];
-#pragma unroll
-        for (int i = 0; i < RG; ++i) s4[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        f32x4_t s4 = {0.f, 0.f, 0.f, 0.f};
         static_for<0, 10>([&](auto sc_) {
             constexpr int s = decltype(sc_)::value;
             if constexpr (s + SD < 10) kload(std::integral_constant<int, s + SD>{});
@@ -339,14 +339,10 @@ __device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit
             lds_wait<(s + SD < 10) ? SD : 9 - s>(v);
             if constexpr (s < 8) {
                 const bf16x8_t k0 = decode8(v[0], v[1], sk), k1 = decode8(v[2], v[3], sk);
-#pragma unroll
-                for (int i = 0; i < RG; ++i) s4[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qf[i][2 * s], s4[i], 0, 0, 0);
-#pragma unroll
-                for (int i = 0; i < RG; ++i) s4[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, qf[i][2 * s + 1], s4[i], 0, 0, 0);
+                s4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qf[2 * s], s4, 0, 0, 0);
+                s4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, qf[2 * s + 1], s4, 0, 0, 0);
             } else {
-#pragma unroll
-                for (int i = 0; i < RG; ++i)
-                    s4[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, v), qf[i][8 + s], s4[i], 0, 0, 0);
+                s4 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, v), qf[8 + s], s4, 0, 0, 0);
             }
         });
 
@@ -355,177 +351,109 @@ __device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit
         if (u0 + C8_TILE - 1 > lim_lo || absent != 0) {
             const uint32_t gone = (uint32_t)(absent >> (16 * w + 4 * g));
 #pragma unroll
-            for (int j = 0; j < RG; ++j)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (u0 + 16 * w + 4 * g + i > lim[j] || ((gone >> i) & 1u)) {
-                        bad |= s4[j][i] != s4[j][i];
-                        s4[j][i] = -INFINITY;
-                    }
-        }
-        float top[RG];
-#pragma unroll
-        for (int j = 0; j < RG; ++j) {
-            float m = fmaxf(fmaxf(s4[j][0], s4[j][1]), fmaxf(s4[j][2], s4[j][3]));
-            top[j] = allreduce_groups(m, [](float p, float q) { return fmaxf(p, q); }) * a.scale_log2;
-        }
-        const bool wave_bad = __ballot(bad) != 0;
-        // the weights against the reference that every wave has; they are written again where it moves
-        float ps[RG];
-        auto weights = [&]() __attribute__((always_inline)) {
-#pragma unroll
-            for (int j = 0; j < RG; ++j) {
-                const float ref = m_run[j] == -INFINITY ? 0.f : m_run[j];
-                bf16x4_t p4;
-                ps[j] = 0.f;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s4[j][i], a.scale_log2, -ref));
-                    ps[j] += p;
-                    p4[i] = (__bf16)(p * sp[i]);
+            for (int i = 0; i < 4; ++i)
+                if (u0 + 16 * w + 4 * g + i > lim || ((gone >> i) & 1u)) {
+                    bad |= s4[i] != s4[i];
+                    s4[i] = -INFINITY;
                 }
-                // slots of a row: as they are (16x16 products), or in each 16 of them rows 4 h + (0..3, 8..11) for half h
-                const int row = 16 * j + c, piece = WIDE ? 2 * w + (g & 1) : 2 * w + (g >> 1), half = WIDE ? g >> 1 : g & 1;
-                lds_write_u2(lds0 + C8_OFF_P + row * (2 * C8_TILE) + 16 * (piece ^ rope_xor(row)) + 8 * half,
-                             __builtin_bit_cast(u32x2_t, p4));
+        }
+        float top = fmaxf(fmaxf(s4[0], s4[1]), fmaxf(s4[2], s4[3]));
+        top = allreduce_groups(top, [](float p, float q) { return fmaxf(p, q); }) * a.scale_log2;
+        const bool wave_bad = __ballot(bad) != 0;
+        float ps;
+        auto weights = [&]() __attribute__((always_inline)) {
+            const float ref = m_run == -INFINITY ? 0.f : m_run;
+            bf16x4_t p4;
+            ps = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s4[i], a.scale_log2, -ref));
+                ps += p;
+                p4[i] = (__bf16)(p * sp[i]);
             }
+            lds_write_u2(lds0 + C8_OFF_P + c * (2 * C8_TILE) + 16 * ((2 * w + (g >> 1)) ^ rope_xor(c)) + 8 * (g & 1),
+                         __builtin_bit_cast(u32x2_t, p4));
         };
         weights();
-        if (g == 0)
-#pragma unroll
-            for (int j = 0; j < RG; ++j) lds_write_u1(lds0 + C8_OFF_TOP + (16 * j + c) * 16 + 4 * w, __float_as_uint(top[j]));
+        if (g == 0) lds_write_u1(lds0 + C8_OFF_TOP + c * 16 + 4 * w, __float_as_uint(top));
         if (lane == 0) lds_write_u1(lds0 + C8_OFF_BAD + 4 * w, wave_bad ? 1u : 0u);
         lds_barrier();
-        u32x4_t tops[RG], bads = lds_read_u4<C8_OFF_BAD>(lds0);
-#pragma unroll
-        for (int j = 0; j < RG; ++j) tops[j] = lds_read_u4<C8_OFF_TOP>(lds0 + (16 * j + c) * 16);
-        lds_wait<0>(bads);
-        bool move = false;
-        float next[RG];
-#pragma unroll
-        for (int j = 0; j < RG; ++j) {
-            lds_wait<0>(tops[j]);
-            const float m = fmaxf(fmaxf(__uint_as_float(tops[j][0]), __uint_as_float(tops[j][1])),
-                                  fmaxf(__uint_as_float(tops[j][2]), __uint_as_float(tops[j][3])));
-            const bool up = m > m_run[j] + C8_SLACK;
-            next[j] = up ? m + C8_ROOM : m_run[j];
-            move |= up;
-        }
+        u32x4_t bads = lds_read_u4<C8_OFF_BAD>(lds0), tops = lds_read_u4<C8_OFF_TOP>(lds0 + c * 16);
+        lds_wait<0>(bads, tops);
+        const float m = fmaxf(fmaxf(__uint_as_float(tops[0]), __uint_as_float(tops[1])),
+                              fmaxf(__uint_as_float(tops[2]), __uint_as_float(tops[3])));
+        const bool move = m > m_run + C8_SLACK;
         if (__ballot(move)) {   // the same in every wave
-            float al[RG];
+            const float next = move ? m + C8_ROOM : m_run, al = move ? __builtin_amdgcn_exp2f(m_run - next) : 1.0f;
+            l_run *= al;
+            m_run = next;
 #pragma unroll
-            for (int j = 0; j < RG; ++j) {
-                al[j] = next[j] == m_run[j] ? 1.0f : __builtin_amdgcn_exp2f(m_run[j] - next[j]);
-                l_run[j] *= al[j];
-                m_run[j] = next[j];
-            }
+            for (int d = 0; d < NO; ++d)
 #pragma unroll
-            for (int r = 0; r < RB; ++r) {
-                float f = al[0];
-                if constexpr (WIDE) f = (lane & 16) ? al[2 * r + 1] : al[2 * r];
-#pragma unroll
-                for (int d = 0; d < NO; ++d)
-#pragma unroll
-                    for (int i = 0; i < (WIDE ? 16 : 4); ++i) {
-                        float v = o[d][r][i];
-                        scale_acc(v, f);
-                        o[d][r][i] = v;
-                    }
-            }
+                for (int i = 0; i < 4; ++i) {
+                    float v = o[d][i];
+                    scale_acc(v, al);
+                    o[d][i] = v;
+                }
             weights();
             lds_barrier();
         }
-#pragma unroll
-        for (int j = 0; j < RG; ++j) l_run[j] += ps[j];   // this lane's share of the sum
+        l_run += ps;   // this lane's share of the sum
 
         // after the waits for every LDS operation, which would be waits for these scalar loads too
         if (k + 2 < nt) loader.fetch(t0 + k + 3);
 
         // ---- outputs, dims 128 w .. + 127
-        u32x4_t pf[KS][RB];
+        u32x4_t pf[KS];
 #pragma unroll
-        for (int s = 0; s < KS; ++s)
-#pragma unroll
-            for (int r = 0; r < RB; ++r) {
-                const int row = WIDE ? 32 * r + (lane & 31) : c, piece = WIDE ? 2 * s + (lane >> 5) : 4 * s + g;
-                pf[s][r] = lds_read_u4<C8_OFF_P>(lds0 + row * (2 * C8_TILE) + 16 * (piece ^ rope_xor(row)));
-            }
-        const int e = c >> 1;       // the row within a lane group's eight, its place among the tile's
-        const int vr = WIDE ? 4 * (lane >> 5) + (e & 3) + 8 * (e >> 2) : 8 * g + e;
-        const int vp = WIDE ? 8 * w + (g & 1) : 8 * w;
-        const uint32_t va = st + vr * D_LAT + 16 * (vp ^ code_xor(vr)) + 8 * (lane & 1);
+        for (int s = 0; s < KS; ++s) pf[s] = lds_read_u4<C8_OFF_P>(lds0 + c * (2 * C8_TILE) + 16 * ((4 * s + g) ^ rope_xor(c)));
+        const int vr = 8 * g + (c >> 1);       // the row within a lane group's eight, its place among the tile's
+        const uint32_t va = st + vr * D_LAT + 16 * ((8 * w) ^ code_xor(vr)) + 8 * (lane & 1);
         if (bads[0] | bads[1] | bads[2] | bads[3]) clean_tile(st, w, lane);
-        {
-            constexpr int N = KS * NO, VD = 6;
-            u32x2_t vv[VD + 1];
-            auto vload = [&](auto ic) {
-                constexpr int i = decltype(ic)::value, s = i / NO, d = i % NO;
-                vv[i % (VD + 1)] = lds_read_tr8<(WIDE ? 16 : 32) * D_LAT * s>(va ^ (WIDE ? 32 * d : 16 * d));
-            };
-            static_for<0, VD>(vload);
-            static_for<0, N>([&](auto ic) {
-                constexpr int i = decltype(ic)::value, s = i / NO, d = i % NO;
-                if constexpr (i + VD < N) vload(std::integral_constant<int, i + VD>{});
-                if constexpr (i == 0)
-#pragma unroll
-                    for (int q = 0; q < KS * RB; ++q) lds_wait<VD + 1>(pf[q / RB][q % RB]);
-                lds_wait<(i + VD < N) ? VD : N - 1 - i>(vv[i % (VD + 1)]);
-                const bf16x8_t v = decode8(vv[i % (VD + 1)][0], vv[i % (VD + 1)][1], 1.0f);
-#pragma unroll
-                for (int r = 0; r < RB; ++r) {
-                    const bf16x8_t p = __builtin_bit_cast(bf16x8_t, pf[s][r]);
-                    if constexpr (WIDE) o[d][r] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p, o[d][r], 0, 0, 0);
-                    else o[d][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p, o[d][r], 0, 0, 0);
-                }
-            });
-        }
+        constexpr int N = KS * NO, VD = 6;
+        u32x2_t vv[VD + 1];
+        auto vload = [&](auto ic) {
+            constexpr int i = decltype(ic)::value, s = i / NO, d = i % NO;
+            vv[i % (VD + 1)] = lds_read_tr8<32 * D_LAT * s>(va ^ (16 * d));
+        };
+        static_for<0, VD>(vload);
+        static_for<0, N>([&](auto ic) {
+            constexpr int i = decltype(ic)::value, s = i / NO, d = i % NO;
+            if constexpr (i + VD < N) vload(std::integral_constant<int, i + VD>{});
+            if constexpr (i == 0) lds_wait<VD + 1>(pf[0], pf[1]);
+            lds_wait<(i + VD < N) ? VD : N - 1 - i>(vv[i % (VD + 1)]);
+            const bf16x8_t v = decode8(vv[i % (VD + 1)][0], vv[i % (VD + 1)][1], 1.0f);
+            o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8_t, pf[s]), o[d], 0, 0, 0);
+        });
     }
 
     // ---- the sums of the waves' rows
     __syncthreads();
     float* sums = reinterpret_cast<float*>(smem + C8_OFF_TOP);   // [row][wave]
-#pragma unroll
-    for (int j = 0; j < RG; ++j) {
-        const float l = allreduce_groups(l_run[j], [](float p, float q) { return p + q; });
-        if (g == 0) sums[4 * (16 * j + c) + w] = l;
-    }
-    float* ref = reinterpret_cast<float*>(smem + C8_OFF_P);      // [row]
-    if (w == 0 && g == 0)
-#pragma unroll
-        for (int j = 0; j < RG; ++j) ref[16 * j + c] = m_run[j];
+    l_run = allreduce_groups(l_run, [](float p, float q) { return p + q; });
+    if (g == 0) sums[4 * c + w] = l_run;
     __syncthreads();
+    const float l = (sums[4 * c] + sums[4 * c + 1]) + (sums[4 * c + 2] + sums[4 * c + 3]);
+    const int R = x.row0 + c;
+    if (part_o) {
+        // accumulator order: [wave][dim block][64 lanes][4]
 #pragma unroll
-    for (int r = 0; r < RB; ++r) {
-        const int row = WIDE ? 32 * r + (lane & 31) : c, R = x.row0 + row;
-        const float m = ref[row], l = (sums[4 * row] + sums[4 * row + 1]) + (sums[4 * row + 2] + sums[4 * row + 3]);
-        if (part_o) {
-            // accumulator order: [wave][dim block][row block][4][64 lanes][4], or [wave][dim block][64 lanes][4]
-#pragma unroll
-            for (int d = 0; d < NO; ++d)
-#pragma unroll
-                for (int q = 0; q < (WIDE ? 4 : 1); ++q) {
-                    const f32x4_t v = {o[d][r][4 * q], o[d][r][4 * q + 1], o[d][r][4 * q + 2], o[d][r][4 * q + 3]};
-                    *reinterpret_cast<f32x4_t*>(part_o + ((((w * NO + d) * RB + r) * (WIDE ? 4 : 1) + q) * 64 + lane) * 4) = v;
-                }
-            if (w == 0 && lane < (WIDE ? 32 : 16)) {
-                part_ml[2 * row] = m;
-                part_ml[2 * row + 1] = l;
-            }
-        } else if (R < x.nrow) {
-            const int64_t at = x.tok0 * a.H + R;
-            const bool none = m == -INFINITY && l == 0.f;
-            const float inv = none ? 0.f : 1.0f / l;
-            uint16_t* out = a.out + at * D_LAT + 128 * w + (WIDE ? 4 * (lane >> 5) : 4 * g);
-#pragma unroll
-            for (int d = 0; d < NO; ++d)
-#pragma unroll
-                for (int q = 0; q < (WIDE ? 4 : 1); ++q) {
-                    const bf16x4_t v = {(__bf16)(o[d][r][4 * q] * inv), (__bf16)(o[d][r][4 * q + 1] * inv),
-                                        (__bf16)(o[d][r][4 * q + 2] * inv), (__bf16)(o[d][r][4 * q + 3] * inv)};
-                    *reinterpret_cast<bf16x4_t*>(out + (WIDE ? 32 * d + 8 * q : 16 * d)) = v;
-                }
-            if (w == 0 && lane < (WIDE ? 32 : 16)) a.lse[at] = lse_of(m, l);
+        for (int d = 0; d < NO; ++d) *reinterpret_cast<f32x4_t*>(part_o + ((w * NO + d) * 64 + lane) * 4) = o[d];
+        if (w == 0 && g == 0) {
+            part_ml[2 * c] = m_run;
+            part_ml[2 * c + 1] = l;
         }
+    } else if (R < x.nrow) {
+        const int64_t at = x.tok0 * a.H + R;
+        const bool none = m_run == -INFINITY && l == 0.f;
+        const float inv = none ? 0.f : 1.0f / l;
+        uint16_t* out = a.out + at * D_LAT + 128 * w + 4 * g;
+#pragma unroll
+        for (int d = 0; d < NO; ++d) {
+            const bf16x4_t v = {(__bf16)(o[d][0] * inv), (__bf16)(o[d][1] * inv), (__bf16)(o[d][2] * inv), (__bf16)(o[d][3] * inv)};
+            *reinterpret_cast<bf16x4_t*>(out + 16 * d) = v;
+        }
+        if (w == 0 && g == 0) a.lse[at] = lse_of(m_run, l);
     }
 }
 
@@ -576,7 +504,7 @@ constexpr int B8_P = 128 * 2 * C8_TILE;                         // weights of a 
 constexpr int B8_OFF_SCALE = C8_OFF_TOP;                        // [64] the tile's scales (every wave writes the same ones)
 constexpr int B8_OFF_ALPHA = B8_OFF_SCALE + 4 * C8_TILE;        // two of [128]: by what a row's outputs are to be multiplied
 constexpr int B8_OFF_BAD = B8_OFF_ALPHA + 2 * 512;              // two of [4]: the waves' flags, outputs to multiply, a hidden NaN
-constexpr int B8_OFF_P = C8_OFF_P;
+constexpr int B8_OFF_P = 3072;
 constexpr int B8_OFF_STAGE = B8_OFF_P + 2 * B8_P;
 constexpr int B8_SMEM = B8_OFF_STAGE + C8_STAGES * C8_STAGE;
 static_assert(B8_OFF_BAD + 32 <= B8_OFF_P && B8_OFF_STAGE % 1024 == 0, "");
@@ -765,7 +693,7 @@ __device__ __forceinline__ void chunk8_big_segment(const Chunk8Args& a, const Ck
     const int lim_lo = __builtin_amdgcn_readfirstlane(min(x.old + first / a.H, x.kv - 1));
     const int nt = x.kv > 0 ? t1 - t0 : 0;
 
-    Loader64 loader{a, (const_i32_t*)(a.table + (int64_t)x.b * a.tstride), x.kv, w, lane, {}};
+    Loader64Lean loader{a, (const_i32_t*)(a.table + (int64_t)x.b * a.tstride), x.kv, w, lane, {}, {}};
     Big8 z;
     {
         const int64_t row = x.tok0 * a.H + Rc;
@@ -858,7 +786,7 @@ __device__ __forceinline__ void chunk8_big_segment(const Chunk8Args& a, const Ck
 
     if (nt > 0) {
         if (nt > 1)
-            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(Loader64::LOADS) : "memory");
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(Loader64Lean::LOADS) : "memory");
         else
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         lds_barrier();
@@ -934,7 +862,7 @@ constexpr int M8_OFF_ALPHA = M8_OFF_SCALE + 4 * M8_TILE;              // two of 
 constexpr int M8_OFF_BAD = M8_OFF_ALPHA + 2 * 256;                    // two of [4]: the waves' flags, outputs to multiply, a hidden NaN
 constexpr int M8_OFF_P = 3072, M8_P = 64 * 2 * M8_TILE;               // weights of a tile, [64][32] bf16; two of them
 constexpr int M8_OFF_STAGE = M8_OFF_P + 2 * M8_P;
-typedef Loader8<8, M8_OFF_WORD, M8_OFF_NOTE> Loader32;
+typedef Loader8<8, M8_OFF_WORD, M8_OFF_NOTE, true> Loader32;
 constexpr int M8_SMEM = M8_OFF_STAGE + M8_STAGES * Loader32::STAGE;
 static_assert(M8_OFF_BAD + 32 <= M8_OFF_P && M8_OFF_STAGE % 1024 == 0 && Loader32::TILE == M8_TILE, "");
 
@@ -1084,7 +1012,8 @@ __device__ __forceinline__ void mid_scores(const Chunk8Args& a, const CkUnit& x,
 template <int RB>
 __device__ __forceinline__ void mid_outputs(const Chunk8Args& a, const CkUnit& x, int t0, int nt, uint8_t* smem, uint32_t lds0, int w, int lane,
                                             f32x16_t (&o)[4][RB]) {
-    Loader32 loader{a, (const_i32_t*)(a.table + (int64_t)x.b * a.tstride), x.kv, w, lane, {}};
+    Loader32 loader{a, (const_i32_t*)(a.table + (int64_t)x.b * a.tstride), x.kv, w, lane, {}, {}};
+    loader.prepare();
     constexpr int FIRST = M8_STAGES - 2;
     {
         Loader32 first[FIRST] = {loader, loader, loader, loader, loader};
@@ -1227,7 +1156,7 @@ __device__ __forceinline__ void segment8(const Chunk8Args& a, const CkUnit& x, i
                                          uint8_t* smem) {
     if constexpr (RG == 8) chunk8_big_segment(a, x, t0, t1, part_o, part_ml, smem);
     else if constexpr (RG > 1) chunk8_mid_segment<RG>(a, x, t0, t1, part_o, part_ml, smem);
-    else chunk8_segment<RG>(a, x, t0, t1, part_o, part_ml, smem);
+    else chunk8_segment(a, x, t0, t1, part_o, part_ml, smem);
 }
 
 // ------------------------------------------------------------------- kernels
@@ -1357,14 +1286,13 @@ __global__ __launch_bounds__(C8J_THREADS) void chunk8_join_kernel(Chunk8Args a) 
 ChunkSplit chunk8_split(int64_t B, int64_t H, int64_t max_q, int64_t max_kv) {
     ChunkSplit s{};
     const int64_t rows = max_q * H;
-    // Rows of a unit.  Many rows: each code is converted once for all of them.  Few rows: more units where the cache alone does not
+    // Rows of a unit.  Many rows: each code is converted once for all of them.  Fewer rows: more units where the cache alone does not
     // give every CU some tiles to work through, a start and a part that take less time, and the cache is read again from
-    // nearby.  128 heads, a token each, units of 16, 64 and 128 rows: one sequence of 4096 rows 21, 27, 42 us, of 32768 rows 45,
-    // 36, 57 us; 16 of 32768 rows 426, 198, 179 us.  32 heads, units of 16 and 32 rows: one of 8192 rows 20, 28 us; 4 of 32768
-    // rows 48, 50 us, 16 of them 121, 96 us.
+    // nearby.  128 heads, a token each, units of 32, 64 and 128 rows: one sequence of 8192 rows 26, 30, 44 us, of 131072 rows 85,
+    // 66, 81 us; 16 of 32768 rows 262, 204, 187 us.  64 heads, units of 32 and 64 rows: 30 and 33 us, 52 and 49 us, 145 and 113 us.
     const int64_t cache = B * std::max<int64_t>(1, (max_kv + C8_TILE - 1) / C8_TILE);   // tiles
-    const int64_t of16 = (rows + 15) / 16 * cache, of64 = (rows + 63) / 64 * cache;
-    s.qg = rows <= 16 || of16 <= 2048 || (rows <= 32 && of16 <= 4096) ? 1 : rows <= 32 ? 2 : rows <= 64 || of64 <= 8192 ? 4 : 8;
+    const int64_t of32 = (rows + 31) / 32 * cache, of64 = (rows + 63) / 64 * cache;
+    s.qg = rows <= 16 ? 1 : rows <= 32 || of32 <= 2048 ? 2 : rows <= 64 || of64 <= 8192 ? 4 : 8;
     s.mb = (rows + 16 * s.qg - 1) / (16 * s.qg);
     s.units = B * s.mb;
     const int64_t tiles = s.mb * cache;
