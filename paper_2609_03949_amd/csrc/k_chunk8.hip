@@ -138,36 +138,34 @@ struct Loader8 {
         return a.page_mask >= NR - 1 && row(t, 0) + NR <= kv && (uint32_t)e[0] < (uint32_t)a.n_pages && a.rs16 < (1u << 24);
     }
     static constexpr int LOADS = NR / 2 + NR / 8 + 1;
-    // this lane's place in load J from the wave's first row on: of two rows' codes, half a wave each, or of eight rows'
-    // branch, eight lanes each
+    // this lane's place in load J from its first row on: of two rows' codes, half a wave each, or of eight rows' branch, eight
+    // lanes each
     template <int J>
     __device__ __forceinline__ uint32_t place(int ln) const {
         const uint32_t rs = 16 * a.rs16;
         if constexpr (J < NR / 2) {
             const uint32_t p16 = (16 * (ln & 31)) ^ (32 * (ln >> 5)) ^ (128 * late());
-            return (p16 ^ (16 * code_xor(2 * J))) + (2 * J + (ln >> 5)) * rs;
+            return (p16 ^ (16 * code_xor(2 * J))) + (ln >> 5) * rs;
         } else {
-            constexpr int i = 8 * (J - NR / 2);
             const uint32_t q16 = 16 * ((ln & 7) ^ ((ln >> 4) & 3)) ^ (64 * late());
-            return (q16 ^ (8 * i)) + (i + (ln >> 3)) * rs + D_LAT;
+            return (q16 ^ (64 * (J - NR / 2))) + (ln >> 3) * rs + D_LAT;
         }
     }
     __device__ __forceinline__ void prepare() {
         if constexpr (HOLD) static_for<0, LOADS - 1>([&](auto ic) { off[decltype(ic)::value] = place<decltype(ic)::value>(lane); });
     }
     template <int J>
-    __device__ __forceinline__ void part(int t, uint8_t* smem, uint32_t lds0, int sg, int stages) const {
+    __device__ __forceinline__ void part(int t, uint8_t* smem, uint32_t lds0, int sg, int stages, int ln) const {
         uint8_t* st = smem + stages + sg * STAGE;
-        int ln = lane;
-        if constexpr (!HOLD) asm volatile("" : "+v"(ln));   // keeps the lane arithmetic out of registers across the loop
         const uint32_t r = row(t, 0) & a.page_mask;
         const char* b = reinterpret_cast<const char*>(a.cache8) + 16 * ((uint64_t)(uint32_t)e[0] * a.ps16 + (uint64_t)r * a.rs16);
         if constexpr (J < LOADS - 1) {
-            const int at = J < NR / 2 ? D_LAT * (NR * wt + 2 * J) : OFF_ROPE + 2 * D_ROPE * (NR * wt + 8 * (J - NR / 2));
+            constexpr int i = J < NR / 2 ? 2 * J : 8 * (J - NR / 2);
+            const int at = J < NR / 2 ? D_LAT * (NR * wt + i) : OFF_ROPE + 2 * D_ROPE * (NR * wt + i);
             uint32_t o;
             if constexpr (HOLD) o = off[J];
             else o = place<J>(ln);
-            __builtin_amdgcn_global_load_lds((gbl_void_t*)(b + o), (lds_void_t*)(st + at), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((gbl_void_t*)(b + (uint64_t)(16 * a.rs16) * i + o), (lds_void_t*)(st + at), 16, 0, 0);
         } else if (ln < NR) {                   // the aligned words around the scale bytes
             const uint64_t s0 = (uint64_t)(uintptr_t)(a.scale + (uint64_t)(uint32_t)e[0] * (uint64_t)a.sstride);
             const uint32_t at = (uint32_t)(s0 & 3) + ((r + ln) >> a.bshift);
@@ -178,7 +176,9 @@ struct Loader8 {
     }
     // the loads of the fetched tile t into stage sg
     __device__ __forceinline__ void issue(int t, uint8_t* smem, uint32_t lds0, int sg, int stages) const {
-        if (plain(t)) static_for<0, LOADS>([&](auto ic) { part<decltype(ic)::value>(t, smem, lds0, sg, stages); });
+        int ln = lane;
+        if constexpr (!HOLD) asm volatile("" : "+v"(ln));   // keeps the lane arithmetic out of registers across the loop
+        if (plain(t)) static_for<0, LOADS>([&](auto ic) { part<decltype(ic)::value>(t, smem, lds0, sg, stages, ln); });
         else issue_any(t, smem, lds0, sg, stages);
     }
     __device__ __forceinline__ void issue_any(int t, uint8_t* smem, uint32_t lds0, int sg, int stages) const {
