@@ -259,9 +259,61 @@ __global__ __launch_bounds__(PO_THREADS) void reserve_give_kernel(PoolArgs a, co
     give(a, want, b, wave_sum(at), wave_sum(copy), a.need[2 * b + 1] != 0, a.head[PO_FREE], a.list, missing, true);
 }
 
+// the copies of pairs of pages, shared by workgroups of THREADS
+
+template <int THREADS, typename T>
+__device__ __forceinline__ void move_plane(const PoolPlane& s, const int32_t* from, const int32_t* to, int pairs, int wg, int wgs) {
+    const int64_t n = s.bytes / (int64_t)sizeof(T);
+    const int64_t per = n < THREADS ? THREADS / n : 1;        // small pages: several by one workgroup
+    const int64_t pages = (int64_t)pairs * s.layers;
+    const int64_t items = per > 1 ? (pages + per - 1) / per : pages * s.pieces;
+    for (int64_t k = wg; k < items; k += wgs) {
+        int64_t page, i, end;
+        if (per > 1) {
+            page = k * per + threadIdx.x / n;
+            i = threadIdx.x % n;
+            end = threadIdx.x < per * n && page < pages ? n : 0;
+        } else {
+            page = k / s.pieces;
+            const int64_t first = (k % s.pieces) * (PO_PIECE / (int64_t)sizeof(T));
+            i = first + threadIdx.x;
+            end = min(n, first + PO_PIECE / (int64_t)sizeof(T));
+        }
+        const int pair = (int)(page % max(pairs, 1)), layer = (int)(page / max(pairs, 1));
+        if (i >= end) continue;
+        const T* src = reinterpret_cast<const T*>(s.base + layer * s.ls + from[pair] * s.ps);
+        T* dst = reinterpret_cast<T*>(s.base + layer * s.ls + to[pair] * s.ps);
+        if (per > 1) {
+            dst[i] = src[i];
+            continue;
+        }
+        if constexpr (sizeof(T) == 16) {
+            constexpr int EACH = PO_PIECE / 16 / THREADS;
+            T v[EACH];
+#pragma unroll
+            for (int q = 0; q < EACH; ++q)
+                if (i + THREADS * q < end) v[q] = src[i + THREADS * q];
+#pragma unroll
+            for (int q = 0; q < EACH; ++q)
+                if (i + THREADS * q < end) dst[i + THREADS * q] = v[q];
+        } else {
+            for (; i < end; i += THREADS) dst[i] = src[i];
+        }
+    }
+}
+template <int THREADS>
+__device__ __forceinline__ void move_pages(const PoolArgs& a, int pairs, int wg, int wgs) {
+    for (int k = 0; k < a.n_planes; ++k) {
+        const PoolPlane& s = a.plane[k];
+        if (s.unit == 16) move_plane<THREADS, u32x4_t>(s, a.from, a.to, pairs, wg, wgs);
+        else if (s.unit == 4) move_plane<THREADS, uint32_t>(s, a.from, a.to, pairs, wg, wgs);
+        else move_plane<THREADS, uint8_t>(s, a.from, a.to, pairs, wg, wgs);
+    }
+}
+
 // The three launches above in one workgroup, for pools of few pages: ranks in registers, needs and free pages in LDS (launches are
-// what such a call costs: fork and reserve of 4 beams over 2048 rows 26.6 us in six launches, 16.3 in three; of 64 beams over 8192
-// rows 26.1 and 20.1).
+// what such a call costs: fork and reserve of 4 beams over 2048 rows 26.6 us in six launches, 12.7 in two; of 64 beams over 8192
+// rows 26.1 in six and 20.4 in four).  Few bytes are copied there too.
 constexpr int PS_SHORT = 8;      // entries up to which a thread looks through its sequence's by itself
 
 // the sum of v over the threads before this one, and over all
@@ -286,7 +338,7 @@ __device__ __forceinline__ int small_before(int v, int* lds, int* total) {
     return s;
 }
 
-__global__ __launch_bounds__(PS_THREADS) void reserve_small_kernel(PoolArgs a, const int32_t* want, int32_t* missing) {
+__global__ __launch_bounds__(PS_THREADS) void reserve_small_kernel(PoolArgs a, const int32_t* want, int32_t* missing, int copies) {
     __shared__ int32_t list[POOL_SMALL];
     __shared__ int lds[PS_WAVES], need[PS_SEQS], share[PS_SEQS];
     const int tid = threadIdx.x, w = tid >> 6, p0 = PS_EACH * tid;
@@ -311,7 +363,7 @@ __global__ __launch_bounds__(PS_THREADS) void reserve_small_kernel(PoolArgs a, c
             const int n = needs(a, want, b, &shares);
             if ((tid & 63) == 0) need[b] = min(n, POOL_SMALL + 1);   // (more than there are, and sums within 32 bits)
         }
-    int free = 0, have, copies, most;
+    int free = 0, have, all, most;
 #pragma unroll
     for (int i = 0; i < PS_EACH; ++i) free += refs[i] <= 0;
     int r = small_before(free, lds, &have);
@@ -319,7 +371,7 @@ __global__ __launch_bounds__(PS_THREADS) void reserve_small_kernel(PoolArgs a, c
     for (int i = 0; i < PS_EACH; ++i)
         if (refs[i] <= 0) list[r++] = p0 + i;
     // (the scan has waited for every wave)
-    const int at = small_before(tid < a.B ? need[tid] : 0, lds, &most), copy = small_before(q.shared >= 0, lds, &copies);
+    const int at = small_before(tid < a.B ? need[tid] : 0, lds, &most), copy = small_before(q.shared >= 0, lds, &all);
     const bool wide = tid < a.B && share[tid];
     __syncthreads();
     if (tid < a.B) need[tid] = at, share[tid] = !wide ? INT32_MIN : q.shared >= 0 ? copy : -1 - copy;
@@ -358,6 +410,9 @@ __global__ __launch_bounds__(PS_THREADS) void reserve_small_kernel(PoolArgs a, c
         const int s = share[b];
         if (s != INT32_MIN) give(a, want, b, need[b], s < 0 ? -1 - s : s, s >= 0, have, list, missing, false);
     }
+    if (!copies) return;
+    __syncthreads();   // the pairs are there
+    move_pages<PS_THREADS>(a, pairs, 0, 1);
 }
 
 // -------------------------------------------------------------------- compact
@@ -420,61 +475,14 @@ __global__ __launch_bounds__(PS_THREADS) void compact_small_kernel(PoolArgs a, i
 
 // ----------------------------------------------------------------------- copy
 
-template <typename T>
-__device__ __forceinline__ void move_plane(const PoolPlane& s, const int32_t* from, const int32_t* to, int pairs, int wg, int wgs) {
-    const int64_t n = s.bytes / (int64_t)sizeof(T);
-    const int64_t per = n < PO_THREADS ? PO_THREADS / n : 1;        // small pages: several by one workgroup
-    const int64_t pages = (int64_t)pairs * s.layers;
-    const int64_t items = per > 1 ? (pages + per - 1) / per : pages * s.pieces;
-    for (int64_t k = wg; k < items; k += wgs) {
-        int64_t page, i, end;
-        if (per > 1) {
-            page = k * per + threadIdx.x / n;
-            i = threadIdx.x % n;
-            end = threadIdx.x < per * n && page < pages ? n : 0;
-        } else {
-            page = k / s.pieces;
-            const int64_t first = (k % s.pieces) * (PO_PIECE / (int64_t)sizeof(T));
-            i = first + threadIdx.x;
-            end = min(n, first + PO_PIECE / (int64_t)sizeof(T));
-        }
-        const int pair = (int)(page % max(pairs, 1)), layer = (int)(page / max(pairs, 1));
-        if (i >= end) continue;
-        const T* src = reinterpret_cast<const T*>(s.base + layer * s.ls + from[pair] * s.ps);
-        T* dst = reinterpret_cast<T*>(s.base + layer * s.ls + to[pair] * s.ps);
-        if (per > 1) {
-            dst[i] = src[i];
-            continue;
-        }
-        if constexpr (sizeof(T) == 16) {
-            T v[PO_PIECE / 16 / PO_THREADS];
-#pragma unroll
-            for (int q = 0; q < PO_PIECE / 16 / PO_THREADS; ++q)
-                if (i + PO_THREADS * q < end) v[q] = src[i + PO_THREADS * q];
-#pragma unroll
-            for (int q = 0; q < PO_PIECE / 16 / PO_THREADS; ++q)
-                if (i + PO_THREADS * q < end) dst[i + PO_THREADS * q] = v[q];
-        } else {
-            for (; i < end; i += PO_THREADS) dst[i] = src[i];
-        }
-    }
+__global__ __launch_bounds__(PO_THREADS) void pool_copy_kernel(PoolArgs a) {
+    move_pages<PO_THREADS>(a, a.head[PO_PAIRS], blockIdx.x, gridDim.x);
 }
-__device__ __forceinline__ void move_pages(const PoolArgs& a, int wg, int wgs) {
-    const int pairs = a.head[PO_PAIRS];
-    for (int k = 0; k < a.n_planes; ++k) {
-        const PoolPlane& s = a.plane[k];
-        if (s.unit == 16) move_plane<u32x4_t>(s, a.from, a.to, pairs, wg, wgs);
-        else if (s.unit == 4) move_plane<uint32_t>(s, a.from, a.to, pairs, wg, wgs);
-        else move_plane<uint8_t>(s, a.from, a.to, pairs, wg, wgs);
-    }
-}
-
-__global__ __launch_bounds__(PO_THREADS) void pool_copy_kernel(PoolArgs a) { move_pages(a, blockIdx.x, gridDim.x); }
 
 // the copies, and beside them the tables and counts of the pages that move
 __global__ __launch_bounds__(PO_THREADS) void compact_move_kernel(PoolArgs a, int movers) {
     if ((int)blockIdx.x < movers) {
-        move_pages(a, blockIdx.x, movers);
+        move_pages<PO_THREADS>(a, a.head[PO_PAIRS], blockIdx.x, movers);
         return;
     }
     const int pairs = a.head[PO_PAIRS];
@@ -538,8 +546,12 @@ static int movers(const PoolArgs& a, int64_t pairs) {
 hipError_t launch_reserve(const PoolArgs& a, const int32_t* want, int32_t* missing, hipStream_t s) {
     hipError_t e;
     if (a.n_pages <= POOL_SMALL && a.B <= PS_SEQS) {
-        hipLaunchKernelGGL(reserve_small_kernel, dim3(1), dim3(PS_THREADS), 0, s, a, want, missing);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
+        int64_t bytes = 0;   // that are copied at the most
+        for (int k = 0; k < a.n_planes; ++k) bytes += a.B * a.plane[k].layers * a.plane[k].bytes;
+        const int copies = bytes <= POOL_SMALL_COPY;
+        hipLaunchKernelGGL(reserve_small_kernel, dim3(1), dim3(PS_THREADS), 0, s, a, want, missing, copies);
+        e = hipGetLastError();
+        if (e != hipSuccess || copies) return e;
     } else {
         const int seqs = (a.B + PO_WAVES - 1) / PO_WAVES;
         hipLaunchKernelGGL(pool_count_kernel, dim3((unsigned)(a.nb + seqs)), dim3(PO_THREADS), 0, s, a, want, 0);

@@ -416,6 +416,7 @@ struct PoolLayout {
 constexpr int POOL_BLOCK = 4096;
 constexpr int POOL_SMALL = 8192;             // pages, and
 constexpr int64_t POOL_SMALL_TABLE = 1 << 13;   // table entries up to which one workgroup does what is not a copy
+constexpr int64_t POOL_SMALL_COPY = 256 * 1024;  // bytes that it copies as well
 PoolLayout pool_layout(int64_t B, int64_t n_pages, int64_t width);
 hipError_t launch_fork(const PoolArgs& a, const int32_t* from, hipStream_t s);
 hipError_t launch_reserve(const PoolArgs& a, const int32_t* want, int32_t* missing, hipStream_t s);

@@ -265,3 +265,12 @@ def test_captured_replayed_and_on_another_stream(ctx):
     twin.fork(ctx, [0, 0, 0], stream=s)
     twin.reserve(ctx, [n + 9 for n in twin.lens], stream=s)
     twin.compact(ctx, stream=s)
+
+
+@pytest.mark.parametrize("B,size", [(4, 2048), (4, 2049), (9, 5000)])
+def test_large_pages(ctx, B, size):
+    """Pages of many pieces, few enough bytes for one workgroup to copy (4 pages of 16 x 2048 bytes twice) and more."""
+    m = Model([21] * B, 16, spare=3 * B, seed=B, layers=2, sizes=(size,))
+    m.fork(ctx, [0] * (B - 1) + [B - 1])
+    m.reserve(ctx, [22 + 16 * b for b in range(B)])
+    m.compact(ctx)
