@@ -1171,12 +1171,54 @@ __device__ __forceinline__ int run_count8(const Chunk8Args& a, int total) {
     return min(max((total + len - 1) / len, 1), a.runs);
 }
 
+// What scan_units finds, for up to 64 units: each wave for itself, a lane a unit.  What is read of the units goes to LDS as well, behind
+// the 64 first tiles, so that nobody waits for it again.
+constexpr int UNIT_WORDS = 6;
+template <int TILE>
+__device__ __forceinline__ int scan_few(const Chunk8Args& a, int rows, int* pre) {
+    const int lane = threadIdx.x & 63, U = a.B * a.mb;
+    int n = 0;
+    if (lane < U) {
+        const CkUnit x = chunk_unit(a, lane, rows);
+        n = unit_tiles<TILE>(a, x, rows);
+        int* at = pre + 64 + UNIT_WORDS * lane;
+        at[0] = x.nrow;
+        at[1] = (int)x.tok0;      // (n_tok is below 2^31)
+        at[2] = x.nq;
+        at[3] = x.kv;
+        at[4] = x.old;
+    }
+    int upto = n;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int t = __shfl_up(upto, d);
+        if (lane >= d) upto += t;
+    }
+    pre[lane] = upto - n;
+    return __builtin_amdgcn_readlane(upto, 63);
+}
+__device__ __forceinline__ CkUnit few_unit(const Chunk8Args& a, int u, int rows, const int* pre) {
+    const int* at = pre + 64 + UNIT_WORDS * u;
+    CkUnit x;
+    x.b = u / a.mb;
+    x.row0 = (u - x.b * a.mb) * rows;
+    x.nrow = __builtin_amdgcn_readfirstlane(at[0]);
+    x.tok0 = __builtin_amdgcn_readfirstlane(at[1]);
+    x.nq = __builtin_amdgcn_readfirstlane(at[2]);
+    x.kv = __builtin_amdgcn_readfirstlane(at[3]);
+    x.old = __builtin_amdgcn_readfirstlane(at[4]);
+    return x;
+}
+
 template <int RG>
 __global__ __launch_bounds__(Shape8<RG>::THREADS, 1) void chunk8_run_kernel(Chunk8Args a) {
     constexpr int ROWS = 16 * RG, TILE = Shape8<RG>::TILE, THREADS = Shape8<RG>::THREADS;
     __shared__ __align__(1024) uint8_t smem[Shape8<RG>::SMEM];
     __shared__ int pre[CK_MAX_UNITS];
-    const int total = scan_units<TILE, THREADS>(a, ROWS, pre), U = a.B * a.mb;
+    static_assert(64 * (1 + UNIT_WORDS) <= CK_MAX_UNITS, "");
+    const int U = a.B * a.mb;
+    const bool few = U <= 64;
+    const int total = few ? scan_few<TILE>(a, ROWS, pre) : scan_units<TILE, THREADS>(a, ROWS, pre);
     const int n = run_count8<RG>(a, total), g = blockIdx.x;
     if (g == 0)   // units without rows: nothing to join
         for (int u = threadIdx.x; u < U; u += THREADS)
@@ -1184,8 +1226,13 @@ __global__ __launch_bounds__(Shape8<RG>::THREADS, 1) void chunk8_run_kernel(Chun
     if (g >= n) return;
     const int beg = run_start(g, n, total), end = run_start(g + 1, n, total);
     int u = 0;   // the last unit that starts at or before beg
-    for (int step = CK_MAX_UNITS / 2; step > 0; step /= 2)
-        if (u + step < U && pre[u + step] <= beg) u += step;
+    if (few) {
+        const int lane = threadIdx.x & 63;
+        u = __popcll(__ballot(lane < U && pre[lane] <= beg)) - 1;
+    } else {
+        for (int step = CK_MAX_UNITS / 2; step > 0; step /= 2)
+            if (u + step < U && pre[u + step] <= beg) u += step;
+    }
     int at = beg;
     while (at < end) {
         u = __builtin_amdgcn_readfirstlane(u);
@@ -1196,7 +1243,7 @@ __global__ __launch_bounds__(Shape8<RG>::THREADS, 1) void chunk8_run_kernel(Chun
             ++u;
             continue;
         }
-        const CkUnit x = chunk_unit(a, u, ROWS);
+        const CkUnit x = few ? few_unit(a, u, ROWS, pre) : chunk_unit(a, u, ROWS);
         const int t0 = at - base, t1 = min(end, next) - base;
         const bool whole = t0 == 0 && t1 == next - base;
         if (threadIdx.x == 0) {   // for the join: the unit's first and last run, and which of its slots the first one fills
@@ -1226,11 +1273,11 @@ __global__ __launch_bounds__(Shape8<RG>::THREADS, 1) void chunk8_unit_kernel(Chu
 // Joins the parts of a unit that several runs cover: block = (unit, F float4 of a part, in the order the segments leave them),
 // thread = one of them in every GROUPS-th part; then the groups join through LDS, in order.  Few rows: more groups, as a
 // part is small and the loads' latency what counts.
-constexpr int C8J_THREADS = 512, C8J_BATCH = 4;
+constexpr int C8J_THREADS = 512;
 
 template <int RG, int F>
 __global__ __launch_bounds__(C8J_THREADS) void chunk8_join_kernel(Chunk8Args a) {
-    constexpr int GROUPS = C8J_THREADS / F, rows = 16 * RG, per = rows * (D_LAT / 4) / F;
+    constexpr int GROUPS = C8J_THREADS / F, BATCH = F == 32 ? 8 : 4, rows = 16 * RG, per = rows * (D_LAT / 4) / F;
     __shared__ JoinSum sums[GROUPS - 1][F];
     const int u = blockIdx.x / per, grp = threadIdx.x / F;
     const int f = (blockIdx.x % per) * F + threadIdx.x % F, lane = f & 63;
@@ -1245,17 +1292,17 @@ __global__ __launch_bounds__(C8J_THREADS) void chunk8_join_kernel(Chunk8Args a) 
         d = 32 * (blk / rb) + 8 * q + 4 * (lane >> 5);
     }
     const int g0 = a.span[3 * u], g1 = a.span[3 * u + 1], late = a.span[3 * u + 2];
-    if (g0 == g1) return;
     const CkUnit x = chunk_unit(a, u, rows);
+    if (g0 == g1) return;
     const int R = x.row0 + r;
     const bool live = R < x.nrow;
     JoinSum t{-INFINITY, 0.f, f32x4_t{0.f, 0.f, 0.f, 0.f}};
     if (live)
-        for (int s0 = g0 + grp; s0 <= g1; s0 += GROUPS * C8J_BATCH) {
-            float m[C8J_BATCH], l[C8J_BATCH];
-            f32x4_t v[C8J_BATCH];
+        for (int s0 = g0 + grp; s0 <= g1; s0 += GROUPS * BATCH) {
+            float m[BATCH], l[BATCH];
+            f32x4_t v[BATCH];
 #pragma unroll
-            for (int j = 0; j < C8J_BATCH; ++j) {   // all loads in flight
+            for (int j = 0; j < BATCH; ++j) {   // all loads in flight
                 const int run = min(s0 + GROUPS * j, g1);
                 const int64_t slot = 2 * run + (run == g0 ? late : 0);
                 const float* ml = a.part_ml + slot * (rows * 2) + 2 * r;
@@ -1264,7 +1311,7 @@ __global__ __launch_bounds__(C8J_THREADS) void chunk8_join_kernel(Chunk8Args a) 
                 v[j] = *reinterpret_cast<const f32x4_t*>(a.part_o + slot * (rows * D_LAT) + 4 * f);
             }
 #pragma unroll
-            for (int j = 0; j < C8J_BATCH; ++j)
+            for (int j = 0; j < BATCH; ++j)
                 if (s0 + GROUPS * j <= g1) join_add(t, m[j], l[j], v[j], 1.0f);
         }
     if (grp > 0) sums[grp - 1][threadIdx.x % F] = t;
