@@ -1343,7 +1343,7 @@ ChunkSplit chunk8_split(int64_t B, int64_t H, int64_t max_q, int64_t max_kv) {
     s.mb = (rows + 16 * s.qg - 1) / (16 * s.qg);
     s.units = B * s.mb;
     const int64_t tiles = s.mb * cache;
-    s.runs = s.units <= CK_MAX_UNITS && tiles < (1ll << 31) ? CK_RUNS : 0;
+    s.runs = s.units <= CK_MAX_UNITS && tiles < (1ll << 30) ? CK_RUNS : 0;   // (tiles of 32 rows are twice as many)
     s.streams = 1;
     if (s.runs) {
         s.runs = std::max<int64_t>(1, std::min<int64_t>(s.runs, tiles));

@@ -539,6 +539,7 @@ hipError_t launch_fork(const PoolArgs& a, const int32_t* from, hipStream_t s) {
 // workgroups that copy up to `pairs` pages
 static int movers(const PoolArgs& a, int64_t pairs) {
     int64_t n = 0;
+    pairs = std::min<int64_t>(pairs, PO_MOVERS);
     for (int k = 0; k < a.n_planes; ++k) n += pairs * a.plane[k].layers * a.plane[k].pieces;
     return (int)std::min<int64_t>(n, PO_MOVERS);
 }

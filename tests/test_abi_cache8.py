@@ -157,6 +157,15 @@ def test_chunk8_call_refusals(ctx):
     assert lib.vkv_chunk8_workspace_size(None, ctypes.byref(ch), ctypes.byref(n)) == -1
     assert lib.vkv_chunk8_workspace_size(ctypes.byref(pg), None, ctypes.byref(n)) == -1
     assert lib.vkv_chunk8_attend(None, ctypes.byref(pg), ctypes.byref(ch), FAKE, 1 << 40, 0.1, FAKE, FAKE, None) == -1
+    # parts of at most 256 runs, two each, of the units' rows; none where units or tiles are too many to be counted
+    def size(B, max_kv, H, max_q):
+        a = make(vkv._Pages8, PAGES8, B=B, max_kv=max_kv, table_stride=1 << 24)
+        assert lib.vkv_chunk8_workspace_size(ctypes.byref(a), ctypes.byref(make(vkv._Chunk, CHUNK, H=H, max_q=max_q)), ctypes.byref(n)) == 0
+        return n.value
+    for args, rows, runs in (((3, 1000, 16, 1), 16, 48), ((1, 1 << 20, 16, 1), 16, 256), ((4, 8192, 32, 1), 32, 256),
+                             ((4, 32768, 128, 1), 64, 256), ((32, 32768, 128, 1), 128, 256)):
+        assert 0 <= size(*args) - 2 * runs * rows * (512 + 2) * 4 < 20000, args
+    assert size(1100, 1000, 16, 1) == 0 and size(100, 1 << 30, 64, 1) == 0 and size(0xFFFF, 1 << 30, 128, 1) == 0
     # nothing to attend from: no device needed
     assert chunk8(ctx, dict(n_tok=0, q_lat=None, q_rope=None), out=None, lse=None) == 0
     assert chunk8(ctx, dict(max_q=0)) == 0
