@@ -6,7 +6,8 @@
 // A block of R rows of one page is one workgroup's (R >= 4: each of its four waves takes every fourth row) or one
 // wave's.  A wave reads a row's 512 bf16 in one 16-byte load a lane and keeps what it read in registers
 // until the block's largest magnitude is known, so every input is read once; a bf16's magnitude is compared as
-// the integer of its bits, and the scale comes from that integer's exponent.  Bound: HBM (1152 + 640 bytes a row).
+// the integer of its bits, and the scale comes from that integer's exponent.  Bound: HBM (1152 + 640 bytes a row): 28600
+// rows in blocks of 16, 12.1 us, 4.2 TB/s; one row of each of 32 sequences 4.2 us, the launch and three loads one after another.
 #include <algorithm>
 
 #include "vkv_pages.h"
