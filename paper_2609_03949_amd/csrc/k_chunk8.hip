@@ -1162,8 +1162,9 @@ __device__ __forceinline__ void segment8(const Chunk8Args& a, const CkUnit& x, i
 // ------------------------------------------------------------------- kernels
 
 // Runs the tiles of all units are cut into: at most one per CU, and as a run costs its tiles and the writing and reading of its
-// part, some sqrt(tiles) of them, twice as many where parts are small.  16 heads over 4 x 8192 rows 20.6 us, 25.0 with half as many
-// runs; 128 heads over 32768 rows 49.1 us, 55.0 with twice as many.
+// part, some sqrt(tiles) of them, more where parts are small beside a tile's time.  16 heads over 4 x 8192 rows 20.6 us, 25.0 with
+// half as many runs; 32 heads over 32768 rows 26 us, 28 with twice as many, 32 with half as many; 128 heads over 32768 rows in
+// units of 128 rows 49.1 us, 55.0 with twice as many.
 template <int RG>
 __device__ __forceinline__ int run_count8(const Chunk8Args& a, int total) {
     int len = 1;

@@ -5,7 +5,7 @@
 // is reduced to one turn in fp64 (far positions times the first frequencies have many turns), its sine and
 // cosine are fp32.  Bound: HBM (each element read and written once): 16387 tokens of 16 heads, 64 of 192 dims turned, 50 us, 4.0
 // TB/s, where a large copy reaches 4.9; with the input in the last-level cache 40 us, the vector units busy 94% of the cycles.
-// 32 tokens of 128 heads 4.6 us (one workgroup a token 5.2).
+// 32 tokens of 128 heads 4.6 us.
 #include <algorithm>
 
 #include "vkv_internal.h"
