@@ -15,8 +15,8 @@
 //   16       four waves; scores by rows of the tile, so that each code is converted once for either product
 //   32, 64   four waves of scores, by rows of the unit, beside four of outputs
 //   128      four waves, both in one stream of instructions, the scores of a tile between the outputs of the one before
-// 16 sequences of up to 65536 rows, 16 heads: 127 us, 4.7 TB/s.  16 of 32768 rows, 32 and 64 heads: 85 and 112 us.  32 of 32768
-// rows, 128 heads: 275 us; 3 x 512 new tokens over 16384 rows, 128 heads: 4.28 ms, 1.16 PFLOP/s.
+// 16 sequences of up to 65536 rows, 16 heads: 126 us, 4.7 TB/s.  16 of 32768 rows, 32 and 64 heads: 85 and 112 us.  32 of 32768
+// rows, 128 heads: 276 us; 3 x 512 new tokens over 16384 rows, 128 heads: 4.16 ms, 1.19 PFLOP/s.
 #include <algorithm>
 
 #include "vkv_runs.h"
