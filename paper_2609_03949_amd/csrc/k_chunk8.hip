@@ -6,8 +6,8 @@
 //
 // Units of (token, head) rows and the runs of cache tiles they are cut into are those of the bf16
 // cache's kernel.  A tile is 64 or 32 rows of 640 bytes, three or seven of them in LDS (direct loads).  Every 8-bit value is a
-// bf16 value, so the products take bf16 operands that are exact: the conversion of the keys multiplies by their power of
-// two, and the weights carry it for the product with the values.  (The 8-bit products of these matrix cores take half the
+// bf16 and an fp16 value, so the products take operands that are exact: the conversion of the keys multiplies by their power of
+// two, and the weights carry it for the product with the values, which is fp16's.  (The 8-bit products of these matrix cores take half the
 // time, but lose 1e-5 of the sum of the magnitudes where bf16 products lose 1e-8.)  The queries stay in registers, so do the
 // outputs, 128 dims a wave; weights go through LDS.  What the vector units convert is as long as the products it is for, and
 // bounds units of many rows as much as these do; units of few rows are bound by HBM.  So there are three ways to work on a unit,
@@ -36,13 +36,18 @@ constexpr int C8_OFF_STAGE = C8_OFF_P + 16 * 2 * C8_TILE;       // 1 KB aligned,
 constexpr int C8_SMEM = C8_OFF_STAGE + C8_STAGES * C8_STAGE;
 static_assert(C8_OFF_BAD + 16 <= C8_OFF_P && C8_OFF_STAGE % 1024 == 0 && C8_OFF_P % 1024 == 0, "");
 constexpr uint32_t C8_ABSENT = 255;
-// Lag allowed to the softmax reference maximum (log2 units): weights up to 2^16, so that outputs are seldom multiplied; a sum
-// over 2^30 rows of 448 * 2^64 stays below 2^119.  (What lies 2^126 below the reference is 0.)
-constexpr float C8_SLACK = 16.0f;
-constexpr float C8_ROOM = 24.0f;   // and a new reference is that far above the maximum, so that it lasts for scores up to 2^40 times as heavy
+// The weight of a code is the row's softmax weight times its power of two, against a reference that follows the largest of
+// these (in log2 units): a new one makes the largest 2^3, and it is kept until one is above 2^15.  So fp16 holds the
+// weights, with three bits more than bf16 (whose rounding would be as large as the output's own): 11 bits down to 2^-17 of the
+// largest at the least, 8 down to 2^-20, and none below 2^-28; the products and sums are fp32.  The sum of the softmax weights
+// themselves, which are 2^-64 to 2^64 times as large, is fp32 from unrounded ones: between 2^-61 and 2^109.
+constexpr float C8_SLACK = 15.0f, C8_ROOM = -3.0f;
 
 typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x4_t __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 
 // XOR of the 16-byte piece index within the 512 bytes of tile row r, so that what a group of lanes
 // reads at a time lies in 16 pieces that differ modulo 16: the keys' 128-bit reads (16 rows, in two sets
@@ -89,6 +94,24 @@ __device__ __forceinline__ bf16x8_t decode8(uint32_t lo, uint32_t hi, float sc) 
     __builtin_memcpy(&r, v, 16);
     return r;
 }
+// eight codes, exact
+__device__ __forceinline__ f16x8_t value8(uint32_t lo, uint32_t hi) {
+    f16x2_t v[4] = {__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true),
+                    __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true)};
+    f16x8_t r;
+    __builtin_memcpy(&r, v, 16);
+    return r;
+}
+// The largest log2 of a code's weight (but for the reference) among four rows of scores s and scales f; one: all four have one
+// scale, as blocks of four rows and more have.
+__device__ __forceinline__ float log_scale(float f) { return (float)((int)(__float_as_uint(f) >> 23) - 127); }
+__device__ __forceinline__ float top4(float s0, float s1, float s2, float s3, const float* f, float scale_log2, bool one) {
+    if (one) return __builtin_fmaf(fmaxf(fmaxf(s0, s1), fmaxf(s2, s3)), scale_log2, log_scale(f[0]));
+    return fmaxf(fmaxf(__builtin_fmaf(s0, scale_log2, log_scale(f[0])), __builtin_fmaf(s1, scale_log2, log_scale(f[1]))),
+                 fmaxf(__builtin_fmaf(s2, scale_log2, log_scale(f[2])), __builtin_fmaf(s3, scale_log2, log_scale(f[3]))));
+}
+// v times 2^d (d <= 0) where 2^d alone may be below what fp32 holds
+__device__ __forceinline__ float times_power(float v, float half) { return v * half * half; }
 __device__ __forceinline__ uint32_t drop_nan(uint32_t w) {   // NaN codes become 0
     const uint32_t n = (((w & 0x7F7F7F7Fu) + 0x01010101u) >> 7) & 0x01010101u;
     return w & ~((n << 8) - n);
@@ -357,19 +380,18 @@ __device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit
                     s4[i] = -INFINITY;
                 }
         }
-        float top = fmaxf(fmaxf(s4[0], s4[1]), fmaxf(s4[2], s4[3]));
-        top = allreduce_groups(top, [](float p, float q) { return fmaxf(p, q); }) * a.scale_log2;
+        const float top = allreduce_groups(top4(s4[0], s4[1], s4[2], s4[3], sp, a.scale_log2, a.bshift >= 2), [](float p, float q) { return fmaxf(p, q); });
         const bool wave_bad = __ballot(bad) != 0;
         float ps;
         auto weights = [&]() __attribute__((always_inline)) {
             const float ref = m_run == -INFINITY ? 0.f : m_run;
-            bf16x4_t p4;
+            f16x4_t p4;
             ps = 0.f;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s4[i], a.scale_log2, -ref));
                 ps += p;
-                p4[i] = (__bf16)(p * sp[i]);
+                p4[i] = (_Float16)(p * sp[i]);
             }
             lds_write_u2(lds0 + C8_OFF_P + c * (2 * C8_TILE) + 16 * ((2 * w + (g >> 1)) ^ rope_xor(c)) + 8 * (g & 1),
                          __builtin_bit_cast(u32x2_t, p4));
@@ -384,8 +406,9 @@ __device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit
                               fmaxf(__uint_as_float(tops[2]), __uint_as_float(tops[3])));
         const bool move = m > m_run + C8_SLACK;
         if (__ballot(move)) {   // the same in every wave
-            const float next = move ? m + C8_ROOM : m_run, al = move ? __builtin_amdgcn_exp2f(m_run - next) : 1.0f;
-            l_run *= al;
+            const float next = move ? m + C8_ROOM : m_run, half = move ? __builtin_amdgcn_exp2f(0.5f * (m_run - next)) : 1.0f;
+            const float al = half * half;
+            l_run = times_power(l_run, half);
             m_run = next;
 #pragma unroll
             for (int d = 0; d < NO; ++d)
@@ -422,8 +445,8 @@ __device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit
             if constexpr (i + VD < N) vload(std::integral_constant<int, i + VD>{});
             if constexpr (i == 0) lds_wait<VD + 1>(pf[0], pf[1]);
             lds_wait<(i + VD < N) ? VD : N - 1 - i>(vv[i % (VD + 1)]);
-            const bf16x8_t v = decode8(vv[i % (VD + 1)][0], vv[i % (VD + 1)][1], 1.0f);
-            o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8_t, pf[s]), o[d], 0, 0, 0);
+            const f16x8_t v = value8(vv[i % (VD + 1)][0], vv[i % (VD + 1)][1]);
+            o[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, __builtin_bit_cast(f16x8_t, pf[s]), o[d], 0, 0, 0);
         });
     }
 
@@ -622,7 +645,8 @@ __device__ __forceinline__ float fused8(Big8& z, uint32_t lds0, uint32_t sv, uin
         sk2[1] = __uint_as_float(sw[1]);
     }
     // the operands of the next products: a key's is decoded while the product before it runs, a step's values during the last one
-    bf16x8_t kd, vd[2];
+    bf16x8_t kd;
+    f16x8_t vd[2];
     auto vwait = [&](auto ic, auto n) {
         lds_wait<decltype(n)::value>(vv[decltype(ic)::value % 2]);
     };
@@ -637,7 +661,7 @@ __device__ __forceinline__ float fused8(Big8& z, uint32_t lds0, uint32_t sv, uin
     }
     if constexpr (OUT) {
         vwait(std::integral_constant<int, 0>{}, std::integral_constant<int, (B8_AHEAD - 1) * (SCORES ? 3 : 1)>{});
-        vd[0] = decode8(vv[0][0], vv[0][1], 1.0f);
+        vd[0] = value8(vv[0][0], vv[0][1]);
     }
     static_for<0, (SCORES ? B8_STEPS : B8_OUT)>([&](auto ic) {
         constexpr int i = decltype(ic)::value;
@@ -667,11 +691,11 @@ __device__ __forceinline__ float fused8(Big8& z, uint32_t lds0, uint32_t sv, uin
                 constexpr int s = i >> 2, d = i & 3;
                 // the weights came at the end of the last step: behind each are the later ones, and this step's keys and values
                 if constexpr (d == 0) lds_wait<3 - q + reads_keys<SCORES, OUT>(i) + reads_values<SCORES, OUT>(i)>(pf[q]);
-                z.o[d][q] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vd[i & 1], __builtin_bit_cast(bf16x8_t, pf[q]), z.o[d][q], 0, 0, 0);
+                z.o[d][q] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vd[i & 1], __builtin_bit_cast(f16x8_t, pf[q]), z.o[d][q], 0, 0, 0);
                 if constexpr (d == 3 && more) pload(std::integral_constant<int, s + 1>{}, rc);
                 if constexpr (more) {        // a quarter of the next step's values
                     const uint32_t word = vv[(i + 1) % 2][q >> 1];
-                    const bf16x2_t two = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(word, 1.0f, q & 1);
+                    const f16x2_t two = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(word, 1.0f, q & 1);
                     vd[(i + 1) & 1][2 * q] = two[0];
                     vd[(i + 1) & 1][2 * q + 1] = two[1];
                 }
@@ -748,31 +772,38 @@ __device__ __forceinline__ void chunk8_big_segment(const Chunk8Args& a, const Ck
                     }
                 }
         }
-        float top = z.s[0][0];
+        static_for<0, 4>([&](auto ic) { lds_wait<0>(f[2 * decltype(ic)::value], f[2 * decltype(ic)::value + 1]); });
+        float top = -INFINITY;
+        auto tops = [&](bool one) __attribute__((always_inline)) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, z.s[b][i]);
-        top = half_max(top) * a.scale_log2;
+            for (int q = 0; q < 8; ++q) {
+                const float scales[4] = {__uint_as_float(f[q][0]), __uint_as_float(f[q][1]), __uint_as_float(f[q][2]), __uint_as_float(f[q][3])};
+                const f32x16_t& s = z.s[q >> 2];
+                const int i = 4 * (q & 3);
+                top = fmaxf(top, top4(s[i], s[i + 1], s[i + 2], s[i + 3], scales, a.scale_log2, one));
+            }
+        };
+        if (a.bshift >= 2) tops(true);
+        else tops(false);
+        top = half_max(top);
         const bool move = top > m_run + C8_SLACK;
         top += C8_ROOM;
-        const float alpha = move ? __builtin_amdgcn_exp2f(m_run - top) : 1.0f;
+        const float half = move ? __builtin_amdgcn_exp2f(0.5f * (m_run - top)) : 1.0f, alpha = half * half;
         if (move) m_run = top;
-        l_run *= alpha;
+        l_run = times_power(l_run, half);
         const float ref = m_run == -INFINITY ? 0.f : m_run;
         const uint32_t flags = (__ballot(move) ? 1u : 0u) | (__ballot(bad) ? 2u : 0u);
         const uint32_t pa = lds0 + B8_OFF_P + (k & 1) * B8_P + (32 * w + c) * (2 * C8_TILE);
         const uint32_t px = rope_xor(c);
         float psum = 0.f;
-        static_for<0, 4>([&](auto ic) { lds_wait<0>(f[2 * decltype(ic)::value], f[2 * decltype(ic)::value + 1]); });
         static_for<0, 4>([&](auto ic) {        // 16 rows of the tile, eight of them this lane's
             constexpr int q = decltype(ic)::value, b = q >> 1;
-            bf16x8_t p8;
+            f16x8_t p8;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(z.s[b][8 * (q & 1) + i], a.scale_log2, -ref));
                 psum += p;
-                p8[i] = (__bf16)(p * __uint_as_float(f[2 * q + (i >> 2)][i & 3]));
+                p8[i] = (_Float16)(p * __uint_as_float(f[2 * q + (i >> 2)][i & 3]));
             }
             const u32x4_t v = __builtin_bit_cast(u32x4_t, p8);
             lds_write_u4(pa + 16 * ((2 * q + h) ^ px), v);
@@ -974,29 +1005,30 @@ __device__ __forceinline__ void mid_scores(const Chunk8Args& a, const CkUnit& x,
                         s4[b][i] = -INFINITY;
                     }
         }
-        float top = s4[0][0];
+        lds_wait<0>(f[0], f[1]);
+        float top = -INFINITY;
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) top = fmaxf(top, s4[b][i]);
-        top = allreduce_groups(top, [](float p, float q) { return fmaxf(p, q); }) * a.scale_log2;
+        for (int b = 0; b < 2; ++b) {
+            const float scales[4] = {__uint_as_float(f[b][0]), __uint_as_float(f[b][1]), __uint_as_float(f[b][2]), __uint_as_float(f[b][3])};
+            top = fmaxf(top, top4(s4[b][0], s4[b][1], s4[b][2], s4[b][3], scales, a.scale_log2, a.bshift >= 2));
+        }
+        top = allreduce_groups(top, [](float p, float q) { return fmaxf(p, q); });
         const bool move = top > m_run + C8_SLACK;
         top += C8_ROOM;
-        const float alpha = move ? __builtin_amdgcn_exp2f(m_run - top) : 1.0f;
+        const float half = move ? __builtin_amdgcn_exp2f(0.5f * (m_run - top)) : 1.0f, alpha = half * half;
         if (move) m_run = top;
-        l_run *= alpha;
+        l_run = times_power(l_run, half);
         const float ref = m_run == -INFINITY ? 0.f : m_run;
         const uint32_t flags = (__ballot(move) ? 1u : 0u) | (__ballot(bad) ? 2u : 0u);
-        lds_wait<0>(f[0], f[1]);
         const int row = 16 * w + c;
         static_for<0, 2>([&](auto bc) {
             constexpr int b = decltype(bc)::value;
-            bf16x4_t p4;
+            f16x4_t p4;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s4[b][i], a.scale_log2, -ref));
                 l_run += p;           // this lane's share of the sum
-                p4[i] = (__bf16)(p * __uint_as_float(f[b][i]));
+                p4[i] = (_Float16)(p * __uint_as_float(f[b][i]));
             }
             // slots of a row: in each 16 of them rows 4 h + (0..3, 8..11) for half h
             lds_write_u2(lds0 + M8_OFF_P + M8_P * (k & 1) + row * (2 * M8_TILE) + 16 * ((2 * b + (g & 1)) ^ weight_xor(row)) + 8 * (g >> 1),
@@ -1091,10 +1123,10 @@ __device__ __forceinline__ void mid_outputs(const Chunk8Args& a, const CkUnit& x
             if constexpr (i + VD < N) vload(std::integral_constant<int, i + VD>{});
             if constexpr (i == 0) static_for<0, 2 * RB>([&](auto q) { lds_wait<VD + 1>(pf[decltype(q)::value / RB][decltype(q)::value % RB]); });
             lds_wait<(i + VD < N) ? VD : N - 1 - i>(vv[i % (VD + 1)]);
-            const bf16x8_t v = decode8(vv[i % (VD + 1)][0], vv[i % (VD + 1)][1], 1.0f);
+            const f16x8_t v = value8(vv[i % (VD + 1)][0], vv[i % (VD + 1)][1]);
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb)
-                o[d][rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8_t, pf[s][rb]), o[d][rb], 0, 0, 0);
+                o[d][rb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, __builtin_bit_cast(f16x8_t, pf[s][rb]), o[d][rb], 0, 0, 0);
         });
         // after the waits for every LDS operation, which would be waits for these scalar loads too
         if (k + 7 < nt) loader.fetch(t0 + k + 7);
@@ -1271,6 +1303,21 @@ __global__ __launch_bounds__(Shape8<RG>::THREADS, 1) void chunk8_unit_kernel(Chu
     segment8<RG>(a, x, 0, n, nullptr, nullptr, smem);
 }
 
+// x += y of reference m: references 2^128 apart still add up right, as a sum may be 2^64 times what its reference stands for
+__device__ __forceinline__ void join8_add(JoinSum& x, float m, float l, const f32x4_t& v) {
+    if (m > x.M) {
+        const float half = x.M == -INFINITY ? 1.0f : exp2f(0.5f * (x.M - m));
+        x.L = times_power(x.L, half);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x.acc[i] *= half * half;
+        x.M = m;
+    }
+    const float half = m == -INFINITY ? 1.0f : exp2f(0.5f * (m - x.M));
+    x.L += times_power(l, half);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x.acc[i] += half * half * v[i];
+}
+
 // Joins the parts of a unit that several runs cover: block = (unit, F float4 of a part, in the order the segments leave them),
 // thread = one of them in every GROUPS-th part; then the groups join through LDS, in order.  Few rows: more groups, as a
 // part is small and the loads' latency what counts.
@@ -1313,7 +1360,7 @@ __global__ __launch_bounds__(C8J_THREADS) void chunk8_join_kernel(Chunk8Args a) 
             }
 #pragma unroll
             for (int j = 0; j < BATCH; ++j)
-                if (s0 + GROUPS * j <= g1) join_add(t, m[j], l[j], v[j], 1.0f);
+                if (s0 + GROUPS * j <= g1) join8_add(t, m[j], l[j], v[j]);
         }
     if (grp > 0) sums[grp - 1][threadIdx.x % F] = t;
     __syncthreads();
@@ -1321,7 +1368,7 @@ __global__ __launch_bounds__(C8J_THREADS) void chunk8_join_kernel(Chunk8Args a) 
 #pragma unroll
     for (int i = 0; i < GROUPS - 1; ++i) {
         const JoinSum y = sums[i][threadIdx.x];
-        join_add(t, y.M, y.L, y.acc, 1.0f);
+        join8_add(t, y.M, y.L, y.acc);
     }
     const int64_t row = x.tok0 * a.H + R;
     const bool none = t.M == -INFINITY && t.L == 0.f;

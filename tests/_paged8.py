@@ -91,6 +91,11 @@ class Case8:
         lat = decode(raw[:, :512], self.scale[p, r // self.block])
         return torch.cat([lat, raw[:, 512:].contiguous().view(torch.bfloat16).double().cpu()], 1)
 
+    def scales(self, b):
+        """The power of two of each of sequence b's rows, fp64 on the CPU."""
+        p, r = self.where[b]
+        return torch.pow(2.0, self.scale[p, r // self.block].cpu().double().clamp(BYTE_MIN, BYTE_MAX) - 127)
+
     def seen(self, b):
         """[nq, kv]: which rows each new token sees."""
         n, nq = self.kv_lens[b], self.q_lens[b]

@@ -2,9 +2,11 @@
 rows, single tokens and chunks, every split of the rows and of the work, pages and blocks of every size, tokens that
 see nothing, NaN where a token does not look, scales at their bounds, strides, graphs, streams.
 
-The bounds are those of the bf16 cache's test: the operands are exact (every code times its power of two is a bf16
-value), so the same roundings remain: fp32 sums of 576 products, the weights' rounding to bf16 (times a power of two,
-which is exact), fp32 sums over the rows, the output's rounding to bf16."""
+The operands are exact (every code is a bf16 and an fp16 value, times its power of two too in bf16), so the bounds are those of the
+bf16 cache's test, in which the weights' rounding is the one to bf16, and one more.  Here w_j, the softmax weight times the power of
+two, is rounded to fp16: half a step of 2^-11 of it, an eighth of bf16's, where it is 2^-14 or more; below by 2^-25 at the most,
+where the reference makes the largest w_j at least 2^3 in the end (and makes what came before smaller, errors with it).
+So a weight is off by 2^-28 of the largest at most, and an output's dim by that times the sum of its codes' magnitudes."""
 import math
 
 import pytest
@@ -64,6 +66,10 @@ def compare(x, out, lse, seen=None, only=None, scale=SCALE):
             kv = torch.where(vis.any(0)[:, None], kv, 0.0)      # what no token sees has no say
             q = x.q[at:at + nq].reshape(nq * x.H, 576)
             o, l, ot, lt = attention(q, kv, kv[:, :512], vis, scale)
+            if kv.shape[0]:
+                f = x.scales(b)
+                p = torch.where(vis, torch.exp(scale * (q.double().cpu() @ kv.T) - torch.where(vis.any(1), l, 0.0)[:, None]), 0.0)
+                ot = ot + 2.0 ** -28 * (p * f).amax(1)[:, None] * (vis.double() @ (kv[:, :512].abs() / f[:, None]))
             check(f"lse of sequence {b}", lse[at:at + nq].reshape(-1), l, lt)
             check(f"out of sequence {b}", out[at:at + nq].reshape(-1, 512), o, ot)
         at += nq
@@ -204,6 +210,43 @@ def test_scales_at_their_bounds(ctx):
         x.scale[p, r // 16] = torch.tensor(bytes_, dtype=torch.uint8, device=DEV).repeat_interleave(16)
     q[1:] *= 2.0 ** -70
     x.q[..., :512] = q
+    compare(x, *run(ctx, x))
+
+
+@pytest.mark.parametrize("page,block", [(1, 1), (16, 2), (16, 4)])
+def test_scores_against_scales(ctx, page, block):
+    """Rows of heavy scores and small scales beside rows of light scores and large ones, 2^100 apart: what is left of either
+    in the outputs, and the sums, which the small ones make up."""
+    x = Case8([200, 90], [1, 2], 16, page=page, block=block, seed=21)
+    for b in range(2):
+        p, r = x.where[b]
+        n = len(p)
+        heavy = (torch.arange(n, device=DEV) // block) % 2 == 0
+        # one direction of the queries and keys decides the scores: branch dim 0
+        branch = x.cache[p, r, 512:].contiguous().view(torch.bfloat16).clone()
+        branch[:, 0] = torch.where(heavy, 10.0, -10.0).to(torch.bfloat16)
+        x.cache[p, r, 512:] = branch.view(torch.uint8)
+        x.scale[p, r // block] = torch.where(heavy, 70, 170).to(torch.uint8)
+    for tilt in (0.0, 60.0, 48.0, 30.0):             # in nats a unit of the branch: 2^(2 tilt 10 / 13.9 / ln 2) between the rows
+        x.q[..., :512] = 0
+        x.q[..., 512:] = 0
+        x.q[..., 512] = tilt
+        x.q_lat, x.q_rope = x.q[..., :512].contiguous(), x.q[..., 512:].contiguous()
+        compare(x, *run(ctx, x))
+
+
+def test_a_heavy_row_among_many(ctx):
+    """One row e^10 times as heavy as each of 60000 others, which together outweigh it: the light ones' weights count."""
+    n = 60000
+    x = Case8([n], [1], 16, page=64, block=16, seed=22)
+    p, r = x.where[0]
+    branch = torch.zeros(n, 64, dtype=torch.bfloat16, device=DEV)
+    branch[7, 0] = 10.0 / SCALE
+    x.cache[p, r, 512:] = branch.view(torch.uint8)
+    x.q[..., :512] *= 0.05
+    x.q[..., 512:] = 0
+    x.q[..., 512] = 1.0
+    x.q_lat, x.q_rope = x.q[..., :512].contiguous(), x.q[..., 512:].contiguous()
     compare(x, *run(ctx, x))
 
 
