@@ -42,6 +42,14 @@ constexpr uint32_t C8_ABSENT = 255;
 // largest at the least, 8 down to 2^-20, and none below 2^-28; the products and sums are fp32.  The sum of the softmax weights
 // themselves, which are 2^-64 to 2^64 times as large, is fp32 from unrounded ones: between 2^-61 and 2^109.
 constexpr float C8_SLACK = 15.0f, C8_ROOM = -3.0f;
+// Does the reference m of this lane's row, whose largest is top, move?  Where one of the wave's rows has to, all do that have come
+// nearer by a bit or more: the outputs are multiplied for all of them at once, and seldom (128-row units with prompts of
+// 512 tokens 4.56 ms where each row moved for itself).
+__device__ __forceinline__ bool moves(float top, float m) {
+    bool move = top > m + C8_SLACK;
+    if (__ballot(move)) move = top > m + (1.0f - C8_ROOM);
+    return move;
+}
 
 typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
@@ -269,12 +277,24 @@ typedef Loader8<16, C8_OFF_WORD, C8_OFF_NOTE, false> Loader64Lean;
 
 // ------------------------------------------------------------------ a segment
 
-// v *= f for an accumulator register: said so that the compiler keeps the outputs where the products add to them (with
-// a plain product it copies all of them to the other registers and back around every tile).  The products that wrote v and
+// v *= f for four accumulator registers: said so that the compiler keeps the outputs where the products add to them (with
+// plain products it copies all of them to the other registers and back around every tile).  The products that wrote v and
 // those that read it next are a barrier away, as far as their wait states go.
-__device__ __forceinline__ void scale_acc(float& v, float f) {
-    float t;
-    asm volatile("v_accvgpr_read_b32 %1, %0\n\tv_mul_f32 %1, %1, %2\n\tv_accvgpr_write_b32 %0, %1" : "+a"(v), "=&v"(t) : "v"(f));
+__device__ __forceinline__ void scale_acc(float& v0, float& v1, float& v2, float& v3, float f) {
+    float t0, t1, t2, t3;
+    asm volatile("v_accvgpr_read_b32 %4, %0\n\tv_accvgpr_read_b32 %5, %1\n\tv_accvgpr_read_b32 %6, %2\n\tv_accvgpr_read_b32 %7, %3\n\t"
+                 "v_mul_f32 %4, %4, %8\n\tv_mul_f32 %5, %5, %8\n\tv_mul_f32 %6, %6, %8\n\tv_mul_f32 %7, %7, %8\n\t"
+                 "v_accvgpr_write_b32 %0, %4\n\tv_accvgpr_write_b32 %1, %5\n\tv_accvgpr_write_b32 %2, %6\n\tv_accvgpr_write_b32 %3, %7"
+                 : "+a"(v0), "+a"(v1), "+a"(v2), "+a"(v3), "=&v"(t0), "=&v"(t1), "=&v"(t2), "=&v"(t3) : "v"(f));
+}
+template <int N, typename V>
+__device__ __forceinline__ void scale_all(V& o, float f) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+        float v0 = o[i], v1 = o[i + 1], v2 = o[i + 2], v3 = o[i + 3];
+        scale_acc(v0, v1, v2, v3, f);
+        o[i] = v0, o[i + 1] = v1, o[i + 2] = v2, o[i + 3] = v3;
+    }
 }
 
 // Tiles [t0, t1) of unit x (16 rows) by one workgroup.  part: where an incomplete unit's (O, m, l) go, or null (outputs).
@@ -320,7 +340,7 @@ __device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit
     f32x4_t o[NO];
 #pragma unroll
     for (int d = 0; d < NO; ++d) o[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    float m_run = -INFINITY, l_run = 0.f;
+    float m_run = -INFINITY, m_top = -INFINITY, l_run = 0.f;   // reference, largest, sum
 
     int sg = 0;   // the stage of tile k
     for (int k = 0; k < nt; ++k) {
@@ -402,22 +422,16 @@ __device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit
         lds_barrier();
         u32x4_t bads = lds_read_u4<C8_OFF_BAD>(lds0), tops = lds_read_u4<C8_OFF_TOP>(lds0 + c * 16);
         lds_wait<0>(bads, tops);
-        const float m = fmaxf(fmaxf(__uint_as_float(tops[0]), __uint_as_float(tops[1])),
-                              fmaxf(__uint_as_float(tops[2]), __uint_as_float(tops[3])));
-        const bool move = m > m_run + C8_SLACK;
+        m_top = fmaxf(m_top, fmaxf(fmaxf(__uint_as_float(tops[0]), __uint_as_float(tops[1])),
+                                   fmaxf(__uint_as_float(tops[2]), __uint_as_float(tops[3]))));
+        const bool move = moves(m_top, m_run);
         if (__ballot(move)) {   // the same in every wave
-            const float next = move ? m + C8_ROOM : m_run, half = move ? __builtin_amdgcn_exp2f(0.5f * (m_run - next)) : 1.0f;
+            const float next = move ? m_top + C8_ROOM : m_run, half = move ? __builtin_amdgcn_exp2f(0.5f * (m_run - next)) : 1.0f;
             const float al = half * half;
             l_run = times_power(l_run, half);
             m_run = next;
 #pragma unroll
-            for (int d = 0; d < NO; ++d)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float v = o[d][i];
-                    scale_acc(v, al);
-                    o[d][i] = v;
-                }
+            for (int d = 0; d < NO; ++d) scale_all<4>(o[d], al);
             weights();
             lds_barrier();
         }
@@ -745,7 +759,7 @@ __device__ __forceinline__ void chunk8_big_segment(const Chunk8Args& a, const Ck
         for (int r = 0; r < 4; ++r)
 #pragma unroll
             for (int i = 0; i < 16; ++i) z.o[d][r][i] = 0.f;
-    float m_run = -INFINITY, l_run = 0.f;
+    float m_run = -INFINITY, m_top = -INFINITY, l_run = 0.f;   // reference, largest, sum
 
     // the weights of the tile whose scores are there (rows from u0 on), into buffer k & 1
     auto weights = [&](int k, int u0, float sc) __attribute__((always_inline)) {
@@ -785,11 +799,10 @@ __device__ __forceinline__ void chunk8_big_segment(const Chunk8Args& a, const Ck
         };
         if (a.bshift >= 2) tops(true);
         else tops(false);
-        top = half_max(top);
-        const bool move = top > m_run + C8_SLACK;
-        top += C8_ROOM;
-        const float half = move ? __builtin_amdgcn_exp2f(0.5f * (m_run - top)) : 1.0f, alpha = half * half;
-        if (move) m_run = top;
+        m_top = fmaxf(m_top, half_max(top));
+        const bool move = moves(m_top, m_run);
+        const float next = m_top + C8_ROOM, half = move ? __builtin_amdgcn_exp2f(0.5f * (m_run - next)) : 1.0f, alpha = half * half;
+        if (move) m_run = next;
         l_run = times_power(l_run, half);
         const float ref = m_run == -INFINITY ? 0.f : m_run;
         const uint32_t flags = (__ballot(move) ? 1u : 0u) | (__ballot(bad) ? 2u : 0u);
@@ -840,13 +853,7 @@ __device__ __forceinline__ void chunk8_big_segment(const Chunk8Args& a, const Ck
                 uint32_t f = lds_read_u1(lds0 + B8_OFF_ALPHA + 512 * (k & 1) + (32 * rb + c) * 4);
                 lds_wait<0>(f);
 #pragma unroll
-                for (int d = 0; d < 4; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        float v = z.o[d][rb][i];
-                        scale_acc(v, __uint_as_float(f));
-                        z.o[d][rb][i] = v;
-                    }
+                for (int d = 0; d < 4; ++d) scale_all<16>(z.o[d][rb], __uint_as_float(f));
             }
         }
         if (all & 2u) clean_tile(stage(sg), w, lane);
@@ -939,6 +946,7 @@ __device__ __forceinline__ void mid_scores(const Chunk8Args& a, const CkUnit& x,
 #pragma unroll
     for (int s = 0; s < 18; ++s) asm volatile("" : "+a"(qf[s]));   // no wait for them inside the tile loop
 
+    float m_top = -INFINITY;   // the rows' largest
     int sg = 0;   // the stage of tile k
     for (int k = 0; k < nt; ++k) {
         lds_barrier();
@@ -1012,11 +1020,10 @@ __device__ __forceinline__ void mid_scores(const Chunk8Args& a, const CkUnit& x,
             const float scales[4] = {__uint_as_float(f[b][0]), __uint_as_float(f[b][1]), __uint_as_float(f[b][2]), __uint_as_float(f[b][3])};
             top = fmaxf(top, top4(s4[b][0], s4[b][1], s4[b][2], s4[b][3], scales, a.scale_log2, a.bshift >= 2));
         }
-        top = allreduce_groups(top, [](float p, float q) { return fmaxf(p, q); });
-        const bool move = top > m_run + C8_SLACK;
-        top += C8_ROOM;
-        const float half = move ? __builtin_amdgcn_exp2f(0.5f * (m_run - top)) : 1.0f, alpha = half * half;
-        if (move) m_run = top;
+        m_top = fmaxf(m_top, allreduce_groups(top, [](float p, float q) { return fmaxf(p, q); }));
+        const bool move = moves(m_top, m_run);
+        const float next = m_top + C8_ROOM, half = move ? __builtin_amdgcn_exp2f(0.5f * (m_run - next)) : 1.0f, alpha = half * half;
+        if (move) m_run = next;
         l_run = times_power(l_run, half);
         const float ref = m_run == -INFINITY ? 0.f : m_run;
         const uint32_t flags = (__ballot(move) ? 1u : 0u) | (__ballot(bad) ? 2u : 0u);
@@ -1099,13 +1106,7 @@ __device__ __forceinline__ void mid_outputs(const Chunk8Args& a, const CkUnit& x
                 uint32_t al = lds_read_u1(lds0 + M8_OFF_ALPHA + 256 * (k & 1) + (32 * rb + r) * 4);
                 lds_wait<0>(al);
 #pragma unroll
-                for (int d = 0; d < 4; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        float v = o[d][rb][i];
-                        scale_acc(v, __uint_as_float(al));
-                        o[d][rb][i] = v;
-                    }
+                for (int d = 0; d < 4; ++d) scale_all<16>(o[d][rb], __uint_as_float(al));
             }
         }
         if (all & 2u) clean_dims(st, w, lane);
