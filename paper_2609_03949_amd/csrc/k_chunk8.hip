@@ -37,14 +37,15 @@ constexpr int C8_SMEM = C8_OFF_STAGE + C8_STAGES * C8_STAGE;
 static_assert(C8_OFF_BAD + 16 <= C8_OFF_P && C8_OFF_STAGE % 1024 == 0 && C8_OFF_P % 1024 == 0, "");
 constexpr uint32_t C8_ABSENT = 255;
 // The weight of a code is the row's softmax weight times its power of two, against a reference that follows the largest of
-// these (in log2 units): a new one makes the largest 2^3, and it is kept until one is above 2^15.  So fp16 holds the
-// weights, with three bits more than bf16 (whose rounding would be as large as the output's own): 11 bits down to 2^-17 of the
-// largest at the least, 8 down to 2^-20, and none below 2^-28; the products and sums are fp32.  The sum of the softmax weights
-// themselves, which are 2^-64 to 2^64 times as large, is fp32 from unrounded ones: between 2^-61 and 2^109.
-constexpr float C8_SLACK = 15.0f, C8_ROOM = -3.0f;
+// these (in log2 units): a new one makes the largest 1, and it is kept until one is above 2^15.  So fp16 holds the
+// weights, with three bits more than bf16 (whose rounding would be as large as the output's own): 11 bits down to 2^-14 of the
+// largest at the least, 8 down to 2^-17, and none below 2^-25; the products and sums are fp32.  (A new largest of 2^-20,
+// and room for 2^35, was 5% faster, and would leave no bits to rows that are light one by one and heavy together.)  The sum of
+// the softmax weights themselves, which are 2^-64 to 2^64 times as large, is fp32 from unrounded ones: between 2^-64 and 2^109.
+constexpr float C8_SLACK = 15.0f, C8_ROOM = 0.0f;
+constexpr float C8_MOST = 32768.0f;   // 2^SLACK: weights are taken as if they were no more, and again where one is
 // Does the reference m of this lane's row, whose largest is top, move?  Where one of the wave's rows has to, all do that have come
-// nearer by a bit or more: the outputs are multiplied for all of them at once, and seldom (128-row units with prompts of
-// 512 tokens 4.56 ms where each row moved for itself).
+// nearer by a bit or more: the outputs are multiplied for all of them at once, and seldom.
 __device__ __forceinline__ bool moves(float top, float m) {
     bool move = top > m + C8_SLACK;
     if (__ballot(move)) move = top > m + (1.0f - C8_ROOM);
@@ -110,11 +111,9 @@ __device__ __forceinline__ f16x8_t value8(uint32_t lo, uint32_t hi) {
     __builtin_memcpy(&r, v, 16);
     return r;
 }
-// The largest log2 of a code's weight (but for the reference) among four rows of scores s and scales f; one: all four have one
-// scale, as blocks of four rows and more have.
-__device__ __forceinline__ float log_scale(float f) { return (float)((int)(__float_as_uint(f) >> 23) - 127); }
-__device__ __forceinline__ float top4(float s0, float s1, float s2, float s3, const float* f, float scale_log2, bool one) {
-    if (one) return __builtin_fmaf(fmaxf(fmaxf(s0, s1), fmaxf(s2, s3)), scale_log2, log_scale(f[0]));
+__device__ __forceinline__ float log_scale(float f) { return (float)((int)(__float_as_uint(f) >> 23) - 127); }   // of a power of two
+// The largest log2 of a code's weight (but for the reference) among four rows of scores s and scales f (powers of two).
+__device__ __forceinline__ float top4(float s0, float s1, float s2, float s3, const float* f, float scale_log2) {
     return fmaxf(fmaxf(__builtin_fmaf(s0, scale_log2, log_scale(f[0])), __builtin_fmaf(s1, scale_log2, log_scale(f[1]))),
                  fmaxf(__builtin_fmaf(s2, scale_log2, log_scale(f[2])), __builtin_fmaf(s3, scale_log2, log_scale(f[3]))));
 }
@@ -340,7 +339,7 @@ __device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit
     f32x4_t o[NO];
 #pragma unroll
     for (int d = 0; d < NO; ++d) o[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    float m_run = -INFINITY, m_top = -INFINITY, l_run = 0.f;   // reference, largest, sum
+    float m_run = -INFINITY, w_top = 0.f, l_run = 0.f;   // reference, this lane's largest weight since it moved, sum
 
     int sg = 0;   // the stage of tile k
     for (int k = 0; k < nt; ++k) {
@@ -389,7 +388,7 @@ __device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit
             }
         });
 
-        // ---- masks, the waves' maxima
+        // ---- masks
         bool bad = false;
         if (u0 + C8_TILE - 1 > lim_lo || absent != 0) {
             const uint32_t gone = (uint32_t)(absent >> (16 * w + 4 * g));
@@ -400,41 +399,53 @@ __device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit
                     s4[i] = -INFINITY;
                 }
         }
-        const float top = allreduce_groups(top4(s4[0], s4[1], s4[2], s4[3], sp, a.scale_log2, a.bshift >= 2), [](float p, float q) { return fmaxf(p, q); });
-        const bool wave_bad = __ballot(bad) != 0;
-        float ps;
+        // ---- weights against the reference that every wave has, and again where one of them is too large for it
+        float ps, most;
         auto weights = [&]() __attribute__((always_inline)) {
             const float ref = m_run == -INFINITY ? 0.f : m_run;
             f16x4_t p4;
-            ps = 0.f;
+            ps = most = 0.f;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s4[i], a.scale_log2, -ref));
+                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s4[i], a.scale_log2, -ref)), v = p * sp[i];
                 ps += p;
-                p4[i] = (_Float16)(p * sp[i]);
+                most = fmaxf(most, v);
+                p4[i] = (_Float16)v;
             }
             lds_write_u2(lds0 + C8_OFF_P + c * (2 * C8_TILE) + 16 * ((2 * w + (g >> 1)) ^ rope_xor(c)) + 8 * (g & 1),
                          __builtin_bit_cast(u32x2_t, p4));
         };
         weights();
-        if (g == 0) lds_write_u1(lds0 + C8_OFF_TOP + c * 16 + 4 * w, __float_as_uint(top));
-        if (lane == 0) lds_write_u1(lds0 + C8_OFF_BAD + 4 * w, wave_bad ? 1u : 0u);
+        const uint32_t flags = (__ballot(most > C8_MOST || m_run == -INFINITY) ? 1u : 0u) | (__ballot(bad) ? 2u : 0u);
+        if (lane == 0) lds_write_u1(lds0 + C8_OFF_BAD + 4 * w, flags);
         lds_barrier();
-        u32x4_t bads = lds_read_u4<C8_OFF_BAD>(lds0), tops = lds_read_u4<C8_OFF_TOP>(lds0 + c * 16);
-        lds_wait<0>(bads, tops);
-        m_top = fmaxf(m_top, fmaxf(fmaxf(__uint_as_float(tops[0]), __uint_as_float(tops[1])),
-                                   fmaxf(__uint_as_float(tops[2]), __uint_as_float(tops[3]))));
-        const bool move = moves(m_top, m_run);
-        if (__ballot(move)) {   // the same in every wave
+        u32x4_t fl = lds_read_u4<C8_OFF_BAD>(lds0);
+        lds_wait<0>(fl);
+        const uint32_t any = __builtin_amdgcn_readfirstlane((fl[0] | fl[1]) | (fl[2] | fl[3]));
+        if (any & 1u) {
+            float top = m_run == -INFINITY ? -INFINITY : m_run + __builtin_amdgcn_logf(w_top);
+            top = fmaxf(top, top4(s4[0], s4[1], s4[2], s4[3], sp, a.scale_log2));
+            top = allreduce_groups(top, [](float p, float q) { return fmaxf(p, q); });
+            if (g == 0) lds_write_u1(lds0 + C8_OFF_TOP + c * 16 + 4 * w, __float_as_uint(top));
+            lds_barrier();
+            u32x4_t tops = lds_read_u4<C8_OFF_TOP>(lds0 + c * 16);
+            lds_wait<0>(tops);
+            const float m_top = fmaxf(fmaxf(__uint_as_float(tops[0]), __uint_as_float(tops[1])),
+                                      fmaxf(__uint_as_float(tops[2]), __uint_as_float(tops[3])));
+            const bool move = moves(m_top, m_run);
             const float next = move ? m_top + C8_ROOM : m_run, half = move ? __builtin_amdgcn_exp2f(0.5f * (m_run - next)) : 1.0f;
             const float al = half * half;
+            if (__ballot(move && m_run != -INFINITY)) {   // (else there is nothing yet; the same in every wave)
+#pragma unroll
+                for (int d = 0; d < NO; ++d) scale_all<4>(o[d], al);
+            }
             l_run = times_power(l_run, half);
             m_run = next;
-#pragma unroll
-            for (int d = 0; d < NO; ++d) scale_all<4>(o[d], al);
+            if (move) w_top = __builtin_amdgcn_exp2f(-C8_ROOM);
             weights();
             lds_barrier();
         }
+        w_top = fmaxf(w_top, most);
         l_run += ps;   // this lane's share of the sum
 
         // after the waits for every LDS operation, which would be waits for these scalar loads too
@@ -446,7 +457,7 @@ __device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit
         for (int s = 0; s < KS; ++s) pf[s] = lds_read_u4<C8_OFF_P>(lds0 + c * (2 * C8_TILE) + 16 * ((4 * s + g) ^ rope_xor(c)));
         const int vr = 8 * g + (c >> 1);       // the row within a lane group's eight, its place among the tile's
         const uint32_t va = st + vr * D_LAT + 16 * ((8 * w) ^ code_xor(vr)) + 8 * (lane & 1);
-        if (bads[0] | bads[1] | bads[2] | bads[3]) clean_tile(st, w, lane);
+        if (any & 2u) clean_tile(st, w, lane);
         constexpr int N = KS * NO, VD = 6;
         u32x2_t vv[VD + 1];
         auto vload = [&](auto ic) {
@@ -787,25 +798,26 @@ __device__ __forceinline__ void chunk8_big_segment(const Chunk8Args& a, const Ck
                 }
         }
         static_for<0, 4>([&](auto ic) { lds_wait<0>(f[2 * decltype(ic)::value], f[2 * decltype(ic)::value + 1]); });
-        float top = -INFINITY;
+        float top = m_top;
         auto tops = [&](bool one) __attribute__((always_inline)) {
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
                 const float scales[4] = {__uint_as_float(f[q][0]), __uint_as_float(f[q][1]), __uint_as_float(f[q][2]), __uint_as_float(f[q][3])};
                 const f32x16_t& s = z.s[q >> 2];
                 const int i = 4 * (q & 3);
-                top = fmaxf(top, top4(s[i], s[i + 1], s[i + 2], s[i + 3], scales, a.scale_log2, one));
+                if (one) top = fmaxf(top, __builtin_fmaf(fmaxf(fmaxf(s[i], s[i + 1]), fmaxf(s[i + 2], s[i + 3])), a.scale_log2, log_scale(scales[0])));
+                else top = fmaxf(top, top4(s[i], s[i + 1], s[i + 2], s[i + 3], scales, a.scale_log2));
             }
         };
-        if (a.bshift >= 2) tops(true);
+        if (a.bshift >= 2) tops(true);        // four rows have one scale
         else tops(false);
-        m_top = fmaxf(m_top, half_max(top));
-        const bool move = moves(m_top, m_run);
+        m_top = half_max(top);
+        const bool move = moves(m_top, m_run), scaled = move && m_run != -INFINITY;   // (else there is nothing yet)
         const float next = m_top + C8_ROOM, half = move ? __builtin_amdgcn_exp2f(0.5f * (m_run - next)) : 1.0f, alpha = half * half;
         if (move) m_run = next;
         l_run = times_power(l_run, half);
         const float ref = m_run == -INFINITY ? 0.f : m_run;
-        const uint32_t flags = (__ballot(move) ? 1u : 0u) | (__ballot(bad) ? 2u : 0u);
+        const uint32_t flags = (__ballot(scaled) ? 1u : 0u) | (__ballot(bad) ? 2u : 0u);
         const uint32_t pa = lds0 + B8_OFF_P + (k & 1) * B8_P + (32 * w + c) * (2 * C8_TILE);
         const uint32_t px = rope_xor(c);
         float psum = 0.f;
@@ -946,7 +958,7 @@ __device__ __forceinline__ void mid_scores(const Chunk8Args& a, const CkUnit& x,
 #pragma unroll
     for (int s = 0; s < 18; ++s) asm volatile("" : "+a"(qf[s]));   // no wait for them inside the tile loop
 
-    float m_top = -INFINITY;   // the rows' largest
+    float w_top = 0.f;   // this lane's largest weight since the reference moved
     int sg = 0;   // the stage of tile k
     for (int k = 0; k < nt; ++k) {
         lds_barrier();
@@ -1014,33 +1026,48 @@ __device__ __forceinline__ void mid_scores(const Chunk8Args& a, const CkUnit& x,
                     }
         }
         lds_wait<0>(f[0], f[1]);
-        float top = -INFINITY;
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            const float scales[4] = {__uint_as_float(f[b][0]), __uint_as_float(f[b][1]), __uint_as_float(f[b][2]), __uint_as_float(f[b][3])};
-            top = fmaxf(top, top4(s4[b][0], s4[b][1], s4[b][2], s4[b][3], scales, a.scale_log2, a.bshift >= 2));
-        }
-        m_top = fmaxf(m_top, allreduce_groups(top, [](float p, float q) { return fmaxf(p, q); }));
-        const bool move = moves(m_top, m_run);
-        const float next = m_top + C8_ROOM, half = move ? __builtin_amdgcn_exp2f(0.5f * (m_run - next)) : 1.0f, alpha = half * half;
-        if (move) m_run = next;
-        l_run = times_power(l_run, half);
-        const float ref = m_run == -INFINITY ? 0.f : m_run;
-        const uint32_t flags = (__ballot(move) ? 1u : 0u) | (__ballot(bad) ? 2u : 0u);
         const int row = 16 * w + c;
-        static_for<0, 2>([&](auto bc) {
-            constexpr int b = decltype(bc)::value;
-            f16x4_t p4;
+        float psum, most;
+        auto store = [&]() __attribute__((always_inline)) {
+            const float ref = m_run == -INFINITY ? 0.f : m_run;
+            psum = most = 0.f;
+            static_for<0, 2>([&](auto bc) {
+                constexpr int b = decltype(bc)::value;
+                f16x4_t p4;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s4[b][i], a.scale_log2, -ref));
-                l_run += p;           // this lane's share of the sum
-                p4[i] = (_Float16)(p * __uint_as_float(f[b][i]));
+                for (int i = 0; i < 4; ++i) {
+                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s4[b][i], a.scale_log2, -ref)), v = p * __uint_as_float(f[b][i]);
+                    psum += p;
+                    most = fmaxf(most, v);
+                    p4[i] = (_Float16)v;
+                }
+                // slots of a row: in each 16 of them rows 4 h + (0..3, 8..11) for half h
+                lds_write_u2(lds0 + M8_OFF_P + M8_P * (k & 1) + row * (2 * M8_TILE) + 16 * ((2 * b + (g & 1)) ^ weight_xor(row)) + 8 * (g >> 1),
+                             __builtin_bit_cast(u32x2_t, p4));
+            });
+        };
+        store();
+        float alpha = 1.0f;
+        bool scaled = false;
+        if (__ballot(most > C8_MOST || m_run == -INFINITY)) {
+            float top = m_run == -INFINITY ? -INFINITY : m_run + __builtin_amdgcn_logf(w_top);
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const float scales[4] = {__uint_as_float(f[b][0]), __uint_as_float(f[b][1]), __uint_as_float(f[b][2]), __uint_as_float(f[b][3])};
+                top = fmaxf(top, top4(s4[b][0], s4[b][1], s4[b][2], s4[b][3], scales, a.scale_log2));
             }
-            // slots of a row: in each 16 of them rows 4 h + (0..3, 8..11) for half h
-            lds_write_u2(lds0 + M8_OFF_P + M8_P * (k & 1) + row * (2 * M8_TILE) + 16 * ((2 * b + (g & 1)) ^ weight_xor(row)) + 8 * (g >> 1),
-                         __builtin_bit_cast(u32x2_t, p4));
-        });
+            top = allreduce_groups(top, [](float p, float q) { return fmaxf(p, q); });
+            const bool move = moves(top, m_run);
+            const float next = top + C8_ROOM, half = move ? __builtin_amdgcn_exp2f(0.5f * (m_run - next)) : 1.0f;
+            alpha = half * half;
+            scaled = move && m_run != -INFINITY;           // (else there is nothing yet)
+            l_run = times_power(l_run, half);
+            if (move) m_run = next, w_top = __builtin_amdgcn_exp2f(-C8_ROOM);
+            store();
+        }
+        w_top = fmaxf(w_top, most);
+        l_run += psum;                // this lane's share of the sum
+        const uint32_t flags = (__ballot(scaled) ? 1u : 0u) | (__ballot(bad) ? 2u : 0u);
         if (g == 0) lds_write_u1(lds0 + M8_OFF_ALPHA + 256 * (k & 1) + row * 4, __float_as_uint(alpha));
         if (lane == 0) lds_write_u1(lds0 + M8_OFF_BAD + 16 * (k & 1) + 4 * w, flags);
     }

@@ -58,7 +58,7 @@ def check(lines):
                 problems.append(f"{text}: names a score in flight")
             if op.startswith(("s_cbranch", "s_branch", "s_endpgm", "s_setpc", "s_swappc")) and flight:
                 problems.append(f"{text}: scores in flight over a branch")
-            if op == "v_accvgpr_read_b32" and len(block) == 3:
+            if op == "v_accvgpr_read_b32" and len(block) > 2:
                 seen["factors"] += 1
                 if since < SETTLED:
                     problems.append(f"{text}: {since} wait states after a product")
