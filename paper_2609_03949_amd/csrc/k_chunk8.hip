@@ -15,8 +15,8 @@
 //   16       four waves; scores by rows of the tile, so that each code is converted once for either product
 //   32, 64   four waves of scores, by rows of the unit, beside four of outputs
 //   128      four waves, both in one stream of instructions, the scores of a tile between the outputs of the one before
-// 16 sequences of up to 65536 rows, 16 heads: 126 us, 4.7 TB/s.  16 of 32768 rows, 32 and 64 heads: 85 and 112 us.  32 of 32768
-// rows, 128 heads: 276 us; 3 x 512 new tokens over 16384 rows, 128 heads: 4.16 ms, 1.19 PFLOP/s.
+// 16 sequences of up to 65536 rows, 16 heads: 128 us, 4.6 TB/s.  16 of 32768 rows, 32 and 64 heads: 86 and 116 us.  32 of 32768
+// rows, 128 heads: 289 us; 3 x 512 new tokens over 16384 rows, 128 heads: 4.43 ms, 1.12 PFLOP/s.
 #include <algorithm>
 
 #include "vkv_runs.h"
@@ -1223,12 +1223,12 @@ __device__ __forceinline__ void segment8(const Chunk8Args& a, const CkUnit& x, i
 
 // Runs the tiles of all units are cut into: at most one per CU, and as a run costs its tiles and the writing and reading of its
 // part, some sqrt(tiles) of them, more where parts are small beside a tile's time.  16 heads over 4 x 8192 rows 20.6 us, 25.0 with
-// half as many runs; 32 heads over 32768 rows 26 us, 28 with twice as many, 32 with half as many; 128 heads over 32768 rows in
-// units of 128 rows 49.1 us, 55.0 with twice as many.
+// half as many runs; 32 heads over 4 x 8192 rows 25.4 us, 27.3 with fewer; 128 heads over 32768 rows in units of 128 rows 49.1 us,
+// 55.0 with twice as many.
 template <int RG>
 __device__ __forceinline__ int run_count8(const Chunk8Args& a, int total) {
     int len = 1;
-    while (2.0f * (float)len <= (RG == 1 ? 0.12f : RG == 8 ? 0.25f : 0.35f) * sqrtf((float)total)) len *= 2;
+    while (2.0f * (float)len <= (RG == 1 ? 0.12f : 0.25f) * sqrtf((float)total)) len *= 2;
     return min(max((total + len - 1) / len, 1), a.runs);
 }
 
