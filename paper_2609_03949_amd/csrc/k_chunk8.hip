@@ -552,7 +552,7 @@ constexpr int B8_P = 128 * 2 * C8_TILE;                         // weights of a 
 constexpr int B8_OFF_SCALE = C8_OFF_TOP;                        // [64] the tile's scales (every wave writes the same ones)
 constexpr int B8_OFF_ALPHA = B8_OFF_SCALE + 4 * C8_TILE;        // two of [128]: by what a row's outputs are to be multiplied
 constexpr int B8_OFF_BAD = B8_OFF_ALPHA + 2 * 512;              // two of [4]: the waves' flags, outputs to multiply, a hidden NaN
-constexpr int B8_OFF_P = 3072;
+constexpr int B8_OFF_P = 3 * 1024;
 constexpr int B8_OFF_STAGE = B8_OFF_P + 2 * B8_P;
 constexpr int B8_SMEM = B8_OFF_STAGE + C8_STAGES * C8_STAGE;
 static_assert(B8_OFF_BAD + 32 <= B8_OFF_P && B8_OFF_STAGE % 1024 == 0, "");
@@ -910,7 +910,7 @@ constexpr int M8_OFF_WORD = 0, M8_OFF_NOTE = M8_OFF_WORD + M8_STAGES * M8_TILE *
 constexpr int M8_OFF_SCALE = M8_OFF_NOTE + M8_STAGES * M8_TILE * 4;   // [32] the tile's scales (every wave writes the same ones)
 constexpr int M8_OFF_ALPHA = M8_OFF_SCALE + 4 * M8_TILE;              // two of [64]: by what a row's outputs are to be multiplied
 constexpr int M8_OFF_BAD = M8_OFF_ALPHA + 2 * 256;                    // two of [4]: the waves' flags, outputs to multiply, a hidden NaN
-constexpr int M8_OFF_P = 3072, M8_P = 64 * 2 * M8_TILE;               // weights of a tile, [64][32] bf16; two of them
+constexpr int M8_OFF_P = 3 * 1024, M8_P = 64 * 2 * M8_TILE;               // weights of a tile, [64][32] bf16; two of them
 constexpr int M8_OFF_STAGE = M8_OFF_P + 2 * M8_P;
 typedef Loader8<8, M8_OFF_WORD, M8_OFF_NOTE, true> Loader32;
 constexpr int M8_SMEM = M8_OFF_STAGE + M8_STAGES * Loader32::STAGE;

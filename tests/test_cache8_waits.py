@@ -77,7 +77,7 @@ def check(lines):
     return problems, seen
 
 
-def test_checker():
+def test_the_reading():
     asm = lambda *t: [";;#ASMSTART", *t, ";;#ASMEND"]
     read, wait = "ds_read_b128 v[20:23], v1 offset:64", "s_waitcnt lgkmcnt(0)"
     product = "v_mfma_f32_32x32x16_bf16 v[0:15], v[16:19], v[24:27], "

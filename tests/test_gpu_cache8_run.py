@@ -194,3 +194,28 @@ def test_a_captured_step(ctx):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip((*state, out, lse, used, s.missing), eager))
         assert s.missing.tolist() == [0] * B and bool(torch.isfinite(lse).all())
+
+
+@pytest.mark.parametrize("H", [4, 32, 64, 128])
+def test_nothing_there(ctx, H):
+    """No cache rows at all, no tokens at all: outputs of tokens that see nothing, and nothing else written."""
+    u8 = torch.uint8
+    cache, scale = torch.full((2, 16, 640), 9, dtype=u8, device=DEV), torch.full((2, 1), 9, dtype=u8, device=DEV)
+    kv = torch.zeros(3, dtype=I32, device=DEV)
+    cu = torch.tensor([0, 2, 2, 5], dtype=I32, device=DEV)
+    q = torch.randn(5, H, 576, device=DEV).to(BF)
+    for table, max_kv in ((torch.empty(3, 0, dtype=I32, device=DEV), 0), (torch.zeros(3, 1 << 14, dtype=I32, device=DEV), 1 << 18)):
+        pages = vkv.Pages8(cache, scale, table, kv, max_kv)
+        chunk = vkv.Chunk(q[..., :512], q[..., 512:], cu, 3)
+        ws = torch.empty(max(vkv.chunk8_workspace_size(pages, chunk), 256), dtype=u8, device=DEV)
+        out, lse = torch.full((5, H, 512), 7.0, dtype=BF, device=DEV), torch.full((5, H), 7.0, device=DEV)
+        vkv.chunk8_attend(ctx, pages, chunk, ws, SCALE, out, lse)
+        vkv.cache8_write(ctx, pages, q[:, 0, :512], q[:, 0, 512:], cu, 3)
+        none = vkv.Chunk(q[:0, :, :512], q[:0, :, 512:], torch.zeros(4, dtype=I32, device=DEV), 3)
+        vkv.chunk8_attend(ctx, pages, none, ws, SCALE, out[:0], lse[:0])
+        vkv.cache8_write(ctx, pages, q[:0, 0, :512], q[:0, 0, 512:], torch.zeros(4, dtype=I32, device=DEV), 3)
+        torch.cuda.synchronize()
+        assert bool((out == 0).all()) and bool((lse == -math.inf).all())
+    x = torch.empty(0, H, 64, dtype=BF, device=DEV)
+    vkv.rope_apply(ctx, vkv.Rope(64), x, torch.empty(0, dtype=I32, device=DEV), x)
+    assert bool((cache == 9).all()) and bool((scale == 9).all())

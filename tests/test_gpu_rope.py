@@ -148,6 +148,23 @@ def test_the_transposed_map_is_the_gradient(ctx):
     assert abs(float(left.sum() - right.sum())) <= (BF + 64 * F32) * size
 
 
+@pytest.mark.parametrize("inter", [False, True])
+def test_the_gradient_against_differences(ctx, inter):
+    """d(y . R x) / dx_j = y . (R(x + e_j) - R x), exactly so for a linear map: with x = 0 the columns of R, each rounded to bf16
+    once (two entries of a column), against the gradient, rounded once."""
+    D, at = 24, 12345
+    rope = vkv.Rope(16, 500.0, inter, magnitude=0.9)
+    one = torch.eye(D, dtype=torch.bfloat16, device=DEV)
+    pos = torch.full((D,), at, dtype=torch.int32, device=DEV)
+    cols, y = torch.empty_like(one), data(1, 1, D, 4, 8)[0][:, 0]
+    vkv.rope_apply(ctx, rope, one, pos, cols, first=4)
+    grad = torch.empty_like(y)
+    vkv.rope_apply(ctx, rope, y, pos[:1], grad, first=4, transposed=True)
+    want = cols.double() @ y[0].double()
+    size = cols.double().abs() @ y[0].double().abs()
+    assert bool(((grad[0].double() - want).abs() <= (2 * BF + 16 * F32) * size).all())
+
+
 def test_not_finite_values_stay_in_their_pairs(ctx):
     x, pos = data(4, 2, 64, 100, 7)
     clean = torch.empty_like(x)
