@@ -750,8 +750,10 @@ typedef struct vkv_pages8 {
  * nearest, ties to even.  Values that are not finite or above 448 * 2^64 are stored as NaN and have no
  * say in the scale; e is kept within [-64, 64].
  * The rows behind the new ones and every other block keep their bytes.  Tokens past the first max_q of a
- * sequence, tokens whose row would be below 0, and rows on absent pages are not written (the rows that the others take stay
- * those of the whole chunk).  A page that is written may be in one place of one table only (vkv_pages_reserve sees to it).
+ * sequence, tokens whose row would be below 0 or from max_kv on, and rows on absent pages are not written (the rows that the
+ * others take stay those of the whole chunk).  So kv_len is not cut to max_kv here: a sequence that has outgrown its table
+ * loses its new rows, not older ones.  (Lengths from 2^30 on, which no sequence has, stand for max_kv.)
+ * A page that is written may be in one place of one table only (vkv_pages_reserve sees to it).
  * Pages may not overlap (page_stride at least (page - 1)*row_stride + 640, or row_stride at least n_pages*page_stride).
  * 0 <= n_tok < 2^31, 0 <= max_q <= 2^30; strides multiples of 8, at least 0, pointers 16-byte aligned (cu 4).
  * No atomics: the same inputs give the same bytes.  Allocates nothing; fit for graph capture.

@@ -41,9 +41,11 @@ __global__ __launch_bounds__(W8_THREADS) void write8_kernel(Write8Args a) {
     const int b = (int)(wg / (uint32_t)a.mb), j = (int)(wg % (uint32_t)a.mb);
     const int64_t s0 = min(max((int64_t)c.cu[b], (int64_t)0), c.n_tok);
     const int64_t e0 = min(max((int64_t)c.cu[b + 1], s0), c.n_tok);
-    const int kv = min(max(c.kv_len[b], 0), c.max_kv);
+    // A sequence longer than its table keeps its rows' places (cut to max_kv, as where it is read, the length would put new rows
+    // over older ones).  No sequence has 2^30 rows and more: such a length stands for max_kv.
+    const int n = c.kv_len[b], kv = n >= (1 << 30) ? c.max_kv : max(n, 0);
     const int64_t before = kv - (e0 - s0);                             // the row of token s0
-    const int first = (int)max(before, (int64_t)0), end = (int)min(before + min(e0 - s0, (int64_t)c.max_q), (int64_t)kv);   // rows that are written
+    const int first = (int)max(before, (int64_t)0), end = (int)min(before + min(e0 - s0, (int64_t)c.max_q), (int64_t)c.max_kv);   // rows that are written
     const int u0 = (first / R + (GW == 1 ? W8_WAVES * j + w : j)) * R;   // the block's first row
     if (first >= end || u0 >= end) return;                             // the whole workgroup, or waves that share nothing
     const int32_t p = c.table[(int64_t)b * c.tstride + (u0 >> c.shift)];
