@@ -83,3 +83,25 @@ def test_a_sequence_that_grows_past_its_table(ctx):
         if step > 47:
             assert torch.equal(cache, full[0]) and torch.equal(scale, full[1])
         assert np.all(refs.cpu().numpy() <= 1)
+
+
+@pytest.mark.parametrize("block", [1, 2, 16])
+def test_the_longest_chunk_beside_the_longest_sequence(ctx, block):
+    """As many workgroups a sequence as 2^30 tokens take, for one whose block lies at the end of 2^30 rows too: block numbers
+    whose rows pass 31 bits.  No page is there but the last one of the second sequence."""
+    n, page = 1 << 30, 65536
+    cache = torch.full((1, page, 640), 9, dtype=torch.uint8, device=DEV)
+    scale = torch.full((1, page // block), 127, dtype=torch.uint8, device=DEV)
+    table = torch.full((2, n // page), -1, dtype=I32, device=DEV)
+    table[1, -1] = 0
+    kv, cu = torch.tensor([n, n - 1], dtype=I32, device=DEV), torch.tensor([0, n, n + 1], dtype=I32, device=DEV)
+    lat, rope = torch.ones(1, 512, dtype=torch.bfloat16, device=DEV), torch.ones(1, 64, dtype=torch.bfloat16, device=DEV)
+    vkv.cache8_write(ctx, vkv.Pages8(cache, scale, table, kv, n), lat.expand(n + 1, 512), rope.expand(n + 1, 64), cu, n)
+    torch.cuda.synchronize()
+    older = block > 2                                 # in the new row's block: it keeps its scale, 1; else the new row's is 2^-8
+    new, byte = cache[0, page - 2], scale[0, (page - 2) // block]
+    assert bool((new[:512] == (0x38 if older else 0x78)).all()) and torch.equal(new[512:].view(torch.bfloat16), rope[0])
+    assert int(byte) == (127 if older else 119)
+    new.fill_(9)
+    byte.fill_(127)
+    assert bool((cache == 9).all()) and bool((scale == 127).all())
