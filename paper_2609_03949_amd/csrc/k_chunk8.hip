@@ -457,7 +457,10 @@ __device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit
         for (int s = 0; s < KS; ++s) pf[s] = lds_read_u4<C8_OFF_P>(lds0 + c * (2 * C8_TILE) + 16 * ((4 * s + g) ^ rope_xor(c)));
         const int vr = 8 * g + (c >> 1);       // the row within a lane group's eight, its place among the tile's
         const uint32_t va = st + vr * D_LAT + 16 * ((8 * w) ^ code_xor(vr)) + 8 * (lane & 1);
-        if (any & 2u) clean_tile(st, w, lane);
+        if (any & 2u) {
+            lds_wait<0>(pf[0], pf[1]);         // nothing is on its way over the call
+            clean_tile(st, w, lane);
+        }
         constexpr int N = KS * NO, VD = 6;
         u32x2_t vv[VD + 1];
         auto vload = [&](auto ic) {
@@ -1136,7 +1139,10 @@ __device__ __forceinline__ void mid_outputs(const Chunk8Args& a, const CkUnit& x
                 for (int d = 0; d < 4; ++d) scale_all<16>(o[d][rb], __uint_as_float(al));
             }
         }
-        if (all & 2u) clean_dims(st, w, lane);
+        if (all & 2u) {
+            static_for<0, 2 * RB>([&](auto q) { lds_wait<0>(pf[decltype(q)::value / RB][decltype(q)::value % RB]); });   // (as above)
+            clean_dims(st, w, lane);
+        }
         const int e = (lane >> 1) & 7, vr = 4 * hh + (e & 3) + 8 * (e >> 2);   // a lane group's eight rows of 16, its place among the dims
         const uint32_t va = st + vr * D_LAT + 16 * ((8 * w + ((lane >> 4) & 1)) ^ code_xor(vr)) + 8 * (lane & 1);
         constexpr int N = 8, VD = 5;
