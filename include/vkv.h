@@ -765,7 +765,8 @@ int vkv_cache8_write(vkv_ctx* ctx, const vkv_pages8* pg, const uint16_t* lat, in
  * vkv_chunk_attend on a cache held in 8 bits: the same chunk, scores, outputs and rules, on the rows
  * that the codes stand for.  bf16 and fp16 MFMA on the exact values of the codes, fp32 accumulation; the weights, times the row's
  * power of two, are rounded to fp16 for the product with the codes: 11 bits down to 2^-14 of the largest of them, fewer
- * below, none under 2^-25.
+ * below; rows too light for fp16 one by one lose at most 2^-11 of what the largest adds to an output together (2^-9 from 2^28
+ * rows on), whatever their number.
  * Rows that a token does not see do not reach it, whatever they hold.
  * ws: vkv_chunk8_workspace_size bytes; the rules of vkv_chunk_attend's.
  */

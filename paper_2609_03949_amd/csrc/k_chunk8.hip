@@ -18,6 +18,7 @@
 // 16 sequences of up to 65536 rows, 16 heads: 128 us, 4.6 TB/s.  16 of 32768 rows, 32 and 64 heads: 86 and 116 us.  32 of 32768
 // rows, 128 heads: 289 us; 3 x 512 new tokens over 16384 rows, 128 heads: 4.43 ms, 1.12 PFLOP/s.
 #include <algorithm>
+#include <cmath>
 
 #include "vkv_runs.h"
 
@@ -37,18 +38,20 @@ constexpr int C8_SMEM = C8_OFF_STAGE + C8_STAGES * C8_STAGE;
 static_assert(C8_OFF_BAD + 16 <= C8_OFF_P && C8_OFF_STAGE % 1024 == 0 && C8_OFF_P % 1024 == 0, "");
 constexpr uint32_t C8_ABSENT = 255;
 // The weight of a code is the row's softmax weight times its power of two, against a reference that follows the largest of
-// these (in log2 units): a new one makes the largest 1, and it is kept until one is above 2^15.  So fp16 holds the
-// weights, with three bits more than bf16 (whose rounding would be as large as the output's own): 11 bits down to 2^-14 of the
-// largest at the least, 8 down to 2^-17, and none below 2^-25; the products and sums are fp32.  (A new largest of 2^-20,
-// and room for 2^35, was 5% faster, and would leave no bits to rows that are light one by one and heavy together.)  The sum of
-// the softmax weights themselves, which are 2^-64 to 2^64 times as large, is fp32 from unrounded ones: between 2^-64 and 2^109.
-constexpr float C8_SLACK = 15.0f, C8_ROOM = 0.0f;
+// these (in log2 units): a new one makes the largest 2^first, and it is kept until one is above 2^15.  fp16 holds 11 bits of a
+// weight down to 2^-14, fewer below, and nothing under 2^-25, so n rows of one segment that are light one by one lose at most
+// n 2^-(25 + first) of what the largest adds to an output.  `first` goes by the rows that a segment may have, so that this is 2^-11 (an
+// eighth of half a step of the output's bf16) up to 2^28 of them, 2^-9 up to 2^30.  The larger it is the sooner a reference
+// moves, and a move multiplies the outputs: with first = 0, 4, 8 and 12 whatever the size, 32 x 32768 rows of 128 heads took 301,
+// 311, 329 and 358 us, 16 x 65536 rows of 16 heads 130, 131, 134 and 142.  The products and sums are fp32, and so is the sum of the
+// softmax weights themselves, which are 2^-64 to 2^64 times as large, from unrounded ones: between 2^-64 and 2^109.
+constexpr float C8_SLACK = 15.0f;
 constexpr float C8_MOST = 32768.0f;   // 2^SLACK: weights are taken as if they were no more, and again where one is
 // Does the reference m of this lane's row, whose largest is top, move?  Where one of the wave's rows has to, all do that have come
 // nearer by a bit or more: the outputs are multiplied for all of them at once, and seldom.
-__device__ __forceinline__ bool moves(float top, float m) {
+__device__ __forceinline__ bool moves(float top, float m, float first) {
     bool move = top > m + C8_SLACK;
-    if (__ballot(move)) move = top > m + (1.0f - C8_ROOM);
+    if (__ballot(move)) move = top > m + (first + 1.0f);
     return move;
 }
 
@@ -432,8 +435,8 @@ __device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit
             lds_wait<0>(tops);
             const float m_top = fmaxf(fmaxf(__uint_as_float(tops[0]), __uint_as_float(tops[1])),
                                       fmaxf(__uint_as_float(tops[2]), __uint_as_float(tops[3])));
-            const bool move = moves(m_top, m_run);
-            const float next = move ? m_top + C8_ROOM : m_run, half = move ? __builtin_amdgcn_exp2f(0.5f * (m_run - next)) : 1.0f;
+            const bool move = moves(m_top, m_run, a.first);
+            const float next = move ? m_top - a.first : m_run, half = move ? __builtin_amdgcn_exp2f(0.5f * (m_run - next)) : 1.0f;
             const float al = half * half;
             if (__ballot(move && m_run != -INFINITY)) {   // (else there is nothing yet; the same in every wave)
 #pragma unroll
@@ -441,7 +444,7 @@ __device__ __forceinline__ void chunk8_segment(const Chunk8Args& a, const CkUnit
             }
             l_run = times_power(l_run, half);
             m_run = next;
-            if (move) w_top = __builtin_amdgcn_exp2f(-C8_ROOM);
+            if (move) w_top = __builtin_amdgcn_exp2f(a.first);
             weights();
             lds_barrier();
         }
@@ -815,8 +818,8 @@ __device__ __forceinline__ void chunk8_big_segment(const Chunk8Args& a, const Ck
         if (a.bshift >= 2) tops(true);        // four rows have one scale
         else tops(false);
         m_top = half_max(top);
-        const bool move = moves(m_top, m_run), scaled = move && m_run != -INFINITY;   // (else there is nothing yet)
-        const float next = m_top + C8_ROOM, half = move ? __builtin_amdgcn_exp2f(0.5f * (m_run - next)) : 1.0f, alpha = half * half;
+        const bool move = moves(m_top, m_run, a.first), scaled = move && m_run != -INFINITY;   // (else there is nothing yet)
+        const float next = m_top - a.first, half = move ? __builtin_amdgcn_exp2f(0.5f * (m_run - next)) : 1.0f, alpha = half * half;
         if (move) m_run = next;
         l_run = times_power(l_run, half);
         const float ref = m_run == -INFINITY ? 0.f : m_run;
@@ -1060,12 +1063,12 @@ __device__ __forceinline__ void mid_scores(const Chunk8Args& a, const CkUnit& x,
                 top = fmaxf(top, top4(s4[b][0], s4[b][1], s4[b][2], s4[b][3], scales, a.scale_log2));
             }
             top = allreduce_groups(top, [](float p, float q) { return fmaxf(p, q); });
-            const bool move = moves(top, m_run);
-            const float next = top + C8_ROOM, half = move ? __builtin_amdgcn_exp2f(0.5f * (m_run - next)) : 1.0f;
+            const bool move = moves(top, m_run, a.first);
+            const float next = top - a.first, half = move ? __builtin_amdgcn_exp2f(0.5f * (m_run - next)) : 1.0f;
             alpha = half * half;
             scaled = move && m_run != -INFINITY;           // (else there is nothing yet)
             l_run = times_power(l_run, half);
-            if (move) m_run = next, w_top = __builtin_amdgcn_exp2f(-C8_ROOM);
+            if (move) m_run = next, w_top = __builtin_amdgcn_exp2f(a.first);
             store();
         }
         w_top = fmaxf(w_top, most);
@@ -1453,7 +1456,18 @@ static hipError_t launch_chunk8_rows(const Chunk8Args& a, const ChunkSplit& sp, 
     return hipGetLastError();
 }
 
-hipError_t launch_chunk8(const Chunk8Args& a, const ChunkSplit& sp, hipStream_t s) {
+// log2 of the largest weight where a reference moves, by the rows that a segment may have (run_count8's lengths, a tile's rest)
+static int first_weight(const ChunkSplit& sp, int64_t max_kv) {
+    const int64_t tile = sp.qg == 2 || sp.qg == 4 ? M8_TILE : C8_TILE, cache = (max_kv + tile - 1) / tile, total = sp.units * cache;
+    int64_t rows = max_kv;
+    if (sp.runs) rows = std::min(rows, tile * (1 + std::max(1 + total / sp.runs, (int64_t)(0.25 * std::sqrt((double)total)))));
+    int log = 0;
+    while (log < 30 && (1ll << log) < rows) ++log;
+    return std::min(std::max(log - 14, 0), 14);
+}
+
+hipError_t launch_chunk8(Chunk8Args a, const ChunkSplit& sp, hipStream_t s) {
+    a.first = (float)first_weight(sp, a.max_kv);
     return sp.qg == 1 ? launch_chunk8_rows<1>(a, sp, s) : sp.qg == 2 ? launch_chunk8_rows<2>(a, sp, s)
          : sp.qg == 4 ? launch_chunk8_rows<4>(a, sp, s) : launch_chunk8_rows<8>(a, sp, s);
 }

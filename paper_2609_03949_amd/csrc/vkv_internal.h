@@ -356,9 +356,10 @@ struct Chunk8Args : ChunkArgs {
     const uint8_t* scale;
     int64_t sstride;       // scale bytes from page to page
     int bshift;            // log2 of the rows that share one
+    float first;           // log2 of the largest weight where a reference moves (set by launch_chunk8)
 };
 ChunkSplit chunk8_split(int64_t B, int64_t H, int64_t max_q, int64_t max_kv);
-hipError_t launch_chunk8(const Chunk8Args& a, const ChunkSplit& sp, hipStream_t s);
+hipError_t launch_chunk8(Chunk8Args a, const ChunkSplit& sp, hipStream_t s);
 
 struct Write8Args {
     Chunk8Args c;          // the pages; cu, n_tok, max_q
