@@ -865,10 +865,12 @@ __device__ __forceinline__ void chunk8_big_segment(const Chunk8Args& a, const Ck
         lds_wait<0>(fl);
         const uint32_t all = __builtin_amdgcn_readfirstlane((fl[0] | fl[1]) | (fl[2] | fl[3]));
         if (all & 1u) {
+            int ln = lane;
+            asm volatile("" : "+v"(ln));          // (as above: an address from memory would wait for the loads just issued)
 #pragma unroll
             for (int rb = 0; rb < 4; ++rb) {      // a wave's rows are a row block
                 if (!(__builtin_amdgcn_readfirstlane(fl[rb]) & 1u)) continue;
-                uint32_t f = lds_read_u1(lds0 + B8_OFF_ALPHA + 512 * (k & 1) + (32 * rb + c) * 4);
+                uint32_t f = lds_read_u1(lds0 + B8_OFF_ALPHA + 512 * (k & 1) + (32 * rb + (ln & 31)) * 4);
                 lds_wait<0>(f);
 #pragma unroll
                 for (int d = 0; d < 4; ++d) scale_all<16>(z.o[d][rb], __uint_as_float(f));

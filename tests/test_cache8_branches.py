@@ -85,22 +85,49 @@ def test_the_following():
     assert follow([read, "s_setpc_b64 s[30:31]"])[0]
 
 
-@pytest.mark.skipif(not os.path.exists(HIPCC), reason="no hipcc")
-def test_every_way_waits(tmp_path):
+def tile_loops(lines):
+    """The innermost loops with matrix products: [first line, last line)."""
+    at = {m.group(1): i for i, l in enumerate(lines) for m in [re.match(r"(\.LBB\w+):", l)] if m}
+    back = {(at[m.group(1)], i) for i, l in enumerate(lines) for m in [re.match(r"\s+s_c?branch\w*\s+(\.LBB\w+)", l)] if m and at[m.group(1)] < i}
+    loops = [(a, b) for a, b in back if any("v_mfma" in l for l in lines[a:b])]
+    return [(a, b) for a, b in loops if not any(a <= x and y <= b for x, y in loops if (x, y) != (a, b))]
+
+
+@pytest.fixture(scope="module")
+def functions(tmp_path_factory):
+    """Name and lines of each device function of the compiled file."""
     from paper_2609_03949_amd.csrc import build
+    if not os.path.exists(HIPCC):
+        pytest.skip("no hipcc")
     flags = [f for f in build.FLAGS if f != "-shared"]
-    out = tmp_path / "k_chunk8.s"
+    out = tmp_path_factory.mktemp("asm") / "k_chunk8.s"
     subprocess.run([HIPCC, *flags, "-I", os.path.join(ROOT, "include"), "--cuda-device-only", "-S",
                     os.path.join(build.HERE, "k_chunk8.hip"), "-o", str(out)], check=True, capture_output=True)
     lines = out.read_text().split("\n")
     starts = [i for i, l in enumerate(lines) if re.match(r"_ZN3vkv\w+:", l)]
+    return [(lines[s].split(":")[0], lines[s + 1:next(i for i in range(s, len(lines)) if lines[i].startswith(".Lfunc_end"))]) for s in starts]
+
+
+def test_every_way_waits(functions):
     found = 0
-    for start in starts:
-        end = next(i for i in range(start, len(lines)) if lines[i].startswith(".Lfunc_end"))
-        problems, reads = follow(lines[start + 1:end])
-        name = lines[start].split(":")[0]
+    for name, lines in functions:
+        problems, reads = follow(lines)
         assert not problems, (name, len(problems), problems[:5])
         if re.search(r"chunk8_(run|unit)_kernel", name):
             found += 1
             assert reads >= 26, name                 # a tile's keys and values
+    assert found == 8
+
+
+def test_no_register_is_kept_in_memory_across_a_tile(functions):
+    """A register that the compiler fetches from memory in the tile loop comes back with a wait for every load before it, the
+    next tiles' among them."""
+    found = 0
+    for name, lines in functions:
+        if re.search(r"chunk8_(run|unit)_kernel", name):
+            loops = tile_loops(lines)
+            found += 1
+            assert len(loops) >= (2 if re.search("ILi[24]E", name) else 1), name      # units of 32 and 64 rows: scores, outputs
+            for a, b in loops:
+                assert not [l for l in lines[a:b] if "scratch_" in l], name
     assert found == 8
