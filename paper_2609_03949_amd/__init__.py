@@ -24,13 +24,14 @@ __all__ = [
     "sigma_tier_size", "sigma_select", "step_run_kept", "pack_rows", "page_box", "page_bound", "SIGMA_BLOCK",
     "Prompt", "prompt_attend", "Pages", "Chunk", "chunk_workspace_size", "chunk_attend",
     "weight_workspace_size", "weight_accumulate", "weight_select", "cache_evict",
-    "VKV_ROPE_PLAIN", "VKV_ROPE_LINEAR", "VKV_ROPE_BASE", "VKV_ROPE_PARTS", "Rope", "rope_apply",
+    "VKV_ROPE_PLAIN", "VKV_ROPE_LINEAR", "VKV_ROPE_BASE", "VKV_ROPE_PARTS", "VKV_ROPE_BY_INDEX", "Rope", "rope_apply",
     "Pages8", "cache8_write", "chunk8_workspace_size", "chunk8_attend",
     "Pool", "pool_workspace_size", "pages_fork", "pages_reserve", "pages_compact", "exported_symbols",
 ]
 
 VKV_MODE_ROPE, VKV_MODE_DIGEST, VKV_MODE_ROPE_DIGEST = 1, 2, 3
 VKV_ROPE_PLAIN, VKV_ROPE_LINEAR, VKV_ROPE_BASE, VKV_ROPE_PARTS = 0, 1, 2, 3
+VKV_ROPE_BY_INDEX = 8   # with VKV_ROPE_PARTS
 D_LAT, D_ROPE, D_ROW = 512, 64, 576
 ROW8, MAX_PLANES = 640, 4
 
@@ -742,7 +743,7 @@ def cache_evict(ctx: Context, pages: Pages, kept: torch.Tensor, count: torch.Ten
 
 class Rope:
     """Rotary positions (``vkv_rope``): `dims` dims in pairs, neighbours if interleaved, else the two halves;
-    scaling one of VKV_ROPE_*."""
+    scaling one of VKV_ROPE_*, or VKV_ROPE_PARTS | VKV_ROPE_BY_INDEX."""
 
     def __init__(self, dims: int, base: float = 10000.0, interleaved: bool = False, scaling: int = VKV_ROPE_PLAIN,
                  factor: float = 1.0, original: float = 4096.0, fast: float = 32.0, slow: float = 1.0,

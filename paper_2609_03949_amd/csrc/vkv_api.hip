@@ -998,31 +998,53 @@ int vkv_chunk8_attend(vkv_ctx* ctx, const vkv_pages8* pg, const vkv_chunk* ch, v
 
 // ------------------------------------------------------ rotary positions
 
+constexpr int ROPE_PARTS_BY_INDEX = VKV_ROPE_PARTS | VKV_ROPE_BY_INDEX;
+
+// the pairs between which the part of theta_i falls from all to none
+static void rope_ramp(const vkv_rope* r, double* lo, double* hi) {
+    auto index = [&](double turns) { return r->dims * std::log(r->original / (turns * 6.283185307179586477)) / (2.0 * std::log(r->base)); };
+    *lo = std::max(std::floor(index(r->fast)), 0.0);
+    *hi = std::min(std::ceil(index(r->slow)), r->dims - 1.0);
+}
+
 static int check_rope(vkv_ctx* ctx, const vkv_rope* r) {
     if (!r) return fail(ctx, VKV_E_ARG, "rope is NULL");
     if (r->dims < 2 || r->dims > VKV_ROPE_MAX_DIMS || r->dims % 2)
         return fail(ctx, VKV_E_SHAPE, "dims=%d: need an even number in [2, %d]", r->dims, VKV_ROPE_MAX_DIMS);
-    if (r->scaling < VKV_ROPE_PLAIN || r->scaling > VKV_ROPE_PARTS) return fail(ctx, VKV_E_ARG, "scaling=%d", r->scaling);
+    const bool by_index = r->scaling == ROPE_PARTS_BY_INDEX;
+    if ((r->scaling < VKV_ROPE_PLAIN || r->scaling > VKV_ROPE_PARTS) && !by_index) return fail(ctx, VKV_E_ARG, "scaling=%d", r->scaling);
     if (!(r->base > 1.0) || !std::isfinite(r->base) || !(r->magnitude > 0.0) || !(r->magnitude <= 3e38))
         return fail(ctx, VKV_E_ARG, "base=%g must be above 1 and magnitude=%g above 0, both finite", r->base, r->magnitude);
     if (r->scaling != VKV_ROPE_PLAIN && (!(r->factor > 0.0) || !std::isfinite(r->factor)))
         return fail(ctx, VKV_E_ARG, "factor=%g must be above 0 and finite", r->factor);
     if (r->scaling == VKV_ROPE_BASE && r->dims < 4) return fail(ctx, VKV_E_SHAPE, "VKV_ROPE_BASE needs at least 4 dims");
-    if (r->scaling == VKV_ROPE_PARTS &&
+    if ((r->scaling == VKV_ROPE_PARTS || by_index) &&
         (!(r->original >= 1.0) || !std::isfinite(r->original) || !(r->slow >= 0.0) || !(r->fast > r->slow) || !std::isfinite(r->fast)))
         return fail(ctx, VKV_E_ARG, "original=%g, fast=%g, slow=%g: need original >= 1 and fast > slow >= 0, finite", r->original,
                     r->fast, r->slow);
+    if (by_index) {
+        if (!(r->slow > 0.0)) return fail(ctx, VKV_E_ARG, "slow=%g must be above 0 with VKV_ROPE_BY_INDEX", r->slow);
+        double lo, hi;
+        rope_ramp(r, &lo, &hi);
+        if (!(lo <= hi)) return fail(ctx, VKV_E_ARG, "the pairs that make fast=%g to slow=%g turns: none of %d", r->fast, r->slow, r->dims / 2);
+    }
     return VKV_OK;
 }
 
 static bool rope_frequencies(const vkv_rope* r, double* f) {
     const double base = r->scaling == VKV_ROPE_BASE ? r->base * std::pow(r->factor, r->dims / (r->dims - 2.0)) : r->base;
+    double lo = 0.0, hi = 0.0;
+    if (r->scaling == ROPE_PARTS_BY_INDEX) rope_ramp(r, &lo, &hi);
     for (int i = 0; i < r->dims / 2; ++i) {
         double t = std::pow(base, -2.0 * i / r->dims);
         if (r->scaling == VKV_ROPE_LINEAR) t /= r->factor;
         if (r->scaling == VKV_ROPE_PARTS) {
             const double turns = r->original * t / 6.283185307179586477;
             const double g = std::min(std::max((turns - r->slow) / (r->fast - r->slow), 0.0), 1.0);
+            t *= (1.0 - g) / r->factor + g;
+        }
+        if (r->scaling == ROPE_PARTS_BY_INDEX) {
+            const double g = i <= lo ? 1.0 : i >= hi ? 0.0 : 1.0 - (i - lo) / (hi - lo);
             t *= (1.0 - g) / r->factor + g;
         }
         if (!(t <= 1024.0)) return false;   // the angle of a far position would have no digit left
