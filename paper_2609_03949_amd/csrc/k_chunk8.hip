@@ -8,7 +8,8 @@
 // cache's kernel.  A tile is 64 or 32 rows of 640 bytes, three or seven of them in LDS (direct loads).  Every 8-bit value is a
 // bf16 and an fp16 value, so the products take operands that are exact: the conversion of the keys multiplies by their power of
 // two, and the weights carry it for the product with the values, which is fp16's.  (The 8-bit products of these matrix cores take half the
-// time, but lose 1e-5 of the sum of the magnitudes where bf16 products lose 1e-8.)  The queries stay in registers, so do the
+// time, but over 512 dims of normal data are off by 8e-7 of the sum of the magnitudes on average, 6e-6 at worst, where bf16 products are
+// by 6e-10 and 3e-8; the weights would be rounded to 8 bits too.)  The queries stay in registers, so do the
 // outputs, 128 dims a wave; weights go through LDS.  What the vector units convert is as long as the products it is for, and
 // bounds units of many rows as much as these do; units of few rows are bound by HBM.  So there are three ways to work on a unit,
 // by its rows:
@@ -32,7 +33,7 @@ constexpr int C8_OFF_WORD = 0;                                  // per stage and
 constexpr int C8_OFF_NOTE = C8_OFF_WORD + C8_STAGES * C8_TILE * 4;   // how far to shift it, or C8_ABSENT
 constexpr int C8_OFF_TOP = C8_OFF_NOTE + C8_STAGES * C8_TILE * 4;    // [16] per row of the unit: the waves' largest scores
 constexpr int C8_OFF_BAD = C8_OFF_TOP + 16 * 16;                // per wave: whether a score that a mask hides is NaN
-constexpr int C8_OFF_P = 2048;                                  // weights: [16][64] bf16
+constexpr int C8_OFF_P = 2048;                                  // weights: [16][64] fp16
 constexpr int C8_OFF_STAGE = C8_OFF_P + 16 * 2 * C8_TILE;       // 1 KB aligned, as pieces are chosen by XORs of the address
 constexpr int C8_SMEM = C8_OFF_STAGE + C8_STAGES * C8_STAGE;
 static_assert(C8_OFF_BAD + 16 <= C8_OFF_P && C8_OFF_STAGE % 1024 == 0 && C8_OFF_P % 1024 == 0, "");
@@ -554,7 +555,7 @@ __device__ __forceinline__ void finish_rows(const Chunk8Args& a, int64_t at, boo
 // A wave has its SIMD to itself, so what keeps the matrix cores busy while codes are converted (vector instructions,
 // about as long as the products that they feed) has to be in the same instruction stream: the scores of tile k + 1 are
 // taken between the outputs of tile k, four products of either at a time.
-constexpr int B8_P = 128 * 2 * C8_TILE;                         // weights of a tile, [128][64] bf16; two of them
+constexpr int B8_P = 128 * 2 * C8_TILE;                         // weights of a tile, [128][64] fp16; two of them
 constexpr int B8_OFF_SCALE = C8_OFF_TOP;                        // [64] the tile's scales (every wave writes the same ones)
 constexpr int B8_OFF_ALPHA = B8_OFF_SCALE + 4 * C8_TILE;        // two of [128]: by what a row's outputs are to be multiplied
 constexpr int B8_OFF_BAD = B8_OFF_ALPHA + 2 * 512;              // two of [4]: the waves' flags, outputs to multiply, a hidden NaN
@@ -918,7 +919,7 @@ constexpr int M8_OFF_WORD = 0, M8_OFF_NOTE = M8_OFF_WORD + M8_STAGES * M8_TILE *
 constexpr int M8_OFF_SCALE = M8_OFF_NOTE + M8_STAGES * M8_TILE * 4;   // [32] the tile's scales (every wave writes the same ones)
 constexpr int M8_OFF_ALPHA = M8_OFF_SCALE + 4 * M8_TILE;              // two of [64]: by what a row's outputs are to be multiplied
 constexpr int M8_OFF_BAD = M8_OFF_ALPHA + 2 * 256;                    // two of [4]: the waves' flags, outputs to multiply, a hidden NaN
-constexpr int M8_OFF_P = 3 * 1024, M8_P = 64 * 2 * M8_TILE;               // weights of a tile, [64][32] bf16; two of them
+constexpr int M8_OFF_P = 3 * 1024, M8_P = 64 * 2 * M8_TILE;               // weights of a tile, [64][32] fp16; two of them
 constexpr int M8_OFF_STAGE = M8_OFF_P + 2 * M8_P;
 typedef Loader8<8, M8_OFF_WORD, M8_OFF_NOTE, true> Loader32;
 constexpr int M8_SMEM = M8_OFF_STAGE + M8_STAGES * Loader32::STAGE;
@@ -1245,7 +1246,7 @@ __device__ __forceinline__ int run_count8(const Chunk8Args& a, int total) {
 
 // What scan_units finds, for up to 64 units: each wave for itself, a lane a unit.  What is read of the units goes to LDS as well, behind
 // the 64 first tiles, so that nobody waits for it again.
-constexpr int UNIT_WORDS = 6;
+constexpr int UNIT_WORDS = 4;
 template <int TILE>
 __device__ __forceinline__ int scan_few(const Chunk8Args& a, int rows, int* pre) {
     const int lane = threadIdx.x & 63, U = a.B * a.mb;
@@ -1256,9 +1257,8 @@ __device__ __forceinline__ int scan_few(const Chunk8Args& a, int rows, int* pre)
         int* at = pre + 64 + UNIT_WORDS * lane;
         at[0] = x.nrow;
         at[1] = (int)x.tok0;      // (n_tok is below 2^31)
-        at[2] = x.nq;
-        at[3] = x.kv;
-        at[4] = x.old;
+        at[2] = x.kv;
+        at[3] = x.old;
     }
     int upto = n;
 #pragma unroll
@@ -1271,14 +1271,13 @@ __device__ __forceinline__ int scan_few(const Chunk8Args& a, int rows, int* pre)
 }
 __device__ __forceinline__ CkUnit few_unit(const Chunk8Args& a, int u, int rows, const int* pre) {
     const int* at = pre + 64 + UNIT_WORDS * u;
-    CkUnit x;
+    CkUnit x{};   // (nq, which gives nrow, is not asked for again)
     x.b = u / a.mb;
     x.row0 = (u - x.b * a.mb) * rows;
     x.nrow = __builtin_amdgcn_readfirstlane(at[0]);
     x.tok0 = __builtin_amdgcn_readfirstlane(at[1]);
-    x.nq = __builtin_amdgcn_readfirstlane(at[2]);
-    x.kv = __builtin_amdgcn_readfirstlane(at[3]);
-    x.old = __builtin_amdgcn_readfirstlane(at[4]);
+    x.kv = __builtin_amdgcn_readfirstlane(at[2]);
+    x.old = __builtin_amdgcn_readfirstlane(at[3]);
     return x;
 }
 
