@@ -722,8 +722,8 @@ int vkv_rope_apply(vkv_ctx* ctx, const vkv_rope* rope, const uint16_t* x, int64_
 /*
  * A paged latent cache held in 8 bits.  A row has VKV_ROW8 bytes: 512 codes of the latent c_u
  * (8-bit floating point: sign, 4 exponent bits of bias 7, 3 fraction bits, largest value 448, no
- * infinities, 0x7F and 0xFF NaN), then the branch r_u as 64 bf16, as the cache of vkv_pages holds it
- * (with whole contexts in one stretch the index scan of VKV_MODE_ROPE reads it there).
+ * infinities, 0x7F and 0xFF NaN), then the branch r_u as 64 bf16, as the cache of vkv_pages holds
+ * it.  The calls of a vkv_step and of vkv_pages read rows of 576 bf16 alone; rows in 8 bits are read by vkv_chunk8_attend.
  * `block` consecutive rows of a page share a scale: row r of page p stands for
  *   c_u = 2^(s - 127) * code,  s = scale[p*scale_stride + r/block],
  * one for each block of tokens, as all heads read the one latent.  Bytes s outside [VKV_SCALE_MIN,
@@ -834,6 +834,9 @@ int vkv_pages_fork(vkv_ctx* ctx, const vkv_pool* pool, const int32_t* from, void
  * the call is over.  Free pages are given lowest first, sequence by sequence, the copy first, then entry by entry.
  * missing [B] int32: the pages that could not be had; their entries are left as they were (no page, or the shared
  * one), and rows may not be written there.  An absent page that should hold rows below kv_len stays absent and counts as missing.
+ * Rows from width*page on have no entry: they are not asked for and not counted, and vkv_cache8_write drops them; a caller that may
+ * come there compares want with width*page.  W sharers that all ask take W pages and copies, the last one too, whose old page
+ * is free after the call.
  * kv_len is not changed.  want [B] int32 (device).
  */
 int vkv_pages_reserve(vkv_ctx* ctx, const vkv_pool* pool, const int32_t* want, int32_t* missing, void* ws,

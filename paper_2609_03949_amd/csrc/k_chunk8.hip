@@ -16,8 +16,8 @@
 //   16       four waves; scores by rows of the tile, so that each code is converted once for either product
 //   32, 64   four waves of scores, by rows of the unit, beside four of outputs
 //   128      four waves, both in one stream of instructions, the scores of a tile between the outputs of the one before
-// 16 sequences of up to 65536 rows, 16 heads: 128 us, 4.6 TB/s.  16 of 32768 rows, 32 and 64 heads: 86 and 116 us.  32 of 32768
-// rows, 128 heads: 289 us; 3 x 512 new tokens over 16384 rows, 128 heads: 4.43 ms, 1.12 PFLOP/s.
+// 16 sequences of up to 65536 rows, 16 heads: 130 us, 4.6 TB/s.  16 of 32768 rows, 32 and 64 heads: 88 and 119 us.  32 of 32768
+// rows, 128 heads: 293 us; 3 x 512 new tokens over 16384 rows, 128 heads: 4.36 ms, 1.14 PFLOP/s.
 #include <algorithm>
 #include <cmath>
 
