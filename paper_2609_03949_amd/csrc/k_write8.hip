@@ -46,8 +46,9 @@ __global__ __launch_bounds__(W8_THREADS) void write8_kernel(Write8Args a) {
     const int n = c.kv_len[b], kv = n >= (1 << 30) ? c.max_kv : max(n, 0);
     const int64_t before = kv - (e0 - s0);                             // the row of token s0
     const int first = (int)max(before, (int64_t)0), end = (int)min(before + min(e0 - s0, (int64_t)c.max_q), (int64_t)c.max_kv);   // rows that are written
-    const int64_t at0 = (int64_t)(first / R + (GW == 1 ? W8_WAVES * j + w : j)) * R;   // the block's first row (another sequence may have 2^30)
-    if (first >= end || at0 >= end) return;                            // the whole workgroup, or waves that share nothing
+    // the block's first row (another sequence may have 2^30 rows to write, so that this passes 31 bits, not 32)
+    const uint32_t at0 = (uint32_t)(first / R + (GW == 1 ? W8_WAVES * j + w : j)) * R;
+    if (first >= end || at0 >= (uint32_t)end) return;                  // the whole workgroup, or waves that share nothing
     const int u0 = (int)at0;
     const int32_t p = c.table[(int64_t)b * c.tstride + (u0 >> c.shift)];
     if ((uint32_t)p >= (uint32_t)c.n_pages) return;
