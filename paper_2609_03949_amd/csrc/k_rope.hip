@@ -4,7 +4,7 @@
 // tokens), finds cosine and sine of their dims / 2 angles once, into LDS, while the first rows are on their way.  The angle
 // is reduced to one turn in fp64 (far positions times the first frequencies have many turns), its sine and
 // cosine are fp32.  Bound: HBM (each element read and written once): 16387 tokens of 16 heads, 64 of 192 dims turned, 50 us, 4.0
-// TB/s, where a large copy reaches 4.9; with the input in the last-level cache 40 us, the vector units busy 94% of the cycles.
+// TB/s, where a large copy reaches 4.9; with the input in the last-level cache 40 us, the vector units busy 92% of the cycles.
 // 32 tokens of 128 heads 4.6 us.
 #include <algorithm>
 
